@@ -44,7 +44,8 @@
  *    enqueued work has completed.  The library keeps no caller pointer after
  *    a call returns.  Tape handles are owned by the library until
  *    ndvm_tape_free().
- *  - Numerics are fp64.  Non-finite lane results are values, not errors; a
+ *  - Numerics are fp64 (but for the encoder operators at the end of this
+ *    file).  Non-finite lane results are values, not errors; a
  *    lane never influences another lane.
  *  - A tape handle may be used from several streams at once; a workspace must
  *    not be shared by calls that can run concurrently.
@@ -390,6 +391,155 @@ const char *ndvm_last_error(void);
 ndvm_status ndvm_adam_step(double *params, const double *grad, double *m, double *v, int64_t L, int64_t P,
                            int64_t ld_p, int64_t ld_g, int64_t t, double lr, double beta1, double beta2,
                            double eps, void *stream);
+
+/*
+ * Operators of a sequence encoder: a network that reads observation series and
+ * answers with the parameters of a program (theta for ndvm_grad), trained
+ * through the loss's exact gradient.  Layer norm, linear attention with a decay
+ * for each head, and the gated feed-forward projections, each with its gradient.
+ *
+ * They take float, bfloat16 or half tensors (`dtype`; one type for all tensors
+ * of a call unless stated), compute in float and round each result once.
+ * Tensors are given as address and strides in elements; the innermost axis is
+ * contiguous; no alignment beyond the element's is needed.  As for the other
+ * compute calls, arguments are checked before anything is enqueued, and a call
+ * only enqueues on `stream`: it allocates nothing and waits for nothing.
+ * Outputs may not overlap inputs.  `workspace`: device memory of the size that
+ * the operator's *_workspace_bytes call names (NULL where that is 0); nothing in
+ * it needs a value, and its contents mean nothing afterwards.
+ * Errors of all of them (synchronous): NDVM_E_ARG for a null pointer to something
+ * that has elements, a negative size, an unknown type, or a row stride smaller
+ * than the row; NDVM_E_UNSUPPORTED for a size past the named limits;
+ * NDVM_E_NOMEM for a workspace too small; NDVM_E_DEVICE for a failed launch.
+ */
+typedef enum { NDVM_F32 = 0, NDVM_BF16 = 1, NDVM_F16 = 2 } ndvm_dtype;
+
+/*
+ * Layer norm of `rows` rows of n values:
+ *   y = (x - mean) * rstd * weight + bias,  rstd = 1 / sqrt(mean((x - mean)^2) + eps)
+ * with the mean over the row.  Row r of x at x + r*ld_x, of y at y + r*ld_y;
+ * weight, bias [n] of the same type, either may be NULL (1 and 0); mean, rstd:
+ * float [rows], what the gradient takes, either may be NULL.  Results are the
+ * same bits whatever the number of rows.
+ */
+ndvm_status ndvm_layer_norm(int dtype, const void *x, int64_t rows, int64_t n, int64_t ld_x, const void *weight,
+                            const void *bias, double eps, void *y, int64_t ld_y, float *mean, float *rstd,
+                            void *stream);
+
+/* Workspace bytes of ndvm_layer_norm_grad.  Host only. */
+ndvm_status ndvm_layer_norm_workspace_bytes(int64_t rows, int64_t n, size_t *bytes);
+
+/*
+ * Gradient of ndvm_layer_norm from dy and the forward pass's x, weight, mean and
+ * rstd.  dx, dweight, dbias: any may be NULL (not wanted); dweight and dbias [n]
+ * are sums over all rows in float, added in a fixed order (the same bits in
+ * every run) and rounded once; with rows = 0 they are 0.
+ */
+ndvm_status ndvm_layer_norm_grad(int dtype, const void *dy, int64_t ld_dy, const void *x, int64_t ld_x, int64_t rows,
+                                 int64_t n, const void *weight, const float *mean, const float *rstd, void *dx,
+                                 int64_t ld_dx, void *dweight, void *dbias, void *workspace, size_t workspace_bytes,
+                                 void *stream);
+
+/*
+ * Linear attention with a decay for each head.  Over the tokens t of a sequence,
+ * for query head h that reads key and value head c = h / (heads / kv_heads):
+ *   S_t = exp(log_decay[h]) S_{t-1} + k_t^T v_t      (S: [dk, dv], float)
+ *   o_t = scale * q_t S_t
+ * S before the first token is `initial_state` (float [n_seq, heads, dk, dv],
+ * contiguous) or 0 where that is NULL; S after the last one goes to
+ * `final_state` (the same layout) unless that is NULL.  log_decay: device float
+ * [heads], constants of the model (they get no gradient).  Evaluated in chunks,
+ * not token by token, with every sum and state in float; a value that is not
+ * finite leaves the outputs of earlier tokens and of other sequences as they are.
+ *
+ * Sequences: offsets = NULL, all of n_tokens / n_seq tokens, token t of sequence
+ * s at data + s*seq_stride + t*tok_stride + head*head_stride; or `offsets`,
+ * device int64 [n_seq + 1] that do not decrease, from 0 to n_tokens: token t of
+ * sequence s at data + (offsets[s] + t)*tok_stride + head*head_stride.
+ * Sequences without tokens are allowed (their final state is the initial one).
+ * Offsets outside 0..n_tokens are read as the nearer end; where they decrease,
+ * results are unspecified, with no access outside the tensors.
+ * Limits: dk, dv <= 256, heads <= 65,535.
+ */
+typedef struct {
+    int dtype;
+    int64_t n_seq, n_tokens;      /* sequences, and tokens of all of them */
+    int64_t heads, kv_heads;      /* heads: a multiple of kv_heads */
+    int64_t dk, dv;
+    double scale;
+} ndvm_attention_shape;
+typedef struct {
+    void *data;
+    int64_t seq_stride, tok_stride, head_stride;
+} ndvm_heads;
+
+/* Workspace bytes of ndvm_linear_attention (with_grad = 0) or its gradient
+ * (with_grad = 1); packed: whether the call has offsets.  Host only. */
+ndvm_status ndvm_linear_attention_workspace_bytes(const ndvm_attention_shape *shape, int packed, int with_grad,
+                                                  size_t *bytes);
+
+/* q, o: heads heads; k, v: kv_heads heads. */
+ndvm_status ndvm_linear_attention(const ndvm_attention_shape *shape, const ndvm_heads *q, const ndvm_heads *k,
+                                  const ndvm_heads *v, const float *log_decay, const int64_t *offsets,
+                                  const float *initial_state, const ndvm_heads *o, float *final_state,
+                                  void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Gradient of ndvm_linear_attention: from d_o (of o) and d_final (float, of the
+ * final state; NULL: 0) those of q, k, v and, unless d_initial is NULL, of the
+ * initial state.  dk and dv add up the query heads that share a key in a fixed
+ * order.  A tensor of dq, dk, dv whose data is NULL is not wanted (d_initial
+ * comes with dv).
+ */
+ndvm_status ndvm_linear_attention_grad(const ndvm_attention_shape *shape, const ndvm_heads *q, const ndvm_heads *k,
+                                       const ndvm_heads *v, const float *log_decay, const int64_t *offsets,
+                                       const float *initial_state, const ndvm_heads *d_o, const float *d_final,
+                                       const ndvm_heads *dq, const ndvm_heads *dk, const ndvm_heads *dv,
+                                       float *d_initial, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The recurrence for one new token of n_seq streams (shape->n_tokens is not
+ * read): stream s updates state slots[s] of `state` (float [n_slots, heads, dk,
+ * dv], contiguous) in place and o = scale * q S with the new S.  slots: device
+ * int64 [n_seq], no slot twice, or NULL (stream s has slot s); a stream whose
+ * slot is not in 0..n_slots-1 has none: its output is 0.  Tensors have a row
+ * for each stream (seq_stride, head_stride; tok_stride is not read).
+ */
+ndvm_status ndvm_linear_attention_step(const ndvm_attention_shape *shape, const ndvm_heads *q, const ndvm_heads *k,
+                                       const ndvm_heads *v, const float *log_decay, float *state, int64_t n_slots,
+                                       const int64_t *slots, const ndvm_heads *o, void *stream);
+
+/*
+ * Gated feed-forward projections of `rows` rows:
+ *   h = act(x w_gate^T) * (x w_up^T)
+ * x [rows, n_in], w_gate and w_up [n_out, n_in], h [rows, n_out], rows at
+ * multiples of their ld.  Limits: n_in, n_out <= 2^21, rows <= 2^22.
+ */
+#define NDVM_ACT_SILU 0       /* g / (1 + exp(-g)) */
+#define NDVM_ACT_GELU 1       /* g (1 + erf(g / sqrt 2)) / 2 */
+#define NDVM_ACT_SIGMOID 2    /* 1 / (1 + exp(-g)) */
+#define NDVM_ACT_RELU 3       /* max(g, 0); derivative 0 at 0 */
+
+/* Workspace bytes of ndvm_gated_ffn (with_grad = 0) or its gradient.  Host only. */
+ndvm_status ndvm_gated_ffn_workspace_bytes(int dtype, int64_t rows, int64_t n_in, int64_t n_out, int with_grad,
+                                           size_t *bytes);
+
+ndvm_status ndvm_gated_ffn(int dtype, int act, const void *x, int64_t rows, int64_t n_in, int64_t ld_x,
+                           const void *w_gate, int64_t ld_gate, const void *w_up, int64_t ld_up, int64_t n_out,
+                           void *h, int64_t ld_h, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Gradient of ndvm_gated_ffn from dh and the forward pass's inputs (x w^T is
+ * formed again).  dx [rows, n_in] may be NULL (not wanted), as may dw_gate and
+ * dw_up [n_out, n_in] together; with rows = 0 the weights' gradients are 0.
+ * The gradients with respect to x w^T are operands of further products and are
+ * rounded to the tensors' type for them (a float keeps its 24 bits).
+ */
+ndvm_status ndvm_gated_ffn_grad(int dtype, int act, const void *dh, int64_t ld_dh, const void *x, int64_t rows,
+                                int64_t n_in, int64_t ld_x, const void *w_gate, int64_t ld_gate, const void *w_up,
+                                int64_t ld_up, int64_t n_out, void *dx, int64_t ld_dx, void *dw_gate,
+                                int64_t ld_dgate, void *dw_up, int64_t ld_dup, void *workspace,
+                                size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

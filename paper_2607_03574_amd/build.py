@@ -22,7 +22,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 SOURCES = ["frontend.cpp", "tape.cpp", "sched.cpp", "wide_sched.cpp", "abi.cpp", "kernels.hip", "wide.hip", "optim.hip",
-           "walk_host.cpp", "walk.hip"]
+           "walk_host.cpp", "walk.hip", "ops_abi.cpp", "norm.hip", "attend.hip", "ffn.hip"]
 EMU_SOURCES = ["frontend.cpp", "tape.cpp", "sched.cpp", "wide_sched.cpp", "emu.cpp"]
 COMMON = ["-O3", "-fPIC", "-std=c++17", "-ffp-contract=off", "-fno-fast-math", "-Wall",
           "-Wno-unused-function"]
@@ -49,10 +49,15 @@ WALK = ["-Xclang", "-disable-lifetime-markers"]
 # branches; the registers its inline asm names are not the compiler's.
 WIDE = ["-mllvm", "-structurizecfg-skip-uniform-regions=true", "-Wno-inline-asm"]
 
+# The encoder operators' kernels compute in float against a tolerance, not bit for
+# bit against the oracle: multiply-adds may be fused.
+OPS = ["-ffp-contract=fast"]
+OPS_OPTIONS_FOR = {"norm.hip", "attend.hip", "ffn.hip"}
 
 
 def _options(src: str) -> list:
-    extra = REPLAY if src in REPLAY_OPTIONS_FOR else WIDE if src == "wide.hip" else []
+    extra = (REPLAY if src in REPLAY_OPTIONS_FOR else WIDE if src == "wide.hip" else
+             OPS if src in OPS_OPTIONS_FOR else [])
     return COMMON + DEVICE + extra + (WALK if src == "walk.hip" else [])
 
 

@@ -2,7 +2,9 @@
 forward is one ndvm_grad replay (loss and exact gradient of every lane in one
 launch) and a calibration loop in which Adam (ndvm_adam_step) drives
 ndvm_grad with the tape uploaded once, as in the paper's Kalman
-maximum-likelihood fit (Section "From buckets to phases").  All arithmetic of
+maximum-likelihood fit (Section "From buckets to phases"); and autograd
+functions of the encoder operators, for networks whose output is the replay's
+parameters.  All arithmetic of
 the replay and of the optimiser runs in the library's kernels; torch supplies
 device memory and streams (and, for autograd, the chain rule of the caller's
 own graph)."""
@@ -10,7 +12,10 @@ from __future__ import annotations
 
 import torch
 
-from . import Tape, _launch_stream, adam_step, grad
+from . import Tape, _launch_stream, adam_step, gated_ffn_grad, grad, layer_norm_grad, linear_attention_grad
+from . import gated_ffn as gated_ffn_op
+from . import layer_norm as layer_norm_op
+from . import linear_attention as linear_attention_op
 
 
 class ReplayLoss(torch.autograd.Function):
@@ -52,3 +57,75 @@ def calibrate(tape: Tape, params, obs, steps: int, lr: float, beta1: float = 0.9
             grad(tape, params, obs, loss=hist[t - 1], grad_out=g, workspace=workspace, stream=s)
             adam_step(params, g, m, v, t, lr, beta1, beta2, eps, stream=s)
     return hist
+
+
+# ---------------------------------------------------------------- encoder operators
+class LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        y, mean, rstd = layer_norm_op(x.detach(), weight, bias, eps)
+        ctx.save_for_backward(x, weight, mean, rstd)
+        ctx.has_bias = bias is not None
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, weight, mean, rstd = ctx.saved_tensors
+        need_weight = ctx.needs_input_grad[1] or ctx.needs_input_grad[2]
+        dx, dw, db = layer_norm_grad(dy.contiguous(), x, weight, mean, rstd, ctx.needs_input_grad[0], need_weight)
+        return dx, dw if ctx.needs_input_grad[1] else None, db if ctx.needs_input_grad[2] else None, None
+
+
+def layer_norm(x, weight=None, bias=None, eps: float = 1e-5):
+    """Layer norm over the last axis with autograd support (layer_norm of the package)."""
+    return LayerNorm.apply(x, weight, bias, eps)
+
+
+class LinearAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, log_decay, offsets, scale, initial_state):
+        o, last = linear_attention_op(q.detach(), k.detach(), v.detach(), log_decay, offsets, scale,
+                                      None if initial_state is None else initial_state.detach(), final_state=True)
+        ctx.save_for_backward(q, k, v, log_decay, offsets, initial_state)
+        ctx.scale = scale
+        ctx.set_materialize_grads(False)
+        return o, last
+
+    @staticmethod
+    def backward(ctx, do, dlast):
+        q, k, v, log_decay, offsets, s0 = ctx.saved_tensors
+        if do is None:
+            do = torch.zeros((*q.shape[:-1], v.shape[-1]), dtype=q.dtype, device=q.device)
+        need = list(ctx.needs_input_grad[:3])
+        need[2] = need[2] or ctx.needs_input_grad[6]        # the state's gradient comes with v's
+        dq, dk, dv, ds0 = linear_attention_grad(do.contiguous(), q, k, v, log_decay, offsets, ctx.scale, s0,
+                                                None if dlast is None else dlast.contiguous(), tuple(need))
+        return (dq, dk, dv if ctx.needs_input_grad[2] else None, None, None, None,
+                ds0 if ctx.needs_input_grad[6] else None)
+
+
+def linear_attention(q, k, v, log_decay, offsets=None, scale=None, initial_state=None):
+    """(o, final state) with autograd support for q, k, v and the initial state
+    (linear_attention of the package; the decay is a constant)."""
+    return LinearAttention.apply(q, k, v, log_decay, offsets, scale, initial_state)
+
+
+class GatedFFN(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, activation):
+        ctx.save_for_backward(x, w_gate, w_up)
+        ctx.activation = activation
+        return gated_ffn_op(x.detach(), w_gate.detach(), w_up.detach(), activation)
+
+    @staticmethod
+    def backward(ctx, dh):
+        x, w_gate, w_up = ctx.saved_tensors
+        need_weight = ctx.needs_input_grad[1] or ctx.needs_input_grad[2]
+        dx, dg, du = gated_ffn_grad(dh.contiguous(), x, w_gate, w_up, ctx.activation, ctx.needs_input_grad[0],
+                                    need_weight)
+        return dx, dg if ctx.needs_input_grad[1] else None, du if ctx.needs_input_grad[2] else None, None
+
+
+def gated_ffn(x, w_gate, w_up, activation: str = "silu"):
+    """act(x w_gate^T) * (x w_up^T) with autograd support (gated_ffn of the package)."""
+    return GatedFFN.apply(x, w_gate, w_up, activation)

@@ -1,0 +1,559 @@
+"""The encoder operators (layer norm, linear attention with decay, its single-token
+step, gated feed-forward; each with its gradient) against plain references in 64
+bits, elementwise within derived bounds, at the sizes, layouts and values where
+they can go wrong; gradients against differences; refusals of bad arguments.
+"""
+import numpy as np
+import pytest
+
+import encoder_ref as ref
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+TYPE = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+KINDS = ["f32", "bf16", "f16"]
+
+
+@pytest.fixture(scope="module")
+def nd():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2607_03574_amd as m
+    return m
+
+
+def make(seed):
+    rng = np.random.default_rng(seed)
+
+    def normal(*shape, kind="f32", scale=1.0, shift=0.0):
+        """A tensor of that type on the GPU, and its values."""
+        t = torch.tensor(rng.normal(size=shape) * scale + shift).to(TYPE[kind]).cuda()
+        return t, values(t)
+
+    return normal
+
+
+def values(t):
+    return t.detach().double().cpu().numpy()
+
+
+def check(got, want, bound, what=""):
+    got = values(got)
+    assert got.shape == want.shape
+    err = np.abs(got - want)
+    worst = np.max(np.where(err <= bound, 0.0, err / np.maximum(bound, 1e-300))) if err.size else 0.0
+    assert np.all(err <= bound), (what, "error over bound", worst, float(np.nanmax(err)))
+
+
+# ---------------------------------------------------------------- layer norm
+NORM_SIZES = [(1, 1), (3, 17), (5, 130), (300, 257), (33, 1000), (7, 2048), (600, 64), (9, 4100), (4, 8192), (3, 20001)]
+
+
+def norm_bounds(x, w, b, y, rstd, n, kind, shift):
+    # the mean's error is the sum's; (x - mean) rstd is off by that over the row's spread
+    e = (n + 16) * ref.F32
+    xh = np.abs((x - x.mean(1, keepdims=True)) * rstd[:, None])
+    mags = np.abs(x).mean(1, keepdims=True) * rstd[:, None]
+    ey = e * (mags + xh + 1) * (1 + xh) * (1.0 if w is None else np.abs(w)) + 4 * ref.F32 * (0 if b is None else np.abs(b))
+    return ref.UNIT[kind] * (np.abs(y) + ey) + ey + ref.TINY[kind]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,n", NORM_SIZES)
+def test_layer_norm(nd, kind, rows, n):
+    normal = make(rows * 31 + n)
+    x, xv = normal(rows, n, kind=kind, scale=1.5, shift=0.5)
+    w, wv = normal(n, kind=kind, scale=0.3, shift=1.0)
+    b, bv = normal(n, kind=kind, scale=0.3)
+    eps = 1e-3
+    for we, be in ((w, b), (None, b), (w, None), (None, None)):
+        y, mean, rstd = nd.layer_norm(x, we, be, eps)
+        wy, wm, wr = ref.norm(xv, None if we is None else wv, None if be is None else bv, eps)
+        e = (n + 16) * ref.F32
+        check(mean, wm, e * np.abs(xv).mean(1) + 1e-37)
+        spread = np.abs(xv).mean(1) * wr
+        check(rstd, wr, e * (2 + spread) ** 2 * wr)
+        check(y, wy, norm_bounds(xv, None if we is None else wv, None if be is None else bv, wy, wr, n, kind, 0), (we is None, be is None))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,n", NORM_SIZES)
+def test_layer_norm_grad(nd, kind, rows, n):
+    normal = make(rows * 37 + n)
+    x, xv = normal(rows, n, kind=kind, scale=1.5, shift=0.5)
+    w, wv = normal(n, kind=kind, scale=0.3, shift=1.0)
+    dy, dyv = normal(rows, n, kind=kind)
+    _, m, r = ref.norm(xv, wv, None, 1e-3)
+    mean, rstd = torch.tensor(m).float().cuda(), torch.tensor(r).float().cuda()
+    m, r = values(mean), values(rstd)
+    for weight in (w, None):
+        wt = wv if weight is not None else np.ones(n)
+        dx, dw, db = nd.layer_norm_grad(dy, x, weight, mean, rstd)
+        wx, ww, wb = ref.norm_grad(dyv, xv, wt, m, r)
+        xh = np.abs(xv - m[:, None]) * r[:, None] + np.abs(m[:, None]) * r[:, None] * ref.F32 * 4
+        g = np.abs(dyv * wt)
+        e = (n + 16) * ref.F32
+        ex = e * r[:, None] * (g + g.mean(1, keepdims=True) + xh * (g * xh).mean(1, keepdims=True))
+        check(dx, wx, ref.UNIT[kind] * (np.abs(wx) + ex) + ex + ref.TINY[kind], "dx")
+        er = (rows + 16) * ref.F32
+        ew, eb = er * (np.abs(dyv) * (xh + 1e-6)).sum(0), er * np.abs(dyv).sum(0)
+        check(dw, ww, ref.UNIT[kind] * (np.abs(ww) + ew) + ew + ref.TINY[kind], "dw")
+        check(db, wb, ref.UNIT[kind] * (np.abs(wb) + eb) + eb + ref.TINY[kind], "db")
+        # what is not wanted is not needed for the rest; the same bits in every run
+        only = nd.layer_norm_grad(dy, x, weight, mean, rstd, need_weight=False)
+        assert only[1] is None and torch.equal(only[0], dx)
+        again = nd.layer_norm_grad(dy, x, weight, mean, rstd, need_input=False)
+        assert again[0] is None and torch.equal(again[1], dw) and torch.equal(again[2], db)
+
+
+def test_layer_norm_rows_with_strides_and_many_rows(nd):
+    normal = make(5)
+    big, bv = normal(2100, 77, kind="bf16", shift=3.0)
+    x, xv = big[:, 3:70], bv[:, 3:70]           # rows start at odd places
+    out = torch.full((2100, 80), -7.25, dtype=torch.bfloat16, device="cuda")
+    y, mean, rstd = nd.layer_norm(x, eps=1e-3, out=out[:, 5:72])
+    wy, wm, wr = ref.norm(xv, None, None, 1e-3)
+    check(y, wy, norm_bounds(xv, None, None, wy, wr, 67, "bf16", 3))
+    assert torch.all(out[:, :5] == -7.25) and torch.all(out[:, 72:] == -7.25)
+    dx, dw, db = nd.layer_norm_grad(y, x, None, mean, rstd)
+    wx, ww, wb = ref.norm_grad(values(y), xv, np.ones(67), values(mean), values(rstd))
+    xh = np.abs((xv - wm[:, None]) * wr[:, None])
+    ew = 2200 * ref.F32 * (np.abs(values(y)) * (xh + 1)).sum(0)
+    check(dw, ww, ref.UNIT["bf16"] * (np.abs(ww) + ew) + ew)
+    # a row with a NaN is NaN, and no other row
+    x2 = x.clone()
+    x2[3, 5] = float("nan")
+    y2 = nd.layer_norm(x2, eps=1e-3)[0]
+    assert torch.isnan(y2[3]).all() and torch.equal(y2[:3], y[:3]) and torch.equal(y2[4:], y[4:])
+
+
+def test_layer_norm_no_rows(nd):
+    x = torch.empty(0, 40, device="cuda")
+    y, mean, rstd = nd.layer_norm(x)
+    assert y.shape == (0, 40) and mean.shape == (0,)
+    dx, dw, db = nd.layer_norm_grad(x, x, None, mean, rstd)
+    assert dx.shape == (0, 40) and torch.all(dw == 0) and torch.all(db == 0)
+
+
+# ---------------------------------------------------------------- linear attention
+# tokens of the sequences, heads, kv heads, dk, dv
+ATTENTION = [([1], 1, 1, 1, 1), ([0, 1, 2], 2, 1, 16, 16), ([15, 16, 17], 2, 2, 33, 20), ([63, 0, 65, 64], 4, 2, 64, 64),
+             ([130, 31, 1, 33], 3, 1, 40, 72), ([97, 200], 2, 2, 128, 128), ([70, 12], 2, 1, 128, 64), ([40, 33], 1, 1, 200, 150),
+             ([5], 1, 1, 256, 256), ([301], 1, 1, 64, 128)]
+
+
+def attention_case(seed, kind, lens, H, Hk, dk, dv, state):
+    normal = make(seed)
+    n = sum(lens)
+    t = dict(q=normal(n, H, dk, kind=kind), k=normal(n, Hk, dk, kind=kind), v=normal(n, Hk, dv, kind=kind),
+             do=normal(n, H, dv, kind=kind), s0=normal(len(lens), H, dk, dv), ds=normal(len(lens), H, dk, dv))
+    g = torch.tensor([-0.3 / 2.0 ** (3 * h) for h in range(H)], dtype=torch.float32)
+    bounds = np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
+    if not state:
+        t["s0"] = t["ds"] = (None, None)
+    return t, g.cuda(), values(g), bounds
+
+
+def gave(a):
+    return None if a is None else np.abs(a)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("state", [False, True])
+@pytest.mark.parametrize("lens,H,Hk,dk,dv", ATTENTION)
+def test_linear_attention(nd, kind, state, lens, H, Hk, dk, dv):
+    t, g, gv, bounds = attention_case(len(lens) + dk, kind, lens, H, Hk, dk, dv, state)
+    q, k, v, s0 = (t[x][0] for x in ("q", "k", "v", "s0"))
+    qv, kv, vv, sv = (t[x][1] for x in ("q", "k", "v", "s0"))
+    off = torch.tensor(bounds).cuda()
+    o, last = nd.linear_attention(q, k, v, g, offsets=off, scale=0.37, initial_state=s0, final_state=True)
+    wo, wl = ref.attention(qv, kv, vv, gv, 0.37, bounds, sv)
+    ao, al = ref.attention(gave(qv), gave(kv), gave(vv), gv, 0.37, bounds, gave(sv))
+    n = max(lens)
+    check(o, wo, ref.attention_bound((wo, ao), kind, n, dk))
+    check(last, wl, ref.attention_bound((wl, al), kind, n, 0, whole=True))
+    if len(set(lens)) == 1:     # the same as sequences of one length
+        shape = lambda x: x.reshape(len(lens), n, *x.shape[1:])
+        o2, last2 = nd.linear_attention(shape(q), shape(k), shape(v), g, scale=0.37, initial_state=s0, final_state=True)
+        check(o2.reshape(o.shape), wo, ref.attention_bound((wo, ao), kind, n, dk))
+        check(last2, wl, ref.attention_bound((wl, al), kind, n, 0, whole=True))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("state", [False, True])
+@pytest.mark.parametrize("lens,H,Hk,dk,dv", ATTENTION)
+def test_linear_attention_grad(nd, kind, state, lens, H, Hk, dk, dv):
+    t, g, gv, bounds = attention_case(len(lens) * 7 + dk, kind, lens, H, Hk, dk, dv, state)
+    q, k, v, do, s0, ds = (t[x][0] for x in ("q", "k", "v", "do", "s0", "ds"))
+    host = [t[x][1] for x in ("do", "q", "k", "v")]
+    sv, dv_ = t["s0"][1], t["ds"][1]
+    off = torch.tensor(bounds).cuda()
+    got = nd.linear_attention_grad(do, q, k, v, g, offsets=off, scale=0.37, initial_state=s0, grad_final_state=ds)
+    want = ref.attention_grad(*host, gv, 0.37, bounds, sv, dv_)
+    mags = ref.attention_grad(*[np.abs(x) for x in host], gv, 0.37, bounds, gave(sv), gave(dv_))
+    n, group = max(lens), H // Hk
+    for i, name in enumerate(("dq", "dk", "dv")):
+        check(got[i], want[i], ref.attention_bound((want[i], mags[i]), kind, n, max(dk, dv) + group), name)
+    if state:
+        check(got[3], want[3], ref.attention_bound((want[3], mags[3]), kind, n, 0, whole=True), "d s0")
+    else:
+        assert got[3] is None
+    again = nd.linear_attention_grad(do, q, k, v, g, offsets=off, scale=0.37, initial_state=s0, grad_final_state=ds)
+    assert all(a is b or torch.equal(a, b) for a, b in zip(got, again))
+    part = nd.linear_attention_grad(do, q, k, v, g, offsets=off, scale=0.37, need=(False, True, False), grad_final_state=ds)
+    assert part[0] is None and part[2] is None and torch.equal(part[1], got[1])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("lens,H,Hk,d", [([2100], 1, 1, 64), ([1500, 3, 700, 0, 900], 2, 1, 32), ([1300, 1300], 1, 1, 128)])
+def test_linear_attention_long(nd, kind, lens, H, Hk, d):
+    """Sequences that are cut into segments, forward and backward, packed and not."""
+    t, g, gv, bounds = attention_case(d, kind, lens, H, Hk, d, d, True)
+    q, k, v, do, s0, ds = (t[x][0] for x in ("q", "k", "v", "do", "s0", "ds"))
+    qv, kv, vv, dov, sv, dsv = (t[x][1] for x in ("q", "k", "v", "do", "s0", "ds"))
+    forms = [dict(offsets=torch.tensor(bounds).cuda())]
+    if len(set(lens)) == 1:
+        forms.append(dict(offsets=None))
+    wo, wl = ref.attention(qv, kv, vv, gv, 0.2, bounds, sv)
+    ao, al = ref.attention(gave(qv), gave(kv), gave(vv), gv, 0.2, bounds, gave(sv))
+    want = ref.attention_grad(dov, qv, kv, vv, gv, 0.2, bounds, sv, dsv)
+    mags = ref.attention_grad(gave(dov), gave(qv), gave(kv), gave(vv), gv, 0.2, bounds, gave(sv), gave(dsv))
+    n = max(lens)
+    for form in forms:
+        view = (lambda x: x) if form["offsets"] is not None else (lambda x: x.reshape(len(lens), n, *x.shape[1:]))
+        o, last = nd.linear_attention(view(q), view(k), view(v), g, scale=0.2, initial_state=s0, final_state=True, **form)
+        check(o.reshape(wo.shape), wo, ref.attention_bound((wo, ao), kind, n, d))
+        check(last, wl, ref.attention_bound((wl, al), kind, n, 0, whole=True))
+        got = nd.linear_attention_grad(view(do), view(q), view(k), view(v), g, scale=0.2, initial_state=s0, grad_final_state=ds, **form)
+        for i, name in enumerate(("dq", "dk", "dv")):
+            check(got[i].reshape(want[i].shape), want[i], ref.attention_bound((want[i], mags[i]), kind, n, d + H // Hk), name)
+        check(got[3], want[3], ref.attention_bound((want[3], mags[3]), kind, n, 0, whole=True), "d s0")
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_linear_attention_strides(nd, kind):
+    """q, k, v as slices of one tensor, heads in front of tokens, an output inside a larger one."""
+    normal = make(3)
+    B, T, H, d = 2, 50, 3, 24
+    x, xv = normal(B, T, 3 * H * d + 5, kind=kind)
+    g = torch.tensor([-0.1, -0.02, 0.0]).cuda()
+    q, k = (x[..., 1 + i * H * d:1 + (i + 1) * H * d].unflatten(-1, (H, d)) for i in (0, 1))
+    vh, vv = normal(B, H, T, d, kind=kind)
+    v = vh.transpose(1, 2)
+    out = torch.full((B, T, H, d + 3), -7.25, dtype=TYPE[kind], device="cuda")
+    o, last = nd.linear_attention(q, k, v, g, scale=0.5, out=out[..., 1:d + 1], final_state=True)
+    flat = lambda t: values(t).reshape(B * T, H, d)
+    args = (flat(q), flat(k), flat(v))
+    bounds = [0, T, 2 * T]
+    wo, wl = ref.attention(*args, values(g), 0.5, bounds)
+    ao, al = ref.attention(*[np.abs(a) for a in args], values(g), 0.5, bounds)
+    check(o.reshape(B * T, H, d), wo, ref.attention_bound((wo, ao), kind, T, d))
+    check(last, wl, ref.attention_bound((wl, al), kind, T, 0, whole=True))
+    assert torch.all(out[..., 0] == -7.25) and torch.all(out[..., d + 1:] == -7.25)
+    do = torch.randn(B, H, T, d, device="cuda").to(TYPE[kind]).transpose(1, 2)
+    got = nd.linear_attention_grad(do, q, k, v, g, scale=0.5)
+    want = nd.linear_attention_grad(do.contiguous(), q.contiguous(), k.contiguous(), v.contiguous(), g, scale=0.5)
+    assert all(torch.equal(a, b) for a, b in zip(got[:3], want[:3]))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("d", [32, 128])
+def test_linear_attention_not_finite(nd, kind, bad, d):
+    """A value that is not finite leaves earlier tokens, other heads and other sequences as they are."""
+    normal = make(9)
+    lens, H = [70, 90, 20], 2
+    n = sum(lens)
+    bounds = torch.tensor([0, 70, 160, 180]).cuda()
+    q, k, v = (normal(n, H, d, kind=kind)[0] for _ in range(3))
+    g = torch.tensor([-0.05, -0.3]).cuda()
+    clean, last = nd.linear_attention(q, k, v, g, offsets=bounds, final_state=True)
+    at = 70 + 41
+    for which in ("q", "k", "v"):
+        t = dict(q=q.clone(), k=k.clone(), v=v.clone())
+        t[which][at, 1, 3] = bad
+        o, s = nd.linear_attention(t["q"], t["k"], t["v"], g, offsets=bounds, final_state=True)
+        same = torch.ones(n, H, d, dtype=torch.bool, device="cuda")
+        if which == "q":
+            same[at, 1] = False
+        elif which == "k":
+            same[at:160, 1] = False
+        else:
+            same[at:160, 1, 3] = False
+        assert torch.isfinite(clean).all()
+        near = torch.isclose(o[same].float(), clean[same].float(), rtol=2.0 ** -7, atol=0.05)
+        assert near.all(), which
+        assert not torch.isfinite(o[~same]).any(), which
+        assert torch.isfinite(s[0]).all() and torch.isfinite(s[2]).all() and torch.isfinite(s[:, 0]).all()
+
+
+def test_linear_attention_decays(nd):
+    """No decay (log 0), all of it (log -inf), growth."""
+    normal = make(13)
+    T, d = 100, 16
+    g = torch.tensor([0.0, float("-inf"), 0.01, -30.0]).cuda()
+    for kind in KINDS:
+        (q, qv), (k, kv), (v, vv) = (normal(T, 4, d, kind=kind) for _ in range(3))
+        o, last = nd.linear_attention(q[None], k[None], v[None], g, scale=1.0, final_state=True)
+        wo, wl = ref.attention(qv, kv, vv, values(g), 1.0, [0, T])
+        ao, al = ref.attention(np.abs(qv), np.abs(kv), np.abs(vv), values(g), 1.0, [0, T])
+        check(o[0], wo, ref.attention_bound((wo, ao), kind, T, d))
+        check(last, wl, ref.attention_bound((wl, al), kind, T, 0, whole=True))
+
+
+def test_linear_attention_empty(nd):
+    g = torch.zeros(2, device="cuda")
+    q = torch.empty(0, 2, 8, device="cuda")
+    s0 = torch.randn(3, 2, 8, 8, device="cuda")
+    off = torch.zeros(4, dtype=torch.int64, device="cuda")
+    o, s = nd.linear_attention(q, q, q, g, offsets=off, initial_state=s0, final_state=True)
+    assert o.shape == (0, 2, 8) and torch.equal(s, s0)
+    got = nd.linear_attention_grad(q, q, q, q, g, offsets=off, initial_state=s0, grad_final_state=2 * s0)
+    assert torch.equal(got[3], 2 * s0)
+    o, s = nd.linear_attention(q[None][:0], q[None][:0], q[None][:0], g, final_state=True)
+    assert o.shape == (0, 0, 2, 8) and s.shape == (0, 2, 8, 8)
+    # offsets that leave the tensor are read as its ends
+    x = torch.randn(6, 2, 8, device="cuda")
+    o, _ = nd.linear_attention(x, x, x, g, offsets=torch.tensor([-5, 3, 99], device="cuda"))
+    want, _ = nd.linear_attention(x, x, x, g, offsets=torch.tensor([0, 3, 6], device="cuda"))
+    assert torch.equal(o, want)
+
+
+# ---------------------------------------------------------------- step
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n,slots,H,Hk,dk,dv", [(1, 1, 1, 1, 1, 1), (3, 7, 4, 2, 33, 20), (40, 64, 16, 16, 128, 128), (2, 2, 2, 1, 256, 250),
+                                                (300, 300, 2, 2, 16, 48)])
+def test_step(nd, kind, n, slots, H, Hk, dk, dv):
+    normal = make(n + dk)
+    (q, qv), (k, kv), (v, vv) = normal(n, H, dk, kind=kind), normal(n, Hk, dk, kind=kind), normal(n, Hk, dv, kind=kind)
+    state, sv = normal(slots, H, dk, dv)
+    g = torch.tensor([-0.1 * (h + 1) for h in range(H)]).cuda()
+    idx = torch.randperm(slots, generator=torch.Generator().manual_seed(1))[:n]
+    where = idx.numpy()
+    o = nd.linear_attention_step(q, k, v, g, state, slots=idx.cuda(), scale=0.7)
+    c = np.arange(H) // (H // Hk)
+    lam = np.exp(values(g))[None, :, None, None]
+    S = lam * sv[where] + kv[:, c][..., None] * vv[:, c][..., None, :]
+    A = lam * np.abs(sv[where]) + np.abs(kv[:, c])[..., None] * np.abs(vv[:, c])[..., None, :]
+    want = sv.copy()
+    want[where] = S
+    bound = np.zeros_like(sv)
+    bound[where] = 8 * ref.F32 * A
+    check(state, want, bound, "state")
+    wo = 0.7 * np.einsum("bhi,bhij->bhj", qv, S)
+    ao = 0.7 * np.einsum("bhi,bhij->bhj", np.abs(qv), A)
+    e = (dk + 16) * ref.F32 * ao
+    check(o, wo, ref.UNIT[kind] * (np.abs(wo) + e) + e + ref.TINY[kind], "o")
+
+
+def test_step_slots_and_agreement_with_the_chunked_form(nd):
+    normal = make(21)
+    B, T, H, d = 3, 40, 2, 32
+    (q, _), (k, _), (v, _) = (normal(B, T, H, d) for _ in range(3))
+    g = torch.tensor([-0.05, 0.0]).cuda()
+    o, last = nd.linear_attention(q, k, v, g, final_state=True)
+    state = torch.zeros(5, H, d, d, device="cuda")
+    slots = torch.tensor([4, 0, 2], device="cuda")
+    steps = torch.stack([nd.linear_attention_step(q[:, t], k[:, t], v[:, t], g, state, slots=slots) for t in range(T)], 1)
+    scale = float(o.abs().max())
+    assert torch.allclose(steps, o, rtol=0, atol=scale * 1e-5)
+    assert torch.allclose(state[slots], last, rtol=0, atol=float(last.abs().max()) * 1e-5)
+    assert torch.all(state[1] == 0) and torch.all(state[3] == 0)
+    # streams without a slot
+    before = state.clone()
+    out = nd.linear_attention_step(q[:, 0], k[:, 0], v[:, 0], g, state, slots=torch.tensor([-1, 5, 1], device="cuda"))
+    assert torch.all(out[:2] == 0) and torch.any(out[2] != 0)
+    assert torch.equal(state[[0, 2, 3, 4]], before[[0, 2, 3, 4]])
+
+
+# ---------------------------------------------------------------- gated feed-forward
+FFN = [(1, 1, 1), (3, 17, 5), (17, 64, 96), (130, 72, 200), (65, 129, 63), (257, 256, 384), (16, 1000, 264)]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("name", ["silu", "gelu", "sigmoid", "relu"])
+@pytest.mark.parametrize("rows,n_in,n_out", FFN)
+def test_gated_ffn(nd, kind, name, rows, n_in, n_out):
+    normal = make(rows + n_in + n_out)
+    x, xv = normal(rows, n_in, kind=kind)
+    wg, wgv = normal(n_out, n_in, kind=kind, scale=n_in ** -0.5)
+    wu, wuv = normal(n_out, n_in, kind=kind, scale=n_in ** -0.5)
+    h = nd.gated_ffn(x, wg, wu, name)
+    check(h, ref.ffn(xv, wgv, wuv, name), ref.ffn_bound(xv, wgv, wuv, name, kind))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("name", ["silu", "gelu", "sigmoid"])
+@pytest.mark.parametrize("rows,n_in,n_out", FFN)
+def test_gated_ffn_grad(nd, kind, name, rows, n_in, n_out):
+    normal = make(rows + n_in * 3 + n_out)
+    x, xv = normal(rows, n_in, kind=kind)
+    wg, wgv = normal(n_out, n_in, kind=kind, scale=n_in ** -0.5)
+    wu, wuv = normal(n_out, n_in, kind=kind, scale=n_in ** -0.5)
+    dh, dhv = normal(rows, n_out, kind=kind)
+    got = nd.gated_ffn_grad(dh, x, wg, wu, name)
+    want = ref.ffn_grad(dhv, xv, wgv, wuv, name)
+    bounds = ref.ffn_grad_bound(dhv, xv, wgv, wuv, name, kind)
+    for a, b, c, what in zip(got, want, bounds, ("dx", "dw_gate", "dw_up")):
+        check(a, b, c, what)
+    assert torch.equal(nd.gated_ffn_grad(dh, x, wg, wu, name, need_weight=False)[0], got[0])
+    only = nd.gated_ffn_grad(dh, x, wg, wu, name, need_input=False)
+    assert only[0] is None and torch.equal(only[1], got[1]) and torch.equal(only[2], got[2])
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_gated_ffn_strides(nd, kind):
+    """Rows that are apart, at odd places: the same values as contiguous ones, and nothing written beside them."""
+    normal = make(2)
+    rows, n_in, n_out = 70, 96, 72
+    big, _ = normal(rows, n_in + 9, kind=kind)
+    w, _ = normal(2 * n_out, n_in + 3, kind=kind, scale=0.1)
+    x, wg, wu = big[:, 5:5 + n_in], w[:n_out, 3:], w[n_out:, 3:]
+    out = torch.full((rows, n_out + 5), -7.25, dtype=TYPE[kind], device="cuda")
+    nd.gated_ffn(x, wg, wu, out=out[:, 2:2 + n_out])
+    want = nd.gated_ffn(x.contiguous(), wg.contiguous(), wu.contiguous())
+    assert torch.equal(out[:, 2:2 + n_out], want)
+    assert torch.all(out[:, :2] == -7.25) and torch.all(out[:, 2 + n_out:] == -7.25)
+    dh, _ = normal(rows, n_out + 1, kind=kind)
+    got = nd.gated_ffn_grad(dh[:, 1:], x, wg, wu)
+    want = nd.gated_ffn_grad(dh[:, 1:].contiguous(), x.contiguous(), wg.contiguous(), wu.contiguous())
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_gated_ffn_no_rows_and_rows_apart(nd):
+    w = torch.randn(24, 16, device="cuda")
+    x = torch.empty(0, 16, device="cuda")
+    assert nd.gated_ffn(x, w, w).shape == (0, 24)
+    dx, dg, du = nd.gated_ffn_grad(torch.empty(0, 24, device="cuda"), x, w, w)
+    assert dx.shape == (0, 16) and torch.all(dg == 0) and torch.all(du == 0)
+    x = torch.randn(5, 16, device="cuda")
+    y = nd.gated_ffn(x, w, w)
+    x[2, 3] = float("nan")
+    y2 = nd.gated_ffn(x, w, w)
+    keep = [0, 1, 3, 4]
+    assert torch.isnan(y2[2]).all() and torch.equal(y2[keep], y[keep])
+
+
+# ---------------------------------------------------------------- gradients against differences
+def slope(f, tensors, directions, weights, eps):
+    """(f(x + eps d) - f(x - eps d)) / 2 eps along `directions`, weighed and summed in 64 bits."""
+    def value(sign):
+        outs = f(*[t + sign * eps * d for t, d in zip(tensors, directions)])
+        return sum(float((o.double() * w.double()).sum()) for o, w in zip(outs, weights))
+    return (value(1.0) - value(-1.0)) / (2 * eps)
+
+
+@pytest.mark.parametrize("op", ["norm", "attention", "ffn"])
+def test_gradients_against_differences(nd, op):
+    from paper_2607_03574_amd import torch_api
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    r = lambda *s: torch.randn(s, generator=gen, device="cuda")
+    if op == "norm":
+        tensors = [r(20, 50), 1 + 0.1 * r(50), r(50)]
+        f = lambda x, w, b: [torch_api.layer_norm(x, w, b, 1e-3)]
+    elif op == "attention":
+        g = torch.tensor([-0.1, -0.01]).cuda()
+        off = torch.tensor([0, 30, 30, 75]).cuda()
+        tensors = [r(75, 2, 12), r(75, 1, 12), r(75, 1, 20), r(3, 2, 12, 20)]
+        f = lambda q, k, v, s: list(torch_api.linear_attention(q, k, v, g, off, 0.3, s))
+    else:
+        tensors = [r(20, 30), 0.2 * r(40, 30), 0.2 * r(40, 30)]
+        f = lambda x, a, b: [torch_api.gated_ffn(x, a, b, "gelu")]
+    tensors = [t.requires_grad_() for t in tensors]
+    outs = f(*tensors)
+    weights = [r(*o.shape) for o in outs]
+    sum((o * w).sum() for o, w in zip(outs, weights)).backward()
+    grads = [t.grad for t in tensors]
+    plain = [t.detach() for t in tensors]
+    for i in range(len(tensors)):
+        # along one input at a time: the other terms of the slope are not there to hide it
+        d = [r(*t.shape) if j == i else torch.zeros_like(t) for j, t in enumerate(plain)]
+        want = float((grads[i].double() * d[i].double()).sum())
+        # truncation is of order eps^2 times the third derivative (sums of the same terms), rounding of order 2^-22 / eps
+        eps = 2.0 ** -9
+        got = slope(f, plain, d, weights, eps)
+        size = float((grads[i].double() * d[i].double()).norm()) * 10 + abs(want)
+        assert abs(got - want) <= 2e-3 * size, (op, i, got, want, size)
+
+
+# ---------------------------------------------------------------- streams, graphs, refusals
+def test_other_streams_and_graphs(nd):
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    r = lambda *s: torch.randn(s, generator=gen, device="cuda").bfloat16()
+    x, w, g = r(64, 128), r(128), torch.full((4,), -0.02, device="cuda")
+    wg, wu, q = r(96, 128) * 0.1, r(96, 128) * 0.1, r(1, 600, 4, 32)
+
+    def everything():
+        y, m, s = nd.layer_norm(x, w)
+        a, last = nd.linear_attention(q, q, q, g, final_state=True)
+        h = nd.gated_ffn(x, wg, wu)
+        return [y, a, last, h, *nd.layer_norm_grad(y, x, w, m, s), *nd.linear_attention_grad(a, q, q, q, g)[:3],
+                *nd.gated_ffn_grad(h, x, wg, wu)]
+
+    want = everything()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = everything()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    y = nd.layer_norm(x, w, stream=side)[0]
+    side.synchronize()
+    assert torch.equal(y, want[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = everything()
+    for _ in range(3):
+        for t in got:
+            t.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_refusals(nd):
+    x = torch.randn(4, 8, device="cuda")
+    w = torch.randn(8, device="cuda")
+    with pytest.raises(TypeError):
+        nd.layer_norm(x.double())
+    with pytest.raises(TypeError):
+        nd.layer_norm(x.cpu())
+    with pytest.raises(TypeError):
+        nd.layer_norm(x, w.bfloat16())
+    with pytest.raises(ValueError):
+        nd.layer_norm(x, w[:4])
+    with pytest.raises(ValueError):
+        nd.layer_norm(x.t())
+    with pytest.raises(ValueError):
+        nd.layer_norm(x, out=torch.empty(4, 9, device="cuda"))
+    with pytest.raises(nd.NdvmError):
+        nd.layer_norm(x, eps=-1.0)
+    q = torch.randn(1, 5, 4, 8, device="cuda")
+    g = torch.zeros(4, device="cuda")
+    with pytest.raises(nd.NdvmError):
+        nd.linear_attention(q, q[:, :, :3], q[:, :, :3], g)            # 4 heads over 3
+    with pytest.raises(ValueError):
+        nd.linear_attention(q, q, q, g[:3])
+    with pytest.raises(ValueError):
+        nd.linear_attention(q, q[:, :4], q, g)
+    with pytest.raises(TypeError):
+        nd.linear_attention(q, q, q, g, offsets=torch.tensor([0, 5], dtype=torch.int32, device="cuda"))
+    with pytest.raises(ValueError):
+        nd.linear_attention(q, q, q, g, offsets=torch.tensor([0, 5], device="cuda"))
+    wide = torch.randn(1, 5, 4, 257, device="cuda")
+    with pytest.raises(nd.NdvmError) as e:
+        nd.linear_attention(wide, wide, q, g)
+    assert e.value.status == nd.E_UNSUPPORTED
+    with pytest.raises(nd.NdvmError):
+        nd.linear_attention(q, q, q, g, scale=float("nan"))
+    state = torch.zeros(1, 4, 8, 8, device="cuda")
+    with pytest.raises(nd.NdvmError):
+        nd.linear_attention_step(q[0], q[0], q[0], g, state)           # 5 streams, 1 slot
+    with pytest.raises(ValueError):
+        nd.gated_ffn(x, x, x[:3])
+    with pytest.raises(ValueError):
+        nd.gated_ffn(x, x, x, "tanh")
+    with pytest.raises(ValueError):
+        nd.gated_ffn_grad(x, x, x, x)
