@@ -13,6 +13,7 @@
 // first launch sums what each segment adds, a second one carries states over
 // the segments in order, and the last one computes the outputs.
 #include <algorithm>
+#include <type_traits>
 
 #include "ops.h"
 #include "ops_types.h"
@@ -203,6 +204,325 @@ __global__ void __launch_bounds__(256) attend_general(AttendArgs A) {
         }
 }
 
+// The kernel for bfloat16 and widths of a and b up to 128: bf16 matrix instructions
+// (16 x 16 x 32), chunks of 32 tokens.  Four waves, 16 NT columns of c each; all
+// share the chunk's rows of a, b and c in LDS, loaded one chunk ahead.
+//  - P^T and S are used from the accumulators as above.  Rows of S are numbered so
+//    that the eight a lane holds in a pair of tiles are eight consecutive widths,
+//    which one 16-byte read of a matches; columns of c so that a lane's results
+//    for a token are consecutive.
+//  - b^T and c^T come from LDS through the transposing reads (four tokens of a
+//    column each), tokens in the order that P^T has them.
+//  - What is float stays float: S enters its product as two bf16 (2^-17), what it
+//    takes, c times its decay, as three (2^-25).  The products of a pair are rounded to
+//    one bf16, as operands; the result has 16 bits too.
+// LDS rows lie in granules of 16 bytes, granule i of row r at i ^ swizzle(r): the 16 rows
+// that one instruction reads are then in different banks.
+typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+#ifdef __HIP_DEVICE_COMPILE__
+__device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+// Lane 4 r + x of 16 names four values of row r; lane i gets column i of the four rows.
+__device__ inline bf16x4 read_transposed(const char *p) {
+    return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(p)));
+}
+// v as the bf16 of its upper half and what is left.
+__device__ inline float upper(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
+#endif
+
+// DS: widths of a and b in 32s.  DIRECT: rows are 16-byte granules at 16-byte
+// addresses, loaded to LDS directly; else through registers.
+template <int DS, int NT, bool DIRECT, bool OUT>
+__global__ void __launch_bounds__(256, 2) attend_bf16(AttendArgs A) {
+#ifdef __HIP_DEVICE_COMPILE__
+    constexpr int N = 32, GA = 4 * DS, GC = 8 * NT;      // tokens of a chunk; granules of a row
+    constexpr int BYTES_A = OUT ? N * GA * 16 : 0, BYTES_B = N * GA * 16, BYTES_C = N * GC * 16;
+    __shared__ __align__(1024) char buffer0[BYTES_A + BYTES_B + BYTES_C], buffer1[BYTES_A + BYTES_B + BYTES_C];
+    __shared__ float power[N + 2];      // lambda^n
+    const Segment g = find_segment(A, blockIdx.x);
+    if (g.count == 0 || (!OUT && g.index == g.count - 1)) return;
+    const int64_t h = blockIdx.y, col0 = int64_t(blockIdx.z) * 64 * NT;
+    const int l = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lm = l % 16, lg = l / 16;
+    const float gl = A.log_decay[h];
+    const int e = A.reversed ? 0 : 1;
+    if (threadIdx.x < N + 2) power[threadIdx.x] = decay(gl, threadIdx.x);
+    __syncthreads();
+
+    const auto swizzle = [](int row, int granules) { return granules >= 16 ? row % 4 * 4 + row / 4 % 4 : row % 2 * 4 + row / 2 % 4; };
+
+    // ---- loads: a wave takes 64 granules at a time
+    constexpr int LA = N * GA / 256, LC = N * GC / 256;
+    constexpr unsigned kNowhere = 0x80000000u;
+    // offset of a lane's i-th granule in a chunk's rows, and the row
+    const auto granule = [&](int i, int granules, int &row) {
+        const int at = (wave + 4 * i) * 64 + l;
+        row = at / granules;
+        return at % granules ^ swizzle(row, granules);
+    };
+    // first byte of the chunk's first token in memory
+    const auto chunk_base = [&](const Heads &H, int64_t base) {
+        const int64_t t = A.reversed ? g.tokens - g.begin - base - N : g.begin + base;
+        const int64_t row = A.offsets ? (g.first + t) * H.tok : g.seq * H.seq + t * H.tok;
+        return static_cast<const bf16 *>(H.p) + row + h / H.group * H.head;
+    };
+    const auto load = [&](const Heads &H, char *to, auto granules_c, auto count_c, int64_t c0, int64_t width, int64_t base) __attribute__((always_inline)) {
+        constexpr int granules = decltype(granules_c)::value, count = decltype(count_c)::value;
+        const bf16 *from = chunk_base(H, base) + c0;
+        if constexpr (DIRECT) {
+            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16 *>(from), 0, 0x7fffffff, 0x00020000);
+#pragma unroll
+            for (int i = 0; i < count; ++i) {
+                int row;
+                const int c = granule(i, granules, row) * 8;
+                const unsigned at = unsigned(A.reversed ? N - 1 - row : row) * unsigned(H.tok * 2) + c * 2;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(to + (wave + 4 * i) * 1024), 16,
+                                                         base + row < g.len && c0 + c < width ? at : kNowhere, 0, 0, 0);
+            }
+        } else {
+            vec<bf16> x[count];
+#pragma unroll
+            for (int i = 0; i < count; ++i) {
+                int row;
+                const int c = granule(i, granules, row) * 8;
+                x[i] = bf16(0.0f);
+                if (base + row < g.len && c0 + c < width)
+                    x[i] = load_vec(from + int64_t(A.reversed ? N - 1 - row : row) * H.tok + c, width - c0 - c);
+            }
+#pragma unroll
+            for (int i = 0; i < count; ++i) *reinterpret_cast<vec<bf16> *>(to + (wave + 4 * i) * 1024 + l * 16) = x[i];
+        }
+    };
+    using std::integral_constant;
+    const auto load_chunk = [&](char *to, int64_t base) __attribute__((always_inline)) {
+        if (OUT) load(A.a, to, integral_constant<int, GA>(), integral_constant<int, LA>(), 0, A.da, base);
+        load(A.b, to + BYTES_A, integral_constant<int, GA>(), integral_constant<int, LA>(), 0, A.da, base);
+        load(A.c, to + BYTES_A + BYTES_B, integral_constant<int, GC>(), integral_constant<int, LC>(), col0, A.dc, base);
+    };
+
+    // ---- the state: tile 2 s + u, register r of lane l: width 32 s + 8 (l / 16) + 4 u + r, and
+    // column (NT = 2) 8 (l % 16 / 4) + 4 nt + l % 4 of the wave's
+    const auto column = [&](int nt) { return col0 + wave * 16 * NT + (NT == 2 ? lm / 4 * 8 + nt * 4 + lm % 4 : lm); };
+    const bool cut = A.n_segments > A.n_seq;
+    f32x4 S[2 * DS][NT];
+    {
+        const float *in = !OUT ? nullptr : cut ? A.segments + (int64_t(blockIdx.x) * A.heads + h) * A.da * A.dc : A.state_in ? A.state_in + (g.seq * A.heads + h) * A.da * A.dc : nullptr;
+        const bool transposed = !cut && A.state_transposed;
+#pragma unroll
+        for (int t = 0; t < 2 * DS; ++t)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int64_t d = t / 2 * 32 + lg * 8 + t % 2 * 4 + r, c = column(nt);
+                    S[t][nt][r] = in && d < A.da && c < A.dc ? in[transposed ? c * A.da + d : d * A.dc + c] : 0.0f;
+                }
+    }
+
+    // ---- decays of a chunk: of a pair (row j of P^T, column i; the same tile, the next one), of what is
+    // read from the state, of what it takes from a full chunk
+    float w0[4], w1[4], rise[2], fall[8];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int far = lm - 4 * lg - r;
+        w0[r] = far >= 0 ? A.scale_pair * power[far] : 0.0f;
+        w1[r] = A.scale_pair * power[far + 16];
+        fall[r] = A.scale_add * power[N - e - 4 * lg - r];
+        fall[4 + r] = A.scale_add * power[N - e - 16 - 4 * lg - r];
+    }
+#pragma unroll
+    for (int it = 0; it < 2; ++it) rise[it] = A.scale_read * power[16 * it + lm + e];
+    float whole = power[N];
+
+    // byte of a lane's reads: 16 bytes of row lm, granule 4 s + lg; and transposed, four values of row
+    // 4 lg + (l / 4 % 4): granule 4 s + l % 4 of b, half u; of c the wave's columns 4 (l % 4) on
+    const int tr_row = 4 * lg + l / 4 % 4;
+    const auto row_at = [&](int row16, int s) { return ((row16 * 16 + lm) * GA + (((4 * s + lg)) ^ swizzle(lm, GA))) * 16; };
+    const auto b_at = [&](int row16, int s, int u) { return ((row16 * 16 + tr_row) * GA + ((4 * s + l % 4) ^ swizzle(tr_row, GA))) * 16 + u * 8; };
+    const auto c_at = [&](int row16, int nt) {
+        const int gr = NT == 2 ? wave * 4 + l % 4 : wave * 2 + l % 4 / 2, half = NT == 2 ? nt : l % 2;
+        return ((row16 * 16 + tr_row) * GC + (gr ^ swizzle(tr_row, GC))) * 16 + half * 8;
+    };
+
+    const auto chunk = [&](char *now, char *next, int64_t base) __attribute__((always_inline)) {
+        const int n = int(min(g.len - base, int64_t(N)));
+        // this wave's loads have landed; after the barrier everybody's have, and nobody reads `next`
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        if (base + N < g.len) load_chunk(next, base + N);
+        const char *la = now, *lb = now + BYTES_A, *lc = now + BYTES_A + BYTES_B;
+        bf16x8 fc[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+            fc[nt] = __builtin_shufflevector(read_transposed(lc + c_at(0, nt)), read_transposed(lc + c_at(1, nt)), 0, 1, 2, 3, 4, 5, 6, 7);
+        if (OUT) {
+            f32x4 P00 = 0, P01 = 0, P11 = 0, O[2][NT];
+            bf16x8 fa[2][DS];
+#pragma unroll
+            for (int s = 0; s < DS; ++s) {
+                fa[0][s] = *reinterpret_cast<const bf16x8 *>(la + row_at(0, s));
+                fa[1][s] = *reinterpret_cast<const bf16x8 *>(la + row_at(1, s));
+                const bf16x8 b0 = *reinterpret_cast<const bf16x8 *>(lb + row_at(0, s)), b1 = *reinterpret_cast<const bf16x8 *>(lb + row_at(1, s));
+                P00 = mfma(b0, fa[0][s], P00);
+                P01 = mfma(b0, fa[1][s], P01);
+                P11 = mfma(b1, fa[1][s], P11);
+            }
+#pragma unroll
+            for (int it = 0; it < 2; ++it)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) O[it][nt] = 0;
+#pragma unroll
+            for (int s = 0; s < DS; ++s)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    bf16x8 hi, lo;
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        const float v = S[2 * s + r / 4][nt][r % 4], up = upper(v);
+                        hi[r] = bf16(up);
+                        lo[r] = bf16(v - up);
+                    }
+#pragma unroll
+                    for (int it = 0; it < 2; ++it) {
+                        O[it][nt] = mfma(lo, fa[it][s], O[it][nt]);
+                        O[it][nt] = mfma(hi, fa[it][s], O[it][nt]);
+                    }
+                }
+            bf16x8 p[2];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                // what is masked is replaced, not multiplied
+                const bool seen = lm >= 4 * lg + r;
+                p[0][r] = bf16(seen ? P00[r] * w0[r] : 0.0f);
+                p[0][4 + r] = bf16(0.0f);
+                p[1][r] = bf16(P01[r] * w1[r]);
+                p[1][4 + r] = bf16(seen ? P11[r] * w0[r] : 0.0f);
+            }
+            f32x4 near[2][NT];
+            float odd = 0;      // NaN if a sum is not finite
+#pragma unroll
+            for (int it = 0; it < 2; ++it)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    near[it][nt] = mfma(fc[nt], p[it], f32x4(0.0f));
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) odd = __builtin_fmaf(near[it][nt][r], 0.0f, odd);
+                }
+            if (__builtin_expect(__any(odd != 0.0f), 0)) {
+                // a value of c may not be finite, and 0 times it is NaN: add the terms up to i alone
+                for (int it = 0; it < 2; ++it) {
+                    typedef int i32x4 __attribute__((ext_vector_type(4)));
+                    const i32x4 packed = __builtin_bit_cast(i32x4, it ? p[1] : p[0]);
+                    f32x4 sum[NT];
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) sum[nt] = 0;
+#pragma unroll 1
+                    for (int j = 0; j < N; ++j) {
+                        const int at = j / 16 * 2 + j % 4 / 2;
+                        const int two = __shfl(at == 0 ? packed[0] : at == 1 ? packed[1] : at == 2 ? packed[2] : packed[3], lm + 16 * (j % 16 / 4));
+                        const float pij = __int_as_float(j % 2 ? two & 0xffff0000 : two << 16);
+                        if (j > 16 * it + lm) continue;
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                const int c = wave * 16 * NT + (NT == 2 ? lg * 8 + nt * 4 + r : lg * 4 + r);
+                                sum[nt][r] += pij * float(*reinterpret_cast<const bf16 *>(lc + (j * GC + (c / 8 ^ swizzle(j, GC))) * 16 + c % 8 * 2));
+                            }
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) (it ? near[1][nt] : near[0][nt]) = sum[nt];
+                }
+            }
+#pragma unroll
+            for (int it = 0; it < 2; ++it)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) O[it][nt] = O[it][nt] * rise[it] + near[it][nt];
+            // lane l: token lm of the tile, columns 4 lg on
+#pragma unroll
+            for (int it = 0; it < 2; ++it) {
+                const int i = 16 * it + lm;
+                const int64_t c = col0 + wave * 16 * NT + lg * 4 * NT;
+                if (i >= n || c >= A.dc) continue;
+                const int64_t pos = g.begin + base + i;
+                constexpr int W = 4 * NT;
+                if (A.out_f32) {
+                    typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+                    float *to = const_cast<float *>(token_ptr<float>(A.out, A, g, pos, h)) + c;
+                    if (c + W <= A.dc) {
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<f4 *>(to + 4 * nt) = O[it][nt];
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < W; ++r)
+                            if (c + r < A.dc) to[r] = O[it][r / 4][r % 4];
+                    }
+                } else {
+                    typedef bf16 out_t __attribute__((ext_vector_type(W), aligned(2)));
+                    bf16 *to = const_cast<bf16 *>(token_ptr<bf16>(A.out, A, g, pos, h)) + c;
+                    out_t v;
+#pragma unroll
+                    for (int r = 0; r < W; ++r) v[r] = bf16(O[it][r / 4][r % 4]);
+                    if (c + W <= A.dc) {
+                        *reinterpret_cast<out_t *>(to) = v;
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < W; ++r)
+                            if (c + r < A.dc) to[r] = v[r];
+                    }
+                }
+            }
+        }
+        if (n < N) {        // the last chunk: decays to its own end; beyond it c is 0
+            whole = power[n];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                const int to_end = n - e - (r / 4 * 16 + 4 * lg + r % 4);
+                fall[r] = to_end >= 0 ? A.scale_add * power[to_end] : 0.0f;
+            }
+        }
+        bf16x8 part[NT][3];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                const float v = float(fc[nt][r]) * fall[r], v1 = upper(v), left = v - v1, v2 = upper(left);
+                part[nt][0][r] = bf16(v1);
+                part[nt][1][r] = bf16(v2);
+                part[nt][2][r] = bf16(left - v2);
+            }
+#pragma unroll
+        for (int t = 0; t < 2 * DS; ++t) {
+            const bf16x8 fb = __builtin_shufflevector(read_transposed(lb + b_at(0, t / 2, t % 2)), read_transposed(lb + b_at(1, t / 2, t % 2)), 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                S[t][nt] *= whole;
+#pragma unroll
+                for (int q = 2; q >= 0; --q) S[t][nt] = mfma(fb, part[nt][q], S[t][nt]);
+            }
+        }
+    };
+    if (g.len > 0) load_chunk(buffer0, 0);
+    for (int64_t base = 0; base < g.len; base += 2 * N) {
+        chunk(buffer0, buffer1, base);
+        if (base + N < g.len) chunk(buffer1, buffer0, base + N);
+    }
+
+    float *out = !OUT ? A.segments + (int64_t(blockIdx.x) * A.heads + h) * A.da * A.dc : g.index == g.count - 1 && A.state_out ? A.state_out + (g.seq * A.heads + h) * A.da * A.dc : nullptr;
+    if (!out) return;
+#pragma unroll
+    for (int t = 0; t < 2 * DS; ++t)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int64_t d = t / 2 * 32 + lg * 8 + t % 2 * 4 + r, c = column(nt);
+                if (d < A.da && c < A.dc) out[OUT && A.state_transposed ? c * A.da + d : d * A.dc + c] = S[t][nt][r];
+            }
+#endif
+}
+
 // States over the segments of a sequence, in order: what each adds is replaced
 // by what enters it.  A thread an element of the state.
 __global__ void __launch_bounds__(256) attend_carry(AttendArgs A) {
@@ -308,9 +628,36 @@ template <class T, int DT, int STAGE> void launch_general(const AttendArgs &a, h
     attend_general<T, DT, STAGE, true><<<grid, 256, 0, stream>>>(a);
 }
 
+template <int DS, int NT, bool DIRECT> void launch_bf16(const AttendArgs &a, hipStream_t stream) {
+    const dim3 grid(uint32_t(a.n_segments), uint32_t(a.heads), uint32_t(ceil_div(a.dc, 64 * NT)));
+    if (a.n_segments > a.n_seq) {
+        attend_bf16<DS, NT, DIRECT, false><<<grid, 256, 0, stream>>>(a);
+        attend_carry<<<dim3(uint32_t(a.n_seq), uint32_t(a.heads), uint32_t(ceil_div(a.da * a.dc, 256))), 256, 0, stream>>>(a);
+    }
+    attend_bf16<DS, NT, DIRECT, true><<<grid, 256, 0, stream>>>(a);
+}
+
+// Whether rows can be loaded to LDS directly: whole granules at 16-byte addresses, and
+// offsets inside a chunk that 31 bits hold.
+bool direct(const AttendArgs &a, const Heads &h, int64_t width) {
+    return reinterpret_cast<uintptr_t>(h.p) % 16 == 0 && h.tok % 8 == 0 && h.head % 8 == 0 && (a.offsets || h.seq % 8 == 0) && width % 8 == 0 && h.tok < (1 << 24);
+}
+
+template <bool DIRECT> void launch_bf16(const AttendArgs &a, hipStream_t stream) {
+    if (a.da <= 64 && a.dc <= 64) launch_bf16<2, 1, DIRECT>(a, stream);
+    else if (a.da <= 64) launch_bf16<2, 2, DIRECT>(a, stream);
+    else if (a.dc <= 64) launch_bf16<4, 1, DIRECT>(a, stream);
+    else launch_bf16<4, 2, DIRECT>(a, stream);
+}
+
 }  // namespace
 
 hipError_t launch_attend(int dtype, const AttendArgs &a, hipStream_t stream) {
+    if (dtype == NDVM_BF16 && a.da <= 128) {
+        if (direct(a, a.a, a.da) && direct(a, a.b, a.da) && direct(a, a.c, a.dc)) launch_bf16<true>(a, stream);
+        else launch_bf16<false>(a, stream);
+        return hipGetLastError();
+    }
     return with_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
         if (a.da <= 64) launch_general<T, 4, 64>(a, stream);
