@@ -10,8 +10,9 @@
 // A workgroup walks the chunks of one segment of a sequence for one head, with S
 // in the accumulator registers of the matrix instructions.  Sequences are cut
 // into segments where sequences and heads alone would not fill the GPU: then a
-// first launch sums what each segment adds, a second one carries states over
-// the segments in order, and the last one computes the outputs.
+// first launch sums what each segment adds (the first one of a sequence: to what
+// the sequence started with), a second one carries states over the segments in
+// order, and the last one computes the outputs.
 #include <algorithm>
 #include <type_traits>
 
@@ -36,36 +37,44 @@ struct Segment {
 
 // Segment `id`: sequences of equal length have equally many segments.  Packed
 // sequences have ids from offsets[s] / seg_len + s on, which leaves room for all of
-// theirs; the spare ids are segments without tokens (count 0).
-__device__ inline Segment find_segment(const AttendArgs &a, int64_t id) {
+// theirs; the spare ids are segments without tokens (count 0).  seg_len is a power of two
+// then, and the 64 lanes of a wave look for the sequence together.
+__device__ inline Segment find_segment(const AttendArgs &a, uint32_t id) {
     Segment g;
     const bool cut = a.n_segments > a.n_seq;
     if (!a.offsets) {
-        g.tokens = a.n_tokens / a.n_seq;
-        const int64_t per = a.n_segments / a.n_seq;
+        const uint32_t per = uint32_t(a.n_segments) / uint32_t(a.n_seq);
+        g.tokens = uint32_t(a.n_tokens) / uint32_t(a.n_seq);
         g.seq = id / per;
         g.index = id % per;
         g.first = g.seq * g.tokens;
+        g.count = per;
     } else {
         const auto at = [&](int64_t s) { return min(max(a.offsets[s], int64_t(0)), a.n_tokens); };
-        const auto base = [&](int64_t s) { return at(s) / a.seg_len + s; };
-        int64_t lo = 0;
-        if (!cut) {
-            lo = id;
-        } else {
-            int64_t hi = a.n_seq;       // the last sequence whose ids begin at or before id
+        const int shift = 63 - __builtin_clzll(a.seg_len);
+        uint32_t lo = id, base = id;
+        if (cut) {
+            // the last sequence whose ids begin at or before id
+            uint32_t hi = uint32_t(a.n_seq);
+            lo = base = 0;
             while (hi - lo > 1) {
-                const int64_t mid = (lo + hi) / 2;
-                if (base(mid) <= id) lo = mid;
-                else hi = mid;
+                const uint32_t step = (hi - lo + 63) / 64, s = lo + (threadIdx.x % 64) * step;
+                const uint32_t mine = s < hi ? uint32_t(at(s) >> shift) + s : 0xffffffffu;
+                const int n = max(__popcll(__ballot(mine <= id)), 1);
+                base = __shfl(mine, n - 1);
+                lo += (n - 1) * step;
+                hi = min(lo + step, hi);
             }
+            if (a.n_seq == 1) base = uint32_t(at(0) >> shift);
+            lo = __builtin_amdgcn_readfirstlane(lo);
+            base = __builtin_amdgcn_readfirstlane(base);
         }
         g.seq = lo;
-        g.index = cut ? id - base(lo) : 0;
+        g.index = int64_t(id) - base;
         g.first = at(lo);
-        g.tokens = max(at(lo + 1) - g.first, int64_t(0));
+        g.tokens = max(at(int64_t(lo) + 1) - g.first, int64_t(0));
+        g.count = cut ? max((g.tokens + a.seg_len - 1) >> shift, int64_t(1)) : 1;
     }
-    g.count = cut ? max((g.tokens + a.seg_len - 1) / a.seg_len, int64_t(1)) : 1;
     g.begin = g.index * a.seg_len;
     g.len = cut ? min(a.seg_len, g.tokens - g.begin) : g.tokens;
     if (g.index < 0 || g.index >= g.count) g.count = 0;
@@ -92,19 +101,22 @@ __global__ void __launch_bounds__(256) attend_general(AttendArgs A) {
     constexpr int D = 16 * DT, LD = D + 4, LC = 64 + 4, V = kVec<T>;
     __shared__ float la[STAGE][LD], lb[STAGE][LD], lc[STAGE][LC];
     __shared__ float power[17];     // lambda^n
-    const Segment g = find_segment(A, blockIdx.x);
+    // heads first: workgroups that run together read whole rows of memory between them
+    const uint32_t id = blockIdx.x / uint32_t(A.heads);
+    const Segment g = find_segment(A, id);
     if (g.count == 0 || (!OUT && g.index == g.count - 1)) return;
-    const int64_t h = blockIdx.y, col0 = int64_t(blockIdx.z) * 64;
+    const int64_t h = blockIdx.x - id * uint32_t(A.heads), col0 = int64_t(blockIdx.y) * 64;
     const int l = threadIdx.x % 64, wave = threadIdx.x / 64, lm = l % 16, lg = l / 16;
     const int64_t col = col0 + wave * 16 + lm;
     const float gl = A.log_decay[h];
     if (threadIdx.x < 17) power[threadIdx.x] = decay(gl, threadIdx.x);
     const int e = A.reversed ? 0 : 1;
-    const bool cut = A.n_segments > A.n_seq;
 
     f32x4 S[DT];
-    const float *in = !OUT ? nullptr : cut ? A.segments + (int64_t(blockIdx.x) * A.heads + h) * A.da * A.dc : A.state_in ? A.state_in + (g.seq * A.heads + h) * A.da * A.dc : nullptr;
-    const bool in_transposed = !cut && A.state_transposed;
+    const bool carried = OUT && g.index > 0;    // from an earlier segment
+    float *mine = A.segments + int64_t(blockIdx.x) * ((A.da * A.dc + 3) / 4 * 4);
+    const float *in = carried ? mine : g.index == 0 && A.state_in ? A.state_in + (g.seq * A.heads + h) * A.da * A.dc : nullptr;
+    const bool in_transposed = !carried && A.state_transposed;
     const auto place = [&](int t, int r, bool transposed) {
         const int64_t d = 16 * t + 4 * lg + r;
         return d < A.da && col < A.dc ? (transposed ? col * A.da + d : d * A.dc + col) : int64_t(-1);
@@ -193,7 +205,7 @@ __global__ void __launch_bounds__(256) attend_general(AttendArgs A) {
             }
         }
     }
-    float *out = !OUT ? A.segments + (int64_t(blockIdx.x) * A.heads + h) * A.da * A.dc : g.index == g.count - 1 && A.state_out ? A.state_out + (g.seq * A.heads + h) * A.da * A.dc : nullptr;
+    float *out = !OUT ? mine : g.index == g.count - 1 && A.state_out ? A.state_out + (g.seq * A.heads + h) * A.da * A.dc : nullptr;
     if (!out) return;
 #pragma unroll
     for (int t = 0; t < DT; ++t)
@@ -239,11 +251,14 @@ __global__ void __launch_bounds__(256, 2) attend_bf16(AttendArgs A) {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int N = 32, GA = 4 * DS, GC = 8 * NT;      // tokens of a chunk; granules of a row
     constexpr int BYTES_A = OUT ? N * GA * 16 : 0, BYTES_B = N * GA * 16, BYTES_C = N * GC * 16;
-    __shared__ __align__(1024) char buffer0[BYTES_A + BYTES_B + BYTES_C], buffer1[BYTES_A + BYTES_B + BYTES_C];
+    constexpr int BYTES = BYTES_A + BYTES_B + BYTES_C;
+    __shared__ __align__(1024) char buffer0[BYTES], buffer1[BYTES], buffer2[BYTES];
     __shared__ float power[N + 2];      // lambda^n
-    const Segment g = find_segment(A, blockIdx.x);
+    // heads first: workgroups that run together read whole rows of memory between them
+    const uint32_t id = blockIdx.x / uint32_t(A.heads);
+    const Segment g = find_segment(A, id);
     if (g.count == 0 || (!OUT && g.index == g.count - 1)) return;
-    const int64_t h = blockIdx.y, col0 = int64_t(blockIdx.z) * 64 * NT;
+    const int64_t h = blockIdx.x - id * uint32_t(A.heads), col0 = int64_t(blockIdx.y) * 64 * NT;
     const int l = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lm = l % 16, lg = l / 16;
     const float gl = A.log_decay[h];
     const int e = A.reversed ? 0 : 1;
@@ -253,71 +268,81 @@ __global__ void __launch_bounds__(256, 2) attend_bf16(AttendArgs A) {
     const auto swizzle = [](int row, int granules) { return granules >= 16 ? row % 4 * 4 + row / 4 % 4 : row % 2 * 4 + row / 2 % 4; };
 
     // ---- loads: a wave takes 64 granules at a time
-    constexpr int LA = N * GA / 256, LC = N * GC / 256;
+    constexpr int LA = N * GA / 256, LC = N * GC / 256, LOADS = (OUT ? 2 : 1) * LA + LC;
     constexpr unsigned kNowhere = 0x80000000u;
-    // offset of a lane's i-th granule in a chunk's rows, and the row
-    const auto granule = [&](int i, int granules, int &row) {
-        const int at = (wave + 4 * i) * 64 + l;
-        row = at / granules;
-        return at % granules ^ swizzle(row, granules);
+    const int len = int(g.len);
+    struct Rows {
+        int64_t at;         // of the first chunk's row that comes first in memory
+        int64_t step;       // from a chunk's to the next chunk's, over the chunk's tokens
     };
-    // first byte of the chunk's first token in memory
-    const auto chunk_base = [&](const Heads &H, int64_t base) {
-        const int64_t t = A.reversed ? g.tokens - g.begin - base - N : g.begin + base;
+    const auto rows_of = [&](const Heads &H) {
+        const int64_t t = A.reversed ? g.tokens - g.begin - N : g.begin;
         const int64_t row = A.offsets ? (g.first + t) * H.tok : g.seq * H.seq + t * H.tok;
-        return static_cast<const bf16 *>(H.p) + row + h / H.group * H.head;
+        return Rows{row + h / H.group * H.head, A.reversed ? -H.tok : H.tok};
     };
-    const auto load = [&](const Heads &H, char *to, auto granules_c, auto count_c, int64_t c0, int64_t width, int64_t base) __attribute__((always_inline)) {
+    const Rows ra = rows_of(A.a), rb = rows_of(A.b), rc = rows_of(A.c), ro = rows_of(A.out);
+    const auto load = [&](const Heads &H, const Rows &R, char *to, auto granules_c, auto count_c, int64_t c0, int64_t width, int base) __attribute__((always_inline)) {
         constexpr int granules = decltype(granules_c)::value, count = decltype(count_c)::value;
-        const bf16 *from = chunk_base(H, base) + c0;
-        if constexpr (DIRECT) {
-            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16 *>(from), 0, 0x7fffffff, 0x00020000);
+        const bf16 *from = static_cast<const bf16 *>(H.p) + R.at + base * R.step + c0;
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16 *>(from), 0, 0x7fffffff, 0x00020000);
+        vec<bf16> x[count];
 #pragma unroll
-            for (int i = 0; i < count; ++i) {
-                int row;
-                const int c = granule(i, granules, row) * 8;
-                const unsigned at = unsigned(A.reversed ? N - 1 - row : row) * unsigned(H.tok * 2) + c * 2;
+        for (int i = 0; i < count; ++i) {
+            const int at = (wave + 4 * i) * 64 + l, row = at / granules, c = (at % granules ^ swizzle(row, granules)) * 8;
+            const int place = A.reversed ? N - 1 - row : row;
+            const bool there = base + row < len && c0 + c < width;
+            if constexpr (DIRECT) {
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(to + (wave + 4 * i) * 1024), 16,
-                                                         base + row < g.len && c0 + c < width ? at : kNowhere, 0, 0, 0);
-            }
-        } else {
-            vec<bf16> x[count];
-#pragma unroll
-            for (int i = 0; i < count; ++i) {
-                int row;
-                const int c = granule(i, granules, row) * 8;
+                                                         there ? unsigned(place) * unsigned(H.tok * 2) + c * 2 : kNowhere, 0, 0, 0);
+            } else {
                 x[i] = bf16(0.0f);
-                if (base + row < g.len && c0 + c < width)
-                    x[i] = load_vec(from + int64_t(A.reversed ? N - 1 - row : row) * H.tok + c, width - c0 - c);
+                if (there) x[i] = load_vec(from + place * H.tok + c, width - c0 - c);
             }
+        }
+        if constexpr (!DIRECT) {
 #pragma unroll
             for (int i = 0; i < count; ++i) *reinterpret_cast<vec<bf16> *>(to + (wave + 4 * i) * 1024 + l * 16) = x[i];
         }
     };
     using std::integral_constant;
-    const auto load_chunk = [&](char *to, int64_t base) __attribute__((always_inline)) {
-        if (OUT) load(A.a, to, integral_constant<int, GA>(), integral_constant<int, LA>(), 0, A.da, base);
-        load(A.b, to + BYTES_A, integral_constant<int, GA>(), integral_constant<int, LA>(), 0, A.da, base);
-        load(A.c, to + BYTES_A + BYTES_B, integral_constant<int, GC>(), integral_constant<int, LC>(), col0, A.dc, base);
+    // always LOADS loads a wave (those past the segment's end fetch nothing)
+    const auto load_chunk = [&](char *to, int base) __attribute__((always_inline)) {
+        if (OUT) load(A.a, ra, to, integral_constant<int, GA>(), integral_constant<int, LA>(), 0, A.da, base);
+        load(A.b, rb, to + BYTES_A, integral_constant<int, GA>(), integral_constant<int, LA>(), 0, A.da, base);
+        load(A.c, rc, to + BYTES_A + BYTES_B, integral_constant<int, GC>(), integral_constant<int, LC>(), col0, A.dc, base);
     };
 
     // ---- the state: tile 2 s + u, register r of lane l: width 32 s + 8 (l / 16) + 4 u + r, and
     // column (NT = 2) 8 (l % 16 / 4) + 4 nt + l % 4 of the wave's
     const auto column = [&](int nt) { return col0 + wave * 16 * NT + (NT == 2 ? lm / 4 * 8 + nt * 4 + lm % 4 : lm); };
-    const bool cut = A.n_segments > A.n_seq;
+    // A segment's state lies in memory as in the registers.
     f32x4 S[2 * DS][NT];
-    {
-        const float *in = !OUT ? nullptr : cut ? A.segments + (int64_t(blockIdx.x) * A.heads + h) * A.da * A.dc : A.state_in ? A.state_in + (g.seq * A.heads + h) * A.da * A.dc : nullptr;
-        const bool transposed = !cut && A.state_transposed;
+    f32x4 *mine = reinterpret_cast<f32x4 *>(A.segments) + ((int64_t(blockIdx.x) * gridDim.y + blockIdx.y) * 4 + wave) * (2 * DS * NT * 64) + l;
+    if (OUT && g.index > 0) {
 #pragma unroll
         for (int t = 0; t < 2 * DS; ++t)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int nt = 0; nt < NT; ++nt) S[t][nt] = mine[(t * NT + nt) * 64];
+    } else {
+        const float *in = g.index == 0 && A.state_in ? A.state_in + (g.seq * A.heads + h) * A.da * A.dc : nullptr;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int64_t d = t / 2 * 32 + lg * 8 + t % 2 * 4 + r, c = column(nt);
-                    S[t][nt][r] = in && d < A.da && c < A.dc ? in[transposed ? c * A.da + d : d * A.dc + c] : 0.0f;
-                }
+        for (int t = 0; t < 2 * DS; ++t)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) S[t][nt] = 0;
+        if (in) {
+            const int64_t step_d = A.state_transposed ? 1 : A.dc, step_c = A.state_transposed ? A.da : 1;
+#pragma unroll
+            for (int t = 0; t < 2 * DS; ++t)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int64_t d = t / 2 * 32 + lg * 8 + t % 2 * 4 + r, c = column(nt);
+                        const bool there = d < A.da && c < A.dc;
+                        const float v = in[there ? d * step_d + c * step_c : 0];
+                        S[t][nt][r] = there ? v : 0.0f;
+                    }
+        }
     }
 
     // ---- decays of a chunk: of a pair (row j of P^T, column i; the same tile, the next one), of what is
@@ -345,19 +370,64 @@ __global__ void __launch_bounds__(256, 2) attend_bf16(AttendArgs A) {
         return ((row16 * 16 + tr_row) * GC + (gr ^ swizzle(tr_row, GC))) * 16 + half * 8;
     };
 
-    const auto chunk = [&](char *now, char *next, int64_t base) __attribute__((always_inline)) {
-        const int n = int(min(g.len - base, int64_t(N)));
-        // this wave's loads have landed; after the barrier everybody's have, and nobody reads `next`
-        __builtin_amdgcn_s_waitcnt(0);
-        __syncthreads();
-        if (base + N < g.len) load_chunk(next, base + N);
+    // A chunk's results are stored during the next one, ahead of its loads: the last LOADS
+    // of a wave's memory operations are then the loads of the chunk after.
+    f32x4 O[2][NT];
+    const auto store = [&](int base) __attribute__((always_inline)) {
+        // lane l: token lm of the tile, columns 4 NT lg on
+        const int c = wave * 16 * NT + lg * 4 * NT;
+        constexpr int W = 4 * NT;
+        const int have = int(min(A.dc - col0 - c, int64_t(W)));
+#pragma unroll
+        for (int it = 0; it < 2; ++it) {
+            const int i = 16 * it + lm;
+            if (base + i >= len || have <= 0) continue;
+            const int64_t at = ro.at + base * ro.step + (A.reversed ? N - 1 - i : i) * A.out.tok + col0 + c;
+            if (A.out_f32) {
+                typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+                float *to = static_cast<float *>(const_cast<void *>(A.out.p)) + at;
+                if (have == W) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<f4 *>(to + 4 * nt) = O[it][nt];
+                } else {
+#pragma unroll
+                    for (int r = 0; r < W; ++r)
+                        if (r < have) to[r] = O[it][r / 4][r % 4];
+                }
+            } else {
+                typedef bf16 out_t __attribute__((ext_vector_type(W), aligned(2)));
+                bf16 *to = static_cast<bf16 *>(const_cast<void *>(A.out.p)) + at;
+                out_t v;
+#pragma unroll
+                for (int r = 0; r < W; ++r) v[r] = bf16(O[it][r / 4][r % 4]);
+                if (have == W) {
+                    *reinterpret_cast<out_t *>(to) = v;
+                } else {
+#pragma unroll
+                    for (int r = 0; r < W; ++r)
+                        if (r < have) to[r] = v[r];
+                }
+            }
+        }
+    };
+
+    const auto chunk = [&](char *now, char *next, int base) __attribute__((always_inline)) {
+        const int n = min(len - base, N);
+        // this wave's loads of the chunk have landed (the next chunk's may not have); after the
+        // barrier everybody's have, and nobody reads `next`
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(DIRECT ? LOADS | 0x0070 : 0x0070);      // of vector memory; all of LDS
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (OUT && base > 0) store(base - N);
+        load_chunk(next, base + 2 * N);
         const char *la = now, *lb = now + BYTES_A, *lc = now + BYTES_A + BYTES_B;
         bf16x8 fc[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
             fc[nt] = __builtin_shufflevector(read_transposed(lc + c_at(0, nt)), read_transposed(lc + c_at(1, nt)), 0, 1, 2, 3, 4, 5, 6, 7);
         if (OUT) {
-            f32x4 P00 = 0, P01 = 0, P11 = 0, O[2][NT];
+            f32x4 P00 = 0, P01 = 0, P11 = 0;
             bf16x8 fa[2][DS];
 #pragma unroll
             for (int s = 0; s < DS; ++s) {
@@ -439,40 +509,6 @@ __global__ void __launch_bounds__(256, 2) attend_bf16(AttendArgs A) {
             for (int it = 0; it < 2; ++it)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) O[it][nt] = O[it][nt] * rise[it] + near[it][nt];
-            // lane l: token lm of the tile, columns 4 lg on
-#pragma unroll
-            for (int it = 0; it < 2; ++it) {
-                const int i = 16 * it + lm;
-                const int64_t c = col0 + wave * 16 * NT + lg * 4 * NT;
-                if (i >= n || c >= A.dc) continue;
-                const int64_t pos = g.begin + base + i;
-                constexpr int W = 4 * NT;
-                if (A.out_f32) {
-                    typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
-                    float *to = const_cast<float *>(token_ptr<float>(A.out, A, g, pos, h)) + c;
-                    if (c + W <= A.dc) {
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<f4 *>(to + 4 * nt) = O[it][nt];
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < W; ++r)
-                            if (c + r < A.dc) to[r] = O[it][r / 4][r % 4];
-                    }
-                } else {
-                    typedef bf16 out_t __attribute__((ext_vector_type(W), aligned(2)));
-                    bf16 *to = const_cast<bf16 *>(token_ptr<bf16>(A.out, A, g, pos, h)) + c;
-                    out_t v;
-#pragma unroll
-                    for (int r = 0; r < W; ++r) v[r] = bf16(O[it][r / 4][r % 4]);
-                    if (c + W <= A.dc) {
-                        *reinterpret_cast<out_t *>(to) = v;
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < W; ++r)
-                            if (c + r < A.dc) to[r] = v[r];
-                    }
-                }
-            }
         }
         if (n < N) {        // the last chunk: decays to its own end; beyond it c is 0
             whole = power[n];
@@ -503,53 +539,75 @@ __global__ void __launch_bounds__(256, 2) attend_bf16(AttendArgs A) {
             }
         }
     };
-    if (g.len > 0) load_chunk(buffer0, 0);
-    for (int64_t base = 0; base < g.len; base += 2 * N) {
-        chunk(buffer0, buffer1, base);
-        if (base + N < g.len) chunk(buffer1, buffer0, base + N);
+    if (len > 0) {
+        load_chunk(buffer0, 0);
+        load_chunk(buffer1, N);
+        int base = 0;
+        for (;;) {
+            chunk(buffer0, buffer2, base);
+            if ((base += N) >= len) break;
+            chunk(buffer1, buffer0, base);
+            if ((base += N) >= len) break;
+            chunk(buffer2, buffer1, base);
+            if ((base += N) >= len) break;
+        }
+        if (OUT) store(base - N);
     }
-
-    float *out = !OUT ? A.segments + (int64_t(blockIdx.x) * A.heads + h) * A.da * A.dc : g.index == g.count - 1 && A.state_out ? A.state_out + (g.seq * A.heads + h) * A.da * A.dc : nullptr;
-    if (!out) return;
+    if (!OUT) {
 #pragma unroll
-    for (int t = 0; t < 2 * DS; ++t)
+        for (int t = 0; t < 2 * DS; ++t)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+            for (int nt = 0; nt < NT; ++nt) mine[(t * NT + nt) * 64] = S[t][nt];
+    } else if (g.index == g.count - 1 && A.state_out) {
+        float *out = A.state_out + (g.seq * A.heads + h) * A.da * A.dc;
+        const int64_t step_d = A.state_transposed ? 1 : A.dc, step_c = A.state_transposed ? A.da : 1;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int64_t d = t / 2 * 32 + lg * 8 + t % 2 * 4 + r, c = column(nt);
-                if (d < A.da && c < A.dc) out[OUT && A.state_transposed ? c * A.da + d : d * A.dc + c] = S[t][nt][r];
-            }
+        for (int t = 0; t < 2 * DS; ++t)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int64_t d = t / 2 * 32 + lg * 8 + t % 2 * 4 + r, c = column(nt);
+                    if (d < A.da && c < A.dc) out[d * step_d + c * step_c] = S[t][nt][r];
+                }
+    }
 #endif
 }
 
 // States over the segments of a sequence, in order: what each adds is replaced
-// by what enters it.  A thread an element of the state.
-__global__ void __launch_bounds__(256) attend_carry(AttendArgs A) {
-    const int64_t size = A.da * A.dc, at = int64_t(blockIdx.z) * 256 + threadIdx.x;
-    const int64_t seq = blockIdx.x, h = blockIdx.y;
-    if (at >= size) return;
-    int64_t id, count;
+// by what enters it (the first one's stays).  A thread four values of the state,
+// wherever they lie; U segments' are read at once.  size: a multiple of 4.
+__global__ void __launch_bounds__(256) attend_carry(AttendArgs A, uint32_t size) {
+    constexpr int U = 8;
+    const uint32_t at = blockIdx.z * 256 + threadIdx.x;
+    const uint32_t seq = blockIdx.x, h = blockIdx.y;
+    uint32_t id, count;
     if (!A.offsets) {
-        count = A.n_segments / A.n_seq;
+        count = uint32_t(A.n_segments) / uint32_t(A.n_seq);
         id = seq * count;
     } else {
+        const int shift = 63 - __builtin_clzll(A.seg_len);
         const int64_t lo = min(max(A.offsets[seq], int64_t(0)), A.n_tokens);
         const int64_t hi = min(max(A.offsets[seq + 1], int64_t(0)), A.n_tokens);
-        id = lo / A.seg_len + seq;
-        count = max((max(hi - lo, int64_t(0)) + A.seg_len - 1) / A.seg_len, int64_t(1));
-        count = min(count, A.n_segments - id);
+        id = uint32_t(lo >> shift) + seq;
+        count = uint32_t((max(hi - lo, int64_t(0)) + A.seg_len - 1) >> shift);
+        count = min(count, uint32_t(A.n_segments) - id);
     }
-    const int64_t from = A.state_transposed ? at % A.dc * A.da + at / A.dc : at;
-    float cur = A.state_in ? A.state_in[(seq * A.heads + h) * size + from] : 0.0f;
+    if (count < 2 || at >= size / 4) return;
     const float whole = decay(A.log_decay[h], A.seg_len);
-    float *p = A.segments + (id * A.heads + h) * size + at;
-    float next = count > 1 ? *p : 0.0f;
-    for (int64_t i = 0; i < count; ++i, p += A.heads * size) {
-        const float add = next;
-        if (i + 2 < count) next = p[A.heads * size];
-        *p = cur;
-        cur = whole * cur + add;
+    const int64_t step = A.heads * int64_t(size / 4);
+    f32x4 *p = reinterpret_cast<f32x4 *>(A.segments) + (int64_t(id) * A.heads + h) * (size / 4) + at;
+    f32x4 cur = *p;
+    for (uint32_t i = 1; i < count; i += U) {
+        f32x4 add[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) add[u] = i + u + 1 < count ? p[(i + u) * step] : f32x4(0.0f);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (i + u < count) {
+                p[(i + u) * step] = cur;
+                cur = whole * cur + add[u];
+            }
     }
 }
 
@@ -619,20 +677,24 @@ template <class T, int X> __global__ void __launch_bounds__(256) attend_step(Ste
     for (int j = 0; j < have; ++j) o[c + j] = T(sum[j] * a.scale);
 }
 
+void launch_carry(const AttendArgs &a, int64_t size, hipStream_t stream) {
+    attend_carry<<<dim3(uint32_t(a.n_seq), uint32_t(a.heads), uint32_t(ceil_div(size, 1024))), 256, 0, stream>>>(a, uint32_t(size));
+}
+
 template <class T, int DT, int STAGE> void launch_general(const AttendArgs &a, hipStream_t stream) {
-    const dim3 grid(uint32_t(a.n_segments), uint32_t(a.heads), uint32_t(ceil_div(a.dc, 64)));
+    const dim3 grid(uint32_t(a.n_segments * a.heads), uint32_t(ceil_div(a.dc, 64)));
     if (a.n_segments > a.n_seq) {
         attend_general<T, DT, STAGE, false><<<grid, 256, 0, stream>>>(a);
-        attend_carry<<<dim3(uint32_t(a.n_seq), uint32_t(a.heads), uint32_t(ceil_div(a.da * a.dc, 256))), 256, 0, stream>>>(a);
+        launch_carry(a, ceil_div(a.da * a.dc, 4) * 4, stream);
     }
     attend_general<T, DT, STAGE, true><<<grid, 256, 0, stream>>>(a);
 }
 
 template <int DS, int NT, bool DIRECT> void launch_bf16(const AttendArgs &a, hipStream_t stream) {
-    const dim3 grid(uint32_t(a.n_segments), uint32_t(a.heads), uint32_t(ceil_div(a.dc, 64 * NT)));
+    const dim3 grid(uint32_t(a.n_segments * a.heads), uint32_t(ceil_div(a.dc, 64 * NT)));
     if (a.n_segments > a.n_seq) {
         attend_bf16<DS, NT, DIRECT, false><<<grid, 256, 0, stream>>>(a);
-        attend_carry<<<dim3(uint32_t(a.n_seq), uint32_t(a.heads), uint32_t(ceil_div(a.da * a.dc, 256))), 256, 0, stream>>>(a);
+        launch_carry(a, int64_t(grid.y) * 4 * 2 * DS * NT * 256, stream);
     }
     attend_bf16<DS, NT, DIRECT, true><<<grid, 256, 0, stream>>>(a);
 }
@@ -651,6 +713,34 @@ template <bool DIRECT> void launch_bf16(const AttendArgs &a, hipStream_t stream)
 }
 
 }  // namespace
+
+// How sequences are cut: into segments of at least 256 tokens, enough of them for two
+// workgroups a compute unit (16 heads x 16384 tokens of 128: 115 us; for one, 126; for four,
+// whose states are twice the traffic, 143).  A packed batch is cut wherever a sequence may be
+// longer than that: its longest sequence is not known here, and would be walked by one
+// workgroup while the others are done.
+Cut attend_cut(int dtype, int64_t n_seq, int64_t n_tokens, int64_t heads, int64_t da, int64_t dc, bool packed) {
+    const bool matrix = dtype == NDVM_BF16 && da <= 128;
+    const int64_t cols = matrix && dc > 64 ? 128 : 64;
+    Cut c;
+    c.state = matrix ? (da <= 64 ? 64 : 128) * ceil_div(dc, cols) * cols : ceil_div(da * dc, 4) * 4;
+    const int64_t longest = packed || n_seq == 0 ? n_tokens : n_tokens / n_seq;
+    const int64_t want = std::max<int64_t>(1, 2 * kCus / (heads * ceil_div(dc, cols)));
+    int64_t len = std::max<int64_t>(256, n_tokens / want);
+    len = ceil_div(len, kSegStep) * kSegStep;
+    if (len >= longest || (!packed && n_seq >= want)) {
+        c.seg_len = std::max<int64_t>(longest, 1);
+        c.n_segments = n_seq;
+    } else if (packed) {
+        c.seg_len = 256;
+        while (c.seg_len * 2 <= len) c.seg_len *= 2;
+        c.n_segments = n_tokens / c.seg_len + n_seq;
+    } else {
+        c.seg_len = ceil_div(ceil_div(longest, ceil_div(longest, len)), kSegStep) * kSegStep;
+        c.n_segments = n_seq * ceil_div(longest, c.seg_len);
+    }
+    return c;
+}
 
 hipError_t launch_attend(int dtype, const AttendArgs &a, hipStream_t stream) {
     if (dtype == NDVM_BF16 && a.da <= 128) {

@@ -50,7 +50,7 @@ struct AttendArgs {
     const int64_t *offsets;     // [n_seq + 1], or null: n_tokens / n_seq tokens each
     const float *state_in;      // [n_seq, heads, da, dc] (or transposed), or null
     float *state_out;           // as state_in, or null
-    float *segments;            // [n_segments, heads, da, dc]: what each segment adds, then what enters it
+    float *segments;            // a state for each segment and head: what the segment adds, then what enters it
     int64_t n_seq, n_tokens, heads, da, dc;
     int64_t seg_len, n_segments;    // tokens of a segment (a multiple of kSegStep); ids of the launch
     float scale_pair, scale_add, scale_read;    // of a pair's product, of what the state takes, of what is read from it
@@ -59,6 +59,11 @@ struct AttendArgs {
     int out_f32;                // `out` is float whatever the type
 };
 constexpr int64_t kSegStep = 64, kMostHeadDim = 256, kMostHeads = 65535;
+struct Cut {
+    int64_t seg_len, n_segments;    // more segments than sequences: sequences are cut
+    int64_t state;                  // floats of a segment's and head's state
+};
+Cut attend_cut(int dtype, int64_t n_seq, int64_t n_tokens, int64_t heads, int64_t da, int64_t dc, bool packed);
 hipError_t launch_attend(int dtype, const AttendArgs &a, hipStream_t stream);
 // sum of `group` consecutive heads of float [heads][tokens][d] into `out` [.., heads / group, d]
 struct FoldHeadsArgs {

@@ -60,6 +60,8 @@ ndvm_status check_shape(const char *who, const ndvm_attention_shape *s, bool tok
     if (s->n_tokens < 0 || (s->n_seq == 0 && s->n_tokens)) return bad(who, "bad token count");
     if (s->n_tokens > INT32_MAX || !fits(s->n_tokens, s->heads, std::max(s->dk, s->dv)))
         return fail(NDVM_E_UNSUPPORTED, who, "too many tokens");
+    if (!fits(s->n_tokens / 64 + s->n_seq + 1, s->heads) || (s->n_tokens / 64 + s->n_seq + 1) * s->heads > INT32_MAX)
+        return fail(NDVM_E_UNSUPPORTED, who, "too many sequences, tokens and heads for one launch");
     return NDVM_OK;
 }
 
@@ -73,37 +75,26 @@ Heads heads_of(const ndvm_heads *h, int64_t group) {
     return Heads{h->data, h->seq_stride, h->tok_stride, h->head_stride, int(group)};
 }
 
-// Segments of a call: enough for four workgroups a compute unit, of at least 256
-// tokens (a segment's state costs the traffic of about 128 tokens to carry).
-struct Cut {
-    int64_t seg_len, n_segments;
-};
-Cut cut_of(const ndvm_attention_shape *s, bool packed, int64_t dc) {
-    const int64_t longest = packed || s->n_seq == 0 ? s->n_tokens : s->n_tokens / s->n_seq;
-    const int64_t per_token = s->heads * ceil_div(dc, 64);
-    const int64_t want = std::max<int64_t>(1, 4 * kCus / per_token);
-    int64_t len = std::max<int64_t>(256, s->n_tokens / want);
-    len = ceil_div(len, kSegStep) * kSegStep;
-    if (s->n_seq >= want || len >= longest) return Cut{std::max<int64_t>(longest, 1), s->n_seq};
-    if (packed) return Cut{len, s->n_tokens / len + s->n_seq};
-    const int64_t per = ceil_div(longest, len);
-    len = ceil_div(ceil_div(longest, per), kSegStep) * kSegStep;
-    return Cut{len, s->n_seq * ceil_div(longest, len)};
+Cut cut_of(const ndvm_attention_shape *s, bool packed, int64_t da, int64_t dc) {
+    return attend_cut(s->dtype, s->n_seq, s->n_tokens, s->heads, da, dc, packed);
 }
 
 size_t segment_bytes(const ndvm_attention_shape *s, const Cut &c) {
-    return c.n_segments > s->n_seq ? round256(size_t(c.n_segments * s->heads) * size_t(s->dk * s->dv) * 4) : 0;
+    return c.n_segments > s->n_seq ? round256(size_t(c.n_segments * s->heads) * size_t(c.state) * 4) : 0;
+}
+
+// of the gradient's calls
+size_t grad_segment_bytes(const ndvm_attention_shape *s, bool packed) {
+    return std::max(segment_bytes(s, cut_of(s, packed, s->dk, s->dv)), segment_bytes(s, cut_of(s, packed, s->dv, s->dk)));
 }
 
 size_t attention_bytes(const ndvm_attention_shape *s, bool packed, bool grad) {
-    size_t n = segment_bytes(s, cut_of(s, packed, s->dv));
-    if (grad) {
-        n = std::max(n, segment_bytes(s, cut_of(s, packed, s->dk)));
-        if (s->heads > s->kv_heads) n += round256(size_t(s->heads * s->n_tokens) * size_t(std::max(s->dk, s->dv)) * 4);
-        n += 256;
-    } else if (n) {
-        n += 256;
+    if (!grad) {
+        const size_t n = segment_bytes(s, cut_of(s, packed, s->dk, s->dv));
+        return n ? n + 256 : 0;
     }
+    size_t n = grad_segment_bytes(s, packed) + 256;
+    if (s->heads > s->kv_heads) n += round256(size_t(s->heads * s->n_tokens) * size_t(std::max(s->dk, s->dv)) * 4);
     return n;
 }
 
@@ -193,7 +184,7 @@ ndvm_status ndvm_linear_attention(const ndvm_attention_shape *shape, const ndvm_
         const size_t need = attention_bytes(s, offsets != nullptr, false);
         if (workspace_bytes < need) return fail(NDVM_E_NOMEM, who, "workspace too small");
         if (need && !workspace) return bad(who, "null workspace");
-        const Cut cut = cut_of(s, offsets != nullptr, s->dv);
+        const Cut cut = cut_of(s, offsets != nullptr, s->dk, s->dv);
         const int64_t group = s->heads / s->kv_heads;
         AttendArgs a{};
         a.a = heads_of(q, 1);
@@ -246,7 +237,7 @@ ndvm_status ndvm_linear_attention_grad(const ndvm_attention_shape *shape, const 
         a.heads = s->heads;
         a.segments = reinterpret_cast<float *>(ws);
         const auto widths = [&](int64_t da, int64_t dc) {
-            const Cut cut = cut_of(s, offsets != nullptr, dc);
+            const Cut cut = cut_of(s, offsets != nullptr, da, dc);
             a.da = da;
             a.dc = dc;
             a.seg_len = cut.seg_len;
@@ -268,7 +259,7 @@ ndvm_status ndvm_linear_attention_grad(const ndvm_attention_shape *shape, const 
         a.state_in = d_final;
         a.scale_pair = a.scale_add = float(s->scale);
         a.scale_read = 1.0f;
-        const size_t segments = std::max(segment_bytes(s, cut_of(s, offsets != nullptr, s->dv)), segment_bytes(s, cut_of(s, offsets != nullptr, s->dk)));
+        const size_t segments = grad_segment_bytes(s, offsets != nullptr);
         float *part = reinterpret_cast<float *>(ws + segments);
         // over the query heads of a group: each head's gradient in float, then their sum
         const auto shared = [&](const ndvm_heads *to, int64_t d) -> ndvm_status {
