@@ -34,7 +34,7 @@ template <> struct Oct<f16> { typedef f16x8 type; };
 __device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ inline f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-constexpr int kStep = 64;       // of the sum, per LDS tile
+[[maybe_unused]] constexpr int kStep = 64;      // of the sum, per LDS tile
 
 // Parts of a value in an operand: itself, or a float's three bf16.
 template <class T> struct Parts {       // 16-bit types
@@ -146,8 +146,8 @@ __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
     constexpr int WA = BA / NA, WB = BB / NB, TA = WA / 16, TB = WB / 16;
     constexpr bool GATED = KIND != kPlain;
     constexpr int COLS = GATED ? BA / 2 : BA;       // columns of C a tile has
-    extern __shared__ __align__(1024) char lds[];
-    constexpr int SIZE = (BA + BB) * kStep * 2;
+    // two arrays, so that the compiler sees that loads into one leave reads of the other alone
+    __shared__ __align__(1024) char buffer0[(BA + BB) * kStep * 2], buffer1[(BA + BB) * kStep * 2];
 
     // Tiles in an order that keeps an XCD (workgroup % 8) on neighbouring ones: its share
     // of the tiles, in bands of 8 tile rows.
@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
     const int64_t steps = ceil_div(A.k, kStep);
     // pairs of parts, largest products first
     constexpr int pair_a[6] = {0, 0, 1, 1, 0, 2}, pair_b[6] = {0, 1, 0, 1, 2, 0};
-    const auto load = [&](int64_t s, int buf) {
+    const auto load = [&](int64_t s, char *to) __attribute__((always_inline)) {
         int64_t k0 = s * kStep;
         int pa = 0, pb = 0;
         if (PAIRS > 1) {
@@ -199,7 +199,6 @@ __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
         const bool some = k0 + granule * 8 < A.k;
         const auto ra = rsrc(base_a + pa * A.a.plane + k0), rb = rsrc(base_b + pb * A.b.plane + k0);
         const auto ra2 = GATED ? rsrc(base_a2 + pa * A.a2.plane + k0) : ra;
-        char *to = lds + buf * SIZE;
 #pragma unroll
         for (int i = 0; i < LA; ++i) {
             const int first = (wave + W * i) * 8;
@@ -221,28 +220,29 @@ __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
 #pragma unroll
         for (int j = 0; j < TB; ++j) acc[i][j] = 0;
     const int64_t total = steps * PAIRS;
-    if (total > 0) load(0, 0);
-    for (int64_t s = 0; s < total; ++s) {
+    const auto step = [&](int64_t s, const char *from, char *next) __attribute__((always_inline)) {
         // every wave's loads of this buffer have landed, and none reads the other one
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
-        const char *from = lds + (s % 2) * SIZE;
-        oct fa[2][TA], fb[2][TB];
+        if (s + 1 < total) load(s + 1, next);
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
+            oct fa[TA], fb[TB];
             const int place = ((kk * 4 + lg) ^ (lm % 8)) * 16;
 #pragma unroll
-            for (int i = 0; i < TA; ++i) fa[kk][i] = *reinterpret_cast<const oct *>(from + (wa * WA + i * 16 + lm) * 128 + place);
+            for (int i = 0; i < TA; ++i) fa[i] = *reinterpret_cast<const oct *>(from + (wa * WA + i * 16 + lm) * 128 + place);
 #pragma unroll
-            for (int j = 0; j < TB; ++j) fb[kk][j] = *reinterpret_cast<const oct *>(from + (BA + wb * WB + j * 16 + lm) * 128 + place);
-        }
-        if (s + 1 < total) load(s + 1, int((s + 1) % 2));
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk)
+            for (int j = 0; j < TB; ++j) fb[j] = *reinterpret_cast<const oct *>(from + (BA + wb * WB + j * 16 + lm) * 128 + place);
 #pragma unroll
             for (int i = 0; i < TA; ++i)
 #pragma unroll
-                for (int j = 0; j < TB; ++j) acc[i][j] = mfma(fa[kk][i], fb[kk][j], acc[i][j]);
+                for (int j = 0; j < TB; ++j) acc[i][j] = mfma(fa[i], fb[j], acc[i][j]);
+        }
+    };
+    if (total > 0) load(0, buffer0);
+    for (int64_t s = 0; s < total; s += 2) {
+        step(s, buffer0, buffer1);
+        if (s + 1 < total) step(s + 1, buffer1, buffer0);
     }
 
     // lane l, register r of tile (i, j): column n = 4 (l / 16) + r, row m = l % 16
@@ -326,14 +326,11 @@ template <class T, int BA, int BB, int NA, int NB, Kind KIND> void launch_tiles(
     a.tiles_n = ceil_div(n, KIND == kPlain ? BA : BA / 2);
     a.tiles_m = ceil_div(m, BB);
     if (a.tiles_n * a.tiles_m == 0) return;
-    constexpr int bytes = 2 * (BA + BB) * kStep * 2;
-    const auto kernel = product<T, BA, BB, NA, NB, KIND>;
-    if (bytes > 64 * 1024)
-        (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    kernel<<<dim3(uint32_t(a.tiles_n * a.tiles_m)), 64 * NA * NB, bytes, stream>>>(a);
+    product<T, BA, BB, NA, NB, KIND><<<dim3(uint32_t(a.tiles_n * a.tiles_m)), 64 * NA * NB, 0, stream>>>(a);
 }
 template <class T, Kind KIND> void launch_product(const ProductArgs &a, int64_t n, int64_t m, hipStream_t stream) {
-    launch_tiles<T, 128, 128, 2, 2, KIND>(a, n, m, stream);
+    if (ceil_div(n, KIND == kPlain ? 256 : 128) * ceil_div(m, 256) >= 2 * kCus) launch_tiles<T, 256, 256, 2, 4, KIND>(a, n, m, stream);
+    else launch_tiles<T, 128, 128, 2, 2, KIND>(a, n, m, stream);
 }
 
 int64_t pad64(int64_t n) { return ceil_div(n, 64) * 64; }

@@ -403,6 +403,23 @@ def test_gated_ffn_grad(nd, kind, name, rows, n_in, n_out):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,n_in,n_out", [(4100, 136, 4200), (2600, 200, 1000), (600, 1030, 300)])
+def test_gated_ffn_many_tiles(nd, kind, rows, n_in, n_out):
+    """Products of many tiles, forward and backward."""
+    normal = make(rows + n_in)
+    x, xv = normal(rows, n_in, kind=kind)
+    wg, wgv = normal(n_out, n_in, kind=kind, scale=n_in ** -0.5)
+    wu, wuv = normal(n_out, n_in, kind=kind, scale=n_in ** -0.5)
+    check(nd.gated_ffn(x, wg, wu), ref.ffn(xv, wgv, wuv, "silu"), ref.ffn_bound(xv, wgv, wuv, "silu", kind))
+    dh, dhv = normal(rows, n_out, kind=kind)
+    got = nd.gated_ffn_grad(dh, x, wg, wu)
+    want = ref.ffn_grad(dhv, xv, wgv, wuv, "silu")
+    bounds = ref.ffn_grad_bound(dhv, xv, wgv, wuv, "silu", kind)
+    for a, b, c, what in zip(got, want, bounds, ("dx", "dw_gate", "dw_up")):
+        check(a, b, c, what)
+
+
+@pytest.mark.parametrize("kind", KINDS)
 def test_gated_ffn_strides(nd, kind):
     """Rows that are apart, at odd places: the same values as contiguous ones, and nothing written beside them."""
     normal = make(2)
