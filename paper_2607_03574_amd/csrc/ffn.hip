@@ -2,19 +2,20 @@
 //   g = x Wg^T,  u = x Wu^T,  h = act(g) u
 //   dg = dh u act'(g),  du = dh act(g),  dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x
 // Matrix products throughout: bound by the matrix instructions for many rows, by
-// reading the weights for few.  One kernel, product(), computes all of them from
-// operands whose rows run along the sum:  C[m][n] = sum_k A[n][k] B[m][k].
+// reading the weights for few.  One kernel, product(), computes C[m][n] = sum_k A[n][k]
+// B[m][k] from operands whose rows run along the sum or along C:
 //  - forward: a tile holds the same columns of both weights, so act(g) u is formed in
 //    the accumulators and g and u never reach memory;
 //  - gradient: g and u are formed again the same way (reading them back would cost their
-//    rounding; the two products are a third of the work), and dg, du leave the tile in
-//    both orders, [rows][2 n_out] and transposed, as operands of
-//    dx = [dg du] [Wg; Wu] and [dWg; dWu] = [dg du]^T x;
-//  - x and the weights are transposed once for those two.
-// 16-bit types are multiplied as they are.  A float is split exactly into three bf16
-// (8 + 8 + 8 bits) and the six products down to 2^-16 of the largest are added up in
-// float: what is left out is below 2^-23 of a term, and bf16 products are 16 times
-// the rate of float ones.
+//    rounding; the two products are a third of the work), and dg, du leave the tile as
+//    one operand [rows][2 n_out] of dx = [dg du] [Wg; Wu] and [dWg; dWu] = [dg du]^T x.
+//    Operands that run along C are turned by the transposing reads from LDS: nothing is
+//    transposed in memory.
+// Few rows have a kernel of their own, few(), that reads weights straight into the
+// matrix instructions' registers.
+// 16-bit types are multiplied as they are.  product() has a float as three bf16 (8 + 8 +
+// 8 bits, exactly) and adds up the six products down to 2^-16 of the largest in float: what
+// is left out is below 2^-23 of a term, and bf16 products are 16 times the rate of float ones.
 #include <algorithm>
 
 #include "ops.h"
@@ -76,40 +77,37 @@ __device__ inline void act_both(int act, float g, float &f, float &d) {
     }
 }
 
-// ---- operands laid out: a copy with rows padded to `ld_to` zeros, or the transpose
+// ---- operands laid out: a copy in parts, rows of `pad` values (zeros beyond the source's)
 struct PackArgs {
-    const void *from;
-    void *to;
-    int64_t rows, cols, ld;     // of `from`
-    int64_t ld_to, pad;         // row length of `to`; columns written (the source's and zeros)
-    int64_t plane;              // elements between a value's parts
+    const void *from[3];
+    void *to[3];
+    int64_t rows[3], ld[3], plane[3];   // plane: elements between a value's parts
+    int64_t cols, pad;                  // pad: a multiple of 64
 };
-template <class T, bool TRANSPOSE> __global__ void __launch_bounds__(256) pack(PackArgs a) {
+// A thread eight values; blockIdx.y: which of the copies.
+template <class T> __global__ void __launch_bounds__(256) pack(PackArgs a) {
     typedef typename Parts<T>::type P;
-    constexpr int N = Parts<T>::count;
-    __shared__ T tile[64][65];
-    const int64_t r0 = int64_t(blockIdx.x) * 64, c0 = int64_t(blockIdx.y) * 64;
-    const int x = threadIdx.x % 64;
-    for (int y = threadIdx.x / 64; y < 64; y += 4) {
-        const int64_t r = r0 + y, c = c0 + x;
-        tile[y][x] = r < a.rows && c < a.cols ? static_cast<const T *>(a.from)[r * a.ld + c] : T(0.0f);
-    }
-    __syncthreads();
-    const int64_t out_rows = TRANSPOSE ? a.cols : a.rows;
-    for (int y = threadIdx.x / 64; y < 64; y += 4) {
-        const int64_t r = (TRANSPOSE ? c0 : r0) + y, c = (TRANSPOSE ? r0 : c0) + x;
-        if (r >= out_rows || c >= a.pad) continue;
-        P part[N];
-        const T v = TRANSPOSE ? tile[x][y] : tile[y][x];
-        Parts<T>::split(float(v), part);
+    typedef P p8 __attribute__((ext_vector_type(8)));
+    constexpr int N = Parts<T>::count, V = kVec<T>;
+    const int w = blockIdx.y;
+    const int64_t per = a.pad / 8, at = int64_t(blockIdx.x) * 256 + threadIdx.x, r = at / per, c = at % per * 8;
+    if (r >= a.rows[w]) return;
+    const T *from = static_cast<const T *>(a.from[w]) + r * a.ld[w] + c;
+    p8 part[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) static_cast<P *>(a.to)[i * a.plane + r * a.ld_to + c] = part[i];
+    for (int j = 0; j < 8 / V; ++j) {
+        vec<T> v = T(0.0f);
+        if (c + j * V < a.cols) v = load_vec(from + j * V, a.cols - c - j * V);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            P q[N];
+            Parts<T>::split(float(v[i]), q);
+#pragma unroll
+            for (int k = 0; k < N; ++k) part[k][j * V + i] = q[k];
+        }
     }
-}
-template <class T, bool TRANSPOSE> void launch_pack(const PackArgs &a, hipStream_t stream) {
-    // the grid covers the padded columns too
-    const int64_t rows = TRANSPOSE ? a.pad : a.rows, cols = TRANSPOSE ? a.cols : a.pad;
-    if (rows && cols) pack<T, TRANSPOSE><<<dim3(uint32_t(ceil_div(rows, 64)), uint32_t(ceil_div(cols, 64))), 256, 0, stream>>>(a);
+#pragma unroll
+    for (int k = 0; k < N; ++k) *reinterpret_cast<p8 *>(static_cast<P *>(a.to[w]) + k * a.plane[w] + r * a.pad + c) = part[k];
 }
 
 // ---- the product
@@ -118,33 +116,46 @@ struct Operand {
     int64_t rows, ld, plane;
 };
 struct ProductArgs {
-    Operand a, a2, b;           // a2: the second weight of a gated product
-    int64_t k;                  // a multiple of 8
+    Operand a, a2, b;           // a2: gated, the second weight; plain, what follows `a` along the sum from k2 on
+    int64_t k, k2;              // the sum's length, a multiple of 8 (of 64 where an operand runs along C)
     int64_t tiles_n, tiles_m;
     int act;
-    // plain: rows m < split go to out + m * ld, the others from split2 on to out2 + (m - split2) * ld2
+    // plain: rows m < split go to out + m * ld, those from split2 to m2 to out2 + (m - split2) * ld2
     void *out, *out2;
     int64_t ld, ld2, n, m, split, split2, m2;
     // gated gradient
     const void *dh;
     int64_t ld_dh;
-    void *p, *pt;               // [dg du] and its transpose, in parts
-    int64_t pad_n, ld_p, plane_p, pad_m, ld_pt, plane_pt;
+    void *p;                    // [m][dg du], each padded with zeros to pad_n, in parts
+    int64_t pad_n, ld_p, plane_p;
 };
 enum Kind { kGated, kGatedGrad, kPlain };
 
-// BA rows of A by BB rows of B a workgroup; NA x NB waves.
-// LDS rows are 64 values (128 bytes, 8 granules of 16); granule i of row r lies at place
-// i ^ (r % 8), so a wave's reads of 16 rows touch all banks evenly.  The loads go to LDS
-// directly and choose their source accordingly; values out of range read as 0.
-template <class T, int BA, int BB, int NA, int NB, Kind KIND>
+#ifdef __HIP_DEVICE_COMPILE__
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+// Lane 4 r + x of 16 names four values of row r; lane i gets column i of the four rows.
+template <class O> __device__ inline O read_transposed(const char *p, const char *q) {
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    const auto four = [](const char *at) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at)); };
+    return __builtin_bit_cast(O, s16x8(__builtin_shufflevector(four(p), four(q), 0, 1, 2, 3, 4, 5, 6, 7)));
+}
+#endif
+
+// BA columns n by BB rows m a workgroup; NA x NB waves.  ALONG_A, ALONG_B: the operand's rows
+// run along C (A[k][n], B[k][m]).
+// An LDS tile of an operand is 64 long along the sum: rows of 64 values, or 64 rows along C,
+// in granules of 16 bytes.  Granule i of row r lies at place i ^ f(r) with f = r % 4 + 4 (r / 8
+// % 2) (twice that for rows along C, which are read two granules at a time), so that the 16
+// rows an instruction reads are in different banks.  The loads go to LDS directly and choose
+// their source accordingly; what is out of range reads as 0.
+template <class T, int BA, int BB, int NA, int NB, Kind KIND, bool ALONG_B>
 __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
 #ifdef __HIP_DEVICE_COMPILE__       // the host's pass does not know the types of the loads to LDS
     typedef typename Parts<T>::type P;
     typedef typename Oct<P>::type oct;
     constexpr int PARTS = Parts<T>::count, PAIRS = PARTS == 1 ? 1 : 6, W = NA * NB;
     constexpr int WA = BA / NA, WB = BB / NB, TA = WA / 16, TB = WB / 16;
-    constexpr bool GATED = KIND != kPlain;
+    constexpr bool GATED = KIND != kPlain, ALONG_A = !GATED;
     constexpr int COLS = GATED ? BA / 2 : BA;       // columns of C a tile has
     // two arrays, so that the compiler sees that loads into one leave reads of the other alone
     __shared__ __align__(1024) char buffer0[(BA + BB) * kStep * 2], buffer1[(BA + BB) * kStep * 2];
@@ -164,53 +175,74 @@ __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
     const int lm = l % 16, lg = l / 16, wa = wave / NB, wb = wave % NB;
     constexpr unsigned kNowhere = 0x80000000u;
     const auto rsrc = [](const void *p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, 0x7fffffff, 0x00020000); };
+    const auto f = [](int row) { return row % 4 + row / 8 % 2 * 4; };
 
-    // Wave-wide loads of 8 rows: which rows, and where a lane's granule of them is.
+    // Wave-wide loads of 1 KB.  Along the sum: 8 rows of 8 granules.
     constexpr int LA = BA / 8 / W, LB = BB / 8 / W;
-    const int sub = l / 8, granule = (l % 8) ^ sub;
+    const int sub = l / 8, granule = (l % 8) ^ f(wave * 8 + sub);      // the same for every load: W is even
+    static_assert(W % 2 == 0, "");
+    // Along C: rows of R / 8 granules, 512 / R rows a load.
+    const auto along_row = [&](int i, int R) { return (wave + W * i) * (512 / R) + l / (R / 8); };
+    const auto along_col = [&](int i, int R) { return ((l % (R / 8)) ^ 2 * f(along_row(i, R))) * 8; };
     unsigned at_a[LA], at_b[LB];
-    const P *base_a = static_cast<const P *>(A.a.p) + n0 * A.a.ld, *base_b = static_cast<const P *>(A.b.p) + m0 * A.b.ld;
-    const P *base_a2 = GATED ? static_cast<const P *>(A.a2.p) + n0 * A.a2.ld : nullptr;
 #pragma unroll
     for (int i = 0; i < LA; ++i) {
-        const int row = (wave + W * i) * 8 + sub;
-        const bool second = GATED && row % WA >= WA / 2;
-        const int r = GATED ? row / WA * (WA / 2) + row % (WA / 2) : row;
-        at_a[i] = n0 + r < A.a.rows ? unsigned(r * (second ? A.a2.ld : A.a.ld) + granule * 8) * 2 : kNowhere;
+        if constexpr (ALONG_A) {
+            const int col = along_col(i, BA);
+            at_a[i] = n0 + col < A.n ? unsigned(along_row(i, BA) * A.a.ld + col) * 2 : kNowhere;
+        } else {
+            const int row = (wave + W * i) * 8 + sub;
+            const bool second = row % WA >= WA / 2;
+            const int r = row / WA * (WA / 2) + row % (WA / 2);
+            at_a[i] = n0 + r < A.a.rows ? unsigned(r * (second ? A.a2.ld : A.a.ld) + granule * 8) * 2 : kNowhere;
+        }
     }
 #pragma unroll
     for (int i = 0; i < LB; ++i) {
-        const int row = (wave + W * i) * 8 + sub;
-        at_b[i] = m0 + row < A.b.rows ? unsigned(row * A.b.ld + granule * 8) * 2 : kNowhere;
+        if constexpr (ALONG_B) {
+            const int col = along_col(i, BB);
+            at_b[i] = m0 + col < A.m ? unsigned(along_row(i, BB) * A.b.ld + col) * 2 : kNowhere;
+        } else {
+            const int row = (wave + W * i) * 8 + sub;
+            at_b[i] = m0 + row < A.b.rows ? unsigned(row * A.b.ld + granule * 8) * 2 : kNowhere;
+        }
     }
-    const int64_t steps = ceil_div(A.k, kStep);
+    const int steps = int((A.k + kStep - 1) / kStep), total = steps * PAIRS;
     // pairs of parts, largest products first
     constexpr int pair_a[6] = {0, 0, 1, 1, 0, 2}, pair_b[6] = {0, 1, 0, 1, 2, 0};
-    const auto load = [&](int64_t s, char *to) __attribute__((always_inline)) {
-        int64_t k0 = s * kStep;
+    const auto load = [&](int s, char *to) __attribute__((always_inline)) {
+        int64_t k0 = int64_t(s) * kStep;
         int pa = 0, pb = 0;
         if (PAIRS > 1) {
-            const int pair = int(s / steps);
-            k0 = s % steps * kStep;
+            const int pair = s / steps;
+            k0 = int64_t(s % steps) * kStep;
 #pragma unroll
             for (int i = 0; i < PAIRS; ++i)
                 if (i == pair) pa = pair_a[i], pb = pair_b[i];
         }
         const bool some = k0 + granule * 8 < A.k;
-        const auto ra = rsrc(base_a + pa * A.a.plane + k0), rb = rsrc(base_b + pb * A.b.plane + k0);
-        const auto ra2 = GATED ? rsrc(base_a2 + pa * A.a2.plane + k0) : ra;
+        {
+            const bool after = ALONG_A && k0 >= A.k2;
+            const Operand &o = after ? A.a2 : A.a;
+            const int64_t k1 = after ? k0 - A.k2 : k0;
+            const P *base = static_cast<const P *>(o.p) + pa * o.plane + (ALONG_A ? k1 * o.ld + n0 : n0 * o.ld + k0);
+            const auto r = rsrc(base);
+            const auto r2 = GATED ? rsrc(static_cast<const P *>(A.a2.p) + pa * A.a2.plane + n0 * A.a2.ld + k0) : r;
 #pragma unroll
-        for (int i = 0; i < LA; ++i) {
-            const int first = (wave + W * i) * 8;
-            const bool second = GATED && first % WA >= WA / 2;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(second ? ra2 : ra, (__attribute__((address_space(3))) void *)(to + first * 128), 16,
-                                                     some ? at_a[i] : kNowhere, 0, 0, 0);
+            for (int i = 0; i < LA; ++i) {
+                const bool second = GATED && (wave + W * i) * 8 % WA >= WA / 2;
+                const bool there = ALONG_A ? k1 + along_row(i, BA) < o.rows : some;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(second ? r2 : r, (__attribute__((address_space(3))) void *)(to + (wave + W * i) * 1024), 16,
+                                                         there ? at_a[i] : kNowhere, 0, 0, 0);
+            }
         }
+        const P *base = static_cast<const P *>(A.b.p) + pb * A.b.plane + (ALONG_B ? k0 * A.b.ld + m0 : m0 * A.b.ld + k0);
+        const auto r = rsrc(base);
 #pragma unroll
         for (int i = 0; i < LB; ++i) {
-            const int first = (wave + W * i) * 8;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (__attribute__((address_space(3))) void *)(to + (BA + first) * 128), 16,
-                                                     some ? at_b[i] : kNowhere, 0, 0, 0);
+            const bool there = ALONG_B ? k0 + along_row(i, BB) < A.b.rows : some;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(to + BA * 128 + (wave + W * i) * 1024), 16,
+                                                     there ? at_b[i] : kNowhere, 0, 0, 0);
         }
     };
 
@@ -219,8 +251,17 @@ __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
     for (int i = 0; i < TA; ++i)
 #pragma unroll
         for (int j = 0; j < TB; ++j) acc[i][j] = 0;
-    const int64_t total = steps * PAIRS;
-    const auto step = [&](int64_t s, const char *from, char *next) __attribute__((always_inline)) {
+    const int tr_row = 8 * lg + lm / 4;     // (+ 4: the same f)
+    // 16 rows and half a step of an operand in the layout of the matrix instructions
+    const auto along = [&](const char *from, int R, int col0, int kk) __attribute__((always_inline)) {
+        const int row = kk * 32 + tr_row, granule = col0 / 8 + lm % 4 / 2;
+        const char *p = from + row * R * 2 + ((granule ^ 2 * f(row)) * 16 + lm % 2 * 8);
+        return read_transposed<oct>(p, p + 4 * R * 2);
+    };
+    const auto summed = [&](const char *from, int row, int kk) __attribute__((always_inline)) {
+        return *reinterpret_cast<const oct *>(from + row * 128 + ((kk * 4 + lg) ^ f(row)) * 16);
+    };
+    const auto step = [&](int s, const char *from, char *next) __attribute__((always_inline)) {
         // every wave's loads of this buffer have landed, and none reads the other one
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
@@ -228,11 +269,17 @@ __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
             oct fa[TA], fb[TB];
-            const int place = ((kk * 4 + lg) ^ (lm % 8)) * 16;
 #pragma unroll
-            for (int i = 0; i < TA; ++i) fa[i] = *reinterpret_cast<const oct *>(from + (wa * WA + i * 16 + lm) * 128 + place);
+            for (int i = 0; i < TA; ++i) {
+                // gated: rows of a pair of tiles in the order that leaves a lane with eight columns side by side
+                if constexpr (ALONG_A) fa[i] = along(from, BA, wa * WA + i * 16, kk);
+                else fa[i] = summed(from, wa * WA + i / 2 * 32 + lm / 4 * 8 + i % 2 * 4 + lm % 4, kk);
+            }
 #pragma unroll
-            for (int j = 0; j < TB; ++j) fb[j] = *reinterpret_cast<const oct *>(from + (BA + wb * WB + j * 16 + lm) * 128 + place);
+            for (int j = 0; j < TB; ++j) {
+                if constexpr (ALONG_B) fb[j] = along(from + BA * 128, BB, wb * WB + j * 16, kk);
+                else fb[j] = summed(from + BA * 128, wb * WB + j * 16 + lm, kk);
+            }
 #pragma unroll
             for (int i = 0; i < TA; ++i)
 #pragma unroll
@@ -240,18 +287,18 @@ __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
         }
     };
     if (total > 0) load(0, buffer0);
-    for (int64_t s = 0; s < total; s += 2) {
+    for (int s = 0; s < total; s += 2) {
         step(s, buffer0, buffer1);
         if (s + 1 < total) step(s + 1, buffer1, buffer0);
     }
 
-    // lane l, register r of tile (i, j): column n = 4 (l / 16) + r, row m = l % 16
-    typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-    typedef P four_p __attribute__((ext_vector_type(4), aligned(8)));
+    // lane l, register r of tile (i, j): row m = l % 16 of j; column 4 (l / 16) + r of i, or,
+    // gated, 8 (l / 16) + 4 (i % 2) + r of the pair of tiles
 #pragma unroll
     for (int j = 0; j < TB; ++j) {
         const int64_t m = m0 + wb * WB + j * 16 + lm;
         if constexpr (KIND == kPlain) {
+            typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
             T *row = nullptr;
             if (m < A.split) row = static_cast<T *>(A.out) + m * A.ld;
             else if (m >= A.split2 && m < A.m2) row = static_cast<T *>(A.out2) + (m - A.split2) * A.ld2;
@@ -268,52 +315,54 @@ __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
                         if (n + r < A.n) row[n + r] = v[r];
             }
         } else {
+            if (m >= A.m) continue;
+            typedef T eight __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+            typedef P eight_p __attribute__((ext_vector_type(8)));
 #pragma unroll
-            for (int i = 0; i < TA / 2; ++i) {
-                const int64_t n = n0 + wa * (WA / 2) + i * 16 + lg * 4;
+            for (int i = 0; i < TA / 2; i += 2) {
+                const int64_t n = n0 + wa * (WA / 2) + i * 16 + lg * 8;
                 if constexpr (KIND == kGated) {
-                    if (m >= A.m) continue;
                     T *row = static_cast<T *>(A.out) + m * A.ld;
-                    four v;
+                    eight v;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        float f, d;
-                        act_both(A.act, acc[i][j][r], f, d);
-                        v[r] = T(f * acc[i + TA / 2][j][r]);
+                    for (int r = 0; r < 8; ++r) {
+                        float value, slope;
+                        act_both(A.act, acc[i + r / 4][j][r % 4], value, slope);
+                        v[r] = T(value * acc[i + r / 4 + TA / 2][j][r % 4]);
                     }
-                    if (n + 4 <= A.n) *reinterpret_cast<four *>(row + n) = v;
+                    if (n + 8 <= A.n) *reinterpret_cast<eight *>(row + n) = v;
                     else
-                        for (int r = 0; r < 4; ++r)
+                        for (int r = 0; r < 8; ++r)
                             if (n + r < A.n) row[n + r] = v[r];
                 } else {
-                    if (n >= A.pad_n || m >= A.pad_m) continue;
-                    const T *row = static_cast<const T *>(A.dh) + m * A.ld_dh;
-                    four_p vg[PARTS], vu[PARTS];
+                    if (n >= A.pad_n) continue;
+                    const T *row = static_cast<const T *>(A.dh) + m * A.ld_dh + n;
+                    eight dh = T(0.0f);
+                    if (n + 8 <= A.n) dh = *reinterpret_cast<const eight *>(row);
+                    else
+                        for (int r = 0; r < 8; ++r)
+                            if (n + r < A.n) dh[r] = row[r];
+                    eight_p vg[PARTS], vu[PARTS];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float dh = m < A.m && n + r < A.n ? float(row[n + r]) : 0.0f;
-                        float f, d;
-                        act_both(A.act, acc[i][j][r], f, d);
+                    for (int r = 0; r < 8; ++r) {
+                        float value, slope;
+                        act_both(A.act, acc[i + r / 4][j][r % 4], value, slope);
                         P pg[PARTS], pu[PARTS];
                         // what lies beyond the operands is 0, whatever act does there
-                        const bool there = m < A.m && n + r < A.n;
-                        Parts<T>::split(there ? dh * acc[i + TA / 2][j][r] * d : 0.0f, pg);
-                        Parts<T>::split(there ? dh * f : 0.0f, pu);
+                        const bool there = n + r < A.n;
+                        Parts<T>::split(there ? float(dh[r]) * acc[i + r / 4 + TA / 2][j][r % 4] * slope : 0.0f, pg);
+                        Parts<T>::split(there ? float(dh[r]) * value : 0.0f, pu);
 #pragma unroll
                         for (int q = 0; q < PARTS; ++q) {
                             vg[q][r] = pg[q];
                             vu[q][r] = pu[q];
-                            P *pt = static_cast<P *>(A.pt) + q * A.plane_pt + m;
-                            pt[(n + r) * A.ld_pt] = pg[q];
-                            pt[(A.pad_n + n + r) * A.ld_pt] = pu[q];
                         }
                     }
-                    if (m >= A.m) continue;
 #pragma unroll
                     for (int q = 0; q < PARTS; ++q) {
                         P *p = static_cast<P *>(A.p) + q * A.plane_p + m * A.ld_p + n;
-                        *reinterpret_cast<four_p *>(p) = vg[q];
-                        *reinterpret_cast<four_p *>(p + A.pad_n) = vu[q];
+                        *reinterpret_cast<eight_p *>(p) = vg[q];
+                        *reinterpret_cast<eight_p *>(p + A.pad_n) = vu[q];
                     }
                 }
             }
@@ -322,15 +371,89 @@ __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
 #endif
 }
 
-template <class T, int BA, int BB, int NA, int NB, Kind KIND> void launch_tiles(ProductArgs a, int64_t n, int64_t m, hipStream_t stream) {
+// ---- few rows: the weights are read once, straight into registers, by workgroups of 16
+// columns whose four waves share the sum; x comes from cache.  TB: rows in 16s.  Values are
+// loaded as 16 bytes of a row at any address, so nothing is laid out first; a float is multiplied as it is
+// (16 x 16 x 4: step r of the instruction takes value r of each lane's four).
+template <class T, int TB> __global__ void __launch_bounds__(256) few(FfnArgs A) {
+#ifdef __HIP_DEVICE_COMPILE__
+    constexpr int V = kVec<T>, K = 4 * V, U = TB > 2 ? 2 : 4;     // values of the sum a wave takes at a time; times in flight
+    __shared__ f32x4 sums[4][2][TB][64];
+    const int l = threadIdx.x % 64, wave = threadIdx.x / 64, lm = l % 16, lg = l / 16;
+    const int64_t n0 = int64_t(blockIdx.x) * 16, n = min(n0 + lm, A.n_out - 1);
+    const T *g = static_cast<const T *>(A.wg) + n * A.ld_wg, *u = static_cast<const T *>(A.wu) + n * A.ld_wu, *x[TB];
+#pragma unroll
+    for (int j = 0; j < TB; ++j) x[j] = static_cast<const T *>(A.x) + min(int64_t(j * 16 + lm), A.rows - 1) * A.ld_x;
+    f32x4 acc[2][TB];
+#pragma unroll
+    for (int j = 0; j < TB; ++j) acc[0][j] = acc[1][j] = 0;
+    const auto multiply = [](vec<T> a, vec<T> b, f32x4 c) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[r], b[r], c, 0, 0, 0);
+            return c;
+        } else {
+            return mfma(__builtin_bit_cast(typename Oct<T>::type, a), __builtin_bit_cast(typename Oct<T>::type, b), c);
+        }
+    };
+    for (int64_t k0 = wave * K; k0 < A.n_in; k0 += 4 * K * U) {
+        vec<T> vg[U], vu[U], vx[U][TB];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int64_t k = k0 + i * 4 * K + lg * V;
+            vg[i] = vu[i] = T(0.0f);
+#pragma unroll
+            for (int j = 0; j < TB; ++j) vx[i][j] = T(0.0f);
+            if (k < A.n_in) {
+                vg[i] = load_vec(g + k, A.n_in - k);
+                vu[i] = load_vec(u + k, A.n_in - k);
+#pragma unroll
+                for (int j = 0; j < TB; ++j) vx[i][j] = load_vec(x[j] + k, A.n_in - k);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+            for (int j = 0; j < TB; ++j) {
+                acc[0][j] = multiply(vg[i], vx[i][j], acc[0][j]);
+                acc[1][j] = multiply(vu[i], vx[i][j], acc[1][j]);
+            }
+    }
+#pragma unroll
+    for (int j = 0; j < TB; ++j) {
+        sums[wave][0][j][l] = acc[0][j];
+        sums[wave][1][j][l] = acc[1][j];
+    }
+    __syncthreads();
+    // wave j sums up rows 16 j on: lane l has row l % 16, columns 4 (l / 16) on
+    if (wave >= TB) return;
+    f32x4 sg = sums[0][0][wave][l], su = sums[0][1][wave][l];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+        sg += sums[w][0][wave][l];
+        su += sums[w][1][wave][l];
+    }
+    const int64_t m = wave * 16 + lm, c = n0 + lg * 4;
+    if (m >= A.rows) return;
+    T *row = static_cast<T *>(A.h) + m * A.ld_h;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        float value, slope;
+        act_both(A.act, sg[r], value, slope);
+        if (c + r < A.n_out) row[c + r] = T(value * su[r]);
+    }
+#endif
+}
+
+template <class T, int BA, int BB, int NA, int NB, Kind KIND, bool ALONG_B> void launch_tiles(ProductArgs a, int64_t n, int64_t m, hipStream_t stream) {
     a.tiles_n = ceil_div(n, KIND == kPlain ? BA : BA / 2);
     a.tiles_m = ceil_div(m, BB);
     if (a.tiles_n * a.tiles_m == 0) return;
-    product<T, BA, BB, NA, NB, KIND><<<dim3(uint32_t(a.tiles_n * a.tiles_m)), 64 * NA * NB, 0, stream>>>(a);
+    product<T, BA, BB, NA, NB, KIND, ALONG_B><<<dim3(uint32_t(a.tiles_n * a.tiles_m)), 64 * NA * NB, 0, stream>>>(a);
 }
-template <class T, Kind KIND> void launch_product(const ProductArgs &a, int64_t n, int64_t m, hipStream_t stream) {
-    if (ceil_div(n, KIND == kPlain ? 256 : 128) * ceil_div(m, 256) >= 2 * kCus) launch_tiles<T, 256, 256, 2, 4, KIND>(a, n, m, stream);
-    else launch_tiles<T, 128, 128, 2, 2, KIND>(a, n, m, stream);
+template <class T, Kind KIND, bool ALONG_B = false> void launch_product(const ProductArgs &a, int64_t n, int64_t m, hipStream_t stream) {
+    if (ceil_div(n, KIND == kPlain ? 256 : 128) * ceil_div(m, 256) >= 2 * kCus) launch_tiles<T, 256, 256, 2, 4, KIND, ALONG_B>(a, n, m, stream);
+    else launch_tiles<T, 128, 128, 2, 2, KIND, ALONG_B>(a, n, m, stream);
 }
 
 int64_t pad64(int64_t n) { return ceil_div(n, 64) * 64; }
@@ -339,6 +462,8 @@ int64_t pad64(int64_t n) { return ceil_div(n, 64) * 64; }
 bool direct(int dtype, const void *p, int64_t ld, int64_t k) {
     return dtype != NDVM_F32 && ld <= kMostFfnWidth && reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && k % 8 == 0;
 }
+
+constexpr int64_t kFewRows = 64;
 
 // Workspace of a call: the parts that it may need, one after the other.
 struct Space {
@@ -357,124 +482,121 @@ struct Space {
 }  // namespace
 
 size_t ffn_bytes(int dtype, int64_t rows, int64_t n_in, int64_t n_out, bool grad) {
+    if (!grad && rows <= kFewRows) return 0;
     // room for copies of x and both weights, whether or not the call's pointers and strides need them
     Space s(nullptr);
     s.take(dtype, rows, pad64(n_in));
-    s.take(dtype, 2 * n_out, pad64(n_in));
-    if (grad) {
-        s.take(dtype, n_in, pad64(rows));
-        s.take(dtype, n_in, 2 * pad64(n_out));
-        s.take(dtype, rows, 2 * pad64(n_out));
-        s.take(dtype, 2 * pad64(n_out), pad64(rows));
-    }
+    s.take(dtype, n_out, pad64(n_in));
+    s.take(dtype, n_out, pad64(n_in));
+    if (grad) s.take(dtype, rows, 2 * pad64(n_out));
     return s.used + 256;
 }
 
 namespace {
 
-template <class T> struct Operands {
+struct Operands {
     Operand x, wg, wu;
     int64_t k;
 };
 // x and the weights as product() reads them: themselves, or padded copies.
-template <class T> Operands<T> operands(const FfnArgs &a, Space &s, hipStream_t stream) {
-    const int64_t pad = pad64(a.n_in);
-    Operands<T> o;
-    const bool as_is = direct(a.dtype, a.x, a.ld_x, a.n_in) && direct(a.dtype, a.wg, a.ld_wg, a.n_in) && direct(a.dtype, a.wu, a.ld_wu, a.n_in);
-    if (as_is) {
+template <class T> Operands operands(const FfnArgs &a, Space &s, hipStream_t stream) {
+    Operands o;
+    if (direct(a.dtype, a.x, a.ld_x, a.n_in) && direct(a.dtype, a.wg, a.ld_wg, a.n_in) && direct(a.dtype, a.wu, a.ld_wu, a.n_in)) {
         o.x = Operand{a.x, a.rows, a.ld_x, 0};
         o.wg = Operand{a.wg, a.n_out, a.ld_wg, 0};
         o.wu = Operand{a.wu, a.n_out, a.ld_wu, 0};
         o.k = a.n_in;
         return o;
     }
-    const auto copy = [&](const void *from, int64_t rows, int64_t ld) {
-        void *to = s.take(a.dtype, rows, pad);
-        launch_pack<T, false>(PackArgs{from, to, rows, a.n_in, ld, pad, pad, s.plane}, stream);
-        return Operand{to, rows, pad, s.plane};
+    PackArgs p{};
+    p.cols = a.n_in;
+    p.pad = o.k = pad64(a.n_in);
+    const auto copy = [&](int i, const void *from, int64_t rows, int64_t ld) {
+        p.from[i] = from;
+        p.to[i] = s.take(a.dtype, rows, p.pad);
+        p.rows[i] = rows;
+        p.ld[i] = ld;
+        p.plane[i] = s.plane;
+        return Operand{p.to[i], rows, p.pad, s.plane};
     };
-    o.x = copy(a.x, a.rows, a.ld_x);
-    o.wg = copy(a.wg, a.n_out, a.ld_wg);
-    o.wu = copy(a.wu, a.n_out, a.ld_wu);
-    o.k = pad;
+    o.x = copy(0, a.x, a.rows, a.ld_x);
+    o.wg = copy(1, a.wg, a.n_out, a.ld_wg);
+    o.wu = copy(2, a.wu, a.n_out, a.ld_wu);
+    const int64_t most = std::max(a.rows, a.n_out) * (p.pad / 8);
+    pack<T><<<dim3(uint32_t(ceil_div(most, 256)), 3), 256, 0, stream>>>(p);
     return o;
 }
 
 char *aligned(void *p) { return reinterpret_cast<char *>(round256(reinterpret_cast<size_t>(p))); }
 
-template <class T> void ffn(const FfnArgs &a, hipStream_t stream) {
-    Space s(aligned(a.ws));
-    const Operands<T> o = operands<T>(a, s, stream);
+ProductArgs gated(const FfnArgs &a, const Operands &o) {
     ProductArgs p{};
     p.a = o.wg;
     p.a2 = o.wu;
     p.b = o.x;
     p.k = o.k;
     p.act = a.act;
-    p.out = a.h;
-    p.ld = a.ld_h;
     p.n = a.n_out;
     p.m = a.rows;
+    return p;
+}
+
+template <class T> void ffn(const FfnArgs &a, hipStream_t stream) {
+    if (a.rows <= kFewRows) {
+        const dim3 grid(uint32_t(ceil_div(a.n_out, 16)));
+        if (a.rows <= 16) few<T, 1><<<grid, 256, 0, stream>>>(a);
+        else if (a.rows <= 32) few<T, 2><<<grid, 256, 0, stream>>>(a);
+        else few<T, 4><<<grid, 256, 0, stream>>>(a);
+        return;
+    }
+    Space s(aligned(a.ws));
+    ProductArgs p = gated(a, operands<T>(a, s, stream));
+    p.out = a.h;
+    p.ld = a.ld_h;
     launch_product<T, kGated>(p, a.n_out, a.rows, stream);
 }
 
 template <class T> void ffn_grad(const FfnArgs &a, hipStream_t stream) {
-    typedef typename Parts<T>::type P;
     Space s(aligned(a.ws));
-    const Operands<T> o = operands<T>(a, s, stream);
-    const int64_t pad_n = pad64(a.n_out), pad_m = pad64(a.rows);
-    ProductArgs p{};
-    p.a = o.wg;
-    p.a2 = o.wu;
-    p.b = o.x;
-    p.k = o.k;
-    p.act = a.act;
-    p.n = a.n_out;
-    p.m = a.rows;
+    const Operands o = operands<T>(a, s, stream);
+    const int64_t pad_n = pad64(a.n_out);
+    ProductArgs p = gated(a, o);
     p.dh = a.dh;
     p.ld_dh = a.ld_dh;
     p.pad_n = pad_n;
-    p.pad_m = pad_m;
     p.p = s.take(a.dtype, a.rows, 2 * pad_n);
     p.ld_p = 2 * pad_n;
     p.plane_p = s.plane;
-    p.pt = s.take(a.dtype, 2 * pad_n, pad_m);
-    p.ld_pt = pad_m;
-    p.plane_pt = s.plane;
-    launch_product<T, kGatedGrad>(p, pad_n, pad_m, stream);
-    if (a.dx) {
-        P *wt = static_cast<P *>(s.take(a.dtype, a.n_in, 2 * pad_n));
-        const int64_t plane = s.plane;
-        launch_pack<T, true>(PackArgs{a.wg, wt, a.n_out, a.n_in, a.ld_wg, 2 * pad_n, pad_n, plane}, stream);
-        launch_pack<T, true>(PackArgs{a.wu, wt + pad_n, a.n_out, a.n_in, a.ld_wu, 2 * pad_n, pad_n, plane}, stream);
+    launch_product<T, kGatedGrad>(p, pad_n, a.rows, stream);
+    const Operand both{p.p, a.rows, 2 * pad_n, p.plane_p};
+    if (a.dx) {     // n: x's columns; the sum: the rows of both weights
         ProductArgs q{};
-        q.a = Operand{wt, a.n_in, 2 * pad_n, plane};
-        q.b = Operand{p.p, a.rows, 2 * pad_n, p.plane_p};
+        q.a = o.wg;
+        q.a2 = o.wu;
+        q.k2 = pad_n;
+        q.b = both;
         q.k = 2 * pad_n;
         q.out = a.dx;
         q.ld = a.ld_dx;
         q.n = a.n_in;
-        q.split = a.rows;
-        q.split2 = q.m2 = a.rows;
+        q.m = q.split = q.split2 = q.m2 = a.rows;
         launch_product<T, kPlain>(q, a.n_in, a.rows, stream);
     }
-    if (a.dwg) {
-        void *xt = s.take(a.dtype, a.n_in, pad_m);
-        const int64_t plane = s.plane;
-        launch_pack<T, true>(PackArgs{a.x, xt, a.rows, a.n_in, a.ld_x, pad_m, pad_m, plane}, stream);
+    if (a.dwg) {    // m: the columns of [dg du]; the sum: rows
         ProductArgs q{};
-        q.a = Operand{xt, a.n_in, pad_m, plane};
-        q.b = Operand{p.pt, 2 * pad_n, pad_m, p.plane_pt};
-        q.k = pad_m;
+        q.a = q.a2 = o.x;
+        q.k = q.k2 = pad64(a.rows);
+        q.b = both;
         q.out = a.dwg;
         q.ld = a.ld_dwg;
         q.out2 = a.dwu;
         q.ld2 = a.ld_dwu;
         q.n = a.n_in;
+        q.m = 2 * pad_n;
         q.split = a.n_out;
         q.split2 = pad_n;
         q.m2 = pad_n + a.n_out;
-        launch_product<T, kPlain>(q, a.n_in, 2 * pad_n, stream);
+        launch_product<T, kPlain, true>(q, a.n_in, 2 * pad_n, stream);
     }
 }
 

@@ -350,7 +350,7 @@ ndvm_status ndvm_gated_ffn(int dtype, int act, const void *x, int64_t rows, int6
         if (!x || !w_gate || !w_up || !h) return bad(who, "null buffer");
         const size_t need = ffn_bytes(dtype, rows, n_in, n_out, false);
         if (workspace_bytes < need) return fail(NDVM_E_NOMEM, who, "workspace too small");
-        if (!workspace) return bad(who, "null workspace");
+        if (need && !workspace) return bad(who, "null workspace");
         FfnArgs a{};
         a.dtype = dtype;
         a.act = act;

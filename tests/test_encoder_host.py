@@ -97,7 +97,8 @@ def test_attention_grad_and_step_refusals():
 
 
 def test_ffn_refusals():
-    ok = dict(dtype=1, act=0, x=FAKE, rows=4, n_in=8, ld_x=8, wg=FAKE, ld_g=8, wu=FAKE, ld_u=8, n_out=16, h=FAKE, ld_h=16, ws=FAKE,
+    # (few rows need no workspace)
+    ok = dict(dtype=1, act=0, x=FAKE, rows=400, n_in=8, ld_x=8, wg=FAKE, ld_g=8, wu=FAKE, ld_u=8, n_out=16, h=FAKE, ld_h=16, ws=FAKE,
               bytes=1 << 30)
 
     def call(**kw):
