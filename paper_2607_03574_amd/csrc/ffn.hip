@@ -17,6 +17,7 @@
 // 8 bits, exactly) and adds up the six products down to 2^-16 of the largest in float: what
 // is left out is below 2^-23 of a term, and bf16 products are 16 times the rate of float ones.
 #include <algorithm>
+#include <type_traits>
 
 #include "ops.h"
 #include "ops_types.h"
@@ -35,7 +36,7 @@ template <> struct Oct<f16> { typedef f16x8 type; };
 __device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ inline f32x4 mfma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-[[maybe_unused]] constexpr int kStep = 64;      // of the sum, per LDS tile
+constexpr int kStep = 32;       // of the sum, per LDS tile
 
 // Parts of a value in an operand: itself, or a float's three bf16.
 template <class T> struct Parts {       // 16-bit types
@@ -119,6 +120,8 @@ struct ProductArgs {
     Operand a, a2, b;           // a2: gated, the second weight; plain, what follows `a` along the sum from k2 on
     int64_t k, k2;              // the sum's length, a multiple of 8 (of 64 where an operand runs along C)
     int64_t tiles_n, tiles_m;
+    int splits;                 // plain: workgroups that share a tile's sum
+    float *part;                // with splits: [splits][m][n], what each sums up
     int act;
     // plain: rows m < split go to out + m * ld, those from split2 to m2 to out2 + (m - split2) * ld2
     void *out, *out2;
@@ -141,32 +144,35 @@ template <class O> __device__ inline O read_transposed(const char *p, const char
 }
 #endif
 
-// BA columns n by BB rows m a workgroup; NA x NB waves.  ALONG_A, ALONG_B: the operand's rows
-// run along C (A[k][n], B[k][m]).
-// An LDS tile of an operand is 64 long along the sum: rows of 64 values, or 64 rows along C,
-// in granules of 16 bytes.  Granule i of row r lies at place i ^ f(r) with f = r % 4 + 4 (r / 8
-// % 2) (twice that for rows along C, which are read two granules at a time), so that the 16
-// rows an instruction reads are in different banks.  The loads go to LDS directly and choose
+// BA columns n by BB rows m a workgroup; NA x NB waves.  ALONG_B: the rows of B run along
+// C (B[k][m]); those of A do in a plain product (A[k][n]).
+// An LDS tile of an operand is 32 long along the sum: rows of 32 values, or 32 rows along C,
+// in granules of 16 bytes.  Along the sum granule i of row r lies at place i ^ (r / 4 % 4), along
+// C at i ^ 2 (r % 4 + r / 8 % 2 * 4) (such rows are read two granules at a time), so that the 16 rows
+// an instruction reads are in different banks.  The loads go to LDS directly and choose
 // their source accordingly; what is out of range reads as 0.
-template <class T, int BA, int BB, int NA, int NB, Kind KIND, bool ALONG_B>
-__global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
+// Four tiles are in LDS: while one is multiplied, from registers, the next is read into
+// registers and two more are on their way, so neither latency is waited for (8192 x 2048 x
+// 8192: 492 us with two tiles of 64 read as they are multiplied).
 #ifdef __HIP_DEVICE_COMPILE__       // the host's pass does not know the types of the loads to LDS
+template <class T, int BA, int BB, int NA, int NB, Kind KIND, bool ALONG_B>
+__device__ __attribute__((always_inline)) inline void product_tile(const ProductArgs &A, int64_t id, char *buffer0, char *buffer1, char *buffer2, char *buffer3) {
     typedef typename Parts<T>::type P;
     typedef typename Oct<P>::type oct;
     constexpr int PARTS = Parts<T>::count, PAIRS = PARTS == 1 ? 1 : 6, W = NA * NB;
     constexpr int WA = BA / NA, WB = BB / NB, TA = WA / 16, TB = WB / 16;
     constexpr bool GATED = KIND != kPlain, ALONG_A = !GATED;
     constexpr int COLS = GATED ? BA / 2 : BA;       // columns of C a tile has
-    // two arrays, so that the compiler sees that loads into one leave reads of the other alone
-    __shared__ __align__(1024) char buffer0[(BA + BB) * kStep * 2], buffer1[(BA + BB) * kStep * 2];
 
     // Tiles in an order that keeps an XCD (workgroup % 8) on neighbouring ones: its share
     // of the tiles, in bands of 8 tile rows.
-    int64_t id = blockIdx.x;
+    const int64_t tiles = A.tiles_n * A.tiles_m;
     {
-        const int64_t total = A.tiles_n * A.tiles_m, x = id % 8, per = total / 8, more = total % 8;
+        const int64_t total = tiles * A.splits, x = id % 8, per = total / 8, more = total % 8;
         id = x * per + min(x, more) + id / 8;
     }
+    const int part = int(id / tiles);
+    id %= tiles;
     const int64_t band = id / (8 * A.tiles_n), in = id % (8 * A.tiles_n);
     const int64_t tall = min(int64_t(8), A.tiles_m - band * 8);
     const int64_t m0 = (band * 8 + in % tall) * BB, n0 = in / tall * COLS;
@@ -177,10 +183,9 @@ __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
     const auto rsrc = [](const void *p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, 0x7fffffff, 0x00020000); };
     const auto f = [](int row) { return row % 4 + row / 8 % 2 * 4; };
 
-    // Wave-wide loads of 1 KB.  Along the sum: 8 rows of 8 granules.
-    constexpr int LA = BA / 8 / W, LB = BB / 8 / W;
-    const int sub = l / 8, granule = (l % 8) ^ f(wave * 8 + sub);      // the same for every load: W is even
-    static_assert(W % 2 == 0, "");
+    // Wave-wide loads of 1 KB.  Along the sum: 16 rows of 4 granules.
+    constexpr int LA = BA / 16 / W, LB = BB / 16 / W;
+    const int sub = l / 4, granule = (l % 4) ^ (sub / 4);
     // Along C: rows of R / 8 granules, 512 / R rows a load.
     const auto along_row = [&](int i, int R) { return (wave + W * i) * (512 / R) + l / (R / 8); };
     const auto along_col = [&](int i, int R) { return ((l % (R / 8)) ^ 2 * f(along_row(i, R))) * 8; };
@@ -191,7 +196,7 @@ __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
             const int col = along_col(i, BA);
             at_a[i] = n0 + col < A.n ? unsigned(along_row(i, BA) * A.a.ld + col) * 2 : kNowhere;
         } else {
-            const int row = (wave + W * i) * 8 + sub;
+            const int row = (wave + W * i) * 16 + sub;
             const bool second = row % WA >= WA / 2;
             const int r = row / WA * (WA / 2) + row % (WA / 2);
             at_a[i] = n0 + r < A.a.rows ? unsigned(r * (second ? A.a2.ld : A.a.ld) + granule * 8) * 2 : kNowhere;
@@ -203,13 +208,16 @@ __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
             const int col = along_col(i, BB);
             at_b[i] = m0 + col < A.m ? unsigned(along_row(i, BB) * A.b.ld + col) * 2 : kNowhere;
         } else {
-            const int row = (wave + W * i) * 8 + sub;
+            const int row = (wave + W * i) * 16 + sub;
             at_b[i] = m0 + row < A.b.rows ? unsigned(row * A.b.ld + granule * 8) * 2 : kNowhere;
         }
     }
-    const int steps = int((A.k + kStep - 1) / kStep), total = steps * PAIRS;
+    const int steps = int((A.k + kStep - 1) / kStep);
+    // this workgroup's share of the sum
+    const int first = int(int64_t(steps) * PAIRS * part / A.splits), total = int(int64_t(steps) * PAIRS * (part + 1) / A.splits);
     // pairs of parts, largest products first
     constexpr int pair_a[6] = {0, 0, 1, 1, 0, 2}, pair_b[6] = {0, 1, 0, 1, 2, 0};
+    // always LA + LB loads a wave (past the end they fetch nothing)
     const auto load = [&](int s, char *to) __attribute__((always_inline)) {
         int64_t k0 = int64_t(s) * kStep;
         int pa = 0, pb = 0;
@@ -220,7 +228,7 @@ __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
             for (int i = 0; i < PAIRS; ++i)
                 if (i == pair) pa = pair_a[i], pb = pair_b[i];
         }
-        const bool some = k0 + granule * 8 < A.k;
+        const bool some = s < total && k0 + granule * 8 < A.k;
         {
             const bool after = ALONG_A && k0 >= A.k2;
             const Operand &o = after ? A.a2 : A.a;
@@ -228,20 +236,22 @@ __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
             const P *base = static_cast<const P *>(o.p) + pa * o.plane + (ALONG_A ? k1 * o.ld + n0 : n0 * o.ld + k0);
             const auto r = rsrc(base);
             const auto r2 = GATED ? rsrc(static_cast<const P *>(A.a2.p) + pa * A.a2.plane + n0 * A.a2.ld + k0) : r;
+            const int rows = s < total ? int(min(o.rows - k1, int64_t(kStep))) : 0;
 #pragma unroll
             for (int i = 0; i < LA; ++i) {
-                const bool second = GATED && (wave + W * i) * 8 % WA >= WA / 2;
-                const bool there = ALONG_A ? k1 + along_row(i, BA) < o.rows : some;
+                const bool second = GATED && (wave + W * i) * 16 % WA >= WA / 2;
+                const bool there = ALONG_A ? along_row(i, BA) < rows : some;
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(second ? r2 : r, (__attribute__((address_space(3))) void *)(to + (wave + W * i) * 1024), 16,
                                                          there ? at_a[i] : kNowhere, 0, 0, 0);
             }
         }
         const P *base = static_cast<const P *>(A.b.p) + pb * A.b.plane + (ALONG_B ? k0 * A.b.ld + m0 : m0 * A.b.ld + k0);
         const auto r = rsrc(base);
+        const int rows = s < total ? int(min(A.b.rows - k0, int64_t(kStep))) : 0;
 #pragma unroll
         for (int i = 0; i < LB; ++i) {
-            const bool there = ALONG_B ? k0 + along_row(i, BB) < A.b.rows : some;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(to + BA * 128 + (wave + W * i) * 1024), 16,
+            const bool there = ALONG_B ? along_row(i, BB) < rows : some;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(to + BA * 64 + (wave + W * i) * 1024), 16,
                                                      there ? at_b[i] : kNowhere, 0, 0, 0);
         }
     };
@@ -252,44 +262,91 @@ __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
 #pragma unroll
         for (int j = 0; j < TB; ++j) acc[i][j] = 0;
     const int tr_row = 8 * lg + lm / 4;     // (+ 4: the same f)
-    // 16 rows and half a step of an operand in the layout of the matrix instructions
-    const auto along = [&](const char *from, int R, int col0, int kk) __attribute__((always_inline)) {
-        const int row = kk * 32 + tr_row, granule = col0 / 8 + lm % 4 / 2;
-        const char *p = from + row * R * 2 + ((granule ^ 2 * f(row)) * 16 + lm % 2 * 8);
+    // 16 rows of an operand in the layout of the matrix instructions
+    const auto along = [&](const char *from, int R, int col0, int place) __attribute__((always_inline)) {
+        const char *p = from + (tr_row * R * 2 + lm % 2 * 8) + (col0 * 2 ^ place);
         return read_transposed<oct>(p, p + 4 * R * 2);
     };
-    const auto summed = [&](const char *from, int row, int kk) __attribute__((always_inline)) {
-        return *reinterpret_cast<const oct *>(from + row * 128 + ((kk * 4 + lg) ^ f(row)) * 16);
+    const auto summed = [&](const char *from, int row) __attribute__((always_inline)) {
+        return *reinterpret_cast<const oct *>(from + row * 64 + (lg ^ row / 4 % 4) * 16);
     };
-    const auto step = [&](int s, const char *from, char *next) __attribute__((always_inline)) {
-        // every wave's loads of this buffer have landed, and none reads the other one
-        __builtin_amdgcn_s_waitcnt(0);
-        __syncthreads();
-        if (s + 1 < total) load(s + 1, next);
+    // One set of A's registers: a tile's is free for the next step's once its row of products is
+    // under way.  Two of B's.
+    oct fa[TA], fb[2][TB];
+    // where a lane's granule of the first columns lies; kept from being worked out for all columns
+    // ahead of the loop, which has no registers for that
+    const auto first_place = [&]() __attribute__((always_inline)) {
+        int place = (lm % 4 / 2 ^ 2 * f(tr_row)) * 16;
+        asm volatile("" : "+v"(place));
+        return place;
+    };
+    const auto read_a = [&](const char *from, int i, int place) __attribute__((always_inline)) {
+        // gated: rows of a pair of tiles in the order that leaves a lane with eight columns side by side
+        if constexpr (ALONG_A) fa[i] = along(from, BA, wa * WA + i * 16, place);
+        else fa[i] = summed(from, wa * WA + i / 2 * 32 + lm / 4 * 8 + i % 2 * 4 + lm % 4);
+    };
+    const auto read_b = [&](const char *from, oct &to, int j, int place) __attribute__((always_inline)) {
+        if constexpr (ALONG_B) to = along(from + BA * 64, BB, wb * WB + j * 16, place);
+        else to = summed(from + BA * 64, wb * WB + j * 16 + lm);
+    };
+    constexpr int LOADS = LA + LB;
+    const auto wait = [&](auto loads) __attribute__((always_inline)) {
+        // this wave's older loads have landed and its reads are done; after the barrier everybody's
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);      // multiplications stay on their side
+        __builtin_amdgcn_s_waitcnt(0x0070 | decltype(loads)::value);
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" ::: "memory");
+    };
+    using std::integral_constant;
+    // step s: its operands are in registers (B's in set `now`); the next tile is in `next`, `to`
+    // takes the third after
+    const auto step = [&](int s, const char *next, char *to, auto now) __attribute__((always_inline)) {
+        constexpr int n = decltype(now)::value;
+        wait(integral_constant<int, LOADS>());
+        load(s + 3, to);
+        const int place = first_place();
+        static_assert(TB <= TA, "");
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            oct fa[TA], fb[TB];
+        for (int i = 0; i < TA; ++i) {
 #pragma unroll
-            for (int i = 0; i < TA; ++i) {
-                // gated: rows of a pair of tiles in the order that leaves a lane with eight columns side by side
-                if constexpr (ALONG_A) fa[i] = along(from, BA, wa * WA + i * 16, kk);
-                else fa[i] = summed(from, wa * WA + i / 2 * 32 + lm / 4 * 8 + i % 2 * 4 + lm % 4, kk);
-            }
+            for (int j = 0; j < TB; ++j) acc[i][j] = mfma(fa[i], fb[n][j], acc[i][j]);
+            if (i < TB) read_b(next, fb[1 - n][i], i, place);
+            read_a(next, i, place);
+        }
+        // loads and reads among the multiplications, none of which waits for them
 #pragma unroll
-            for (int j = 0; j < TB; ++j) {
-                if constexpr (ALONG_B) fb[j] = along(from + BA * 128, BB, wb * WB + j * 16, kk);
-                else fb[j] = summed(from + BA * 128, wb * WB + j * 16 + lm, kk);
-            }
+        for (int i = 0; i < TB; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, TB, 0);
+            __builtin_amdgcn_sched_group_barrier(0x020, (LOADS + TB - 1) / TB, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, (ALONG_A ? 2 : 1) + (ALONG_B ? 2 : 1), 0);
+        }
 #pragma unroll
-            for (int i = 0; i < TA; ++i)
-#pragma unroll
-                for (int j = 0; j < TB; ++j) acc[i][j] = mfma(fa[i], fb[j], acc[i][j]);
+        for (int i = TB; i < TA; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, TB, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, ALONG_A ? 2 : 1, 0);
         }
     };
-    if (total > 0) load(0, buffer0);
-    for (int s = 0; s < total; s += 2) {
-        step(s, buffer0, buffer1);
-        if (s + 1 < total) step(s + 1, buffer1, buffer0);
+    if (first < total) {
+        load(first, buffer0);
+        load(first + 1, buffer1);
+        load(first + 2, buffer2);
+        wait(integral_constant<int, 2 * LOADS>());
+        const int place = first_place();
+#pragma unroll
+        for (int i = 0; i < TA; ++i) {
+            if (i < TB) read_b(buffer0, fb[0][i], i, place);
+            read_a(buffer0, i, place);
+        }
+        const integral_constant<int, 0> even;
+        const integral_constant<int, 1> odd;
+        for (int s = first; s < total; s += 4) {    // steps past the end add zeros
+            step(s, buffer1, buffer3, even);
+            step(s + 1, buffer2, buffer0, odd);
+            step(s + 2, buffer3, buffer1, even);
+            step(s + 3, buffer0, buffer2, odd);
+        }
     }
 
     // lane l, register r of tile (i, j): row m = l % 16 of j; column 4 (l / 16) + r of i, or,
@@ -299,6 +356,20 @@ __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
         const int64_t m = m0 + wb * WB + j * 16 + lm;
         if constexpr (KIND == kPlain) {
             typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+            if (A.splits > 1) {
+                typedef float four_f __attribute__((ext_vector_type(4), aligned(4)));
+                if (m >= A.m) continue;
+                float *row = A.part + (int64_t(part) * A.m + m) * A.n;
+#pragma unroll
+                for (int i = 0; i < TA; ++i) {
+                    const int64_t n = n0 + wa * WA + i * 16 + lg * 4;
+                    if (n + 4 <= A.n) *reinterpret_cast<four_f *>(row + n) = acc[i][j];
+                    else
+                        for (int r = 0; r < 4; ++r)
+                            if (n + r < A.n) row[n + r] = acc[i][j][r];
+                }
+                continue;
+            }
             T *row = nullptr;
             if (m < A.split) row = static_cast<T *>(A.out) + m * A.ld;
             else if (m >= A.split2 && m < A.m2) row = static_cast<T *>(A.out2) + (m - A.split2) * A.ld2;
@@ -368,7 +439,56 @@ __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
             }
         }
     }
+}
 #endif
+
+template <class T, int BA, int BB, int NA, int NB, Kind KIND>
+__global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
+#ifdef __HIP_DEVICE_COMPILE__
+    // separate arrays, so that the compiler sees that loads into one leave reads of the others alone
+    constexpr int SIZE = (BA + BB) * kStep * 2;
+    __shared__ __align__(1024) char buffer0[SIZE], buffer1[SIZE], buffer2[SIZE], buffer3[SIZE];
+    product_tile<T, BA, BB, NA, NB, KIND, false>(A, blockIdx.x, buffer0, buffer1, buffer2, buffer3);
+#endif
+}
+
+// Two plain products in one launch: dx = [dg du] [Wg; Wu], and [dWg; dWu] = [dg du]^T x.
+template <class T, int BA, int BB, int NA, int NB>
+__global__ void __launch_bounds__(64 * NA * NB) product_pair(ProductArgs A, ProductArgs B) {
+#ifdef __HIP_DEVICE_COMPILE__
+    constexpr int SIZE = (BA + BB) * kStep * 2;
+    __shared__ __align__(1024) char buffer0[SIZE], buffer1[SIZE], buffer2[SIZE], buffer3[SIZE];
+    const int64_t of_a = A.tiles_n * A.tiles_m * A.splits;
+    if (int64_t(blockIdx.x) < of_a) product_tile<T, BA, BB, NA, NB, kPlain, false>(A, blockIdx.x, buffer0, buffer1, buffer2, buffer3);
+    else product_tile<T, BA, BB, NA, NB, kPlain, true>(B, blockIdx.x - of_a, buffer0, buffer1, buffer2, buffer3);
+#endif
+}
+
+// The sums of a plain product that was split, added up in order.  A thread four columns.
+template <class T> __global__ void __launch_bounds__(256) fold_splits(ProductArgs A) {
+    typedef float four_f __attribute__((ext_vector_type(4), aligned(4)));
+    const int64_t per = (A.n + 3) / 4, at = int64_t(blockIdx.x) * 256 + threadIdx.x, m = at / per, n = at % per * 4;
+    if (m >= A.m) return;
+    T *row = nullptr;
+    if (m < A.split) row = static_cast<T *>(A.out) + m * A.ld;
+    else if (m >= A.split2 && m < A.m2) row = static_cast<T *>(A.out2) + (m - A.split2) * A.ld2;
+    if (!row) return;
+    const float *p = A.part + m * A.n + n;
+    if (n + 4 <= A.n) {
+        f32x4 sum = *reinterpret_cast<const four_f *>(p);
+        for (int i = 1; i < A.splits; ++i) sum += *reinterpret_cast<const four_f *>(p + i * A.m * A.n);
+        typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+        four v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[r] = T(sum[r]);
+        *reinterpret_cast<four *>(row + n) = v;
+    } else {
+        for (int r = 0; n + r < A.n; ++r) {
+            float sum = p[r];
+            for (int i = 1; i < A.splits; ++i) sum += p[i * A.m * A.n + r];
+            row[n + r] = T(sum);
+        }
+    }
 }
 
 // ---- few rows: the weights are read once, straight into registers, by workgroups of 16
@@ -445,15 +565,48 @@ template <class T, int TB> __global__ void __launch_bounds__(256) few(FfnArgs A)
 #endif
 }
 
-template <class T, int BA, int BB, int NA, int NB, Kind KIND, bool ALONG_B> void launch_tiles(ProductArgs a, int64_t n, int64_t m, hipStream_t stream) {
-    a.tiles_n = ceil_div(n, KIND == kPlain ? BA : BA / 2);
+template <class T, int BA, int BB, int NA, int NB, Kind KIND> void launch_tiles(ProductArgs a, int64_t n, int64_t m, hipStream_t stream) {
+    a.tiles_n = ceil_div(n, BA / 2);
     a.tiles_m = ceil_div(m, BB);
+    a.splits = 1;
     if (a.tiles_n * a.tiles_m == 0) return;
-    product<T, BA, BB, NA, NB, KIND, ALONG_B><<<dim3(uint32_t(a.tiles_n * a.tiles_m)), 64 * NA * NB, 0, stream>>>(a);
+    product<T, BA, BB, NA, NB, KIND><<<dim3(uint32_t(a.tiles_n * a.tiles_m)), 64 * NA * NB, 0, stream>>>(a);
 }
-template <class T, Kind KIND, bool ALONG_B = false> void launch_product(const ProductArgs &a, int64_t n, int64_t m, hipStream_t stream) {
-    if (ceil_div(n, KIND == kPlain ? 256 : 128) * ceil_div(m, 256) >= 2 * kCus) launch_tiles<T, 256, 256, 2, 4, KIND, ALONG_B>(a, n, m, stream);
-    else launch_tiles<T, 128, 128, 2, 2, KIND, ALONG_B>(a, n, m, stream);
+template <class T, Kind KIND> void launch_product(const ProductArgs &a, int64_t n, int64_t m, hipStream_t stream) {
+    if (ceil_div(n, 128) * ceil_div(m, 256) >= 2 * kCus) launch_tiles<T, 256, 256, 2, 4, KIND>(a, n, m, stream);
+    else launch_tiles<T, 128, 128, 2, 2, KIND>(a, n, m, stream);
+}
+
+// How the gradient's two plain products are cut: tiles of `tile` squared, each one's sum over so
+// many workgroups.  Both have the same number of steps in all.  Unless there are tiles for two
+// workgroups a compute unit, sums are cut into pieces of about a compute unit's share, of
+// at least 16 steps, but not so many that the pieces' sums cost more traffic than they save.
+struct Pieces {
+    int64_t tile, dx, dw;
+};
+Pieces pieces(int dtype, int64_t rows, int64_t n_in, int64_t n_out) {
+    const int64_t pairs = dtype == NDVM_F32 ? 6 : 1, width = 2 * ceil_div(n_out, 64) * 64;
+    const int64_t steps_dx = width / kStep * pairs, steps_dw = ceil_div(rows, 64) * 2 * pairs;
+    const auto tiles_dx = [&](int64_t t) { return ceil_div(n_in, t) * ceil_div(rows, t); };
+    const auto tiles_dw = [&](int64_t t) { return ceil_div(n_in, t) * ceil_div(width, t); };
+    const auto work = [&](int64_t t) { return tiles_dx(t) * steps_dx + tiles_dw(t) * steps_dw; };
+    Pieces c{work(256) >= 32 * kCus ? 256 : 128, 1, 1};
+    if (tiles_dx(c.tile) + tiles_dw(c.tile) >= 4 * kCus) return c;
+    const int64_t share = std::max<int64_t>(16, work(c.tile) / kCus);
+    const auto cut = [&](int64_t steps) { return std::max<int64_t>(1, std::min<int64_t>(8, (steps + share / 2) / share)); };
+    c.dx = cut(steps_dx);
+    c.dw = cut(steps_dw);
+    return c;
+}
+template <class T, int BT, int NA, int NB> void launch_pair(ProductArgs a, ProductArgs b, hipStream_t stream) {
+    for (ProductArgs *q : {&a, &b}) {
+        q->tiles_n = ceil_div(q->n, BT);
+        q->tiles_m = ceil_div(q->m, BT);
+    }
+    const int64_t wgs = a.tiles_n * a.tiles_m * a.splits + b.tiles_n * b.tiles_m * b.splits;
+    if (wgs) product_pair<T, BT, BT, NA, NB><<<dim3(uint32_t(wgs)), 64 * NA * NB, 0, stream>>>(a, b);
+    for (const ProductArgs *q : {&a, &b})
+        if (q->splits > 1 && q->m && q->n) fold_splits<T><<<dim3(uint32_t(ceil_div(ceil_div(q->n, 4) * q->m, 256))), 256, 0, stream>>>(*q);
 }
 
 int64_t pad64(int64_t n) { return ceil_div(n, 64) * 64; }
@@ -477,6 +630,11 @@ struct Space {
         used += round256(size_t(plane) * (dtype == NDVM_F32 ? 6 : 2));
         return p;
     }
+    float *take_floats(int64_t n) {
+        void *p = base ? base + used : nullptr;
+        used += round256(size_t(n) * 4);
+        return static_cast<float *>(p);
+    }
 };
 
 }  // namespace
@@ -488,7 +646,12 @@ size_t ffn_bytes(int dtype, int64_t rows, int64_t n_in, int64_t n_out, bool grad
     s.take(dtype, rows, pad64(n_in));
     s.take(dtype, n_out, pad64(n_in));
     s.take(dtype, n_out, pad64(n_in));
-    if (grad) s.take(dtype, rows, 2 * pad64(n_out));
+    if (grad) {
+        s.take(dtype, rows, 2 * pad64(n_out));
+        const Pieces c = pieces(dtype, rows, n_in, n_out);
+        if (c.dx > 1) s.take_floats(c.dx * rows * n_in);
+        if (c.dw > 1) s.take_floats(c.dw * 2 * pad64(n_out) * n_in);
+    }
     return s.used + 256;
 }
 
@@ -569,35 +732,40 @@ template <class T> void ffn_grad(const FfnArgs &a, hipStream_t stream) {
     p.plane_p = s.plane;
     launch_product<T, kGatedGrad>(p, pad_n, a.rows, stream);
     const Operand both{p.p, a.rows, 2 * pad_n, p.plane_p};
+    const Pieces c = pieces(a.dtype, a.rows, a.n_in, a.n_out);
+    ProductArgs dx{}, dw{};
+    dx.splits = dw.splits = 1;
     if (a.dx) {     // n: x's columns; the sum: the rows of both weights
-        ProductArgs q{};
-        q.a = o.wg;
-        q.a2 = o.wu;
-        q.k2 = pad_n;
-        q.b = both;
-        q.k = 2 * pad_n;
-        q.out = a.dx;
-        q.ld = a.ld_dx;
-        q.n = a.n_in;
-        q.m = q.split = q.split2 = q.m2 = a.rows;
-        launch_product<T, kPlain>(q, a.n_in, a.rows, stream);
+        dx.a = o.wg;
+        dx.a2 = o.wu;
+        dx.k2 = pad_n;
+        dx.b = both;
+        dx.k = 2 * pad_n;
+        dx.out = a.dx;
+        dx.ld = a.ld_dx;
+        dx.n = a.n_in;
+        dx.m = dx.split = dx.split2 = dx.m2 = a.rows;
+        dx.splits = int(c.dx);
+        if (c.dx > 1) dx.part = s.take_floats(c.dx * a.rows * a.n_in);
     }
     if (a.dwg) {    // m: the columns of [dg du]; the sum: rows
-        ProductArgs q{};
-        q.a = q.a2 = o.x;
-        q.k = q.k2 = pad64(a.rows);
-        q.b = both;
-        q.out = a.dwg;
-        q.ld = a.ld_dwg;
-        q.out2 = a.dwu;
-        q.ld2 = a.ld_dwu;
-        q.n = a.n_in;
-        q.m = 2 * pad_n;
-        q.split = a.n_out;
-        q.split2 = pad_n;
-        q.m2 = pad_n + a.n_out;
-        launch_product<T, kPlain, true>(q, a.n_in, 2 * pad_n, stream);
+        dw.a = dw.a2 = o.x;
+        dw.k = dw.k2 = pad64(a.rows);
+        dw.b = both;
+        dw.out = a.dwg;
+        dw.ld = a.ld_dwg;
+        dw.out2 = a.dwu;
+        dw.ld2 = a.ld_dwu;
+        dw.n = a.n_in;
+        dw.m = 2 * pad_n;
+        dw.split = a.n_out;
+        dw.split2 = pad_n;
+        dw.m2 = pad_n + a.n_out;
+        dw.splits = int(c.dw);
+        if (c.dw > 1) dw.part = s.take_floats(c.dw * dw.m * a.n_in);
     }
+    if (c.tile == 256) launch_pair<T, 256, 2, 4>(dx, dw, stream);
+    else launch_pair<T, 128, 2, 2>(dx, dw, stream);
 }
 
 }  // namespace
