@@ -60,22 +60,30 @@ template <> struct Parts<float> {
 };
 
 // ---- activations: value and derivative
-__device__ inline void act_both(int act, float g, float &f, float &d) {
-    if (act == NDVM_ACT_SILU) {
-        const float s = 1.0f / (1.0f + __expf(-g));
+template <int ACT> __device__ inline void act_both(float g, float &f, float &d) {
+    if constexpr (ACT == NDVM_ACT_SILU) {
+        const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-g));
         f = g * s;
         d = s * (1.0f + g * (1.0f - s));
-    } else if (act == NDVM_ACT_GELU) {
+    } else if constexpr (ACT == NDVM_ACT_GELU) {
         const float p = 0.5f * (1.0f + erff(g * 0.70710678118654752f));
         f = g * p;
         d = p + g * 0.39894228040143268f * __expf(-0.5f * g * g);
-    } else if (act == NDVM_ACT_SIGMOID) {
-        f = 1.0f / (1.0f + __expf(-g));
+    } else if constexpr (ACT == NDVM_ACT_SIGMOID) {
+        f = __builtin_amdgcn_rcpf(1.0f + __expf(-g));
         d = f * (1.0f - f);
     } else {
         f = g > 0.0f ? g : g != g ? g : 0.0f;
         d = g > 0.0f ? 1.0f : 0.0f;
     }
+}
+// Calls f with the activation as a constant: the branch is taken once, not for every value.
+template <class F> __device__ __attribute__((always_inline)) inline void with_act(int act, F f) {
+    using std::integral_constant;
+    if (act == NDVM_ACT_SILU) f(integral_constant<int, NDVM_ACT_SILU>());
+    else if (act == NDVM_ACT_GELU) f(integral_constant<int, NDVM_ACT_GELU>());
+    else if (act == NDVM_ACT_SIGMOID) f(integral_constant<int, NDVM_ACT_SIGMOID>());
+    else f(integral_constant<int, NDVM_ACT_RELU>());
 }
 
 // ---- operands laid out: a copy in parts, rows of `pad` values (zeros beyond the source's)
@@ -152,7 +160,7 @@ template <class O> __device__ inline O read_transposed(const char *p, const char
 // an instruction reads are in different banks.  The loads go to LDS directly and choose
 // their source accordingly; what is out of range reads as 0.
 // Four tiles are in LDS: while one is multiplied, from registers, the next is read into
-// registers and two more are on their way, so neither latency is waited for (8192 x 2048 x
+// registers and three more are on their way, so neither latency is waited for (8192 x 2048 x
 // 8192: 492 us with two tiles of 64 read as they are multiplied).
 #ifdef __HIP_DEVICE_COMPILE__       // the host's pass does not know the types of the loads to LDS
 template <class T, int BA, int BB, int NA, int NB, Kind KIND, bool ALONG_B>
@@ -187,14 +195,16 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
     constexpr int LA = BA / 16 / W, LB = BB / 16 / W;
     const int sub = l / 4, granule = (l % 4) ^ (sub / 4);
     // Along C: rows of R / 8 granules, 512 / R rows a load.
-    const auto along_row = [&](int i, int R) { return (wave + W * i) * (512 / R) + l / (R / 8); };
-    const auto along_col = [&](int i, int R) { return ((l % (R / 8)) ^ 2 * f(along_row(i, R))) * 8; };
+    // A load's rows are 512 W / R after those of the load before, which is a multiple of 16: the same f.
+    const auto along_row = [&](int R) { return wave * (512 / R) + l / (R / 8); };
+    const auto along_col = [&](int R) { return ((l % (R / 8)) ^ 2 * f(along_row(R))) * 8; };
+    static_assert(512 * W / BA % 16 == 0 && 512 * W / BB % 16 == 0, "");
     unsigned at_a[LA], at_b[LB];
 #pragma unroll
     for (int i = 0; i < LA; ++i) {
         if constexpr (ALONG_A) {
-            const int col = along_col(i, BA);
-            at_a[i] = n0 + col < A.n ? unsigned(along_row(i, BA) * A.a.ld + col) * 2 : kNowhere;
+            const int col = along_col(BA);
+            at_a[i] = n0 + col < A.n ? unsigned(along_row(BA) * A.a.ld + col) * 2 : kNowhere;
         } else {
             const int row = (wave + W * i) * 16 + sub;
             const bool second = row % WA >= WA / 2;
@@ -205,8 +215,8 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
 #pragma unroll
     for (int i = 0; i < LB; ++i) {
         if constexpr (ALONG_B) {
-            const int col = along_col(i, BB);
-            at_b[i] = m0 + col < A.m ? unsigned(along_row(i, BB) * A.b.ld + col) * 2 : kNowhere;
+            const int col = along_col(BB);
+            at_b[i] = m0 + col < A.m ? unsigned(along_row(BB) * A.b.ld + col) * 2 : kNowhere;
         } else {
             const int row = (wave + W * i) * 16 + sub;
             at_b[i] = m0 + row < A.b.rows ? unsigned(row * A.b.ld + granule * 8) * 2 : kNowhere;
@@ -240,9 +250,10 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
 #pragma unroll
             for (int i = 0; i < LA; ++i) {
                 const bool second = GATED && (wave + W * i) * 16 % WA >= WA / 2;
-                const bool there = ALONG_A ? along_row(i, BA) < rows : some;
+                constexpr int apart = 512 * W / BA;
+                const bool there = ALONG_A ? along_row(BA) < rows - apart * i : some;
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(second ? r2 : r, (__attribute__((address_space(3))) void *)(to + (wave + W * i) * 1024), 16,
-                                                         there ? at_a[i] : kNowhere, 0, 0, 0);
+                                                         there ? at_a[i] : kNowhere, ALONG_A ? unsigned(apart * i * o.ld) * 2 : 0, 0, 0);
             }
         }
         const P *base = static_cast<const P *>(A.b.p) + pb * A.b.plane + (ALONG_B ? k0 * A.b.ld + m0 : m0 * A.b.ld + k0);
@@ -250,9 +261,10 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
         const int rows = s < total ? int(min(A.b.rows - k0, int64_t(kStep))) : 0;
 #pragma unroll
         for (int i = 0; i < LB; ++i) {
-            const bool there = ALONG_B ? along_row(i, BB) < rows : some;
+            constexpr int apart = 512 * W / BB;
+            const bool there = ALONG_B ? along_row(BB) < rows - apart * i : some;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(to + BA * 64 + (wave + W * i) * 1024), 16,
-                                                     there ? at_b[i] : kNowhere, 0, 0, 0);
+                                                     there ? at_b[i] : kNowhere, ALONG_B ? unsigned(apart * i * A.b.ld) * 2 : 0, 0, 0);
         }
     };
 
@@ -262,34 +274,45 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
 #pragma unroll
         for (int j = 0; j < TB; ++j) acc[i][j] = 0;
     const int tr_row = 8 * lg + lm / 4;     // (+ 4: the same f)
-    // 16 rows of an operand in the layout of the matrix instructions
-    const auto along = [&](const char *from, int R, int col0, int place) __attribute__((always_inline)) {
-        const char *p = from + (tr_row * R * 2 + lm % 2 * 8) + (col0 * 2 ^ place);
-        return read_transposed<oct>(p, p + 4 * R * 2);
-    };
-    const auto summed = [&](const char *from, int row) __attribute__((always_inline)) {
-        return *reinterpret_cast<const oct *>(from + row * 64 + (lg ^ row / 4 % 4) * 16);
-    };
     // One set of A's registers: a tile's is free for the next step's once its row of products is
     // under way.  Two of B's.
     oct fa[TA], fb[2][TB];
-    // where a lane's granule of the first columns lies; kept from being worked out for all columns
-    // ahead of the loop, which has no registers for that
-    const auto first_place = [&]() __attribute__((always_inline)) {
-        int place = (lm % 4 / 2 ^ 2 * f(tr_row)) * 16;
-        asm volatile("" : "+v"(place));
-        return place;
+    // Where a lane's values of the first 16 rows of an operand's tile lie: along the sum, in tiles of
+    // even and of odd number (gated: rows of a pair of tiles are in the order that leaves a lane with eight
+    // columns side by side); along C, the row and the granule's place, to be crossed with the columns'.
+    // Kept from the compiler's sight, or it works out the address of every read of every buffer
+    // ahead of the loop, which has no registers for them.
+    struct Places {
+        int a0, a1, b;
     };
-    const auto read_a = [&](const char *from, int i, int place) __attribute__((always_inline)) {
-        // gated: rows of a pair of tiles in the order that leaves a lane with eight columns side by side
-        if constexpr (ALONG_A) fa[i] = along(from, BA, wa * WA + i * 16, place);
-        else fa[i] = summed(from, wa * WA + i / 2 * 32 + lm / 4 * 8 + i % 2 * 4 + lm % 4);
+    const auto places = [&]() __attribute__((always_inline)) {
+        const int row_a = lm / 4 * 8 + lm % 4, row_b = lm, crossed = (lm % 4 / 2 ^ 2 * f(tr_row)) * 16;
+        Places p;
+        if constexpr (ALONG_A) p = Places{crossed, tr_row * BA * 2 + lm % 2 * 8, crossed};
+        else p = Places{(wa * WA + row_a) * 64 + (lg ^ row_a / 4 % 4) * 16, (wa * WA + row_a + 4) * 64 + (lg ^ (row_a + 4) / 4 % 4) * 16, 0};
+        if constexpr (ALONG_B) p.b = tr_row * BB * 2 + lm % 2 * 8;
+        else p.b = (wb * WB + row_b) * 64 + (lg ^ row_b / 4 % 4) * 16;
+        asm volatile("" : "+v"(p.a0), "+v"(p.a1), "+v"(p.b));
+        return p;
     };
-    const auto read_b = [&](const char *from, oct &to, int j, int place) __attribute__((always_inline)) {
-        if constexpr (ALONG_B) to = along(from + BA * 64, BB, wb * WB + j * 16, place);
-        else to = summed(from + BA * 64, wb * WB + j * 16 + lm);
+    const auto read_a = [&](const char *from, int i, const Places &p) __attribute__((always_inline)) {
+        if constexpr (ALONG_A) {
+            const char *at = from + p.a1 + ((wa * WA + i * 16) * 2 ^ p.a0);
+            fa[i] = read_transposed<oct>(at, at + 4 * BA * 2);
+        } else {
+            fa[i] = *reinterpret_cast<const oct *>(from + (i % 2 ? p.a1 : p.a0) + i / 2 * (32 * 64));
+        }
+    };
+    const auto read_b = [&](const char *from, oct &to, int j, const Places &p) __attribute__((always_inline)) {
+        if constexpr (ALONG_B) {
+            const char *at = from + BA * 64 + p.b + ((wb * WB + j * 16) * 2 ^ p.a0);
+            to = read_transposed<oct>(at, at + 4 * BB * 2);
+        } else {
+            to = *reinterpret_cast<const oct *>(from + BA * 64 + p.b + j * (16 * 64));
+        }
     };
     constexpr int LOADS = LA + LB;
+    static_assert(3 * LOADS < 16, "");
     const auto wait = [&](auto loads) __attribute__((always_inline)) {
         // this wave's older loads have landed and its reads are done; after the barrier everybody's
         asm volatile("" ::: "memory");
@@ -300,13 +323,13 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
         asm volatile("" ::: "memory");
     };
     using std::integral_constant;
-    // step s: its operands are in registers (B's in set `now`); the next tile is in `next`, `to`
-    // takes the third after
+    // step s: its operands are in registers (B's in set `now`); the next tile is in `next`; the tile
+    // four on takes its place, `to`
     const auto step = [&](int s, const char *next, char *to, auto now) __attribute__((always_inline)) {
         constexpr int n = decltype(now)::value;
-        wait(integral_constant<int, LOADS>());
-        load(s + 3, to);
-        const int place = first_place();
+        wait(integral_constant<int, 2 * LOADS>());
+        load(s + 4, to);
+        const Places place = places();
         static_assert(TB <= TA, "");
 #pragma unroll
         for (int i = 0; i < TA; ++i) {
@@ -332,8 +355,9 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
         load(first, buffer0);
         load(first + 1, buffer1);
         load(first + 2, buffer2);
-        wait(integral_constant<int, 2 * LOADS>());
-        const int place = first_place();
+        load(first + 3, buffer3);
+        wait(integral_constant<int, 3 * LOADS>());
+        const Places place = places();
 #pragma unroll
         for (int i = 0; i < TA; ++i) {
             if (i < TB) read_b(buffer0, fb[0][i], i, place);
@@ -342,10 +366,10 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
         const integral_constant<int, 0> even;
         const integral_constant<int, 1> odd;
         for (int s = first; s < total; s += 4) {    // steps past the end add zeros
-            step(s, buffer1, buffer3, even);
-            step(s + 1, buffer2, buffer0, odd);
-            step(s + 2, buffer3, buffer1, even);
-            step(s + 3, buffer0, buffer2, odd);
+            step(s, buffer1, buffer0, even);
+            step(s + 1, buffer2, buffer1, odd);
+            step(s + 2, buffer3, buffer2, even);
+            step(s + 3, buffer0, buffer3, odd);
         }
     }
 
@@ -385,10 +409,16 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
                     for (int r = 0; r < 4; ++r)
                         if (n + r < A.n) row[n + r] = v[r];
             }
-        } else {
+        }
+    }
+    if constexpr (GATED) with_act(A.act, [&](auto act) __attribute__((always_inline)) {
+        constexpr int ACT = decltype(act)::value;
+        typedef T eight __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+        typedef P eight_p __attribute__((ext_vector_type(8)));
+#pragma unroll
+        for (int j = 0; j < TB; ++j) {
+            const int64_t m = m0 + wb * WB + j * 16 + lm;
             if (m >= A.m) continue;
-            typedef T eight __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-            typedef P eight_p __attribute__((ext_vector_type(8)));
 #pragma unroll
             for (int i = 0; i < TA / 2; i += 2) {
                 const int64_t n = n0 + wa * (WA / 2) + i * 16 + lg * 8;
@@ -398,7 +428,7 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
 #pragma unroll
                     for (int r = 0; r < 8; ++r) {
                         float value, slope;
-                        act_both(A.act, acc[i + r / 4][j][r % 4], value, slope);
+                        act_both<ACT>(acc[i + r / 4][j][r % 4], value, slope);
                         v[r] = T(value * acc[i + r / 4 + TA / 2][j][r % 4]);
                     }
                     if (n + 8 <= A.n) *reinterpret_cast<eight *>(row + n) = v;
@@ -417,7 +447,7 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
 #pragma unroll
                     for (int r = 0; r < 8; ++r) {
                         float value, slope;
-                        act_both(A.act, acc[i + r / 4][j][r % 4], value, slope);
+                        act_both<ACT>(acc[i + r / 4][j][r % 4], value, slope);
                         P pg[PARTS], pu[PARTS];
                         // what lies beyond the operands is 0, whatever act does there
                         const bool there = n + r < A.n;
@@ -438,7 +468,7 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
                 }
             }
         }
-    }
+    });
 }
 #endif
 
@@ -556,12 +586,14 @@ template <class T, int TB> __global__ void __launch_bounds__(256) few(FfnArgs A)
     const int64_t m = wave * 16 + lm, c = n0 + lg * 4;
     if (m >= A.rows) return;
     T *row = static_cast<T *>(A.h) + m * A.ld_h;
+    with_act(A.act, [&](auto act) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        float value, slope;
-        act_both(A.act, sg[r], value, slope);
-        if (c + r < A.n_out) row[c + r] = T(value * su[r]);
-    }
+        for (int r = 0; r < 4; ++r) {
+            float value, slope;
+            act_both<decltype(act)::value>(sg[r], value, slope);
+            if (c + r < A.n_out) row[c + r] = T(value * su[r]);
+        }
+    });
 #endif
 }
 
