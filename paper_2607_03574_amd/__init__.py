@@ -477,46 +477,71 @@ def adam_step(params, grad_in, m, v, t: int, lr: float, beta1: float = 0.9, beta
 
 
 # ---------------------------------------------------------------- encoder operators
-def _op_type(*tensors):
-    """dtype code of the (name, tensor) pairs, which have to be of one supported type on one device."""
-    import torch
-    codes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-    first = tensors[0][1]
-    for name, t in tensors:
-        if t is None:
-            continue
-        if not isinstance(t, torch.Tensor) or t.dtype not in codes or not t.is_cuda:
-            raise TypeError(f"{name} must be a float32, bfloat16 or float16 CUDA/ROCm tensor")
-        if t.dtype != first.dtype or t.device != first.device:
-            raise TypeError(f"{name} must have the type and device of {tensors[0][0]}")
-    return codes[first.dtype]
+# These are called for single tokens too, whose kernels take a few microseconds:
+# the checks below are written to cost little when they pass.
+class _Torch:
+    """torch, the type codes, and the current stream's handle, looked up once."""
+
+    def __init__(self):
+        import torch
+        self.torch = torch
+        self.codes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+        self.f32, self.u8, self.i64 = torch.float32, torch.uint8, torch.int64
+        self.Tensor = torch.Tensor
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        self.raw_stream = raw or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _of(t, name, dtype, shape, device):
-    """A contiguous tensor of that type and shape, or None."""
-    import torch
-    if t is None:
+_torch_once = None
+
+
+def _t():
+    global _torch_once
+    if _torch_once is None:
+        _torch_once = _Torch()
+    return _torch_once
+
+
+def _op_type(t, x, name):
+    """The dtype code of x, a tensor of a supported type on the GPU."""
+    if isinstance(x, t.Tensor) and x.is_cuda:
+        code = t.codes.get(x.dtype)
+        if code is not None:
+            return code
+    raise TypeError(f"{name} must be a float32, bfloat16 or float16 CUDA/ROCm tensor")
+
+
+def _alike(x, *others):
+    """Raises unless the (name, tensor) pairs have the type and device of x."""
+    for name, o in others:
+        if getattr(o, "dtype", None) is not x.dtype or o.device != x.device:
+            raise TypeError(f"{name} must be a tensor of the type and device of the first")
+
+
+def _of(x, name, dtype, shape, device):
+    """Address of a contiguous tensor of that type and shape, or None."""
+    if x is None:
         return None
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device:
+    if getattr(x, "dtype", None) is not dtype or x.device != device:
         raise TypeError(f"{name} must be a {dtype} tensor on {device}")
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if x.shape != shape or not x.is_contiguous():
         raise ValueError(f"{name} must be contiguous, of shape {tuple(shape)}")
-    return t.data_ptr()
+    return x.data_ptr()
 
 
-def _row_stride(t, name, width=None):
+def _row_stride(x, name):
     """Stride of the rows (last axis) of a tensor whose other axes flatten into one."""
-    if t.dim() < 1 or (width is not None and t.shape[-1] != width):
-        raise ValueError(f"{name} must have rows of {width}")
-    n = t.shape[-1]
-    if n > 1 and t.stride(-1) != 1:
+    shape = x.shape
+    if not shape:
+        raise ValueError(f"{name} must have rows")
+    n = shape[-1]
+    if x.is_contiguous():
+        return n if n > 1 else 1
+    strides = x.stride()
+    if n > 1 and strides[-1] != 1:
         raise ValueError(f"{name} must have unit inner stride")
-    if t.dim() == 2:
-        return t.stride(0) if t.shape[0] > 1 else max(n, 1)
-    if t.is_contiguous():
-        return max(n, 1)
     step, ld = None, max(n, 1)
-    for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+    for size, stride in zip(reversed(shape[:-1]), reversed(strides[:-1])):
         if size == 1:
             continue
         if step is None:
@@ -530,15 +555,14 @@ def _row_stride(t, name, width=None):
 class _On:
     """Where a call launches and allocates: the current stream (nothing to
     switch), or the given one (see _launch_stream)."""
+    __slots__ = ("ctx", "ptr")
 
-    def __init__(self, stream, device):
-        import torch
-        self.ctx = None
+    def __init__(self, t, stream, device):
         if stream is None:
-            self.ptr = torch.cuda.current_stream(device).cuda_stream
+            self.ctx, self.ptr = None, t.raw_stream(device.index)
         else:
             s = _launch_stream(stream, device)
-            self.ctx, self.ptr = torch.cuda.stream(s), s.cuda_stream
+            self.ctx, self.ptr = t.torch.cuda.stream(s), s.cuda_stream
 
     def __enter__(self):
         if self.ctx is not None:
@@ -553,20 +577,24 @@ class _On:
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, out=None, stream=None):
     """(y, mean, rstd) of the rows (last axis) of x (ndvm_layer_norm); mean and
     rstd are float32 of x's leading shape, what layer_norm_grad takes."""
-    import torch
-    dt = _op_type(("x", x), ("weight", weight), ("bias", bias), ("out", out))
-    n = x.shape[-1] if x.dim() else 0
+    t = _t()
+    dt, dtype, dev, shape = _op_type(t, x, "x"), x.dtype, x.device, x.shape
     ld = _row_stride(x, "x")
+    n, lead = shape[-1], shape[:-1]
     rows = x.numel() // n if n else 0
-    w, b = (_of(t, name, x.dtype, (n,), x.device) for t, name in ((weight, "weight"), (bias, "bias")))
-    with _On(stream, x.device) as s:
+    w, b = _of(weight, "weight", dtype, (n,), dev), _of(bias, "bias", dtype, (n,), dev)
+    with _On(t, stream, dev) as s:
         if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        elif out.shape != x.shape:
-            raise ValueError("out must have the shape of x")
-        mean, rstd = torch.empty((2,) + tuple(x.shape[:-1]), dtype=torch.float32, device=x.device).unbind(0)
-        _check(_norm(dt, x.data_ptr(), rows, n, ld, w, b, float(eps), out.data_ptr(), _row_stride(out, "out"),
-                     mean.data_ptr(), rstd.data_ptr(), s), "ndvm_layer_norm")
+            out, ld_out = x.new_empty(shape), n
+        else:
+            _alike(x, ("out", out))
+            if out.shape != shape:
+                raise ValueError("out must have the shape of x")
+            ld_out = _row_stride(out, "out")
+        mean, rstd = x.new_empty(lead, dtype=t.f32), x.new_empty(lead, dtype=t.f32)
+        st = _norm(dt, x.data_ptr(), rows, n, ld, w, b, eps, out.data_ptr(), ld_out, mean.data_ptr(), rstd.data_ptr(), s)
+        if st:
+            _check(st, "ndvm_layer_norm")
     return out, mean, rstd
 
 
@@ -574,24 +602,24 @@ def layer_norm_grad(dy, x, weight, mean, rstd, need_input: bool = True, need_wei
     """(dx, dweight, dbias) of layer_norm (ndvm_layer_norm_grad); what is not
     needed is None.  weight may be None (no dweight's factor; its gradient is
     still that of a weight of ones)."""
-    import torch
-    dt = _op_type(("x", x), ("dy", dy), ("weight", weight))
-    if dy.shape != x.shape:
+    t = _t()
+    dt, dtype, dev, shape = _op_type(t, x, "x"), x.dtype, x.device, x.shape
+    _alike(x, ("dy", dy))
+    if dy.shape != shape:
         raise ValueError("dy must have the shape of x")
-    n = x.shape[-1] if x.dim() else 0
     ld_x, ld_dy = _row_stride(x, "x"), _row_stride(dy, "dy")
+    n, lead = shape[-1], shape[:-1]
     rows = x.numel() // n if n else 0
-    dev = x.device
-    w = _of(weight, "weight", x.dtype, (n,), dev)
-    m, r = (_of(t, name, torch.float32, x.shape[:-1], dev) for t, name in ((mean, "mean"), (rstd, "rstd")))
-    with _On(stream, dev) as s:
-        dx = torch.empty(x.shape, dtype=x.dtype, device=dev) if need_input else None
+    w = _of(weight, "weight", dtype, (n,), dev)
+    m, r = _of(mean, "mean", t.f32, lead, dev), _of(rstd, "rstd", t.f32, lead, dev)
+    with _On(t, stream, dev) as s:
+        dx = x.new_empty(shape) if need_input else None
         dw = db = ws = None
         need = _sz()
         if need_weight:
-            dw, db = torch.empty((2, n), dtype=x.dtype, device=dev).unbind(0)
+            dw, db = x.new_empty(n), x.new_empty(n)
             _check(_norm_ws(rows, n, ctypes.byref(need)), "ndvm_layer_norm_workspace_bytes")
-            ws = torch.empty(need.value, dtype=torch.uint8, device=dev)
+            ws = x.new_empty(need.value, dtype=t.u8)
         _check(_norm_grad(dt, dy.data_ptr(), ld_dy, x.data_ptr(), ld_x, rows, n, w, m, r,
                           dx.data_ptr() if need_input else None, n, dw.data_ptr() if need_weight else None,
                           db.data_ptr() if need_weight else None, ws.data_ptr() if need_weight else None, need.value, s),
@@ -599,46 +627,46 @@ def layer_norm_grad(dy, x, weight, mean, rstd, need_input: bool = True, need_wei
     return dx, dw, db
 
 
-def _heads(t, name, lead, heads, width):
-    """An ndvm_heads of t [seqs, tokens, heads, width] (lead of two) or [tokens, heads, width]."""
-    if tuple(t.shape) != (*lead, heads, width):
-        raise ValueError(f"{name} must have shape {(*lead, heads, width)}, not {tuple(t.shape)}")
-    if width > 1 and t.stride(-1) != 1:
+def _heads(x, name, lead, heads, width):
+    """An ndvm_heads of x [seqs, tokens, heads, width] (lead of two) or [tokens, heads, width]."""
+    if x.shape != (*lead, heads, width):
+        raise ValueError(f"{name} must have shape {(*lead, heads, width)}, not {tuple(x.shape)}")
+    strides = x.stride()
+    if width > 1 and strides[-1] != 1:
         raise ValueError(f"{name} must have unit inner stride")
     if len(lead) == 2:
-        return _Heads(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
-    return _Heads(t.data_ptr(), 0, t.stride(0), t.stride(1))
+        return _Heads(x.data_ptr(), strides[0], strides[1], strides[2])
+    return _Heads(x.data_ptr(), 0, strides[0], strides[1])
 
 
-def _attention(q, k, v, log_decay, offsets, scale):
+def _attention(t, q, k, v, log_decay, offsets, scale):
     """Checks of the arguments that the attention calls share: shape struct, q, k, v, decay and offset pointers."""
-    import torch
-    dt = _op_type(("q", q), ("k", k), ("v", v))
+    dt = _op_type(t, q, "q")
+    _alike(q, ("k", k), ("v", v))
     packed = offsets is not None
     if packed:
-        off = _of(offsets, "offsets", torch.int64, (offsets.numel(),), q.device)
+        off = _of(offsets, "offsets", t.i64, (offsets.numel(),), q.device)
         if offsets.numel() < 1:
             raise ValueError("offsets must hold one more than there are sequences")
     if q.dim() != (3 if packed else 4) or k.dim() != q.dim() or v.dim() != q.dim():
         raise ValueError("q, k and v must be [sequences, tokens, heads, d], or [tokens, heads, d] with offsets")
-    lead = tuple(q.shape[:-2])
-    H, dk = q.shape[-2:]
+    *lead, H, dk = q.shape
+    lead = tuple(lead)
     Hk, dv = v.shape[-2:]
-    decay = _of(log_decay, "log_decay", torch.float32, (H,), q.device)
+    decay = _of(log_decay, "log_decay", t.f32, (H,), q.device)
     if packed:
         n_seq, n = offsets.numel() - 1, lead[0]
     else:
         off, n_seq, n = None, lead[0], lead[0] * lead[1]
-    shape = _AttentionShape(dt, n_seq, n, H, Hk, dk, dv, float(dk ** -0.5 if scale is None else scale))
+    shape = _AttentionShape(dt, n_seq, n, H, Hk, dk, dv, dk ** -0.5 if scale is None else scale)
     return (shape, lead, off, decay, _heads(q, "q", lead, H, dk), _heads(k, "k", lead, Hk, dk),
             _heads(v, "v", lead, Hk, dv))
 
 
-def _attention_workspace(shape, packed, grad, device):
-    import torch
+def _attention_workspace(t, x, shape, packed, grad):
     need = _sz()
     _check(_attn_ws(shape, packed, grad, ctypes.byref(need)), "ndvm_linear_attention_workspace_bytes")
-    ws = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
+    ws = x.new_empty(need.value, dtype=t.u8) if need.value else None
     return ws, ws.data_ptr() if ws is not None else None, need.value
 
 
@@ -650,17 +678,17 @@ def linear_attention(q, k, v, log_decay, offsets=None, scale=None, initial_state
     device) the sequences lie one after the other in [tokens, heads, d].
     log_decay: float32 [heads]; scale: dk**-0.5 unless given; states are
     float32 [sequences, heads, dk, dv]."""
-    import torch
-    shape, lead, off, decay, hq, hk, hv = _attention(q, k, v, log_decay, offsets, scale)
-    dims = (shape.n_seq, shape.heads, shape.dk, shape.dv)
-    s0 = _of(initial_state, "initial_state", torch.float32, dims, q.device)
-    with _On(stream, q.device) as s:
+    t = _t()
+    shape, lead, off, decay, hq, hk, hv = _attention(t, q, k, v, log_decay, offsets, scale)
+    dims, dev = (shape.n_seq, shape.heads, shape.dk, shape.dv), q.device
+    s0 = _of(initial_state, "initial_state", t.f32, dims, dev)
+    with _On(t, stream, dev) as s:
         if out is None:
-            out = torch.empty((*lead, shape.heads, shape.dv), dtype=q.dtype, device=q.device)
+            out = q.new_empty((*lead, shape.heads, shape.dv))
         else:
-            _op_type(("q", q), ("out", out))
-        last = torch.empty(dims, dtype=torch.float32, device=q.device) if final_state else None
-        ws, ws_ptr, need = _attention_workspace(shape, off is not None, 0, q.device)
+            _alike(q, ("out", out))
+        last = q.new_empty(dims, dtype=t.f32) if final_state else None
+        ws, ws_ptr, need = _attention_workspace(t, q, shape, off is not None, 0)
         _check(_attn(shape, hq, hk, hv, decay, off, s0, _heads(out, "out", lead, shape.heads, shape.dv),
                      last.data_ptr() if final_state else None, ws_ptr, need, s), "ndvm_linear_attention")
     return out, last
@@ -670,26 +698,26 @@ def linear_attention_grad(do, q, k, v, log_decay, offsets=None, scale=None, init
                           grad_final_state=None, need=(True, True, True), stream=None):
     """(dq, dk, dv, d initial_state) of linear_attention (ndvm_linear_attention_grad);
     what is not needed, or has no initial state, is None."""
-    import torch
-    shape, lead, off, decay, hq, hk, hv = _attention(q, k, v, log_decay, offsets, scale)
-    _op_type(("q", q), ("do", do))
-    H, Hk, dk, dv = shape.heads, shape.kv_heads, shape.dk, shape.dv
+    t = _t()
+    shape, lead, off, decay, hq, hk, hv = _attention(t, q, k, v, log_decay, offsets, scale)
+    _alike(q, ("do", do))
+    H, Hk, dk, dv, dev = shape.heads, shape.kv_heads, shape.dk, shape.dv, q.device
     dims = (shape.n_seq, H, dk, dv)
-    s0 = _of(initial_state, "initial_state", torch.float32, dims, q.device)
-    ds = _of(grad_final_state, "grad_final_state", torch.float32, dims, q.device)
+    s0 = _of(initial_state, "initial_state", t.f32, dims, dev)
+    ds = _of(grad_final_state, "grad_final_state", t.f32, dims, dev)
     hdo = _heads(do, "do", lead, H, dv)
-    with _On(stream, q.device) as s:
+    with _On(t, stream, dev) as s:
         def empty(wanted, heads, width):
             if not wanted:
                 return None, _Heads(None, 0, 0, 0)
-            t = torch.empty((*lead, heads, width), dtype=q.dtype, device=q.device)
-            return t, _heads(t, "", lead, heads, width)
+            x = q.new_empty((*lead, heads, width))
+            return x, _heads(x, "", lead, heads, width)
 
         gq, hgq = empty(need[0], H, dk)
         gk, hgk = empty(need[1], Hk, dk)
         gv, hgv = empty(need[2], Hk, dv)
-        d0 = torch.empty(dims, dtype=torch.float32, device=q.device) if s0 is not None and need[2] else None
-        ws, ws_ptr, n = _attention_workspace(shape, off is not None, 1, q.device)
+        d0 = q.new_empty(dims, dtype=t.f32) if s0 is not None and need[2] else None
+        ws, ws_ptr, n = _attention_workspace(t, q, shape, off is not None, 1)
         _check(_attn_grad(shape, hq, hk, hv, decay, off, s0, hdo, ds, hgq, hgk, hgv,
                           d0.data_ptr() if d0 is not None else None, ws_ptr, n, s), "ndvm_linear_attention_grad")
     return gq, gk, gv, d0
@@ -701,8 +729,9 @@ def linear_attention_step(q, k, v, log_decay, state, slots=None, scale=None, out
     state[slots[i]] (float32 [slots, heads, dk, dv], updated in place; slot i
     without `slots`), or none, with output 0, where slots[i] is out of range.
     Returns o [streams, heads, dv]."""
-    import torch
-    dt = _op_type(("q", q), ("k", k), ("v", v), ("out", out))
+    t = _t()
+    dt = _op_type(t, q, "q")
+    _alike(q, ("k", k), ("v", v))
     if q.dim() != 3 or v.dim() != 3 or k.dim() != 3:
         raise ValueError("q, k and v must be [streams, heads, d]")
     n, H, dk = q.shape
@@ -710,78 +739,83 @@ def linear_attention_step(q, k, v, log_decay, state, slots=None, scale=None, out
     dev = q.device
     if state.dim() != 4:
         raise ValueError("state must be [slots, heads, dk, dv]")
-    st = _of(state, "state", torch.float32, (state.shape[0], H, dk, dv), dev)
-    sl = _of(slots, "slots", torch.int64, (n,), dev)
-    decay = _of(log_decay, "log_decay", torch.float32, (H,), dev)
+    st = _of(state, "state", t.f32, (state.shape[0], H, dk, dv), dev)
+    sl = _of(slots, "slots", t.i64, (n,), dev)
+    decay = _of(log_decay, "log_decay", t.f32, (H,), dev)
 
-    def one(t, name, heads, width):
-        if tuple(t.shape) != (n, heads, width) or (width > 1 and t.stride(2) != 1):
+    def one(x, name, heads, width):
+        strides = x.stride()
+        if x.shape != (n, heads, width) or (width > 1 and strides[2] != 1):
             raise ValueError(f"{name} must have shape {(n, heads, width)} and unit inner stride")
-        return _Heads(t.data_ptr(), t.stride(0), 0, t.stride(1))
+        return _Heads(x.data_ptr(), strides[0], 0, strides[1])
 
     hq, hk, hv = one(q, "q", H, dk), one(k, "k", Hk, dk), one(v, "v", Hk, dv)
-    shape = _AttentionShape(dt, n, 0, H, Hk, dk, dv, float(dk ** -0.5 if scale is None else scale))
-    with _On(stream, dev) as s:
+    shape = _AttentionShape(dt, n, 0, H, Hk, dk, dv, dk ** -0.5 if scale is None else scale)
+    with _On(t, stream, dev) as s:
         if out is None:
-            out = torch.empty((n, H, dv), dtype=q.dtype, device=dev)
+            out = q.new_empty((n, H, dv))
+        else:
+            _alike(q, ("out", out))
         _check(_attn_step(shape, hq, hk, hv, decay, st, state.shape[0], sl, one(out, "out", H, dv), s),
                "ndvm_linear_attention_step")
     return out
 
 
-def _ffn_args(x, w_gate, w_up, activation, dh=None):
-    dt = _op_type(("x", x), ("w_gate", w_gate), ("w_up", w_up), ("dh", dh))
-    if activation not in ACTIVATIONS:
+def _ffn_args(t, x, w_gate, w_up, activation):
+    dt = _op_type(t, x, "x")
+    _alike(x, ("w_gate", w_gate), ("w_up", w_up))
+    act = ACTIVATIONS.get(activation)
+    if act is None:
         raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}")
     if w_gate.dim() != 2 or w_gate.shape != w_up.shape or x.dim() < 1 or x.shape[-1] != w_gate.shape[1]:
         raise ValueError("w_gate and w_up must be [n_out, n_in], x [.., n_in]")
     n_out, n_in = w_gate.shape
-    rows = x.numel() // n_in if n_in else 0
-    return dt, ACTIVATIONS[activation], rows, n_in, n_out
+    return dt, act, x.numel() // n_in if n_in else 0, n_in, n_out
 
 
-def _ffn_workspace(dt, rows, n_in, n_out, grad, device):
-    import torch
+def _ffn_workspace(t, x, dt, rows, n_in, n_out, grad):
     need = _sz()
     _check(_ffn_ws(dt, rows, n_in, n_out, grad, ctypes.byref(need)), "ndvm_gated_ffn_workspace_bytes")
-    return torch.empty(need.value, dtype=torch.uint8, device=device), need.value
+    ws = x.new_empty(need.value, dtype=t.u8) if need.value else None
+    return ws, ws.data_ptr() if ws is not None else None, need.value
 
 
 def gated_ffn(x, w_gate, w_up, activation: str = "silu", out=None, stream=None):
     """act(x w_gate^T) * (x w_up^T) (ndvm_gated_ffn) for x [.., n_in] and weights [n_out, n_in]."""
-    import torch
-    dt, act, rows, n_in, n_out = _ffn_args(x, w_gate, w_up, activation)
+    t = _t()
+    dt, act, rows, n_in, n_out = _ffn_args(t, x, w_gate, w_up, activation)
     ld_x, ld_g, ld_u = _row_stride(x, "x"), _row_stride(w_gate, "w_gate"), _row_stride(w_up, "w_up")
-    with _On(stream, x.device) as s:
+    with _On(t, stream, x.device) as s:
         if out is None:
-            out = torch.empty((*x.shape[:-1], n_out), dtype=x.dtype, device=x.device)
+            out, ld_out = x.new_empty((*x.shape[:-1], n_out)), n_out
         else:
-            _op_type(("x", x), ("out", out))
-            if tuple(out.shape) != (*x.shape[:-1], n_out):
+            _alike(x, ("out", out))
+            if out.shape != (*x.shape[:-1], n_out):
                 raise ValueError("out must be [.., n_out]")
-        ws, need = _ffn_workspace(dt, rows, n_in, n_out, 0, x.device)
+            ld_out = _row_stride(out, "out")
+        ws, ws_ptr, need = _ffn_workspace(t, x, dt, rows, n_in, n_out, 0)
         _check(_ffn(dt, act, x.data_ptr(), rows, n_in, ld_x, w_gate.data_ptr(), ld_g, w_up.data_ptr(), ld_u, n_out,
-                    out.data_ptr(), _row_stride(out, "out"), ws.data_ptr(), need, s), "ndvm_gated_ffn")
+                    out.data_ptr(), ld_out, ws_ptr, need, s), "ndvm_gated_ffn")
     return out
 
 
 def gated_ffn_grad(dh, x, w_gate, w_up, activation: str = "silu", need_input: bool = True, need_weight: bool = True,
                    stream=None):
     """(dx, dw_gate, dw_up) of gated_ffn (ndvm_gated_ffn_grad); what is not needed is None."""
-    import torch
-    dt, act, rows, n_in, n_out = _ffn_args(x, w_gate, w_up, activation, dh)
-    if tuple(dh.shape) != (*x.shape[:-1], n_out):
+    t = _t()
+    dt, act, rows, n_in, n_out = _ffn_args(t, x, w_gate, w_up, activation)
+    _alike(x, ("dh", dh))
+    if dh.shape != (*x.shape[:-1], n_out):
         raise ValueError("dh must be [.., n_out]")
-    dev = x.device
-    with _On(stream, dev) as s:
-        dx = torch.empty(x.shape, dtype=x.dtype, device=dev) if need_input else None
+    with _On(t, stream, x.device) as s:
+        dx = x.new_empty(x.shape) if need_input else None
         dg = du = None
         if need_weight:
-            dg, du = torch.empty((2, n_out, n_in), dtype=x.dtype, device=dev).unbind(0)
-        ws, need = _ffn_workspace(dt, rows, n_in, n_out, 1, dev)
+            dg, du = (x.new_empty((n_out, n_in)) for _ in range(2))
+        ws, ws_ptr, need = _ffn_workspace(t, x, dt, rows, n_in, n_out, 1)
         _check(_ffn_grad(dt, act, dh.data_ptr(), _row_stride(dh, "dh"), x.data_ptr(), rows, n_in, _row_stride(x, "x"),
                          w_gate.data_ptr(), _row_stride(w_gate, "w_gate"), w_up.data_ptr(), _row_stride(w_up, "w_up"),
                          n_out, dx.data_ptr() if need_input else None, n_in, dg.data_ptr() if need_weight else None,
-                         n_in, du.data_ptr() if need_weight else None, n_in, ws.data_ptr(), need, s),
+                         n_in, du.data_ptr() if need_weight else None, n_in, ws_ptr, need, s),
                "ndvm_gated_ffn_grad")
     return dx, dg, du
