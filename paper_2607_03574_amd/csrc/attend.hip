@@ -88,8 +88,7 @@ template <class T> __device__ inline const T *token_ptr(const Heads &h, const At
     return static_cast<const T *>(h.p) + row + head / h.group * h.head;
 }
 
-// The general kernel: any type, widths up to 16 DT, float matrix instructions
-// (16 x 16 x 4).  Four waves, 16 columns of c each; chunks of 16 tokens, STAGE
+// The kernel for widths of a and b past 128: float matrix instructions (16 x 16 x 4).  Four waves, 16 columns of c each; chunks of 16 tokens, STAGE
 // tokens in LDS at a time.
 // A 16 x 16 accumulator has column l % 16, rows 4 (l / 16) + r in lane l, register r.
 // S (rows: widths of b) and the transposed products P^T (rows: j, columns: i) are
@@ -216,18 +215,20 @@ __global__ void __launch_bounds__(256) attend_general(AttendArgs A) {
         }
 }
 
-// The kernel for bfloat16 and widths of a and b up to 128: bf16 matrix instructions
-// (16 x 16 x 32), chunks of 32 tokens.  Four waves, 16 NT columns of c each; all
-// share the chunk's rows of a, b and c in LDS, loaded one chunk ahead.
+// The kernel for widths of a and b up to 128: bf16 matrix instructions (16 x 16 x 32), chunks
+// of 32 tokens.  Four waves, 16 NT columns of c each; all share the chunk's rows of a,
+// b and c in LDS.
 //  - P^T and S are used from the accumulators as above.  Rows of S are numbered so
 //    that the eight a lane holds in a pair of tiles are eight consecutive widths,
 //    which one 16-byte read of a matches; columns of c so that a lane's results
 //    for a token are consecutive.
 //  - b^T and c^T come from LDS through the transposing reads (four tokens of a
 //    column each), tokens in the order that P^T has them.
-//  - What is float stays float: S enters its product as two bf16 (2^-17), what it
-//    takes, c times its decay, as three (2^-25).  The products of a pair are rounded to
-//    one bf16, as operands; the result has 16 bits too.
+//  - A float is multiplied as bf16 parts, each the next 8 bits of it: half inputs are
+//    exactly two, float inputs three; what is left out of a product of parts is below 2^-24
+//    of it for float, 2^-16 for half.  The state stays float for every type: it enters
+//    its product as two parts (three for float), and takes c times its decay as three.  The
+//    products of a pair are one part for bfloat16, whose result has 8 bits too.
 // LDS rows lie in granules of 16 bytes, granule i of row r at i ^ swizzle(r): the 16 rows
 // that one instruction reads are then in different banks.
 typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -240,19 +241,47 @@ __device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amd
 __device__ inline bf16x4 read_transposed(const char *p) {
     return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(p)));
 }
-// v as the bf16 of its upper half and what is left.
+// The upper 8 bits of v's significand.
 __device__ inline float upper(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
+template <int N> __device__ inline void split(float v, bf16x8 (&to)[N], int at) {
+#pragma unroll
+    for (int i = 0; i < N - 1; ++i) {
+        const float up = upper(v);
+        to[i][at] = bf16(up);
+        v -= up;
+    }
+    to[N - 1][at] = bf16(v);
+}
+// c + x y of parts whose places add up to ORDER at most, small ones first.
+template <int ORDER, int NX, int NY> __device__ inline f32x4 multiply(const bf16x8 (&x)[NX], const bf16x8 (&y)[NY], f32x4 c) {
+#pragma unroll
+    for (int o = ORDER; o >= 0; --o)
+#pragma unroll
+        for (int i = 0; i < NX; ++i)
+            if (o - i >= 0 && o - i < NY) c = mfma(x[i], y[o - i], c);
+    return c;
+}
 #endif
+template <class T> struct InputParts {
+    static constexpr int count = 1;
+};
+template <> struct InputParts<f16> {
+    static constexpr int count = 2;
+};
+template <> struct InputParts<float> {
+    static constexpr int count = 3;
+};
 
-// DS: widths of a and b in 32s.  DIRECT: rows are 16-byte granules at 16-byte
-// addresses, loaded to LDS directly; else through registers.
-template <int DS, int NT, bool DIRECT, bool OUT>
-__global__ void __launch_bounds__(256, 2) attend_bf16(AttendArgs A) {
+// DS: widths of a and b in 32s.  DIRECT (bfloat16): rows are 16-byte granules at 16-byte
+// addresses, loaded to LDS directly, two chunks ahead; else through registers, one ahead.
+template <class T, int DS, int NT, bool DIRECT, bool OUT>
+__global__ void __launch_bounds__(256, 2) attend_parts(AttendArgs A) {
 #ifdef __HIP_DEVICE_COMPILE__
+    constexpr int PARTS = InputParts<T>::count, ORDER = PARTS - 1, STATE = PARTS > 2 ? PARTS : 2;
     constexpr int N = 32, GA = 4 * DS, GC = 8 * NT;      // tokens of a chunk; granules of a row
-    constexpr int BYTES_A = OUT ? N * GA * 16 : 0, BYTES_B = N * GA * 16, BYTES_C = N * GC * 16;
+    constexpr int BYTES_A = OUT ? N * GA * 16 : 0, BYTES_B = N * GA * 16, BYTES_C = N * GC * 16;      // of a part
     constexpr int BYTES = BYTES_A + BYTES_B + BYTES_C;
-    __shared__ __align__(1024) char buffer0[BYTES], buffer1[BYTES], buffer2[BYTES];
+    __shared__ __align__(1024) char buffer0[PARTS * BYTES], buffer1[DIRECT ? BYTES : 16], buffer2[DIRECT ? BYTES : 16];
     __shared__ float power[N + 2];      // lambda^n
     // heads first: workgroups that run together read whole rows of memory between them
     const uint32_t id = blockIdx.x / uint32_t(A.heads);
@@ -281,35 +310,68 @@ __global__ void __launch_bounds__(256, 2) attend_bf16(AttendArgs A) {
         return Rows{row + h / H.group * H.head, A.reversed ? -H.tok : H.tok};
     };
     const Rows ra = rows_of(A.a), rb = rows_of(A.b), rc = rows_of(A.c), ro = rows_of(A.out);
-    const auto load = [&](const Heads &H, const Rows &R, char *to, auto granules_c, auto count_c, int64_t c0, int64_t width, int base) __attribute__((always_inline)) {
+    using std::integral_constant;
+    // a wave's loads of `count` granules a lane: where they lie in the chunk's rows
+    const auto each = [&](const Heads &H, const Rows &R, auto granules_c, auto count_c, int64_t c0, int64_t width, int base, auto f) __attribute__((always_inline)) {
         constexpr int granules = decltype(granules_c)::value, count = decltype(count_c)::value;
-        const bf16 *from = static_cast<const bf16 *>(H.p) + R.at + base * R.step + c0;
-        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16 *>(from), 0, 0x7fffffff, 0x00020000);
-        vec<bf16> x[count];
+        const T *from = static_cast<const T *>(H.p) + R.at + base * R.step + c0;
 #pragma unroll
         for (int i = 0; i < count; ++i) {
             const int at = (wave + 4 * i) * 64 + l, row = at / granules, c = (at % granules ^ swizzle(row, granules)) * 8;
-            const int place = A.reversed ? N - 1 - row : row;
-            const bool there = base + row < len && c0 + c < width;
-            if constexpr (DIRECT) {
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(to + (wave + 4 * i) * 1024), 16,
-                                                         there ? unsigned(place) * unsigned(H.tok * 2) + c * 2 : kNowhere, 0, 0, 0);
-            } else {
-                x[i] = bf16(0.0f);
-                if (there) x[i] = load_vec(from + place * H.tok + c, width - c0 - c);
-            }
-        }
-        if constexpr (!DIRECT) {
-#pragma unroll
-            for (int i = 0; i < count; ++i) *reinterpret_cast<vec<bf16> *>(to + (wave + 4 * i) * 1024 + l * 16) = x[i];
+            f(i, from, A.reversed ? N - 1 - row : row, c, base + row < len && c0 + c < width);
         }
     };
-    using std::integral_constant;
     // always LOADS loads a wave (those past the segment's end fetch nothing)
+    const auto load = [&](const Heads &H, const Rows &R, char *to, auto granules, auto count, int64_t c0, int64_t width, int base) __attribute__((always_inline)) {
+        each(H, R, granules, count, c0, width, base, [&](int i, const T *from, int row, int c, bool there) __attribute__((always_inline)) {
+            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(from), 0, 0x7fffffff, 0x00020000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(to + (wave + 4 * i) * 1024), 16,
+                                                     there ? unsigned(row) * unsigned(H.tok * 2) + c * 2 : kNowhere, 0, 0, 0);
+        });
+    };
+    const integral_constant<int, GA> granules_a;
+    const integral_constant<int, GC> granules_c;
+    const integral_constant<int, LA> count_a;
+    const integral_constant<int, LC> count_c;
     const auto load_chunk = [&](char *to, int base) __attribute__((always_inline)) {
-        if (OUT) load(A.a, ra, to, integral_constant<int, GA>(), integral_constant<int, LA>(), 0, A.da, base);
-        load(A.b, rb, to + BYTES_A, integral_constant<int, GA>(), integral_constant<int, LA>(), 0, A.da, base);
-        load(A.c, rc, to + BYTES_A + BYTES_B, integral_constant<int, GC>(), integral_constant<int, LC>(), col0, A.dc, base);
+        if (OUT) load(A.a, ra, to, granules_a, count_a, 0, A.da, base);
+        load(A.b, rb, to + BYTES_A, granules_a, count_a, 0, A.da, base);
+        load(A.c, rc, to + BYTES_A + BYTES_B, granules_c, count_c, col0, A.dc, base);
+    };
+    // Through registers: eight values a granule, split on their way to LDS.
+    constexpr int V = kVec<T>;
+    vec<T> held[LOADS][8 / V];
+    const auto fetch = [&](int base) __attribute__((always_inline)) {
+        int k = 0;
+        const auto one = [&](const Heads &H, int64_t c0, int64_t width) {
+            return [&, c0, width](int i, const T *from, int row, int c, bool there) __attribute__((always_inline)) {
+#pragma unroll
+                for (int j = 0; j < 8 / V; ++j) {
+                    held[k + i][j] = T(0.0f);
+                    if (there && c0 + c + j * V < width) held[k + i][j] = load_vec(from + row * H.tok + c + j * V, width - c0 - c - j * V);
+                }
+            };
+        };
+        if (OUT) {
+            each(A.a, ra, granules_a, count_a, 0, A.da, base, one(A.a, 0, A.da));
+            k += LA;
+        }
+        each(A.b, rb, granules_a, count_a, 0, A.da, base, one(A.b, 0, A.da));
+        k += LA;
+        each(A.c, rc, granules_c, count_c, col0, A.dc, base, one(A.c, col0, A.dc));
+    };
+    const auto put = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k) {
+            const int of_a = OUT ? LA : 0, i = k < of_a ? k : k < of_a + LA ? k - of_a : k - of_a - LA;
+            const int tile = k < of_a ? 0 : k < of_a + LA ? PARTS * BYTES_A : PARTS * (BYTES_A + BYTES_B);
+            const int part = k < of_a ? BYTES_A : k < of_a + LA ? BYTES_B : BYTES_C;
+            bf16x8 parts[PARTS];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) split(float(held[k][j / V][j % V]), parts, j);
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) *reinterpret_cast<bf16x8 *>(buffer0 + tile + q * part + (wave + 4 * i) * 1024 + l * 16) = parts[q];
+        }
     };
 
     // ---- the state: tile 2 s + u, register r of lane l: width 32 s + 8 (l / 16) + 4 u + r, and
@@ -395,11 +457,11 @@ __global__ void __launch_bounds__(256, 2) attend_bf16(AttendArgs A) {
                         if (r < have) to[r] = O[it][r / 4][r % 4];
                 }
             } else {
-                typedef bf16 out_t __attribute__((ext_vector_type(W), aligned(2)));
-                bf16 *to = static_cast<bf16 *>(const_cast<void *>(A.out.p)) + at;
+                typedef T out_t __attribute__((ext_vector_type(W), aligned(sizeof(T))));
+                T *to = static_cast<T *>(const_cast<void *>(A.out.p)) + at;
                 out_t v;
 #pragma unroll
-                for (int r = 0; r < W; ++r) v[r] = bf16(O[it][r / 4][r % 4]);
+                for (int r = 0; r < W; ++r) v[r] = T(O[it][r / 4][r % 4]);
                 if (have == W) {
                     *reinterpret_cast<out_t *>(to) = v;
                 } else {
@@ -411,63 +473,52 @@ __global__ void __launch_bounds__(256, 2) attend_bf16(AttendArgs A) {
         }
     };
 
-    const auto chunk = [&](char *now, char *next, int base) __attribute__((always_inline)) {
+    const auto compute = [&](const char *now, int base) __attribute__((always_inline)) {
         const int n = min(len - base, N);
-        // this wave's loads of the chunk have landed (the next chunk's may not have); after the
-        // barrier everybody's have, and nobody reads `next`
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(DIRECT ? LOADS | 0x0070 : 0x0070);      // of vector memory; all of LDS
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if (OUT && base > 0) store(base - N);
-        load_chunk(next, base + 2 * N);
-        const char *la = now, *lb = now + BYTES_A, *lc = now + BYTES_A + BYTES_B;
-        bf16x8 fc[NT];
+        const char *la = now, *lb = now + PARTS * BYTES_A, *lc = now + PARTS * (BYTES_A + BYTES_B);
+        const auto pair = [](const char *p, const char *q) { return __builtin_shufflevector(read_transposed(p), read_transposed(q), 0, 1, 2, 3, 4, 5, 6, 7); };
+        bf16x8 fc[NT][PARTS];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
-            fc[nt] = __builtin_shufflevector(read_transposed(lc + c_at(0, nt)), read_transposed(lc + c_at(1, nt)), 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) fc[nt][q] = pair(lc + q * BYTES_C + c_at(0, nt), lc + q * BYTES_C + c_at(1, nt));
         if (OUT) {
             f32x4 P00 = 0, P01 = 0, P11 = 0;
-            bf16x8 fa[2][DS];
-#pragma unroll
-            for (int s = 0; s < DS; ++s) {
-                fa[0][s] = *reinterpret_cast<const bf16x8 *>(la + row_at(0, s));
-                fa[1][s] = *reinterpret_cast<const bf16x8 *>(la + row_at(1, s));
-                const bf16x8 b0 = *reinterpret_cast<const bf16x8 *>(lb + row_at(0, s)), b1 = *reinterpret_cast<const bf16x8 *>(lb + row_at(1, s));
-                P00 = mfma(b0, fa[0][s], P00);
-                P01 = mfma(b0, fa[1][s], P01);
-                P11 = mfma(b1, fa[1][s], P11);
-            }
 #pragma unroll
             for (int it = 0; it < 2; ++it)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) O[it][nt] = 0;
 #pragma unroll
-            for (int s = 0; s < DS; ++s)
+            for (int s = 0; s < DS; ++s) {
+                bf16x8 a0[PARTS], a1[PARTS], b0[PARTS], b1[PARTS];
+#pragma unroll
+                for (int q = 0; q < PARTS; ++q) {
+                    a0[q] = *reinterpret_cast<const bf16x8 *>(la + q * BYTES_A + row_at(0, s));
+                    a1[q] = *reinterpret_cast<const bf16x8 *>(la + q * BYTES_A + row_at(1, s));
+                    b0[q] = *reinterpret_cast<const bf16x8 *>(lb + q * BYTES_B + row_at(0, s));
+                    b1[q] = *reinterpret_cast<const bf16x8 *>(lb + q * BYTES_B + row_at(1, s));
+                }
+                P00 = multiply<ORDER>(b0, a0, P00);
+                P01 = multiply<ORDER>(b0, a1, P01);
+                P11 = multiply<ORDER>(b1, a1, P11);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    bf16x8 hi, lo;
+                    bf16x8 state[STATE];
 #pragma unroll
-                    for (int r = 0; r < 8; ++r) {
-                        const float v = S[2 * s + r / 4][nt][r % 4], up = upper(v);
-                        hi[r] = bf16(up);
-                        lo[r] = bf16(v - up);
-                    }
-#pragma unroll
-                    for (int it = 0; it < 2; ++it) {
-                        O[it][nt] = mfma(lo, fa[it][s], O[it][nt]);
-                        O[it][nt] = mfma(hi, fa[it][s], O[it][nt]);
-                    }
+                    for (int r = 0; r < 8; ++r) split(S[2 * s + r / 4][nt][r % 4], state, r);
+                    O[0][nt] = multiply<STATE - 1>(state, a0, O[0][nt]);
+                    O[1][nt] = multiply<STATE - 1>(state, a1, O[1][nt]);
                 }
-            bf16x8 p[2];
+            }
+            bf16x8 p[2][PARTS];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 // what is masked is replaced, not multiplied
                 const bool seen = lm >= 4 * lg + r;
-                p[0][r] = bf16(seen ? P00[r] * w0[r] : 0.0f);
-                p[0][4 + r] = bf16(0.0f);
-                p[1][r] = bf16(P01[r] * w1[r]);
-                p[1][4 + r] = bf16(seen ? P11[r] * w0[r] : 0.0f);
+                split(seen ? P00[r] * w0[r] : 0.0f, p[0], r);
+                split(0.0f, p[0], 4 + r);
+                split(P01[r] * w1[r], p[1], r);
+                split(seen ? P11[r] * w0[r] : 0.0f, p[1], 4 + r);
             }
             f32x4 near[2][NT];
             float odd = 0;      // NaN if a sum is not finite
@@ -475,30 +526,38 @@ __global__ void __launch_bounds__(256, 2) attend_bf16(AttendArgs A) {
             for (int it = 0; it < 2; ++it)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    near[it][nt] = mfma(fc[nt], p[it], f32x4(0.0f));
+                    near[it][nt] = multiply<ORDER>(fc[nt], p[it], f32x4(0.0f));
 #pragma unroll
                     for (int r = 0; r < 4; ++r) odd = __builtin_fmaf(near[it][nt][r], 0.0f, odd);
                 }
             if (__builtin_expect(__any(odd != 0.0f), 0)) {
                 // a value of c may not be finite, and 0 times it is NaN: add the terms up to i alone
                 for (int it = 0; it < 2; ++it) {
-                    typedef int i32x4 __attribute__((ext_vector_type(4)));
-                    const i32x4 packed = __builtin_bit_cast(i32x4, it ? p[1] : p[0]);
                     f32x4 sum[NT];
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) sum[nt] = 0;
 #pragma unroll 1
                     for (int j = 0; j < N; ++j) {
                         const int at = j / 16 * 2 + j % 4 / 2;
-                        const int two = __shfl(at == 0 ? packed[0] : at == 1 ? packed[1] : at == 2 ? packed[2] : packed[3], lm + 16 * (j % 16 / 4));
-                        const float pij = __int_as_float(j % 2 ? two & 0xffff0000 : two << 16);
+                        float pij = 0;
+#pragma unroll
+                        for (int q = 0; q < PARTS; ++q) {
+                            typedef int i32x4 __attribute__((ext_vector_type(4)));
+                            const i32x4 packed = __builtin_bit_cast(i32x4, it ? p[1][q] : p[0][q]);
+                            const int two = __shfl(at == 0 ? packed[0] : at == 1 ? packed[1] : at == 2 ? packed[2] : packed[3], lm + 16 * (j % 16 / 4));
+                            pij += __int_as_float(j % 2 ? two & 0xffff0000 : two << 16);
+                        }
                         if (j > 16 * it + lm) continue;
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
                                 const int c = wave * 16 * NT + (NT == 2 ? lg * 8 + nt * 4 + r : lg * 4 + r);
-                                sum[nt][r] += pij * float(*reinterpret_cast<const bf16 *>(lc + (j * GC + (c / 8 ^ swizzle(j, GC))) * 16 + c % 8 * 2));
+                                float cj = 0;
+#pragma unroll
+                                for (int q = 0; q < PARTS; ++q)
+                                    cj += float(*reinterpret_cast<const bf16 *>(lc + q * BYTES_C + (j * GC + (c / 8 ^ swizzle(j, GC))) * 16 + c % 8 * 2));
+                                sum[nt][r] += pij * cj;
                             }
                     }
 #pragma unroll
@@ -518,40 +577,61 @@ __global__ void __launch_bounds__(256, 2) attend_bf16(AttendArgs A) {
                 fall[r] = to_end >= 0 ? A.scale_add * power[to_end] : 0.0f;
             }
         }
-        bf16x8 part[NT][3];
+        bf16x8 add[NT][3];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int r = 0; r < 8; ++r) {
-                const float v = float(fc[nt][r]) * fall[r], v1 = upper(v), left = v - v1, v2 = upper(left);
-                part[nt][0][r] = bf16(v1);
-                part[nt][1][r] = bf16(v2);
-                part[nt][2][r] = bf16(left - v2);
+                float c = float(fc[nt][0][r]);
+#pragma unroll
+                for (int q = 1; q < PARTS; ++q) c += float(fc[nt][q][r]);
+                split(c * fall[r], add[nt], r);
             }
 #pragma unroll
         for (int t = 0; t < 2 * DS; ++t) {
-            const bf16x8 fb = __builtin_shufflevector(read_transposed(lb + b_at(0, t / 2, t % 2)), read_transposed(lb + b_at(1, t / 2, t % 2)), 0, 1, 2, 3, 4, 5, 6, 7);
+            bf16x8 fb[PARTS];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                S[t][nt] *= whole;
+            for (int q = 0; q < PARTS; ++q) fb[q] = pair(lb + q * BYTES_B + b_at(0, t / 2, t % 2), lb + q * BYTES_B + b_at(1, t / 2, t % 2));
 #pragma unroll
-                for (int q = 2; q >= 0; --q) S[t][nt] = mfma(fb, part[nt][q], S[t][nt]);
-            }
+            for (int nt = 0; nt < NT; ++nt) S[t][nt] = multiply<2>(fb, add[nt], S[t][nt] * whole);
         }
     };
-    if (len > 0) {
-        load_chunk(buffer0, 0);
-        load_chunk(buffer1, N);
-        int base = 0;
-        for (;;) {
-            chunk(buffer0, buffer2, base);
-            if ((base += N) >= len) break;
-            chunk(buffer1, buffer0, base);
-            if ((base += N) >= len) break;
-            chunk(buffer2, buffer1, base);
-            if ((base += N) >= len) break;
+    if constexpr (DIRECT) {
+        const auto chunk = [&](char *now, char *next, int base) __attribute__((always_inline)) {
+            // this wave's loads of the chunk have landed (the next chunk's may not have) and its reads of the
+            // last one are done; after the barrier everybody's
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(LOADS | 0x0070);
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (OUT && base > 0) store(base - N);
+            load_chunk(next, base + 2 * N);
+            compute(now, base);
+        };
+        if (len > 0) {
+            load_chunk(buffer0, 0);
+            load_chunk(buffer1, N);
+            int base = 0;
+            for (;;) {
+                chunk(buffer0, buffer2, base);
+                if ((base += N) >= len) break;
+                chunk(buffer1, buffer0, base);
+                if ((base += N) >= len) break;
+                chunk(buffer2, buffer1, base);
+                if ((base += N) >= len) break;
+            }
+            if (OUT) store(base - N);
         }
-        if (OUT) store(base - N);
+    } else {
+        fetch(0);
+        for (int base = 0; base < len; base += N) {
+            __syncthreads();
+            put();
+            __syncthreads();
+            fetch(base + N);
+            compute(buffer0, base);
+            if (OUT) store(base);
+        }
     }
     if (!OUT) {
 #pragma unroll
@@ -690,13 +770,13 @@ template <class T, int DT, int STAGE> void launch_general(const AttendArgs &a, h
     attend_general<T, DT, STAGE, true><<<grid, 256, 0, stream>>>(a);
 }
 
-template <int DS, int NT, bool DIRECT> void launch_bf16(const AttendArgs &a, hipStream_t stream) {
+template <class T, int DS, int NT, bool DIRECT> void launch_parts(const AttendArgs &a, hipStream_t stream) {
     const dim3 grid(uint32_t(a.n_segments * a.heads), uint32_t(ceil_div(a.dc, 64 * NT)));
     if (a.n_segments > a.n_seq) {
-        attend_bf16<DS, NT, DIRECT, false><<<grid, 256, 0, stream>>>(a);
+        attend_parts<T, DS, NT, DIRECT, false><<<grid, 256, 0, stream>>>(a);
         launch_carry(a, int64_t(grid.y) * 4 * 2 * DS * NT * 256, stream);
     }
-    attend_bf16<DS, NT, DIRECT, true><<<grid, 256, 0, stream>>>(a);
+    attend_parts<T, DS, NT, DIRECT, true><<<grid, 256, 0, stream>>>(a);
 }
 
 // Whether rows can be loaded to LDS directly: whole granules at 16-byte addresses, and
@@ -705,11 +785,11 @@ bool direct(const AttendArgs &a, const Heads &h, int64_t width) {
     return reinterpret_cast<uintptr_t>(h.p) % 16 == 0 && h.tok % 8 == 0 && h.head % 8 == 0 && (a.offsets || h.seq % 8 == 0) && width % 8 == 0 && h.tok < (1 << 24);
 }
 
-template <bool DIRECT> void launch_bf16(const AttendArgs &a, hipStream_t stream) {
-    if (a.da <= 64 && a.dc <= 64) launch_bf16<2, 1, DIRECT>(a, stream);
-    else if (a.da <= 64) launch_bf16<2, 2, DIRECT>(a, stream);
-    else if (a.dc <= 64) launch_bf16<4, 1, DIRECT>(a, stream);
-    else launch_bf16<4, 2, DIRECT>(a, stream);
+template <class T, bool DIRECT> void launch_parts(const AttendArgs &a, hipStream_t stream) {
+    if (a.da <= 64 && a.dc <= 64) launch_parts<T, 2, 1, DIRECT>(a, stream);
+    else if (a.da <= 64) launch_parts<T, 2, 2, DIRECT>(a, stream);
+    else if (a.dc <= 64) launch_parts<T, 4, 1, DIRECT>(a, stream);
+    else launch_parts<T, 4, 2, DIRECT>(a, stream);
 }
 
 }  // namespace
@@ -719,8 +799,8 @@ template <bool DIRECT> void launch_bf16(const AttendArgs &a, hipStream_t stream)
 // whose states are twice the traffic, 143).  A packed batch is cut wherever a sequence may be
 // longer than that: its longest sequence is not known here, and would be walked by one
 // workgroup while the others are done.
-Cut attend_cut(int dtype, int64_t n_seq, int64_t n_tokens, int64_t heads, int64_t da, int64_t dc, bool packed) {
-    const bool matrix = dtype == NDVM_BF16 && da <= 128;
+Cut attend_cut(int64_t n_seq, int64_t n_tokens, int64_t heads, int64_t da, int64_t dc, bool packed) {
+    const bool matrix = da <= 128;
     const int64_t cols = matrix && dc > 64 ? 128 : 64;
     Cut c;
     c.state = matrix ? (da <= 64 ? 64 : 128) * ceil_div(dc, cols) * cols : ceil_div(da * dc, 4) * 4;
@@ -743,16 +823,12 @@ Cut attend_cut(int dtype, int64_t n_seq, int64_t n_tokens, int64_t heads, int64_
 }
 
 hipError_t launch_attend(int dtype, const AttendArgs &a, hipStream_t stream) {
-    if (dtype == NDVM_BF16 && a.da <= 128) {
-        if (direct(a, a.a, a.da) && direct(a, a.b, a.da) && direct(a, a.c, a.dc)) launch_bf16<true>(a, stream);
-        else launch_bf16<false>(a, stream);
-        return hipGetLastError();
-    }
     return with_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
-        if (a.da <= 64) launch_general<T, 4, 64>(a, stream);
-        else if (a.da <= 128) launch_general<T, 8, 32>(a, stream);
-        else launch_general<T, 16, 16>(a, stream);
+        if (a.da > 128) launch_general<T, 16, 16>(a, stream);
+        else if (std::is_same<T, bf16>::value && direct(a, a.a, a.da) && direct(a, a.b, a.da) && direct(a, a.c, a.dc))
+            launch_parts<bf16, true>(a, stream);
+        else launch_parts<T, false>(a, stream);
         return hipGetLastError();
     });
 }
