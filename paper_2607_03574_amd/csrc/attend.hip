@@ -262,22 +262,14 @@ template <int ORDER, int NX, int NY> __device__ inline f32x4 multiply(const bf16
     return c;
 }
 #endif
-template <class T> struct InputParts {
-    static constexpr int count = 1;
-};
-template <> struct InputParts<f16> {
-    static constexpr int count = 2;
-};
-template <> struct InputParts<float> {
-    static constexpr int count = 3;
-};
+template <class T> constexpr int input_parts() { return sizeof(T) == 4 ? 3 : std::is_same<T, f16>::value ? 2 : 1; }
 
 // DS: widths of a and b in 32s.  DIRECT (bfloat16): rows are 16-byte granules at 16-byte
 // addresses, loaded to LDS directly, two chunks ahead; else through registers, one ahead.
 template <class T, int DS, int NT, bool DIRECT, bool OUT>
 __global__ void __launch_bounds__(256, 2) attend_parts(AttendArgs A) {
 #ifdef __HIP_DEVICE_COMPILE__
-    constexpr int PARTS = InputParts<T>::count, ORDER = PARTS - 1, STATE = PARTS > 2 ? PARTS : 2;
+    constexpr int PARTS = input_parts<T>(), ORDER = PARTS - 1, STATE = PARTS > 2 ? PARTS : 2;
     constexpr int N = 32, GA = 4 * DS, GC = 8 * NT;      // tokens of a chunk; granules of a row
     constexpr int BYTES_A = OUT ? N * GA * 16 : 0, BYTES_B = N * GA * 16, BYTES_C = N * GC * 16;      // of a part
     constexpr int BYTES = BYTES_A + BYTES_B + BYTES_C;
@@ -380,7 +372,22 @@ __global__ void __launch_bounds__(256, 2) attend_parts(AttendArgs A) {
     // A segment's state lies in memory as in the registers.
     f32x4 S[2 * DS][NT];
     f32x4 *mine = reinterpret_cast<f32x4 *>(A.segments) + ((int64_t(blockIdx.x) * gridDim.y + blockIdx.y) * 4 + wave) * (2 * DS * NT * 64) + l;
-    if (OUT && g.index > 0) {
+    if (OUT && g.index > 0 && A.shared_segments) {
+        // the states as a call for the transposed sums left them: its tiles, waves and lanes by (column, width)
+        const int nt_of = A.da <= 64 ? 1 : 2, tiles = (A.dc <= 64 ? 4 : 8) * nt_of;
+        const float *theirs = A.segments + int64_t(blockIdx.x) * (4 * 2 * DS * NT * 256);
+#pragma unroll
+        for (int t = 0; t < 2 * DS; ++t)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int d = t / 2 * 32 + lg * 8 + t % 2 * 4 + r, c = int(column(nt));
+                    const int in = d % (16 * nt_of), lane = c % 32 / 8 * 16 + (nt_of == 2 ? in / 8 * 4 + in % 4 : in);
+                    const int tile = (c / 32 * 2 + c % 8 / 4) * nt_of + (nt_of == 2 ? in / 4 % 2 : 0);
+                    S[t][nt][r] = theirs[((d / (16 * nt_of) * tiles + tile) * 64 + lane) * 4 + c % 4];
+                }
+    } else if (OUT && g.index > 0) {
 #pragma unroll
         for (int t = 0; t < 2 * DS; ++t)
 #pragma unroll
@@ -772,11 +779,11 @@ template <class T, int DT, int STAGE> void launch_general(const AttendArgs &a, h
 
 template <class T, int DS, int NT, bool DIRECT> void launch_parts(const AttendArgs &a, hipStream_t stream) {
     const dim3 grid(uint32_t(a.n_segments * a.heads), uint32_t(ceil_div(a.dc, 64 * NT)));
-    if (a.n_segments > a.n_seq) {
+    if (a.n_segments > a.n_seq && !a.shared_segments) {
         attend_parts<T, DS, NT, DIRECT, false><<<grid, 256, 0, stream>>>(a);
         launch_carry(a, int64_t(grid.y) * 4 * 2 * DS * NT * 256, stream);
     }
-    attend_parts<T, DS, NT, DIRECT, true><<<grid, 256, 0, stream>>>(a);
+    if (!a.only_segments) attend_parts<T, DS, NT, DIRECT, true><<<grid, 256, 0, stream>>>(a);
 }
 
 // Whether rows can be loaded to LDS directly: whole granules at 16-byte addresses, and
@@ -800,7 +807,7 @@ template <class T, bool DIRECT> void launch_parts(const AttendArgs &a, hipStream
 // longer than that: its longest sequence is not known here, and would be walked by one
 // workgroup while the others are done.
 Cut attend_cut(int64_t n_seq, int64_t n_tokens, int64_t heads, int64_t da, int64_t dc, bool packed) {
-    const bool matrix = da <= 128;
+    const bool matrix = da <= kMostPartsDim;
     const int64_t cols = matrix && dc > 64 ? 128 : 64;
     Cut c;
     c.state = matrix ? (da <= 64 ? 64 : 128) * ceil_div(dc, cols) * cols : ceil_div(da * dc, 4) * 4;
@@ -825,7 +832,7 @@ Cut attend_cut(int64_t n_seq, int64_t n_tokens, int64_t heads, int64_t da, int64
 hipError_t launch_attend(int dtype, const AttendArgs &a, hipStream_t stream) {
     return with_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
-        if (a.da > 128) launch_general<T, 16, 16>(a, stream);
+        if (a.da > kMostPartsDim) launch_general<T, 16, 16>(a, stream);
         else if (std::is_same<T, bf16>::value && direct(a, a.a, a.da) && direct(a, a.b, a.da) && direct(a, a.c, a.dc))
             launch_parts<bf16, true>(a, stream);
         else launch_parts<T, false>(a, stream);

@@ -276,14 +276,23 @@ ndvm_status ndvm_linear_attention_grad(const ndvm_attention_shape *shape, const 
             FoldHeadsArgs f{part, heads_of(to, group), s->n_seq, s->n_tokens, s->heads, d, offsets != nullptr};
             return launched(who, launch_fold_heads(s->dtype, f, st));
         };
-        if (dv->data || d_initial) {
+        // the sums q^T d_o of the segments serve dk too, transposed
+        const bool share = std::max(s->dk, s->dv) <= kMostPartsDim;
+        const bool want_v = dv->data || d_initial;
+        if (want_v || (share && dk->data)) {
+            a.only_segments = !want_v;
             a.a = hk;
             a.b = hq;
             a.c = ho;
             a.state_out = d_initial;
             a.state_transposed = 0;
             widths(s->dk, s->dv);
-            if (const ndvm_status r = shared(dv, s->dv)) return r;
+            if (want_v) {
+                if (const ndvm_status r = shared(dv, s->dv)) return r;
+            } else if (a.n_segments > a.n_seq) {
+                if (const ndvm_status r = launched(who, launch_attend(s->dtype, a, st))) return r;
+            }
+            a.only_segments = 0;
         }
         if (dk->data) {
             a.a = hv;
@@ -292,6 +301,7 @@ ndvm_status ndvm_linear_attention_grad(const ndvm_attention_shape *shape, const 
             a.state_out = nullptr;
             a.state_transposed = 1;
             widths(s->dv, s->dk);
+            a.shared_segments = share;
             if (const ndvm_status r = shared(dk, s->dk)) return r;
         }
         return NDVM_OK;
