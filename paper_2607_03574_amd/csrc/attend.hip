@@ -801,25 +801,28 @@ template <class T, bool DIRECT> void launch_parts(const AttendArgs &a, hipStream
 
 }  // namespace
 
-// How sequences are cut: into segments of at least 256 tokens, enough of them for two
-// workgroups a compute unit (16 heads x 16384 tokens of 128: 115 us; for one, 126; for four,
-// whose states are twice the traffic, 143).  A packed batch is cut wherever a sequence may be
-// longer than that: its longest sequence is not known here, and would be walked by one
-// workgroup while the others are done.
-Cut attend_cut(int64_t n_seq, int64_t n_tokens, int64_t heads, int64_t da, int64_t dc, bool packed) {
+// How sequences are cut: into segments for two workgroups a compute unit (16 heads x
+// 16384 tokens of 128: 115 us; for one, 126; for four, whose states are twice the traffic, 143),
+// but of at least 128 tokens, a few chunks' work (16 heads x 2048 tokens: 34 us; of 64, 41; of
+// 256, 39), or 64 in float, whose chunks take three times as long (2 x 1000 tokens, 4 heads of
+// 100: 29 us; of 128, 36).  A packed batch is cut wherever a sequence may be longer than that: its
+// longest sequence is not known here, and would be walked by one workgroup while the others
+// are done.
+Cut attend_cut(int dtype, int64_t n_seq, int64_t n_tokens, int64_t heads, int64_t da, int64_t dc, bool packed) {
+    const int64_t least = dtype == NDVM_F32 ? 64 : 128;
     const bool matrix = da <= kMostPartsDim;
     const int64_t cols = matrix && dc > 64 ? 128 : 64;
     Cut c;
     c.state = matrix ? (da <= 64 ? 64 : 128) * ceil_div(dc, cols) * cols : ceil_div(da * dc, 4) * 4;
     const int64_t longest = packed || n_seq == 0 ? n_tokens : n_tokens / n_seq;
     const int64_t want = std::max<int64_t>(1, 2 * kCus / (heads * ceil_div(dc, cols)));
-    int64_t len = std::max<int64_t>(256, n_tokens / want);
+    int64_t len = std::max<int64_t>(least, n_tokens / want);
     len = ceil_div(len, kSegStep) * kSegStep;
     if (len >= longest || (!packed && n_seq >= want)) {
         c.seg_len = std::max<int64_t>(longest, 1);
         c.n_segments = n_seq;
     } else if (packed) {
-        c.seg_len = 256;
+        c.seg_len = least;
         while (c.seg_len * 2 <= len) c.seg_len *= 2;
         c.n_segments = n_tokens / c.seg_len + n_seq;
     } else {

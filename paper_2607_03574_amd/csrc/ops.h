@@ -65,7 +65,7 @@ struct Cut {
     int64_t seg_len, n_segments;    // more segments than sequences: sequences are cut
     int64_t state;                  // floats of a segment's and head's state
 };
-Cut attend_cut(int64_t n_seq, int64_t n_tokens, int64_t heads, int64_t da, int64_t dc, bool packed);
+Cut attend_cut(int dtype, int64_t n_seq, int64_t n_tokens, int64_t heads, int64_t da, int64_t dc, bool packed);
 hipError_t launch_attend(int dtype, const AttendArgs &a, hipStream_t stream);
 // sum of `group` consecutive heads of float [heads][tokens][d] into `out` [.., heads / group, d]
 struct FoldHeadsArgs {

@@ -76,7 +76,7 @@ Heads heads_of(const ndvm_heads *h, int64_t group) {
 }
 
 Cut cut_of(const ndvm_attention_shape *s, bool packed, int64_t da, int64_t dc) {
-    return attend_cut(s->n_seq, s->n_tokens, s->heads, da, dc, packed);
+    return attend_cut(s->dtype, s->n_seq, s->n_tokens, s->heads, da, dc, packed);
 }
 
 size_t segment_bytes(const ndvm_attention_shape *s, const Cut &c) {
