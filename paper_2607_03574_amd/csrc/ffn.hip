@@ -128,8 +128,8 @@ struct ProductArgs {
     Operand a, a2, b;           // a2: gated, the second weight; plain, what follows `a` along the sum from k2 on
     int64_t k, k2;              // the sum's length, a multiple of 8 (of 64 where an operand runs along C)
     int64_t tiles_n, tiles_m;
-    int splits;                 // plain: workgroups that share a tile's sum
-    float *part;                // with splits: [splits][m][n], what each sums up
+    int splits;                 // workgroups that share a tile's sum
+    float *part;                // with splits: [splits][m][n], what each sums up (gated: [splits][m][2][pad_n])
     int act;
     // plain: rows m < split go to out + m * ld, those from split2 to m2 to out2 + (m - split2) * ld2
     void *out, *out2;
@@ -138,7 +138,8 @@ struct ProductArgs {
     const void *dh;
     int64_t ld_dh;
     void *p;                    // [m][dg du], each padded with zeros to pad_n, in parts
-    int64_t pad_n, ld_p, plane_p;
+    int64_t ld_p, plane_p;
+    int64_t pad_n;              // n_out padded to a multiple of 64
 };
 enum Kind { kGated, kGatedGrad, kPlain };
 
@@ -151,6 +152,58 @@ template <class O> __device__ inline O read_transposed(const char *p, const char
     return __builtin_bit_cast(O, s16x8(__builtin_shufflevector(four(p), four(q), 0, 1, 2, 3, 4, 5, 6, 7)));
 }
 #endif
+
+// What becomes of eight columns (n on) of a row of g and u: h, or dg and du.
+template <class T, Kind KIND, int ACT> __device__ __attribute__((always_inline)) inline void gated_out(const ProductArgs &A, int64_t m, int64_t n, const float (&g)[8], const float (&u)[8]) {
+    typedef typename Parts<T>::type P;
+    constexpr int PARTS = Parts<T>::count;
+    typedef T eight __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    typedef P eight_p __attribute__((ext_vector_type(8)));
+    if constexpr (KIND == kGated) {
+        T *row = static_cast<T *>(A.out) + m * A.ld;
+        eight v;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            float value, slope;
+            act_both<ACT>(g[r], value, slope);
+            v[r] = T(value * u[r]);
+        }
+        if (n + 8 <= A.n) *reinterpret_cast<eight *>(row + n) = v;
+        else
+            for (int r = 0; r < 8; ++r)
+                if (n + r < A.n) row[n + r] = v[r];
+    } else {
+        if (n >= A.pad_n) return;
+        const T *row = static_cast<const T *>(A.dh) + m * A.ld_dh + n;
+        eight dh = T(0.0f);
+        if (n + 8 <= A.n) dh = *reinterpret_cast<const eight *>(row);
+        else
+            for (int r = 0; r < 8; ++r)
+                if (n + r < A.n) dh[r] = row[r];
+        eight_p vg[PARTS], vu[PARTS];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            float value, slope;
+            act_both<ACT>(g[r], value, slope);
+            P pg[PARTS], pu[PARTS];
+            // what lies beyond the operands is 0, whatever act does there
+            const bool there = n + r < A.n;
+            Parts<T>::split(there ? float(dh[r]) * u[r] * slope : 0.0f, pg);
+            Parts<T>::split(there ? float(dh[r]) * value : 0.0f, pu);
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) {
+                vg[q][r] = pg[q];
+                vu[q][r] = pu[q];
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) {
+            P *p = static_cast<P *>(A.p) + q * A.plane_p + m * A.ld_p + n;
+            *reinterpret_cast<eight_p *>(p) = vg[q];
+            *reinterpret_cast<eight_p *>(p + A.pad_n) = vu[q];
+        }
+    }
+}
 
 // BA columns n by BB rows m a workgroup; NA x NB waves.  ALONG_B: the rows of B run along
 // C (B[k][m]); those of A do in a plain product (A[k][n]).
@@ -411,64 +464,41 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
             }
         }
     }
-    if constexpr (GATED) with_act(A.act, [&](auto act) __attribute__((always_inline)) {
-        constexpr int ACT = decltype(act)::value;
-        typedef T eight __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-        typedef P eight_p __attribute__((ext_vector_type(8)));
+    if constexpr (GATED) {
+        if (A.splits > 1) {
 #pragma unroll
-        for (int j = 0; j < TB; ++j) {
-            const int64_t m = m0 + wb * WB + j * 16 + lm;
-            if (m >= A.m) continue;
+            for (int j = 0; j < TB; ++j) {
+                const int64_t m = m0 + wb * WB + j * 16 + lm;
+                if (m >= A.m) continue;
 #pragma unroll
-            for (int i = 0; i < TA / 2; i += 2) {
-                const int64_t n = n0 + wa * (WA / 2) + i * 16 + lg * 8;
-                if constexpr (KIND == kGated) {
-                    T *row = static_cast<T *>(A.out) + m * A.ld;
-                    eight v;
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) {
-                        float value, slope;
-                        act_both<ACT>(acc[i + r / 4][j][r % 4], value, slope);
-                        v[r] = T(value * acc[i + r / 4 + TA / 2][j][r % 4]);
-                    }
-                    if (n + 8 <= A.n) *reinterpret_cast<eight *>(row + n) = v;
-                    else
-                        for (int r = 0; r < 8; ++r)
-                            if (n + r < A.n) row[n + r] = v[r];
-                } else {
+                for (int i = 0; i < TA / 2; ++i) {
+                    const int64_t n = n0 + wa * (WA / 2) + i / 2 * 32 + lg * 8 + i % 2 * 4;
                     if (n >= A.pad_n) continue;
-                    const T *row = static_cast<const T *>(A.dh) + m * A.ld_dh + n;
-                    eight dh = T(0.0f);
-                    if (n + 8 <= A.n) dh = *reinterpret_cast<const eight *>(row);
-                    else
-                        for (int r = 0; r < 8; ++r)
-                            if (n + r < A.n) dh[r] = row[r];
-                    eight_p vg[PARTS], vu[PARTS];
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) {
-                        float value, slope;
-                        act_both<ACT>(acc[i + r / 4][j][r % 4], value, slope);
-                        P pg[PARTS], pu[PARTS];
-                        // what lies beyond the operands is 0, whatever act does there
-                        const bool there = n + r < A.n;
-                        Parts<T>::split(there ? float(dh[r]) * acc[i + r / 4 + TA / 2][j][r % 4] * slope : 0.0f, pg);
-                        Parts<T>::split(there ? float(dh[r]) * value : 0.0f, pu);
-#pragma unroll
-                        for (int q = 0; q < PARTS; ++q) {
-                            vg[q][r] = pg[q];
-                            vu[q][r] = pu[q];
-                        }
-                    }
-#pragma unroll
-                    for (int q = 0; q < PARTS; ++q) {
-                        P *p = static_cast<P *>(A.p) + q * A.plane_p + m * A.ld_p + n;
-                        *reinterpret_cast<eight_p *>(p) = vg[q];
-                        *reinterpret_cast<eight_p *>(p + A.pad_n) = vu[q];
-                    }
+                    float *to = A.part + (int64_t(part) * A.m + m) * 2 * A.pad_n + n;
+                    *reinterpret_cast<f32x4 *>(to) = acc[i][j];
+                    *reinterpret_cast<f32x4 *>(to + A.pad_n) = acc[i + TA / 2][j];
                 }
             }
+            return;
         }
-    });
+        with_act(A.act, [&](auto act) __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < TB; ++j) {
+                const int64_t m = m0 + wb * WB + j * 16 + lm;
+                if (m >= A.m) continue;
+#pragma unroll
+                for (int i = 0; i < TA / 2; i += 2) {
+                    float g[8], u[8];
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        g[r] = acc[i + r / 4][j][r % 4];
+                        u[r] = acc[i + r / 4 + TA / 2][j][r % 4];
+                    }
+                    gated_out<T, KIND, decltype(act)::value>(A, m, n0 + wa * (WA / 2) + i * 16 + lg * 8, g, u);
+                }
+            }
+        });
+    }
 }
 #endif
 
@@ -519,6 +549,31 @@ template <class T> __global__ void __launch_bounds__(256) fold_splits(ProductArg
             row[n + r] = T(sum);
         }
     }
+}
+
+// ... of a gated product.  A thread eight columns.
+template <class T, Kind KIND> __global__ void __launch_bounds__(256) fold_gated(ProductArgs A) {
+#ifdef __HIP_DEVICE_COMPILE__
+    const int64_t per = A.pad_n / 8, at = int64_t(blockIdx.x) * 256 + threadIdx.x, m = at / per, n = at % per * 8;
+    if (m >= A.m) return;
+    f32x4 sum[4] = {};
+    for (int i = 0; i < A.splits; ++i) {
+        const f32x4 *p = reinterpret_cast<const f32x4 *>(A.part + (i * A.m + m) * 2 * A.pad_n + n), *q = p + A.pad_n / 4;
+        sum[0] += p[0];
+        sum[1] += p[1];
+        sum[2] += q[0];
+        sum[3] += q[1];
+    }
+    with_act(A.act, [&](auto act) __attribute__((always_inline)) {
+        float g[8], u[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            g[r] = sum[r / 4][r % 4];
+            u[r] = sum[2 + r / 4][r % 4];
+        }
+        gated_out<T, KIND, decltype(act)::value>(A, m, n, g, u);
+    });
+#endif
 }
 
 // ---- few rows: the weights are read once, straight into registers, by workgroups of 16
@@ -600,13 +655,35 @@ template <class T, int TB> __global__ void __launch_bounds__(256) few(FfnArgs A)
 template <class T, int BA, int BB, int NA, int NB, Kind KIND> void launch_tiles(ProductArgs a, int64_t n, int64_t m, hipStream_t stream) {
     a.tiles_n = ceil_div(n, BA / 2);
     a.tiles_m = ceil_div(m, BB);
-    a.splits = 1;
-    if (a.tiles_n * a.tiles_m == 0) return;
-    product<T, BA, BB, NA, NB, KIND><<<dim3(uint32_t(a.tiles_n * a.tiles_m)), 64 * NA * NB, 0, stream>>>(a);
+    const int64_t wgs = a.tiles_n * a.tiles_m * a.splits;
+    if (wgs) product<T, BA, BB, NA, NB, KIND><<<dim3(uint32_t(wgs)), 64 * NA * NB, 0, stream>>>(a);
 }
-template <class T, Kind KIND> void launch_product(const ProductArgs &a, int64_t n, int64_t m, hipStream_t stream) {
-    if (ceil_div(n, 128) * ceil_div(m, 256) >= 2 * kCus) launch_tiles<T, 256, 256, 2, 4, KIND>(a, n, m, stream);
+
+// How a gated product is cut.  Tiles of 256 x 256, 256 x 128 (n by m) or 128 x 128: by the time of a
+// step of the largest tile (1; 8192 x 2048 x 8192), one workgroup a compute unit; the
+// others' measured at half and a quarter of the work, the smallest with two workgroups side by
+// side.  Their loads take 1.5 and 2 times the bandwidth for the same work, which is what
+// holds them back.  Too few tiles for the compute units, and long sums: several workgroups
+// share a sum, of 32 steps at least (about 15 us, three times what adding their parts up costs).
+struct Gated {
+    int64_t ba, bb, splits;
+};
+Gated gated_cut(int dtype, int64_t rows, int64_t n_in, int64_t n_out) {
+    const int64_t steps = ceil_div(n_in, kStep) * (dtype == NDVM_F32 ? 6 : 1);
+    const auto tiles = [&](int64_t ba, int64_t bb) { return ceil_div(n_out, ba / 2) * ceil_div(rows, bb); };
+    const int64_t large = ceil_div(tiles(256, 256), kCus) * 100, middle = ceil_div(tiles(256, 128), kCus) * 56;
+    const int64_t few_tiles = tiles(128, 128), small = few_tiles <= kCus ? 40 : ceil_div(few_tiles, 2 * kCus) * 64;
+    if (large <= middle && large <= small) return Gated{256, 256, 1};
+    if (middle <= small) return Gated{256, 128, 1};
+    const int64_t splits = few_tiles ? std::min(2 * kCus / few_tiles, std::min<int64_t>(steps / 32, 16)) : 1;
+    return Gated{128, 128, std::max<int64_t>(splits, 1)};
+}
+template <class T, Kind KIND> void launch_product(const Gated &c, ProductArgs a, int64_t n, int64_t m, hipStream_t stream) {
+    a.splits = int(c.splits);
+    if (c.bb == 256) launch_tiles<T, 256, 256, 2, 4, KIND>(a, n, m, stream);
+    else if (c.ba == 256) launch_tiles<T, 256, 128, 4, 2, KIND>(a, n, m, stream);
     else launch_tiles<T, 128, 128, 2, 2, KIND>(a, n, m, stream);
+    if (c.splits > 1) fold_gated<T, KIND><<<dim3(uint32_t(ceil_div(a.pad_n / 8 * a.m, 256))), 256, 0, stream>>>(a);
 }
 
 // How the gradient's two plain products are cut: tiles of `tile` squared, each one's sum over so
@@ -625,7 +702,7 @@ Pieces pieces(int dtype, int64_t rows, int64_t n_in, int64_t n_out) {
     Pieces c{work(256) >= 32 * kCus ? 256 : 128, 1, 1};
     if (tiles_dx(c.tile) + tiles_dw(c.tile) >= 4 * kCus) return c;
     const int64_t share = std::max<int64_t>(16, work(c.tile) / kCus);
-    const auto cut = [&](int64_t steps) { return std::max<int64_t>(1, std::min<int64_t>(8, (steps + share / 2) / share)); };
+    const auto cut = [&](int64_t steps) { return std::max<int64_t>(1, std::min<int64_t>(32, (steps + share / 2) / share)); };
     c.dx = cut(steps_dx);
     c.dw = cut(steps_dw);
     return c;
@@ -678,6 +755,8 @@ size_t ffn_bytes(int dtype, int64_t rows, int64_t n_in, int64_t n_out, bool grad
     s.take(dtype, rows, pad64(n_in));
     s.take(dtype, n_out, pad64(n_in));
     s.take(dtype, n_out, pad64(n_in));
+    const Gated g = gated_cut(dtype, rows, n_in, n_out);
+    if (g.splits > 1) s.take_floats(g.splits * rows * 2 * pad64(n_out));
     if (grad) {
         s.take(dtype, rows, 2 * pad64(n_out));
         const Pieces c = pieces(dtype, rows, n_in, n_out);
@@ -724,8 +803,11 @@ template <class T> Operands operands(const FfnArgs &a, Space &s, hipStream_t str
 
 char *aligned(void *p) { return reinterpret_cast<char *>(round256(reinterpret_cast<size_t>(p))); }
 
-ProductArgs gated(const FfnArgs &a, const Operands &o) {
+// Also takes the room for the sums of a product that is split.
+ProductArgs gated(const FfnArgs &a, const Operands &o, const Gated &c, Space &s) {
     ProductArgs p{};
+    p.pad_n = pad64(a.n_out);
+    if (c.splits > 1) p.part = s.take_floats(c.splits * a.rows * 2 * p.pad_n);
     p.a = o.wg;
     p.a2 = o.wu;
     p.b = o.x;
@@ -745,24 +827,26 @@ template <class T> void ffn(const FfnArgs &a, hipStream_t stream) {
         return;
     }
     Space s(aligned(a.ws));
-    ProductArgs p = gated(a, operands<T>(a, s, stream));
+    const Gated g = gated_cut(a.dtype, a.rows, a.n_in, a.n_out);
+    const Operands o = operands<T>(a, s, stream);
+    ProductArgs p = gated(a, o, g, s);
     p.out = a.h;
     p.ld = a.ld_h;
-    launch_product<T, kGated>(p, a.n_out, a.rows, stream);
+    launch_product<T, kGated>(g, p, a.n_out, a.rows, stream);
 }
 
 template <class T> void ffn_grad(const FfnArgs &a, hipStream_t stream) {
     Space s(aligned(a.ws));
     const Operands o = operands<T>(a, s, stream);
     const int64_t pad_n = pad64(a.n_out);
-    ProductArgs p = gated(a, o);
+    const Gated g = gated_cut(a.dtype, a.rows, a.n_in, a.n_out);
+    ProductArgs p = gated(a, o, g, s);
     p.dh = a.dh;
     p.ld_dh = a.ld_dh;
-    p.pad_n = pad_n;
     p.p = s.take(a.dtype, a.rows, 2 * pad_n);
     p.ld_p = 2 * pad_n;
     p.plane_p = s.plane;
-    launch_product<T, kGatedGrad>(p, pad_n, a.rows, stream);
+    launch_product<T, kGatedGrad>(g, p, pad_n, a.rows, stream);
     const Operand both{p.p, a.rows, 2 * pad_n, p.plane_p};
     const Pieces c = pieces(a.dtype, a.rows, a.n_in, a.n_out);
     ProductArgs dx{}, dw{};
