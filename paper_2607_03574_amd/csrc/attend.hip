@@ -267,7 +267,7 @@ template <class T> constexpr int input_parts() { return sizeof(T) == 4 ? 3 : std
 // DS: widths of a and b in 32s.  DIRECT (bfloat16): rows are 16-byte granules at 16-byte
 // addresses, loaded to LDS directly, two chunks ahead; else through registers, one ahead.
 template <class T, int DS, int NT, bool DIRECT, bool OUT>
-__global__ void __launch_bounds__(256, 2) attend_parts(AttendArgs A) {
+__global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(AttendArgs A) {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int PARTS = input_parts<T>(), ORDER = PARTS - 1, STATE = PARTS > 2 ? PARTS : 2;
     constexpr int N = 32, GA = 4 * DS, GC = 8 * NT;      // tokens of a chunk; granules of a row
@@ -283,8 +283,6 @@ __global__ void __launch_bounds__(256, 2) attend_parts(AttendArgs A) {
     const int l = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lm = l % 16, lg = l / 16;
     const float gl = A.log_decay[h];
     const int e = A.reversed ? 0 : 1;
-    if (threadIdx.x < N + 2) power[threadIdx.x] = decay(gl, threadIdx.x);
-    __syncthreads();
 
     const auto swizzle = [](int row, int granules) { return granules >= 16 ? row % 4 * 4 + row / 4 % 4 : row % 2 * 4 + row / 2 % 4; };
 
@@ -366,6 +364,14 @@ __global__ void __launch_bounds__(256, 2) attend_parts(AttendArgs A) {
         }
     };
 
+    if constexpr (DIRECT) {
+        load_chunk(buffer0, 0);
+        load_chunk(buffer1, N);
+    } else {
+        fetch(0);
+    }
+    if (threadIdx.x < N + 2) power[threadIdx.x] = decay(gl, threadIdx.x);
+
     // ---- the state: tile 2 s + u, register r of lane l: width 32 s + 8 (l / 16) + 4 u + r, and
     // column (NT = 2) 8 (l % 16 / 4) + 4 nt + l % 4 of the wave's
     const auto column = [&](int nt) { return col0 + wave * 16 * NT + (NT == 2 ? lm / 4 * 8 + nt * 4 + lm % 4 : lm); };
@@ -413,6 +419,8 @@ __global__ void __launch_bounds__(256, 2) attend_parts(AttendArgs A) {
                     }
         }
     }
+
+    __syncthreads();
 
     // ---- decays of a chunk: of a pair (row j of P^T, column i; the same tile, the next one), of what is
     // read from the state, of what it takes from a full chunk
@@ -616,8 +624,6 @@ __global__ void __launch_bounds__(256, 2) attend_parts(AttendArgs A) {
             compute(now, base);
         };
         if (len > 0) {
-            load_chunk(buffer0, 0);
-            load_chunk(buffer1, N);
             int base = 0;
             for (;;) {
                 chunk(buffer0, buffer2, base);
@@ -630,7 +636,6 @@ __global__ void __launch_bounds__(256, 2) attend_parts(AttendArgs A) {
             if (OUT) store(base - N);
         }
     } else {
-        fetch(0);
         for (int base = 0; base < len; base += N) {
             __syncthreads();
             put();
