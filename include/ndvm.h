@@ -448,7 +448,8 @@ ndvm_status ndvm_layer_norm_grad(int dtype, const void *dy, int64_t ld_dy, const
  * S before the first token is `initial_state` (float [n_seq, heads, dk, dv],
  * contiguous) or 0 where that is NULL; S after the last one goes to
  * `final_state` (the same layout) unless that is NULL.  log_decay: device float
- * [heads], constants of the model (they get no gradient).  Evaluated in chunks,
+ * [heads], constants of the model (they get no gradient), at most 0 (beyond it
+ * states grow and may overflow).  Evaluated in chunks,
  * not token by token, with every sum and state in float; a value that is not
  * finite leaves the outputs of earlier tokens and of other sequences as they are.
  *
@@ -459,7 +460,8 @@ ndvm_status ndvm_layer_norm_grad(int dtype, const void *dy, int64_t ld_dy, const
  * Sequences without tokens are allowed (their final state is the initial one).
  * Offsets outside 0..n_tokens are read as the nearer end; where they decrease,
  * results are unspecified, with no access outside the tensors.
- * Limits: dk, dv <= 256, heads <= 65,535.
+ * Limits: dk, dv <= 256, heads <= 65,535, n_tokens <= 2^30, and (n_tokens / 64 +
+ * n_seq + 1) heads < 2^31.
  */
 typedef struct {
     int dtype;

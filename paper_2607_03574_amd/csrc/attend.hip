@@ -635,13 +635,19 @@ __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(A
             }
             if (OUT) store(base - N);
         }
+        // the loads past the end fetch nothing, but write zeros to LDS, which has to be this workgroup's still
+        __builtin_amdgcn_s_waitcnt(0x0f70);
     } else {
+        // The widest float tiles have no registers to hold the next chunk in meanwhile: the other workgroup on
+        // the compute unit covers its loads (16384 tokens x 16 heads of 128: 270 us; held and spilled, 326).
+        constexpr bool AHEAD = !(PARTS == 3 && DS == 4 && NT == 2);
         for (int base = 0; base < len; base += N) {
             __syncthreads();
             put();
             __syncthreads();
-            fetch(base + N);
+            if (AHEAD) fetch(base + N);
             compute(buffer0, base);
+            if (!AHEAD) fetch(base + N);
             if (OUT) store(base);
         }
     }

@@ -424,6 +424,8 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
             step(s + 2, buffer3, buffer2, even);
             step(s + 3, buffer0, buffer3, odd);
         }
+        // the loads past the end fetch nothing, but write zeros to LDS, which has to be this workgroup's still
+        __builtin_amdgcn_s_waitcnt(0x0f70);
     }
 
     // lane l, register r of tile (i, j): row m = l % 16 of j; column 4 (l / 16) + r of i, or,

@@ -60,7 +60,7 @@ struct AttendArgs {
     int only_segments;          // no outputs: `segments` for a call that shares them
     int shared_segments;        // `segments` hold what a call with b and c exchanged has left there (widths up to 128)
 };
-constexpr int64_t kSegStep = 64, kMostPartsDim = 128, kMostHeadDim = 256, kMostHeads = 65535;
+constexpr int64_t kSegStep = 64, kMostPartsDim = 128, kMostHeadDim = 256, kMostHeads = 65535, kMostTokens = 1 << 30;
 struct Cut {
     int64_t seg_len, n_segments;    // more segments than sequences: sequences are cut
     int64_t state;                  // floats of a segment's and head's state

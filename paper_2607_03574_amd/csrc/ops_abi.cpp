@@ -58,7 +58,7 @@ ndvm_status check_shape(const char *who, const ndvm_attention_shape *s, bool tok
     if (s->n_seq > INT32_MAX / 2 || !fits(s->n_seq, s->heads, s->dk * s->dv)) return fail(NDVM_E_UNSUPPORTED, who, "too many sequences");
     if (!tokens) return NDVM_OK;
     if (s->n_tokens < 0 || (s->n_seq == 0 && s->n_tokens)) return bad(who, "bad token count");
-    if (s->n_tokens > INT32_MAX || !fits(s->n_tokens, s->heads, std::max(s->dk, s->dv)))
+    if (s->n_tokens > kMostTokens || !fits(s->n_tokens, s->heads, std::max(s->dk, s->dv)))
         return fail(NDVM_E_UNSUPPORTED, who, "too many tokens");
     if (!fits(s->n_tokens / 64 + s->n_seq + 1, s->heads) || (s->n_tokens / 64 + s->n_seq + 1) * s->heads > INT32_MAX)
         return fail(NDVM_E_UNSUPPORTED, who, "too many sequences, tokens and heads for one launch");
