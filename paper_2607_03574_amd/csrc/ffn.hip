@@ -278,46 +278,66 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
     const int steps = int((A.k + kStep - 1) / kStep);
     // this workgroup's share of the sum
     const int first = int(int64_t(steps) * PAIRS * part / A.splits), total = int(int64_t(steps) * PAIRS * (part + 1) / A.splits);
-    // pairs of parts, largest products first
-    constexpr int pair_a[6] = {0, 0, 1, 1, 0, 2}, pair_b[6] = {0, 1, 0, 1, 2, 0};
-    // always LA + LB loads a wave (past the end they fetch nothing)
-    const auto load = [&](int s, char *to) __attribute__((always_inline)) {
-        int64_t k0 = int64_t(s) * kStep;
+    // Where the next tiles to load begin: moved on from step to step, or worked out again where there are
+    // pairs of parts (in order of size).  No branches: the accumulators would be moved about at each.
+    const P *next_a = nullptr, *next_a2 = nullptr, *next_b = nullptr;
+    int left = 0;               // of the sum, from there to the end of these operands
+    int rows_a = 0, rows_b = 0; // rows there are from there on, for operands along C
+    int at = first;             // the step
+    const auto find = [&]() __attribute__((always_inline)) {
+        constexpr int pair_a[6] = {0, 0, 1, 1, 0, 2}, pair_b[6] = {0, 1, 0, 1, 2, 0};
         int pa = 0, pb = 0;
+        int64_t k0 = int64_t(at) * kStep;
         if (PAIRS > 1) {
-            const int pair = s / steps;
-            k0 = int64_t(s % steps) * kStep;
+            const int pair = at / steps;
+            k0 = int64_t(at % steps) * kStep;
 #pragma unroll
             for (int i = 0; i < PAIRS; ++i)
                 if (i == pair) pa = pair_a[i], pb = pair_b[i];
         }
-        const bool some = s < total && k0 + granule * 8 < A.k;
-        {
-            const bool after = ALONG_A && k0 >= A.k2;
-            const Operand &o = after ? A.a2 : A.a;
-            const int64_t k1 = after ? k0 - A.k2 : k0;
-            const P *base = static_cast<const P *>(o.p) + pa * o.plane + (ALONG_A ? k1 * o.ld + n0 : n0 * o.ld + k0);
-            const auto r = rsrc(base);
-            const auto r2 = GATED ? rsrc(static_cast<const P *>(A.a2.p) + pa * A.a2.plane + n0 * A.a2.ld + k0) : r;
-            const int rows = s < total ? int(min(o.rows - k1, int64_t(kStep))) : 0;
+        const bool after = ALONG_A && k0 >= A.k2;
+        const Operand &o = after ? A.a2 : A.a;
+        const int64_t k1 = after ? k0 - A.k2 : k0;
+        next_a = static_cast<const P *>(o.p) + pa * o.plane + (ALONG_A ? k1 * o.ld + n0 : n0 * o.ld + k0);
+        if (GATED) next_a2 = static_cast<const P *>(A.a2.p) + pa * A.a2.plane + n0 * A.a2.ld + k0;
+        next_b = static_cast<const P *>(A.b.p) + pb * A.b.plane + (ALONG_B ? k0 * A.b.ld + m0 : m0 * A.b.ld + k0);
+        left = int((ALONG_A && !after ? A.k2 : A.k) - k0);
+        rows_a = int(min(o.rows - k1, int64_t(1) << 30));
+        rows_b = int(min(A.b.rows - k0, int64_t(1) << 30));
+    };
+    const unsigned apart_a = ALONG_A ? unsigned(512 * W / BA * A.a.ld) * 2 : 0, apart_b = ALONG_B ? unsigned(512 * W / BB * A.b.ld) * 2 : 0;
+    // The next tile into `to`: always LA + LB loads a wave (past the end they fetch nothing).
+    const auto load = [&](char *to) __attribute__((always_inline)) {
+        if (PAIRS > 1) find();
+        const bool some = at < total && granule * 8 < left;
+        const int have_a = at < total ? rows_a : 0, have_b = at < total ? rows_b : 0;
+        const auto r = rsrc(next_a), r2 = GATED ? rsrc(next_a2) : r, rb = rsrc(next_b);
 #pragma unroll
-            for (int i = 0; i < LA; ++i) {
-                const bool second = GATED && (wave + W * i) * 16 % WA >= WA / 2;
-                constexpr int apart = 512 * W / BA;
-                const bool there = ALONG_A ? along_row(BA) < rows - apart * i : some;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(second ? r2 : r, (__attribute__((address_space(3))) void *)(to + (wave + W * i) * 1024), 16,
-                                                         there ? at_a[i] : kNowhere, ALONG_A ? unsigned(apart * i * o.ld) * 2 : 0, 0, 0);
-            }
+        for (int i = 0; i < LA; ++i) {
+            const bool second = GATED && (wave + W * i) * 16 % WA >= WA / 2;
+            const bool there = ALONG_A ? along_row(BA) < have_a - 512 * W / BA * i : some;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(second ? r2 : r, (__attribute__((address_space(3))) void *)(to + (wave + W * i) * 1024), 16,
+                                                     there ? at_a[i] : kNowhere, apart_a * i, 0, 0);
         }
-        const P *base = static_cast<const P *>(A.b.p) + pb * A.b.plane + (ALONG_B ? k0 * A.b.ld + m0 : m0 * A.b.ld + k0);
-        const auto r = rsrc(base);
-        const int rows = s < total ? int(min(A.b.rows - k0, int64_t(kStep))) : 0;
 #pragma unroll
         for (int i = 0; i < LB; ++i) {
-            constexpr int apart = 512 * W / BB;
-            const bool there = ALONG_B ? along_row(BB) < rows - apart * i : some;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(to + BA * 64 + (wave + W * i) * 1024), 16,
-                                                     there ? at_b[i] : kNowhere, ALONG_B ? unsigned(apart * i * A.b.ld) * 2 : 0, 0, 0);
+            const bool there = ALONG_B ? along_row(BB) < have_b - 512 * W / BB * i : some;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (__attribute__((address_space(3))) void *)(to + BA * 64 + (wave + W * i) * 1024), 16,
+                                                     there ? at_b[i] : kNowhere, apart_b * i, 0, 0);
+        }
+        ++at;
+        if (PAIRS > 1) return;
+        left -= kStep;
+        next_a += ALONG_A ? kStep * A.a.ld : kStep;
+        if (GATED) next_a2 += kStep;
+        next_b += ALONG_B ? kStep * A.b.ld : kStep;
+        rows_a -= kStep;
+        rows_b -= kStep;
+        if (ALONG_A && !ALONG_B) {      // on to what follows along the sum
+            const bool wrap = left <= 0;
+            next_a = wrap ? static_cast<const P *>(A.a2.p) + n0 : next_a;
+            rows_a = wrap ? int(A.a2.rows) : rows_a;
+            left = wrap ? int(A.k - A.k2) : left;
         }
     };
 
@@ -376,12 +396,12 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
         asm volatile("" ::: "memory");
     };
     using std::integral_constant;
-    // step s: its operands are in registers (B's in set `now`); the next tile is in `next`; the tile
-    // four on takes its place, `to`
-    const auto step = [&](int s, const char *next, char *to, auto now) __attribute__((always_inline)) {
+    // A step: its operands are in registers (B's in set `now`); the next tile is in `next`; the tile
+    // four on takes its own place, `to`
+    const auto step = [&](const char *next, char *to, auto now) __attribute__((always_inline)) {
         constexpr int n = decltype(now)::value;
         wait(integral_constant<int, 2 * LOADS>());
-        load(s + 4, to);
+        load(to);
         const Places place = places();
         static_assert(TB <= TA, "");
 #pragma unroll
@@ -396,19 +416,22 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
         for (int i = 0; i < TB; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, TB, 0);
             __builtin_amdgcn_sched_group_barrier(0x020, (LOADS + TB - 1) / TB, 0);
+            if (ALONG_A) __builtin_amdgcn_sched_group_barrier(0x002, 1 + ALONG_B, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, (ALONG_A ? 2 : 1) + (ALONG_B ? 2 : 1), 0);
         }
 #pragma unroll
         for (int i = TB; i < TA; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, TB, 0);
+            if (ALONG_A) __builtin_amdgcn_sched_group_barrier(0x002, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, ALONG_A ? 2 : 1, 0);
         }
     };
     if (first < total) {
-        load(first, buffer0);
-        load(first + 1, buffer1);
-        load(first + 2, buffer2);
-        load(first + 3, buffer3);
+        find();
+        load(buffer0);
+        load(buffer1);
+        load(buffer2);
+        load(buffer3);
         wait(integral_constant<int, 3 * LOADS>());
         const Places place = places();
 #pragma unroll
@@ -419,10 +442,10 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
         const integral_constant<int, 0> even;
         const integral_constant<int, 1> odd;
         for (int s = first; s < total; s += 4) {    // steps past the end add zeros
-            step(s, buffer1, buffer0, even);
-            step(s + 1, buffer2, buffer1, odd);
-            step(s + 2, buffer3, buffer2, even);
-            step(s + 3, buffer0, buffer3, odd);
+            step(buffer1, buffer0, even);
+            step(buffer2, buffer1, odd);
+            step(buffer3, buffer2, even);
+            step(buffer0, buffer3, odd);
         }
         // the loads past the end fetch nothing, but write zeros to LDS, which has to be this workgroup's still
         __builtin_amdgcn_s_waitcnt(0x0f70);
@@ -774,10 +797,12 @@ struct Operands {
     Operand x, wg, wu;
     int64_t k;
 };
-// x and the weights as product() reads them: themselves, or padded copies.
+// x and the weights as product() reads them: themselves, or padded copies.  (The weights one after the
+// other along a sum have one row stride.)
 template <class T> Operands operands(const FfnArgs &a, Space &s, hipStream_t stream) {
     Operands o;
-    if (direct(a.dtype, a.x, a.ld_x, a.n_in) && direct(a.dtype, a.wg, a.ld_wg, a.n_in) && direct(a.dtype, a.wu, a.ld_wu, a.n_in)) {
+    if (direct(a.dtype, a.x, a.ld_x, a.n_in) && direct(a.dtype, a.wg, a.ld_wg, a.n_in) && direct(a.dtype, a.wu, a.ld_wu, a.n_in) &&
+        (!a.dx || a.ld_wg == a.ld_wu)) {
         o.x = Operand{a.x, a.rows, a.ld_x, 0};
         o.wg = Operand{a.wg, a.n_out, a.ld_wg, 0};
         o.wu = Operand{a.wu, a.n_out, a.ld_wu, 0};

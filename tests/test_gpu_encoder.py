@@ -438,6 +438,20 @@ def test_gated_ffn_strides(nd, kind):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+@pytest.mark.parametrize("kind", KINDS)
+def test_gated_ffn_weights_of_different_strides(nd, kind):
+    """Weights whose rows are 16-byte aligned, but not equally far apart."""
+    normal = make(4)
+    rows, n_in, n_out = 100, 64, 136
+    x, _ = normal(rows, n_in, kind=kind)
+    dh, _ = normal(rows, n_out, kind=kind)
+    wg, wu = normal(n_out, n_in + 32, kind=kind, scale=0.1)[0][:, :n_in], normal(n_out, n_in + 8, kind=kind, scale=0.1)[0][:, :n_in]
+    assert torch.equal(nd.gated_ffn(x, wg, wu), nd.gated_ffn(x, wg.contiguous(), wu.contiguous()))
+    got = nd.gated_ffn_grad(dh, x, wg, wu)
+    want = nd.gated_ffn_grad(dh, x, wg.contiguous(), wu.contiguous())
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_gated_ffn_no_rows_and_rows_apart(nd):
     w = torch.randn(24, 16, device="cuda")
     x = torch.empty(0, 16, device="cuda")
