@@ -266,7 +266,9 @@ template <class T> constexpr int input_parts() { return sizeof(T) == 4 ? 3 : std
 
 // DS: widths of a and b in 32s.  DIRECT (bfloat16): rows are 16-byte granules at 16-byte
 // addresses, loaded to LDS directly, two chunks ahead; else through registers, one ahead.
-template <class T, int DS, int NT, bool DIRECT, bool OUT>
+// PASSING: a and the outputs, which this launch alone touches, are more than the last cache should
+// hold next to b and c, which the launch before has read too.
+template <class T, int DS, int NT, bool DIRECT, bool OUT, bool PASSING = false>
 __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(AttendArgs A) {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int PARTS = input_parts<T>(), ORDER = PARTS - 1, STATE = PARTS > 2 ? PARTS : 2;
@@ -312,11 +314,11 @@ __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(A
         }
     };
     // always LOADS loads a wave (those past the segment's end fetch nothing)
-    const auto load = [&](const Heads &H, const Rows &R, char *to, auto granules, auto count, int64_t c0, int64_t width, int base) __attribute__((always_inline)) {
+    const auto load = [&](const Heads &H, const Rows &R, char *to, auto granules, auto count, int64_t c0, int64_t width, int base, auto passing) __attribute__((always_inline)) {
         each(H, R, granules, count, c0, width, base, [&](int i, const T *from, int row, int c, bool there) __attribute__((always_inline)) {
             const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(from), 0, 0x7fffffff, 0x00020000);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(to + (wave + 4 * i) * 1024), 16,
-                                                     there ? unsigned(row) * unsigned(H.tok * 2) + c * 2 : kNowhere, 0, 0, 0);
+                                                     there ? unsigned(row) * unsigned(H.tok * 2) + c * 2 : kNowhere, 0, 0, decltype(passing)::value ? 2 : 0);
         });
     };
     const integral_constant<int, GA> granules_a;
@@ -324,9 +326,10 @@ __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(A
     const integral_constant<int, LA> count_a;
     const integral_constant<int, LC> count_c;
     const auto load_chunk = [&](char *to, int base) __attribute__((always_inline)) {
-        if (OUT) load(A.a, ra, to, granules_a, count_a, 0, A.da, base);
-        load(A.b, rb, to + BYTES_A, granules_a, count_a, 0, A.da, base);
-        load(A.c, rc, to + BYTES_A + BYTES_B, granules_c, count_c, col0, A.dc, base);
+        const std::false_type stays;
+        if (OUT) load(A.a, ra, to, granules_a, count_a, 0, A.da, base, integral_constant<bool, PASSING>());
+        load(A.b, rb, to + BYTES_A, granules_a, count_a, 0, A.da, base, stays);
+        load(A.c, rc, to + BYTES_A + BYTES_B, granules_c, count_c, col0, A.dc, base, stays);
     };
     // Through registers: eight values a granule, split on their way to LDS.
     constexpr int V = kVec<T>;
@@ -478,7 +481,8 @@ __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(A
 #pragma unroll
                 for (int r = 0; r < W; ++r) v[r] = T(O[it][r / 4][r % 4]);
                 if (have == W) {
-                    *reinterpret_cast<out_t *>(to) = v;
+                    if (PASSING) __builtin_nontemporal_store(v, reinterpret_cast<out_t *>(to));
+                    else *reinterpret_cast<out_t *>(to) = v;
                 } else {
 #pragma unroll
                     for (int r = 0; r < W; ++r)
@@ -724,7 +728,7 @@ template <class T> __global__ void __launch_bounds__(256) fold_heads(FoldHeadsAr
 // One token of every stream: S <- lambda S + k^T v, o = scale q S.  Bound by the
 // state's way through memory: 8 dk dv bytes.  X threads of four columns each side by
 // side, 256 / X rows at a time.
-template <class T, int X> __global__ void __launch_bounds__(256) attend_step(StepArgs a) {
+template <class T, int X, bool PASSING> __global__ void __launch_bounds__(256) attend_step(StepArgs a) {
     typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
     constexpr int G = 256 / X;
     __shared__ float lq[256], lk[256];
@@ -755,9 +759,11 @@ template <class T, int X> __global__ void __launch_bounds__(256) attend_step(Ste
     if (have == 4) {
 #pragma unroll 4
         for (int64_t d = g; d < a.dk; d += G) {
-            f32x4 s = *reinterpret_cast<f4 *>(S + d * a.dv);
+            f4 *at = reinterpret_cast<f4 *>(S + d * a.dv);
+            f32x4 s = PASSING ? __builtin_nontemporal_load(at) : *at;
             s = s * lambda + vv * lk[d];
-            *reinterpret_cast<f4 *>(S + d * a.dv) = s;
+            if (PASSING) __builtin_nontemporal_store(f4(s), at);
+            else *at = s;
             sum += s * lq[d];
         }
     } else {
@@ -794,7 +800,11 @@ template <class T, int DS, int NT, bool DIRECT> void launch_parts(const AttendAr
         attend_parts<T, DS, NT, DIRECT, false><<<grid, 256, 0, stream>>>(a);
         launch_carry(a, int64_t(grid.y) * 4 * 2 * DS * NT * 256, stream);
     }
-    if (!a.only_segments) attend_parts<T, DS, NT, DIRECT, true><<<grid, 256, 0, stream>>>(a);
+    if (a.only_segments) return;
+    // 16 heads x 16384 tokens of 128 (268 MB): 119 us, against 129 with all data as if it stayed
+    const bool passing = DIRECT && a.n_tokens * a.heads * (a.da + a.dc) * 4 >= kPassingTraffic;
+    if (passing) attend_parts<T, DS, NT, DIRECT, true, DIRECT><<<grid, 256, 0, stream>>>(a);
+    else attend_parts<T, DS, NT, DIRECT, true><<<grid, 256, 0, stream>>>(a);
 }
 
 // Whether rows can be loaded to LDS directly: whole granules at 16-byte addresses, and
@@ -865,10 +875,13 @@ hipError_t launch_fold_heads(int dtype, const FoldHeadsArgs &a, hipStream_t stre
 hipError_t launch_step(int dtype, const StepArgs &a, hipStream_t stream) {
     return with_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
-        if (a.n_seq * a.heads * ceil_div(a.dv, 128) >= 2 * kCus)
-            attend_step<T, 32><<<dim3(uint32_t(a.n_seq), uint32_t(a.heads), uint32_t(ceil_div(a.dv, 128))), 256, 0, stream>>>(a);
-        else
-            attend_step<T, 8><<<dim3(uint32_t(a.n_seq), uint32_t(a.heads), uint32_t(ceil_div(a.dv, 32))), 256, 0, stream>>>(a);
+        const int64_t narrow = ceil_div(a.dv, 32), wide = ceil_div(a.dv, 128);
+        const auto grid = [&](int64_t tiles) { return dim3(uint32_t(a.n_seq), uint32_t(a.heads), uint32_t(tiles)); };
+        // states that do not stay in the last cache until the next token (16 heads of 128 x 128: 192 streams 79 us,
+        // as if they stayed 87; 96 streams, which do stay, 33, as if they passed 44)
+        if (a.n_seq * a.heads * a.dk * a.dv * 4 >= kPassingStates) attend_step<T, 32, true><<<grid(wide), 256, 0, stream>>>(a);
+        else if (a.n_seq * a.heads * wide >= 2 * kCus) attend_step<T, 32, false><<<grid(wide), 256, 0, stream>>>(a);
+        else attend_step<T, 8, false><<<grid(narrow), 256, 0, stream>>>(a);
         return hipGetLastError();
     });
 }

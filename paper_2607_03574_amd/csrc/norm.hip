@@ -45,7 +45,7 @@ template <int L> __device__ inline float row_sum(float v, int t, float *lds) {
 }
 
 // L threads a row, NV vectors a thread.
-template <class T, int L, int NV> __global__ void __launch_bounds__(256) norm_rows(NormArgs a) {
+template <class T, int L, int NV, bool PASSING> __global__ void __launch_bounds__(256) norm_rows(NormArgs a) {
     constexpr int V = kVec<T>, R = 256 / L;
     __shared__ float lds[8];
     const int lane = threadIdx.x % L;
@@ -85,7 +85,7 @@ template <class T, int L, int NV> __global__ void __launch_bounds__(256) norm_ro
             if (b) bv = load_vec(b + c, a.n - c);
 #pragma unroll
             for (int j = 0; j < V; ++j) out[j] = T((float(xv[i][j]) - mean) * rstd * float(wv[j]) + float(bv[j]));
-            store_vec(y + c, out, a.n - c);
+            store_vec<PASSING>(y + c, out, a.n - c);
         }
         if (lane == 0) {
             if (a.mean) a.mean[row] = mean;
@@ -143,7 +143,7 @@ constexpr int64_t kLongCols = 256, kLongGroups = 64;
 // row, so its sums for dweight and dbias stay in registers over all rows of the
 // workgroup; at the end the workgroup's rows of threads are added in order and
 // one partial sum a workgroup goes to memory (no atomics: the sum's order is fixed).
-template <class T, int L, int NV, bool SUMS>
+template <class T, int L, int NV, bool SUMS, bool PASSING>
 __global__ void __launch_bounds__(kGradThreads) norm_grad_rows(NormGradArgs a) {
     constexpr int V = kVec<T>, R = kGradThreads / L;
     __shared__ float lds[2 * (L / 64) * R + 1];
@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_rows(NormGradArgs a) {
                         const float xh = (float(xv[i][j]) - mean) * rstd;
                         out[j] = T(rstd * (float(gv[i][j]) * float(wv[i][j]) - m1 - xh * m2));
                     }
-                    store_vec(dx + c, out, a.n - c);
+                    store_vec<PASSING>(dx + c, out, a.n - c);
                 }
             }
         }
@@ -339,7 +339,9 @@ hipError_t launch_norm(int dtype, const NormArgs &a, hipStream_t stream) {
         const bool held = with_shape<T>(a.n, [&](auto l, auto nv) {
             constexpr int L = decltype(l)::value, NV = decltype(nv)::value;
             const int64_t blocks = std::min<int64_t>(ceil_div(a.rows, 256 / L), 1 << 20);
-            norm_rows<T, L, NV><<<dim3(uint32_t(blocks)), 256, 0, stream>>>(a);
+            // results that pass the caches by leave them to what is read: 32768 x 2048 bf16 46 us, through them 55
+            if (2 * a.rows * a.n * int64_t(sizeof(T)) >= kPassingTraffic) norm_rows<T, L, NV, true><<<dim3(uint32_t(blocks)), 256, 0, stream>>>(a);
+            else norm_rows<T, L, NV, false><<<dim3(uint32_t(blocks)), 256, 0, stream>>>(a);
         });
         if (!held) norm_long<T><<<dim3(uint32_t(std::min<int64_t>(a.rows, 1 << 20))), 256, 0, stream>>>(a);
         return hipGetLastError();
@@ -358,8 +360,12 @@ hipError_t launch_norm_grad(int dtype, const NormGradArgs &a, hipStream_t stream
             constexpr int R = kGradThreads / L;
             groups = std::min(ceil_div(a.rows, R), sums ? kGradGroups : int64_t(1) << 20);
             if (groups == 0) return;
-            if (sums) norm_grad_rows<T, L, NV, true><<<dim3(uint32_t(groups)), kGradThreads, 0, stream>>>(a);
-            else norm_grad_rows<T, L, NV, false><<<dim3(uint32_t(groups)), kGradThreads, 0, stream>>>(a);
+            const bool passing = 3 * a.rows * a.n * int64_t(sizeof(T)) >= kPassingTraffic;      // 16384 x 2048 bf16: 47 us, else 50
+            const dim3 grid(static_cast<uint32_t>(groups));
+            if (sums && passing) norm_grad_rows<T, L, NV, true, true><<<grid, kGradThreads, 0, stream>>>(a);
+            else if (sums) norm_grad_rows<T, L, NV, true, false><<<grid, kGradThreads, 0, stream>>>(a);
+            else if (passing) norm_grad_rows<T, L, NV, false, true><<<grid, kGradThreads, 0, stream>>>(a);
+            else norm_grad_rows<T, L, NV, false, false><<<grid, kGradThreads, 0, stream>>>(a);
         });
         if (!held) {
             if (a.dx && a.rows) norm_grad_long<T><<<dim3(uint32_t(std::min<int64_t>(a.rows, 1 << 20))), 256, 0, stream>>>(a);

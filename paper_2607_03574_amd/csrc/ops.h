@@ -12,6 +12,9 @@ namespace ndvm {
 namespace ops {
 
 constexpr int64_t kCus = 256;    // compute units a launch is sized to fill
+// The last cache holds 256 MB.  Calls that read and write more than this in all, or streams whose states
+// are together more than that, mark data that they touch once as passing through.
+constexpr int64_t kPassingTraffic = int64_t(192) << 20, kPassingStates = int64_t(128) << 20;
 
 inline size_t type_bytes(int dtype) { return dtype == NDVM_F32 ? 4 : 2; }
 __host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }

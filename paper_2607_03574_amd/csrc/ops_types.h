@@ -30,9 +30,11 @@ template <class T> __device__ inline vec<T> load_vec(const T *p, int64_t count) 
         if (i < count) r[i] = p[i];
     return r;
 }
-template <class T> __device__ inline void store_vec(T *p, vec<T> v, int64_t count) {
+// PASSING: not to be kept in the caches.
+template <bool PASSING = false, class T> __device__ inline void store_vec(T *p, vec<T> v, int64_t count) {
     if (count >= kVec<T>) {
-        *reinterpret_cast<vec<T> *>(p) = v;
+        if (PASSING) __builtin_nontemporal_store(v, reinterpret_cast<vec<T> *>(p));
+        else *reinterpret_cast<vec<T> *>(p) = v;
         return;
     }
 #pragma unroll

@@ -367,6 +367,31 @@ def test_step_slots_and_agreement_with_the_chunked_form(nd):
     assert torch.equal(state[[0, 2, 3, 4]], before[[0, 2, 3, 4]])
 
 
+def test_calls_of_more_than_the_caches_hold(nd):
+    """Large calls mark data as passing through: the same values as those of their parts."""
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    r = lambda *s: torch.randn(s, generator=gen, device="cuda", dtype=torch.bfloat16)
+    x, w = r(26000, 2048), r(2048)
+    y, m, s = nd.layer_norm(x, w)
+    half = nd.layer_norm(x[:13000], w)
+    assert torch.equal(y[:13000], half[0]) and torch.equal(m[:13000], half[1])
+    dx = nd.layer_norm_grad(y, x, w, m, s, need_weight=False)[0]
+    assert torch.equal(dx[:13000], nd.layer_norm_grad(y[:13000], x[:13000], w, m[:13000], s[:13000], need_weight=False)[0])
+    g = torch.full((16,), -0.01, device="cuda")
+    q, k, v = (r(8, 1600, 16, 128) for _ in range(3))
+    o, last = nd.linear_attention(q, k, v, g, final_state=True)
+    # the sequences alone are cut elsewhere: sums in another order
+    for b in (0, 7):
+        o1, last1 = nd.linear_attention(q[b:b + 1], k[b:b + 1], v[b:b + 1], g, final_state=True)
+        assert float((o[b].float() - o1[0].float()).abs().max()) <= 2.0 ** -7 * float(o1.float().abs().max())
+        assert float((last[b] - last1[0]).abs().max()) <= 1e-5 * float(last1.abs().max())
+    state = torch.randn(140, 16, 128, 128, generator=gen, device="cuda")
+    q, k, v = (r(140, 16, 128) for _ in range(3))
+    few = state[:40].clone()        # enough streams for the same split of a state over threads
+    o = nd.linear_attention_step(q, k, v, g, state)
+    assert torch.equal(o[:40], nd.linear_attention_step(q[:40], k[:40], v[:40], g, few)) and torch.equal(state[:40], few)
+
+
 # ---------------------------------------------------------------- gated feed-forward
 FFN = [(1, 1, 1), (3, 17, 5), (17, 64, 96), (130, 72, 200), (65, 129, 63), (257, 256, 384), (16, 1000, 264)]
 
