@@ -404,6 +404,7 @@ ndvm_status ndvm_adam_step(double *params, const double *grad, double *m, double
  * contiguous; no alignment beyond the element's is needed.  As for the other
  * compute calls, arguments are checked before anything is enqueued, and a call
  * only enqueues on `stream`: it allocates nothing and waits for nothing.
+ * Where a result takes in an infinity it may be NaN (a float is multiplied in parts).
  * Outputs may not overlap inputs.  `workspace`: device memory of the size that
  * the operator's *_workspace_bytes call names (NULL where that is 0); nothing in
  * it needs a value, and its contents mean nothing afterwards.
@@ -433,7 +434,7 @@ ndvm_status ndvm_layer_norm_workspace_bytes(int64_t rows, int64_t n, size_t *byt
  * Gradient of ndvm_layer_norm from dy and the forward pass's x, weight, mean and
  * rstd.  dx, dweight, dbias: any may be NULL (not wanted); dweight and dbias [n]
  * are sums over all rows in float, added in a fixed order (the same bits in
- * every run) and rounded once; with rows = 0 they are 0.
+ * every run) and rounded once; with rows = 0 they are 0.  Limit: n <= 2^27.
  */
 ndvm_status ndvm_layer_norm_grad(int dtype, const void *dy, int64_t ld_dy, const void *x, int64_t ld_x, int64_t rows,
                                  int64_t n, const void *weight, const float *mean, const float *rstd, void *dx,
@@ -460,8 +461,8 @@ ndvm_status ndvm_layer_norm_grad(int dtype, const void *dy, int64_t ld_dy, const
  * Sequences without tokens are allowed (their final state is the initial one).
  * Offsets outside 0..n_tokens are read as the nearer end; where they decrease,
  * results are unspecified, with no access outside the tensors.
- * Limits: dk, dv <= 256, heads <= 65,535, n_tokens <= 2^30, and (n_tokens / 64 +
- * n_seq + 1) heads < 2^31.
+ * Limits: dk, dv <= 256, heads <= 65,535, n_tokens <= 2^30, and fewer than 2^24
+ * pairs of a sequence (or a piece that a long one is cut into) and a head.
  */
 typedef struct {
     int dtype;

@@ -714,15 +714,15 @@ __global__ void __launch_bounds__(256) attend_carry(AttendArgs A, uint32_t size)
 }
 
 template <class T> __global__ void __launch_bounds__(256) fold_heads(FoldHeadsArgs a) {
-    const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x;
     const int group = a.out.group;
-    if (at >= a.n_tokens * a.d) return;
-    const int64_t tok = at / a.d, c = at % a.d, kv = blockIdx.y;
-    float s = 0;
-    for (int i = 0; i < group; ++i) s += a.part[((kv * group + i) * a.n_tokens + tok) * a.d + c];
     const int64_t per = a.n_tokens / max(a.n_seq, int64_t(1));
-    const int64_t row = a.packed ? tok * a.out.tok : tok / per * a.out.seq + tok % per * a.out.tok;
-    static_cast<T *>(const_cast<void *>(a.out.p))[row + kv * a.out.head + c] = T(s);
+    for (int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x; at < a.n_tokens * a.d; at += int64_t(gridDim.x) * 256) {
+        const int64_t tok = at / a.d, c = at % a.d, kv = blockIdx.y;
+        float s = 0;
+        for (int i = 0; i < group; ++i) s += a.part[((kv * group + i) * a.n_tokens + tok) * a.d + c];
+        const int64_t row = a.packed ? tok * a.out.tok : tok / per * a.out.seq + tok % per * a.out.tok;
+        static_cast<T *>(const_cast<void *>(a.out.p))[row + kv * a.out.head + c] = T(s);
+    }
 }
 
 // One token of every stream: S <- lambda S + k^T v, o = scale q S.  Bound by the
@@ -867,7 +867,7 @@ hipError_t launch_attend(int dtype, const AttendArgs &a, hipStream_t stream) {
 hipError_t launch_fold_heads(int dtype, const FoldHeadsArgs &a, hipStream_t stream) {
     return with_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
-        fold_heads<T><<<dim3(uint32_t(ceil_div(a.n_tokens * a.d, 256)), uint32_t(a.heads / a.out.group)), 256, 0, stream>>>(a);
+        fold_heads<T><<<dim3(uint32_t(std::min(ceil_div(a.n_tokens * a.d, 256), kMostGroups)), uint32_t(a.heads / a.out.group)), 256, 0, stream>>>(a);
         return hipGetLastError();
     });
 }

@@ -99,24 +99,26 @@ template <class T> __global__ void __launch_bounds__(256) pack(PackArgs a) {
     typedef P p8 __attribute__((ext_vector_type(8)));
     constexpr int N = Parts<T>::count, V = kVec<T>;
     const int w = blockIdx.y;
-    const int64_t per = a.pad / 8, at = int64_t(blockIdx.x) * 256 + threadIdx.x, r = at / per, c = at % per * 8;
-    if (r >= a.rows[w]) return;
-    const T *from = static_cast<const T *>(a.from[w]) + r * a.ld[w] + c;
-    p8 part[N];
+    const int64_t per = a.pad / 8;
+    for (int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x; at < a.rows[w] * per; at += int64_t(gridDim.x) * 256) {
+        const int64_t r = at / per, c = at % per * 8;
+        const T *from = static_cast<const T *>(a.from[w]) + r * a.ld[w] + c;
+        p8 part[N];
 #pragma unroll
-    for (int j = 0; j < 8 / V; ++j) {
-        vec<T> v = T(0.0f);
-        if (c + j * V < a.cols) v = load_vec(from + j * V, a.cols - c - j * V);
+        for (int j = 0; j < 8 / V; ++j) {
+            vec<T> v = T(0.0f);
+            if (c + j * V < a.cols) v = load_vec(from + j * V, a.cols - c - j * V);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            P q[N];
-            Parts<T>::split(float(v[i]), q);
+            for (int i = 0; i < V; ++i) {
+                P q[N];
+                Parts<T>::split(float(v[i]), q);
 #pragma unroll
-            for (int k = 0; k < N; ++k) part[k][j * V + i] = q[k];
+                for (int k = 0; k < N; ++k) part[k][j * V + i] = q[k];
+            }
         }
-    }
 #pragma unroll
-    for (int k = 0; k < N; ++k) *reinterpret_cast<p8 *>(static_cast<P *>(a.to[w]) + k * a.plane[w] + r * a.pad + c) = part[k];
+        for (int k = 0; k < N; ++k) *reinterpret_cast<p8 *>(static_cast<P *>(a.to[w]) + k * a.plane[w] + r * a.pad + c) = part[k];
+    }
 }
 
 // ---- the product
@@ -824,7 +826,7 @@ template <class T> Operands operands(const FfnArgs &a, Space &s, hipStream_t str
     o.wg = copy(1, a.wg, a.n_out, a.ld_wg);
     o.wu = copy(2, a.wu, a.n_out, a.ld_wu);
     const int64_t most = std::max(a.rows, a.n_out) * (p.pad / 8);
-    pack<T><<<dim3(uint32_t(ceil_div(most, 256)), 3), 256, 0, stream>>>(p);
+    pack<T><<<dim3(uint32_t(std::min(ceil_div(most, 256), kMostGroups)), 3), 256, 0, stream>>>(p);
     return o;
 }
 

@@ -12,6 +12,8 @@ namespace ndvm {
 namespace ops {
 
 constexpr int64_t kCus = 256;    // compute units a launch is sized to fill
+// Workgroups of 256 threads along one axis of a launch, whose threads are counted in 32 bits.
+constexpr int64_t kMostGroups = (1 << 24) - 1;
 // The last cache holds 256 MB.  Calls that read and write more than this in all, or streams whose states
 // are together more than that, mark data that they touch once as passing through.
 constexpr int64_t kPassingTraffic = int64_t(192) << 20, kPassingStates = int64_t(128) << 20;
@@ -37,6 +39,7 @@ struct NormGradArgs {
     float *part;                // [groups][2][n] partial sums of dweight and dbias
     int64_t rows, n, ld_dy, ld_x, ld_dx;
 };
+constexpr int64_t kMostNormGrad = int64_t(1) << 27;     // values of a row
 size_t norm_grad_bytes(int64_t rows, int64_t n);
 hipError_t launch_norm_grad(int dtype, const NormGradArgs &a, hipStream_t stream);
 

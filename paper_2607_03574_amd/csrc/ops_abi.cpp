@@ -47,7 +47,11 @@ bool fits(int64_t a, int64_t b) { return a == 0 || b == 0 || a <= kMostElements 
 bool fits(int64_t a, int64_t b, int64_t c) { return fits(a, b) && fits(a * b, c); }
 
 // ---- linear attention
-ndvm_status check_shape(const char *who, const ndvm_attention_shape *s, bool tokens) {
+Cut cut_of(const ndvm_attention_shape *s, bool packed, int64_t da, int64_t dc) {
+    return attend_cut(s->dtype, s->n_seq, s->n_tokens, s->heads, da, dc, packed);
+}
+
+ndvm_status check_shape(const char *who, const ndvm_attention_shape *s, bool tokens, bool packed) {
     if (!s) return bad(who, "null shape");
     if (!known_type(s->dtype)) return bad(who, "unknown type");
     if (s->n_seq < 0 || s->heads < 1 || s->kv_heads < 1 || s->heads % s->kv_heads || s->dk < 1 || s->dv < 1)
@@ -55,12 +59,12 @@ ndvm_status check_shape(const char *who, const ndvm_attention_shape *s, bool tok
     if (s->heads > kMostHeads || s->dk > kMostHeadDim || s->dv > kMostHeadDim)
         return fail(NDVM_E_UNSUPPORTED, who, "more than 65,535 heads, or a head wider than 256");
     if (!std::isfinite(s->scale)) return bad(who, "scale is not finite");
-    if (s->n_seq > INT32_MAX / 2 || !fits(s->n_seq, s->heads, s->dk * s->dv)) return fail(NDVM_E_UNSUPPORTED, who, "too many sequences");
+    if (s->n_seq > kMostGroups || !fits(s->n_seq, s->heads, s->dk * s->dv)) return fail(NDVM_E_UNSUPPORTED, who, "too many sequences");
     if (!tokens) return NDVM_OK;
     if (s->n_tokens < 0 || (s->n_seq == 0 && s->n_tokens)) return bad(who, "bad token count");
     if (s->n_tokens > kMostTokens || !fits(s->n_tokens, s->heads, std::max(s->dk, s->dv)))
         return fail(NDVM_E_UNSUPPORTED, who, "too many tokens");
-    if (!fits(s->n_tokens / 64 + s->n_seq + 1, s->heads) || (s->n_tokens / 64 + s->n_seq + 1) * s->heads > INT32_MAX)
+    if (std::max(cut_of(s, packed, s->dk, s->dv).n_segments, cut_of(s, packed, s->dv, s->dk).n_segments) * s->heads > kMostGroups)
         return fail(NDVM_E_UNSUPPORTED, who, "too many sequences, tokens and heads for one launch");
     return NDVM_OK;
 }
@@ -73,10 +77,6 @@ bool bad_heads(const ndvm_heads *h, int64_t elements) {
 
 Heads heads_of(const ndvm_heads *h, int64_t group) {
     return Heads{h->data, h->seq_stride, h->tok_stride, h->head_stride, int(group)};
-}
-
-Cut cut_of(const ndvm_attention_shape *s, bool packed, int64_t da, int64_t dc) {
-    return attend_cut(s->dtype, s->n_seq, s->n_tokens, s->heads, da, dc, packed);
 }
 
 size_t segment_bytes(const ndvm_attention_shape *s, const Cut &c) {
@@ -124,7 +124,8 @@ ndvm_status ndvm_layer_norm_workspace_bytes(int64_t rows, int64_t n, size_t *byt
     return guarded([&]() -> ndvm_status {
         const char *who = "ndvm_layer_norm_workspace_bytes";
         if (!bytes) return bad(who, "null pointer");
-        if (rows < 0 || n < 1 || !fits(rows, n) || !fits(n, 4096)) return bad(who, "bad size");
+        if (rows < 0 || n < 1 || !fits(rows, n)) return bad(who, "bad size");
+        if (n > kMostNormGrad) return fail(NDVM_E_UNSUPPORTED, who, "more than 2^27 values in a row");
         *bytes = norm_grad_bytes(rows, n);
         return NDVM_OK;
     });
@@ -138,7 +139,8 @@ ndvm_status ndvm_layer_norm_grad(int dtype, const void *dy, int64_t ld_dy, const
         const char *who = "ndvm_layer_norm_grad";
         if (!known_type(dtype)) return bad(who, "unknown type");
         if (rows < 0 || n < 1 || ld_dy < n || ld_x < n || (dx && ld_dx < n)) return bad(who, "bad size or stride");
-        if (!fits(rows, std::max(std::max(ld_x, ld_dy), dx ? ld_dx : 0)) || !fits(n, 4096)) return bad(who, "sizes overflow");
+        if (!fits(rows, std::max(std::max(ld_x, ld_dy), dx ? ld_dx : 0))) return bad(who, "sizes overflow");
+        if (n > kMostNormGrad) return fail(NDVM_E_UNSUPPORTED, who, "more than 2^27 values in a row");
         if (rows && (!dy || !x || !mean || !rstd)) return bad(who, "null buffer");
         if (!dx && !dweight && !dbias) return NDVM_OK;
         if (dweight || dbias) {
@@ -155,7 +157,7 @@ ndvm_status ndvm_linear_attention_workspace_bytes(const ndvm_attention_shape *sh
     return guarded([&]() -> ndvm_status {
         const char *who = "ndvm_linear_attention_workspace_bytes";
         if (!bytes) return bad(who, "null pointer");
-        if (const ndvm_status st = check_shape(who, shape, true)) return st;
+        if (const ndvm_status st = check_shape(who, shape, true, packed != 0)) return st;
         *bytes = attention_bytes(shape, packed != 0, with_grad != 0);
         return NDVM_OK;
     });
@@ -163,7 +165,7 @@ ndvm_status ndvm_linear_attention_workspace_bytes(const ndvm_attention_shape *sh
 
 static ndvm_status check_call(const char *who, const ndvm_attention_shape *s, const ndvm_heads *q, const ndvm_heads *k,
                               const ndvm_heads *v, const float *log_decay, const int64_t *offsets) {
-    if (const ndvm_status st = check_shape(who, s, true)) return st;
+    if (const ndvm_status st = check_shape(who, s, true, offsets != nullptr)) return st;
     if (!offsets && s->n_seq && s->n_tokens % s->n_seq) return bad(who, "n_tokens is no multiple of n_seq, and there are no offsets");
     if (!q || !k || !v || (s->n_seq && !log_decay)) return bad(who, "null argument");
     if (bad_heads(q, s->n_tokens) || bad_heads(k, s->n_tokens) || bad_heads(v, s->n_tokens))
@@ -314,7 +316,7 @@ ndvm_status ndvm_linear_attention_step(const ndvm_attention_shape *shape, const 
     return guarded([&]() -> ndvm_status {
         const char *who = "ndvm_linear_attention_step";
         const ndvm_attention_shape *s = shape;
-        if (const ndvm_status st = check_shape(who, s, false)) return st;
+        if (const ndvm_status st = check_shape(who, s, false, false)) return st;
         if (n_slots < 0 || !fits(n_slots, s->heads, s->dk * s->dv) || (!slots && n_slots < s->n_seq))
             return bad(who, "bad slot count");
         if (!q || !k || !v || !o || bad_heads(q, s->n_seq) || bad_heads(k, s->n_seq) || bad_heads(v, s->n_seq) || bad_heads(o, s->n_seq))

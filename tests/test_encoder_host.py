@@ -135,6 +135,23 @@ def test_workspace_sizes_do_not_overflow():
     assert nd._attn_ws(shape(n_seq=1, n_tokens=1 << 16, heads=1, kv_heads=1), 0, 0, ctypes.byref(n)) == nd.OK and n.value > 0
 
 
+def test_launches_of_too_many_threads_are_refused():
+    # an axis of a launch has fewer than 2^32 threads
+    n = nd._sz()
+    for s, packed in ((shape(n_seq=1 << 24, n_tokens=1 << 24, heads=1, kv_heads=1), 0),
+                      (shape(n_seq=1 << 18, n_tokens=1 << 18, heads=64, kv_heads=64, dk=4, dv=4), 1)):
+        for grad in (0, 1):
+            assert nd._attn_ws(s, packed, grad, ctypes.byref(n)) == nd.E_UNSUPPORTED
+    assert nd._attn_ws(shape(n_seq=(1 << 24) - 1, n_tokens=0, heads=1, kv_heads=1), 0, 1, ctypes.byref(n)) == nd.OK
+    # many tokens are no reason: pieces grow with them
+    assert nd._attn_ws(shape(n_seq=1, n_tokens=1 << 30, heads=16, kv_heads=16), 1, 1, ctypes.byref(n)) == nd.OK
+    big = shape(n_seq=1 << 24, n_tokens=0, heads=1, kv_heads=1)
+    assert nd._attn_step(big, heads(), heads(), heads(), FAKE, FAKE, 1 << 25, FAKE, heads(), None) == nd.E_UNSUPPORTED
+    assert nd._norm_ws(8, 1 << 28, ctypes.byref(n)) == nd.E_UNSUPPORTED
+    assert nd._norm_grad(0, FAKE, 1 << 28, FAKE, 1 << 28, 4, 1 << 28, None, FAKE, FAKE, FAKE, 1 << 28, FAKE, FAKE, FAKE,
+                         1 << 50, None) == nd.E_UNSUPPORTED
+
+
 # ---------------------------------------------------------------- the references
 def differences(f, x, eps=1e-6):
     g = np.zeros_like(x)
