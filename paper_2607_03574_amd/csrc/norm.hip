@@ -161,23 +161,39 @@ __global__ void __launch_bounds__(kGradThreads) norm_grad_rows(NormGradArgs a) {
         for (int j = 0; j < V; ++j) dw[i][j] = db[i][j] = 0;
     }
     const int64_t step = int64_t(gridDim.x) * R;
+    // A row is read while the one before it is worked on, where the registers hold two.
+    constexpr bool AHEAD = NV <= 4;
+    vec<T> xv[NV], gv[NV], next_x[NV], next_g[NV];
+    float mean = 0, rstd = 0, next_mean = 0, next_rstd = 0;
+    const auto fetch = [&](int64_t row) __attribute__((always_inline)) {
+        if (row >= a.rows) return;
+        const T *x = static_cast<const T *>(a.x) + row * a.ld_x;
+        const T *dy = static_cast<const T *>(a.dy) + row * a.ld_dy;
+        next_mean = a.mean[row];
+        next_rstd = a.rstd[row];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int64_t c = int64_t(i * L + lane) * V;
+            next_x[i] = load_vec(x + c, a.n - c);
+            next_g[i] = load_vec(dy + c, a.n - c);      // 0 beyond the row: adds nothing anywhere
+        }
+    };
+    if (AHEAD) fetch(int64_t(blockIdx.x) * R + sub);
     // a workgroup's threads take the same number of turns (they meet at barriers)
     for (int64_t base = int64_t(blockIdx.x) * R; base < a.rows; base += step) {
         const int64_t row = base + sub;
         const bool on = row < a.rows;
-        vec<T> xv[NV], gv[NV];
-        float mean = 0, rstd = 0, s1 = 0, s2 = 0;
-        if (on) {
-            const T *x = static_cast<const T *>(a.x) + row * a.ld_x;
-            const T *dy = static_cast<const T *>(a.dy) + row * a.ld_dy;
-            mean = a.mean[row];
-            rstd = a.rstd[row];
+        if (!AHEAD) fetch(row);
+        mean = next_mean;
+        rstd = next_rstd;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int64_t c = int64_t(i * L + lane) * V;
-                xv[i] = load_vec(x + c, a.n - c);
-                gv[i] = load_vec(dy + c, a.n - c);      // 0 beyond the row: adds nothing anywhere
-            }
+        for (int i = 0; i < NV; ++i) {
+            xv[i] = next_x[i];
+            gv[i] = next_g[i];
+        }
+        if (AHEAD) fetch(row + step);
+        float s1 = 0, s2 = 0;
+        if (on) {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -315,7 +331,8 @@ template <class T, class F> bool with_shape(int64_t n, F f) {
     constexpr int64_t most = 32 / V;        // vectors a thread
     using std::integral_constant;
 #define NDVM_SHAPE(L, NV) \
-    if (NV <= most && v <= int64_t(L) * NV) return f(integral_constant<int, L>(), integral_constant<int, NV>()), true;
+    if constexpr (NV <= most) \
+        if (v <= int64_t(L) * NV) return f(integral_constant<int, L>(), integral_constant<int, NV>()), true;
     NDVM_SHAPE(16, 1)
     NDVM_SHAPE(16, 2)
     NDVM_SHAPE(64, 1)
