@@ -226,9 +226,9 @@ __global__ void __launch_bounds__(256) attend_general(AttendArgs A) {
 //    column each), tokens in the order that P^T has them.
 //  - A float is multiplied as bf16 parts, each the next 8 bits of it: half inputs are
 //    exactly two, float inputs three; what is left out of a product of parts is below 2^-24
-//    of it for float, 2^-16 for half.  The state stays float for every type: it enters
-//    its product as two parts (three for float), and takes c times its decay as three.  The
-//    products of a pair are one part for bfloat16, whose result has 8 bits too.
+//    of it for float, 2^-16 for half.  The state stays float for every type and takes c times
+//    its decay as three parts; what is read from it, and the products of a pair, are as many parts
+//    as an input: one for bfloat16, whose result has 8 bits too.
 // LDS rows lie in granules of 16 bytes, granule i of row r at i ^ swizzle(r): the 16 rows
 // that one instruction reads are then in different banks.
 typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -271,7 +271,7 @@ template <class T> constexpr int input_parts() { return sizeof(T) == 4 ? 3 : std
 template <class T, int DS, int NT, bool DIRECT, bool OUT, bool PASSING = false>
 __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(AttendArgs A) {
 #ifdef __HIP_DEVICE_COMPILE__
-    constexpr int PARTS = input_parts<T>(), ORDER = PARTS - 1, STATE = PARTS > 2 ? PARTS : 2;
+    constexpr int PARTS = input_parts<T>(), ORDER = PARTS - 1;
     constexpr int N = 32, GA = 4 * DS, GC = 8 * NT;      // tokens of a chunk; granules of a row
     constexpr int BYTES_A = OUT ? N * GA * 16 : 0, BYTES_B = N * GA * 16, BYTES_C = N * GC * 16;      // of a part
     constexpr int BYTES = BYTES_A + BYTES_B + BYTES_C;
@@ -522,11 +522,11 @@ __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(A
                 P11 = multiply<ORDER>(b1, a1, P11);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    bf16x8 state[STATE];
+                    bf16x8 state[PARTS];
 #pragma unroll
                     for (int r = 0; r < 8; ++r) split(S[2 * s + r / 4][nt][r % 4], state, r);
-                    O[0][nt] = multiply<STATE - 1>(state, a0, O[0][nt]);
-                    O[1][nt] = multiply<STATE - 1>(state, a1, O[1][nt]);
+                    O[0][nt] = multiply<ORDER>(state, a0, O[0][nt]);
+                    O[1][nt] = multiply<ORDER>(state, a1, O[1][nt]);
                 }
             }
             bf16x8 p[2][PARTS];
