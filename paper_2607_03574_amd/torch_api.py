@@ -11,6 +11,7 @@ own graph)."""
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import Tape, _launch_stream, adam_step, gated_ffn_grad, grad, layer_norm_grad, linear_attention_grad
 from . import gated_ffn as gated_ffn_op
@@ -69,6 +70,7 @@ class LayerNorm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, weight, mean, rstd = ctx.saved_tensors
         need_weight = ctx.needs_input_grad[1] or ctx.needs_input_grad[2]
@@ -92,6 +94,7 @@ class LinearAttention(torch.autograd.Function):
         return o, last
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, do, dlast):
         q, k, v, log_decay, offsets, s0 = ctx.saved_tensors
         if do is None:
@@ -106,7 +109,10 @@ class LinearAttention(torch.autograd.Function):
 
 def linear_attention(q, k, v, log_decay, offsets=None, scale=None, initial_state=None):
     """(o, final state) with autograd support for q, k, v and the initial state
-    (linear_attention of the package; the decay is a constant)."""
+    (linear_attention of the package; the decay is a constant, and refused where it
+    would need a gradient)."""
+    if log_decay.requires_grad and torch.is_grad_enabled():
+        raise ValueError("log_decay has no gradient: detach it")
     return LinearAttention.apply(q, k, v, log_decay, offsets, scale, initial_state)
 
 
@@ -118,6 +124,7 @@ class GatedFFN(torch.autograd.Function):
         return gated_ffn_op(x.detach(), w_gate.detach(), w_up.detach(), activation)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dh):
         x, w_gate, w_up = ctx.saved_tensors
         need_weight = ctx.needs_input_grad[1] or ctx.needs_input_grad[2]

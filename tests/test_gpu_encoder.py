@@ -533,6 +533,21 @@ def test_gradients_against_differences(nd, op):
         assert abs(got - want) <= 2e-3 * size, (op, i, got, want, size)
 
 
+def test_gradients_that_there_are_not(nd):
+    """A gradient of a gradient, and the decay's: an error, not a missing term."""
+    from paper_2607_03574_amd import torch_api
+    r = lambda *s: torch.randn(s, device="cuda", requires_grad=True)
+    q, g = r(1, 9, 2, 8), torch.full((2,), -0.1, device="cuda")
+    with pytest.raises(ValueError):
+        torch_api.linear_attention(q, q, q, g.clone().requires_grad_())
+    x, w = r(5, 8), r(12, 8)
+    for y in (torch_api.layer_norm(x), torch_api.linear_attention(q, q, q, g)[0], torch_api.gated_ffn(x, w, w)):
+        leaf = q if y.dim() == 4 else x
+        first, = torch.autograd.grad(y.sum(), leaf, create_graph=True)
+        with pytest.raises(RuntimeError):
+            first.sum().backward()
+
+
 # ---------------------------------------------------------------- streams, graphs, refusals
 def test_other_streams_and_graphs(nd):
     gen = torch.Generator(device="cuda").manual_seed(8)
