@@ -264,24 +264,36 @@ template <int ORDER, int NX, int NY> __device__ inline f32x4 multiply(const bf16
 #endif
 template <class T> constexpr int input_parts() { return sizeof(T) == 4 ? 3 : std::is_same<T, f16>::value ? 2 : 1; }
 
+// The segment and head of its set that a workgroup has, and the set: the sets of a segment and head lie eight
+// workgroups apart, on the same XCD, since they read the same tensors.  Heads first: workgroups that run
+// together read whole rows of memory between them.
+__device__ inline uint32_t place_of(const AttendArgs &) { return blockIdx.x; }
+__device__ inline uint32_t place_of(const AttendSets &s) { return blockIdx.x / 8 / s.count * 8 + blockIdx.x % 8; }
+__device__ inline const AttendArgs &set_of(const AttendArgs &a) { return a; }
+__device__ inline const AttendArgs &set_of(const AttendSets &s) { return s.set[blockIdx.x / 8 % s.count]; }
+
 // DS: widths of a and b in 32s.  DIRECT (bfloat16): rows are 16-byte granules at 16-byte
 // addresses, loaded to LDS directly, two chunks ahead; else through registers, one ahead.
-// PASSING: a and the outputs, which this launch alone touches, are more than the last cache should
-// hold next to b and c, which the launch before has read too.
-template <class T, int DS, int NT, bool DIRECT, bool OUT, bool PASSING = false>
-__global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(AttendArgs A) {
+// Args: AttendSets, or AttendArgs of a single set, whose values stay in scalar registers (16384 tokens x 16
+// heads 105 us, found by a set's number 115).
+// PASSING: the outputs, and a where no other set reads it, which this launch alone touches, are more than the
+// last cache should hold next to b and c, which the launch before has read too.
+template <class T, int DS, int NT, bool DIRECT, bool OUT, class Args, bool PASSING = false>
+__global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(Args args) {
 #ifdef __HIP_DEVICE_COMPILE__
+    constexpr bool MANY = std::is_same<Args, AttendSets>::value;
     constexpr int PARTS = input_parts<T>(), ORDER = PARTS - 1;
     constexpr int N = 32, GA = 4 * DS, GC = 8 * NT;      // tokens of a chunk; granules of a row
     constexpr int BYTES_A = OUT ? N * GA * 16 : 0, BYTES_B = N * GA * 16, BYTES_C = N * GC * 16;      // of a part
     constexpr int BYTES = BYTES_A + BYTES_B + BYTES_C;
     __shared__ __align__(1024) char buffer0[PARTS * BYTES], buffer1[DIRECT ? BYTES : 16], buffer2[DIRECT ? BYTES : 16];
     __shared__ float power[N + 2];      // lambda^n
-    // heads first: workgroups that run together read whole rows of memory between them
-    const uint32_t id = blockIdx.x / uint32_t(A.heads);
+    const AttendArgs &A = set_of(args);
+    const uint32_t place = place_of(args), id = place / uint32_t(A.heads);
+    if (MANY && id >= uint32_t(A.n_segments)) return;
     const Segment g = find_segment(A, id);
     if (g.count == 0 || (!OUT && g.index == g.count - 1)) return;
-    const int64_t h = blockIdx.x - id * uint32_t(A.heads), col0 = int64_t(blockIdx.y) * 64 * NT;
+    const int64_t h = place - id * uint32_t(A.heads), col0 = int64_t(blockIdx.y) * 64 * NT;
     const int l = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lm = l % 16, lg = l / 16;
     const float gl = A.log_decay[h];
     const int e = A.reversed ? 0 : 1;
@@ -327,7 +339,7 @@ __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(A
     const integral_constant<int, LC> count_c;
     const auto load_chunk = [&](char *to, int base) __attribute__((always_inline)) {
         const std::false_type stays;
-        if (OUT) load(A.a, ra, to, granules_a, count_a, 0, A.da, base, integral_constant<bool, PASSING>());
+        if (OUT) load(A.a, ra, to, granules_a, count_a, 0, A.da, base, integral_constant<bool, PASSING && !MANY>());
         load(A.b, rb, to + BYTES_A, granules_a, count_a, 0, A.da, base, stays);
         load(A.c, rc, to + BYTES_A + BYTES_B, granules_c, count_c, col0, A.dc, base, stays);
     };
@@ -380,11 +392,11 @@ __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(A
     const auto column = [&](int nt) { return col0 + wave * 16 * NT + (NT == 2 ? lm / 4 * 8 + nt * 4 + lm % 4 : lm); };
     // A segment's state lies in memory as in the registers.
     f32x4 S[2 * DS][NT];
-    f32x4 *mine = reinterpret_cast<f32x4 *>(A.segments) + ((int64_t(blockIdx.x) * gridDim.y + blockIdx.y) * 4 + wave) * (2 * DS * NT * 64) + l;
+    f32x4 *mine = reinterpret_cast<f32x4 *>(A.segments) + ((int64_t(place) * gridDim.y + blockIdx.y) * 4 + wave) * (2 * DS * NT * 64) + l;
     if (OUT && g.index > 0 && A.shared_segments) {
-        // the states as a call for the transposed sums left them: its tiles, waves and lanes by (column, width)
+        // the states as the transposed sum left them: its tiles, waves and lanes by (column, width)
         const int nt_of = A.da <= 64 ? 1 : 2, tiles = (A.dc <= 64 ? 4 : 8) * nt_of;
-        const float *theirs = A.segments + int64_t(blockIdx.x) * (4 * 2 * DS * NT * 256);
+        const float *theirs = A.segments + int64_t(place) * (4 * 2 * DS * NT * 256);
 #pragma unroll
         for (int t = 0; t < 2 * DS; ++t)
 #pragma unroll
@@ -679,9 +691,12 @@ __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(A
 // States over the segments of a sequence, in order: what each adds is replaced
 // by what enters it (the first one's stays).  A thread four values of the state,
 // wherever they lie; U segments' are read at once.  size: a multiple of 4.
-__global__ void __launch_bounds__(256) attend_carry(AttendArgs A, uint32_t size) {
+__device__ inline const AttendArgs &carried_set(const AttendArgs &a, uint32_t) { return a; }
+__device__ inline const AttendArgs &carried_set(const AttendSets &s, uint32_t tiles) { return s.set[blockIdx.z / tiles]; }
+template <class Args> __global__ void __launch_bounds__(256) attend_carry(Args args, uint32_t size) {
     constexpr int U = 8;
-    const uint32_t at = blockIdx.z * 256 + threadIdx.x;
+    const uint32_t tiles = (size + 1023) / 1024, at = blockIdx.z % tiles * 256 + threadIdx.x;
+    const AttendArgs &A = carried_set(args, tiles);
     const uint32_t seq = blockIdx.x, h = blockIdx.y;
     uint32_t id, count;
     if (!A.offsets) {
@@ -713,7 +728,8 @@ __global__ void __launch_bounds__(256) attend_carry(AttendArgs A, uint32_t size)
     }
 }
 
-template <class T> __global__ void __launch_bounds__(256) fold_heads(FoldHeadsArgs a) {
+template <class T> __global__ void __launch_bounds__(256) fold_heads(FoldHeadsSets sets) {
+    const FoldHeadsArgs &a = sets.set[blockIdx.z];
     const int group = a.out.group;
     const int64_t per = a.n_tokens / max(a.n_seq, int64_t(1));
     for (int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x; at < a.n_tokens * a.d; at += int64_t(gridDim.x) * 256) {
@@ -781,30 +797,24 @@ template <class T, int X, bool PASSING> __global__ void __launch_bounds__(256) a
     for (int j = 0; j < have; ++j) o[c + j] = T(sum[j] * a.scale);
 }
 
-void launch_carry(const AttendArgs &a, int64_t size, hipStream_t stream) {
-    attend_carry<<<dim3(uint32_t(a.n_seq), uint32_t(a.heads), uint32_t(ceil_div(size, 1024))), 256, 0, stream>>>(a, uint32_t(size));
+void launch_carry(const AttendSets &s, int64_t size, hipStream_t stream) {
+    const AttendArgs &a = s.set[0];
+    const dim3 grid(uint32_t(a.n_seq), uint32_t(a.heads), uint32_t(ceil_div(size, 1024) * s.count));
+    if (s.count == 1) attend_carry<<<grid, 256, 0, stream>>>(a, uint32_t(size));
+    else attend_carry<<<grid, 256, 0, stream>>>(s, uint32_t(size));
 }
 
-template <class T, int DT, int STAGE> void launch_general(const AttendArgs &a, hipStream_t stream) {
-    const dim3 grid(uint32_t(a.n_segments * a.heads), uint32_t(ceil_div(a.dc, 64)));
-    if (a.n_segments > a.n_seq) {
-        attend_general<T, DT, STAGE, false><<<grid, 256, 0, stream>>>(a);
-        launch_carry(a, ceil_div(a.da * a.dc, 4) * 4, stream);
-    }
-    attend_general<T, DT, STAGE, true><<<grid, 256, 0, stream>>>(a);
+template <class T, bool OUT> void launch_general(const AttendArgs &a, hipStream_t stream) {
+    attend_general<T, 16, 16, OUT><<<dim3(uint32_t(a.n_segments * a.heads), uint32_t(ceil_div(a.dc, 64))), 256, 0, stream>>>(a);
 }
 
-template <class T, int DS, int NT, bool DIRECT> void launch_parts(const AttendArgs &a, hipStream_t stream) {
-    const dim3 grid(uint32_t(a.n_segments * a.heads), uint32_t(ceil_div(a.dc, 64 * NT)));
-    if (a.n_segments > a.n_seq && !a.shared_segments) {
-        attend_parts<T, DS, NT, DIRECT, false><<<grid, 256, 0, stream>>>(a);
-        launch_carry(a, int64_t(grid.y) * 4 * 2 * DS * NT * 256, stream);
-    }
-    if (a.only_segments) return;
-    // 16 heads x 16384 tokens of 128 (268 MB): 119 us, against 129 with all data as if it stayed
-    const bool passing = DIRECT && a.n_tokens * a.heads * (a.da + a.dc) * 4 >= kPassingTraffic;
-    if (passing) attend_parts<T, DS, NT, DIRECT, true, DIRECT><<<grid, 256, 0, stream>>>(a);
-    else attend_parts<T, DS, NT, DIRECT, true><<<grid, 256, 0, stream>>>(a);
+template <int NT> dim3 parts_grid(const AttendSets &s) {
+    const int64_t n = s.set[0].n_segments * s.set[0].heads;
+    return dim3(uint32_t(s.count == 1 ? n : ceil_div(n, 8) * 8 * s.count), uint32_t(ceil_div(s.set[0].dc, 64 * NT)));
+}
+template <class T, int DS, int NT, bool DIRECT, bool OUT, bool PASSING> void launch_parts(const AttendSets &s, hipStream_t stream) {
+    if (s.count == 1) attend_parts<T, DS, NT, DIRECT, OUT, AttendArgs, PASSING><<<parts_grid<NT>(s), 256, 0, stream>>>(s.set[0]);
+    else attend_parts<T, DS, NT, DIRECT, OUT, AttendSets, PASSING><<<parts_grid<NT>(s), 256, 0, stream>>>(s);
 }
 
 // Whether rows can be loaded to LDS directly: whole granules at 16-byte addresses, and
@@ -813,11 +823,31 @@ bool direct(const AttendArgs &a, const Heads &h, int64_t width) {
     return reinterpret_cast<uintptr_t>(h.p) % 16 == 0 && h.tok % 8 == 0 && h.head % 8 == 0 && (a.offsets || h.seq % 8 == 0) && width % 8 == 0 && h.tok < (1 << 24);
 }
 
-template <class T, bool DIRECT> void launch_parts(const AttendArgs &a, hipStream_t stream) {
-    if (a.da <= 64 && a.dc <= 64) launch_parts<T, 2, 1, DIRECT>(a, stream);
-    else if (a.da <= 64) launch_parts<T, 2, 2, DIRECT>(a, stream);
-    else if (a.dc <= 64) launch_parts<T, 4, 1, DIRECT>(a, stream);
-    else launch_parts<T, 4, 2, DIRECT>(a, stream);
+// Calls f with the sizes that the kernel is built for.
+template <class T, class F> void with_parts(const AttendArgs &a, F f) {
+    using std::integral_constant;
+    const auto sized = [&](auto d) {
+        const integral_constant<int, 1> one;
+        const integral_constant<int, 2> two;
+        const integral_constant<int, 4> four;
+        if (a.da <= 64 && a.dc <= 64) f(two, one, d);
+        else if (a.da <= 64) f(two, two, d);
+        else if (a.dc <= 64) f(four, one, d);
+        else f(four, two, d);
+    };
+    if constexpr (std::is_same<T, bf16>::value)
+        if (direct(a, a.a, a.da) && direct(a, a.b, a.da) && direct(a, a.c, a.dc)) return sized(std::true_type());
+    sized(std::false_type());
+}
+
+// Whether one launch can form both.
+template <class T> bool together(const AttendArgs &a, const AttendArgs &b) {
+    const auto kind = [](const AttendArgs &x) {
+        int64_t k = 0;
+        with_parts<T>(x, [&](auto ds, auto nt, auto d) { k = (ds.value * 4 + nt.value) * 2 + d.value; });
+        return k * 8 + ceil_div(x.dc, 64);
+    };
+    return kind(a) == kind(b);
 }
 
 }  // namespace
@@ -829,17 +859,26 @@ template <class T, bool DIRECT> void launch_parts(const AttendArgs &a, hipStream
 // 100: 29 us; of 128, 36).  A packed batch is cut wherever a sequence may be longer than that: its
 // longest sequence is not known here, and would be walked by one workgroup while the others
 // are done.
-Cut attend_cut(int dtype, int64_t n_seq, int64_t n_tokens, int64_t heads, int64_t da, int64_t dc, bool packed) {
+// Sequences of equal length are left whole where they fill three quarters of the compute units: one walk of
+// longer chains takes less than three launches and the states' way through memory (16 heads of
+// 128, bfloat16: 16 x 1024 tokens 63 us, cut 96; gradient of 8 x 2048 184, cut 227; of 4 x 4096 254, cut 270; of
+// 3 x 4096, which are too few, 254, cut 204).  Heads of up to 64 in 16 bits have shorter
+// chunks, and three workgroups on a compute unit hide each other's latency: past 1536 tokens they gain from
+// pieces (gradient of 4 x 4096: cut 117 us, whole 156; of 16 x 1024 forward: cut 43, whole 34).
+Cut attend_cut(int dtype, int64_t n_seq, int64_t n_tokens, int64_t heads, int64_t da, int64_t dc, bool packed, int sets) {
     const int64_t least = dtype == NDVM_F32 ? 64 : 128;
     const bool matrix = da <= kMostPartsDim;
     const int64_t cols = matrix && dc > 64 ? 128 : 64;
     Cut c;
     c.state = matrix ? (da <= 64 ? 64 : 128) * ceil_div(dc, cols) * cols : ceil_div(da * dc, 4) * 4;
     const int64_t longest = packed || n_seq == 0 ? n_tokens : n_tokens / n_seq;
-    const int64_t want = std::max<int64_t>(1, 2 * kCus / (heads * ceil_div(dc, cols)));
+    const int64_t want = std::max<int64_t>(1, 2 * kCus / (heads * ceil_div(dc, cols) * sets));
     int64_t len = std::max<int64_t>(least, n_tokens / want);
     len = ceil_div(len, kSegStep) * kSegStep;
-    if (len >= longest || (!packed && n_seq >= want)) {
+    const int64_t groups = n_seq * heads * ceil_div(dc, cols) * sets;
+    const bool short_chunks = std::max(da, dc) <= 64 && dtype != NDVM_F32;
+    const bool whole = !packed && (n_seq >= want || (matrix && groups >= kCus * 3 / 4 && (!short_chunks || longest <= 1536)));
+    if (len >= longest || whole) {
         c.seg_len = std::max<int64_t>(longest, 1);
         c.n_segments = n_seq;
     } else if (packed) {
@@ -853,21 +892,69 @@ Cut attend_cut(int dtype, int64_t n_seq, int64_t n_tokens, int64_t heads, int64_
     return c;
 }
 
-hipError_t launch_attend(int dtype, const AttendArgs &a, hipStream_t stream) {
+hipError_t launch_attend_segments(int dtype, const AttendSets &s, hipStream_t stream) {
     return with_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
-        if (a.da > kMostPartsDim) launch_general<T, 16, 16>(a, stream);
-        else if (std::is_same<T, bf16>::value && direct(a, a.a, a.da) && direct(a, a.b, a.da) && direct(a, a.c, a.dc))
-            launch_parts<bf16, true>(a, stream);
-        else launch_parts<T, false>(a, stream);
+        const AttendArgs &a = s.set[0];
+        if (a.n_segments <= a.n_seq) return hipSuccess;
+        if (a.da > kMostPartsDim) {
+            for (int i = 0; i < s.count; ++i) launch_general<T, false>(s.set[i], stream);
+            launch_carry(s, ceil_div(a.da * a.dc, 4) * 4, stream);
+            return hipGetLastError();
+        }
+        AttendSets run{};
+        const auto launch = [&]() {
+            with_parts<T>(run.set[0], [&](auto ds, auto nt, auto d) {
+                launch_parts<T, ds.value, nt.value, d.value, false, false>(run, stream);
+            });
+            run.count = 0;
+        };
+        for (int i = 0; i < s.count; ++i) {
+            if (run.count && !together<T>(run.set[0], s.set[i])) launch();
+            run.set[run.count++] = s.set[i];
+        }
+        launch();
+        const int64_t cols = a.dc <= 64 ? 64 : ceil_div(a.dc, 128) * 128;
+        launch_carry(s, (a.da <= 64 ? 64 : 128) * cols, stream);
         return hipGetLastError();
     });
 }
 
-hipError_t launch_fold_heads(int dtype, const FoldHeadsArgs &a, hipStream_t stream) {
+hipError_t launch_attend(int dtype, const AttendSets &s, hipStream_t stream) {
     return with_type(dtype, [&](auto zero) {
         typedef decltype(zero) T;
-        fold_heads<T><<<dim3(uint32_t(std::min(ceil_div(a.n_tokens * a.d, 256), kMostGroups)), uint32_t(a.heads / a.out.group)), 256, 0, stream>>>(a);
+        bool done[kMostSets] = {};
+        for (int i = 0; i < s.count; ++i) {
+            if (done[i]) continue;
+            if (s.set[i].da > kMostPartsDim) {
+                launch_general<T, true>(s.set[i], stream);
+                continue;
+            }
+            AttendSets run{};
+            for (int j = i; j < s.count; ++j) {
+                const bool fits = ceil_div(s.set[j].n_segments * s.set[j].heads, 8) * 8 * (run.count + 1) <= kMostGroups;
+                if (done[j] || s.set[j].da > kMostPartsDim || (run.count && !(fits && together<T>(s.set[i], s.set[j])))) continue;
+                done[j] = true;
+                run.set[run.count++] = s.set[j];
+            }
+            with_parts<T>(run.set[0], [&](auto ds, auto nt, auto d) {
+                const AttendArgs &a = run.set[0];
+                // 16 heads x 16384 tokens of 128 (268 MB): 119 us, against 129 with all data as if it stayed
+                const bool passing = d.value && a.n_tokens * a.heads * (a.da + a.dc) * 4 >= kPassingTraffic;
+                if (passing) launch_parts<T, ds.value, nt.value, d.value, true, d.value>(run, stream);
+                else launch_parts<T, ds.value, nt.value, d.value, true, false>(run, stream);
+            });
+        }
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_fold_heads(int dtype, const FoldHeadsSets &s, hipStream_t stream) {
+    return with_type(dtype, [&](auto zero) {
+        typedef decltype(zero) T;
+        const FoldHeadsArgs &a = s.set[0];
+        const int64_t most = a.n_tokens * std::max(a.d, s.set[s.count - 1].d);
+        fold_heads<T><<<dim3(uint32_t(std::min(ceil_div(most, 256), kMostGroups)), uint32_t(a.heads / a.out.group), uint32_t(s.count)), 256, 0, stream>>>(s);
         return hipGetLastError();
     });
 }

@@ -63,24 +63,37 @@ struct AttendArgs {
     int reversed;
     int state_transposed;       // state_in and state_out are [dc, da]
     int out_f32;                // `out` is float whatever the type
-    int only_segments;          // no outputs: `segments` for a call that shares them
-    int shared_segments;        // `segments` hold what a call with b and c exchanged has left there (widths up to 128)
+    int shared_segments;        // `segments` are those of a sum with b and c exchanged (widths up to 128)
+};
+// Sums over the same sequences and heads, cut alike, that one launch forms together.
+constexpr int kMostSets = 3;
+struct AttendSets {
+    AttendArgs set[kMostSets];
+    int count;
 };
 constexpr int64_t kSegStep = 64, kMostPartsDim = 128, kMostHeadDim = 256, kMostHeads = 65535, kMostTokens = 1 << 30;
 struct Cut {
     int64_t seg_len, n_segments;    // more segments than sequences: sequences are cut
     int64_t state;                  // floats of a segment's and head's state
 };
-Cut attend_cut(int dtype, int64_t n_seq, int64_t n_tokens, int64_t heads, int64_t da, int64_t dc, bool packed);
-hipError_t launch_attend(int dtype, const AttendArgs &a, hipStream_t stream);
-// sum of `group` consecutive heads of float [heads][tokens][d] into `out` [.., heads / group, d]
+// sets: how many sums a launch forms together
+Cut attend_cut(int dtype, int64_t n_seq, int64_t n_tokens, int64_t heads, int64_t da, int64_t dc, bool packed, int sets);
+// What enters each segment of sums of the same widths, where there are more segments than sequences.
+hipError_t launch_attend_segments(int dtype, const AttendSets &s, hipStream_t stream);
+// The outputs, and the states that the sequences end with.
+hipError_t launch_attend(int dtype, const AttendSets &s, hipStream_t stream);
+// sums of `group` consecutive heads of float [heads][tokens][d] into `out` [.., heads / group, d], two at most
 struct FoldHeadsArgs {
     const float *part;
     Heads out;
     int64_t n_seq, n_tokens, heads, d;
     bool packed;
 };
-hipError_t launch_fold_heads(int dtype, const FoldHeadsArgs &a, hipStream_t stream);
+struct FoldHeadsSets {
+    FoldHeadsArgs set[2];
+    int count;
+};
+hipError_t launch_fold_heads(int dtype, const FoldHeadsSets &s, hipStream_t stream);
 
 struct StepArgs {
     Heads q, k, v, o;           // seq and head strides

@@ -47,8 +47,15 @@ bool fits(int64_t a, int64_t b) { return a == 0 || b == 0 || a <= kMostElements 
 bool fits(int64_t a, int64_t b, int64_t c) { return fits(a, b) && fits(a * b, c); }
 
 // ---- linear attention
-Cut cut_of(const ndvm_attention_shape *s, bool packed, int64_t da, int64_t dc) {
-    return attend_cut(s->dtype, s->n_seq, s->n_tokens, s->heads, da, dc, packed);
+Cut cut_of(const ndvm_attention_shape *s, bool packed, int64_t da, int64_t dc, int sets = 1) {
+    return attend_cut(s->dtype, s->n_seq, s->n_tokens, s->heads, da, dc, packed, sets);
+}
+
+// The gradient's three sums: of widths up to 128 they are cut alike and formed together, those of dq and dk in one
+// launch, with dv where its widths have the same kernel; dk and dv start from the same segments' sums.
+bool grad_together(const ndvm_attention_shape *s) { return std::max(s->dk, s->dv) <= kMostPartsDim; }
+Cut grad_cut(const ndvm_attention_shape *s, bool packed) {
+    return cut_of(s, packed, s->dk, s->dv, (s->dk <= 64) == (s->dv <= 64) ? 3 : 2);
 }
 
 ndvm_status check_shape(const char *who, const ndvm_attention_shape *s, bool tokens, bool packed) {
@@ -83,10 +90,14 @@ size_t segment_bytes(const ndvm_attention_shape *s, const Cut &c) {
     return c.n_segments > s->n_seq ? round256(size_t(c.n_segments * s->heads) * size_t(c.state) * 4) : 0;
 }
 
-// of the gradient's calls
+// of the gradient's calls: one for dq, one for dk and dv
 size_t grad_segment_bytes(const ndvm_attention_shape *s, bool packed) {
+    if (grad_together(s)) return 2 * segment_bytes(s, grad_cut(s, packed));
     return std::max(segment_bytes(s, cut_of(s, packed, s->dk, s->dv)), segment_bytes(s, cut_of(s, packed, s->dv, s->dk)));
 }
+
+// a gradient for each query head, before those that share a key are added up
+size_t grad_part_bytes(const ndvm_attention_shape *s, int64_t d) { return round256(size_t(s->heads * s->n_tokens) * size_t(d) * 4); }
 
 size_t attention_bytes(const ndvm_attention_shape *s, bool packed, bool grad) {
     if (!grad) {
@@ -94,7 +105,7 @@ size_t attention_bytes(const ndvm_attention_shape *s, bool packed, bool grad) {
         return n ? n + 256 : 0;
     }
     size_t n = grad_segment_bytes(s, packed) + 256;
-    if (s->heads > s->kv_heads) n += round256(size_t(s->heads * s->n_tokens) * size_t(std::max(s->dk, s->dv)) * 4);
+    if (s->heads > s->kv_heads) n += grad_part_bytes(s, s->dk) + grad_part_bytes(s, s->dv);
     return n;
 }
 
@@ -188,7 +199,9 @@ ndvm_status ndvm_linear_attention(const ndvm_attention_shape *shape, const ndvm_
         if (need && !workspace) return bad(who, "null workspace");
         const Cut cut = cut_of(s, offsets != nullptr, s->dk, s->dv);
         const int64_t group = s->heads / s->kv_heads;
-        AttendArgs a{};
+        AttendSets sets{};
+        sets.count = 1;
+        AttendArgs &a = sets.set[0];
         a.a = heads_of(q, 1);
         a.b = heads_of(k, group);
         a.c = heads_of(v, group);
@@ -207,7 +220,8 @@ ndvm_status ndvm_linear_attention(const ndvm_attention_shape *shape, const ndvm_
         a.n_segments = cut.n_segments;
         a.scale_pair = a.scale_read = float(s->scale);
         a.scale_add = 1.0f;
-        return launched(who, launch_attend(s->dtype, a, static_cast<hipStream_t>(stream)));
+        if (const ndvm_status r = launched(who, launch_attend_segments(s->dtype, sets, static_cast<hipStream_t>(stream)))) return r;
+        return launched(who, launch_attend(s->dtype, sets, static_cast<hipStream_t>(stream)));
     });
 }
 
@@ -230,83 +244,88 @@ ndvm_status ndvm_linear_attention_grad(const ndvm_attention_shape *shape, const 
         const hipStream_t st = static_cast<hipStream_t>(stream);
         const int64_t group = s->heads / s->kv_heads;
         const Heads hq = heads_of(q, 1), hk = heads_of(k, group), hv = heads_of(v, group), ho = heads_of(d_o, 1);
+        const bool packed = offsets != nullptr, together = grad_together(s);
         char *ws = static_cast<char *>(aligned(workspace));
-        AttendArgs a{};
-        a.log_decay = log_decay;
-        a.offsets = offsets;
-        a.n_seq = s->n_seq;
-        a.n_tokens = s->n_tokens;
-        a.heads = s->heads;
-        a.segments = reinterpret_cast<float *>(ws);
-        const auto widths = [&](int64_t da, int64_t dc) {
-            const Cut cut = cut_of(s, offsets != nullptr, da, dc);
+        const size_t segments = grad_segment_bytes(s, packed);
+        float *const of_q = reinterpret_cast<float *>(ws), *const of_kv = reinterpret_cast<float *>(ws + (together ? segments / 2 : 0));
+        float *part = reinterpret_cast<float *>(ws + segments);
+        AttendArgs all{};
+        all.log_decay = log_decay;
+        all.offsets = offsets;
+        all.n_seq = s->n_seq;
+        all.n_tokens = s->n_tokens;
+        all.heads = s->heads;
+        const auto widths = [&](AttendArgs &a, int64_t da, int64_t dc) {
+            const Cut cut = together ? grad_cut(s, packed) : cut_of(s, packed, da, dc);
             a.da = da;
             a.dc = dc;
             a.seg_len = cut.seg_len;
             a.n_segments = cut.n_segments;
         };
-        if (dq->data) {
-            a.a = ho;
-            a.b = hv;
-            a.c = hk;
-            a.out = heads_of(dq, 1);
-            widths(s->dv, s->dk);
-            a.state_in = initial_state;
-            a.state_transposed = 1;
-            a.scale_pair = a.scale_read = float(s->scale);
-            a.scale_add = 1.0f;
-            if (const ndvm_status r = launched(who, launch_attend(s->dtype, a, st))) return r;
-        }
-        a.reversed = 1;
-        a.state_in = d_final;
-        a.scale_pair = a.scale_add = float(s->scale);
-        a.scale_read = 1.0f;
-        const size_t segments = grad_segment_bytes(s, offsets != nullptr);
-        float *part = reinterpret_cast<float *>(ws + segments);
+        AttendArgs of_dq = all;
+        of_dq.a = ho;
+        of_dq.b = hv;
+        of_dq.c = hk;
+        of_dq.out = heads_of(dq, 1);
+        widths(of_dq, s->dv, s->dk);
+        of_dq.state_in = initial_state;
+        of_dq.state_transposed = 1;
+        of_dq.scale_pair = of_dq.scale_read = float(s->scale);
+        of_dq.scale_add = 1.0f;
+        of_dq.segments = of_q;
+        all.reversed = 1;
+        all.state_in = d_final;
+        all.scale_pair = all.scale_add = float(s->scale);
+        all.scale_read = 1.0f;
+        all.segments = of_kv;
         // over the query heads of a group: each head's gradient in float, then their sum
-        const auto shared = [&](const ndvm_heads *to, int64_t d) -> ndvm_status {
-            const int64_t per = s->n_tokens / s->n_seq;
+        FoldHeadsSets folds{};
+        const auto shared = [&](AttendArgs &a, const ndvm_heads *to, int64_t d) {
             if (group == 1) {
                 a.out = heads_of(to, 1);
-                a.out_f32 = 0;
-            } else {
-                a.out = Heads{part, per * d, d, s->n_tokens * d, 1};
-                a.out_f32 = 1;
+                return;
             }
-            if (const ndvm_status r = launched(who, launch_attend(s->dtype, a, st))) return r;
-            if (group == 1 || s->n_tokens == 0) return NDVM_OK;
-            FoldHeadsArgs f{part, heads_of(to, group), s->n_seq, s->n_tokens, s->heads, d, offsets != nullptr};
-            return launched(who, launch_fold_heads(s->dtype, f, st));
+            a.out = Heads{part, s->n_tokens / s->n_seq * d, d, s->n_tokens * d, 1};
+            a.out_f32 = 1;
+            folds.set[folds.count++] = FoldHeadsArgs{part, heads_of(to, group), s->n_seq, s->n_tokens, s->heads, d, packed};
+            part += grad_part_bytes(s, d) / 4;
         };
-        // the sums q^T d_o of the segments serve dk too, transposed
-        const bool share = std::max(s->dk, s->dv) <= kMostPartsDim;
-        const bool want_v = dv->data || d_initial;
-        if (want_v || (share && dk->data)) {
-            a.only_segments = !want_v;
-            a.a = hk;
-            a.b = hq;
-            a.c = ho;
-            a.state_out = d_initial;
-            a.state_transposed = 0;
-            widths(s->dk, s->dv);
-            if (want_v) {
-                if (const ndvm_status r = shared(dv, s->dv)) return r;
-            } else if (a.n_segments > a.n_seq) {
-                if (const ndvm_status r = launched(who, launch_attend(s->dtype, a, st))) return r;
+        AttendArgs of_dk = all, of_dv = all;
+        of_dk.a = hv;
+        of_dk.b = ho;
+        of_dk.c = hq;
+        of_dk.state_transposed = 1;
+        widths(of_dk, s->dv, s->dk);
+        of_dv.a = hk;
+        of_dv.b = hq;
+        of_dv.c = ho;
+        of_dv.state_out = d_initial;
+        widths(of_dv, s->dk, s->dv);
+        of_dv.shared_segments = together;
+        const bool want_q = dq->data, want_k = dk->data, want_v = dv->data || d_initial;
+        if (want_k) shared(of_dk, dk, s->dk);
+        if (want_v) shared(of_dv, dv, s->dv);
+        if (together) {
+            AttendSets sums{}, sets{};
+            if (want_q) sums.set[sums.count++] = of_dq;
+            if (want_k || want_v) sums.set[sums.count++] = of_dk;
+            if (want_q) sets.set[sets.count++] = of_dq;
+            if (want_k) sets.set[sets.count++] = of_dk;
+            if (want_v) sets.set[sets.count++] = of_dv;
+            if (sets.count == 0) return NDVM_OK;
+            if (const ndvm_status r = launched(who, launch_attend_segments(s->dtype, sums, st))) return r;
+            if (const ndvm_status r = launched(who, launch_attend(s->dtype, sets, st))) return r;
+        } else {
+            for (const AttendArgs *a : {want_q ? &of_dq : nullptr, want_v ? &of_dv : nullptr, want_k ? &of_dk : nullptr}) {
+                if (!a) continue;
+                AttendSets one{};
+                one.set[one.count++] = *a;
+                if (const ndvm_status r = launched(who, launch_attend_segments(s->dtype, one, st))) return r;
+                if (const ndvm_status r = launched(who, launch_attend(s->dtype, one, st))) return r;
             }
-            a.only_segments = 0;
         }
-        if (dk->data) {
-            a.a = hv;
-            a.b = ho;
-            a.c = hq;
-            a.state_out = nullptr;
-            a.state_transposed = 1;
-            widths(s->dv, s->dk);
-            a.shared_segments = share;
-            if (const ndvm_status r = shared(dk, s->dk)) return r;
-        }
-        return NDVM_OK;
+        if (folds.count == 0 || s->n_tokens == 0) return NDVM_OK;
+        return launched(who, launch_fold_heads(s->dtype, folds, st));
     });
 }
 

@@ -392,6 +392,65 @@ def test_calls_of_more_than_the_caches_hold(nd):
     assert torch.equal(o[:40], nd.linear_attention_step(q[:40], k[:40], v[:40], g, few)) and torch.equal(state[:40], few)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dk,dv", [(64, 64), (128, 128), (40, 72), (16, 130)])
+def test_linear_attention_whole_sequences(nd, kind, dk, dv):
+    """Enough sequences and heads that none is cut; their number is no multiple of eight."""
+    n, H, T = 33, 6, 140
+    t, g, gv, bounds = attention_case(dk, kind, [T] * n, H, 3, dk, dv, True)
+    names = ("do", "q", "k", "v")
+    do, q, k, v = (t[x][0].reshape(n, T, *t[x][0].shape[1:]) for x in names)
+    s0, ds, sv, dsv = t["s0"][0], t["ds"][0], t["s0"][1], t["ds"][1]
+    host = [t[x][1] for x in names]
+    wo, wl = ref.attention(*host[1:], gv, 0.3, bounds, sv)
+    ao, al = ref.attention(*[gave(x) for x in host[1:]], gv, 0.3, bounds, gave(sv))
+    o, last = nd.linear_attention(q, k, v, g, scale=0.3, initial_state=s0, final_state=True)
+    check(o.reshape(wo.shape), wo, ref.attention_bound((wo, ao), kind, T, max(dk, dv)))
+    check(last, wl, ref.attention_bound((wl, al), kind, T, 0, whole=True))
+    want = ref.attention_grad(*host, gv, 0.3, bounds, sv, dsv)
+    mags = ref.attention_grad(*[gave(x) for x in host], gv, 0.3, bounds, gave(sv), gave(dsv))
+    got = nd.linear_attention_grad(do, q, k, v, g, scale=0.3, initial_state=s0, grad_final_state=ds)
+    for i, name in enumerate(("dq", "dk", "dv")):
+        check(got[i].reshape(want[i].shape), want[i], ref.attention_bound((want[i], mags[i]), kind, T, max(dk, dv) + 2), name)
+    check(got[3], want[3], ref.attention_bound((want[3], mags[3]), kind, T, 0, whole=True), "d s0")
+    for i in range(3):
+        one = nd.linear_attention_grad(do, q, k, v, g, scale=0.3, initial_state=s0, grad_final_state=ds,
+                                       need=tuple(j == i for j in range(3)))
+        assert torch.equal(one[i], got[i]) and sum(x is None for x in one[:3]) == 2
+
+
+@pytest.mark.parametrize("off", ["q", "k", "v", "do"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_linear_attention_grad_of_tensors_aligned_differently(nd, off, d):
+    """The gradient's sums are formed together or apart by how their tensors lie; cut sequences share sums either way."""
+    t, g, gv, bounds = attention_case(d, "bf16", [700], 2, 1, d, d, True)
+    names = ("do", "q", "k", "v")
+    on_gpu = {}
+    for x in names:
+        a = t[x][0]
+        room = torch.empty(a.numel() + 1, dtype=a.dtype, device="cuda")
+        on_gpu[x] = room[1:].view(a.shape).copy_(a) if x == off else a
+    host = [t[x][1] for x in names]
+    want = ref.attention_grad(*host, gv, 0.3, bounds, t["s0"][1], t["ds"][1])
+    mags = ref.attention_grad(*[gave(x) for x in host], gv, 0.3, bounds, gave(t["s0"][1]), gave(t["ds"][1]))
+    got = nd.linear_attention_grad(*[on_gpu[x] for x in names], g, offsets=torch.tensor(bounds).cuda(), scale=0.3,
+                                   initial_state=t["s0"][0], grad_final_state=t["ds"][0])
+    for i, name in enumerate(("dq", "dk", "dv")):
+        check(got[i], want[i], ref.attention_bound((want[i], mags[i]), "bf16", 700, d + 2), name)
+
+
+def test_gradients_of_more_than_the_caches_hold(nd):
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    g = torch.full((16,), -0.01, device="cuda")
+    q, k, v, do = (torch.randn(8, 1600, 16, 128, generator=gen, device="cuda", dtype=torch.bfloat16) for _ in range(4))
+    got = nd.linear_attention_grad(do, q, k, v, g)[:3]
+    # the sequences alone are cut elsewhere: sums in another order
+    for b in (0, 7):
+        one = nd.linear_attention_grad(*(x[b:b + 1] for x in (do, q, k, v)), g)[:3]
+        for x, y in zip(got, one):
+            assert float((x[b].float() - y[0].float()).abs().max()) <= 2.0 ** -7 * float(y.float().abs().max())
+
+
 # ---------------------------------------------------------------- gated feed-forward
 FFN = [(1, 1, 1), (3, 17, 5), (17, 64, 96), (130, 72, 200), (65, 129, 63), (257, 256, 384), (16, 1000, 264)]
 
