@@ -487,7 +487,7 @@ class _Torch:
         self.torch = torch
         self.codes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
         self.f32, self.u8, self.i64 = torch.float32, torch.uint8, torch.int64
-        self.Tensor = torch.Tensor
+        self.Tensor, self.empty_like = torch.Tensor, torch.empty_like
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self.raw_stream = raw or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
@@ -552,6 +552,11 @@ def _row_stride(x, name):
     return ld
 
 
+def _like(t, x):
+    """A contiguous tensor of x's shape (empty_like takes half a microsecond less than new_empty)."""
+    return t.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
+
+
 class _On:
     """Where a call launches and allocates: the current stream (nothing to
     switch), or the given one (see _launch_stream)."""
@@ -585,13 +590,14 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, out=None, stream=No
     w, b = _of(weight, "weight", dtype, (n,), dev), _of(bias, "bias", dtype, (n,), dev)
     with _On(t, stream, dev) as s:
         if out is None:
-            out, ld_out = x.new_empty(shape), n
+            out, ld_out = _like(t, x), n
         else:
             _alike(x, ("out", out))
             if out.shape != shape:
                 raise ValueError("out must have the shape of x")
             ld_out = _row_stride(out, "out")
-        mean, rstd = x.new_empty(lead, dtype=t.f32), x.new_empty(lead, dtype=t.f32)
+        mean = x.new_empty(lead, dtype=t.f32)
+        rstd = t.empty_like(mean)
         st = _norm(dt, x.data_ptr(), rows, n, ld, w, b, eps, out.data_ptr(), ld_out, mean.data_ptr(), rstd.data_ptr(), s)
         if st:
             _check(st, "ndvm_layer_norm")
@@ -613,11 +619,12 @@ def layer_norm_grad(dy, x, weight, mean, rstd, need_input: bool = True, need_wei
     w = _of(weight, "weight", dtype, (n,), dev)
     m, r = _of(mean, "mean", t.f32, lead, dev), _of(rstd, "rstd", t.f32, lead, dev)
     with _On(t, stream, dev) as s:
-        dx = x.new_empty(shape) if need_input else None
+        dx = _like(t, x) if need_input else None
         dw = db = ws = None
         need = _sz()
         if need_weight:
-            dw, db = x.new_empty(n), x.new_empty(n)
+            dw = x.new_empty(n)
+            db = t.empty_like(dw)
             _check(_norm_ws(rows, n, ctypes.byref(need)), "ndvm_layer_norm_workspace_bytes")
             ws = x.new_empty(need.value, dtype=t.u8)
         _check(_norm_grad(dt, dy.data_ptr(), ld_dy, x.data_ptr(), ld_x, rows, n, w, m, r,
@@ -808,10 +815,10 @@ def gated_ffn_grad(dh, x, w_gate, w_up, activation: str = "silu", need_input: bo
     if dh.shape != (*x.shape[:-1], n_out):
         raise ValueError("dh must be [.., n_out]")
     with _On(t, stream, x.device) as s:
-        dx = x.new_empty(x.shape) if need_input else None
+        dx = _like(t, x) if need_input else None
         dg = du = None
         if need_weight:
-            dg, du = (x.new_empty((n_out, n_in)) for _ in range(2))
+            dg, du = _like(t, w_gate), _like(t, w_up)
         ws, ws_ptr, need = _ffn_workspace(t, x, dt, rows, n_in, n_out, 1)
         _check(_ffn_grad(dt, act, dh.data_ptr(), _row_stride(dh, "dh"), x.data_ptr(), rows, n_in, _row_stride(x, "x"),
                          w_gate.data_ptr(), _row_stride(w_gate, "w_gate"), w_up.data_ptr(), _row_stride(w_up, "w_up"),
