@@ -268,9 +268,9 @@ template <class T> constexpr int input_parts() { return sizeof(T) == 4 ? 3 : std
 // workgroups apart, on the same XCD, since they read the same tensors.  Heads first: workgroups that run
 // together read whole rows of memory between them.
 __device__ inline uint32_t place_of(const AttendArgs &) { return blockIdx.x; }
-__device__ inline uint32_t place_of(const AttendSets &s) { return blockIdx.x / 8 / s.count * 8 + blockIdx.x % 8; }
+__device__ inline uint32_t place_of(const AttendSets &s) { return __builtin_amdgcn_readfirstlane(blockIdx.x / 8 / s.count) * 8 + blockIdx.x % 8; }
 __device__ inline const AttendArgs &set_of(const AttendArgs &a) { return a; }
-__device__ inline const AttendArgs &set_of(const AttendSets &s) { return s.set[blockIdx.x / 8 % s.count]; }
+__device__ inline const AttendArgs &set_of(const AttendSets &s) { return s.set[__builtin_amdgcn_readfirstlane(blockIdx.x / 8 % s.count)]; }
 
 // DS: widths of a and b in 32s.  DIRECT (bfloat16): rows are 16-byte granules at 16-byte
 // addresses, loaded to LDS directly, two chunks ahead; else through registers, one ahead.
@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(A
     __shared__ __align__(1024) char buffer0[PARTS * BYTES], buffer1[DIRECT ? BYTES : 16], buffer2[DIRECT ? BYTES : 16];
     __shared__ float power[N + 2];      // lambda^n
     const AttendArgs &A = set_of(args);
-    const uint32_t place = place_of(args), id = place / uint32_t(A.heads);
+    const uint32_t place = place_of(args), id = __builtin_amdgcn_readfirstlane(place / uint32_t(A.heads));
     if (MANY && id >= uint32_t(A.n_segments)) return;
     const Segment g = find_segment(A, id);
     if (g.count == 0 || (!OUT && g.index == g.count - 1)) return;
@@ -325,23 +325,46 @@ __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(A
             f(i, from, A.reversed ? N - 1 - row : row, c, base + row < len && c0 + c < width);
         }
     };
-    // always LOADS loads a wave (those past the segment's end fetch nothing)
-    const auto load = [&](const Heads &H, const Rows &R, char *to, auto granules, auto count, int64_t c0, int64_t width, int base, auto passing) __attribute__((always_inline)) {
-        each(H, R, granules, count, c0, width, base, [&](int i, const T *from, int row, int c, bool there) __attribute__((always_inline)) {
-            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(from), 0, 0x7fffffff, 0x00020000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(to + (wave + 4 * i) * 1024), 16,
-                                                     there ? unsigned(row) * unsigned(H.tok * 2) + c * 2 : kNowhere, 0, 0, decltype(passing)::value ? 2 : 0);
-        });
-    };
     const integral_constant<int, GA> granules_a;
     const integral_constant<int, GC> granules_c;
     const integral_constant<int, LA> count_a;
     const integral_constant<int, LC> count_c;
-    const auto load_chunk = [&](char *to, int base) __attribute__((always_inline)) {
+    // To LDS directly: where the next chunk's rows begin, and a lane's first granule in them; the
+    // others are 256 / granules rows apart (a multiple of 16: the same swizzle), counted from the end if reversed.
+    struct Stream {
+        const T *next;
+        int64_t step;
+        unsigned at, apart;
+    };
+    const bool reversed = A.reversed;
+    const auto stream = [&](const Heads &H, const Rows &R, auto granules, auto count, int64_t c0, int64_t width) {
+        constexpr int rows = 256 / granules.value;
+        static_assert(rows % 16 == 0 && rows * count.value == N, "");
+        const int first = (wave * 64 + l) / granules.value, c = ((wave * 64 + l) % granules.value ^ swizzle(first, granules.value)) * 8;
+        const int row = reversed ? N - 1 - first - (count.value - 1) * rows : first;
+        return Stream{static_cast<const T *>(H.p) + R.at + c0, N * R.step, c0 + c < width ? unsigned(row) * unsigned(H.tok * 2) + c * 2 : kNowhere,
+                      unsigned(rows * H.tok * 2)};
+    };
+    Stream sa, sb = stream(A.b, rb, granules_a, count_a, 0, A.da), sc = stream(A.c, rc, granules_c, count_c, col0, A.dc);
+    if (OUT) sa = stream(A.a, ra, granules_a, count_a, 0, A.da);
+    int left = len;         // tokens from the next chunk's first on
+    // always LOADS loads a wave (those past the segment's end fetch nothing)
+    const auto load = [&](Stream &s, char *to, auto granules, auto count, auto passing) __attribute__((always_inline)) {
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(s.next), 0, 0x7fffffff, 0x00020000);
+        const int first = (wave * 64 + l) / granules.value;
+#pragma unroll
+        for (int i = 0; i < count.value; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(to + (wave + 4 * i) * 1024), 16,
+                                                     first < left - i * (256 / granules.value) ? s.at : kNowhere,
+                                                     __builtin_amdgcn_readfirstlane((reversed ? count.value - 1 - i : i) * s.apart), 0, passing.value ? 2 : 0);
+        s.next += s.step;
+    };
+    const auto load_chunk = [&](char *to) __attribute__((always_inline)) {
         const std::false_type stays;
-        if (OUT) load(A.a, ra, to, granules_a, count_a, 0, A.da, base, integral_constant<bool, PASSING && !MANY>());
-        load(A.b, rb, to + BYTES_A, granules_a, count_a, 0, A.da, base, stays);
-        load(A.c, rc, to + BYTES_A + BYTES_B, granules_c, count_c, col0, A.dc, base, stays);
+        if (OUT) load(sa, to, granules_a, count_a, integral_constant<bool, PASSING && !MANY>());
+        load(sb, to + BYTES_A, granules_a, count_a, stays);
+        load(sc, to + BYTES_A + BYTES_B, granules_c, count_c, stays);
+        left -= N;
     };
     // Through registers: eight values a granule, split on their way to LDS.
     constexpr int V = kVec<T>;
@@ -380,8 +403,8 @@ __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(A
     };
 
     if constexpr (DIRECT) {
-        load_chunk(buffer0, 0);
-        load_chunk(buffer1, N);
+        load_chunk(buffer0);
+        load_chunk(buffer1);
     } else {
         fetch(0);
     }
@@ -636,7 +659,7 @@ __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(A
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             if (OUT && base > 0) store(base - N);
-            load_chunk(next, base + 2 * N);
+            load_chunk(next);
             compute(now, base);
         };
         if (len > 0) {
@@ -692,7 +715,7 @@ __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(A
 // by what enters it (the first one's stays).  A thread four values of the state,
 // wherever they lie; U segments' are read at once.  size: a multiple of 4.
 __device__ inline const AttendArgs &carried_set(const AttendArgs &a, uint32_t) { return a; }
-__device__ inline const AttendArgs &carried_set(const AttendSets &s, uint32_t tiles) { return s.set[blockIdx.z / tiles]; }
+__device__ inline const AttendArgs &carried_set(const AttendSets &s, uint32_t tiles) { return s.set[__builtin_amdgcn_readfirstlane(blockIdx.z / tiles)]; }
 template <class Args> __global__ void __launch_bounds__(256) attend_carry(Args args, uint32_t size) {
     constexpr int U = 8;
     const uint32_t tiles = (size + 1023) / 1024, at = blockIdx.z % tiles * 256 + threadIdx.x;
