@@ -12,7 +12,13 @@
 // into segments where sequences and heads alone would not fill the GPU: then a
 // first launch sums what each segment adds (the first one of a sequence: to what
 // the sequence started with), a second one carries states over the segments in
-// order, and the last one computes the outputs.
+// order, and the last one computes the outputs.  The gradient's three sums are formed
+// together where their widths allow it: dq's and dk's segments in one launch (dv starts from dk's,
+// transposed), all outputs in another.
+// Bound, at heads of 128: by memory and the instructions about evenly.  16 heads x 16384 tokens: 101 to
+// 109 us (the segments' sums 32, carrying 11, outputs 59: 270 MB of inputs and outputs at 2.5 TB/s, and
+// 270 more of segments' states and second reads); gradient of 8 x 2048 tokens, uncut, 181 us (470 MB at 2.6
+// TB/s; vector and matrix instructions fill 80% of the time of compute units with two workgroups).
 #include <algorithm>
 #include <type_traits>
 
@@ -765,8 +771,8 @@ template <class T> __global__ void __launch_bounds__(256) fold_heads(FoldHeadsSe
 }
 
 // One token of every stream: S <- lambda S + k^T v, o = scale q S.  Bound by the
-// state's way through memory: 8 dk dv bytes.  X threads of four columns each side by
-// side, 256 / X rows at a time.
+// state's way through memory: 8 dk dv bytes (192 streams x 16 heads of 128 x 128: 79 us, 5.1 TB/s).  X
+// threads of four columns each side by side, 256 / X rows at a time.
 template <class T, int X, bool PASSING> __global__ void __launch_bounds__(256) attend_step(StepArgs a) {
     typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
     constexpr int G = 256 / X;
@@ -962,7 +968,7 @@ hipError_t launch_attend(int dtype, const AttendSets &s, hipStream_t stream) {
             }
             with_parts<T>(run.set[0], [&](auto ds, auto nt, auto d) {
                 const AttendArgs &a = run.set[0];
-                // 16 heads x 16384 tokens of 128 (268 MB): 119 us, against 129 with all data as if it stayed
+                // 16 heads x 16384 tokens of 128 (268 MB): passing was 10 us faster than all data as if it stayed (119, 129)
                 const bool passing = d.value && a.n_tokens * a.heads * (a.da + a.dc) * 4 >= kPassingTraffic;
                 if (passing) launch_parts<T, ds.value, nt.value, d.value, true, d.value>(run, stream);
                 else launch_parts<T, ds.value, nt.value, d.value, true, false>(run, stream);
