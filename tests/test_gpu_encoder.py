@@ -302,6 +302,54 @@ def test_linear_attention_decays(nd):
         check(last, wl, ref.attention_bound((wl, al), kind, T, 0, whole=True))
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("d", [32, 128])
+def test_linear_attention_grad_not_finite(nd, kind, bad, d):
+    """... and in the gradient the tokens whose gradients the formula keeps it from, in cut sequences too."""
+    lens, H, at = [70, 330, 20], 2, 70 + 141
+    t, g, gv, bounds = attention_case(d, kind, lens, H, H, d, d, False)
+    names = ("do", "q", "k", "v")
+    host = [t[x][1] for x in names]
+    want = ref.attention_grad(*host, gv, 0.3, bounds, None, None)
+    mags = ref.attention_grad(*[np.abs(x) for x in host], gv, 0.3, bounds, None, None)
+    n, end, off = sum(lens), 400, torch.tensor(bounds).cuda()
+    # first and last token whose (dq, dk, dv) a value of head 1 at token `at` reaches
+    reach = dict(do=((at, at), (70, at), (70, at)), q=(None, (70, at), (70, at)), k=((at, end - 1), None, (at, at)),
+                 v=((at, end - 1), (at, at), None))
+    for which in names:
+        on_gpu = [t[x][0].clone() for x in names]
+        on_gpu[names.index(which)][at, 1, 3] = bad
+        got = nd.linear_attention_grad(*on_gpu, g, offsets=off, scale=0.3)
+        for i in range(3):
+            same = np.ones((n, H), dtype=bool)
+            if reach[which][i]:
+                lo, hi = reach[which][i]
+                same[lo:hi + 1, 1] = False
+                assert not torch.isfinite(got[i][at, 1]).all(), (which, i)
+            bound = ref.attention_bound((want[i], mags[i]), kind, max(lens), d + 1)
+            err = np.abs(values(got[i]) - want[i])[same]
+            assert np.all(err <= bound[same]), (which, i)
+
+
+def test_linear_attention_grad_decays(nd):
+    """Gradients with no decay and all of it, sequences cut and not."""
+    g = torch.tensor([0.0, float("-inf"), -30.0]).cuda()
+    for kind in KINDS:
+        for T in (40, 700):
+            t, _, _, bounds = attention_case(T, kind, [T], 3, 1, 32, 48, True)
+            names = ("do", "q", "k", "v")
+            host = [t[x][1] for x in names]
+            s0, ds = t["s0"], t["ds"]
+            want = ref.attention_grad(*host, values(g), 0.3, bounds, s0[1], ds[1])
+            mags = ref.attention_grad(*[np.abs(x) for x in host], values(g), 0.3, bounds, gave(s0[1]), gave(ds[1]))
+            got = nd.linear_attention_grad(*[t[x][0] for x in names], g, offsets=torch.tensor(bounds).cuda(), scale=0.3,
+                                           initial_state=s0[0], grad_final_state=ds[0])
+            for i in range(3):
+                check(got[i], want[i], ref.attention_bound((want[i], mags[i]), kind, T, 48 + 3), (kind, T, i))
+            check(got[3], want[3], ref.attention_bound((want[3], mags[3]), kind, T, 0, whole=True), (kind, T))
+
+
 def test_linear_attention_empty(nd):
     g = torch.zeros(2, device="cuda")
     q = torch.empty(0, 2, 8, device="cuda")
