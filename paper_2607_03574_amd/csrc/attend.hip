@@ -15,10 +15,10 @@
 // order, and the last one computes the outputs.  The gradient's three sums are formed
 // together where their widths allow it: dq's and dk's segments in one launch (dv starts from dk's,
 // transposed), all outputs in another.
-// Bound, at heads of 128: by memory and the instructions about evenly.  16 heads x 16384 tokens: 101 to
-// 109 us (the segments' sums 32, carrying 11, outputs 59: 270 MB of inputs and outputs at 2.5 TB/s, and
-// 270 more of segments' states and second reads); gradient of 8 x 2048 tokens, uncut, 181 us (470 MB at 2.6
-// TB/s; vector and matrix instructions fill 80% of the time of compute units with two workgroups).
+// Bound, at heads of 128, by memory: 16 heads x 16384 tokens 101 to 109 us (the segments' sums 33,
+// carrying 12, outputs 60: 270 MB of inputs and outputs, and as much again of segments' states and
+// second reads, at 5.2 TB/s); gradient of 8 x 2048 tokens, uncut, 175 to 181 us (470 MB needed, 710 moved at
+// 4.0 TB/s: a tensor is read by up to three sums).  Fewer instructions a chunk changed neither by 1%.
 #include <algorithm>
 #include <type_traits>
 
