@@ -869,8 +869,10 @@ template <class T, class F> void with_parts(const AttendArgs &a, F f) {
     sized(std::false_type());
 }
 
-// Whether one launch can form both.
-template <class T> bool together(const AttendArgs &a, const AttendArgs &b) {
+// Whether a launch can form the sets that it has, and another one.
+template <class T> bool together(const AttendSets &s, const AttendArgs &b) {
+    const AttendArgs &a = s.set[0];
+    if (ceil_div(b.n_segments * b.heads, 8) * 8 * (s.count + 1) > kMostGroups) return false;
     const auto kind = [](const AttendArgs &x) {
         int64_t k = 0;
         with_parts<T>(x, [&](auto ds, auto nt, auto d) { k = (ds.value * 4 + nt.value) * 2 + d.value; });
@@ -939,7 +941,7 @@ hipError_t launch_attend_segments(int dtype, const AttendSets &s, hipStream_t st
             run.count = 0;
         };
         for (int i = 0; i < s.count; ++i) {
-            if (run.count && !together<T>(run.set[0], s.set[i])) launch();
+            if (run.count && !together<T>(run, s.set[i])) launch();
             run.set[run.count++] = s.set[i];
         }
         launch();
@@ -961,8 +963,7 @@ hipError_t launch_attend(int dtype, const AttendSets &s, hipStream_t stream) {
             }
             AttendSets run{};
             for (int j = i; j < s.count; ++j) {
-                const bool fits = ceil_div(s.set[j].n_segments * s.set[j].heads, 8) * 8 * (run.count + 1) <= kMostGroups;
-                if (done[j] || s.set[j].da > kMostPartsDim || (run.count && !(fits && together<T>(s.set[i], s.set[j])))) continue;
+                if (done[j] || s.set[j].da > kMostPartsDim || (run.count && !together<T>(run, s.set[j]))) continue;
                 done[j] = true;
                 run.set[run.count++] = s.set[j];
             }
