@@ -480,7 +480,7 @@ def adam_step(params, grad_in, m, v, t: int, lr: float, beta1: float = 0.9, beta
 # These are called for single tokens too, whose kernels take a few microseconds:
 # the checks below are written to cost little when they pass.
 class _Torch:
-    """torch, the type codes, and the current stream's handle, looked up once."""
+    """torch, the type codes, and the look-ups of the current device and a device's current stream, found once."""
 
     def __init__(self):
         import torch
@@ -490,6 +490,7 @@ class _Torch:
         self.Tensor, self.empty_like = torch.Tensor, torch.empty_like
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self.raw_stream = raw or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+        self.current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 _torch_once = None
@@ -558,15 +559,20 @@ def _like(t, x):
 
 
 class _On:
-    """Where a call launches and allocates: the current stream (nothing to
-    switch), or the given one (see _launch_stream)."""
+    """Where a call launches and allocates: the current stream of the tensors'
+    device, or the given one (see _launch_stream).  A launch goes to the current
+    device (a default stream's handle, 0, names none), so another one is made current
+    meanwhile; where the tensors' is, there is nothing to switch."""
     __slots__ = ("ctx", "ptr")
 
     def __init__(self, t, stream, device):
         if stream is None:
-            self.ctx, self.ptr = None, t.raw_stream(device.index)
+            self.ctx = None if device.index == t.current_device() else t.torch.cuda.device(device)
+            self.ptr = t.raw_stream(device.index)
         else:
             s = _launch_stream(stream, device)
+            if s.device != device:
+                raise ValueError(f"stream must be on {device}, where the tensors are, not on {s.device}")
             self.ctx, self.ptr = t.torch.cuda.stream(s), s.cuda_stream
 
     def __enter__(self):
