@@ -451,8 +451,11 @@ ndvm_status ndvm_layer_norm_grad(int dtype, const void *dy, int64_t ld_dy, const
  * `final_state` (the same layout) unless that is NULL.  log_decay: device float
  * [heads], constants of the model (they get no gradient), at most 0 (beyond it
  * states grow and may overflow).  Evaluated in chunks,
- * not token by token, with every sum and state in float; a value that is not
- * finite leaves the outputs of earlier tokens and of other sequences as they are.
+ * not token by token, with every sum and state in float (the products q.k of
+ * tokens of a chunk, and the state where a token reads it, are multiplied with 16
+ * of their bits for 16-bit types: a result is off by its own rounding); a value
+ * that is not finite leaves the outputs of earlier tokens and of other sequences
+ * as they are.
  *
  * Sequences: offsets = NULL, all of n_tokens / n_seq tokens, token t of sequence
  * s at data + s*seq_stride + t*tok_stride + head*head_stride; or `offsets`,

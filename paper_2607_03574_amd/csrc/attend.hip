@@ -233,8 +233,8 @@ __global__ void __launch_bounds__(256) attend_general(AttendArgs A) {
 //  - A float is multiplied as bf16 parts, each the next 8 bits of it: half inputs are
 //    exactly two, float inputs three; what is left out of a product of parts is below 2^-24
 //    of it for float, 2^-16 for half.  The state stays float for every type and takes c times
-//    its decay as three parts; what is read from it, and the products of a pair, are as many parts
-//    as an input: one for bfloat16, whose result has 8 bits too.
+//    its decay as three parts; what is read from it, and the products of a pair, are two parts
+//    (three for float): a 16-bit result then differs from the exact one by its own rounding alone.
 // LDS rows lie in granules of 16 bytes, granule i of row r at i ^ swizzle(r): the 16 rows
 // that one instruction reads are then in different banks.
 typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -289,6 +289,7 @@ __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(A
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr bool MANY = std::is_same<Args, AttendSets>::value;
     constexpr int PARTS = input_parts<T>(), ORDER = PARTS - 1;
+    constexpr int HELD = PARTS > 2 ? PARTS : 2;      // parts of the state where it is read, and of a pair's product
     constexpr int N = 32, GA = 4 * DS, GC = 8 * NT;      // tokens of a chunk; granules of a row
     constexpr int BYTES_A = OUT ? N * GA * 16 : 0, BYTES_B = N * GA * 16, BYTES_C = N * GC * 16;      // of a part
     constexpr int BYTES = BYTES_A + BYTES_B + BYTES_C;
@@ -563,14 +564,14 @@ __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(A
                 P11 = multiply<ORDER>(b1, a1, P11);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    bf16x8 state[PARTS];
+                    bf16x8 state[HELD];
 #pragma unroll
                     for (int r = 0; r < 8; ++r) split(S[2 * s + r / 4][nt][r % 4], state, r);
-                    O[0][nt] = multiply<ORDER>(state, a0, O[0][nt]);
-                    O[1][nt] = multiply<ORDER>(state, a1, O[1][nt]);
+                    O[0][nt] = multiply<HELD - 1>(state, a0, O[0][nt]);
+                    O[1][nt] = multiply<HELD - 1>(state, a1, O[1][nt]);
                 }
             }
-            bf16x8 p[2][PARTS];
+            bf16x8 p[2][HELD];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 // what is masked is replaced, not multiplied
@@ -586,7 +587,7 @@ __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(A
             for (int it = 0; it < 2; ++it)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    near[it][nt] = multiply<ORDER>(fc[nt], p[it], f32x4(0.0f));
+                    near[it][nt] = multiply<HELD - 1>(fc[nt], p[it], f32x4(0.0f));
 #pragma unroll
                     for (int r = 0; r < 4; ++r) odd = __builtin_fmaf(near[it][nt][r], 0.0f, odd);
                 }
@@ -601,7 +602,7 @@ __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(A
                         const int at = j / 16 * 2 + j % 4 / 2;
                         float pij = 0;
 #pragma unroll
-                        for (int q = 0; q < PARTS; ++q) {
+                        for (int q = 0; q < HELD; ++q) {
                             typedef int i32x4 __attribute__((ext_vector_type(4)));
                             const i32x4 packed = __builtin_bit_cast(i32x4, it ? p[1][q] : p[0][q]);
                             const int two = __shfl(at == 0 ? packed[0] : at == 1 ? packed[1] : at == 2 ? packed[2] : packed[3], lm + 16 * (j % 16 / 4));
