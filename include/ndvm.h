@@ -539,7 +539,10 @@ ndvm_status ndvm_gated_ffn(int dtype, int act, const void *x, int64_t rows, int6
  * formed again).  dx [rows, n_in] may be NULL (not wanted), as may dw_gate and
  * dw_up [n_out, n_in] together; with rows = 0 the weights' gradients are 0.
  * The gradients with respect to x w^T are operands of further products and are
- * rounded to the tensors' type for them (a float keeps its 24 bits).
+ * rounded to the tensors' type for them (a float keeps its 24 bits).  In half
+ * they are rounded times a power of two where the largest of them that is finite
+ * is not between 1 and 2^15: none becomes an infinity by it, and none above
+ * 2^-38 of the largest is lost.
  */
 ndvm_status ndvm_gated_ffn_grad(int dtype, int act, const void *dh, int64_t ld_dh, const void *x, int64_t rows,
                                 int64_t n_in, int64_t ld_x, const void *w_gate, int64_t ld_gate, const void *w_up,

@@ -142,6 +142,8 @@ struct ProductArgs {
     void *p;                    // [m][dg du], each padded with zeros to pad_n, in parts
     int64_t ld_p, plane_p;
     int64_t pad_n;              // n_out padded to a multiple of 64
+    unsigned *largest;          // gradient in half: see scale_of
+    int again;
 };
 enum Kind { kGated, kGatedGrad, kPlain };
 
@@ -155,8 +157,40 @@ template <class O> __device__ inline O read_transposed(const char *p, const char
 }
 #endif
 
-// What becomes of eight columns (n on) of a row of g and u: h, or dg and du.
-template <class T, Kind KIND, int ACT> __device__ __attribute__((always_inline)) inline void gated_out(const ProductArgs &A, int64_t m, int64_t n, const float (&g)[8], const float (&u)[8]) {
+// dg and du are rounded to the tensors' type: in two parts the two products that take them would be twice the
+// work (4096 x 1024 x 4096 bf16: 124 us of 204).  A half has not the range for that: dh u act' of halves can pass
+// 65504, and small ones fall below 2^-24.  So the first pass over a gradient in half notes the largest value of
+// dg and du that is finite (`largest`, its bits; a maximum does not depend on the order of the atomics); where that is
+// not between 1 and 2^15, a second pass writes them again times a power of two that brings it there, and
+// the products are divided by it.  Values down to 2^-24 of the largest are kept to half's 11 bits or to 2^-38 of the
+// largest.  Calls within the range pay for a clear and for a pass that returns: 4096 x 1024 x 4096 249 us,
+// 241 without; out of it 301.
+__device__ inline float scale_of(const ProductArgs &A) {
+    const unsigned bits = *A.largest;
+    const int e = int(bits >> 23) - 127;
+    return bits == 0 || (e >= 0 && e < 15) ? 1.0f : __uint_as_float(unsigned(min(14 - e, 100) + 127) << 23);
+}
+template <class T> __device__ inline float unscaled(const ProductArgs &A) {
+    if constexpr (std::is_same<T, f16>::value) return 1.0f / scale_of(A);
+    return 1.0f;
+}
+// Whether a pass over dg and du has to write anything.
+template <class T, Kind KIND> __device__ inline bool nothing_to_do(const ProductArgs &A) {
+    if constexpr (std::is_same<T, f16>::value && KIND == kGatedGrad) return A.again && scale_of(A) == 1.0f;
+    return false;
+}
+__device__ inline void note_largest(const ProductArgs &A, float top) {
+    if (A.again) return;
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s));
+    const unsigned bits = __float_as_uint(top);
+    if (threadIdx.x % 64 == 0 && bits > __hip_atomic_load(A.largest, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(A.largest, bits);
+}
+__global__ void clear_largest(unsigned *p) { *p = 0; }
+
+// What becomes of eight columns (n on) of a row of g and u: h, or dg and du.  top: the largest of these so far.
+template <class T, Kind KIND, int ACT> __device__ __attribute__((always_inline)) inline void gated_out(const ProductArgs &A, int64_t m, int64_t n, const float (&g)[8], const float (&u)[8], float scale, float &top) {
+    constexpr bool RANGED = std::is_same<T, f16>::value && KIND == kGatedGrad;
     typedef typename Parts<T>::type P;
     constexpr int PARTS = Parts<T>::count;
     typedef T eight __attribute__((ext_vector_type(8), aligned(sizeof(T))));
@@ -190,8 +224,15 @@ template <class T, Kind KIND, int ACT> __device__ __attribute__((always_inline))
             P pg[PARTS], pu[PARTS];
             // what lies beyond the operands is 0, whatever act does there
             const bool there = n + r < A.n;
-            Parts<T>::split(there ? float(dh[r]) * u[r] * slope : 0.0f, pg);
-            Parts<T>::split(there ? float(dh[r]) * value : 0.0f, pu);
+            float dg = there ? float(dh[r]) * u[r] * slope : 0.0f, du = there ? float(dh[r]) * value : 0.0f;
+            if constexpr (RANGED) {
+                const float a = fabsf(dg), b = fabsf(du);
+                top = fmaxf(top, fmaxf(a <= 3.402823466e38f ? a : 0.0f, b <= 3.402823466e38f ? b : 0.0f));
+                dg *= scale;
+                du *= scale;
+            }
+            Parts<T>::split(dg, pg);
+            Parts<T>::split(du, pu);
 #pragma unroll
             for (int q = 0; q < PARTS; ++q) {
                 vg[q][r] = pg[q];
@@ -453,6 +494,7 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
         __builtin_amdgcn_s_waitcnt(0x0f70);
     }
 
+    const float unscale = KIND == kPlain ? unscaled<T>(A) : 1.0f;
     // lane l, register r of tile (i, j): row m = l % 16 of j; column 4 (l / 16) + r of i, or,
     // gated, 8 (l / 16) + 4 (i % 2) + r of the pair of tiles
 #pragma unroll
@@ -483,7 +525,7 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
                 const int64_t n = n0 + wa * WA + i * 16 + lg * 4;
                 four v;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) v[r] = T(acc[i][j][r]);
+                for (int r = 0; r < 4; ++r) v[r] = T(acc[i][j][r] * unscale);
                 if (n + 4 <= A.n) *reinterpret_cast<four *>(row + n) = v;
                 else
                     for (int r = 0; r < 4; ++r)
@@ -508,6 +550,9 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
             }
             return;
         }
+        constexpr bool RANGED = std::is_same<T, f16>::value && KIND == kGatedGrad;
+        const float scale = RANGED && A.again ? scale_of(A) : 1.0f;
+        float top = 0;
         with_act(A.act, [&](auto act) __attribute__((always_inline)) {
 #pragma unroll
             for (int j = 0; j < TB; ++j) {
@@ -521,10 +566,11 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
                         g[r] = acc[i + r / 4][j][r % 4];
                         u[r] = acc[i + r / 4 + TA / 2][j][r % 4];
                     }
-                    gated_out<T, KIND, decltype(act)::value>(A, m, n0 + wa * (WA / 2) + i * 16 + lg * 8, g, u);
+                    gated_out<T, KIND, decltype(act)::value>(A, m, n0 + wa * (WA / 2) + i * 16 + lg * 8, g, u, scale, top);
                 }
             }
         });
+        if (RANGED) note_largest(A, top);
     }
 }
 #endif
@@ -535,6 +581,7 @@ __global__ void __launch_bounds__(64 * NA * NB) product(ProductArgs A) {
     // separate arrays, so that the compiler sees that loads into one leave reads of the others alone
     constexpr int SIZE = (BA + BB) * kStep * 2;
     __shared__ __align__(1024) char buffer0[SIZE], buffer1[SIZE], buffer2[SIZE], buffer3[SIZE];
+    if (nothing_to_do<T, KIND>(A)) return;
     product_tile<T, BA, BB, NA, NB, KIND, false>(A, blockIdx.x, buffer0, buffer1, buffer2, buffer3);
 #endif
 }
@@ -560,6 +607,7 @@ template <class T> __global__ void __launch_bounds__(256) fold_splits(ProductArg
     if (m < A.split) row = static_cast<T *>(A.out) + m * A.ld;
     else if (m >= A.split2 && m < A.m2) row = static_cast<T *>(A.out2) + (m - A.split2) * A.ld2;
     if (!row) return;
+    const float unscale = unscaled<T>(A);
     const float *p = A.part + m * A.n + n;
     if (n + 4 <= A.n) {
         f32x4 sum = *reinterpret_cast<const four_f *>(p);
@@ -567,13 +615,13 @@ template <class T> __global__ void __launch_bounds__(256) fold_splits(ProductArg
         typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
         four v;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = T(sum[r]);
+        for (int r = 0; r < 4; ++r) v[r] = T(sum[r] * unscale);
         *reinterpret_cast<four *>(row + n) = v;
     } else {
         for (int r = 0; n + r < A.n; ++r) {
             float sum = p[r];
             for (int i = 1; i < A.splits; ++i) sum += p[i * A.m * A.n + r];
-            row[n + r] = T(sum);
+            row[n + r] = T(sum * unscale);
         }
     }
 }
@@ -581,25 +629,31 @@ template <class T> __global__ void __launch_bounds__(256) fold_splits(ProductArg
 // ... of a gated product.  A thread eight columns.
 template <class T, Kind KIND> __global__ void __launch_bounds__(256) fold_gated(ProductArgs A) {
 #ifdef __HIP_DEVICE_COMPILE__
+    if (nothing_to_do<T, KIND>(A)) return;
+    constexpr bool RANGED = std::is_same<T, f16>::value && KIND == kGatedGrad;
+    const float scale = RANGED && A.again ? scale_of(A) : 1.0f;
+    float top = 0;
     const int64_t per = A.pad_n / 8, at = int64_t(blockIdx.x) * 256 + threadIdx.x, m = at / per, n = at % per * 8;
-    if (m >= A.m) return;
-    f32x4 sum[4] = {};
-    for (int i = 0; i < A.splits; ++i) {
-        const f32x4 *p = reinterpret_cast<const f32x4 *>(A.part + (i * A.m + m) * 2 * A.pad_n + n), *q = p + A.pad_n / 4;
-        sum[0] += p[0];
-        sum[1] += p[1];
-        sum[2] += q[0];
-        sum[3] += q[1];
-    }
-    with_act(A.act, [&](auto act) __attribute__((always_inline)) {
-        float g[8], u[8];
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            g[r] = sum[r / 4][r % 4];
-            u[r] = sum[2 + r / 4][r % 4];
+    if (m < A.m) {
+        f32x4 sum[4] = {};
+        for (int i = 0; i < A.splits; ++i) {
+            const f32x4 *p = reinterpret_cast<const f32x4 *>(A.part + (i * A.m + m) * 2 * A.pad_n + n), *q = p + A.pad_n / 4;
+            sum[0] += p[0];
+            sum[1] += p[1];
+            sum[2] += q[0];
+            sum[3] += q[1];
         }
-        gated_out<T, KIND, decltype(act)::value>(A, m, n, g, u);
-    });
+        with_act(A.act, [&](auto act) __attribute__((always_inline)) {
+            float g[8], u[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                g[r] = sum[r / 4][r % 4];
+                u[r] = sum[2 + r / 4][r % 4];
+            }
+            gated_out<T, KIND, decltype(act)::value>(A, m, n, g, u, scale, top);
+        });
+    }
+    if (RANGED) note_largest(A, top);
 #endif
 }
 
@@ -706,11 +760,21 @@ Gated gated_cut(int dtype, int64_t rows, int64_t n_in, int64_t n_out) {
     return Gated{128, 128, std::max<int64_t>(splits, 1)};
 }
 template <class T, Kind KIND> void launch_product(const Gated &c, ProductArgs a, int64_t n, int64_t m, hipStream_t stream) {
+    constexpr bool RANGED = std::is_same<T, f16>::value && KIND == kGatedGrad;
+    if (RANGED) clear_largest<<<1, 1, 0, stream>>>(a.largest);
     a.splits = int(c.splits);
-    if (c.bb == 256) launch_tiles<T, 256, 256, 2, 4, KIND>(a, n, m, stream);
-    else if (c.ba == 256) launch_tiles<T, 256, 128, 4, 2, KIND>(a, n, m, stream);
-    else launch_tiles<T, 128, 128, 2, 2, KIND>(a, n, m, stream);
-    if (c.splits > 1) fold_gated<T, KIND><<<dim3(uint32_t(ceil_div(a.pad_n / 8 * a.m, 256))), 256, 0, stream>>>(a);
+    const auto sums = [&]() {
+        if (c.bb == 256) launch_tiles<T, 256, 256, 2, 4, KIND>(a, n, m, stream);
+        else if (c.ba == 256) launch_tiles<T, 256, 128, 4, 2, KIND>(a, n, m, stream);
+        else launch_tiles<T, 128, 128, 2, 2, KIND>(a, n, m, stream);
+    };
+    const auto fold = [&]() { fold_gated<T, KIND><<<dim3(uint32_t(ceil_div(a.pad_n / 8 * a.m, 256))), 256, 0, stream>>>(a); };
+    sums();
+    if (c.splits > 1) fold();
+    if (!RANGED) return;
+    a.again = 1;        // split sums are still there
+    if (c.splits > 1) fold();
+    else sums();
 }
 
 // How the gradient's two plain products are cut: tiles of `tile` squared, each one's sum over so
@@ -786,6 +850,7 @@ size_t ffn_bytes(int dtype, int64_t rows, int64_t n_in, int64_t n_out, bool grad
     if (g.splits > 1) s.take_floats(g.splits * rows * 2 * pad64(n_out));
     if (grad) {
         s.take(dtype, rows, 2 * pad64(n_out));
+        if (dtype == NDVM_F16) s.take_floats(1);
         const Pieces c = pieces(dtype, rows, n_in, n_out);
         if (c.dx > 1) s.take_floats(c.dx * rows * n_in);
         if (c.dw > 1) s.take_floats(c.dw * 2 * pad64(n_out) * n_in);
@@ -875,11 +940,13 @@ template <class T> void ffn_grad(const FfnArgs &a, hipStream_t stream) {
     p.p = s.take(a.dtype, a.rows, 2 * pad_n);
     p.ld_p = 2 * pad_n;
     p.plane_p = s.plane;
+    if (std::is_same<T, f16>::value) p.largest = reinterpret_cast<unsigned *>(s.take_floats(1));
     launch_product<T, kGatedGrad>(g, p, pad_n, a.rows, stream);
     const Operand both{p.p, a.rows, 2 * pad_n, p.plane_p};
     const Pieces c = pieces(a.dtype, a.rows, a.n_in, a.n_out);
     ProductArgs dx{}, dw{};
     dx.splits = dw.splits = 1;
+    dx.largest = dw.largest = p.largest;
     if (a.dx) {     // n: x's columns; the sum: the rows of both weights
         dx.a = o.wg;
         dx.a2 = o.wu;
