@@ -541,8 +541,8 @@ ndvm_status ndvm_gated_ffn(int dtype, int act, const void *x, int64_t rows, int6
  * The gradients with respect to x w^T are operands of further products and are
  * rounded to the tensors' type for them (a float keeps its 24 bits).  In half
  * they are rounded times a power of two where the largest of them that is finite
- * is not between 1 and 2^15: none becomes an infinity by it, and none above
- * 2^-38 of the largest is lost.
+ * is not between 1 and 2^15: none becomes an infinity by it, and each is off by
+ * at most 2^-11 of itself or 2^-25 of the largest.
  */
 ndvm_status ndvm_gated_ffn_grad(int dtype, int act, const void *dh, int64_t ld_dh, const void *x, int64_t rows,
                                 int64_t n_in, int64_t ld_x, const void *w_gate, int64_t ld_gate, const void *w_up,

@@ -162,9 +162,9 @@ template <class O> __device__ inline O read_transposed(const char *p, const char
 // 65504, and small ones fall below 2^-24.  So the first pass over a gradient in half notes the largest value of
 // dg and du that is finite (`largest`, its bits; a maximum does not depend on the order of the atomics); where that is
 // not between 1 and 2^15, a second pass writes them again times a power of two that brings it there, and
-// the products are divided by it.  Values down to 2^-24 of the largest are kept to half's 11 bits or to 2^-38 of the
-// largest.  Calls within the range pay for a clear and for a pass that returns: 4096 x 1024 x 4096 249 us,
-// 241 without; out of it 301.
+// the products are divided by it.  A value is then off by at most 2^-11 of itself or 2^-25 of the largest.
+// Calls within the range pay for a clear and for a pass that returns: 4096 x 1024 x 4096 249 us,
+// 241 without them; out of it 301.
 __device__ inline float scale_of(const ProductArgs &A) {
     const unsigned bits = *A.largest;
     const int e = int(bits >> 23) - 127;
