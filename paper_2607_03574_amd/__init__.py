@@ -478,7 +478,8 @@ def adam_step(params, grad_in, m, v, t: int, lr: float, beta1: float = 0.9, beta
 
 # ---------------------------------------------------------------- encoder operators
 # These are called for single tokens too, whose kernels take a few microseconds:
-# the checks below are written to cost little when they pass.
+# the checks below are written to cost little when they pass.  Their results carry no
+# gradient, whatever the arguments require: torch_api has the differentiable forms.
 class _Torch:
     """torch, the type codes, and the look-ups of the current device and a device's current stream, found once."""
 
@@ -488,6 +489,7 @@ class _Torch:
         self.codes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
         self.f32, self.u8, self.i64 = torch.float32, torch.uint8, torch.int64
         self.Tensor, self.empty_like = torch.Tensor, torch.empty_like
+        self.grad_enabled, self.increment_version = torch.is_grad_enabled, torch.autograd.graph.increment_version
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self.raw_stream = raw or (lambda index: torch.cuda.current_stream(index).cuda_stream)
         self.current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
@@ -528,6 +530,14 @@ def _of(x, name, dtype, shape, device):
     if x.shape != shape or not x.is_contiguous():
         raise ValueError(f"{name} must be contiguous, of shape {tuple(shape)}")
     return x.data_ptr()
+
+
+def _to_write(t, x, name):
+    """Before a call that writes x through its address: autograd has to see the write, so that a backward pass
+    that saved x refuses to run on the new values, and a graph that x is part of may not lose it."""
+    if x.requires_grad and t.grad_enabled():
+        raise ValueError(f"{name} is written in place, which has no gradient: detach it")
+    t.increment_version(x)
 
 
 def _row_stride(x, name):
@@ -587,7 +597,8 @@ class _On:
 
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, out=None, stream=None):
     """(y, mean, rstd) of the rows (last axis) of x (ndvm_layer_norm); mean and
-    rstd are float32 of x's leading shape, what layer_norm_grad takes."""
+    rstd are float32 of x's leading shape, what layer_norm_grad takes.  (With
+    autograd: torch_api.layer_norm.)"""
     t = _t()
     dt, dtype, dev, shape = _op_type(t, x, "x"), x.dtype, x.device, x.shape
     ld = _row_stride(x, "x")
@@ -602,6 +613,7 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, out=None, stream=No
             if out.shape != shape:
                 raise ValueError("out must have the shape of x")
             ld_out = _row_stride(out, "out")
+            _to_write(t, out, "out")
         mean = x.new_empty(lead, dtype=t.f32)
         rstd = t.empty_like(mean)
         st = _norm(dt, x.data_ptr(), rows, n, ld, w, b, eps, out.data_ptr(), ld_out, mean.data_ptr(), rstd.data_ptr(), s)
@@ -690,7 +702,7 @@ def linear_attention(q, k, v, log_decay, offsets=None, scale=None, initial_state
     [.., kv_heads, dk or dv]; with `offsets` (int64 [sequences + 1], on the
     device) the sequences lie one after the other in [tokens, heads, d].
     log_decay: float32 [heads]; scale: dk**-0.5 unless given; states are
-    float32 [sequences, heads, dk, dv]."""
+    float32 [sequences, heads, dk, dv].  (With autograd: torch_api.linear_attention.)"""
     t = _t()
     shape, lead, off, decay, hq, hk, hv = _attention(t, q, k, v, log_decay, offsets, scale)
     dims, dev = (shape.n_seq, shape.heads, shape.dk, shape.dv), q.device
@@ -700,6 +712,7 @@ def linear_attention(q, k, v, log_decay, offsets=None, scale=None, initial_state
             out = q.new_empty((*lead, shape.heads, shape.dv))
         else:
             _alike(q, ("out", out))
+            _to_write(t, out, "out")
         last = q.new_empty(dims, dtype=t.f32) if final_state else None
         ws, ws_ptr, need = _attention_workspace(t, q, shape, off is not None, 0)
         _check(_attn(shape, hq, hk, hv, decay, off, s0, _heads(out, "out", lead, shape.heads, shape.dv),
@@ -741,7 +754,7 @@ def linear_attention_step(q, k, v, log_decay, state, slots=None, scale=None, out
     heads, dk], k and v [streams, kv_heads, d]; stream i's state is
     state[slots[i]] (float32 [slots, heads, dk, dv], updated in place; slot i
     without `slots`), or none, with output 0, where slots[i] is out of range.
-    Returns o [streams, heads, dv]."""
+    Returns o [streams, heads, dv].  There is no gradient through a step."""
     t = _t()
     dt = _op_type(t, q, "q")
     _alike(q, ("k", k), ("v", v))
@@ -769,6 +782,8 @@ def linear_attention_step(q, k, v, log_decay, state, slots=None, scale=None, out
             out = q.new_empty((n, H, dv))
         else:
             _alike(q, ("out", out))
+            _to_write(t, out, "out")
+        _to_write(t, state, "state")
         _check(_attn_step(shape, hq, hk, hv, decay, st, state.shape[0], sl, one(out, "out", H, dv), s),
                "ndvm_linear_attention_step")
     return out
@@ -794,7 +809,8 @@ def _ffn_workspace(t, x, dt, rows, n_in, n_out, grad):
 
 
 def gated_ffn(x, w_gate, w_up, activation: str = "silu", out=None, stream=None):
-    """act(x w_gate^T) * (x w_up^T) (ndvm_gated_ffn) for x [.., n_in] and weights [n_out, n_in]."""
+    """act(x w_gate^T) * (x w_up^T) (ndvm_gated_ffn) for x [.., n_in] and weights [n_out, n_in].
+    (With autograd: torch_api.gated_ffn.)"""
     t = _t()
     dt, act, rows, n_in, n_out = _ffn_args(t, x, w_gate, w_up, activation)
     ld_x, ld_g, ld_u = _row_stride(x, "x"), _row_stride(w_gate, "w_gate"), _row_stride(w_up, "w_up")
@@ -806,6 +822,7 @@ def gated_ffn(x, w_gate, w_up, activation: str = "silu", out=None, stream=None):
             if out.shape != (*x.shape[:-1], n_out):
                 raise ValueError("out must be [.., n_out]")
             ld_out = _row_stride(out, "out")
+            _to_write(t, out, "out")
         ws, ws_ptr, need = _ffn_workspace(t, x, dt, rows, n_in, n_out, 0)
         _check(_ffn(dt, act, x.data_ptr(), rows, n_in, ld_x, w_gate.data_ptr(), ld_g, w_up.data_ptr(), ld_u, n_out,
                     out.data_ptr(), ld_out, ws_ptr, need, s), "ndvm_gated_ffn")
