@@ -406,7 +406,7 @@ ndvm_status ndvm_adam_step(double *params, const double *grad, double *m, double
  * only enqueues on `stream`: it allocates nothing and waits for nothing.
  * Where a result takes in an infinity it may be NaN: in matrix products a float is
  * multiplied in three parts of 8 bits (what is left out is below 2^-21 of a term,
- * 2^-23 on average), and a half in attention in two (below 2^-14).
+ * 2^-24 on average), and a half in attention in two (below 2^-14).
  * Outputs may not overlap inputs.  `workspace`: device memory of the size that
  * the operator's *_workspace_bytes call names (NULL where that is 0); nothing in
  * it needs a value, and its contents mean nothing afterwards.

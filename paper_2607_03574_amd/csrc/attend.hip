@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(256) attend_general(AttendArgs A) {
 //    column each), tokens in the order that P^T has them.
 //  - A float is multiplied as bf16 parts, each the next 8 bits of it: half inputs are
 //    exactly two, float inputs three.  Parts are cut (the last one is rounded): a second part can be 2^-7 of
-//    the value, a third 2^-15, so what is left out of a product is below 2^-21 of it for float (2^-23 on average)
+//    the value, a third 2^-15, so what is left out of a product is below 2^-21 of it for float (2^-24 on average)
 //    and 2^-14 for half, whose results are rounded to 2^-11, and has the product's sign.  The state stays float for every type and takes c times
 //    its decay as three parts; what is read from it, and the products of a pair, are two parts
 //    (three for float): a 16-bit result then differs from the exact one by its own rounding alone.

@@ -17,7 +17,7 @@
 // 8 bits, exactly) and adds up the six products down to 2^-14 of the largest in float: what
 // is left out, the second part times the third and less, is below 2^-21 of a term (parts are cut, not
 // rounded: a second part can be 2^-7 of the value, a third 2^-15, and what is left out has the term's
-// sign), 2^-23 on average; bf16 products are 16 times the rate of float ones.  Norm-wise error 3 to 4 10^-7.
+// sign), 2^-24 on average; bf16 products are 16 times the rate of float ones.  Norm-wise error 3 to 4 10^-7.
 #include <algorithm>
 #include <type_traits>
 

@@ -9,7 +9,7 @@ result.  Operands of at least 16 bits on the way (errors below 2^-16 of each ter
 less than 0.3 r in norm, even where they add up over terms, so the error is within sqrt(1 + 0.3^2) r
 < 1.05 r.  One more rounding to the type's bits on the way would make it sqrt(2) r.
 
-float results: products of parts leave out at most 2^-21 of a term, 2^-23 on average, and float sums of some
+float results: products of parts leave out at most 2^-21 of a term, 2^-24 on average, and float sums of some
 hundred steps 2^-24 times the root of their number: 3e-7 to 5e-7, the limit twice that.  Without the third
 part of an operand the error is 2^-16 or so, fifteen times the limit.
 """
