@@ -323,13 +323,14 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
     // this workgroup's share of the sum
     const int first = int(int64_t(steps) * PAIRS * part / A.splits), total = int(int64_t(steps) * PAIRS * (part + 1) / A.splits);
     // Where the next tiles to load begin: moved on from step to step, or worked out again where there are
-    // pairs of parts (in order of size).  No branches: the accumulators would be moved about at each.
+    // pairs of parts (small products first: the large ones' sum is then rounded in a sixth of the steps;
+    // 1289 x 2668 x 1028 5.0e-7 of the result, largest first 1.2e-6).  No branches: the accumulators would be moved about at each.
     const P *next_a = nullptr, *next_a2 = nullptr, *next_b = nullptr;
     int left = 0;               // of the sum, from there to the end of these operands
     int rows_a = 0, rows_b = 0; // rows there are from there on, for operands along C
     int at = first;             // the step
     const auto find = [&]() __attribute__((always_inline)) {
-        constexpr int pair_a[6] = {0, 0, 1, 1, 0, 2}, pair_b[6] = {0, 1, 0, 1, 2, 0};
+        constexpr int pair_a[6] = {2, 0, 1, 1, 0, 0}, pair_b[6] = {0, 2, 1, 0, 1, 0};     // small products first
         int pa = 0, pb = 0;
         int64_t k0 = int64_t(at) * kStep;
         if (PAIRS > 1) {

@@ -104,6 +104,14 @@ def test_gated_ffn(nd, kind, rows, n_in, n_out):
         close(a, b, kind, what, once=1.5)
 
 
+@pytest.mark.parametrize("rows,n_in,n_out", [(7020, 1036, 423), (1289, 2668, 1028)])
+def test_float_ffn_of_long_sums(nd, rows, n_in, n_out):
+    """Sums that one workgroup forms whole, over six products of parts."""
+    normal = make(n_in)
+    (x, xv), (wg, wgv), (wu, wuv) = normal(rows, n_in), normal(n_out, n_in, scale=n_in ** -0.5), normal(n_out, n_in, scale=n_in ** -0.5)
+    close(nd.gated_ffn(x, wg, wu), ref.ffn(xv, wgv, wuv, "silu"), "f32", "h")
+
+
 # ---------------------------------------------------------------- float: all 24 bits of an operand
 FINE = 1.0 + 2.0 ** -12 + 2.0 ** -20        # a value in each of its three parts
 REST = 2.0 ** -12 + 2.0 ** -20              # what is left where the leading part cancels
