@@ -282,7 +282,7 @@ __device__ inline const AttendArgs &set_of(const AttendSets &s) { return s.set[_
 // DS: widths of a and b in 32s.  DIRECT (bfloat16): rows are 16-byte granules at 16-byte
 // addresses, loaded to LDS directly, two chunks ahead; else through registers, one ahead.
 // Args: AttendSets, or AttendArgs of a single set, whose values stay in scalar registers (16384 tokens x 16
-// heads 105 us, found by a set's number 115).
+// heads of 128 114 us, found by a set's number 116; 12 x 4096 tokens x 16 heads of 64 123 and 139).
 // PASSING: the outputs, and a where no other set reads it, which this launch alone touches, are more than the
 // last cache should hold next to b and c, which the launch before has read too.
 template <class T, int DS, int NT, bool DIRECT, bool OUT, class Args, bool PASSING = false>
@@ -686,7 +686,7 @@ __global__ void __launch_bounds__(256, DIRECT && DS == 2 ? 3 : 2) attend_parts(A
         __builtin_amdgcn_s_waitcnt(0x0f70);
     } else {
         // The widest float tiles have no registers to hold the next chunk in meanwhile: the other workgroup on
-        // the compute unit covers its loads (16384 tokens x 16 heads of 128: 270 us; held and spilled, 326).
+        // the compute unit covers its loads (16384 tokens x 16 heads of 128: 260 us; held and spilled, 330).
         constexpr bool AHEAD = !(PARTS == 3 && DS == 4 && NT == 2);
         for (int base = 0; base < len; base += N) {
             __syncthreads();
@@ -886,18 +886,23 @@ template <class T> bool together(const AttendSets &s, const AttendArgs &b) {
 }  // namespace
 
 // How sequences are cut: into segments for two workgroups a compute unit (16 heads x
-// 16384 tokens of 128: 115 us; for one, 126; for four, whose states are twice the traffic, 143),
-// but of at least 128 tokens, a few chunks' work (16 heads x 2048 tokens: 34 us; of 64, 41; of
-// 256, 39), or 64 in float, whose chunks take three times as long (2 x 1000 tokens, 4 heads of
-// 100: 29 us; of 128, 36).  A packed batch is cut wherever a sequence may be longer than that: its
+// 16384 tokens of 128: 108 us; for one, 113; for four, whose states are twice the traffic, 126),
+// but of at least 128 tokens, a few chunks' work (16 heads x 2048 tokens: 31 us; of 64, 40; of
+// 256, 36), or 64 in float, whose chunks take three times as long (2 x 1000 tokens, 4 heads of
+// 100: 36 us; of 128, 48).  A packed batch is cut wherever a sequence may be longer than that: its
 // longest sequence is not known here, and would be walked by one workgroup while the others
 // are done.
 // Sequences of equal length are left whole where they fill three quarters of the compute units: one walk of
-// longer chains takes less than three launches and the states' way through memory (16 heads of
-// 128, bfloat16: 16 x 1024 tokens 63 us, cut 96; gradient of 8 x 2048 184, cut 227; of 4 x 4096 254, cut 270; of
-// 3 x 4096, which are too few, 254, cut 204).  Heads of up to 64 in 16 bits have shorter
-// chunks, and three workgroups on a compute unit hide each other's latency: past 1536 tokens they gain from
-// pieces (gradient of 4 x 4096: cut 117 us, whole 156; of 16 x 1024 forward: cut 43, whole 34).
+// longer chains takes less than three launches and the states' way through memory.  Measured at 128 to 576
+// workgroups of 16 heads and 256 to 16384 tokens, us cut / whole:
+//   heads of 128   12 x 1024 tokens   12 x 16384       gradient of 4 x 4096   of 8 x 2048   of 3 x 4096, too few
+//   bfloat16          96 /  65       1170 /  968         288 / 258             239 / 210      224 / 258
+//   half             143 / 119       1949 / 1837         484 / 461             385 / 340      364 / 458
+//   float            227 / 210       3441 / 3156         769 / 785             622 / 573      585 / 773
+// Heads of up to 64 in 16 bits have shorter chunks, and up to three workgroups on a compute unit hide each other's
+// latency: past 1536 tokens the gradient, and half's forward pass, gain from pieces (gradient of 4 x 4096: bfloat16
+// cut 119 us, whole 139, half 208 and 246; forward of 12 x 4096: half 200 and 229, but bfloat16 142 and 125; gradient of
+// 4 x 1024: 44 and 40).
 Cut attend_cut(int dtype, int64_t n_seq, int64_t n_tokens, int64_t heads, int64_t da, int64_t dc, bool packed, int sets) {
     const int64_t least = dtype == NDVM_F32 ? 64 : 128;
     const bool matrix = da <= kMostPartsDim;
@@ -909,7 +914,7 @@ Cut attend_cut(int dtype, int64_t n_seq, int64_t n_tokens, int64_t heads, int64_
     int64_t len = std::max<int64_t>(least, n_tokens / want);
     len = ceil_div(len, kSegStep) * kSegStep;
     const int64_t groups = n_seq * heads * ceil_div(dc, cols) * sets;
-    const bool short_chunks = std::max(da, dc) <= 64 && dtype != NDVM_F32;
+    const bool short_chunks = std::max(da, dc) <= 64 && (dtype == NDVM_F16 || (dtype == NDVM_BF16 && sets > 1));
     const bool whole = !packed && (n_seq >= want || (matrix && groups >= kCus * 3 / 4 && (!short_chunks || longest <= 1536)));
     if (len >= longest || whole) {
         c.seg_len = std::max<int64_t>(longest, 1);
@@ -971,7 +976,7 @@ hipError_t launch_attend(int dtype, const AttendSets &s, hipStream_t stream) {
             }
             with_parts<T>(run.set[0], [&](auto ds, auto nt, auto d) {
                 const AttendArgs &a = run.set[0];
-                // 16 heads x 16384 tokens of 128 (268 MB): passing was 10 us faster than all data as if it stayed (119, 129)
+                // 16 heads of 128: 16 x 2048 tokens 134 us, as if all data stayed 143; gradient of 16384 tokens 257 and 266
                 const bool passing = d.value && a.n_tokens * a.heads * (a.da + a.dc) * 4 >= kPassingTraffic;
                 if (passing) launch_parts<T, ds.value, nt.value, d.value, true, d.value>(run, stream);
                 else launch_parts<T, ds.value, nt.value, d.value, true, false>(run, stream);
