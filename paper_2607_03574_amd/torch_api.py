@@ -13,7 +13,7 @@ from __future__ import annotations
 import torch
 from torch.autograd.function import once_differentiable
 
-from . import Tape, _launch_stream, adam_step, gated_ffn_grad, grad, layer_norm_grad, linear_attention_grad
+from . import Tape, _launch_stream, _row_stride, adam_step, gated_ffn_grad, grad, layer_norm_grad, linear_attention_grad
 from . import gated_ffn as gated_ffn_op
 from . import layer_norm as layer_norm_op
 from . import linear_attention as linear_attention_op
@@ -61,10 +61,20 @@ def calibrate(tape: Tape, params, obs, steps: int, lr: float, beta1: float = 0.9
 
 
 # ---------------------------------------------------------------- encoder operators
+def _rows(x):
+    """x, or a copy of it where its rows are not contiguous or do not lie at one stride."""
+    try:
+        _row_stride(x, "x")
+    except ValueError:
+        return x.contiguous()
+    return x
+
+
 class LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, eps):
-        y, mean, rstd = layer_norm_op(x.detach(), weight, bias, eps)
+        x = _rows(x.detach())
+        y, mean, rstd = layer_norm_op(x, weight, bias, eps)
         ctx.save_for_backward(x, weight, mean, rstd)
         ctx.has_bias = bias is not None
         return y
@@ -119,9 +129,10 @@ def linear_attention(q, k, v, log_decay, offsets=None, scale=None, initial_state
 class GatedFFN(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w_gate, w_up, activation):
+        x, w_gate, w_up = (_rows(t.detach()) for t in (x, w_gate, w_up))
         ctx.save_for_backward(x, w_gate, w_up)
         ctx.activation = activation
-        return gated_ffn_op(x.detach(), w_gate.detach(), w_up.detach(), activation)
+        return gated_ffn_op(x, w_gate, w_up, activation)
 
     @staticmethod
     @once_differentiable
