@@ -464,8 +464,10 @@ ndvm_status ndvm_layer_norm_grad(int dtype, const void *dy, int64_t ld_dy, const
  * device int64 [n_seq + 1] that do not decrease, from 0 to n_tokens: token t of
  * sequence s at data + (offsets[s] + t)*tok_stride + head*head_stride.
  * Sequences without tokens are allowed (their final state is the initial one).
- * Offsets outside 0..n_tokens are read as the nearer end; where they decrease,
- * results are unspecified, with no access outside the tensors.
+ * Offsets outside 0..n_tokens are read as the nearer end; tokens ahead of the first
+ * or behind the last one belong to no sequence, and nothing is written for them;
+ * where offsets decrease, results are unspecified, with no access outside the
+ * tensors.
  * Limits: dk, dv <= 256, heads <= 65,535, n_tokens <= 2^30, and fewer than 2^24
  * pairs of a sequence (or a piece that a long one is cut into) and a head.
  */

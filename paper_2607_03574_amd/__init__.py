@@ -700,7 +700,8 @@ def linear_attention(q, k, v, log_decay, offsets=None, scale=None, initial_state
     """Linear attention with a decay for each head (ndvm_linear_attention):
     (o, final state or None) for q [sequences, tokens, heads, dk], k and v
     [.., kv_heads, dk or dv]; with `offsets` (int64 [sequences + 1], on the
-    device) the sequences lie one after the other in [tokens, heads, d].
+    device, from 0 to the number of tokens) the sequences lie one after the other in
+    [tokens, heads, d]; tokens outside them get no output.
     log_decay: float32 [heads]; scale: dk**-0.5 unless given; states are
     float32 [sequences, heads, dk, dv].  (With autograd: torch_api.linear_attention.)"""
     t = _t()
