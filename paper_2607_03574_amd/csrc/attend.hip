@@ -15,10 +15,12 @@
 // order, and the last one computes the outputs.  The gradient's three sums are formed
 // together where their widths allow it: dq's and dk's segments in one launch (dv starts from dk's,
 // transposed), all outputs in another.
-// Bound, at heads of 128, by memory: 16 heads x 16384 tokens 101 to 109 us (the segments' sums 33,
-// carrying 12, outputs 60: 270 MB of inputs and outputs, and as much again of segments' states and
-// second reads, at 5.2 TB/s); gradient of 8 x 2048 tokens, uncut, 175 to 181 us (470 MB needed, 710 moved at
-// 4.0 TB/s: a tensor is read by up to three sums).  Fewer instructions a chunk changed neither by 1%.
+// Bound, at heads of 128 in bfloat16, by memory and the vector instructions that split the state and pairs' products
+// in two parts: 16 heads x 16384 tokens 115 to 118 us (the segments' sums 33 to 39, carrying 12, outputs 70 to 85: 270 MB
+// of inputs and outputs, and as much again of segments' states and second reads, at 4.6 TB/s; with one part, an error of
+// sqrt(2) of the result's rounding, 104); gradient of 8 x 2048 tokens, uncut, 205 to 217 us (470 MB needed, 730 moved
+// at 3.4 TB/s: a tensor is read by up to three sums; one part: 177).  Half, through registers, 159 us and float 260 at
+// the first size.
 #include <algorithm>
 #include <type_traits>
 

@@ -5,8 +5,8 @@
 // written once.  A row stays in the registers of the threads that loaded it
 // (16, 64 or 256 of them, by its length), so mean, squares and result come
 // from one read; rows too long for that are read again, from cache.
-// Measured: 32768 x 2048 bf16 49 us a call, the kernel 44 (6.0 TB/s; a copy of 2 GiB runs at 4.8, one that
-// the last cache holds part of at 7.1); its gradient at 16384 x 2048 49 us, the kernel 41 (4.9 TB/s) and the
+// Measured: 32768 x 2048 bf16 49 us a call, the kernel 45 (6.0 TB/s; a copy that moves as much, part of it in the
+// last cache, 7.2, a larger one 5.5); its gradient at 16384 x 2048 49 us, the kernel 42 (4.8 TB/s) and the
 // sum of its partial sums 5.
 #include <algorithm>
 #include <type_traits>
