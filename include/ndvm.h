@@ -444,6 +444,47 @@ ndvm_status ndvm_layer_norm_grad(int dtype, const void *dy, int64_t ld_dy, const
                                  void *stream);
 
 /*
+ * Root-mean-square norm of `rows` rows of n values, with the addition of a residual:
+ *   h = x + residual, rounded to the tensors' type (x itself where residual is NULL)
+ *   y = h * rstd * weight,  rstd = 1 / sqrt(mean(h^2) + eps)
+ * Rows at multiples of their ld; weight [n] may be NULL (1).  h: where the sum goes
+ * (not read or written without a residual); rstd: float [rows], what the gradient
+ * takes, may be NULL.  Results are the same bits whatever the number of rows.
+ */
+ndvm_status ndvm_rms_norm(int dtype, const void *x, int64_t rows, int64_t n, int64_t ld_x, const void *residual,
+                          int64_t ld_residual, const void *weight, double eps, void *y, int64_t ld_y, void *h,
+                          int64_t ld_h, float *rstd, void *stream);
+
+/* Workspace bytes of ndvm_rms_norm_grad.  Host only. */
+ndvm_status ndvm_rms_norm_workspace_bytes(int64_t rows, int64_t n, size_t *bytes);
+
+/*
+ * Gradient of ndvm_rms_norm from dy, the forward pass's h, weight and rstd, and dh,
+ * what arrives at h from elsewhere (NULL: nothing): dx, which is the residual's
+ * gradient too, and dweight [n]; either may be NULL (not wanted).  dweight is a sum
+ * over all rows in float, added in a fixed order and rounded once; with rows = 0 it
+ * is 0.  Limit: n <= 2^27.
+ */
+ndvm_status ndvm_rms_norm_grad(int dtype, const void *dy, int64_t ld_dy, const void *h, int64_t ld_h, int64_t rows,
+                               int64_t n, const void *weight, const float *rstd, const void *dh, int64_t ld_dh,
+                               void *dx, int64_t ld_dx, void *dweight, void *workspace, size_t workspace_bytes,
+                               void *stream);
+
+/*
+ * Rows in 8 bits: bytes in e4m3 (OCP: largest value 448, no infinities) and a float
+ * scale for each row, value = byte * scale, with
+ *   scale = max(largest |value| of the row, 448 * 2^-126) / 448.
+ * A row with a NaN has the scale NaN.  (Read by ndvm_linear_8bit.)
+ * ndvm_rms_norm_8bit: y of ndvm_rms_norm, rounded once, to 8 bits;
+ * ndvm_quantize_rows: the rows of x.  ld_y is in bytes.
+ */
+ndvm_status ndvm_rms_norm_8bit(int dtype, const void *x, int64_t rows, int64_t n, int64_t ld_x, const void *residual,
+                               int64_t ld_residual, const void *weight, double eps, void *y, int64_t ld_y,
+                               float *scale, void *h, int64_t ld_h, void *stream);
+ndvm_status ndvm_quantize_rows(int dtype, const void *x, int64_t rows, int64_t n, int64_t ld_x, void *y, int64_t ld_y,
+                               float *scale, void *stream);
+
+/*
  * Linear attention with a decay for each head.  Over the tokens t of a sequence,
  * for query head h that reads key and value head c = h / (heads / kv_heads):
  *   S_t = exp(log_decay[h]) S_{t-1} + k_t^T v_t      (S: [dk, dv], float)

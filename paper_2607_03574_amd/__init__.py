@@ -31,6 +31,7 @@ EXPORTS = ["ndvm_tape_build", "ndvm_tape_upload", "ndvm_tape_upload_many", "ndvm
            "ndvm_grad_points", "ndvm_workspace_bytes_points", "ndvm_walk_prepare", "ndvm_walk_measure", "ndvm_walk_workspace_bytes",
            "ndvm_walk_grad", "ndvm_walk_status", "ndvm_walk_free",
            "ndvm_layer_norm", "ndvm_layer_norm_workspace_bytes", "ndvm_layer_norm_grad",
+           "ndvm_rms_norm", "ndvm_rms_norm_workspace_bytes", "ndvm_rms_norm_grad", "ndvm_rms_norm_8bit", "ndvm_quantize_rows",
            "ndvm_linear_attention_workspace_bytes", "ndvm_linear_attention", "ndvm_linear_attention_grad",
            "ndvm_linear_attention_step", "ndvm_gated_ffn_workspace_bytes", "ndvm_gated_ffn", "ndvm_gated_ffn_grad"]
 ACTIVATIONS = {"silu": 0, "gelu": 1, "sigmoid": 2, "relu": 3}     # NDVM_ACT_*
@@ -109,6 +110,12 @@ _norm = _sig("ndvm_layer_norm", _int, [_int, _vp, _i64, _i64, _i64, _vp, _vp, _f
 _norm_ws = _sig("ndvm_layer_norm_workspace_bytes", _int, [_i64, _i64, ctypes.POINTER(_sz)])
 _norm_grad = _sig("ndvm_layer_norm_grad", _int, [_int, _vp, _i64, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _i64, _vp,
                                                  _vp, _vp, _sz, _vp])
+_rms = _sig("ndvm_rms_norm", _int, [_int, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _f64, _vp, _i64, _vp, _i64, _vp, _vp])
+_rms_ws = _sig("ndvm_rms_norm_workspace_bytes", _int, [_i64, _i64, ctypes.POINTER(_sz)])
+_rms_grad = _sig("ndvm_rms_norm_grad", _int, [_int, _vp, _i64, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp,
+                                              _sz, _vp])
+_rms_8bit = _sig("ndvm_rms_norm_8bit", _int, [_int, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _f64, _vp, _i64, _vp, _vp, _i64, _vp])
+_quantize = _sig("ndvm_quantize_rows", _int, [_int, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _vp])
 _attn_ws = _sig("ndvm_linear_attention_workspace_bytes", _int, [_shape_p, _int, _int, ctypes.POINTER(_sz)])
 _attn = _sig("ndvm_linear_attention", _int, [_shape_p, _heads_p, _heads_p, _heads_p, _vp, _vp, _vp, _heads_p, _vp, _vp,
                                              _sz, _vp])
@@ -487,7 +494,7 @@ class _Torch:
         import torch
         self.torch = torch
         self.codes = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-        self.f32, self.u8, self.i64 = torch.float32, torch.uint8, torch.int64
+        self.f32, self.u8, self.i64, self.e4m3 = torch.float32, torch.uint8, torch.int64, torch.float8_e4m3fn
         self.Tensor, self.empty_like = torch.Tensor, torch.empty_like
         self.grad_enabled, self.increment_version = torch.is_grad_enabled, torch.autograd.graph.increment_version
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -650,6 +657,102 @@ def layer_norm_grad(dy, x, weight, mean, rstd, need_input: bool = True, need_wei
                           db.data_ptr() if need_weight else None, ws.data_ptr() if need_weight else None, need.value, s),
                "ndvm_layer_norm_grad")
     return dx, dw, db
+
+
+def _rms_args(t, x, weight, residual):
+    """Checks of the norm's inputs: type, rows, their width, strides of x and of the residual, and addresses."""
+    dt, dtype, dev, shape = _op_type(t, x, "x"), x.dtype, x.device, x.shape
+    ld = _row_stride(x, "x")
+    n = shape[-1]
+    w, r, ld_r = _of(weight, "weight", dtype, (n,), dev), None, 0
+    if residual is not None:
+        _alike(x, ("residual", residual))
+        if residual.shape != shape:
+            raise ValueError("residual must have the shape of x")
+        r, ld_r = residual.data_ptr(), _row_stride(residual, "residual")
+    return dt, x.numel() // n if n else 0, n, ld, w, r, ld_r
+
+
+def rms_norm(x, weight=None, residual=None, eps: float = 1e-5, out=None, stream=None):
+    """(y, h, rstd) of the rows (last axis) of x (ndvm_rms_norm): h = x + residual
+    (x itself without one), y its norm; rstd, float32 of x's leading shape, is what
+    rms_norm_grad takes.  (With autograd: torch_api.rms_norm.)"""
+    t = _t()
+    dt, rows, n, ld, w, r, ld_r = _rms_args(t, x, weight, residual)
+    with _On(t, stream, x.device) as s:
+        if out is None:
+            out, ld_out = _like(t, x), n
+        else:
+            _alike(x, ("out", out))
+            if out.shape != x.shape:
+                raise ValueError("out must have the shape of x")
+            ld_out = _row_stride(out, "out")
+            _to_write(t, out, "out")
+        h = x if r is None else _like(t, x)
+        rstd = x.new_empty(x.shape[:-1], dtype=t.f32)
+        st = _rms(dt, x.data_ptr(), rows, n, ld, r, ld_r, w, eps, out.data_ptr(), ld_out, h.data_ptr(), n, rstd.data_ptr(), s)
+        if st:
+            _check(st, "ndvm_rms_norm")
+    return out, h, rstd
+
+
+def rms_norm_grad(dy, h, weight, rstd, dh=None, need_input: bool = True, need_weight: bool = True, stream=None):
+    """(dx, dweight) of rms_norm (ndvm_rms_norm_grad), dx with dh, what arrives at h
+    from elsewhere, added: it is the residual's gradient too.  What is not needed is
+    None; weight may be None (its gradient is still that of a weight of ones)."""
+    t = _t()
+    dt, dtype, dev, shape = _op_type(t, h, "h"), h.dtype, h.device, h.shape
+    _alike(h, ("dy", dy))
+    if dy.shape != shape:
+        raise ValueError("dy must have the shape of h")
+    ld_h, ld_dy = _row_stride(h, "h"), _row_stride(dy, "dy")
+    n, lead = shape[-1], shape[:-1]
+    rows = h.numel() // n if n else 0
+    w, r = _of(weight, "weight", dtype, (n,), dev), _of(rstd, "rstd", t.f32, lead, dev)
+    more, ld_more = None, 0
+    if dh is not None:
+        _alike(h, ("dh", dh))
+        if dh.shape != shape:
+            raise ValueError("dh must have the shape of h")
+        more, ld_more = dh.data_ptr(), _row_stride(dh, "dh")
+    with _On(t, stream, dev) as s:
+        dx = _like(t, h) if need_input else None
+        dw = ws = None
+        need = _sz()
+        if need_weight:
+            dw = h.new_empty(n)
+            _check(_rms_ws(rows, n, ctypes.byref(need)), "ndvm_rms_norm_workspace_bytes")
+            ws = h.new_empty(need.value, dtype=t.u8)
+        _check(_rms_grad(dt, dy.data_ptr(), ld_dy, h.data_ptr(), ld_h, rows, n, w, r, more, ld_more,
+                         dx.data_ptr() if need_input else None, n, dw.data_ptr() if need_weight else None,
+                         ws.data_ptr() if need_weight else None, need.value, s), "ndvm_rms_norm_grad")
+    return dx, dw
+
+
+def rms_norm_8bit(x, weight=None, residual=None, eps: float = 1e-5, stream=None):
+    """(y, scale, h) (ndvm_rms_norm_8bit): rms_norm's y rounded once to float8_e4m3fn, whose
+    values stand for themselves times their row's scale (float32 of x's leading shape).
+    There is no gradient through it."""
+    t = _t()
+    dt, rows, n, ld, w, r, ld_r = _rms_args(t, x, weight, residual)
+    with _On(t, stream, x.device) as s:
+        y = x.new_empty(x.shape, dtype=t.e4m3)
+        h = x if r is None else _like(t, x)
+        scale = x.new_empty(x.shape[:-1], dtype=t.f32)
+        _check(_rms_8bit(dt, x.data_ptr(), rows, n, ld, r, ld_r, w, eps, y.data_ptr(), n, scale.data_ptr(), h.data_ptr(), n, s),
+               "ndvm_rms_norm_8bit")
+    return y, scale, h
+
+
+def quantize_rows(x, stream=None):
+    """(y, scale) (ndvm_quantize_rows): the rows of x in float8_e4m3fn and their scales, as
+    rms_norm_8bit returns them; for the weights of linear_8bit."""
+    t = _t()
+    dt, rows, n, ld, _, _, _ = _rms_args(t, x, None, None)
+    with _On(t, stream, x.device) as s:
+        y, scale = x.new_empty(x.shape, dtype=t.e4m3), x.new_empty(x.shape[:-1], dtype=t.f32)
+        _check(_quantize(dt, x.data_ptr(), rows, n, ld, y.data_ptr(), n, scale.data_ptr(), s), "ndvm_quantize_rows")
+    return y, scale
 
 
 def _heads(x, name, lead, heads, width):

@@ -1,5 +1,5 @@
-// Operators of a sequence encoder (layer norm, linear attention with decay,
-// gated feed-forward): what their kernels' files and the C entry points share.
+// Operators of a sequence encoder (norms, linear attention with decay, gated
+// feed-forward): what their kernels' files and the C entry points share.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -42,6 +42,27 @@ struct NormGradArgs {
 constexpr int64_t kMostNormGrad = int64_t(1) << 27;     // values of a row
 size_t norm_grad_bytes(int64_t rows, int64_t n);
 hipError_t launch_norm_grad(int dtype, const NormGradArgs &a, hipStream_t stream);
+
+// ---- root-mean-square norm with a residual, and rows in 8 bits
+struct RmsArgs {
+    const void *x, *residual, *weight;
+    void *y, *h;                // y in e4m3 where there is a scale
+    float *rstd, *scale;
+    int64_t rows, n, ld_x, ld_r, ld_y, ld_h;
+    float eps;
+    int rows_only;              // with a scale: x itself in 8 bits, not its norm
+};
+hipError_t launch_rms(int dtype, const RmsArgs &a, hipStream_t stream);
+
+struct RmsGradArgs {
+    const void *dy, *h, *weight, *dh;
+    const float *rstd;
+    void *dx, *dweight;
+    float *part;                // [groups][n] partial sums of dweight
+    int64_t rows, n, ld_dy, ld_h, ld_dh, ld_dx;
+};
+size_t rms_grad_bytes(int64_t rows, int64_t n);
+hipError_t launch_rms_grad(int dtype, const RmsGradArgs &a, hipStream_t stream);
 
 // ---- linear attention: out_i = sum_{j<=i} lambda^(i-j) (a_i . b_j) c_j over the
 // tokens of a sequence taken in order (or, reversed, from the last to the first)

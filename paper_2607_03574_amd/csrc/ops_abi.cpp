@@ -163,6 +163,81 @@ ndvm_status ndvm_layer_norm_grad(int dtype, const void *dy, int64_t ld_dy, const
     });
 }
 
+// rms_norm and its form with an 8-bit result: checks, and the launch
+static ndvm_status run_rms(const char *who, int dtype, const RmsArgs &a, double eps, void *stream) {
+    if (!known_type(dtype)) return bad(who, "unknown type");
+    if (a.rows < 0 || a.n < 1 || a.ld_x < a.n || a.ld_y < a.n || (a.residual && (a.ld_r < a.n || a.ld_h < a.n)) || !(eps >= 0.0) ||
+        !std::isfinite(eps))
+        return bad(who, "bad size, stride or eps");
+    if (!fits(a.rows, std::max(std::max(a.ld_x, a.ld_y), a.residual ? std::max(a.ld_r, a.ld_h) : 0))) return bad(who, "sizes overflow");
+    if (a.rows == 0) return NDVM_OK;
+    if (!a.x || !a.y || (a.residual && !a.h)) return bad(who, "null buffer");
+    return launched(who, launch_rms(dtype, a, static_cast<hipStream_t>(stream)));
+}
+
+ndvm_status ndvm_rms_norm(int dtype, const void *x, int64_t rows, int64_t n, int64_t ld_x, const void *residual,
+                          int64_t ld_residual, const void *weight, double eps, void *y, int64_t ld_y, void *h, int64_t ld_h,
+                          float *rstd, void *stream) {
+    return guarded([&]() -> ndvm_status {
+        const RmsArgs a{x, residual, weight, y, h, rstd, nullptr, rows, n, ld_x, ld_residual, ld_y, ld_h, float(eps), 0};
+        return run_rms("ndvm_rms_norm", dtype, a, eps, stream);
+    });
+}
+
+ndvm_status ndvm_rms_norm_8bit(int dtype, const void *x, int64_t rows, int64_t n, int64_t ld_x, const void *residual,
+                               int64_t ld_residual, const void *weight, double eps, void *y, int64_t ld_y, float *scale, void *h,
+                               int64_t ld_h, void *stream) {
+    return guarded([&]() -> ndvm_status {
+        const char *who = "ndvm_rms_norm_8bit";
+        if (rows > 0 && !scale) return bad(who, "null buffer");
+        const RmsArgs a{x, residual, weight, y, h, nullptr, scale, rows, n, ld_x, ld_residual, ld_y, ld_h, float(eps), 0};
+        return run_rms(who, dtype, a, eps, stream);
+    });
+}
+
+ndvm_status ndvm_quantize_rows(int dtype, const void *x, int64_t rows, int64_t n, int64_t ld_x, void *y, int64_t ld_y, float *scale,
+                               void *stream) {
+    return guarded([&]() -> ndvm_status {
+        const char *who = "ndvm_quantize_rows";
+        if (rows > 0 && !scale) return bad(who, "null buffer");
+        const RmsArgs a{x, nullptr, nullptr, y, nullptr, nullptr, scale, rows, n, ld_x, 0, ld_y, 0, 0.0f, 1};
+        return run_rms(who, dtype, a, 0.0, stream);
+    });
+}
+
+ndvm_status ndvm_rms_norm_workspace_bytes(int64_t rows, int64_t n, size_t *bytes) {
+    return guarded([&]() -> ndvm_status {
+        const char *who = "ndvm_rms_norm_workspace_bytes";
+        if (!bytes) return bad(who, "null pointer");
+        if (rows < 0 || n < 1 || !fits(rows, n)) return bad(who, "bad size");
+        if (n > kMostNormGrad) return fail(NDVM_E_UNSUPPORTED, who, "more than 2^27 values in a row");
+        *bytes = rms_grad_bytes(rows, n);
+        return NDVM_OK;
+    });
+}
+
+ndvm_status ndvm_rms_norm_grad(int dtype, const void *dy, int64_t ld_dy, const void *h, int64_t ld_h, int64_t rows, int64_t n,
+                               const void *weight, const float *rstd, const void *dh, int64_t ld_dh, void *dx, int64_t ld_dx,
+                               void *dweight, void *workspace, size_t workspace_bytes, void *stream) {
+    return guarded([&]() -> ndvm_status {
+        const char *who = "ndvm_rms_norm_grad";
+        if (!known_type(dtype)) return bad(who, "unknown type");
+        if (rows < 0 || n < 1 || ld_dy < n || ld_h < n || (dx && ld_dx < n) || (dh && ld_dh < n)) return bad(who, "bad size or stride");
+        if (!fits(rows, std::max(std::max(ld_h, ld_dy), std::max(dx ? ld_dx : 0, dh ? ld_dh : 0)))) return bad(who, "sizes overflow");
+        if (n > kMostNormGrad) return fail(NDVM_E_UNSUPPORTED, who, "more than 2^27 values in a row");
+        if (rows && (!dy || !h || !rstd)) return bad(who, "null buffer");
+        if (!dx && !dweight) return NDVM_OK;
+        if (dweight) {
+            if (workspace_bytes < rms_grad_bytes(rows, n)) return fail(NDVM_E_NOMEM, who, "workspace too small");
+            if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 4) return bad(who, "null or misaligned workspace");
+        } else if (rows == 0) {
+            return NDVM_OK;
+        }
+        const RmsGradArgs a{dy, h, weight, dh, rstd, dx, dweight, static_cast<float *>(workspace), rows, n, ld_dy, ld_h, ld_dh, ld_dx};
+        return launched(who, launch_rms_grad(dtype, a, static_cast<hipStream_t>(stream)));
+    });
+}
+
 ndvm_status ndvm_linear_attention_workspace_bytes(const ndvm_attention_shape *shape, int packed, int with_grad,
                                                   size_t *bytes) {
     return guarded([&]() -> ndvm_status {

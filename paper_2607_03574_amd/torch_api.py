@@ -13,10 +13,12 @@ from __future__ import annotations
 import torch
 from torch.autograd.function import once_differentiable
 
-from . import Tape, _launch_stream, _row_stride, adam_step, gated_ffn_grad, grad, layer_norm_grad, linear_attention_grad
+from . import (Tape, _launch_stream, _row_stride, adam_step, gated_ffn_grad, grad, layer_norm_grad, linear_attention_grad,
+               rms_norm_grad)
 from . import gated_ffn as gated_ffn_op
 from . import layer_norm as layer_norm_op
 from . import linear_attention as linear_attention_op
+from . import rms_norm as rms_norm_op
 
 
 class ReplayLoss(torch.autograd.Function):
@@ -91,6 +93,33 @@ class LayerNorm(torch.autograd.Function):
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5):
     """Layer norm over the last axis with autograd support (layer_norm of the package)."""
     return LayerNorm.apply(x, weight, bias, eps)
+
+
+class RmsNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, residual, eps):
+        x = _rows(x.detach())
+        y, h, rstd = rms_norm_op(x, weight, None if residual is None else _rows(residual.detach()), eps)
+        ctx.save_for_backward(h, weight, rstd)
+        ctx.set_materialize_grads(False)
+        return y if residual is None else (y, h)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dh=None):
+        h, weight, rstd = ctx.saved_tensors
+        if dy is None:      # y went nowhere
+            return dh if ctx.needs_input_grad[0] else None, None, dh if ctx.needs_input_grad[2] else None, None
+        need_input = ctx.needs_input_grad[0] or ctx.needs_input_grad[2]
+        dx, dw = rms_norm_grad(dy.contiguous(), h, weight, rstd, None if dh is None else dh.contiguous(), need_input,
+                               ctx.needs_input_grad[1])
+        return dx if ctx.needs_input_grad[0] else None, dw, dx if ctx.needs_input_grad[2] else None, None
+
+
+def rms_norm(x, weight=None, residual=None, eps: float = 1e-5):
+    """Root-mean-square norm over the last axis with autograd support (rms_norm of the package):
+    y, or (y, h) with a residual, h = x + residual."""
+    return RmsNorm.apply(x, weight, residual, eps)
 
 
 class LinearAttention(torch.autograd.Function):
