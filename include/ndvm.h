@@ -570,6 +570,7 @@ ndvm_status ndvm_linear_attention_step(const ndvm_attention_shape *shape, const 
 #define NDVM_ACT_GELU 1       /* g (1 + erf(g / sqrt 2)) / 2 */
 #define NDVM_ACT_SIGMOID 2    /* 1 / (1 + exp(-g)) */
 #define NDVM_ACT_RELU 3       /* max(g, 0); derivative 0 at 0 */
+#define NDVM_ACT_NONE 4       /* g; of ndvm_linear and its like only */
 
 /* Workspace bytes of ndvm_gated_ffn (with_grad = 0) or its gradient.  Host only. */
 ndvm_status ndvm_gated_ffn_workspace_bytes(int dtype, int64_t rows, int64_t n_in, int64_t n_out, int with_grad,
@@ -594,6 +595,49 @@ ndvm_status ndvm_gated_ffn_grad(int dtype, int act, const void *dh, int64_t ld_d
                                 int64_t ld_up, int64_t n_out, void *dx, int64_t ld_dx, void *dw_gate,
                                 int64_t ld_dgate, void *dw_up, int64_t ld_dup, void *workspace,
                                 size_t workspace_bytes, void *stream);
+
+/*
+ * Projection of `rows` rows:
+ *   y = act(x w^T + bias) + residual
+ * x [rows, n_in], w [n_out, n_in], residual and y [rows, n_out], rows at multiples of
+ * their ld; bias [n_out]; bias and residual may be NULL (0).  act: NDVM_ACT_*.
+ * Limits: n_in, n_out <= 2^21, rows <= 2^22.
+ */
+/* Workspace bytes of ndvm_linear (with_grad = 0) or its gradient.  Host only. */
+ndvm_status ndvm_linear_workspace_bytes(int dtype, int act, int64_t rows, int64_t n_in, int64_t n_out, int with_grad,
+                                        size_t *bytes);
+
+ndvm_status ndvm_linear(int dtype, int act, const void *x, int64_t rows, int64_t n_in, int64_t ld_x, const void *w,
+                        int64_t ld_w, int64_t n_out, const void *bias, const void *residual, int64_t ld_residual,
+                        void *y, int64_t ld_y, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Gradient of ndvm_linear from dy (which is the residual's gradient itself) and the
+ * forward pass's x, w and bias (x w^T is formed again where there is an activation;
+ * bias is read only then).  dx [rows, n_in], dw [n_out, n_in], db [n_out]: any may be
+ * NULL (not wanted); with rows = 0 dw and db are 0.  dz = dy act'(z) is an operand of
+ * further products and is rounded to the tensors' type for them, in half as the
+ * operands of ndvm_gated_ffn_grad are.  Sums are in float, in a fixed order.
+ */
+ndvm_status ndvm_linear_grad(int dtype, int act, const void *dy, int64_t ld_dy, const void *x, int64_t rows,
+                             int64_t n_in, int64_t ld_x, const void *w, int64_t ld_w, int64_t n_out, const void *bias,
+                             void *dx, int64_t ld_dx, void *dw, int64_t ld_dw, void *db, void *workspace,
+                             size_t workspace_bytes, void *stream);
+
+/*
+ * ndvm_linear of 8-bit rows (ndvm_rms_norm_8bit, ndvm_quantize_rows): x and w hold bytes
+ * in e4m3, ld_x and ld_w in bytes, x_scale [rows] and w_scale [n_out] their rows' scales:
+ *   y = act((x w^T) * x_scale * w_scale + bias) + residual
+ * with bias, residual and y of type `dtype`: NDVM_BF16 or NDVM_F16 (NDVM_F32 is
+ * NDVM_E_UNSUPPORTED: of every eight products the bits below 2^-13 of the largest may be
+ * cut before they are added in float, which is little beside the rounding of a 16-bit
+ * result only).
+ */
+ndvm_status ndvm_linear_8bit_workspace_bytes(int64_t rows, int64_t n_in, int64_t n_out, size_t *bytes);
+ndvm_status ndvm_linear_8bit(int dtype, int act, const void *x, const float *x_scale, int64_t rows, int64_t n_in,
+                             int64_t ld_x, const void *w, const float *w_scale, int64_t ld_w, int64_t n_out,
+                             const void *bias, const void *residual, int64_t ld_residual, void *y, int64_t ld_y,
+                             void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -33,8 +33,10 @@ EXPORTS = ["ndvm_tape_build", "ndvm_tape_upload", "ndvm_tape_upload_many", "ndvm
            "ndvm_layer_norm", "ndvm_layer_norm_workspace_bytes", "ndvm_layer_norm_grad",
            "ndvm_rms_norm", "ndvm_rms_norm_workspace_bytes", "ndvm_rms_norm_grad", "ndvm_rms_norm_8bit", "ndvm_quantize_rows",
            "ndvm_linear_attention_workspace_bytes", "ndvm_linear_attention", "ndvm_linear_attention_grad",
-           "ndvm_linear_attention_step", "ndvm_gated_ffn_workspace_bytes", "ndvm_gated_ffn", "ndvm_gated_ffn_grad"]
+           "ndvm_linear_attention_step", "ndvm_gated_ffn_workspace_bytes", "ndvm_gated_ffn", "ndvm_gated_ffn_grad",
+           "ndvm_linear_workspace_bytes", "ndvm_linear", "ndvm_linear_grad", "ndvm_linear_8bit_workspace_bytes", "ndvm_linear_8bit"]
 ACTIVATIONS = {"silu": 0, "gelu": 1, "sigmoid": 2, "relu": 3}     # NDVM_ACT_*
+ACT_NONE = 4           # NDVM_ACT_NONE: no activation (linear)
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is missing: build it with paper_2607_03574_amd/build.py "
@@ -128,6 +130,14 @@ _ffn = _sig("ndvm_gated_ffn", _int, [_int, _int, _vp, _i64, _i64, _i64, _vp, _i6
                                      _vp])
 _ffn_grad = _sig("ndvm_gated_ffn_grad", _int, [_int, _int, _vp, _i64, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _i64,
                                                _vp, _i64, _vp, _i64, _vp, _i64, _vp, _sz, _vp])
+
+_linear_ws = _sig("ndvm_linear_workspace_bytes", _int, [_int, _int, _i64, _i64, _i64, _int, ctypes.POINTER(_sz)])
+_linear = _sig("ndvm_linear", _int, [_int, _int, _vp, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _sz, _vp])
+_linear_grad = _sig("ndvm_linear_grad", _int, [_int, _int, _vp, _i64, _vp, _i64, _i64, _i64, _vp, _i64, _i64, _vp, _vp, _i64, _vp,
+                                               _i64, _vp, _vp, _sz, _vp])
+_linear8_ws = _sig("ndvm_linear_8bit_workspace_bytes", _int, [_i64, _i64, _i64, ctypes.POINTER(_sz)])
+_linear8 = _sig("ndvm_linear_8bit", _int, [_int, _int, _vp, _vp, _i64, _i64, _i64, _vp, _vp, _i64, _i64, _vp, _vp, _i64, _vp,
+                                           _i64, _vp, _sz, _vp])
 
 
 class NdvmError(RuntimeError):
@@ -953,3 +963,108 @@ def gated_ffn_grad(dh, x, w_gate, w_up, activation: str = "silu", need_input: bo
                          n_in, du.data_ptr() if need_weight else None, n_in, ws_ptr, need, s),
                "ndvm_gated_ffn_grad")
     return dx, dg, du
+
+
+def _linear_sizes(x, weight, activation):
+    """Checks of a projection's activation and sizes: (its code, rows, n_in, n_out)."""
+    act = ACT_NONE if activation is None else ACTIVATIONS.get(activation)
+    if act is None:
+        raise ValueError(f"activation must be None or one of {sorted(ACTIVATIONS)}")
+    if weight.dim() != 2 or x.dim() < 1 or x.shape[-1] != weight.shape[1]:
+        raise ValueError("weight must be [n_out, n_in], x [.., n_in]")
+    n_out, n_in = weight.shape
+    return act, x.numel() // n_in if n_in else 0, n_in, n_out
+
+
+def _linear_out(t, x, dtype, n_out, residual, out):
+    """Output of a projection, and the residual's address and stride; under the call's stream."""
+    shape = (*x.shape[:-1], n_out)
+    r, ld_r = None, 0
+    if residual is not None:
+        if getattr(residual, "dtype", None) is not dtype or residual.device != x.device:
+            raise TypeError("residual must be a tensor of the output's type and device")
+        if residual.shape != shape:
+            raise ValueError("residual must be [.., n_out]")
+        r, ld_r = residual.data_ptr(), _row_stride(residual, "residual")
+    if out is None:
+        return x.new_empty(shape, dtype=dtype), n_out, r, ld_r
+    if getattr(out, "dtype", None) is not dtype or out.device != x.device:
+        raise TypeError("out must be a tensor of the output's type and device")
+    if out.shape != shape:
+        raise ValueError("out must be [.., n_out]")
+    ld = _row_stride(out, "out")
+    _to_write(t, out, "out")
+    return out, ld, r, ld_r
+
+
+def linear(x, weight, bias=None, activation: Optional[str] = None, residual=None, out=None, stream=None):
+    """act(x weight^T + bias) + residual (ndvm_linear) for x [.., n_in], weight [n_out, n_in],
+    bias [n_out] and residual [.., n_out]; activation: None, silu, gelu, sigmoid or relu.
+    (With autograd: torch_api.linear.)"""
+    t = _t()
+    dt = _op_type(t, x, "x")
+    _alike(x, ("weight", weight))
+    act, rows, n_in, n_out = _linear_sizes(x, weight, activation)
+    ld_x, ld_w = _row_stride(x, "x"), _row_stride(weight, "weight")
+    b = _of(bias, "bias", x.dtype, (n_out,), x.device)
+    with _On(t, stream, x.device) as s:
+        out, ld_out, r, ld_r = _linear_out(t, x, x.dtype, n_out, residual, out)
+        need = _sz()
+        _check(_linear_ws(dt, act, rows, n_in, n_out, 0, ctypes.byref(need)), "ndvm_linear_workspace_bytes")
+        ws = x.new_empty(need.value, dtype=t.u8) if need.value else None
+        _check(_linear(dt, act, x.data_ptr(), rows, n_in, ld_x, weight.data_ptr(), ld_w, n_out, b, r, ld_r, out.data_ptr(), ld_out,
+                       ws.data_ptr() if ws is not None else None, need.value, s), "ndvm_linear")
+    return out
+
+
+def linear_grad(dy, x, weight, bias=None, activation: Optional[str] = None, need_input: bool = True, need_weight: bool = True,
+                need_bias: bool = True, stream=None):
+    """(dx, dweight, dbias) of linear (ndvm_linear_grad); what is not needed is None, as is
+    dbias without a bias.  (The residual's gradient is dy.)"""
+    t = _t()
+    dt = _op_type(t, x, "x")
+    _alike(x, ("weight", weight), ("dy", dy))
+    act, rows, n_in, n_out = _linear_sizes(x, weight, activation)
+    if dy.shape != (*x.shape[:-1], n_out):
+        raise ValueError("dy must be [.., n_out]")
+    b = _of(bias, "bias", x.dtype, (n_out,), x.device)
+    ld_dy, ld_x, ld_w = _row_stride(dy, "dy"), _row_stride(x, "x"), _row_stride(weight, "weight")
+    with _On(t, stream, x.device) as s:
+        dx = _like(t, x) if need_input else None
+        dw = _like(t, weight) if need_weight else None
+        db = x.new_empty(n_out) if need_bias and b is not None else None
+        need = _sz()
+        _check(_linear_ws(dt, act, rows, n_in, n_out, 1, ctypes.byref(need)), "ndvm_linear_workspace_bytes")
+        ws = x.new_empty(need.value, dtype=t.u8)
+        _check(_linear_grad(dt, act, dy.data_ptr(), ld_dy, x.data_ptr(), rows, n_in, ld_x, weight.data_ptr(), ld_w, n_out, b,
+                            dx.data_ptr() if dx is not None else None, n_in, dw.data_ptr() if dw is not None else None, n_in,
+                            db.data_ptr() if db is not None else None, ws.data_ptr(), need.value, s), "ndvm_linear_grad")
+    return dx, dw, db
+
+
+def linear_8bit(x, x_scale, weight, weight_scale, bias=None, activation: Optional[str] = None, residual=None, dtype=None,
+                out=None, stream=None):
+    """linear of 8-bit rows (ndvm_linear_8bit): x [.., n_in] and weight [n_out, n_in] in
+    float8_e4m3fn with a float32 scale for each row (rms_norm_8bit, quantize_rows); the
+    result, bias and residual have the type `dtype` (bfloat16, unless it is float16).  There is
+    no gradient through it."""
+    t = _t()
+    dtype = t.torch.bfloat16 if dtype is None else dtype
+    dt = t.codes.get(dtype)
+    if dt is None or dtype is t.f32:
+        raise TypeError("dtype must be bfloat16 or float16")
+    if not isinstance(x, t.Tensor) or not x.is_cuda or x.dtype is not t.e4m3:
+        raise TypeError("x must be a float8_e4m3fn CUDA/ROCm tensor")
+    _alike(x, ("weight", weight))
+    act, rows, n_in, n_out = _linear_sizes(x, weight, activation)
+    ld_x, ld_w = _row_stride(x, "x"), _row_stride(weight, "weight")
+    xs, ws_ = _of(x_scale, "x_scale", t.f32, x.shape[:-1], x.device), _of(weight_scale, "weight_scale", t.f32, (n_out,), x.device)
+    b = _of(bias, "bias", dtype, (n_out,), x.device)
+    with _On(t, stream, x.device) as s:
+        out, ld_out, r, ld_r = _linear_out(t, x, dtype, n_out, residual, out)
+        need = _sz()
+        _check(_linear8_ws(rows, n_in, n_out, ctypes.byref(need)), "ndvm_linear_8bit_workspace_bytes")
+        ws = x.new_empty(need.value, dtype=t.u8) if need.value else None
+        _check(_linear8(dt, act, x.data_ptr(), xs, rows, n_in, ld_x, weight.data_ptr(), ws_, ld_w, n_out, b, r, ld_r, out.data_ptr(),
+                        ld_out, ws.data_ptr() if ws is not None else None, need.value, s), "ndvm_linear_8bit")
+    return out

@@ -1,4 +1,4 @@
-// How the products of the gated feed-forward are cut into tiles and sums, by their sizes.
+// How the products of the projections are cut into tiles and sums, by their sizes.
 #pragma once
 #include <algorithm>
 
@@ -18,9 +18,8 @@ constexpr int kStep = 32;       // of the sum, per LDS tile
 struct Gated {
     int64_t ba, bb, splits;
 };
-inline Gated gated_cut(int dtype, int64_t rows, int64_t n_in, int64_t n_out) {
-    const int64_t steps = ceil_div(n_in, kStep) * (dtype == NDVM_F32 ? 6 : 1);
-    const auto tiles = [&](int64_t ba, int64_t bb) { return ceil_div(n_out, ba / 2) * ceil_div(rows, bb); };
+inline Gated cut_tiles(int64_t rows, int64_t steps, int64_t columns) {
+    const auto tiles = [&](int64_t ba, int64_t bb) { return ceil_div(columns, ba) * ceil_div(rows, bb); };
     const int64_t large = ceil_div(tiles(256, 256), kCus) * 100, middle = ceil_div(tiles(256, 128), kCus) * 56;
     const int64_t few_tiles = tiles(128, 128), small = few_tiles <= kCus ? 40 : ceil_div(few_tiles, 2 * kCus) * 64;
     if (large <= middle && large <= small) return Gated{256, 256, 1};
@@ -28,6 +27,11 @@ inline Gated gated_cut(int dtype, int64_t rows, int64_t n_in, int64_t n_out) {
     const int64_t splits = few_tiles ? std::min(2 * kCus / few_tiles, std::min<int64_t>(steps / 32, 16)) : 1;
     return Gated{128, 128, std::max<int64_t>(splits, 1)};
 }
+inline int64_t steps_of(int dtype, int64_t n_in) { return ceil_div(n_in, kStep) * (dtype == NDVM_F32 ? 6 : 1); }
+// (ceil(n_out / 64) = ceil(2 n_out / 128): a gated tile holds both weights' columns)
+inline Gated gated_cut(int dtype, int64_t rows, int64_t n_in, int64_t n_out) { return cut_tiles(rows, steps_of(dtype, n_in), 2 * n_out); }
+// Of one weight.
+inline Gated linear_cut(int dtype, int64_t rows, int64_t n_in, int64_t n_out) { return cut_tiles(rows, steps_of(dtype, n_in), n_out); }
 
 // How the gradient's two plain products are cut: tiles of `tile` squared, each one's sum over so
 // many workgroups.  Both have the same number of steps in all.  Unless there are tiles for two
@@ -36,8 +40,8 @@ inline Gated gated_cut(int dtype, int64_t rows, int64_t n_in, int64_t n_out) {
 struct Pieces {
     int64_t tile, dx, dw;
 };
-inline Pieces pieces(int dtype, int64_t rows, int64_t n_in, int64_t n_out) {
-    const int64_t pairs = dtype == NDVM_F32 ? 6 : 1, width = 2 * ceil_div(n_out, 64) * 64;
+inline Pieces cut_gradient(int dtype, int64_t rows, int64_t n_in, int64_t width) {
+    const int64_t pairs = dtype == NDVM_F32 ? 6 : 1;
     const int64_t steps_dx = width / kStep * pairs, steps_dw = ceil_div(rows, 64) * 2 * pairs;
     const auto tiles_dx = [&](int64_t t) { return ceil_div(n_in, t) * ceil_div(rows, t); };
     const auto tiles_dw = [&](int64_t t) { return ceil_div(n_in, t) * ceil_div(width, t); };
@@ -50,6 +54,9 @@ inline Pieces pieces(int dtype, int64_t rows, int64_t n_in, int64_t n_out) {
     c.dw = cut(steps_dw);
     return c;
 }
+inline Pieces pieces(int dtype, int64_t rows, int64_t n_in, int64_t n_out) { return cut_gradient(dtype, rows, n_in, 2 * ceil_div(n_out, 64) * 64); }
+// Of one weight.
+inline Pieces linear_pieces(int dtype, int64_t rows, int64_t n_in, int64_t n_out) { return cut_gradient(dtype, rows, n_in, ceil_div(n_out, 64) * 64); }
 
 }  // namespace ops
 }  // namespace ndvm

@@ -143,5 +143,23 @@ size_t ffn_bytes(int dtype, int64_t rows, int64_t n_in, int64_t n_out, bool grad
 hipError_t launch_ffn(const FfnArgs &a, hipStream_t stream);
 hipError_t launch_ffn_grad(const FfnArgs &a, hipStream_t stream);
 
+// ---- projections
+struct LinearArgs {
+    int dtype, act;             // dtype: of y where x and w are bytes
+    const void *x, *w, *bias, *residual, *dy;
+    const float *x_scale, *w_scale;     // of the rows of x and w in e4m3, or null
+    int64_t rows, n_in, n_out, ld_x, ld_w, ld_r, ld_dy;
+    void *y;
+    int64_t ld_y;
+    void *dx, *dw, *db;
+    int64_t ld_dx, ld_dw;
+    void *ws;
+};
+size_t linear_bytes(int dtype, int act, int64_t rows, int64_t n_in, int64_t n_out, bool grad);
+size_t linear_8bit_bytes(int64_t rows, int64_t n_in, int64_t n_out);
+hipError_t launch_linear(const LinearArgs &a, hipStream_t stream);
+hipError_t launch_linear_8bit(const LinearArgs &a, hipStream_t stream);
+hipError_t launch_linear_grad(const LinearArgs &a, hipStream_t stream);
+
 }  // namespace ops
 }  // namespace ndvm

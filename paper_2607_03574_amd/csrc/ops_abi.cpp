@@ -522,4 +522,142 @@ ndvm_status ndvm_gated_ffn_grad(int dtype, int act, const void *dh, int64_t ld_d
     });
 }
 
+static ndvm_status check_linear(const char *who, int act, const LinearArgs &a) {
+    if (const ndvm_status st = check_ffn(who, a.dtype, a.rows, a.n_in, a.n_out)) return st;
+    if (act < NDVM_ACT_SILU || act > NDVM_ACT_NONE) return bad(who, "unknown activation");
+    if (a.ld_x < a.n_in || a.ld_w < a.n_in) return bad(who, "bad stride");
+    if (!fits(a.rows, a.ld_x) || !fits(a.n_out, a.ld_w)) return bad(who, "sizes overflow");
+    return NDVM_OK;
+}
+// what the forms of the forward pass share; need: bytes of workspace
+static ndvm_status check_linear_out(const char *who, const LinearArgs &a, size_t need, size_t have) {
+    if (a.ld_y < a.n_out || (a.residual && a.ld_r < a.n_out)) return bad(who, "bad stride");
+    if (!fits(a.rows, a.ld_y) || (a.residual && !fits(a.rows, a.ld_r))) return bad(who, "sizes overflow");
+    if (a.rows == 0) return NDVM_OK;
+    if (!a.x || !a.w || !a.y) return bad(who, "null buffer");
+    if (have < need) return fail(NDVM_E_NOMEM, who, "workspace too small");
+    if (need && !a.ws) return bad(who, "null workspace");
+    return NDVM_OK;
+}
+
+ndvm_status ndvm_linear_workspace_bytes(int dtype, int act, int64_t rows, int64_t n_in, int64_t n_out, int with_grad,
+                                        size_t *bytes) {
+    return guarded([&]() -> ndvm_status {
+        const char *who = "ndvm_linear_workspace_bytes";
+        if (!bytes) return bad(who, "null pointer");
+        if (const ndvm_status st = check_ffn(who, dtype, rows, n_in, n_out)) return st;
+        if (act < NDVM_ACT_SILU || act > NDVM_ACT_NONE) return bad(who, "unknown activation");
+        *bytes = linear_bytes(dtype, act, rows, n_in, n_out, with_grad != 0);
+        return NDVM_OK;
+    });
+}
+
+ndvm_status ndvm_linear(int dtype, int act, const void *x, int64_t rows, int64_t n_in, int64_t ld_x, const void *w,
+                        int64_t ld_w, int64_t n_out, const void *bias, const void *residual, int64_t ld_residual, void *y,
+                        int64_t ld_y, void *workspace, size_t workspace_bytes, void *stream) {
+    return guarded([&]() -> ndvm_status {
+        const char *who = "ndvm_linear";
+        LinearArgs a{};
+        a.dtype = dtype;
+        a.act = act;
+        a.x = x;
+        a.w = w;
+        a.bias = bias;
+        a.residual = residual;
+        a.rows = rows;
+        a.n_in = n_in;
+        a.n_out = n_out;
+        a.ld_x = ld_x;
+        a.ld_w = ld_w;
+        a.ld_r = ld_residual;
+        a.y = y;
+        a.ld_y = ld_y;
+        a.ws = workspace;
+        if (const ndvm_status st = check_linear(who, act, a)) return st;
+        if (const ndvm_status st = check_linear_out(who, a, linear_bytes(dtype, act, rows, n_in, n_out, false), workspace_bytes)) return st;
+        if (rows == 0) return NDVM_OK;
+        return launched(who, launch_linear(a, static_cast<hipStream_t>(stream)));
+    });
+}
+
+ndvm_status ndvm_linear_8bit_workspace_bytes(int64_t rows, int64_t n_in, int64_t n_out, size_t *bytes) {
+    return guarded([&]() -> ndvm_status {
+        const char *who = "ndvm_linear_8bit_workspace_bytes";
+        if (!bytes) return bad(who, "null pointer");
+        if (const ndvm_status st = check_ffn(who, NDVM_BF16, rows, n_in, n_out)) return st;
+        *bytes = linear_8bit_bytes(rows, n_in, n_out);
+        return NDVM_OK;
+    });
+}
+
+ndvm_status ndvm_linear_8bit(int dtype, int act, const void *x, const float *x_scale, int64_t rows, int64_t n_in, int64_t ld_x,
+                             const void *w, const float *w_scale, int64_t ld_w, int64_t n_out, const void *bias,
+                             const void *residual, int64_t ld_residual, void *y, int64_t ld_y, void *workspace,
+                             size_t workspace_bytes, void *stream) {
+    return guarded([&]() -> ndvm_status {
+        const char *who = "ndvm_linear_8bit";
+        LinearArgs a{};
+        a.dtype = dtype;
+        a.act = act;
+        a.x = x;
+        a.w = w;
+        a.x_scale = x_scale;
+        a.w_scale = w_scale;
+        a.bias = bias;
+        a.residual = residual;
+        a.rows = rows;
+        a.n_in = n_in;
+        a.n_out = n_out;
+        a.ld_x = ld_x;
+        a.ld_w = ld_w;
+        a.ld_r = ld_residual;
+        a.y = y;
+        a.ld_y = ld_y;
+        a.ws = workspace;
+        if (const ndvm_status st = check_linear(who, act, a)) return st;
+        if (dtype == NDVM_F32) return fail(NDVM_E_UNSUPPORTED, who, "a float result, whose bits the 8-bit products do not have");
+        if (rows && (!x_scale || !w_scale)) return bad(who, "null buffer");
+        if (const ndvm_status st = check_linear_out(who, a, linear_8bit_bytes(rows, n_in, n_out), workspace_bytes)) return st;
+        if (rows == 0) return NDVM_OK;
+        return launched(who, launch_linear_8bit(a, static_cast<hipStream_t>(stream)));
+    });
+}
+
+ndvm_status ndvm_linear_grad(int dtype, int act, const void *dy, int64_t ld_dy, const void *x, int64_t rows, int64_t n_in,
+                             int64_t ld_x, const void *w, int64_t ld_w, int64_t n_out, const void *bias, void *dx,
+                             int64_t ld_dx, void *dw, int64_t ld_dw, void *db, void *workspace, size_t workspace_bytes,
+                             void *stream) {
+    return guarded([&]() -> ndvm_status {
+        const char *who = "ndvm_linear_grad";
+        LinearArgs a{};
+        a.dtype = dtype;
+        a.act = act;
+        a.x = x;
+        a.w = w;
+        a.bias = bias;
+        a.dy = dy;
+        a.rows = rows;
+        a.n_in = n_in;
+        a.n_out = n_out;
+        a.ld_x = ld_x;
+        a.ld_w = ld_w;
+        a.ld_dy = ld_dy;
+        a.dx = rows ? dx : nullptr;
+        a.ld_dx = ld_dx;
+        a.dw = dw;
+        a.ld_dw = ld_dw;
+        a.db = db;
+        a.ws = workspace;
+        if (const ndvm_status st = check_linear(who, act, a)) return st;
+        if (ld_dy < n_out || (dx && ld_dx < n_in) || (dw && ld_dw < n_in)) return bad(who, "bad stride");
+        if (!fits(rows, ld_dy) || (dx && !fits(rows, ld_dx)) || (dw && !fits(n_out, ld_dw))) return bad(who, "sizes overflow");
+        if (!dx && !dw && !db) return NDVM_OK;
+        if (!w || (rows && (!x || !dy))) return bad(who, "null buffer");
+        const size_t need = linear_bytes(dtype, act, rows, n_in, n_out, true);
+        if (workspace_bytes < need) return fail(NDVM_E_NOMEM, who, "workspace too small");
+        if (!workspace) return bad(who, "null workspace");
+        return launched(who, launch_linear_grad(a, static_cast<hipStream_t>(stream)));
+    });
+}
+
 }  // extern "C"

@@ -14,9 +14,10 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import (Tape, _launch_stream, _row_stride, adam_step, gated_ffn_grad, grad, layer_norm_grad, linear_attention_grad,
-               rms_norm_grad)
+               linear_grad, rms_norm_grad)
 from . import gated_ffn as gated_ffn_op
 from . import layer_norm as layer_norm_op
+from . import linear as linear_op
 from . import linear_attention as linear_attention_op
 from . import rms_norm as rms_norm_op
 
@@ -176,3 +177,27 @@ class GatedFFN(torch.autograd.Function):
 def gated_ffn(x, w_gate, w_up, activation: str = "silu"):
     """act(x w_gate^T) * (x w_up^T) with autograd support (gated_ffn of the package)."""
     return GatedFFN.apply(x, w_gate, w_up, activation)
+
+
+class Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, activation, residual):
+        x, weight = _rows(x.detach()), _rows(weight.detach())
+        ctx.save_for_backward(x, weight, bias)
+        ctx.activation = activation
+        return linear_op(x, weight, bias, activation, None if residual is None else _rows(residual.detach()))
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        x, weight, bias = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dx = dw = db = None
+        if any(need[:3]):
+            dx, dw, db = linear_grad(dy.contiguous(), x, weight, bias, ctx.activation, *need[:3])
+        return dx, dw, db, None, dy if need[4] else None
+
+
+def linear(x, weight, bias=None, activation=None, residual=None):
+    """act(x weight^T + bias) + residual with autograd support (linear of the package)."""
+    return Linear.apply(x, weight, bias, activation, residual)

@@ -1,11 +1,17 @@
 """The operators around the attention of an encoder block, without a GPU: what the C entry points refuse before anything
 is enqueued, workspace sizes, and the references that the GPU tests compare with, pinned to differences."""
 import ctypes
+import importlib.util
+import os
+import subprocess
 
 import numpy as np
 import pytest
 
+import linear_ref
 import rms_ref
+from conftest import ROOT
+from linear_sizes import LINEAR_CUTS
 from test_encoder_host import FAKE, differences
 
 nd = pytest.importorskip("paper_2607_03574_amd")
@@ -58,3 +64,101 @@ def test_reference_rms_gradient():
     dx, dw = rms_ref.rms_grad(dy, h, w, rstd, dh)
     np.testing.assert_allclose(dx, differences(lambda t: (rms_ref.rms(t, w, 1e-3)[0] * dy).sum() + (t * dh).sum(), h), atol=1e-7)
     np.testing.assert_allclose(dw, differences(lambda t: (rms_ref.rms(h, t, 1e-3)[0] * dy).sum(), w), atol=1e-7)
+
+
+def test_linear_refusals():
+    # (few rows need no workspace)
+    ok = dict(dtype=1, act=4, x=FAKE, rows=400, n_in=8, ld_x=8, w=FAKE, ld_w=8, n_out=16, b=None, r=FAKE, ld_r=16, y=FAKE, ld_y=16,
+              ws=FAKE, bytes=1 << 30)
+
+    def call(**kw):
+        return nd._linear(*{**ok, **kw}.values(), None)
+
+    for kw in (dict(dtype=7), dict(act=5), dict(act=-1), dict(rows=-1), dict(n_in=0), dict(n_out=0), dict(ld_x=7), dict(ld_w=7),
+               dict(ld_r=15), dict(ld_y=15), dict(x=None), dict(w=None), dict(y=None), dict(ws=None)):
+        assert call(**kw) == nd.E_ARG, kw
+    for kw in (dict(rows=1 << 23), dict(n_in=1 << 22, ld_x=1 << 22, ld_w=1 << 22), dict(n_out=1 << 22, ld_y=1 << 22, ld_r=1 << 22)):
+        assert call(**kw) == nd.E_UNSUPPORTED, kw
+    assert call(bytes=10) == nd.E_NOMEM
+    assert call(rows=0, x=None, y=None) == nd.OK
+    grad = dict(dtype=1, act=0, dy=FAKE, ld_dy=16, x=FAKE, rows=4, n_in=8, ld_x=8, w=FAKE, ld_w=8, n_out=16, b=None, dx=FAKE, ld_dx=8,
+                dw=FAKE, ld_dw=8, db=FAKE, ws=FAKE, bytes=1 << 30)
+
+    def call_grad(**kw):
+        return nd._linear_grad(*{**grad, **kw}.values(), None)
+
+    for kw in (dict(ld_dw=7), dict(ld_dx=7), dict(ld_dy=15), dict(dy=None), dict(x=None), dict(w=None), dict(ws=None), dict(act=9)):
+        assert call_grad(**kw) == nd.E_ARG, kw
+    assert call_grad(bytes=100) == nd.E_NOMEM
+    assert call_grad(dx=None, dw=None, db=None) == nd.OK
+    eight = dict(dtype=1, act=4, x=FAKE, sx=FAKE, rows=400, n_in=8, ld_x=8, w=FAKE, sw=FAKE, ld_w=8, n_out=16, b=None, r=None, ld_r=0,
+                 y=FAKE, ld_y=16, ws=FAKE, bytes=1 << 30)
+
+    def call_8bit(**kw):
+        return nd._linear8(*{**eight, **kw}.values(), None)
+
+    for kw in (dict(sx=None), dict(sw=None), dict(ld_x=7), dict(r=FAKE, ld_r=15), dict(y=None), dict(ws=None), dict(dtype=3)):
+        assert call_8bit(**kw) == nd.E_ARG, kw
+    assert call_8bit(bytes=10) == nd.E_NOMEM and call_8bit(dtype=0) == nd.E_UNSUPPORTED
+    assert call_8bit(rows=0, x=None, sx=None, sw=None, y=None) == nd.OK
+    n = nd._sz()
+    assert nd._linear_ws(0, 0, 1 << 22, 1 << 21, 1 << 21, 1, ctypes.byref(n)) == nd.OK and n.value > 1 << 44
+    assert nd._linear_ws(0, 0, 64, 1 << 21, 1 << 21, 0, ctypes.byref(n)) == nd.OK and n.value == 0
+    assert nd._linear8_ws(1 << 22, 1 << 21, 1 << 21, ctypes.byref(n)) == nd.OK and n.value > 1 << 43
+    assert nd._linear8_ws(1, 0, 1, ctypes.byref(n)) == nd.E_ARG and nd._linear_ws(0, 5, 1, 1, 1, 0, ctypes.byref(n)) == nd.E_ARG
+
+
+def test_reference_linear_gradient():
+    torch = pytest.importorskip("torch")
+    rng = np.random.default_rng(2)
+    x, w, b, dy = (rng.normal(size=s) for s in ((3, 4), (5, 4), (5,), (3, 5)))
+    t = torch.tensor
+    for name in linear_ref.ACTS:
+        got = linear_ref.linear_grad(t(dy), t(x), t(w), t(b), name)
+        args = [x, w, b]
+        for i in range(3):
+            want = differences(lambda v: float((linear_ref.linear(*(t(a) for a in args[:i] + [v] + args[i + 1:]), name) * t(dy)).sum()), args[i])
+            np.testing.assert_allclose(got[i].numpy(), want, atol=1e-6)
+
+
+CUTS = '''
+#include "%s"
+extern "C" void cuts(int dtype, int64_t rows, int64_t n_in, int64_t n_out, int64_t *to) {
+    const auto g = ndvm::ops::linear_cut(dtype, rows, n_in, n_out);
+    const auto p = ndvm::ops::linear_pieces(dtype, rows, n_in, n_out);
+    const int64_t all[] = {g.ba, g.bb, g.splits, p.tile, p.dx, p.dw};
+    for (int i = 0; i < 6; ++i) to[i] = all[i];
+}
+'''
+
+
+@pytest.fixture(scope="module")
+def cuts(tmp_path_factory):
+    spec = importlib.util.spec_from_file_location("_b", os.path.join(ROOT, "paper_2607_03574_amd", "build.py"))
+    b = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(b)
+    if not os.path.exists(b.HIPCC):
+        pytest.skip("no compiler")
+    d = tmp_path_factory.mktemp("cuts")
+    (d / "cuts.cpp").write_text(CUTS % os.path.join(b.CSRC, "ffn_cut.h"))
+    subprocess.run([b.HIPCC, "-O1", "-std=c++17", "-shared", "-fPIC", str(d / "cuts.cpp"), "-o", str(d / "cuts.so")],
+                   check=True, capture_output=True)
+    f = ctypes.CDLL(str(d / "cuts.so")).cuts
+    f.argtypes, f.restype = [ctypes.c_int] + [ctypes.c_int64] * 3 + [ctypes.c_void_p], None
+
+    def call(dtype, *size):
+        to = (ctypes.c_int64 * 6)()
+        f(dtype, *size, to)
+        return tuple(to)
+
+    return call
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_linear_sizes_cover_every_cut(cuts, dtype):
+    taken = [cuts(dtype, *size) for size in LINEAR_CUTS]
+    assert {(a, b, s > 1) for a, b, s, *_ in taken} == {(256, 256, False), (256, 128, False), (128, 128, False), (128, 128, True)}
+    assert {(t, x > 1, w > 1) for *_, t, x, w in taken} == {(t, x, w) for t in (128, 256) for x in (False, True) for w in (False, True)}
+    # the 8-bit form takes the tiles of half as long a sum of 16 bits
+    eight = [cuts(1, rows, (n_in + 1) // 2, n_out) for rows, n_in, n_out in LINEAR_CUTS]
+    assert {(a, b, s > 1) for a, b, s, *_ in eight} == {(256, 256, False), (256, 128, False), (128, 128, False), (128, 128, True)}
