@@ -561,6 +561,61 @@ ndvm_status ndvm_linear_attention_step(const ndvm_attention_shape *shape, const 
                                        const int64_t *slots, const ndvm_heads *o, void *stream);
 
 /*
+ * Attention by the gated delta rule.  Over the tokens t of a sequence, for head h of
+ * v, which reads head h / (heads / qk_heads) of q and k:
+ *   u_t = beta_t (v_t - exp(g_t) k_t S_{t-1})
+ *   S_t = exp(g_t) S_{t-1} + k_t^T u_t               (S: [dk, dv], float)
+ *   o_t = scale * q_t S_t
+ * S before the first token is `initial_state` (float [n_seq, heads, dk, dv],
+ * contiguous) or 0 where that is NULL; S after the last one goes to `final_state`
+ * (the same layout) unless that is NULL.  g (the log of a decay, at most 0; what is
+ * below -128, an infinity too, decays to 0) and beta have a value for each token and
+ * head, of the tensors' type.  States stay bounded where |k_t|^2 beta_t is at most 2:
+ * keys are usually of length one and beta between 0 and 1.
+ * Evaluated in chunks of 32 tokens, not token by token, with every sum and state in
+ * float.  From the first token of a sequence on at which k, g or beta of a head is not
+ * finite, that head's outputs and state are NaN; a value of v that is not finite makes
+ * its column of v so, one of q its own output.  Earlier tokens, other columns, heads and
+ * sequences keep their results.
+ *
+ * Sequences as for ndvm_linear_attention: of n_tokens / n_seq tokens each, or given by
+ * `offsets`, with what is said there of offsets.  g and beta are given as the other
+ * tensors are, with one value a head.
+ * Limits: dk, dv <= 256, heads <= 65,535, n_tokens <= 2^30, and at most 2^26 pairs of
+ * 32 tokens of a sequence and a head.
+ */
+typedef struct {
+    int dtype;
+    int64_t n_seq, n_tokens;      /* sequences, and tokens of all of them */
+    int64_t heads, qk_heads;      /* heads of v, g, beta and o: a multiple of q's and k's */
+    int64_t dk, dv;
+    double scale;
+} ndvm_delta_shape;
+
+/* Workspace bytes of ndvm_delta_attention (with_grad = 0) or its gradient
+ * (with_grad = 1); packed: whether the call has offsets.  Host only. */
+ndvm_status ndvm_delta_attention_workspace_bytes(const ndvm_delta_shape *shape, int packed, int with_grad,
+                                                 size_t *bytes);
+
+ndvm_status ndvm_delta_attention(const ndvm_delta_shape *shape, const ndvm_heads *q, const ndvm_heads *k,
+                                 const ndvm_heads *v, const ndvm_heads *g, const ndvm_heads *beta,
+                                 const int64_t *offsets, const float *initial_state, const ndvm_heads *o,
+                                 float *final_state, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The recurrence for one new token of n_seq streams (shape->n_tokens is not read):
+ * stream s updates state slots[s] of `state` (float [n_slots, heads, dk, dv],
+ * contiguous) in place; o = scale * q S with the new S.  slots: device int64 [n_seq],
+ * no slot twice, or NULL (stream s has slot s); a stream whose slot is not in
+ * 0..n_slots-1 has none: its output is 0.  Tensors have a row for each stream
+ * (seq_stride, head_stride; tok_stride is not read).
+ */
+ndvm_status ndvm_delta_attention_step(const ndvm_delta_shape *shape, const ndvm_heads *q, const ndvm_heads *k,
+                                      const ndvm_heads *v, const ndvm_heads *g, const ndvm_heads *beta,
+                                      float *state, int64_t n_slots, const int64_t *slots, const ndvm_heads *o,
+                                      void *stream);
+
+/*
  * Gated feed-forward projections of `rows` rows:
  *   h = act(x w_gate^T) * (x w_up^T)
  * x [rows, n_in], w_gate and w_up [n_out, n_in], h [rows, n_out], rows at

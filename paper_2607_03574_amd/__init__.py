@@ -33,7 +33,8 @@ EXPORTS = ["ndvm_tape_build", "ndvm_tape_upload", "ndvm_tape_upload_many", "ndvm
            "ndvm_layer_norm", "ndvm_layer_norm_workspace_bytes", "ndvm_layer_norm_grad",
            "ndvm_rms_norm", "ndvm_rms_norm_workspace_bytes", "ndvm_rms_norm_grad", "ndvm_rms_norm_8bit", "ndvm_quantize_rows",
            "ndvm_linear_attention_workspace_bytes", "ndvm_linear_attention", "ndvm_linear_attention_grad",
-           "ndvm_linear_attention_step", "ndvm_gated_ffn_workspace_bytes", "ndvm_gated_ffn", "ndvm_gated_ffn_grad",
+           "ndvm_linear_attention_step", "ndvm_delta_attention_workspace_bytes", "ndvm_delta_attention",
+           "ndvm_delta_attention_step", "ndvm_gated_ffn_workspace_bytes", "ndvm_gated_ffn", "ndvm_gated_ffn_grad",
            "ndvm_linear_workspace_bytes", "ndvm_linear", "ndvm_linear_grad", "ndvm_linear_8bit_workspace_bytes", "ndvm_linear_8bit"]
 ACTIVATIONS = {"silu": 0, "gelu": 1, "sigmoid": 2, "relu": 3}     # NDVM_ACT_*
 ACT_NONE = 4           # NDVM_ACT_NONE: no activation (linear)
@@ -125,6 +126,17 @@ _attn_grad = _sig("ndvm_linear_attention_grad", _int, [_shape_p, _heads_p, _head
                                                        _vp, _heads_p, _heads_p, _heads_p, _vp, _vp, _sz, _vp])
 _attn_step = _sig("ndvm_linear_attention_step", _int, [_shape_p, _heads_p, _heads_p, _heads_p, _vp, _vp, _i64, _vp,
                                                        _heads_p, _vp])
+
+
+class _DeltaShape(ctypes.Structure):
+    _fields_ = [("dtype", _int), ("n_seq", _i64), ("n_tokens", _i64), ("heads", _i64), ("qk_heads", _i64),
+                ("dk", _i64), ("dv", _i64), ("scale", _f64)]
+
+
+_delta_p = ctypes.POINTER(_DeltaShape)
+_delta_ws = _sig("ndvm_delta_attention_workspace_bytes", _int, [_delta_p, _int, _int, ctypes.POINTER(_sz)])
+_delta = _sig("ndvm_delta_attention", _int, [_delta_p] + [_heads_p] * 5 + [_vp, _vp, _heads_p, _vp, _vp, _sz, _vp])
+_delta_step = _sig("ndvm_delta_attention_step", _int, [_delta_p] + [_heads_p] * 5 + [_vp, _i64, _vp, _heads_p, _vp])
 _ffn_ws = _sig("ndvm_gated_ffn_workspace_bytes", _int, [_int, _i64, _i64, _i64, _int, ctypes.POINTER(_sz)])
 _ffn = _sig("ndvm_gated_ffn", _int, [_int, _int, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _vp, _i64, _vp, _sz,
                                      _vp])
@@ -900,6 +912,111 @@ def linear_attention_step(q, k, v, log_decay, state, slots=None, scale=None, out
         _to_write(t, state, "state")
         _check(_attn_step(shape, hq, hk, hv, decay, st, state.shape[0], sl, one(out, "out", H, dv), s),
                "ndvm_linear_attention_step")
+    return out
+
+
+def _gates(x, name, lead, heads):
+    """An ndvm_heads of x [seqs, tokens, heads] (lead of two) or [tokens, heads]."""
+    if x.shape != (*lead, heads):
+        raise ValueError(f"{name} must have shape {(*lead, heads)}, not {tuple(x.shape)}")
+    strides = x.stride()
+    if len(lead) == 2:
+        return _Heads(x.data_ptr(), strides[0], strides[1], strides[2])
+    return _Heads(x.data_ptr(), 0, strides[0], strides[1])
+
+
+def _delta_args(t, q, k, v, g, beta, offsets, scale):
+    """Checks of the arguments that the delta rule's calls share: shape struct, leading sizes, offset pointer, and q, k, v,
+    g and beta."""
+    dt = _op_type(t, q, "q")
+    _alike(q, ("k", k), ("v", v), ("g", g), ("beta", beta))
+    packed = offsets is not None
+    if packed:
+        off = _of(offsets, "offsets", t.i64, (offsets.numel(),), q.device)
+        if offsets.numel() < 1:
+            raise ValueError("offsets must hold one more than there are sequences")
+    if q.dim() != (3 if packed else 4) or k.dim() != q.dim() or v.dim() != q.dim():
+        raise ValueError("q, k and v must be [sequences, tokens, heads, d], or [tokens, heads, d] with offsets")
+    *lead, Hk, dk = q.shape
+    lead = tuple(lead)
+    H, dv = v.shape[-2:]
+    if packed:
+        n_seq, n = offsets.numel() - 1, lead[0]
+    else:
+        off, n_seq, n = None, lead[0], lead[0] * lead[1]
+    shape = _DeltaShape(dt, n_seq, n, H, Hk, dk, dv, dk ** -0.5 if scale is None else scale)
+    return (shape, lead, off, _heads(q, "q", lead, Hk, dk), _heads(k, "k", lead, Hk, dk), _heads(v, "v", lead, H, dv),
+            _gates(g, "g", lead, H), _gates(beta, "beta", lead, H))
+
+
+def _delta_workspace(t, x, shape, packed, grad):
+    need = _sz()
+    _check(_delta_ws(shape, packed, grad, ctypes.byref(need)), "ndvm_delta_attention_workspace_bytes")
+    ws = x.new_empty(need.value, dtype=t.u8)
+    return ws, ws.data_ptr(), need.value
+
+
+def delta_attention(q, k, v, g, beta, offsets=None, scale=None, initial_state=None, out=None, final_state: bool = False,
+                    stream=None):
+    """Attention by the gated delta rule (ndvm_delta_attention): (o, final state or None)
+    for q and k [sequences, tokens, qk_heads, dk], v [.., heads, dv], and g (log decays) and
+    beta [.., heads]; with `offsets` (int64 [sequences + 1], on the device, from 0 to the
+    number of tokens) the sequences lie one after the other in [tokens, heads, ..]; tokens
+    outside them get no output.  heads: a multiple of qk_heads; scale: dk**-0.5 unless
+    given; states are float32 [sequences, heads, dk, dv].  (With autograd:
+    torch_api.delta_attention.)"""
+    t = _t()
+    shape, lead, off, *heads = _delta_args(t, q, k, v, g, beta, offsets, scale)
+    dims, dev = (shape.n_seq, shape.heads, shape.dk, shape.dv), q.device
+    s0 = _of(initial_state, "initial_state", t.f32, dims, dev)
+    with _On(t, stream, dev) as s:
+        if out is None:
+            out = q.new_empty((*lead, shape.heads, shape.dv))
+        else:
+            _alike(q, ("out", out))
+            _to_write(t, out, "out")
+        last = q.new_empty(dims, dtype=t.f32) if final_state else None
+        ws, ws_ptr, need = _delta_workspace(t, q, shape, off is not None, 0)
+        _check(_delta(shape, *heads, off, s0, _heads(out, "out", lead, shape.heads, shape.dv),
+                      last.data_ptr() if final_state else None, ws_ptr, need, s), "ndvm_delta_attention")
+    return out, last
+
+
+def delta_attention_step(q, k, v, g, beta, state, slots=None, scale=None, out=None, stream=None):
+    """One new token of every stream (ndvm_delta_attention_step): q and k [streams,
+    qk_heads, dk], v [streams, heads, dv], g and beta [streams, heads]; stream i's state is
+    state[slots[i]] (float32 [slots, heads, dk, dv], updated in place; slot i without
+    `slots`), or none, with output 0, where slots[i] is out of range.  Returns o [streams,
+    heads, dv].  There is no gradient through a step."""
+    t = _t()
+    dt = _op_type(t, q, "q")
+    _alike(q, ("k", k), ("v", v), ("g", g), ("beta", beta))
+    if q.dim() != 3 or v.dim() != 3 or k.dim() != 3:
+        raise ValueError("q, k and v must be [streams, heads, d]")
+    n, Hk, dk = q.shape
+    H, dv = v.shape[1:]
+    dev = q.device
+    if state.dim() != 4:
+        raise ValueError("state must be [slots, heads, dk, dv]")
+    st = _of(state, "state", t.f32, (state.shape[0], H, dk, dv), dev)
+    sl = _of(slots, "slots", t.i64, (n,), dev)
+
+    def one(x, name, *shape):
+        strides = x.stride()
+        if x.shape != (n, *shape) or (len(shape) == 2 and shape[1] > 1 and strides[2] != 1):
+            raise ValueError(f"{name} must have shape {(n, *shape)} and unit inner stride")
+        return _Heads(x.data_ptr(), strides[0], 0, strides[1])
+
+    heads = (one(q, "q", Hk, dk), one(k, "k", Hk, dk), one(v, "v", H, dv), one(g, "g", H), one(beta, "beta", H))
+    shape = _DeltaShape(dt, n, 0, H, Hk, dk, dv, dk ** -0.5 if scale is None else scale)
+    with _On(t, stream, dev) as s:
+        if out is None:
+            out = q.new_empty((n, H, dv))
+        else:
+            _alike(q, ("out", out))
+            _to_write(t, out, "out")
+        _to_write(t, state, "state")
+        _check(_delta_step(shape, *heads, st, state.shape[0], sl, one(out, "out", H, dv), s), "ndvm_delta_attention_step")
     return out
 
 

@@ -1,0 +1,336 @@
+// What the kernels of the gated delta rule share: pieces of sequences, values as bf16 parts, and the
+// record that is kept for a chunk of 32 tokens and a head.
+//   S_t = a_t S_{t-1} + k_t^T u_t,  u_t = b_t (v_t - a_t k_t S_{t-1}),  o_t = s q_t S_t,  a_t = exp(g_t)
+// Over a chunk, with G the running sum of g in it, L_ij = exp(G_i - G_j) and S what entered it:
+//   (I + A) U = R = diag(b) (V - diag(exp G) K S),  A_ij = b_i L_ij k_i.k_j for j < i
+//   O = s (diag(exp G) Q S + P U),  P_ij = L_ij q_i.k_j for j <= i
+//   S' = exp(G_last) S + sum_j exp(G_last - G_j) k_j^T u_j
+// All sums and states are in float; products are made of bf16 parts on the bf16 matrix instructions (16 times the
+// rate of the float ones): 16-bit inputs are one part (bfloat16) or two (half), floats three; what the state is made
+// of is three parts, products whose places add up to 2 at most: 2^-21 of a term is left out at most, 2^-24 on
+// average.  What only reaches a 16-bit result is two parts, so that the result is off by its own rounding alone.
+#pragma once
+#include <algorithm>
+#include <type_traits>
+
+#include "ops.h"
+#include "ops_types.h"
+
+namespace ndvm {
+namespace ops {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+template <class T> constexpr int kInputParts = sizeof(T) == 4 ? 3 : std::is_same<T, f16>::value ? 2 : 1;
+// of what reaches a result only
+template <class T> constexpr int kResultParts = sizeof(T) == 4 ? 3 : 2;
+constexpr int kStateParts = 3;
+
+#ifdef __HIP_DEVICE_COMPILE__
+__device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ inline f32x4 mfma(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+// Lane 4 r + x of 16 names four values of row r; lane i gets column i of the four rows.
+__device__ inline bf16x4 read_transposed(const char *p) {
+    return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(p)));
+}
+#endif
+// The upper 8 bits of v's significand.
+__device__ inline float upper(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
+// v as N parts, the last one rounded, into place `at` of vectors.
+template <int N, class V> __device__ inline void split(float v, V (&to)[N], int at) {
+#pragma unroll
+    for (int i = 0; i < N - 1; ++i) {
+        const float up = upper(v);
+        to[i][at] = bf16(up);
+        v -= up;
+    }
+    to[N - 1][at] = bf16(v);
+}
+#ifdef __HIP_DEVICE_COMPILE__
+// c + x y of parts whose places add up to ORDER at most, small ones first.
+template <int ORDER, int NX, int NY> __device__ inline f32x4 multiply(const bf16x8 (&x)[NX], const bf16x8 (&y)[NY], f32x4 c) {
+#pragma unroll
+    for (int o = ORDER; o >= 0; --o)
+#pragma unroll
+        for (int i = 0; i < NX; ++i)
+            if (o - i >= 0 && o - i < NY) c = mfma(x[i], y[o - i], c);
+    return c;
+}
+#endif
+
+// Eight values of a row, as they are.
+template <class T> struct Eight {
+    vec<T> v[8 / kVec<T>];
+};
+template <class T> __device__ inline Eight<T> load_eight(const T *p, int64_t count) {
+    Eight<T> e;
+#pragma unroll
+    for (int i = 0; i < 8 / kVec<T>; ++i) {
+        e.v[i] = T(0.0f);
+        if (count > i * kVec<T>) e.v[i] = load_vec(p + i * kVec<T>, count - i * kVec<T>);
+    }
+    return e;
+}
+template <class T> __device__ inline float value(const Eight<T> &e, int i) { return float(e.v[i / kVec<T>][i % kVec<T>]); }
+template <class T, int N> __device__ inline void parts_of(const Eight<T> &e, bf16x8 (&to)[N]) {
+    if constexpr (std::is_same<T, bf16>::value && N == 1) {
+        to[0] = __builtin_bit_cast(bf16x8, e.v[0]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) split(value(e, i), to, i);
+    }
+}
+__device__ inline bool finite(float v) { return fabsf(v) <= 3.402823466e38f; }
+
+// Sequences cut into pieces of `len` tokens (packed ones: a power of two).  Those of equal length have equally many;
+// packed ones have ids from offsets[s] / len + s on, which leaves room for all of theirs: the spare ids have no tokens.
+struct Piece {
+    int64_t seq, first, tokens;     // sequence, its first token, its length
+    int64_t begin, len;             // the piece's place in the sequence
+    int64_t index, count;           // of the sequence's pieces; count 0: a spare id
+    int64_t id0;                    // the id of the sequence's first piece
+};
+__device__ inline int64_t token_at(const DeltaArgs &a, int64_t s) { return min(max(a.offsets[s], int64_t(0)), a.n_tokens); }
+__device__ inline int shift_of(int64_t len) { return 63 - __builtin_clzll(len); }
+// The id of a sequence's first piece.
+__device__ inline int64_t first_piece(const DeltaArgs &a, int64_t seq, int64_t len) {
+    if (a.offsets) return (token_at(a, seq) >> shift_of(len)) + seq;
+    return seq * ((a.n_tokens / a.n_seq + len - 1) / len);
+}
+// 64 lanes of a wave look for it together.  whole: pieces are sequences.
+__device__ inline Piece find_piece(const DeltaArgs &a, uint32_t id, int64_t len, bool whole = false) {
+    Piece g;
+    if (!a.offsets) {
+        g.tokens = uint32_t(a.n_tokens) / uint32_t(a.n_seq);
+        const uint32_t per = whole ? 1 : uint32_t((g.tokens + len - 1) / len);
+        g.seq = id / per;
+        g.index = id % per;
+        g.first = g.seq * g.tokens;
+        g.count = per;
+    } else {
+        const int shift = shift_of(len);
+        uint32_t lo = id, base = id;
+        if (!whole) {
+            // the last sequence whose ids begin at or before id
+            uint32_t hi = uint32_t(a.n_seq);
+            lo = base = 0;
+            while (hi - lo > 1) {
+                const uint32_t step = (hi - lo + 63) / 64, s = lo + (threadIdx.x % 64) * step;
+                const uint32_t mine = s < hi ? uint32_t(token_at(a, s) >> shift) + s : 0xffffffffu;
+                const int n = max(__popcll(__ballot(mine <= id)), 1);
+                base = __shfl(mine, n - 1);
+                lo += (n - 1) * step;
+                hi = min(lo + step, hi);
+            }
+            if (a.n_seq == 1) base = uint32_t(token_at(a, 0) >> shift);
+            lo = __builtin_amdgcn_readfirstlane(lo);
+            base = __builtin_amdgcn_readfirstlane(base);
+        }
+        g.seq = lo;
+        g.index = int64_t(id) - base;
+        g.first = token_at(a, lo);
+        g.tokens = max(token_at(a, int64_t(lo) + 1) - g.first, int64_t(0));
+        g.count = whole ? 1 : (g.tokens + len - 1) >> shift;
+    }
+    g.id0 = int64_t(id) - g.index;
+    g.begin = whole ? 0 : g.index * len;
+    g.len = whole ? g.tokens : min(len, g.tokens - g.begin);
+    if (g.index < 0 || g.index >= g.count) g.count = 0;
+    return g;
+}
+inline int64_t piece_ids(const DeltaArgs &a, int64_t len) {
+    if (a.offsets) return a.n_tokens / len + a.n_seq;
+    return a.n_seq ? a.n_seq * ceil_div(a.n_tokens / a.n_seq, len) : 0;
+}
+
+// Token t of a sequence, head h.
+template <class T> __device__ inline const T *at_token(const Heads &x, const DeltaArgs &a, const Piece &g, int64_t t, int64_t h) {
+    const int64_t row = a.offsets ? (g.first + t) * x.tok : g.seq * x.seq + t * x.tok;
+    return static_cast<const T *>(x.p) + row + h / x.group * x.head;
+}
+
+// The record of a chunk and head: 32 values each of b, exp G and exp(G_last - G), exp(G_last), and the first token whose k,
+// g or beta is not finite (32: none); then 32 x 32 matrices as operands of the matrix instructions: row 16 t + l % 16,
+// columns 8 (l / 16) on, of tile t in lane l, a part of a tile after the other.
+constexpr int kRecordHead = 512, kTile = 1024;
+struct RecordHead {
+    float beta[32], rise[32], fall[32], whole;
+    int bad;
+};
+static_assert(sizeof(RecordHead) <= kRecordHead, "");
+constexpr int kRecordMatrix = 2 * kStateParts * kTile;
+template <class T> constexpr int kRecordPairs = 2 * kResultParts<T> * kTile;
+// forward: (I + A)^-1 and P; gradient: the inverse, its transpose and that of P
+template <class T> constexpr int kRecord = kRecordHead + kRecordMatrix + kRecordPairs<T>;
+template <class T> constexpr int kRecordGrad = kRecord<T> + kRecordMatrix;
+
+// A log decay as it is used: what lies below -128 is a factor of 0 in float in any case, and its sums stay exact.
+template <class T> __device__ inline double log_decay(T g) {
+    const float v = float(g);
+    return v < -128.0f ? -128.0 : double(v);
+}
+
+// One wave: the record of chunk `id` and head h.  lds: 2 x 32 x 36 floats and 32 doubles of its own.
+constexpr int kPrepareLds = 2 * 32 * 36 * 4 + 256;
+template <class T, bool GRAD> __global__ void __launch_bounds__(256) delta_prepare(DeltaArgs a, int64_t pairs) {
+#ifdef __HIP_DEVICE_COMPILE__
+    constexpr int PARTS = kInputParts<T>, HELD = kResultParts<T>, LD = 36;
+    __shared__ __align__(16) char shared[4][kPrepareLds];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l = threadIdx.x % 64, lm = l % 16, lg = l / 16;
+    const int64_t pair = int64_t(blockIdx.x) * 4 + wave;
+    if (pair >= pairs) return;
+    float(*const m)[LD] = reinterpret_cast<float(*)[LD]>(shared[wave]), (*const p)[LD] = m + 32;
+    double *const sum = reinterpret_cast<double *>(shared[wave] + 2 * 32 * LD * 4);
+    const int64_t h = pair % a.heads;
+    const Piece g = find_piece(a, uint32_t(pair / a.heads), kDeltaChunk);
+    if (g.count == 0) return;
+    char *const record = a.chunks + pair * (GRAD ? kRecordGrad<T> : kRecord<T>);
+    const int len = int(g.len);
+
+    // k k^T and q k^T, the tiles (0, 0), (1, 0) and (1, 1)
+    f32x4 kk[3], qk[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) kk[i] = qk[i] = 0;
+    bool odd[2] = {false, false};
+    for (int64_t c = 8 * lg; c < (a.dk + 31) / 32 * 32; c += 32) {
+        bf16x8 k[2][PARTS], q[2][PARTS];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int row = 16 * t + lm;
+            const int64_t have = row < len ? a.dk - c : 0;
+            const Eight<T> e = load_eight(at_token<T>(a.k, a, g, g.begin + row, h) + c, have);
+            const Eight<T> f = load_eight(at_token<T>(a.q, a, g, g.begin + row, h) + c, have);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) odd[t] |= !finite(value(e, i));
+            parts_of(e, k[t]);
+            parts_of(f, q[t]);
+        }
+        kk[0] = multiply<2>(k[0], k[0], kk[0]);
+        kk[1] = multiply<2>(k[1], k[0], kk[1]);
+        kk[2] = multiply<2>(k[1], k[1], kk[2]);
+        qk[0] = multiply<2>(q[0], k[0], qk[0]);
+        qk[1] = multiply<2>(q[1], k[0], qk[1]);
+        qk[2] = multiply<2>(q[1], k[1], qk[2]);
+    }
+    // gates: lane i % 32 has token i
+    const int token = l % 32;
+    float beta = 0.0f;
+    double log_a = 0.0;
+    if (token < len) {
+        beta = float(*at_token<T>(a.beta, a, g, g.begin + token, h));
+        log_a = log_decay(*at_token<T>(a.g, a, g, g.begin + token, h));
+    }
+    const auto rows = [](uint64_t b) { return uint32_t((b | b >> 16 | b >> 32 | b >> 48) & 0xffff); };
+    const uint32_t unfit = rows(__ballot(odd[0])) | rows(__ballot(odd[1])) << 16 | uint32_t(__ballot(!finite(beta) || !(log_a <= 3.5e38)));
+    const int bad = unfit ? __builtin_ctz(unfit) : 32, fit = min(bad, len);
+    if (token >= fit) beta = 0.0f, log_a = 0.0;
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+        const double before = __shfl_up(log_a, s, 32);
+        if (token >= s) log_a += before;
+    }
+    const double last = __shfl(log_a, 31, 32);
+    RecordHead *const head = reinterpret_cast<RecordHead *>(record);
+    if (l < 32) {
+        sum[l] = log_a;
+        head->beta[l] = beta;
+        head->rise[l] = expf(float(log_a));
+        head->fall[l] = expf(float(last - log_a));
+        if (l == 0) {
+            head->whole = expf(float(last));
+            head->bad = bad;
+        }
+    }
+    // A and P; beta by row
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {       // tiles (0, 0), (0, 1), (1, 0), (1, 1)
+        const int ti = t / 2, tj = t % 2, j = 16 * tj + lm;
+        const double gj = sum[j];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = 16 * ti + 4 * lg + r;
+            const float b = __shfl(beta, i);
+            float ma = 0.0f, pa = 0.0f;
+            if (t != 1) {
+                const int at = t == 0 ? 0 : t - 1;
+                const float decay = expf(float(sum[i] - gj));
+                if (j < i && i < fit) ma = b * decay * kk[at][r];
+                if (j <= i && i < fit) pa = decay * qk[at][r];
+            }
+            m[i][j] = ma;
+            p[i][j] = pa;
+        }
+    }
+    // The inverse of I + A: of both diagonal blocks by substitution, a column a lane; then the block below them.
+    // Rows of the blocks are read before any is written over.
+    {
+        const int b = token / 16 * 16, c = token % 16;
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float s = i == c ? 1.0f : 0.0f;
+#pragma unroll
+            for (int j = 0; j < i; ++j) s -= m[b + i][b + j] * x[j];
+            x[i] = s;
+        }
+        float below[4];         // A's block as an operand
+#pragma unroll
+        for (int r = 0; r < 4; ++r) below[r] = m[16 + lm][4 * r + lg];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) m[b + i][b + c] = x[i];
+        f32x4 y = 0, z = 0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y = mfma(below[r], m[4 * r + lg][lm], y);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) z = mfma(m[16 + lm][16 + 4 * lg + r], y[r], z);      // rows 4 (l / 16) + r of y are in lane l
+#pragma unroll
+        for (int r = 0; r < 4; ++r) m[16 + 4 * lg + r][lm] = -z[r];
+    }
+    char *to = record + kRecordHead + l * 16;
+    const auto store = [&](const float(*x)[LD], auto parts, auto transposed) __attribute__((always_inline)) {
+        constexpr int N = decltype(parts)::value;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            bf16x8 v[N];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) split(decltype(transposed)::value ? x[8 * lg + i][16 * t + lm] : x[16 * t + lm][8 * lg + i], v, i);
+#pragma unroll
+            for (int q = 0; q < N; ++q) *reinterpret_cast<bf16x8 *>(to + (t * N + q) * kTile) = v[q];
+        }
+        to += 2 * N * kTile;
+    };
+    const std::integral_constant<int, kStateParts> of_state;
+    const std::integral_constant<int, HELD> of_result;
+    store(m, of_state, std::false_type());
+    if (GRAD) store(m, of_state, std::true_type());
+    store(p, of_result, std::integral_constant<bool, GRAD>());
+#endif
+}
+
+// ---- rows of q and k in LDS, in granules of 16 bytes: granule i of row r of G lies at i ^ turned<G>(r), so that the rows
+// one instruction reads, along them or (transposed) four of them across, are in different banks
+template <int G> __device__ inline int turned(int r) {
+    return G >= 16 ? r % 4 * 4 + r / 4 % 4 : G == 8 ? r / 2 % 2 * 4 + r / 4 % 2 : r / 4 % 2;
+}
+
+// How a workgroup of four waves divides a chunk: WK waves share the widths of k (KPW times 32 each), the others have
+// other columns of v; a wave has 32 columns.
+template <int DK> struct Split {
+    static constexpr int WK = DK >= 128 ? 4 : DK / 32, WN = 4 / WK, KPW = DK / 32 / WK, NC = 32 * WN, G = DK / 8, OWN = 4 / WK;
+};
+
+template <class T, class F> void with_width(int64_t dk, F f) {
+    using std::integral_constant;
+    if (dk <= 32) f(integral_constant<int, 32>());
+    else if (dk <= 64) f(integral_constant<int, 64>());
+    else if (dk <= 128) f(integral_constant<int, 128>());
+    else f(integral_constant<int, 256>());
+}
+
+}  // namespace
+}  // namespace ops
+}  // namespace ndvm

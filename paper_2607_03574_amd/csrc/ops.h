@@ -143,6 +143,44 @@ size_t ffn_bytes(int dtype, int64_t rows, int64_t n_in, int64_t n_out, bool grad
 hipError_t launch_ffn(const FfnArgs &a, hipStream_t stream);
 hipError_t launch_ffn_grad(const FfnArgs &a, hipStream_t stream);
 
+// ---- attention by the gated delta rule
+// Tokens of a chunk, and of a block of the gradient that whole states are kept for.
+constexpr int64_t kDeltaChunk = 32, kDeltaBlock = 64;
+struct DeltaArgs {
+    Heads q, k, v, g, beta;     // widths dk, dk, dv, 1, 1
+    const int64_t *offsets;     // [n_seq + 1], or null: n_tokens / n_seq tokens each
+    int64_t n_seq, n_tokens, heads, dk, dv;
+    float scale;
+    // forward pass
+    Heads o;
+    const float *state_in;      // [n_seq, heads, dk, dv], or null
+    float *state_out;           // or null
+    // gradient
+    Heads d_o, dq, dk_out, dv_out, dg, dbeta;   // dq, dk_out: of q's and k's heads; any but d_o without address: not wanted
+    const float *d_state_out;   // or null
+    float *d_state_in;          // or null
+    void *ws;
+    // laid out by the launches
+    char *chunks;               // a record for each chunk and head
+    float *states, *d_states;   // [block][heads][dk][dv]
+    float *u, *dr;              // [heads][n_tokens][dv]
+    float *dq_part, *dk_part;   // [heads][n_tokens][dk], where heads share q and k
+    float *segments;            // [segment][heads]: what it adds [dk][dv], then what enters it; its transition [dk][dk]
+    int64_t seg_len, n_segments;
+};
+size_t delta_bytes(int dtype, const DeltaArgs &a, bool grad);
+hipError_t launch_delta(int dtype, DeltaArgs a, hipStream_t stream);
+hipError_t launch_delta_grad(int dtype, DeltaArgs a, hipStream_t stream);
+
+struct DeltaStepArgs {
+    Heads q, k, v, g, beta, o;  // seq and head strides
+    float *state;               // [n_slots, heads, dk, dv]
+    const int64_t *slots;       // [n_seq], or null: slot i
+    int64_t n_seq, n_slots, heads, dk, dv;
+    float scale;
+};
+hipError_t launch_delta_step(int dtype, const DeltaStepArgs &a, hipStream_t stream);
+
 // ---- projections
 struct LinearArgs {
     int dtype, act;             // dtype: of y where x and w are bytes

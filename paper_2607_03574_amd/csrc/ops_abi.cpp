@@ -522,6 +522,112 @@ ndvm_status ndvm_gated_ffn_grad(int dtype, int act, const void *dh, int64_t ld_d
     });
 }
 
+// ---- the gated delta rule
+static ndvm_status check_delta(const char *who, const ndvm_delta_shape *s, bool tokens, bool packed) {
+    if (!s) return bad(who, "null shape");
+    if (!known_type(s->dtype)) return bad(who, "unknown type");
+    if (s->n_seq < 0 || s->heads < 1 || s->qk_heads < 1 || s->heads % s->qk_heads || s->dk < 1 || s->dv < 1)
+        return bad(who, "bad size, or heads that are no multiple of qk_heads");
+    if (s->heads > kMostHeads || s->dk > kMostHeadDim || s->dv > kMostHeadDim)
+        return fail(NDVM_E_UNSUPPORTED, who, "more than 65,535 heads, or a head wider than 256");
+    if (!std::isfinite(s->scale)) return bad(who, "scale is not finite");
+    if (s->n_seq > kMostGroups || s->n_seq * s->heads > kMostGroups || !fits(s->n_seq, s->heads, s->dk * s->dv))
+        return fail(NDVM_E_UNSUPPORTED, who, "too many sequences and heads");
+    if (!tokens) return NDVM_OK;
+    if (s->n_tokens < 0 || (s->n_seq == 0 && s->n_tokens)) return bad(who, "bad token count");
+    if (s->n_tokens > kMostTokens || !fits(s->n_tokens, s->heads, std::max(s->dk, s->dv)) ||
+        (s->n_tokens / kDeltaChunk + s->n_seq) * s->heads > int64_t(1) << 26)
+        return fail(NDVM_E_UNSUPPORTED, who, "too many tokens and heads");
+    if (!packed && s->n_seq && s->n_tokens % s->n_seq) return bad(who, "n_tokens is no multiple of n_seq, and there are no offsets");
+    return NDVM_OK;
+}
+
+static ndvm_status check_delta_inputs(const char *who, const ndvm_delta_shape *s, int64_t rows, const ndvm_heads *q, const ndvm_heads *k,
+                                      const ndvm_heads *v, const ndvm_heads *g, const ndvm_heads *beta) {
+    if (!q || !k || !v || !g || !beta) return bad(who, "null argument");
+    for (const ndvm_heads *x : {q, k, v, g, beta})
+        if (bad_heads(x, rows)) return bad(who, "null buffer or bad stride");
+    return NDVM_OK;
+}
+
+static DeltaArgs delta_args(const ndvm_delta_shape *s, const ndvm_heads *q, const ndvm_heads *k, const ndvm_heads *v, const ndvm_heads *g,
+                            const ndvm_heads *beta, const int64_t *offsets, const float *initial_state, void *workspace) {
+    DeltaArgs a{};
+    a.n_seq = s->n_seq;
+    a.n_tokens = s->n_tokens;
+    a.heads = s->heads;
+    a.dk = s->dk;
+    a.dv = s->dv;
+    a.scale = float(s->scale);
+    a.offsets = offsets;
+    a.ws = workspace;
+    a.state_in = initial_state;
+    if (!q) return a;
+    const int64_t group = s->heads / s->qk_heads;
+    a.q = heads_of(q, group);
+    a.k = heads_of(k, group);
+    a.v = heads_of(v, 1);
+    a.g = heads_of(g, 1);
+    a.beta = heads_of(beta, 1);
+    return a;
+}
+// packed calls have some offsets' address here
+static size_t delta_need(const ndvm_delta_shape *s, bool packed, bool grad) {
+    static const int64_t some = 0;
+    DeltaArgs a = delta_args(s, nullptr, nullptr, nullptr, nullptr, nullptr, packed ? &some : nullptr, nullptr, nullptr);
+    a.q.group = int(s->heads / s->qk_heads);
+    return delta_bytes(s->dtype, a, grad);
+}
+
+ndvm_status ndvm_delta_attention_workspace_bytes(const ndvm_delta_shape *shape, int packed, int with_grad, size_t *bytes) {
+    return guarded([&]() -> ndvm_status {
+        const char *who = "ndvm_delta_attention_workspace_bytes";
+        if (!bytes) return bad(who, "null pointer");
+        if (const ndvm_status st = check_delta(who, shape, true, packed != 0)) return st;
+        *bytes = delta_need(shape, packed != 0, with_grad != 0);
+        return NDVM_OK;
+    });
+}
+
+ndvm_status ndvm_delta_attention(const ndvm_delta_shape *shape, const ndvm_heads *q, const ndvm_heads *k, const ndvm_heads *v,
+                                 const ndvm_heads *g, const ndvm_heads *beta, const int64_t *offsets, const float *initial_state,
+                                 const ndvm_heads *o, float *final_state, void *workspace, size_t workspace_bytes, void *stream) {
+    return guarded([&]() -> ndvm_status {
+        const char *who = "ndvm_delta_attention";
+        const ndvm_delta_shape *s = shape;
+        if (const ndvm_status st = check_delta(who, s, true, offsets != nullptr)) return st;
+        if (const ndvm_status st = check_delta_inputs(who, s, s->n_tokens, q, k, v, g, beta)) return st;
+        if (!o || bad_heads(o, s->n_tokens)) return bad(who, "null buffer or bad stride");
+        if (s->n_seq == 0) return NDVM_OK;
+        const size_t need = delta_need(s, offsets != nullptr, false);
+        if (workspace_bytes < need) return fail(NDVM_E_NOMEM, who, "workspace too small");
+        if (need && !workspace) return bad(who, "null workspace");
+        DeltaArgs a = delta_args(s, q, k, v, g, beta, offsets, initial_state, workspace);
+        a.o = heads_of(o, 1);
+        a.state_out = final_state;
+        return launched(who, launch_delta(s->dtype, a, static_cast<hipStream_t>(stream)));
+    });
+}
+
+ndvm_status ndvm_delta_attention_step(const ndvm_delta_shape *shape, const ndvm_heads *q, const ndvm_heads *k, const ndvm_heads *v,
+                                      const ndvm_heads *g, const ndvm_heads *beta, float *state, int64_t n_slots, const int64_t *slots,
+                                      const ndvm_heads *o, void *stream) {
+    return guarded([&]() -> ndvm_status {
+        const char *who = "ndvm_delta_attention_step";
+        const ndvm_delta_shape *s = shape;
+        if (const ndvm_status st = check_delta(who, s, false, false)) return st;
+        if (n_slots < 0 || !fits(n_slots, s->heads, s->dk * s->dv) || (!slots && n_slots < s->n_seq)) return bad(who, "bad slot count");
+        if (const ndvm_status st = check_delta_inputs(who, s, s->n_seq, q, k, v, g, beta)) return st;
+        if (!o || bad_heads(o, s->n_seq)) return bad(who, "null buffer or bad stride");
+        if (s->n_seq == 0) return NDVM_OK;
+        if (n_slots && !state) return bad(who, "null buffer");
+        const int64_t group = s->heads / s->qk_heads;
+        const DeltaStepArgs a{heads_of(q, group), heads_of(k, group), heads_of(v, 1), heads_of(g, 1), heads_of(beta, 1), heads_of(o, 1),
+                              state, slots, s->n_seq, n_slots, s->heads, s->dk, s->dv, float(s->scale)};
+        return launched(who, launch_delta_step(s->dtype, a, static_cast<hipStream_t>(stream)));
+    });
+}
+
 static ndvm_status check_linear(const char *who, int act, const LinearArgs &a) {
     if (const ndvm_status st = check_ffn(who, a.dtype, a.rows, a.n_in, a.n_out)) return st;
     if (act < NDVM_ACT_SILU || act > NDVM_ACT_NONE) return bad(who, "unknown activation");
