@@ -581,7 +581,7 @@ ndvm_status ndvm_linear_attention_step(const ndvm_attention_shape *shape, const 
  * Sequences as for ndvm_linear_attention: of n_tokens / n_seq tokens each, or given by
  * `offsets`, with what is said there of offsets.  g and beta are given as the other
  * tensors are, with one value a head.
- * Limits: dk, dv <= 256, heads <= 65,535, n_tokens <= 2^30, and at most 2^26 pairs of
+ * Limits: dk, dv <= 256, heads <= 65,535, n_tokens <= 2^30, and less than 2^24 pairs of
  * 32 tokens of a sequence and a head.
  */
 typedef struct {
@@ -601,6 +601,23 @@ ndvm_status ndvm_delta_attention(const ndvm_delta_shape *shape, const ndvm_heads
                                  const ndvm_heads *v, const ndvm_heads *g, const ndvm_heads *beta,
                                  const int64_t *offsets, const float *initial_state, const ndvm_heads *o,
                                  float *final_state, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Its gradient, from that of o (`d_o`) and of the final state (d_final, float, or NULL for
+ * 0): of q and k (with qk_heads heads), of v, g and beta (with `heads`), and of the initial
+ * state (d_initial, float).  An argument without data, or d_initial NULL, is not wanted.
+ * The states on the way are formed again; the workspace holds one for each 64 tokens and
+ * head, and its gradient.  A value of g below -128 has gradient 0.  What is not finite in a
+ * head of a sequence may reach all of that head's gradients in that sequence, and those of
+ * the heads of q and k it reads; other sequences and heads keep theirs.  Tokens of no
+ * sequence are left as they are.
+ */
+ndvm_status ndvm_delta_attention_grad(const ndvm_delta_shape *shape, const ndvm_heads *q, const ndvm_heads *k,
+                                      const ndvm_heads *v, const ndvm_heads *g, const ndvm_heads *beta,
+                                      const int64_t *offsets, const float *initial_state, const ndvm_heads *d_o,
+                                      const float *d_final, const ndvm_heads *dq, const ndvm_heads *dk,
+                                      const ndvm_heads *dv, const ndvm_heads *dg, const ndvm_heads *dbeta,
+                                      float *d_initial, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * The recurrence for one new token of n_seq streams (shape->n_tokens is not read):

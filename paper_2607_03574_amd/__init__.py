@@ -34,7 +34,7 @@ EXPORTS = ["ndvm_tape_build", "ndvm_tape_upload", "ndvm_tape_upload_many", "ndvm
            "ndvm_rms_norm", "ndvm_rms_norm_workspace_bytes", "ndvm_rms_norm_grad", "ndvm_rms_norm_8bit", "ndvm_quantize_rows",
            "ndvm_linear_attention_workspace_bytes", "ndvm_linear_attention", "ndvm_linear_attention_grad",
            "ndvm_linear_attention_step", "ndvm_delta_attention_workspace_bytes", "ndvm_delta_attention",
-           "ndvm_delta_attention_step", "ndvm_gated_ffn_workspace_bytes", "ndvm_gated_ffn", "ndvm_gated_ffn_grad",
+           "ndvm_delta_attention_grad", "ndvm_delta_attention_step", "ndvm_gated_ffn_workspace_bytes", "ndvm_gated_ffn", "ndvm_gated_ffn_grad",
            "ndvm_linear_workspace_bytes", "ndvm_linear", "ndvm_linear_grad", "ndvm_linear_8bit_workspace_bytes", "ndvm_linear_8bit"]
 ACTIVATIONS = {"silu": 0, "gelu": 1, "sigmoid": 2, "relu": 3}     # NDVM_ACT_*
 ACT_NONE = 4           # NDVM_ACT_NONE: no activation (linear)
@@ -136,6 +136,8 @@ class _DeltaShape(ctypes.Structure):
 _delta_p = ctypes.POINTER(_DeltaShape)
 _delta_ws = _sig("ndvm_delta_attention_workspace_bytes", _int, [_delta_p, _int, _int, ctypes.POINTER(_sz)])
 _delta = _sig("ndvm_delta_attention", _int, [_delta_p] + [_heads_p] * 5 + [_vp, _vp, _heads_p, _vp, _vp, _sz, _vp])
+_delta_grad = _sig("ndvm_delta_attention_grad", _int, [_delta_p] + [_heads_p] * 5 + [_vp, _vp, _heads_p, _vp] + [_heads_p] * 5
+                   + [_vp, _vp, _sz, _vp])
 _delta_step = _sig("ndvm_delta_attention_step", _int, [_delta_p] + [_heads_p] * 5 + [_vp, _i64, _vp, _heads_p, _vp])
 _ffn_ws = _sig("ndvm_gated_ffn_workspace_bytes", _int, [_int, _i64, _i64, _i64, _int, ctypes.POINTER(_sz)])
 _ffn = _sig("ndvm_gated_ffn", _int, [_int, _int, _vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _i64, _vp, _i64, _vp, _sz,
@@ -980,6 +982,34 @@ def delta_attention(q, k, v, g, beta, offsets=None, scale=None, initial_state=No
         _check(_delta(shape, *heads, off, s0, _heads(out, "out", lead, shape.heads, shape.dv),
                       last.data_ptr() if final_state else None, ws_ptr, need, s), "ndvm_delta_attention")
     return out, last
+
+
+def delta_attention_grad(do, q, k, v, g, beta, offsets=None, scale=None, initial_state=None, grad_final_state=None,
+                         need=(True, True, True, True, True), stream=None):
+    """(dq, dk, dv, dg, dbeta, d initial_state) of delta_attention
+    (ndvm_delta_attention_grad); what is not needed, or has no initial state, is None;
+    tokens outside the sequences of `offsets` have gradient 0."""
+    t = _t()
+    shape, lead, off, *heads = _delta_args(t, q, k, v, g, beta, offsets, scale)
+    _alike(q, ("do", do))
+    H, Hk, dk, dv, dev = shape.heads, shape.qk_heads, shape.dk, shape.dv, q.device
+    dims = (shape.n_seq, H, dk, dv)
+    s0 = _of(initial_state, "initial_state", t.f32, dims, dev)
+    ds = _of(grad_final_state, "grad_final_state", t.f32, dims, dev)
+    hdo = _heads(do, "do", lead, H, dv)
+    with _On(t, stream, dev) as s:
+        def made(wanted, *size):
+            if not wanted:
+                return None, _Heads(None, 0, 0, 0)
+            x = (q.new_empty if off is None else q.new_zeros)((*lead, *size))
+            return x, _heads(x, "", lead, *size) if len(size) == 2 else _gates(x, "", lead, *size)
+
+        grads, to = zip(*(made(*w) for w in ((need[0], Hk, dk), (need[1], Hk, dk), (need[2], H, dv), (need[3], H), (need[4], H))))
+        d0 = q.new_empty(dims, dtype=t.f32) if s0 is not None else None
+        ws, ws_ptr, n = _delta_workspace(t, q, shape, off is not None, 1)
+        _check(_delta_grad(shape, *heads, off, s0, hdo, ds, *to, d0.data_ptr() if d0 is not None else None, ws_ptr, n, s),
+               "ndvm_delta_attention_grad")
+    return (*grads, d0)
 
 
 def delta_attention_step(q, k, v, g, beta, state, slots=None, scale=None, out=None, stream=None):

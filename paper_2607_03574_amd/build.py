@@ -22,7 +22,8 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
 SOURCES = ["frontend.cpp", "tape.cpp", "sched.cpp", "wide_sched.cpp", "abi.cpp", "kernels.hip", "wide.hip", "optim.hip",
-           "walk_host.cpp", "walk.hip", "ops_abi.cpp", "norm.hip", "rms.hip", "attend.hip", "ffn.hip", "linear.hip", "delta.hip"]
+           "walk_host.cpp", "walk.hip", "ops_abi.cpp", "norm.hip", "rms.hip", "attend.hip", "ffn.hip", "linear.hip", "delta.hip",
+           "delta_grad.hip"]
 EMU_SOURCES = ["frontend.cpp", "tape.cpp", "sched.cpp", "wide_sched.cpp", "emu.cpp"]
 COMMON = ["-O3", "-fPIC", "-std=c++17", "-ffp-contract=off", "-fno-fast-math", "-Wall",
           "-Wno-unused-function"]
@@ -52,7 +53,7 @@ WIDE = ["-mllvm", "-structurizecfg-skip-uniform-regions=true", "-Wno-inline-asm"
 # The encoder operators' kernels compute in float against a tolerance, not bit for
 # bit against the oracle: multiply-adds may be fused.
 OPS = ["-ffp-contract=fast"]
-OPS_OPTIONS_FOR = {"norm.hip", "rms.hip", "attend.hip", "ffn.hip", "linear.hip", "delta.hip"}
+OPS_OPTIONS_FOR = {"norm.hip", "rms.hip", "attend.hip", "ffn.hip", "linear.hip", "delta.hip", "delta_grad.hip"}
 
 
 def _options(src: str) -> list:

@@ -1,0 +1,514 @@
+// Gradient of attention by the gated delta rule.  (Formulas: delta_parts.h.)
+// Launches: the chunks' records; where few sequences are long, their segments; the walk forwards, which leaves m and the state
+// before each block of 64 tokens, beside the walk backwards, which leaves dv, e and the state's gradient after each block;
+// then every block by itself.  With u = b m, x = b e, and within a block
+//   Pd_ij = s L_ij do_i.u_j (j <= i),  Ad_ij = -L_ij x_i.u_j (j < i)
+//   dq = diag(s exp G) do S^T + Pd K
+//   dk = diag(exp(G_last - G)) U D^T - diag(exp G) X S^T + (Ad + Ad^T) K + Pd^T Q
+//   db_i = e_i.m_i
+//   dg_t = exp(G_last) <D, S> + sum_{j<t} f_j + sum_{i>=t} (y_i - z_i) + sum_{i>=t>j} (Pd_ij q_i.k_j + Ad_ij k_i.k_j)
+// f, y, z: the products of k's, q's and k's rows with those of the first terms above.  What decays between two tokens counts
+// for every t between them: no difference of large sums.
+#include "delta_walk.h"
+
+namespace ndvm {
+namespace ops {
+namespace {
+
+// z: 0 forwards, 1 backwards.
+template <class T, int DK, Walk WALK> __global__ void __launch_bounds__(256) delta_grad_walk(DeltaArgs a) {
+    __shared__ __align__(16) char lds[kWalkLds<T, DK, true>];
+    const uint32_t id = blockIdx.x / uint32_t(a.heads);
+    const int64_t h = blockIdx.x - id * uint32_t(a.heads), tile = int64_t(blockIdx.y) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const Piece g = find_piece(a, id, a.seg_len, !a.segments);
+    if (g.count == 0) return;
+    if (blockIdx.z == 0) {
+        if (a.m || WALK == kSums) walk<T, DK, WALK>(a, lds, g, blockIdx.x, h, tile);
+    } else {
+        walk_back<T, DK, WALK>(a, lds, g, blockIdx.x, h, tile);
+    }
+}
+
+template <int DK> __global__ void __launch_bounds__(256) delta_grad_carry(DeltaArgs a) {
+    const uint32_t seq = blockIdx.x / uint32_t(a.heads);
+    const int64_t h = blockIdx.x - seq * uint32_t(a.heads), tile = int64_t(blockIdx.y) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    if (blockIdx.z == 0) {
+        if (a.m) carry<DK, false>(a, seq, h, tile);
+    } else {
+        carry<DK, true>(a, seq, h, tile);
+    }
+}
+
+// A block's LDS: 32 columns of u, x and do as parts, later the pairs' matrices; the rows of q, later of k.
+template <class T> constexpr int kSlab = 64 * 64;      // bytes of 32 columns of a part
+template <class T> constexpr int kPair = 64 * 128;     // of a part of a pairs' matrix, [j][i]
+template <class T> constexpr int kArea = 2 * kResultParts<T> * kPair<T>;
+static_assert((2 * kResultParts<float> + kInputParts<float>) * kSlab<float> <= kArea<float>, "");
+
+// Four waves and a block: a wave has 64 tokens x 16 NT widths of dq and dk, and 16 rows of the pairs' matrices.
+template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(DeltaArgs a) {
+#ifdef __HIP_DEVICE_COMPILE__
+    constexpr int PARTS = kInputParts<T>, HELD = kResultParts<T>, NT = DK <= 64 ? 1 : DK / 64, G = DK / 8, ROWS = 64 * G * 16;
+    constexpr int LOADS = 64 * G / 256, SLAB = kSlab<T>, PAIR = kPair<T>;
+    __shared__ __align__(16) char area[kArea<T>], rows[PARTS * ROWS];
+    __shared__ double sum[64], row_sum[64], col_sum[4][64];
+    __shared__ float betas[64], rise[64], fall[64], dots[4][3][64], between[4];
+    const uint32_t id = blockIdx.x / uint32_t(a.heads);
+    const int64_t h = blockIdx.x - id * uint32_t(a.heads);
+    const Piece g = find_piece(a, id, kDeltaBlock);
+    if (g.count == 0) return;
+    const int l = threadIdx.x % 64, lm = l % 16, lg = l / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int len = int(g.len);
+    const int w0 = wave * 16 * NT;
+    const bool has = w0 < DK;
+    const auto width = [&](int n) { return NT == 1 ? w0 + lm : w0 + 32 * (n / 2) + 8 * (lm / 4) + 4 * (n % 2) + lm % 4; };
+
+    Eight<T> held[LOADS];
+    const auto fetch_rows = [&](const Heads &x) __attribute__((always_inline)) {
+        const T *p = at_token<T>(x, a, g, g.begin, h);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int at = i * 256 + threadIdx.x, row = at / G, gr = at % G;
+            held[i] = load_eight(p + row * x.tok + gr * 8, row < len ? a.dk - gr * 8 : 0);
+        }
+    };
+    const auto put_rows = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int at = i * 256 + threadIdx.x, row = at / G, gr = at % G;
+            bf16x8 p[PARTS];
+            parts_of(held[i], p);
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) *reinterpret_cast<bf16x8 *>(rows + q * ROWS + (row * G + (gr ^ turned<G>(row))) * 16) = p[q];
+        }
+    };
+    fetch_rows(a.q);
+    put_rows();
+    if (wave == 0) {
+        double log_a = 0.0;
+        float beta = 0.0f;
+        if (l < len) {
+            beta = float(*at_token<T>(a.beta, a, g, g.begin + l, h));
+            log_a = log_decay(*at_token<T>(a.g, a, g, g.begin + l, h));
+        }
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) {
+            const double before = __shfl_up(log_a, s);
+            if (l >= s) log_a += before;
+        }
+        sum[l] = log_a;
+        betas[l] = beta;
+        rise[l] = expf(float(log_a));
+        fall[l] = expf(float(__shfl(log_a, 63) - log_a));
+    }
+
+    // over 32 columns of v after the other: do S^T, X S^T, U D^T, do U^T, X U^T, e.m and <D, S>
+    const int srow = threadIdx.x / 4, sgr = threadIdx.x % 4;
+    const int64_t at_row = (h * a.n_tokens + g.first + g.begin + srow) * a.dv;
+    const T *const dop = at_token<T>(a.d_o, a, g, g.begin + srow, h);
+    const float beta = srow < len ? float(*at_token<T>(a.beta, a, g, g.begin + srow, h)) : 0.0f;
+    const float *const sp = a.states + (int64_t(id) * a.heads + h) * a.dk * a.dv, *const dp = a.d_states + (int64_t(id) * a.heads + h) * a.dk * a.dv;
+    Eight<float> m, e, S[NT], D[NT];
+    Eight<T> o;
+    const auto fetch = [&](int64_t c) __attribute__((always_inline)) {
+        const int64_t have = srow < len ? a.dv - c - sgr * 8 : 0;
+        m = load_eight(a.m + at_row + c + sgr * 8, have);
+        e = load_eight(a.e + at_row + c + sgr * 8, have);
+        o = load_eight(dop + c + sgr * 8, have);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int64_t d = width(n), left = d < a.dk ? a.dv - c - 8 * lg : 0;
+            S[n] = load_eight(sp + d * a.dv + c + 8 * lg, left);
+            D[n] = load_eight(dp + d * a.dv + c + 8 * lg, left);
+        }
+    };
+    f32x4 a1[4][NT], a2[4][NT], a3[4][NT], pd[4], ad[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        pd[i] = ad[i] = 0;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) a1[i][n] = a2[i][n] = a3[i][n] = 0;
+    }
+    float db = 0.0f, ds = 0.0f;
+    char *const of_u = area, *const of_x = area + HELD * SLAB, *const of_o = area + 2 * HELD * SLAB;
+    fetch(0);
+    for (int64_t c = 0; c < a.dv; c += 32) {
+        __syncthreads();
+        {
+            bf16x8 u[HELD], x[HELD], p[PARTS];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float mi = value(m, i), ei = value(e, i);
+                db += ei * mi;
+                split(beta * mi, u, i);
+                split(beta * ei, x, i);
+            }
+            parts_of(o, p);
+            const int at = srow * 64 + (sgr ^ turned<4>(srow)) * 16;
+#pragma unroll
+            for (int q = 0; q < HELD; ++q) {
+                *reinterpret_cast<bf16x8 *>(of_u + q * SLAB + at) = u[q];
+                *reinterpret_cast<bf16x8 *>(of_x + q * SLAB + at) = x[q];
+            }
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) *reinterpret_cast<bf16x8 *>(of_o + q * SLAB + at) = p[q];
+        }
+        bf16x8 s[NT][HELD], d[NT][HELD];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ds += value(S[n], i) * value(D[n], i);
+            parts_of(S[n], s[n]);
+            parts_of(D[n], d[n]);
+        }
+        __syncthreads();
+        if (c + 32 < a.dv) fetch(c + 32);
+        const auto operand = [&](const char *from, int tile, auto &x) __attribute__((always_inline)) {
+            const int row = 16 * tile + lm;
+            constexpr int N = sizeof(x) / sizeof(bf16x8);
+#pragma unroll
+            for (int q = 0; q < N; ++q) x[q] = *reinterpret_cast<const bf16x8 *>(from + q * SLAB + row * 64 + (lg ^ turned<4>(row)) * 16);
+        };
+        bf16x8 own_o[PARTS], own_x[HELD];
+        operand(of_o, wave, own_o);
+        operand(of_x, wave, own_x);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            bf16x8 u[HELD], x[HELD], p[PARTS];
+            operand(of_u, t, u);
+            if (has) {
+                operand(of_x, t, x);
+                operand(of_o, t, p);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    a1[t][n] = multiply<HELD - 1>(p, s[n], a1[t][n]);
+                    a2[t][n] = multiply<HELD - 1>(x, s[n], a2[t][n]);
+                    a3[t][n] = multiply<HELD - 1>(u, d[n], a3[t][n]);
+                }
+            }
+            if (t <= wave) {
+                pd[t] = multiply<HELD - 1>(own_o, u, pd[t]);
+                ad[t] = multiply<HELD - 1>(own_x, u, ad[t]);
+            }
+        }
+    }
+    __syncthreads();
+    fetch_rows(a.k);
+    // Pd and Ad, transposed, where the columns of v lay
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const int j = 16 * t + lm;
+        const double gj = sum[j];
+        bf16x4 p[HELD], x[HELD];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = 16 * wave + 4 * lg + r;
+            const float decay = j <= i ? expf(float(sum[i] - gj)) : 0.0f;
+            pd[t][r] = j <= i ? a.scale * decay * pd[t][r] : 0.0f;
+            ad[t][r] = j < i ? -decay * ad[t][r] : 0.0f;
+            split(pd[t][r], p, r);
+            split(ad[t][r], x, r);
+        }
+        const int at = j * 128 + ((2 * wave + lg / 2) ^ turned<8>(j)) * 16 + lg % 2 * 8;
+#pragma unroll
+        for (int q = 0; q < HELD; ++q) {
+            *reinterpret_cast<bf16x4 *>(area + q * PAIR + at) = p[q];
+            *reinterpret_cast<bf16x4 *>(area + (HELD + q) * PAIR + at) = x[q];
+        }
+    }
+    __syncthreads();
+    // operands of the pairs' matrices: 16 rows j, 32 columns i as they lie; or 16 rows i, 32 columns j
+    const auto down = [&](const char *from, int tile, int step, bf16x8(&x)[HELD]) __attribute__((always_inline)) {
+        const int row = 16 * tile + lm;
+#pragma unroll
+        for (int q = 0; q < HELD; ++q) x[q] = *reinterpret_cast<const bf16x8 *>(from + q * PAIR + row * 128 + ((4 * step + lg) ^ turned<8>(row)) * 16);
+    };
+    const auto across = [&](const char *from, int tile, int step, bf16x8(&x)[HELD]) __attribute__((always_inline)) {
+        const int row = 32 * step + 8 * lg + lm / 4, gr = 2 * tile + lm % 4 / 2;
+#pragma unroll
+        for (int q = 0; q < HELD; ++q) {
+            const char *p = from + q * PAIR + lm % 2 * 8;
+            const bf16x4 lo = read_transposed(p + row * 128 + (gr ^ turned<8>(row)) * 16);
+            const bf16x4 hi = read_transposed(p + (row + 4) * 128 + (gr ^ turned<8>(row + 4)) * 16);
+            x[q] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    };
+    // 32 rows of q or k, the wave's widths, as the right operand
+    const auto widths = [&](int step, int n, bf16x8(&x)[PARTS]) __attribute__((always_inline)) {
+        const int row = 32 * step + 8 * lg + lm / 4;
+        const int gr = NT == 1 ? w0 / 8 + lm % 4 / 2 : w0 / 8 + 4 * (n / 2) + lm % 4, off = NT == 1 ? lm % 2 * 8 : n % 2 * 8;
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) {
+            const char *p = rows + q * ROWS + off;
+            const bf16x4 lo = read_transposed(p + (row * G + (gr ^ turned<G>(row))) * 16);
+            const bf16x4 hi = read_transposed(p + ((row + 4) * G + (gr ^ turned<G>(row + 4))) * 16);
+            x[q] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    };
+    // a value of q or k
+    const auto value_at = [&](int row, int w) __attribute__((always_inline)) {
+        const char *p = rows + (row * G + ((w / 8) ^ turned<G>(row))) * 16 + w % 8 * 2;
+        float v = float(*reinterpret_cast<const bf16 *>(p));
+#pragma unroll
+        for (int q = 1; q < PARTS; ++q) v += float(*reinterpret_cast<const bf16 *>(p + q * ROWS));
+        return v;
+    };
+    // over the widths of the wave: the product of a token's row and what it gets
+    const auto dot = [&](int which, int t, const f32x4(&x)[NT]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int token = 16 * t + 4 * lg + r;
+            float v = 0.0f;
+            if (has)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) v += value_at(token, width(n)) * x[n][r];
+#pragma unroll
+            for (int s = 1; s < 16; s <<= 1) v += __shfl_xor(v, s);
+            if (lm == 0) dots[wave][which][token] = v;
+        }
+    };
+    f32x4 out[4][NT];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            out[t][n] = 0;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 16 * t + 4 * lg + r;
+                a1[t][n][r] *= rise[i] * a.scale;
+                a2[t][n][r] *= rise[i];
+                a3[t][n][r] *= fall[i];
+            }
+        }
+        dot(0, t, a1[t]);
+    }
+    if (has) {
+#pragma unroll
+        for (int step = 0; step < 2; ++step) {
+            bf16x8 y[NT][PARTS];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) widths(step, n, y[n]);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                if (32 * step + 31 < 16 * t) continue;      // all of its i lie before j
+                bf16x8 p[HELD];
+                down(area, t, step, p);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) out[t][n] = multiply<HELD - 1>(p, y[n], out[t][n]);
+            }
+        }
+    }
+    __syncthreads();
+    put_rows();
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        dot(1, t, a2[t]);
+        dot(2, t, a3[t]);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) out[t][n] += a3[t][n] - a2[t][n];
+    }
+    if (has) {
+#pragma unroll
+        for (int step = 0; step < 2; ++step) {
+            bf16x8 y[NT][PARTS];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) widths(step, n, y[n]);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                bf16x8 p[HELD];
+                if (32 * step <= 16 * t + 15) {
+                    across(area, t, step, p);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) a1[t][n] = multiply<HELD - 1>(p, y[n], a1[t][n]);
+                    across(area + HELD * PAIR, t, step, p);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) out[t][n] = multiply<HELD - 1>(p, y[n], out[t][n]);
+                }
+                if (32 * step + 31 >= 16 * t) {
+                    down(area + HELD * PAIR, t, step, p);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) out[t][n] = multiply<HELD - 1>(p, y[n], out[t][n]);
+                }
+            }
+        }
+    }
+    // what pairs add to dg: q k^T and k k^T of the wave's rows
+    {
+        f32x4 qk[4], kk[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) qk[t] = kk[t] = 0;
+        const auto operand = [&](int tile, int ks, bf16x8(&x)[PARTS]) __attribute__((always_inline)) {
+            const int row = 16 * tile + lm;
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) x[q] = *reinterpret_cast<const bf16x8 *>(rows + q * ROWS + (row * G + ((4 * ks + lg) ^ turned<G>(row))) * 16);
+        };
+        const int row = 16 * wave + lm;
+        const T *const qp = at_token<T>(a.q, a, g, g.begin + row, h);
+#pragma unroll
+        for (int ks = 0; ks < DK / 32; ++ks) {
+            bf16x8 q[PARTS], k[PARTS];
+            parts_of(load_eight(qp + ks * 32 + 8 * lg, row < len ? a.dk - ks * 32 - 8 * lg : 0), q);
+            operand(wave, ks, k);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                if (t > wave) continue;
+                bf16x8 x[PARTS];
+                operand(t, ks, x);
+                qk[t] = multiply<HELD - 1>(q, x, qk[t]);
+                kk[t] = multiply<HELD - 1>(k, x, kk[t]);
+            }
+        }
+        double of_row[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            double of_col = 0;
+            const int j = 16 * t + lm;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 16 * wave + 4 * lg + r;
+                const double w = j < i ? double(pd[t][r] * qk[t][r] + ad[t][r] * kk[t][r]) : 0.0;
+                of_row[r] += w;
+                of_col += w;
+            }
+            of_col += __shfl_xor(of_col, 16);
+            of_col += __shfl_xor(of_col, 32);
+            if (lg == 0) col_sum[wave][j] = of_col;
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+#pragma unroll
+            for (int s = 1; s < 16; s <<= 1) of_row[r] += __shfl_xor(of_row[r], s);
+            if (lm == 0) row_sum[16 * wave + 4 * lg + r] = of_row[r];
+        }
+    }
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) ds += __shfl_xor(ds, s);
+    if (l == 0) between[wave] = ds;
+    __syncthreads();
+    if (wave == 0 && a.dg.p) {
+        float y = 0, z = 0, f = 0;
+        double c = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            y += dots[w][0][l];
+            z += dots[w][1][l];
+            f += dots[w][2][l];
+            c += col_sum[w][l];
+        }
+        double after = double(y) - double(z) + row_sum[l] - c, before = f;
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) {
+            const double x = __shfl_down(after, s), y2 = __shfl_up(before, s);
+            if (l + s < 64) after += x;
+            if (l >= s) before += y2;
+        }
+        const double whole = rise[63] * (double(between[0]) + between[1] + between[2] + between[3]);
+        if (l < len) *const_cast<T *>(at_token<T>(a.dg, a, g, g.begin + l, h)) = T(float(whole + (before - f) + after));
+    }
+    db += __shfl_xor(db, 1);
+    db += __shfl_xor(db, 2);
+    if (a.dbeta.p && sgr == 0 && srow < len) *const_cast<T *>(at_token<T>(a.dbeta, a, g, g.begin + srow, h)) = T(db);
+    if (!has) return;
+    const auto store = [&](const Heads &to, float *part, const f32x4(&x)[4][NT]) __attribute__((always_inline)) {
+        if (!to.p) return;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int token = 16 * t + 4 * lg + r;
+                if (token >= len) continue;
+                T *at = part ? nullptr : const_cast<T *>(at_token<T>(to, a, g, g.begin + token, h));
+                float *wide = part ? part + (h * a.n_tokens + g.first + g.begin + token) * a.dk : nullptr;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const int64_t d = width(n);
+                    if (d >= a.dk) continue;
+                    if (part) wide[d] = x[t][n][r];
+                    else at[d] = T(x[t][n][r]);
+                }
+            }
+    };
+    store(a.dq, a.dq_part, a1);
+    store(a.dk_out, a.dk_part, out);
+#endif
+}
+
+// What heads that share q and k give them, added up; rows of no sequence stay as they are.  y: heads of q and k; z: dq, dk.
+template <class T> __global__ void __launch_bounds__(256) delta_fold(DeltaArgs a) {
+    const Heads &to = blockIdx.z ? a.dk_out : a.dq;
+    const float *part = blockIdx.z ? a.dk_part : a.dq_part;
+    if (!to.p) return;
+    const int64_t begin = a.offsets ? token_at(a, 0) : 0, end = a.offsets ? token_at(a, a.n_seq) : a.n_tokens, per = a.n_tokens / a.n_seq;
+    for (int64_t at = begin * a.dk + int64_t(blockIdx.x) * 256 + threadIdx.x; at < end * a.dk; at += int64_t(gridDim.x) * 256) {
+        const int64_t token = at / a.dk, d = at - token * a.dk;
+        float s = 0;
+        for (int i = 0; i < to.group; ++i) s += part[((int64_t(blockIdx.y) * to.group + i) * a.n_tokens) * a.dk + at];
+        const int64_t row = a.offsets ? token * to.tok : token / per * to.seq + token % per * to.tok;
+        static_cast<T *>(const_cast<void *>(to.p))[row + blockIdx.y * to.head + d] = T(s);
+    }
+}
+
+// need: whether anything but dv and the initial state's gradient is wanted
+template <class T> size_t lay_out(DeltaArgs &a, Space s, bool need) {
+    const int64_t states = a.heads * a.dk * a.dv * 4;
+    a.record = kRecordGrad;
+    s.take(a.chunks, piece_ids(a, kDeltaChunk) * a.heads * a.record);
+    if (cut(a)) {
+        s.take(a.segments, a.n_segments * states);
+        s.take(a.d_segments, a.n_segments * states);
+        s.take(a.moves, a.n_segments * a.heads * a.dk * a.dk * 4);
+        s.take(a.moves_t, a.n_segments * a.heads * a.dk * a.dk * 4);
+    }
+    if (!need) return s.used + 256;
+    const int64_t blocks = piece_ids(a, kDeltaBlock);
+    s.take(a.states, blocks * states);
+    s.take(a.d_states, blocks * states);
+    s.take(a.m, a.heads * a.n_tokens * a.dv * 4);
+    s.take(a.e, a.heads * a.n_tokens * a.dv * 4);
+    if (a.q.group > 1) {
+        s.take(a.dq_part, a.heads * a.n_tokens * a.dk * 4);
+        s.take(a.dk_part, a.heads * a.n_tokens * a.dk * 4);
+    }
+    return s.used + 256;
+}
+
+template <class T> void delta_grad(DeltaArgs a, hipStream_t stream) {
+    const bool need = a.dq.p || a.dk_out.p || a.dg.p || a.dbeta.p;
+    lay_out<T>(a, Space(a.ws), need);
+    const int64_t pairs = piece_ids(a, kDeltaChunk) * a.heads;
+    if (a.n_tokens) delta_prepare<T, true><<<dim3(uint32_t(ceil_div(pairs, 4))), 256, 0, stream>>>(a, pairs);
+    with_width(a.dk, [&](auto d) {
+        constexpr int DK = decltype(d)::value;
+        const auto grid = [&](int64_t ids, int64_t tiles) { return dim3(uint32_t(ids * a.heads), uint32_t(ceil_div(tiles, 4)), 2); };
+        const int64_t of_v = ceil_div(a.dv, 16), of_k = ceil_div(a.dk, 16);
+        if (a.segments) {
+            delta_grad_walk<T, DK, kSums><<<grid(a.n_segments, of_v + of_k), 256, 0, stream>>>(a);
+            delta_grad_carry<DK><<<grid(a.n_seq, of_v), 256, 0, stream>>>(a);
+        }
+        delta_grad_walk<T, DK, kKept><<<grid(a.n_segments, of_v), 256, 0, stream>>>(a);
+        if (need && a.n_tokens) delta_blocks<T, DK><<<dim3(uint32_t(piece_ids(a, kDeltaBlock) * a.heads)), 256, 0, stream>>>(a);
+    });
+    if (a.dq_part && (a.dq.p || a.dk_out.p) && a.n_tokens) {
+        const int64_t groups = std::min(ceil_div(a.n_tokens * a.dk, 256), kMostGroups);
+        delta_fold<T><<<dim3(uint32_t(groups), uint32_t(a.heads / a.q.group), 2), 256, 0, stream>>>(a);
+    }
+}
+
+}  // namespace
+
+size_t delta_grad_bytes(int dtype, const DeltaArgs &a) {
+    DeltaArgs b = a;
+    return dtype == NDVM_F32 ? lay_out<float>(b, Space(nullptr), true) : lay_out<bf16>(b, Space(nullptr), true);
+}
+
+hipError_t launch_delta_grad(int dtype, DeltaArgs a, hipStream_t stream) {
+    return with_type(dtype, [&](auto zero) {
+        delta_grad<decltype(zero)>(a, stream);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace ops
+}  // namespace ndvm

@@ -2,9 +2,13 @@
 // record that is kept for a chunk of 32 tokens and a head.
 //   S_t = a_t S_{t-1} + k_t^T u_t,  u_t = b_t (v_t - a_t k_t S_{t-1}),  o_t = s q_t S_t,  a_t = exp(g_t)
 // Over a chunk, with G the running sum of g in it, L_ij = exp(G_i - G_j) and S what entered it:
-//   (I + A) U = R = diag(b) (V - diag(exp G) K S),  A_ij = b_i L_ij k_i.k_j for j < i
+//   (I + A) M = X = V - diag(exp G) K S,  U = diag(b) M,  A_ij = L_ij k_i.k_j b_j for j < i
 //   O = s (diag(exp G) Q S + P U),  P_ij = L_ij q_i.k_j for j <= i
 //   S' = exp(G_last) S + sum_j exp(G_last - G_j) k_j^T u_j
+// The gradient, with D that of S', do that of O, and A_ij = A'_ij b_j:
+//   dU = s P^T do + diag(exp(G_last - G)) K D,  E = (I + diag(b) A')^-T dU,  dV = dX = diag(b) E,  db_i = e_i.m_i
+//   dS = exp(G_last) D + Q^T diag(s exp G) do - K^T diag(exp G) dX
+// Both inverses come from B = (I + A)^-1 A': they are I - B diag(b) and I - diag(b) B.
 // All sums and states are in float; products are made of bf16 parts on the bf16 matrix instructions (16 times the
 // rate of the float ones): 16-bit inputs are one part (bfloat16) or two (half), floats three; what the state is made
 // of is three parts, products whose places add up to 2 at most: 2^-21 of a term is left out at most, 2^-24 on
@@ -154,8 +158,9 @@ template <class T> __device__ inline const T *at_token(const Heads &x, const Del
 }
 
 // The record of a chunk and head: 32 values each of b, exp G and exp(G_last - G), exp(G_last), and the first token whose k,
-// g or beta is not finite (32: none); then 32 x 32 matrices as operands of the matrix instructions: row 16 t + l % 16,
-// columns 8 (l / 16) on, of tile t in lane l, a part of a tile after the other.
+// g or beta is not finite (32: none); then 32 x 32 matrices as operands of the matrix instructions: row 16 t + l % 16 of tile
+// t in lane l, its columns in the order of the accumulators' rows: 16 (e / 4) + 4 (l / 16) + e % 4, e = 0..7.  What a product
+// leaves in a wave's accumulators is so the next one's operand as it stands.
 constexpr int kRecordHead = 512, kTile = 1024;
 struct RecordHead {
     float beta[32], rise[32], fall[32], whole;
@@ -163,10 +168,9 @@ struct RecordHead {
 };
 static_assert(sizeof(RecordHead) <= kRecordHead, "");
 constexpr int kRecordMatrix = 2 * kStateParts * kTile;
-template <class T> constexpr int kRecordPairs = 2 * kResultParts<T> * kTile;
-// forward: (I + A)^-1 and P; gradient: the inverse, its transpose and that of P
-template <class T> constexpr int kRecord = kRecordHead + kRecordMatrix + kRecordPairs<T>;
-template <class T> constexpr int kRecordGrad = kRecord<T> + kRecordMatrix;
+// forward: (I + A)^-1 and P; gradient: (I + A)^-1, (I + diag(b) A')^-T and P^T
+template <class T> constexpr int kRecord = kRecordHead + kRecordMatrix + 2 * kResultParts<T> * kTile;
+constexpr int kRecordGrad = kRecordHead + 3 * kRecordMatrix;
 
 // A log decay as it is used: what lies below -128 is a factor of 0 in float in any case, and its sums stay exact.
 template <class T> __device__ inline double log_decay(T g) {
@@ -174,8 +178,8 @@ template <class T> __device__ inline double log_decay(T g) {
     return v < -128.0f ? -128.0 : double(v);
 }
 
-// One wave: the record of chunk `id` and head h.  lds: 2 x 32 x 36 floats and 32 doubles of its own.
-constexpr int kPrepareLds = 2 * 32 * 36 * 4 + 256;
+// One wave: the record of chunk `id` and head h.  Its own LDS: 2 x 32 x 36 floats, 32 doubles and 32 floats.
+constexpr int kPrepareLds = 2 * 32 * 36 * 4 + 384;
 template <class T, bool GRAD> __global__ void __launch_bounds__(256) delta_prepare(DeltaArgs a, int64_t pairs) {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int PARTS = kInputParts<T>, HELD = kResultParts<T>, LD = 36;
@@ -185,10 +189,11 @@ template <class T, bool GRAD> __global__ void __launch_bounds__(256) delta_prepa
     if (pair >= pairs) return;
     float(*const m)[LD] = reinterpret_cast<float(*)[LD]>(shared[wave]), (*const p)[LD] = m + 32;
     double *const sum = reinterpret_cast<double *>(shared[wave] + 2 * 32 * LD * 4);
+    float *const betas = reinterpret_cast<float *>(sum + 32);
     const int64_t h = pair % a.heads;
     const Piece g = find_piece(a, uint32_t(pair / a.heads), kDeltaChunk);
     if (g.count == 0) return;
-    char *const record = a.chunks + pair * (GRAD ? kRecordGrad<T> : kRecord<T>);
+    char *const record = a.chunks + pair * a.record;
     const int len = int(g.len);
 
     // k k^T and q k^T, the tiles (0, 0), (1, 0) and (1, 1)
@@ -237,6 +242,7 @@ template <class T, bool GRAD> __global__ void __launch_bounds__(256) delta_prepa
     RecordHead *const head = reinterpret_cast<RecordHead *>(record);
     if (l < 32) {
         sum[l] = log_a;
+        betas[l] = beta;
         head->beta[l] = beta;
         head->rise[l] = expf(float(log_a));
         head->fall[l] = expf(float(last - log_a));
@@ -245,7 +251,7 @@ template <class T, bool GRAD> __global__ void __launch_bounds__(256) delta_prepa
             head->bad = bad;
         }
     }
-    // A and P; beta by row
+    // A' and P
 #pragma unroll
     for (int t = 0; t < 4; ++t) {       // tiles (0, 0), (0, 1), (1, 0), (1, 1)
         const int ti = t / 2, tj = t % 2, j = 16 * tj + lm;
@@ -253,51 +259,57 @@ template <class T, bool GRAD> __global__ void __launch_bounds__(256) delta_prepa
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int i = 16 * ti + 4 * lg + r;
-            const float b = __shfl(beta, i);
             float ma = 0.0f, pa = 0.0f;
             if (t != 1) {
                 const int at = t == 0 ? 0 : t - 1;
                 const float decay = expf(float(sum[i] - gj));
-                if (j < i && i < fit) ma = b * decay * kk[at][r];
+                if (j < i && i < fit) ma = decay * kk[at][r];
                 if (j <= i && i < fit) pa = decay * qk[at][r];
             }
             m[i][j] = ma;
             p[i][j] = pa;
         }
     }
-    // The inverse of I + A: of both diagonal blocks by substitution, a column a lane; then the block below them.
+    // B: its diagonal blocks by substitution, a column a lane; then the block below them, (I - B22 b2) A'21 (I - b1 B11).
     // Rows of the blocks are read before any is written over.
     {
         const int b = token / 16 * 16, c = token % 16;
-        float x[16];
+        float x[16], bx[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            float s = i == c ? 1.0f : 0.0f;
+            float s = i > c ? m[b + i][b + c] : 0.0f;
 #pragma unroll
-            for (int j = 0; j < i; ++j) s -= m[b + i][b + j] * x[j];
+            for (int j = 0; j < i; ++j) s -= m[b + i][b + j] * bx[j];
             x[i] = s;
+            bx[i] = betas[b + i] * s;
         }
-        float below[4];         // A's block as an operand
+        float below[4];         // A' below the blocks, as an operand
 #pragma unroll
         for (int r = 0; r < 4; ++r) below[r] = m[16 + lm][4 * r + lg];
 #pragma unroll
         for (int i = 0; i < 16; ++i) m[b + i][b + c] = x[i];
         f32x4 y = 0, z = 0;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) y = mfma(below[r], m[4 * r + lg][lm], y);
+        for (int r = 0; r < 4; ++r) {
+            const int k = 4 * r + lg;
+            y = mfma(below[r], (k == lm ? 1.0f : 0.0f) - betas[k] * m[k][lm], y);
+        }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) z = mfma(m[16 + lm][16 + 4 * lg + r], y[r], z);      // rows 4 (l / 16) + r of y are in lane l
+        for (int r = 0; r < 4; ++r) {       // rows 4 (l / 16) + r of y are in lane l
+            const int k = 4 * lg + r;
+            z = mfma((k == lm ? 1.0f : 0.0f) - m[16 + lm][16 + k] * betas[16 + k], y[r], z);
+        }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) m[16 + 4 * lg + r][lm] = -z[r];
+        for (int r = 0; r < 4; ++r) m[16 + 4 * lg + r][lm] = z[r];
     }
     char *to = record + kRecordHead + l * 16;
-    const auto store = [&](const float(*x)[LD], auto parts, auto transposed) __attribute__((always_inline)) {
+    const auto store = [&](auto parts, auto f) __attribute__((always_inline)) {
         constexpr int N = decltype(parts)::value;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             bf16x8 v[N];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) split(decltype(transposed)::value ? x[8 * lg + i][16 * t + lm] : x[16 * t + lm][8 * lg + i], v, i);
+            for (int e = 0; e < 8; ++e) split(f(16 * t + lm, 16 * (e / 4) + 4 * lg + e % 4), v, e);
 #pragma unroll
             for (int q = 0; q < N; ++q) *reinterpret_cast<bf16x8 *>(to + (t * N + q) * kTile) = v[q];
         }
@@ -305,25 +317,23 @@ template <class T, bool GRAD> __global__ void __launch_bounds__(256) delta_prepa
     };
     const std::integral_constant<int, kStateParts> of_state;
     const std::integral_constant<int, HELD> of_result;
-    store(m, of_state, std::false_type());
-    if (GRAD) store(m, of_state, std::true_type());
-    store(p, of_result, std::integral_constant<bool, GRAD>());
+    store(of_state, [&](int i, int j) { return (i == j ? 1.0f : 0.0f) - m[i][j] * betas[j]; });
+    if constexpr (GRAD) {
+        store(of_state, [&](int i, int j) { return (i == j ? 1.0f : 0.0f) - betas[j] * m[j][i]; });
+        store(of_state, [&](int i, int j) { return p[j][i]; });
+    } else {
+        store(of_result, [&](int i, int j) { return p[i][j]; });
+    }
 #endif
 }
 
 // ---- rows of q and k in LDS, in granules of 16 bytes: granule i of row r of G lies at i ^ turned<G>(r), so that the rows
 // one instruction reads, along them or (transposed) four of them across, are in different banks
 template <int G> __device__ inline int turned(int r) {
-    return G >= 16 ? r % 4 * 4 + r / 4 % 4 : G == 8 ? r / 2 % 2 * 4 + r / 4 % 2 : r / 4 % 2;
+    return G >= 16 ? r % 4 * 4 + r / 4 % 4 : G == 8 ? r / 2 % 2 * 4 + r / 4 % 4 : r / 4 % 4;
 }
 
-// How a workgroup of four waves divides a chunk: WK waves share the widths of k (KPW times 32 each), the others have
-// other columns of v; a wave has 32 columns.
-template <int DK> struct Split {
-    static constexpr int WK = DK >= 128 ? 4 : DK / 32, WN = 4 / WK, KPW = DK / 32 / WK, NC = 32 * WN, G = DK / 8, OWN = 4 / WK;
-};
-
-template <class T, class F> void with_width(int64_t dk, F f) {
+template <class F> void with_width(int64_t dk, F f) {
     using std::integral_constant;
     if (dk <= 32) f(integral_constant<int, 32>());
     else if (dk <= 64) f(integral_constant<int, 64>());

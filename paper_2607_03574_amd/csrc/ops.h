@@ -162,13 +162,17 @@ struct DeltaArgs {
     void *ws;
     // laid out by the launches
     char *chunks;               // a record for each chunk and head
-    float *states, *d_states;   // [block][heads][dk][dv]
-    float *u, *dr;              // [heads][n_tokens][dv]
+    int64_t record;             // bytes of one
+    float *states, *d_states;   // [block][heads][dk][dv]: S before a block, and its gradient after it
+    float *m, *e;               // [heads][n_tokens][dv]
     float *dq_part, *dk_part;   // [heads][n_tokens][dk], where heads share q and k
-    float *segments;            // [segment][heads]: what it adds [dk][dv], then what enters it; its transition [dk][dk]
+    // sequences cut into segments: what one adds to a state [segment][heads][dk][dv], then the state that enters it; the
+    // same of the gradient, from the back; what it makes of a state [segment][heads][dk][dk], and transposed
+    float *segments, *d_segments, *moves, *moves_t;
     int64_t seg_len, n_segments;
 };
 size_t delta_bytes(int dtype, const DeltaArgs &a, bool grad);
+size_t delta_grad_bytes(int dtype, const DeltaArgs &a);
 hipError_t launch_delta(int dtype, DeltaArgs a, hipStream_t stream);
 hipError_t launch_delta_grad(int dtype, DeltaArgs a, hipStream_t stream);
 

@@ -536,7 +536,7 @@ static ndvm_status check_delta(const char *who, const ndvm_delta_shape *s, bool 
     if (!tokens) return NDVM_OK;
     if (s->n_tokens < 0 || (s->n_seq == 0 && s->n_tokens)) return bad(who, "bad token count");
     if (s->n_tokens > kMostTokens || !fits(s->n_tokens, s->heads, std::max(s->dk, s->dv)) ||
-        (s->n_tokens / kDeltaChunk + s->n_seq) * s->heads > int64_t(1) << 26)
+        (s->n_tokens / kDeltaChunk + s->n_seq) * s->heads > kMostGroups)
         return fail(NDVM_E_UNSUPPORTED, who, "too many tokens and heads");
     if (!packed && s->n_seq && s->n_tokens % s->n_seq) return bad(who, "n_tokens is no multiple of n_seq, and there are no offsets");
     return NDVM_OK;
@@ -606,6 +606,40 @@ ndvm_status ndvm_delta_attention(const ndvm_delta_shape *shape, const ndvm_heads
         a.o = heads_of(o, 1);
         a.state_out = final_state;
         return launched(who, launch_delta(s->dtype, a, static_cast<hipStream_t>(stream)));
+    });
+}
+
+ndvm_status ndvm_delta_attention_grad(const ndvm_delta_shape *shape, const ndvm_heads *q, const ndvm_heads *k, const ndvm_heads *v,
+                                      const ndvm_heads *g, const ndvm_heads *beta, const int64_t *offsets, const float *initial_state,
+                                      const ndvm_heads *d_o, const float *d_final, const ndvm_heads *dq, const ndvm_heads *dk,
+                                      const ndvm_heads *dv, const ndvm_heads *dg, const ndvm_heads *dbeta, float *d_initial, void *workspace,
+                                      size_t workspace_bytes, void *stream) {
+    return guarded([&]() -> ndvm_status {
+        const char *who = "ndvm_delta_attention_grad";
+        const ndvm_delta_shape *s = shape;
+        if (const ndvm_status st = check_delta(who, s, true, offsets != nullptr)) return st;
+        if (const ndvm_status st = check_delta_inputs(who, s, s->n_tokens, q, k, v, g, beta)) return st;
+        if (!d_o || bad_heads(d_o, s->n_tokens)) return bad(who, "null buffer or bad stride");
+        bool wanted = d_initial != nullptr;
+        for (const ndvm_heads *x : {dq, dk, dv, dg, dbeta}) {
+            if (!x || bad_heads(x, 0)) return bad(who, "null argument or bad stride");
+            wanted |= x->data != nullptr;
+        }
+        if (s->n_seq == 0 || !wanted) return NDVM_OK;
+        const size_t need = delta_need(s, offsets != nullptr, true);
+        if (workspace_bytes < need) return fail(NDVM_E_NOMEM, who, "workspace too small");
+        if (!workspace) return bad(who, "null workspace");
+        const int64_t group = s->heads / s->qk_heads;
+        DeltaArgs a = delta_args(s, q, k, v, g, beta, offsets, initial_state, workspace);
+        a.d_o = heads_of(d_o, 1);
+        a.d_state_out = d_final;
+        a.d_state_in = d_initial;
+        a.dq = heads_of(dq, group);
+        a.dk_out = heads_of(dk, group);
+        a.dv_out = heads_of(dv, 1);
+        a.dg = heads_of(dg, 1);
+        a.dbeta = heads_of(dbeta, 1);
+        return launched(who, launch_delta_grad(s->dtype, a, static_cast<hipStream_t>(stream)));
     });
 }
 

@@ -13,8 +13,9 @@ from __future__ import annotations
 import torch
 from torch.autograd.function import once_differentiable
 
-from . import (Tape, _launch_stream, _row_stride, adam_step, gated_ffn_grad, grad, layer_norm_grad, linear_attention_grad,
-               linear_grad, rms_norm_grad)
+from . import (Tape, _launch_stream, _row_stride, adam_step, delta_attention_grad, gated_ffn_grad, grad, layer_norm_grad,
+               linear_attention_grad, linear_grad, rms_norm_grad)
+from . import delta_attention as delta_attention_op
 from . import gated_ffn as gated_ffn_op
 from . import layer_norm as layer_norm_op
 from . import linear as linear_op
@@ -154,6 +155,39 @@ def linear_attention(q, k, v, log_decay, offsets=None, scale=None, initial_state
     if log_decay.requires_grad and torch.is_grad_enabled():
         raise ValueError("log_decay has no gradient: detach it")
     return LinearAttention.apply(q, k, v, log_decay, offsets, scale, initial_state)
+
+
+def _inner(x):
+    """x, or a copy of it where the values of a head do not lie side by side."""
+    return x if x.shape[-1] <= 1 or x.stride(-1) == 1 else x.contiguous()
+
+
+class DeltaAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, g, beta, offsets, scale, initial_state):
+        q, k, v = (_inner(x.detach()) for x in (q, k, v))
+        o, last = delta_attention_op(q, k, v, g.detach(), beta.detach(), offsets, scale,
+                                     None if initial_state is None else initial_state.detach(), final_state=True)
+        ctx.save_for_backward(q, k, v, g, beta, offsets, initial_state)
+        ctx.scale = scale
+        ctx.set_materialize_grads(False)
+        return o, last
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, do, dlast):
+        q, k, v, g, beta, offsets, s0 = ctx.saved_tensors
+        if do is None:
+            do = torch.zeros_like(v)
+        found = delta_attention_grad(_inner(do), q, k, v, g, beta, offsets, ctx.scale, s0,
+                                     None if dlast is None else dlast.contiguous(), ctx.needs_input_grad[:5])
+        return (*found[:5], None, None, found[5] if ctx.needs_input_grad[7] else None)
+
+
+def delta_attention(q, k, v, g, beta, offsets=None, scale=None, initial_state=None):
+    """(o, final state) with autograd support (delta_attention of the package); tokens outside
+    the sequences of `offsets` get no output."""
+    return DeltaAttention.apply(q, k, v, g, beta, offsets, scale, initial_state)
 
 
 class GatedFFN(torch.autograd.Function):

@@ -82,3 +82,43 @@ def bounds_forward(q, k, v, g, beta, scale, bounds, s0, o, last, kind):
             e_o[t] = abs(scale) * qn * (c * E + (0 if kind == "f32" else 2.0 ** -13) * (W + np.abs(v[t])))
         e_last[s] = (c * E)[:, None, :]
     return UNIT[kind] * (np.abs(o) + e_o) + e_o + TINY[kind], e_last + 1e-37
+
+
+def bounds_grad(do, q, k, v, g, beta, scale, bounds, s0, ds, grads, kind):
+    """Bounds on the gradients' errors, from lengths of the columns of S (W), of its gradient (Z) and of what a token writes,
+    and what the states are off by (E, F): backwards as forwards, a token adds at most a few hundred roundings of what there is."""
+    n, H, dv = v.shape
+    Hk, dk = q.shape[1:]
+    q = heads_of(q, H)
+    c = (dk + 1500) * F32
+    qn = np.sqrt((q ** 2).sum(2))[:, :, None]
+    do = np.abs(do)
+    W, E, Z, F = (np.zeros((n, H, dv)) for _ in range(4))
+    d0 = np.zeros((len(bounds) - 1, H, dv))
+    for s in range(len(bounds) - 1):
+        w = np.zeros((H, dv)) if s0 is None else np.sqrt((s0[s] ** 2).sum(1))
+        e = w.copy()
+        for t in range(bounds[s], bounds[s + 1]):
+            a, b = np.exp(g[t])[:, None], beta[t][:, None]
+            w0 = w
+            w = a * w + b * np.abs(v[t])
+            e = a * e + w + np.abs(v[t])
+            W[t], E[t] = np.maximum(w, a * w0) + np.abs(v[t]), e + w
+        z = np.zeros((H, dv)) if ds is None else np.sqrt((ds[s] ** 2).sum(1))
+        f = z.copy()
+        for t in range(bounds[s + 1] - 1, bounds[s] - 1, -1):
+            a = np.exp(g[t])[:, None]
+            z = z + abs(scale) * qn[t] * do[t]
+            f = f + z
+            Z[t], F[t] = z, f
+            z, f = a * z, a * f
+        d0[s] = f
+    # what two parts leave out, where the result has 16 bits
+    two = 0 if kind == "f32" else 2.0 ** -13
+    both = (4 * c * (F * W + Z * E) + two * Z * W).sum(2)
+    fold = lambda x: x.reshape(n, Hk, H // Hk).sum(2)[:, :, None]
+    of_q = fold((abs(scale) * do * (4 * c * E + two * W)).sum(2))
+    # dg adds up what up to 64 tokens pass on
+    off = (of_q, fold(2 * both), beta[:, :, None] * (4 * c * F + two * Z), 64 * both, both)
+    found = [UNIT[kind] * (np.abs(x) + y) + y + TINY[kind] for x, y in zip(grads, off)]
+    return found + [(4 * c * d0)[:, :, None, :] + 1e-37]

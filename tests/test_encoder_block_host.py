@@ -162,3 +162,63 @@ def test_linear_sizes_cover_every_cut(cuts, dtype):
     # the 8-bit form takes the tiles of half as long a sum of 16 bits
     eight = [cuts(1, rows, (n_in + 1) // 2, n_out) for rows, n_in, n_out in LINEAR_CUTS]
     assert {(a, b, s > 1) for a, b, s, *_ in eight} == {(256, 256, False), (256, 128, False), (128, 128, False), (128, 128, True)}
+
+
+def test_delta_refusals():
+    def shape(**kw):
+        return nd._DeltaShape(*{**dict(dtype=1, n_seq=2, n_tokens=8, heads=4, qk_heads=2, dk=8, dv=16, scale=1.0), **kw}.values())
+
+    h, none = nd._Heads(FAKE, 0, 64, 16), nd._Heads(None, 0, 0, 0)
+    far = nd._Heads(FAKE, 0, -1, 16)
+
+    def forward(s=None, q=h, v=h, g=h, o=h, off=FAKE, ws=FAKE, size=1 << 30):
+        return nd._delta(s or shape(), q, h, v, g, h, off, None, o, None, ws, size, None)
+
+    def gradient(s=None, do=h, dq=h, dg=h, off=FAKE, ws=FAKE, size=1 << 30):
+        return nd._delta_grad(s or shape(), h, h, h, h, h, off, None, do, None, dq, none, none, dg, none, None, ws, size, None)
+
+    for call in (forward, gradient):
+        for kw in (dict(dtype=3), dict(n_seq=-1), dict(heads=0), dict(qk_heads=3), dict(dk=0), dict(dv=0), dict(scale=float("nan")),
+                   dict(n_tokens=-1), dict(n_seq=0)):
+            assert call(shape(**kw)) == nd.E_ARG, kw
+        for kw in (dict(dk=257), dict(dv=257), dict(heads=1 << 16, qk_heads=1), dict(n_tokens=(1 << 30) + 1), dict(n_seq=1 << 24)):
+            assert call(shape(**kw)) == nd.E_UNSUPPORTED, kw
+        assert call(shape(n_tokens=9), off=None) == nd.E_ARG
+        assert call(size=100) == nd.E_NOMEM and call(ws=None) == nd.E_ARG
+        assert call(shape(n_seq=0, n_tokens=0)) == nd.OK
+        assert nd.last_error()
+    for kw in (dict(q=none), dict(v=far), dict(g=none), dict(o=none), dict(o=far)):
+        assert forward(**kw) == nd.E_ARG, kw
+    assert gradient(do=none) == nd.E_ARG and gradient(dq=far) == nd.E_ARG and gradient(dq=none, dg=none) == nd.OK
+
+    def step(s=None, q=h, o=h, state=FAKE, n=2, slots=None):
+        return nd._delta_step(s or shape(), q, h, h, h, h, state, n, slots, o, None)
+
+    assert step(q=none) == nd.E_ARG and step(o=far) == nd.E_ARG and step(state=None) == nd.E_ARG and step(n=1) == nd.E_ARG
+    assert step(shape(n_seq=0)) == nd.OK and step(shape(dk=300)) == nd.E_UNSUPPORTED and step(n=-1, slots=FAKE) == nd.E_ARG
+    n = nd._sz()
+    assert nd._delta_ws(shape(), 1, 0, ctypes.byref(n)) == nd.OK
+    less = n.value
+    assert nd._delta_ws(shape(), 1, 1, ctypes.byref(n)) == nd.OK and n.value > less
+    assert nd._delta_ws(shape(heads=65535, qk_heads=65535, n_seq=1, n_tokens=1 << 12, dk=256, dv=256), 0, 1, ctypes.byref(n)) == nd.OK
+    assert n.value > 1 << 40
+    assert nd._delta_ws(shape(heads=65535, qk_heads=65535, n_seq=1, n_tokens=1 << 13), 0, 1, ctypes.byref(n)) == nd.E_UNSUPPORTED
+    assert nd._delta_ws(shape(), 1, 1, None) == nd.E_ARG
+
+
+def test_reference_delta_gradient():
+    import delta_ref
+    rng = np.random.default_rng(3)
+    bounds, shapes = [0, 4, 4, 6], ((6, 1, 3), (6, 1, 3), (6, 2, 2), (6, 2), (6, 2), (3, 2, 3, 2))
+    args = [rng.normal(size=s) for s in shapes]
+    args[3], args[4] = -np.abs(args[3]), np.abs(args[4])
+    do, ds = rng.normal(size=(6, 2, 2)), rng.normal(size=shapes[5])
+
+    def loss(*x):
+        o, last, _, _ = delta_ref.attention(*x[:5], 0.7, bounds, x[5])
+        return (o * do).sum() + (last * ds).sum()
+
+    got = delta_ref.attention_grad(do, *args[:5], 0.7, bounds, args[5], ds)
+    for i in range(6):
+        want = differences(lambda v: loss(*args[:i], v, *args[i + 1:]), args[i])
+        np.testing.assert_allclose(got[i], want, atol=1e-6)
