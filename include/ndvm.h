@@ -581,8 +581,9 @@ ndvm_status ndvm_linear_attention_step(const ndvm_attention_shape *shape, const 
  * Sequences as for ndvm_linear_attention: of n_tokens / n_seq tokens each, or given by
  * `offsets`, with what is said there of offsets.  g and beta are given as the other
  * tensors are, with one value a head.
- * Limits: dk, dv <= 256, heads <= 65,535, n_tokens <= 2^30, and less than 2^24 pairs of
- * 32 tokens of a sequence and a head.
+ * Limits: dk, dv <= 256, heads <= 65,535, n_tokens <= 2^30, less than 2^24 pairs of
+ * 32 tokens of a sequence and a head, and tok_stride < 2^24 of q, k, v, o and their
+ * gradients (not of g, beta and the step's).
  */
 typedef struct {
     int dtype;

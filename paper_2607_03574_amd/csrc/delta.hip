@@ -7,8 +7,8 @@ namespace ndvm {
 namespace ops {
 namespace {
 
-template <class T, int DK, Walk WALK> __global__ void __launch_bounds__(256) delta_walk(DeltaArgs a) {
-    __shared__ __align__(16) char lds[kWalkLds<T, DK, WALK == kOutputs>];
+template <class T, int DK, Walk WALK> __global__ void __launch_bounds__(256, (kResident<T, DK>)) delta_walk(DeltaArgs a) {
+    __shared__ __align__(16) char lds[kWalkLds<T, DK, WALK == kOutputs, kRead<T, WALK>>];
     const uint32_t id = blockIdx.x / uint32_t(a.heads);
     const int64_t h = blockIdx.x - id * uint32_t(a.heads);
     const Piece g = find_piece(a, id, a.seg_len, !a.segments);
@@ -18,8 +18,9 @@ template <class T, int DK, Walk WALK> __global__ void __launch_bounds__(256) del
 }
 
 template <int DK> __global__ void __launch_bounds__(256) delta_carry(DeltaArgs a) {
+    __shared__ __align__(16) char lds[kCarryLds<DK>];
     const uint32_t seq = blockIdx.x / uint32_t(a.heads);
-    carry<DK, false>(a, seq, blockIdx.x - seq * uint32_t(a.heads), int64_t(blockIdx.y) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64));
+    carry<DK, false>(a, lds, seq, blockIdx.x - seq * uint32_t(a.heads), int64_t(blockIdx.y) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64));
 }
 
 // One token of every stream: S <- a S + k^T u, u = b (v - a k S), o = scale q S = scale (q (a S) + (q k) u).  Bound by the
@@ -106,17 +107,25 @@ template <class T, int X, int RG, bool PASSING> __global__ void __launch_bounds_
 }
 
 template <class T> size_t lay_out(DeltaArgs &a, Space s) {
+    a.dkp = padded(a.dk);
+    a.dvp = padded(a.dv);
     a.record = kRecord<T>;
+    if (a.dk % 8) {
+        s.take(a.k_rows, a.n_tokens * (a.heads / a.k.group) * a.dkp * int64_t(sizeof(T)));
+        s.take(a.q_rows, a.n_tokens * (a.heads / a.k.group) * a.dkp * int64_t(sizeof(T)));
+    }
     s.take(a.chunks, piece_ids(a, kDeltaChunk) * a.heads * a.record);
     if (cut(a)) {
         s.take(a.segments, a.n_segments * a.heads * a.dk * a.dv * 4);
-        s.take(a.moves, a.n_segments * a.heads * a.dk * a.dk * 4);
+        s.take(a.moves, a.n_segments * a.heads * a.dk * a.dkp * 4);
     }
     return s.used + 256;
 }
 
 template <class T> void delta(DeltaArgs a, hipStream_t stream) {
     lay_out<T>(a, Space(a.ws));
+    pad_rows<T>(a, a.k, a.k_rows, a.dk, stream);
+    pad_rows<T>(a, a.q, a.q_rows, a.dk, stream);
     const int64_t pairs = piece_ids(a, kDeltaChunk) * a.heads;
     if (a.n_tokens) delta_prepare<T, false><<<dim3(uint32_t(ceil_div(pairs, 4))), 256, 0, stream>>>(a, pairs);
     with_width(a.dk, [&](auto d) {

@@ -16,12 +16,12 @@ namespace ops {
 namespace {
 
 // z: 0 forwards, 1 backwards.
-template <class T, int DK, Walk WALK> __global__ void __launch_bounds__(256) delta_grad_walk(DeltaArgs a) {
-    __shared__ __align__(16) char lds[kWalkLds<T, DK, true>];
+template <class T, int DK, Walk WALK> __global__ void __launch_bounds__(256, (kResident<T, DK>)) delta_grad_walk(DeltaArgs a) {
+    __shared__ __align__(16) char lds[kWalkLds<T, DK, true, kReadBack>];
     const uint32_t id = blockIdx.x / uint32_t(a.heads);
     const int64_t h = blockIdx.x - id * uint32_t(a.heads), tile = int64_t(blockIdx.y) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const Piece g = find_piece(a, id, a.seg_len, !a.segments);
-    if (g.count == 0) return;
+    if (g.count == 0 || (blockIdx.z && blockIdx.y * 64 >= a.dv)) return;
     if (blockIdx.z == 0) {
         if (a.m || WALK == kSums) walk<T, DK, WALK>(a, lds, g, blockIdx.x, h, tile);
     } else {
@@ -30,12 +30,13 @@ template <class T, int DK, Walk WALK> __global__ void __launch_bounds__(256) del
 }
 
 template <int DK> __global__ void __launch_bounds__(256) delta_grad_carry(DeltaArgs a) {
+    __shared__ __align__(16) char lds[kCarryLds<DK>];
     const uint32_t seq = blockIdx.x / uint32_t(a.heads);
     const int64_t h = blockIdx.x - seq * uint32_t(a.heads), tile = int64_t(blockIdx.y) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     if (blockIdx.z == 0) {
-        if (a.m) carry<DK, false>(a, seq, h, tile);
+        if (a.m) carry<DK, false>(a, lds, seq, h, tile);
     } else {
-        carry<DK, true>(a, seq, h, tile);
+        carry<DK, true>(a, lds, seq, h, tile);
     }
 }
 
@@ -63,23 +64,25 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
     const bool has = w0 < DK;
     const auto width = [&](int n) { return NT == 1 ? w0 + lm : w0 + 32 * (n / 2) + 8 * (lm / 4) + 4 * (n % 2) + lm % 4; };
 
+    // (what is not there is read at another place, and is 0 when it is put)
     Eight<T> held[LOADS];
     const auto fetch_rows = [&](const Heads &x) __attribute__((always_inline)) {
         const T *p = at_token<T>(x, a, g, g.begin, h);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int at = i * 256 + threadIdx.x, row = at / G, gr = at % G;
-            held[i] = load_eight(p + row * x.tok + gr * 8, row < len ? a.dk - gr * 8 : 0);
+            get_eight(held[i], p, row < len && gr * 8 < a.dkp ? (uint32_t(row) * uint32_t(x.tok) + gr * 8) * sizeof(T) : 0);
         }
     };
     const auto put_rows = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int at = i * 256 + threadIdx.x, row = at / G, gr = at % G;
+            const bool in = row < len && gr * 8 < a.dkp;
             bf16x8 p[PARTS];
             parts_of(held[i], p);
 #pragma unroll
-            for (int q = 0; q < PARTS; ++q) *reinterpret_cast<bf16x8 *>(rows + q * ROWS + (row * G + (gr ^ turned<G>(row))) * 16) = p[q];
+            for (int q = 0; q < PARTS; ++q) *reinterpret_cast<bf16x8 *>(rows + q * ROWS + (row * G + (gr ^ turned<G>(row))) * 16) = in ? p[q] : bf16x8(bf16(0.0f));
         }
     };
     fetch_rows(a.q);
@@ -104,22 +107,24 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
 
     // over 32 columns of v after the other: do S^T, X S^T, U D^T, do U^T, X U^T, e.m and <D, S>
     const int srow = threadIdx.x / 4, sgr = threadIdx.x % 4;
-    const int64_t at_row = (h * a.n_tokens + g.first + g.begin + srow) * a.dv;
-    const T *const dop = at_token<T>(a.d_o, a, g, g.begin + srow, h);
+    const int64_t at_row = (h * a.n_tokens + g.first + g.begin) * a.dvp;
+    const T *const dop = at_token<T>(a.d_o, a, g, g.begin, h);
     const float beta = srow < len ? float(*at_token<T>(a.beta, a, g, g.begin + srow, h)) : 0.0f;
-    const float *const sp = a.states + (int64_t(id) * a.heads + h) * a.dk * a.dv, *const dp = a.d_states + (int64_t(id) * a.heads + h) * a.dk * a.dv;
+    const float *const sp = a.states + (int64_t(id) * a.heads + h) * a.dk * a.dvp, *const dp = a.d_states + (int64_t(id) * a.heads + h) * a.dk * a.dvp;
     Eight<float> m, e, S[NT], D[NT];
     Eight<T> o;
-    const auto fetch = [&](int64_t c) __attribute__((always_inline)) {
-        const int64_t have = srow < len ? a.dv - c - sgr * 8 : 0;
-        m = load_eight(a.m + at_row + c + sgr * 8, have);
-        e = load_eight(a.e + at_row + c + sgr * 8, have);
-        o = load_eight(dop + c + sgr * 8, have);
+    const int dvp = int(a.dvp);
+    const auto fetch = [&](int c) __attribute__((always_inline)) {
+        const bool in = srow < len && c + sgr * 8 < dvp;
+        const uint32_t off = in ? (uint32_t(srow) * uint32_t(dvp) + c + sgr * 8) * 4 : 0;
+        get_eight(m, a.m + at_row, off);
+        get_eight(e, a.e + at_row, off);
+        get_eight(o, dop, in ? (uint32_t(srow) * uint32_t(a.d_o.tok) + c + sgr * 8) * sizeof(T) : 0);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int64_t d = width(n), left = d < a.dk ? a.dv - c - 8 * lg : 0;
-            S[n] = load_eight(sp + d * a.dv + c + 8 * lg, left);
-            D[n] = load_eight(dp + d * a.dv + c + 8 * lg, left);
+            const uint32_t at = width(n) < a.dk && c + 8 * lg < dvp ? (uint32_t(width(n)) * uint32_t(dvp) + c + 8 * lg) * 4 : 0;
+            get_eight(S[n], sp, at);
+            get_eight(D[n], dp, at);
         }
     };
     f32x4 a1[4][NT], a2[4][NT], a3[4][NT], pd[4], ad[4];
@@ -132,13 +137,14 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
     float db = 0.0f, ds = 0.0f;
     char *const of_u = area, *const of_x = area + HELD * SLAB, *const of_o = area + 2 * HELD * SLAB;
     fetch(0);
-    for (int64_t c = 0; c < a.dv; c += 32) {
+    for (int c = 0; c < dvp; c += 32) {
         __syncthreads();
         {
+            const bool in = srow < len && c + sgr * 8 < dvp;
             bf16x8 u[HELD], x[HELD], p[PARTS];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float mi = value(m, i), ei = value(e, i);
+                const float mi = in ? value(m, i) : 0.0f, ei = in ? value(e, i) : 0.0f;
                 db += ei * mi;
                 split(beta * mi, u, i);
                 split(beta * ei, x, i);
@@ -151,18 +157,24 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
                 *reinterpret_cast<bf16x8 *>(of_x + q * SLAB + at) = x[q];
             }
 #pragma unroll
-            for (int q = 0; q < PARTS; ++q) *reinterpret_cast<bf16x8 *>(of_o + q * SLAB + at) = p[q];
+            for (int q = 0; q < PARTS; ++q) *reinterpret_cast<bf16x8 *>(of_o + q * SLAB + at) = in ? p[q] : bf16x8(bf16(0.0f));
         }
         bf16x8 s[NT][HELD], d[NT][HELD];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
+            const bool in = width(n) < a.dk && c + 8 * lg < dvp;
+            float sd = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) ds += value(S[n], i) * value(D[n], i);
+            for (int i = 0; i < 8; ++i) sd += value(S[n], i) * value(D[n], i);
+            ds += in ? sd : 0.0f;
             parts_of(S[n], s[n]);
             parts_of(D[n], d[n]);
+#pragma unroll
+            for (int q = 0; q < HELD; ++q)
+                if (!in) s[n][q] = d[n][q] = bf16x8(bf16(0.0f));
         }
         __syncthreads();
-        if (c + 32 < a.dv) fetch(c + 32);
+        if (c + 32 < dvp) fetch(c + 32);
         const auto operand = [&](const char *from, int tile, auto &x) __attribute__((always_inline)) {
             const int row = 16 * tile + lm;
             constexpr int N = sizeof(x) / sizeof(bf16x8);
@@ -345,11 +357,17 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
             for (int q = 0; q < PARTS; ++q) x[q] = *reinterpret_cast<const bf16x8 *>(rows + q * ROWS + (row * G + ((4 * ks + lg) ^ turned<G>(row))) * 16);
         };
         const int row = 16 * wave + lm;
-        const T *const qp = at_token<T>(a.q, a, g, g.begin + row, h);
+        const T *const qp = at_token<T>(a.q, a, g, g.begin, h);
 #pragma unroll
         for (int ks = 0; ks < DK / 32; ++ks) {
             bf16x8 q[PARTS], k[PARTS];
-            parts_of(load_eight(qp + ks * 32 + 8 * lg, row < len ? a.dk - ks * 32 - 8 * lg : 0), q);
+            const bool in = row < len && ks * 32 + 8 * lg < a.dkp;
+            Eight<T> eight;
+            get_eight(eight, qp, in ? (uint32_t(row) * uint32_t(a.q.tok) + ks * 32 + 8 * lg) * sizeof(T) : 0);
+            parts_of(eight, q);
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i)
+                if (!in) q[i] = bf16x8(bf16(0.0f));
             operand(wave, ks, k);
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
@@ -453,21 +471,28 @@ template <class T> __global__ void __launch_bounds__(256) delta_fold(DeltaArgs a
 // need: whether anything but dv and the initial state's gradient is wanted
 template <class T> size_t lay_out(DeltaArgs &a, Space s, bool need) {
     const int64_t states = a.heads * a.dk * a.dv * 4;
+    a.dkp = padded(a.dk);
+    a.dvp = padded(a.dv);
     a.record = kRecordGrad;
+    if (a.dk % 8) {
+        s.take(a.k_rows, a.n_tokens * (a.heads / a.k.group) * a.dkp * int64_t(sizeof(T)));
+        s.take(a.q_rows, a.n_tokens * (a.heads / a.k.group) * a.dkp * int64_t(sizeof(T)));
+    }
+    if (a.dv % 8) s.take(a.d_rows, a.n_tokens * a.heads * a.dvp * int64_t(sizeof(T)));
     s.take(a.chunks, piece_ids(a, kDeltaChunk) * a.heads * a.record);
     if (cut(a)) {
         s.take(a.segments, a.n_segments * states);
         s.take(a.d_segments, a.n_segments * states);
-        s.take(a.moves, a.n_segments * a.heads * a.dk * a.dk * 4);
-        s.take(a.moves_t, a.n_segments * a.heads * a.dk * a.dk * 4);
+        s.take(a.moves, a.n_segments * a.heads * a.dk * a.dkp * 4);
+        s.take(a.moves_t, a.n_segments * a.heads * a.dk * a.dkp * 4);
     }
     if (!need) return s.used + 256;
     const int64_t blocks = piece_ids(a, kDeltaBlock);
-    s.take(a.states, blocks * states);
-    s.take(a.d_states, blocks * states);
-    s.take(a.m, a.heads * a.n_tokens * a.dv * 4);
-    s.take(a.e, a.heads * a.n_tokens * a.dv * 4);
-    if (a.q.group > 1) {
+    s.take(a.states, blocks * a.heads * a.dk * a.dvp * 4);
+    s.take(a.d_states, blocks * a.heads * a.dk * a.dvp * 4);
+    s.take(a.m, a.heads * a.n_tokens * a.dvp * 4);
+    s.take(a.e, a.heads * a.n_tokens * a.dvp * 4);
+    if (a.k.group > 1) {
         s.take(a.dq_part, a.heads * a.n_tokens * a.dk * 4);
         s.take(a.dk_part, a.heads * a.n_tokens * a.dk * 4);
     }
@@ -477,6 +502,9 @@ template <class T> size_t lay_out(DeltaArgs &a, Space s, bool need) {
 template <class T> void delta_grad(DeltaArgs a, hipStream_t stream) {
     const bool need = a.dq.p || a.dk_out.p || a.dg.p || a.dbeta.p;
     lay_out<T>(a, Space(a.ws), need);
+    pad_rows<T>(a, a.k, a.k_rows, a.dk, stream);
+    pad_rows<T>(a, a.q, a.q_rows, a.dk, stream);
+    pad_rows<T>(a, a.d_o, a.d_rows, a.dv, stream);
     const int64_t pairs = piece_ids(a, kDeltaChunk) * a.heads;
     if (a.n_tokens) delta_prepare<T, true><<<dim3(uint32_t(ceil_div(pairs, 4))), 256, 0, stream>>>(a, pairs);
     with_width(a.dk, [&](auto d) {
@@ -492,7 +520,7 @@ template <class T> void delta_grad(DeltaArgs a, hipStream_t stream) {
     });
     if (a.dq_part && (a.dq.p || a.dk_out.p) && a.n_tokens) {
         const int64_t groups = std::min(ceil_div(a.n_tokens * a.dk, 256), kMostGroups);
-        delta_fold<T><<<dim3(uint32_t(groups), uint32_t(a.heads / a.q.group), 2), 256, 0, stream>>>(a);
+        delta_fold<T><<<dim3(uint32_t(groups), uint32_t(a.heads / a.k.group), 2), 256, 0, stream>>>(a);
     }
 }
 

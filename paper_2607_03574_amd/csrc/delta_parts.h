@@ -70,15 +70,6 @@ template <int ORDER, int NX, int NY> __device__ inline f32x4 multiply(const bf16
 template <class T> struct Eight {
     vec<T> v[8 / kVec<T>];
 };
-template <class T> __device__ inline Eight<T> load_eight(const T *p, int64_t count) {
-    Eight<T> e;
-#pragma unroll
-    for (int i = 0; i < 8 / kVec<T>; ++i) {
-        e.v[i] = T(0.0f);
-        if (count > i * kVec<T>) e.v[i] = load_vec(p + i * kVec<T>, count - i * kVec<T>);
-    }
-    return e;
-}
 template <class T> __device__ inline float value(const Eight<T> &e, int i) { return float(e.v[i / kVec<T>][i % kVec<T>]); }
 template <class T, int N> __device__ inline void parts_of(const Eight<T> &e, bf16x8 (&to)[N]) {
     if constexpr (std::is_same<T, bf16>::value && N == 1) {
@@ -87,6 +78,21 @@ template <class T, int N> __device__ inline void parts_of(const Eight<T> &e, bf1
 #pragma unroll
         for (int i = 0; i < 8; ++i) split(value(e, i), to, i);
     }
+}
+// Where a lane's value lies: bytes behind an address that is the same for the wave.
+#ifdef __HIP_DEVICE_COMPILE__
+#define GLOBAL __attribute__((address_space(1)))
+#else
+#define GLOBAL
+#endif
+template <class V> __device__ inline V get(const void *base, uint32_t off) {
+    return *(const GLOBAL V *)((const GLOBAL char *)base + off);
+}
+template <class V> __device__ inline void set(void *base, uint32_t off, V v) { *(GLOBAL V *)((GLOBAL char *)base + off) = v; }
+#undef GLOBAL
+template <class T> __device__ inline void get_eight(Eight<T> &e, const void *base, uint32_t off) {
+#pragma unroll
+    for (int i = 0; i < 8 / kVec<T>; ++i) e.v[i] = get<vec<T>>(base, off + i * 16);
 }
 __device__ inline bool finite(float v) { return fabsf(v) <= 3.402823466e38f; }
 
@@ -201,19 +207,41 @@ template <class T, bool GRAD> __global__ void __launch_bounds__(256) delta_prepa
 #pragma unroll
     for (int i = 0; i < 3; ++i) kk[i] = qk[i] = 0;
     bool odd[2] = {false, false};
-    for (int64_t c = 8 * lg; c < (a.dk + 31) / 32 * 32; c += 32) {
+    const T *kp = at_token<T>(a.k, a, g, g.begin, h), *qp = at_token<T>(a.q, a, g, g.begin, h);
+    const int most = int(a.dkp);
+    uint32_t k_at[2], q_at[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const uint32_t row = min(16 * t + lm, len - 1);
+        k_at[t] = (row * uint32_t(a.k.tok) + 8 * lg) * sizeof(T);
+        q_at[t] = (row * uint32_t(a.q.tok) + 8 * lg) * sizeof(T);
+    }
+    // (rows and widths that are not there are read at others' places, and are 0 when they are used)
+    Eight<T> e[2], f[2];
+    const auto fetch = [&](int c) __attribute__((always_inline)) {
+        const uint32_t off = c + 8 * lg < most ? c * sizeof(T) : 0, back = 8 * lg < most ? 0 : 8 * lg * sizeof(T);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            get_eight(e[t], kp, k_at[t] + off - back);
+            get_eight(f[t], qp, q_at[t] + off - back);
+        }
+    };
+    fetch(0);
+    for (int c = 0; c < most; c += 32) {
         bf16x8 k[2][PARTS], q[2][PARTS];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int row = 16 * t + lm;
-            const int64_t have = row < len ? a.dk - c : 0;
-            const Eight<T> e = load_eight(at_token<T>(a.k, a, g, g.begin + row, h) + c, have);
-            const Eight<T> f = load_eight(at_token<T>(a.q, a, g, g.begin + row, h) + c, have);
+            const bool in = 16 * t + lm < len && c + 8 * lg < most;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) odd[t] |= !finite(value(e, i));
-            parts_of(e, k[t]);
-            parts_of(f, q[t]);
+            for (int i = 0; i < 8; ++i) odd[t] |= in && !finite(value(e[t], i));
+            parts_of(e[t], k[t]);
+            parts_of(f[t], q[t]);
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i) {
+                if (!in) k[t][i] = q[t][i] = bf16x8(bf16(0.0f));
+            }
         }
+        if (c + 32 < most) fetch(c + 32);
         kk[0] = multiply<2>(k[0], k[0], kk[0]);
         kk[1] = multiply<2>(k[1], k[0], kk[1]);
         kk[2] = multiply<2>(k[1], k[1], kk[2]);
@@ -331,6 +359,28 @@ template <class T, bool GRAD> __global__ void __launch_bounds__(256) delta_prepa
 // one instruction reads, along them or (transposed) four of them across, are in different banks
 template <int G> __device__ inline int turned(int r) {
     return G >= 16 ? r % 4 * 4 + r / 4 % 4 : G == 8 ? r / 2 % 2 * 4 + r / 4 % 4 : r / 4 % 4;
+}
+
+// Rows of heads with zeros behind them, up to `pad` values: what follows reads eight values of a row at a time, and q, k and
+// do of widths that are no multiple of eight go through here first.
+template <class T> __global__ void __launch_bounds__(256) delta_pad(DeltaArgs a, Heads from, T *to, int64_t heads, int64_t width, int64_t pad) {
+    const int64_t per = a.n_tokens / a.n_seq, n = a.n_tokens * heads * pad;
+    for (int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x; at < n; at += int64_t(gridDim.x) * 256) {
+        const int64_t c = at % pad, h = at / pad % heads, t = at / pad / heads;
+        const int64_t row = a.offsets ? t * from.tok : t / per * from.seq + t % per * from.tok;
+        to[at] = c < width ? static_cast<const T *>(from.p)[row + h * from.head + c] : T(0.0f);
+    }
+}
+inline int64_t padded(int64_t width) { return (width + 7) / 8 * 8; }
+// `from` or, where its width is no multiple of eight, its copy.
+template <class T> void pad_rows(const DeltaArgs &a, Heads &from, void *copy, int64_t width, hipStream_t stream) {
+    if (width % 8 == 0 || a.n_tokens == 0) return;
+    const int64_t heads = a.heads / from.group, pad = padded(width);
+    delta_pad<T><<<dim3(uint32_t(std::min(ceil_div(a.n_tokens * heads * pad, 256), int64_t(16384)))), 256, 0, stream>>>(a, from, static_cast<T *>(copy), heads, width, pad);
+    from.p = copy;
+    from.head = pad;
+    from.tok = heads * pad;
+    from.seq = a.n_tokens / a.n_seq * from.tok;
 }
 
 template <class F> void with_width(int64_t dk, F f) {

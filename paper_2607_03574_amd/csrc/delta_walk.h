@@ -13,31 +13,57 @@ namespace {
 // or what a segment adds to a state of 0, and what it makes of other states.
 enum Walk { kOutputs, kKept, kSums };
 
-// Bytes of a chunk's rows of k (or q) in LDS, and how many chunks are there at once.
+// Bytes of a chunk's rows of k (or q) in LDS; how many chunks are there at once; and bytes of a record, as far as a walk reads it.
 template <class T, int DK> constexpr int kRows = kInputParts<T> * 32 * DK * 2;
 template <class T, int DK> constexpr int kBuffers = 4 * kRows<T, DK> <= 131072 ? 2 : 1;
-template <class T, int DK, bool BOTH> constexpr int kWalkLds = kBuffers<T, DK> * kRows<T, DK> * (BOTH ? 2 : 1);
+template <class T, Walk WALK> constexpr int kRead = WALK == kOutputs ? kRecord<T> : kRecordHead + kRecordMatrix;
+constexpr int kReadBack = kRecordHead + 2 * kRecordMatrix;
+template <class T, int DK, bool BOTH, int READ> constexpr int kWalkLds = kBuffers<T, DK> * (kRows<T, DK> * (BOTH ? 2 : 1) + READ);
+// workgroups on a compute unit: as many as their LDS leaves room for
+template <class T, int DK> constexpr int kResident = kInputParts<T> * DK < 256 ? 2 : 1;
 
 // The workgroup's way of the rows of a chunk into LDS.
 template <class T, int DK> struct Stage {
     static constexpr int G = DK / 8, PARTS = kInputParts<T>, PART = 32 * G * 16, LOADS = 32 * G > 256 ? 32 * G / 256 : 1;
     Eight<T> held[LOADS];
-    __device__ inline void fetch(const T *rows, int64_t step, int left, int64_t dk) {
+    // what is not there is read at the first row's place, and is 0 when it is put
+    __device__ inline void fetch(const T *rows, uint32_t step, int left, int dkp) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int at = i * 256 + threadIdx.x, row = at / G, gr = at % G;
-            held[i] = load_eight(rows + row * step + gr * 8, row < left ? dk - gr * 8 : 0);
+            get_eight(held[i], rows, row < left && gr * 8 < dkp ? (uint32_t(row) * step + gr * 8) * sizeof(T) : 0);
         }
     }
-    __device__ inline void put(char *to) const {
+    // (a chunk later: what touched the values before would wait for them)
+    __device__ inline void put(char *to, int left, int dkp) const {
         if (32 * G < 256 && int(threadIdx.x) >= 32 * G) return;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int at = i * 256 + threadIdx.x, row = at / G, gr = at % G;
             bf16x8 p[PARTS];
             parts_of(held[i], p);
+            const bool in = row < left && gr * 8 < dkp;
 #pragma unroll
-            for (int q = 0; q < PARTS; ++q) *reinterpret_cast<bf16x8 *>(to + q * PART + (row * G + (gr ^ turned<G>(row))) * 16) = p[q];
+            for (int q = 0; q < PARTS; ++q) *reinterpret_cast<bf16x8 *>(to + q * PART + (row * G + (gr ^ turned<G>(row))) * 16) = in ? p[q] : bf16x8(bf16(0.0f));
+        }
+    }
+};
+// And of a record: its first FIRST bytes, and those behind a gap.
+template <int READ, int FIRST, int GAP> struct StageRecord {
+    static constexpr int LOADS = (READ / 16 + 255) / 256;
+    f32x4 held[LOADS];
+    __device__ inline void fetch(const char *record) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const uint32_t at = min(uint32_t(i * 256 + threadIdx.x) * 16, uint32_t(READ - 16));
+            held[i] = get<f32x4>(record, at < uint32_t(FIRST) ? at : at + GAP);
+        }
+    }
+    __device__ inline void put(char *to) const {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int at = (i * 256 + threadIdx.x) * 16;
+            if (at < READ) *reinterpret_cast<f32x4 *>(to + at) = held[i];
         }
     }
 };
@@ -80,12 +106,21 @@ template <int DK> struct State {
     __device__ inline void fill(float v) {
         each([&](f32x4 &x, int r, int) { x[r] = v; });
     }
-    __device__ inline void load(const float *from, int64_t dk, int64_t cols, int64_t col) {
-        each([&](f32x4 &x, int r, int d) { x[r] = d < dk && col < cols ? from[d * cols + col] : 0.0f; });
+    // col0: the first of the wave's 16 columns; rows are `step` values apart
+    __device__ inline void load(const float *from, int64_t dk, int64_t cols, int64_t step, int64_t col0) {
+        const int lm = threadIdx.x % 16;
+        const bool in = col0 + lm < cols;
+        each([&](f32x4 &x, int r, int d) { x[r] = get<float>(from + col0, in && d < dk ? (uint32_t(d) * uint32_t(step) + lm) * 4 : 0); });
+        if (dk < DK || col0 + 16 > cols)
+            each([&](f32x4 &x, int r, int d) { x[r] = in && d < dk ? x[r] : 0.0f; });
     }
-    __device__ inline void store(float *to, int64_t dk, int64_t cols, int64_t col) {
+    // (columns from `cols` to `step` are 0)
+    __device__ inline void store(float *to, int64_t dk, int64_t cols, int64_t step, int64_t col0) {
+        const int lm = threadIdx.x % 16;
+        if (col0 + lm >= step) return;
+        const bool in = col0 + lm < cols;
         each([&](f32x4 &x, int r, int d) {
-            if (d < dk && col < cols) to[d * cols + col] = x[r];
+            if (dk == DK || d < dk) set<float>(to + col0, (uint32_t(d) * uint32_t(step) + lm) * 4, in ? x[r] : 0.0f);
         });
     }
 #ifdef __HIP_DEVICE_COMPILE__
@@ -102,12 +137,12 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int PARTS = kInputParts<T>, HELD = kResultParts<T>, SP = kStateParts, KS = DK / 32, BUFFERS = kBuffers<T, DK>;
     constexpr bool OUT = WALK == kOutputs;
-    constexpr int MATRIX = kRows<T, DK>;
+    constexpr int MATRIX = kRows<T, DK>, READ = kRead<T, WALK>, SLOT = MATRIX * (OUT ? 2 : 1) + READ;
     const int l = threadIdx.x % 64, lm = l % 16, lg = l / 16;
     const int64_t tiles = ceil_div(a.dv, 16);
     const bool moves = WALK == kSums && tile >= tiles;
-    const int64_t cols = moves ? a.dk : a.dv, col = (moves ? tile - tiles : tile) * 16 + lm;
-    const bool works = col - lm < cols;
+    const int64_t cols = moves ? a.dk : a.dv, col0 = (moves ? tile - tiles : tile) * 16, col = col0 + lm;
+    const bool works = col0 < cols;
     const auto token_of = [&](int e) { return 16 * (e / 4) + 4 * lg + e % 4; };
     const int64_t chunk0 = first_piece(a, g.seq, kDeltaChunk) + g.begin / kDeltaChunk;
     const int chunks = int((g.len + 31) / 32);
@@ -116,80 +151,65 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const
 
     State<DK> S;
     if (WALK == kSums) S.each([&](f32x4 &x, int r, int d) { x[r] = moves && d == col ? 1.0f : 0.0f; });
-    else if (a.segments) S.load(a.segments + slot * states, a.dk, a.dv, col);
-    else if (a.state_in) S.load(a.state_in + (g.seq * a.heads + h) * states, a.dk, a.dv, col);
+    else if (!works) S.fill(0.0f);
+    else if (a.segments) S.load(a.segments + slot * states, a.dk, a.dv, a.dv, col0);
+    else if (a.state_in) S.load(a.state_in + (g.seq * a.heads + h) * states, a.dk, a.dv, a.dv, col0);
     else S.fill(0.0f);
 
     const T *kp = at_token<T>(a.k, a, g, g.begin, h), *qp = OUT ? at_token<T>(a.q, a, g, g.begin, h) : nullptr;
-    const T *vp = at_token<T>(a.v, a, g, g.begin, h) + col;
-    T *op = OUT ? const_cast<T *>(at_token<T>(a.o, a, g, g.begin, h)) + col : nullptr;
-    float *mp = WALK == kKept ? a.m + (h * a.n_tokens + g.first + g.begin) * a.dv + col : nullptr;
+    const T *vp = at_token<T>(a.v, a, g, g.begin, h) + (moves ? 0 : col0);
+    T *op = OUT ? const_cast<T *>(at_token<T>(a.o, a, g, g.begin, h)) + col0 : nullptr;
+    float *mp = WALK == kKept ? a.m + (h * a.n_tokens + g.first + g.begin) * a.dvp + col0 : nullptr;
+    const uint32_t v_tok = uint32_t(a.v.tok), o_tok = uint32_t(a.o.tok), column = uint32_t(min(int64_t(lm), max(cols - 1 - col0, int64_t(0))));
     Stage<T, DK> rk, rq;
-    struct Small {
-        bf16x8 t[2][SP], p[OUT ? 2 : 1][OUT ? HELD : 1];
-        f32x4 beta[2], rise[2], fall[2];
-        float whole;
-        int bad;
-        T v[8];
-    };
-    const auto fetch_small = [&](int c, Small &s) __attribute__((always_inline)) {
-        const char *record = a.chunks + ((chunk0 + c) * a.heads + h) * a.record;
-        const RecordHead *head = reinterpret_cast<const RecordHead *>(record);
-        const char *t = record + kRecordHead + l * 16, *p = t + kRecordMatrix;
+    StageRecord<READ, READ, 0> record;
+    T v_next[8];
+    uint32_t v_at[8];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-#pragma unroll
-            for (int q = 0; q < SP; ++q) s.t[i][q] = *reinterpret_cast<const bf16x8 *>(t + (i * SP + q) * kTile);
-            if constexpr (OUT)
-#pragma unroll
-                for (int q = 0; q < HELD; ++q) s.p[i][q] = *reinterpret_cast<const bf16x8 *>(p + (i * HELD + q) * kTile);
-            const int row = 16 * i + 4 * lg;
-            s.beta[i] = *reinterpret_cast<const f32x4 *>(head->beta + row);
-            s.rise[i] = *reinterpret_cast<const f32x4 *>(head->rise + row);
-            s.fall[i] = *reinterpret_cast<const f32x4 *>(head->fall + row);
-        }
-        s.whole = head->whole;
-        s.bad = head->bad;
+    for (int e = 0; e < 8; ++e) v_at[e] = (token_of(e) * v_tok + column) * sizeof(T);
+    // values of v: of columns and tokens that are not there, those of the last ones; they reach nothing
+    const auto fetch = [&](int c) __attribute__((always_inline)) {
         const int left = left_of(c);
-        const bool there = !moves && col < cols;
+        record.fetch(a.chunks + ((chunk0 + c) * a.heads + h) * a.record);
+        rk.fetch(kp + int64_t(c) * 32 * a.k.tok, uint32_t(a.k.tok), left, int(a.dkp));
+        if constexpr (OUT) rq.fetch(qp + int64_t(c) * 32 * a.q.tok, uint32_t(a.q.tok), left, int(a.dkp));
+        const T *v = vp + int64_t(c) * 32 * a.v.tok;
+        if (moves || !works)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            s.v[e] = T(0.0f);
-            if (there && token_of(e) < left) s.v[e] = vp[(int64_t(c) * 32 + token_of(e)) * a.v.tok];
-        }
+            for (int e = 0; e < 8; ++e) v_next[e] = T(0.0f);
+        else
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v_next[e] = get<T>(v, min(v_at[e], (uint32_t(left - 1) * v_tok + column) * uint32_t(sizeof(T))));
     };
-    const auto fetch_rows = [&](int c) __attribute__((always_inline)) {
-        rk.fetch(kp + int64_t(c) * 32 * a.k.tok, a.k.tok, left_of(c), a.dk);
-        if constexpr (OUT) rq.fetch(qp + int64_t(c) * 32 * a.q.tok, a.q.tok, left_of(c), a.dk);
-    };
-    const auto put_rows = [&](int c) __attribute__((always_inline)) {
-        char *to = lds + c % BUFFERS * MATRIX * (OUT ? 2 : 1);
-        rk.put(to);
-        if constexpr (OUT) rq.put(to + MATRIX);
+    const auto put = [&](int c) __attribute__((always_inline)) {
+        char *to = lds + c % BUFFERS * SLOT;
+        rk.put(to, left_of(c), int(a.dkp));
+        if constexpr (OUT) rq.put(to + MATRIX, left_of(c), int(a.dkp));
+        record.put(to + SLOT - READ);
     };
 
-    Small cur;
+    T v_now[8];
     if (chunks) {
-        fetch_rows(0);
-        fetch_small(0, cur);
-        put_rows(0);
+        fetch(0);
+        put(0);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v_now[e] = v_next[e];
     }
     __syncthreads();
     for (int c = 0; c < chunks; ++c) {
-        const char *k = lds + c % BUFFERS * MATRIX * (OUT ? 2 : 1), *q = k + MATRIX;
+        const char *k = lds + c % BUFFERS * SLOT, *q = k + MATRIX, *matrices = k + SLOT - READ + kRecordHead + l * 16;
+        const RecordHead *head = reinterpret_cast<const RecordHead *>(k + SLOT - READ);
         const int left = left_of(c);
-        Small next;
-        if (c + 1 < chunks) {
-            fetch_rows(c + 1);
-            fetch_small(c + 1, next);
-        }
+        if (c + 1 < chunks) fetch(c + 1);
+        f32x4 o[2];
+        int first = 32;
         if (works) {
             if (WALK == kKept && c % 2 == 0) {
                 const int64_t block = first_piece(a, g.seq, kDeltaBlock) + (g.begin + int64_t(c) * 32) / kDeltaBlock;
-                S.store(a.states + (block * a.heads + h) * states, a.dk, a.dv, col);
+                S.store(a.states + (block * a.heads + h) * a.dk * a.dvp, a.dk, a.dv, a.dvp, col0);
             }
             // Y = K S, Z = Q S
-            f32x4 y[2], z[2];
+            f32x4 y[2], z[2], beta[2], rise[2], fall[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) y[i] = z[i] = 0;
 #pragma unroll
@@ -206,13 +226,21 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const
                     }
                 }
             }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                beta[i] = *reinterpret_cast<const f32x4 *>(head->beta + 16 * i + 4 * lg);
+                rise[i] = *reinterpret_cast<const f32x4 *>(head->rise + 16 * i + 4 * lg);
+                fall[i] = *reinterpret_cast<const f32x4 *>(head->fall + 16 * i + 4 * lg);
+            }
+            const float whole = head->whole;
+            const int bad = head->bad, fit = min(bad, left);
             // a value of v that is not finite counts as 0; what follows it in its column is set below
-            int first = cur.bad;
+            first = bad;
             float v[8];
             bool odd = false;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                v[e] = float(cur.v[e]);
+                v[e] = float(v_now[e]);
                 odd |= !finite(v[e]);
             }
             if (__ballot(odd)) {
@@ -228,17 +256,20 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const
             // X, M and U
             bf16x8 x[SP], w[SP], u[HELD];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) split(token_of(e) < cur.bad ? v[e] - cur.rise[e / 4][e % 4] * y[e / 4][e % 4] : 0.0f, x, e);
+            for (int e = 0; e < 8; ++e) split(token_of(e) < fit ? v[e] - rise[e / 4][e % 4] * y[e / 4][e % 4] : 0.0f, x, e);
             f32x4 m[2];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) m[i] = multiply<SP - 1>(cur.t[i], x, f32x4{0, 0, 0, 0});
+            for (int i = 0; i < 2; ++i) {
+                bf16x8 t[SP];
+#pragma unroll
+                for (int p = 0; p < SP; ++p) t[p] = *reinterpret_cast<const bf16x8 *>(matrices + (i * SP + p) * kTile);
+                m[i] = multiply<SP - 1>(t, x, f32x4{0, 0, 0, 0});
+            }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float ue = cur.beta[e / 4][e % 4] * m[e / 4][e % 4];
-                split(ue * cur.fall[e / 4][e % 4], w, e);
+                const float ue = beta[e / 4][e % 4] * m[e / 4][e % 4];
+                split(ue * fall[e / 4][e % 4], w, e);
                 if constexpr (OUT) split(ue, u, e);
-                if (WALK == kKept && token_of(e) < left && col < cols)
-                    mp[(int64_t(c) * 32 + token_of(e)) * a.dv] = token_of(e) < first ? m[e / 4][e % 4] : __builtin_nanf("");
             }
             // S' = exp(G_last) S + K^T (fall U)
 #pragma unroll
@@ -247,36 +278,58 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const
                 for (int t = 0; t < 2; ++t) {
                     bf16x8 kt[PARTS];
                     widths_operand<T, DK>(k, ks, t, kt);
-                    S.s[ks][t] = multiply<SP - 1>(kt, w, S.s[ks][t] * cur.whole);
+                    S.s[ks][t] = multiply<SP - 1>(kt, w, S.s[ks][t] * whole);
                 }
-            if constexpr (OUT) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const f32x4 o = multiply<HELD - 1>(cur.p[i], u, cur.rise[i] * z[i]);
+            for (int i = 0; i < 2; ++i) {
+                if constexpr (OUT) {
+                    bf16x8 p[HELD];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int token = token_of(4 * i + r);
-                        if (token < left && col < cols)
-                            op[(int64_t(c) * 32 + token) * a.o.tok] = T(token < first ? o[r] * a.scale : __builtin_nanf(""));
-                    }
+                    for (int j = 0; j < HELD; ++j) p[j] = *reinterpret_cast<const bf16x8 *>(matrices + kRecordMatrix + (i * HELD + j) * kTile);
+                    o[i] = multiply<HELD - 1>(p, u, rise[i] * z[i]) * a.scale;
+                } else {
+                    o[i] = m[i];
                 }
             }
             // a column with a value that is not finite, or a head with a key or gate that is not, has none from there on
-            if (first < left) S.fill(__builtin_nanf(""));
+            if (__ballot(first < left))
+                S.each([&](f32x4 &x, int r, int) {
+                    if (first < left) x[r] = __builtin_nanf("");
+                });
         }
         if (BUFFERS == 1) __syncthreads();
-        if (c + 1 < chunks) put_rows(c + 1);
+        if (c + 1 < chunks) {
+            put(c + 1);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v_now[e] = v_next[e];
+        }
+        if (WALK != kSums && works && col < (OUT ? a.dv : a.dvp)) {      // (behind the wait for what the next chunk brings)
+            if (__ballot(first < left))
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e / 4][e % 4] = token_of(e) < first ? o[e / 4][e % 4] : __builtin_nanf("");
+            const auto store = [&](int e) __attribute__((always_inline)) {
+                const uint32_t token = uint32_t(token_of(e));
+                if constexpr (OUT) set<T>(op + int64_t(c) * 32 * a.o.tok, (token * o_tok + lm) * sizeof(T), T(o[e / 4][e % 4]));
+                else set<float>(mp + int64_t(c) * 32 * a.dvp, (token * uint32_t(a.dvp) + lm) * 4, col < a.dv ? o[e / 4][e % 4] : 0.0f);
+            };
+            if (left == 32)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) store(e);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (token_of(e) < left) store(e);
+        }
         __syncthreads();
-        cur = next;
     }
     if (!works) return;
-    if (OUT && a.state_out && g.index == g.count - 1) S.store(a.state_out + (g.seq * a.heads + h) * states, a.dk, a.dv, col);
-    if (WALK == kSums && !moves) S.store(a.segments + slot * states, a.dk, a.dv, col);
+    if (OUT && a.state_out && g.index == g.count - 1) S.store(a.state_out + (g.seq * a.heads + h) * states, a.dk, a.dv, a.dv, col0);
+    if (WALK == kSums && !moves) S.store(a.segments + slot * states, a.dk, a.dv, a.dv, col0);
     if (WALK == kSums && moves) {
-        S.store(a.moves + slot * a.dk * a.dk, a.dk, a.dk, col);
-        if (a.moves_t)
+        S.store(a.moves + slot * a.dk * a.dkp, a.dk, a.dk, a.dkp, col0);
+        if (a.moves_t)      // (rows from dk on are 0)
             S.each([&](f32x4 &x, int r, int d) {
-                if (d < a.dk && col < cols) a.moves_t[(slot * a.dk + col) * a.dk + d] = x[r];
+                if (d < a.dkp && col < cols) set<float>(a.moves_t + (slot * a.dk + col0) * a.dkp, (uint32_t(lm) * uint32_t(a.dkp) + d) * 4, d < a.dk ? x[r] : 0.0f);
             });
     }
 #endif
@@ -285,10 +338,11 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const
 // Backwards: the gradient of the state, from the piece's end to its beginning; e and the gradient of v.
 template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk_back(const DeltaArgs &a, char *lds, const Piece &g, int64_t slot, int64_t h, int64_t tile) {
 #ifdef __HIP_DEVICE_COMPILE__
-    constexpr int PARTS = kInputParts<T>, SP = kStateParts, KS = DK / 32, BUFFERS = kBuffers<T, DK>, MATRIX = kRows<T, DK>;
+    constexpr int PARTS = kInputParts<T>, SP = kStateParts, KS = DK / 32, BUFFERS = kBuffers<T, DK>;
+    constexpr int MATRIX = kRows<T, DK>, READ = kReadBack, SLOT = MATRIX * 2 + READ;
     const int l = threadIdx.x % 64, lm = l % 16, lg = l / 16;
-    const int64_t col = tile * 16 + lm;
-    const bool works = col - lm < a.dv;
+    const int64_t col0 = tile * 16, col = col0 + lm;
+    const bool works = col0 < a.dv;
     const auto token_of = [&](int e) { return 16 * (e / 4) + 4 * lg + e % 4; };
     const int64_t chunk0 = first_piece(a, g.seq, kDeltaChunk) + g.begin / kDeltaChunk;
     const int chunks = int((g.len + 31) / 32);
@@ -296,81 +350,60 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk_back(
     const auto left_of = [&](int c) { return int(min(g.len - int64_t(c) * 32, int64_t(32))); };
 
     State<DK> D;
-    if (WALK == kSums) D.fill(0.0f);
-    else if (a.d_segments) D.load(a.d_segments + slot * states, a.dk, a.dv, col);
-    else if (a.d_state_out) D.load(a.d_state_out + (g.seq * a.heads + h) * states, a.dk, a.dv, col);
+    if (WALK == kSums || !works) D.fill(0.0f);
+    else if (a.d_segments) D.load(a.d_segments + slot * states, a.dk, a.dv, a.dv, col0);
+    else if (a.d_state_out) D.load(a.d_state_out + (g.seq * a.heads + h) * states, a.dk, a.dv, a.dv, col0);
     else D.fill(0.0f);
 
     const T *kp = at_token<T>(a.k, a, g, g.begin, h), *qp = at_token<T>(a.q, a, g, g.begin, h);
-    const T *dp = at_token<T>(a.d_o, a, g, g.begin, h) + col;
-    T *vp = WALK == kKept && a.dv_out.p ? const_cast<T *>(at_token<T>(a.dv_out, a, g, g.begin, h)) + col : nullptr;
-    float *ep = WALK == kKept && a.e ? a.e + (h * a.n_tokens + g.first + g.begin) * a.dv + col : nullptr;
+    const T *dp = at_token<T>(a.d_o, a, g, g.begin, h) + col0;
+    T *vp = WALK == kKept && a.dv_out.p ? const_cast<T *>(at_token<T>(a.dv_out, a, g, g.begin, h)) + col0 : nullptr;
+    float *ep = WALK == kKept && a.e ? a.e + (h * a.n_tokens + g.first + g.begin) * a.dvp + col0 : nullptr;
+    const uint32_t d_tok = uint32_t(a.d_o.tok), v_tok = uint32_t(a.dv_out.tok), column = uint32_t(min(int64_t(lm), max(a.dv - 1 - col0, int64_t(0))));
     Stage<T, DK> rk, rq;
-    struct Small {
-        bf16x8 t[2][SP], p[2][SP];
-        f32x4 beta[2], rise[2], fall[2];
-        float whole;
-        int bad;
-        T d[8];
-    };
-    const auto fetch_small = [&](int c, Small &s) __attribute__((always_inline)) {
-        const char *record = a.chunks + ((chunk0 + c) * a.heads + h) * a.record;
-        const RecordHead *head = reinterpret_cast<const RecordHead *>(record);
-        const char *t = record + kRecordHead + kRecordMatrix + l * 16, *p = t + kRecordMatrix;
+    StageRecord<READ, kRecordHead, kRecordMatrix> record;
+    T d_next[8], d_now[8];
+    uint32_t d_at[8];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-#pragma unroll
-            for (int q = 0; q < SP; ++q) {
-                s.t[i][q] = *reinterpret_cast<const bf16x8 *>(t + (i * SP + q) * kTile);
-                s.p[i][q] = *reinterpret_cast<const bf16x8 *>(p + (i * SP + q) * kTile);
-            }
-            const int row = 16 * i + 4 * lg;
-            s.beta[i] = *reinterpret_cast<const f32x4 *>(head->beta + row);
-            s.rise[i] = *reinterpret_cast<const f32x4 *>(head->rise + row);
-            s.fall[i] = *reinterpret_cast<const f32x4 *>(head->fall + row);
-        }
-        s.whole = head->whole;
-        s.bad = head->bad;
+    for (int e = 0; e < 8; ++e) d_at[e] = (token_of(e) * d_tok + column) * sizeof(T);
+    const auto fetch = [&](int c) __attribute__((always_inline)) {
         const int left = left_of(c);
+        record.fetch(a.chunks + ((chunk0 + c) * a.heads + h) * a.record);
+        rk.fetch(kp + int64_t(c) * 32 * a.k.tok, uint32_t(a.k.tok), left, int(a.dkp));
+        rq.fetch(qp + int64_t(c) * 32 * a.q.tok, uint32_t(a.q.tok), left, int(a.dkp));
+        const T *d = dp + int64_t(c) * 32 * a.d_o.tok;
+        if (works)      // (of columns that are not there, the last one's)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            s.d[e] = T(0.0f);
-            if (col < a.dv && token_of(e) < left) s.d[e] = dp[(int64_t(c) * 32 + token_of(e)) * a.d_o.tok];
-        }
+            for (int e = 0; e < 8; ++e) d_next[e] = get<T>(d, min(d_at[e], (uint32_t(left - 1) * d_tok + column) * uint32_t(sizeof(T))));
     };
-    const auto fetch_rows = [&](int c) __attribute__((always_inline)) {
-        rk.fetch(kp + int64_t(c) * 32 * a.k.tok, a.k.tok, left_of(c), a.dk);
-        rq.fetch(qp + int64_t(c) * 32 * a.q.tok, a.q.tok, left_of(c), a.dk);
-    };
-    const auto put_rows = [&](int c) __attribute__((always_inline)) {
-        char *to = lds + c % BUFFERS * MATRIX * 2;
-        rk.put(to);
-        rq.put(to + MATRIX);
+    const auto put = [&](int c) __attribute__((always_inline)) {
+        char *to = lds + c % BUFFERS * SLOT;
+        rk.put(to, left_of(c), int(a.dkp));
+        rq.put(to + MATRIX, left_of(c), int(a.dkp));
+        record.put(to + 2 * MATRIX);
     };
 
-    Small cur;
     if (chunks) {
-        fetch_rows(chunks - 1);
-        fetch_small(chunks - 1, cur);
-        put_rows(chunks - 1);
+        fetch(chunks - 1);
+        put(chunks - 1);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d_now[e] = d_next[e];
     }
     __syncthreads();
     for (int c = chunks - 1; c >= 0; --c) {
-        const char *k = lds + c % BUFFERS * MATRIX * 2, *q = k + MATRIX;
+        const char *k = lds + c % BUFFERS * SLOT, *q = k + MATRIX, *matrices = k + 2 * MATRIX + kRecordHead + l * 16;
+        const RecordHead *head = reinterpret_cast<const RecordHead *>(k + 2 * MATRIX);
         const int left = left_of(c);
-        Small next;
-        if (c > 0) {
-            fetch_rows(c - 1);
-            fetch_small(c - 1, next);
-        }
+        if (c > 0) fetch(c - 1);
+        f32x4 e_now[2], x_now[2];
         if (works) {
             if (WALK == kKept && a.d_states && (c % 2 == 1 || c == chunks - 1)) {
                 const int64_t block = first_piece(a, g.seq, kDeltaBlock) + (g.begin + int64_t(c) * 32) / kDeltaBlock;
-                D.store(a.d_states + (block * a.heads + h) * states, a.dk, a.dv, col);
+                D.store(a.d_states + (block * a.heads + h) * a.dk * a.dvp, a.dk, a.dv, a.dvp, col0);
             }
-            f32x4 w[2], o[2];
+            f32x4 w[2], o[2], beta[2], rise[2], fall[2];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) w[i] = o[i] = 0;
+            for (int i = 0; i < 2; ++i) w[i] = 0;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 bf16x8 s[SP], x[PARTS];
@@ -381,27 +414,42 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk_back(
                     w[i] = multiply<SP - 1>(x, s, w[i]);
                 }
             }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                beta[i] = *reinterpret_cast<const f32x4 *>(head->beta + 16 * i + 4 * lg);
+                rise[i] = *reinterpret_cast<const f32x4 *>(head->rise + 16 * i + 4 * lg);
+                fall[i] = *reinterpret_cast<const f32x4 *>(head->fall + 16 * i + 4 * lg);
+            }
             bf16x8 od[PARTS], du[SP], x[SP];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) split(float(cur.d[e]), od, e);
+            for (int e = 0; e < 8; ++e) {
+                if (token_of(e) >= left) d_now[e] = T(0.0f);
+                split(float(d_now[e]), od, e);
+            }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) o[i] = multiply<SP - 1>(cur.p[i], od, o[i]);
+            for (int i = 0; i < 2; ++i) {
+                bf16x8 t[SP];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) split(a.scale * o[e / 4][e % 4] + cur.fall[e / 4][e % 4] * w[e / 4][e % 4], du, e);
+                for (int p = 0; p < SP; ++p) t[p] = *reinterpret_cast<const bf16x8 *>(matrices + kRecordMatrix + (i * SP + p) * kTile);
+                o[i] = multiply<SP - 1>(t, od, f32x4{0, 0, 0, 0}) * a.scale + fall[i] * w[i];
+            }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) o[i] = multiply<SP - 1>(cur.t[i], du, f32x4{0, 0, 0, 0});
+            for (int e = 0; e < 8; ++e) split(o[e / 4][e % 4], du, e);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                bf16x8 t[SP];
+#pragma unroll
+                for (int p = 0; p < SP; ++p) t[p] = *reinterpret_cast<const bf16x8 *>(matrices + (i * SP + p) * kTile);
+                e_now[i] = multiply<SP - 1>(t, du, f32x4{0, 0, 0, 0});
+                x_now[i] = beta[i] * e_now[i];
+            }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float ee = o[e / 4][e % 4], xe = cur.beta[e / 4][e % 4] * ee, rise = cur.rise[e / 4][e % 4];
-                split(rise * a.scale * float(cur.d[e]), du, e);
-                split(-rise * xe, x, e);
-                if (WALK == kKept && token_of(e) < left && col < a.dv) {
-                    const int64_t token = int64_t(c) * 32 + token_of(e);
-                    if (ep) ep[token * a.dv] = ee;
-                    if (vp) vp[token * a.dv_out.tok] = T(xe);
-                }
+                const float up = rise[e / 4][e % 4];
+                split(up * a.scale * float(d_now[e]), du, e);
+                split(-up * x_now[e / 4][e % 4], x, e);
             }
-            const float whole = cur.bad < left ? __builtin_nanf("") : cur.whole;
+            const float whole = head->bad < left ? __builtin_nanf("") : head->whole;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
@@ -415,54 +463,104 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk_back(
                 }
         }
         if (BUFFERS == 1) __syncthreads();
-        if (c > 0) put_rows(c - 1);
+        if (c > 0) {
+            put(c - 1);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d_now[e] = d_next[e];
+        }
+        if (WALK == kKept && works && col < a.dvp) {      // (behind the wait for what the next chunk brings)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t token = uint32_t(token_of(e));
+                if (left < 32 && int(token) >= left) continue;
+                if (ep) set<float>(ep + int64_t(c) * 32 * a.dvp, (token * uint32_t(a.dvp) + lm) * 4, col < a.dv ? e_now[e / 4][e % 4] : 0.0f);
+                if (vp && col < a.dv) set<T>(vp + int64_t(c) * 32 * a.dv_out.tok, (token * v_tok + lm) * sizeof(T), T(x_now[e / 4][e % 4]));
+            }
+        }
         __syncthreads();
-        cur = next;
     }
     if (!works) return;
-    if (WALK == kKept && a.d_state_in && g.index == 0) D.store(a.d_state_in + (g.seq * a.heads + h) * states, a.dk, a.dv, col);
-    if (WALK == kSums) D.store(a.d_segments + slot * states, a.dk, a.dv, col);
+    if (WALK == kKept && a.d_state_in && g.index == 0) D.store(a.d_state_in + (g.seq * a.heads + h) * states, a.dk, a.dv, a.dv, col0);
+    if (WALK == kSums) D.store(a.d_segments + slot * states, a.dk, a.dv, a.dv, col0);
 #endif
 }
 
 // From segment to segment of a sequence: what enters each takes the place of what it adds.  BACK: of the gradient, from the
-// back.  Four waves, 16 columns of v each.  A sequence without tokens has its final state (its initial state's gradient) here.
-template <int DK, bool BACK> __device__ __forceinline__ void carry(const DeltaArgs &a, int64_t seq, int64_t h, int64_t tile) {
+// back.  Four waves, 16 columns of v each; 64 widths at a time of what a segment makes of a state lie in LDS as parts, the next
+// ones on their way.  A sequence without tokens has its final state (its initial state's gradient) here.
+template <int DK> constexpr int kCarryWide = DK < 64 ? DK : 64;
+template <int DK> constexpr int kCarryLds = kStateParts * kCarryWide<DK> * DK * 2;
+template <int DK, bool BACK> __device__ __forceinline__ void carry(const DeltaArgs &a, char *lds, int64_t seq, int64_t h, int64_t tile) {
 #ifdef __HIP_DEVICE_COMPILE__
-    constexpr int KS = DK / 32, SP = kStateParts;
+    constexpr int KS = DK / 32, SP = kStateParts, WIDE = kCarryWide<DK>, G = WIDE / 8, PART = DK * G * 16, LOADS = DK * G / 256 > 0 ? DK * G / 256 : 1;
     const int l = threadIdx.x % 64, lm = l % 16, lg = l / 16;
-    const int64_t col = tile * 16 + lm, states = a.dk * a.dv, own = (seq * a.heads + h) * states;
-    if (col - lm >= a.dv) return;
+    const int64_t col0 = tile * 16, states = a.dk * a.dv, own = (seq * a.heads + h) * states;
+    const bool works = col0 < a.dv;
     const int64_t id0 = first_piece(a, seq, a.seg_len);
     const int64_t tokens = a.offsets ? max(token_at(a, seq + 1) - token_at(a, seq), int64_t(0)) : a.n_tokens / a.n_seq;
-    const int64_t count = (tokens + a.seg_len - 1) / a.seg_len;
+    const int count = int((tokens + a.seg_len - 1) / a.seg_len);
     const float *in = BACK ? a.d_state_out : a.state_in;
     float *const out = BACK ? a.d_state_in : a.state_out, *const adds = BACK ? a.d_segments : a.segments;
     const float *const moves = BACK ? a.moves_t : a.moves;
-    State<DK> S;
-    if (in) S.load(in + own, a.dk, a.dv, col);
+    State<DK> S, next, later;
+    if (in && works) S.load(in + own, a.dk, a.dv, a.dv, col0);
     else S.fill(0.0f);
-    if (count == 0 && out) S.store(out + own, a.dk, a.dv, col);
-    for (int64_t i = 0; i < count; ++i) {
-        const int64_t slot = (id0 + (BACK ? count - 1 - i : i)) * a.heads + h;
-        State<DK> next;
-        next.load(adds + slot * states, a.dk, a.dv, col);
-        S.store(adds + slot * states, a.dk, a.dv, col);
-        if (i == count - 1) return;
-        const float *m = moves + slot * a.dk * a.dk;
+    if (count == 0 && out && works) S.store(out + own, a.dk, a.dv, a.dv, col0);
+    const auto slot_of = [&](int i) { return (id0 + (BACK ? count - 1 - i : i)) * a.heads + h; };
+    // widths `wide` on of the rows of what segment i makes of a state
+    Eight<float> held[LOADS];
+    const auto fetch = [&](int i, int wide) __attribute__((always_inline)) {
+        const float *m = moves + slot_of(i) * a.dk * a.dkp;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            bf16x8 s[SP];
-            S.operand(ks, s);
+        for (int j = 0; j < LOADS; ++j) {
+            const int at = j * 256 + threadIdx.x, d = at / G, w = wide + at % G * 8;
+            get_eight(held[j], m, d < a.dk && w < a.dkp ? (uint32_t(d) * uint32_t(a.dkp) + w) * 4 : 0);
+        }
+    };
+    if (count > 1) {
+        fetch(0, 0);
+        if (works) next.load(adds + slot_of(0) * states, a.dk, a.dv, a.dv, col0);
+    }
+    for (int i = 0; i < count; ++i) {
+        if (works) S.store(adds + slot_of(i) * states, a.dk, a.dv, a.dv, col0);
+        if (i + 1 == count) return;
 #pragma unroll
-            for (int to = 0; to < 2 * KS; ++to) {
-                const int64_t d = to / 2 * 32 + 8 * (lm / 4) + 4 * (to % 2) + lm % 4, from = ks * 32 + 8 * lg;
-                bf16x8 x[SP];
-                parts_of(load_eight(m + d * a.dk + from, d < a.dk ? a.dk - from : 0), x);
-                next.s[to / 2][to % 2] = multiply<SP - 1>(x, s, next.s[to / 2][to % 2]);
+        for (int wide = 0; wide < DK; wide += WIDE) {
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) {
+                const int at = j * 256 + threadIdx.x, row = at / G, gr = at % G;
+                const bool in = row < a.dk && wide + gr * 8 < a.dkp;
+                bf16x8 p[SP];
+                parts_of(held[j], p);
+                if (at < DK * G)
+#pragma unroll
+                    for (int q = 0; q < SP; ++q) *reinterpret_cast<bf16x8 *>(lds + q * PART + (row * G + (gr ^ turned<G>(row))) * 16) = in ? p[q] : bf16x8(bf16(0.0f));
+            }
+            __syncthreads();
+            if (wide + WIDE < DK) {
+                fetch(i, wide + WIDE);
+            } else if (i + 2 < count) {
+                fetch(i + 1, 0);
+                if (works) later.load(adds + slot_of(i + 1) * states, a.dk, a.dv, a.dv, col0);
+            }
+            if (!works) continue;
+#pragma unroll
+            for (int ks = 0; ks < WIDE / 32; ++ks) {
+                bf16x8 s[SP];
+                S.operand(wide / 32 + ks, s);
+#pragma unroll
+                for (int to = 0; to < 2 * KS; ++to) {
+                    const int row = to / 2 * 32 + 8 * (lm / 4) + 4 * (to % 2) + lm % 4, at = (row * G + ((4 * ks + lg) ^ turned<G>(row))) * 16;
+                    bf16x8 x[SP];
+#pragma unroll
+                    for (int q = 0; q < SP; ++q) x[q] = *reinterpret_cast<const bf16x8 *>(lds + q * PART + at);
+                    next.s[to / 2][to % 2] = multiply<SP - 1>(x, s, next.s[to / 2][to % 2]);
+                }
             }
         }
         S = next;
+        next = later;
     }
 #endif
 }

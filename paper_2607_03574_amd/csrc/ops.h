@@ -161,13 +161,15 @@ struct DeltaArgs {
     float *d_state_in;          // or null
     void *ws;
     // laid out by the launches
+    int64_t dkp, dvp;           // dk and dv, up to a multiple of eight
+    void *k_rows, *q_rows, *d_rows;     // copies of k, q and d_o of other widths
     char *chunks;               // a record for each chunk and head
     int64_t record;             // bytes of one
-    float *states, *d_states;   // [block][heads][dk][dv]: S before a block, and its gradient after it
-    float *m, *e;               // [heads][n_tokens][dv]
+    float *states, *d_states;   // [block][heads][dk][dvp]: S before a block, and its gradient after it
+    float *m, *e;               // [heads][n_tokens][dvp], 0 from dv on
     float *dq_part, *dk_part;   // [heads][n_tokens][dk], where heads share q and k
     // sequences cut into segments: what one adds to a state [segment][heads][dk][dv], then the state that enters it; the
-    // same of the gradient, from the back; what it makes of a state [segment][heads][dk][dk], and transposed
+    // same of the gradient, from the back; what it makes of a state [segment][heads][dk][dkp], and transposed
     float *segments, *d_segments, *moves, *moves_t;
     int64_t seg_len, n_segments;
 };

@@ -550,6 +550,13 @@ static ndvm_status check_delta_inputs(const char *who, const ndvm_delta_shape *s
     return NDVM_OK;
 }
 
+// The kernels count the 32 rows of a chunk in 32 bits.
+static ndvm_status check_rows_near(const char *who, std::initializer_list<const ndvm_heads *> all) {
+    for (const ndvm_heads *x : all)
+        if (x->tok_stride >= int64_t(1) << 24) return fail(NDVM_E_UNSUPPORTED, who, "rows are 2^24 values apart, or more");
+    return NDVM_OK;
+}
+
 static DeltaArgs delta_args(const ndvm_delta_shape *s, const ndvm_heads *q, const ndvm_heads *k, const ndvm_heads *v, const ndvm_heads *g,
                             const ndvm_heads *beta, const int64_t *offsets, const float *initial_state, void *workspace) {
     DeltaArgs a{};
@@ -575,7 +582,7 @@ static DeltaArgs delta_args(const ndvm_delta_shape *s, const ndvm_heads *q, cons
 static size_t delta_need(const ndvm_delta_shape *s, bool packed, bool grad) {
     static const int64_t some = 0;
     DeltaArgs a = delta_args(s, nullptr, nullptr, nullptr, nullptr, nullptr, packed ? &some : nullptr, nullptr, nullptr);
-    a.q.group = int(s->heads / s->qk_heads);
+    a.q.group = a.k.group = int(s->heads / s->qk_heads);
     return delta_bytes(s->dtype, a, grad);
 }
 
@@ -598,6 +605,7 @@ ndvm_status ndvm_delta_attention(const ndvm_delta_shape *shape, const ndvm_heads
         if (const ndvm_status st = check_delta(who, s, true, offsets != nullptr)) return st;
         if (const ndvm_status st = check_delta_inputs(who, s, s->n_tokens, q, k, v, g, beta)) return st;
         if (!o || bad_heads(o, s->n_tokens)) return bad(who, "null buffer or bad stride");
+        if (const ndvm_status st = check_rows_near(who, {q, k, v, o})) return st;
         if (s->n_seq == 0) return NDVM_OK;
         const size_t need = delta_need(s, offsets != nullptr, false);
         if (workspace_bytes < need) return fail(NDVM_E_NOMEM, who, "workspace too small");
@@ -625,6 +633,7 @@ ndvm_status ndvm_delta_attention_grad(const ndvm_delta_shape *shape, const ndvm_
             if (!x || bad_heads(x, 0)) return bad(who, "null argument or bad stride");
             wanted |= x->data != nullptr;
         }
+        if (const ndvm_status st = check_rows_near(who, {q, k, v, d_o, dv})) return st;
         if (s->n_seq == 0 || !wanted) return NDVM_OK;
         const size_t need = delta_need(s, offsets != nullptr, true);
         if (workspace_bytes < need) return fail(NDVM_E_NOMEM, who, "workspace too small");

@@ -169,7 +169,7 @@ def test_delta_refusals():
         return nd._DeltaShape(*{**dict(dtype=1, n_seq=2, n_tokens=8, heads=4, qk_heads=2, dk=8, dv=16, scale=1.0), **kw}.values())
 
     h, none = nd._Heads(FAKE, 0, 64, 16), nd._Heads(None, 0, 0, 0)
-    far = nd._Heads(FAKE, 0, -1, 16)
+    far, apart = nd._Heads(FAKE, 0, -1, 16), nd._Heads(FAKE, 0, 1 << 24, 16)
 
     def forward(s=None, q=h, v=h, g=h, o=h, off=FAKE, ws=FAKE, size=1 << 30):
         return nd._delta(s or shape(), q, h, v, g, h, off, None, o, None, ws, size, None)
@@ -189,6 +189,7 @@ def test_delta_refusals():
         assert nd.last_error()
     for kw in (dict(q=none), dict(v=far), dict(g=none), dict(o=none), dict(o=far)):
         assert forward(**kw) == nd.E_ARG, kw
+    assert forward(v=apart) == forward(o=apart) == gradient(do=apart) == nd.E_UNSUPPORTED
     assert gradient(do=none) == nd.E_ARG and gradient(dq=far) == nd.E_ARG and gradient(dq=none, dg=none) == nd.OK
 
     def step(s=None, q=h, o=h, state=FAKE, n=2, slots=None):
