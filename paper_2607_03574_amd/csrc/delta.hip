@@ -14,13 +14,13 @@ template <class T, int DK, Walk WALK> __global__ void __launch_bounds__(256, (kR
     const Piece g = find_piece(a, id, a.seg_len, !a.segments);
     // (what the last segment makes of a state enters none)
     if (g.count == 0 || (WALK == kSums && g.index == g.count - 1)) return;
-    walk<T, DK, WALK>(a, lds, g, blockIdx.x, h, int64_t(blockIdx.y) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64));
+    walk<T, DK, WALK>(a, lds, g, blockIdx.x, h, int(blockIdx.y) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64));
 }
 
 template <int DK> __global__ void __launch_bounds__(256) delta_carry(DeltaArgs a) {
     __shared__ __align__(16) char lds[kCarryLds<DK>];
     const uint32_t seq = blockIdx.x / uint32_t(a.heads);
-    carry<DK, false>(a, lds, seq, blockIdx.x - seq * uint32_t(a.heads), int64_t(blockIdx.y) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64));
+    carry<DK, false>(a, lds, seq, blockIdx.x - seq * uint32_t(a.heads), int(blockIdx.y) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64));
 }
 
 // One token of every stream: S <- a S + k^T u, u = b (v - a k S), o = scale q S = scale (q (a S) + (q k) u).  Bound by the

@@ -19,7 +19,8 @@ namespace {
 template <class T, int DK, Walk WALK> __global__ void __launch_bounds__(256, (kResident<T, DK>)) delta_grad_walk(DeltaArgs a) {
     __shared__ __align__(16) char lds[kWalkLds<T, DK, true, kReadBack>];
     const uint32_t id = blockIdx.x / uint32_t(a.heads);
-    const int64_t h = blockIdx.x - id * uint32_t(a.heads), tile = int64_t(blockIdx.y) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int64_t h = blockIdx.x - id * uint32_t(a.heads);
+    const int tile = int(blockIdx.y) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const Piece g = find_piece(a, id, a.seg_len, !a.segments);
     if (g.count == 0 || (blockIdx.z && blockIdx.y * 64 >= a.dv)) return;
     if (blockIdx.z == 0) {
@@ -32,7 +33,8 @@ template <class T, int DK, Walk WALK> __global__ void __launch_bounds__(256, (kR
 template <int DK> __global__ void __launch_bounds__(256) delta_grad_carry(DeltaArgs a) {
     __shared__ __align__(16) char lds[kCarryLds<DK>];
     const uint32_t seq = blockIdx.x / uint32_t(a.heads);
-    const int64_t h = blockIdx.x - seq * uint32_t(a.heads), tile = int64_t(blockIdx.y) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int64_t h = blockIdx.x - seq * uint32_t(a.heads);
+    const int tile = int(blockIdx.y) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     if (blockIdx.z == 0) {
         if (a.m) carry<DK, false>(a, lds, seq, h, tile);
     } else {

@@ -90,6 +90,12 @@ template <class V> __device__ inline V get(const void *base, uint32_t off) {
 }
 template <class V> __device__ inline void set(void *base, uint32_t off, V v) { *(GLOBAL V *)((GLOBAL char *)base + off) = v; }
 #undef GLOBAL
+// v, known from here on only: an offset that the compiler takes out of a loop it no longer sees to be 32 bits wide, and adds it to
+// the address in vector registers, once for every access.
+__device__ inline uint32_t here(uint32_t v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
 template <class T> __device__ inline void get_eight(Eight<T> &e, const void *base, uint32_t off) {
 #pragma unroll
     for (int i = 0; i < 8 / kVec<T>; ++i) e.v[i] = get<vec<T>>(base, off + i * 16);
@@ -102,7 +108,6 @@ struct Piece {
     int64_t seq, first, tokens;     // sequence, its first token, its length
     int64_t begin, len;             // the piece's place in the sequence
     int64_t index, count;           // of the sequence's pieces; count 0: a spare id
-    int64_t id0;                    // the id of the sequence's first piece
 };
 __device__ inline int64_t token_at(const DeltaArgs &a, int64_t s) { return min(max(a.offsets[s], int64_t(0)), a.n_tokens); }
 __device__ inline int shift_of(int64_t len) { return 63 - __builtin_clzll(len); }
@@ -146,7 +151,13 @@ __device__ inline Piece find_piece(const DeltaArgs &a, uint32_t id, int64_t len,
         g.tokens = max(token_at(a, int64_t(lo) + 1) - g.first, int64_t(0));
         g.count = whole ? 1 : (g.tokens + len - 1) >> shift;
     }
-    g.id0 = int64_t(id) - g.index;
+    // the same for the wave, and below 2^31: in scalar registers
+    const auto same = [](int64_t v) { return int64_t(__builtin_amdgcn_readfirstlane(int(v))); };
+    g.seq = same(g.seq);
+    g.first = same(g.first);
+    g.tokens = same(g.tokens);
+    g.index = same(g.index);
+    g.count = same(g.count);
     g.begin = whole ? 0 : g.index * len;
     g.len = whole ? g.tokens : min(len, g.tokens - g.begin);
     if (g.index < 0 || g.index >= g.count) g.count = 0;

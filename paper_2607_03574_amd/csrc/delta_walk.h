@@ -94,34 +94,52 @@ template <class T, int DK> __device__ inline void widths_operand(const char *row
 template <int DK> struct State {
     static constexpr int KS = DK / 32;
     f32x4 s[KS][2];
+    // f(values, place, width): the lane's own width is 8 (l / 16) more
     template <class F> __device__ inline void each(F f) {
-        const int lg = threadIdx.x % 64 / 16;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) f(s[ks][t], r, ks * 32 + 8 * lg + 4 * t + r);
+                for (int r = 0; r < 4; ++r) f(s[ks][t], r, ks * 32 + 4 * t + r);
     }
     __device__ inline void fill(float v) {
         each([&](f32x4 &x, int r, int) { x[r] = v; });
     }
-    // col0: the first of the wave's 16 columns; rows are `step` values apart
-    __device__ inline void load(const float *from, int64_t dk, int64_t cols, int64_t step, int64_t col0) {
-        const int lm = threadIdx.x % 16;
-        const bool in = col0 + lm < cols;
-        each([&](f32x4 &x, int r, int d) { x[r] = get<float>(from + col0, in && d < dk ? (uint32_t(d) * uint32_t(step) + lm) * 4 : 0); });
-        if (dk < DK || col0 + 16 > cols)
-            each([&](f32x4 &x, int r, int d) { x[r] = in && d < dk ? x[r] : 0.0f; });
+    // col0: the first of the wave's 16 columns; rows are `step` values apart.  (A lane has one offset for all its values: an
+    // address for each, which the compiler would keep all the while, is twice as many registers as the state.)
+    __device__ inline void load(const float *from, int dk, int cols, int step, int col0) {
+        const int lm = threadIdx.x % 16, up = threadIdx.x % 64 / 16 * 8;
+        from += col0;
+        if (dk == DK && col0 + 16 <= cols) {
+            const uint32_t at = here(uint32_t(up * step + lm) * 4);
+            each([&](f32x4 &x, int r, int d) {
+                x[r] = get<float>(from, at);
+                from += d % 8 == 7 ? 25 * step : step;
+            });
+        } else {
+            each([&](f32x4 &x, int r, int d) {
+                const bool in = col0 + lm < cols && d + up < dk;
+                const float v = get<float>(from, in ? uint32_t((d + up) * step + lm) * 4 : 0);
+                x[r] = in ? v : 0.0f;
+            });
+        }
     }
     // (columns from `cols` to `step` are 0)
-    __device__ inline void store(float *to, int64_t dk, int64_t cols, int64_t step, int64_t col0) {
-        const int lm = threadIdx.x % 16;
-        if (col0 + lm >= step) return;
-        const bool in = col0 + lm < cols;
-        each([&](f32x4 &x, int r, int d) {
-            if (dk == DK || d < dk) set<float>(to + col0, (uint32_t(d) * uint32_t(step) + lm) * 4, in ? x[r] : 0.0f);
-        });
+    __device__ inline void store(float *to, int dk, int cols, int step, int col0) {
+        const int lm = threadIdx.x % 16, up = threadIdx.x % 64 / 16 * 8;
+        to += col0;
+        if (dk == DK && col0 + 16 <= cols) {
+            const uint32_t at = here(uint32_t(up * step + lm) * 4);
+            each([&](f32x4 &x, int r, int d) {
+                set<float>(to, at, x[r]);
+                to += d % 8 == 7 ? 25 * step : step;
+            });
+        } else if (col0 + lm < step) {
+            each([&](f32x4 &x, int r, int d) {
+                if (d + up < dk) set<float>(to + d * step, uint32_t(up * step + lm) * 4, col0 + lm < cols ? x[r] : 0.0f);
+            });
+        }
     }
 #ifdef __HIP_DEVICE_COMPILE__
     __device__ inline void operand(int ks, bf16x8 (&x)[kStateParts]) const {
@@ -131,17 +149,50 @@ template <int DK> struct State {
 #endif
 };
 
+// A lane's eight tokens of a column: 16 (e / 4) + e % 4, and 4 (l / 16) more.  Of tokens that are not there, the last one.
+template <class T> __device__ inline void load_column(T (&v)[8], const T *p, int64_t tok, int left, uint32_t column) {
+    const uint32_t up = threadIdx.x % 64 / 16 * 4;
+    if (left == 32) {
+        const uint32_t at = here((up * uint32_t(tok) + column) * sizeof(T));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            v[e] = get<T>(p, at);
+            p += e == 3 ? 13 * tok : tok;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v[e] = get<T>(p, (min(16 * (e / 4) + e % 4 + up, uint32_t(left - 1)) * uint32_t(tok) + column) * sizeof(T));
+    }
+}
+template <class T, class F> __device__ inline void store_column(T *p, int64_t tok, int left, F f) {
+    const uint32_t up = threadIdx.x % 64 / 16 * 4, at = here((up * uint32_t(tok) + threadIdx.x % 16) * sizeof(T));
+    if (left == 32) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            set<T>(p, at, f(e));
+            p += e == 3 ? 13 * tok : tok;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (16 * (e / 4) + e % 4 + int(up) < left) set<T>(p, at, f(e));
+            p += e == 3 ? 13 * tok : tok;
+        }
+    }
+}
+
 // Forwards.  tile: the wave's columns; from ceil(dv / 16) on (kSums) those of what the piece makes of a state.
 // (Inlined by force: called, its arrays would live in memory.)
-template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const DeltaArgs &a, char *lds, const Piece &g, int64_t slot, int64_t h, int64_t tile) {
+template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const DeltaArgs &a, char *lds, const Piece &g, int64_t slot, int64_t h, int tile) {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int PARTS = kInputParts<T>, HELD = kResultParts<T>, SP = kStateParts, KS = DK / 32, BUFFERS = kBuffers<T, DK>;
     constexpr bool OUT = WALK == kOutputs;
     constexpr int MATRIX = kRows<T, DK>, READ = kRead<T, WALK>, SLOT = MATRIX * (OUT ? 2 : 1) + READ;
     const int l = threadIdx.x % 64, lm = l % 16, lg = l / 16;
-    const int64_t tiles = ceil_div(a.dv, 16);
+    const int dk = int(a.dk), dv = int(a.dv), dkp = int(a.dkp), dvp = int(a.dvp), tiles = (dv + 15) / 16;
     const bool moves = WALK == kSums && tile >= tiles;
-    const int64_t cols = moves ? a.dk : a.dv, col0 = (moves ? tile - tiles : tile) * 16, col = col0 + lm;
+    const int cols = moves ? dk : dv, col0 = (moves ? tile - tiles : tile) * 16, col = col0 + lm;
     const bool works = col0 < cols;
     const auto token_of = [&](int e) { return 16 * (e / 4) + 4 * lg + e % 4; };
     const int64_t chunk0 = first_piece(a, g.seq, kDeltaChunk) + g.begin / kDeltaChunk;
@@ -150,44 +201,42 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const
     const auto left_of = [&](int c) { return int(min(g.len - int64_t(c) * 32, int64_t(32))); };
 
     State<DK> S;
-    if (WALK == kSums) S.each([&](f32x4 &x, int r, int d) { x[r] = moves && d == col ? 1.0f : 0.0f; });
+    if (WALK == kSums) S.each([&](f32x4 &x, int r, int d) { x[r] = moves && d + 8 * lg == col ? 1.0f : 0.0f; });
     else if (!works) S.fill(0.0f);
-    else if (a.segments) S.load(a.segments + slot * states, a.dk, a.dv, a.dv, col0);
-    else if (a.state_in) S.load(a.state_in + (g.seq * a.heads + h) * states, a.dk, a.dv, a.dv, col0);
+    else if (a.segments) S.load(a.segments + slot * states, dk, dv, dv, col0);
+    else if (a.state_in) S.load(a.state_in + (g.seq * a.heads + h) * states, dk, dv, dv, col0);
     else S.fill(0.0f);
 
     const T *kp = at_token<T>(a.k, a, g, g.begin, h), *qp = OUT ? at_token<T>(a.q, a, g, g.begin, h) : nullptr;
     const T *vp = at_token<T>(a.v, a, g, g.begin, h) + (moves ? 0 : col0);
     T *op = OUT ? const_cast<T *>(at_token<T>(a.o, a, g, g.begin, h)) + col0 : nullptr;
     float *mp = WALK == kKept ? a.m + (h * a.n_tokens + g.first + g.begin) * a.dvp + col0 : nullptr;
-    const uint32_t v_tok = uint32_t(a.v.tok), o_tok = uint32_t(a.o.tok), column = uint32_t(min(int64_t(lm), max(cols - 1 - col0, int64_t(0))));
+    const uint32_t column = uint32_t(min(lm, max(cols - 1 - col0, 0)));
     Stage<T, DK> rk, rq;
     StageRecord<READ, READ, 0> record;
     T v_next[8];
-    uint32_t v_at[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v_at[e] = (token_of(e) * v_tok + column) * sizeof(T);
     // values of v: of columns and tokens that are not there, those of the last ones; they reach nothing
     const auto fetch = [&](int c) __attribute__((always_inline)) {
         const int left = left_of(c);
         record.fetch(a.chunks + ((chunk0 + c) * a.heads + h) * a.record);
-        rk.fetch(kp + int64_t(c) * 32 * a.k.tok, uint32_t(a.k.tok), left, int(a.dkp));
-        if constexpr (OUT) rq.fetch(qp + int64_t(c) * 32 * a.q.tok, uint32_t(a.q.tok), left, int(a.dkp));
+        rk.fetch(kp + int64_t(c) * 32 * a.k.tok, uint32_t(a.k.tok), left, dkp);
+        if constexpr (OUT) rq.fetch(qp + int64_t(c) * 32 * a.q.tok, uint32_t(a.q.tok), left, dkp);
         const T *v = vp + int64_t(c) * 32 * a.v.tok;
         if (moves || !works)
 #pragma unroll
             for (int e = 0; e < 8; ++e) v_next[e] = T(0.0f);
-        else
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v_next[e] = get<T>(v, min(v_at[e], (uint32_t(left - 1) * v_tok + column) * uint32_t(sizeof(T))));
+        else load_column(v_next, v, a.v.tok, left, column);
     };
     const auto put = [&](int c) __attribute__((always_inline)) {
         char *to = lds + c % BUFFERS * SLOT;
-        rk.put(to, left_of(c), int(a.dkp));
-        if constexpr (OUT) rq.put(to + MATRIX, left_of(c), int(a.dkp));
+        rk.put(to, left_of(c), dkp);
+        if constexpr (OUT) rq.put(to + MATRIX, left_of(c), dkp);
         record.put(to + SLOT - READ);
     };
 
+    // the state before a block
+    float *kept = WALK == kKept ? a.states + ((first_piece(a, g.seq, kDeltaBlock) + g.begin / kDeltaBlock) * a.heads + h) * dk * dvp : nullptr;
+    const auto keep = [&](int c) __attribute__((always_inline)) { S.store(kept + int64_t(c / 2) * a.heads * dk * dvp, dk, dv, dvp, col0); };
     T v_now[8];
     if (chunks) {
         fetch(0);
@@ -195,6 +244,7 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const
 #pragma unroll
         for (int e = 0; e < 8; ++e) v_now[e] = v_next[e];
     }
+    if (WALK == kKept && works && chunks) keep(0);
     __syncthreads();
     for (int c = 0; c < chunks; ++c) {
         const char *k = lds + c % BUFFERS * SLOT, *q = k + MATRIX, *matrices = k + SLOT - READ + kRecordHead + l * 16;
@@ -204,10 +254,6 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const
         f32x4 o[2];
         int first = 32;
         if (works) {
-            if (WALK == kKept && c % 2 == 0) {
-                const int64_t block = first_piece(a, g.seq, kDeltaBlock) + (g.begin + int64_t(c) * 32) / kDeltaBlock;
-                S.store(a.states + (block * a.heads + h) * a.dk * a.dvp, a.dk, a.dv, a.dvp, col0);
-            }
             // Y = K S, Z = Q S
             f32x4 y[2], z[2], beta[2], rise[2], fall[2];
 #pragma unroll
@@ -303,46 +349,38 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const
 #pragma unroll
             for (int e = 0; e < 8; ++e) v_now[e] = v_next[e];
         }
-        if (WALK != kSums && works && col < (OUT ? a.dv : a.dvp)) {      // (behind the wait for what the next chunk brings)
+        // (what is stored comes behind the wait for what the next chunk brings)
+        if (WALK == kKept && works && c % 2 && c + 1 < chunks) keep(c + 1);
+        if (WALK != kSums && works && col < (OUT ? dv : dvp)) {
             if (__ballot(first < left))
 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[e / 4][e % 4] = token_of(e) < first ? o[e / 4][e % 4] : __builtin_nanf("");
-            const auto store = [&](int e) __attribute__((always_inline)) {
-                const uint32_t token = uint32_t(token_of(e));
-                if constexpr (OUT) set<T>(op + int64_t(c) * 32 * a.o.tok, (token * o_tok + lm) * sizeof(T), T(o[e / 4][e % 4]));
-                else set<float>(mp + int64_t(c) * 32 * a.dvp, (token * uint32_t(a.dvp) + lm) * 4, col < a.dv ? o[e / 4][e % 4] : 0.0f);
-            };
-            if (left == 32)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) store(e);
-            else
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (token_of(e) < left) store(e);
+            if constexpr (OUT) store_column(op + int64_t(c) * 32 * a.o.tok, a.o.tok, left, [&](int e) { return T(o[e / 4][e % 4]); });
+            else store_column(mp + int64_t(c) * 32 * dvp, dvp, left, [&](int e) { return col < dv ? o[e / 4][e % 4] : 0.0f; });
         }
         __syncthreads();
     }
     if (!works) return;
-    if (OUT && a.state_out && g.index == g.count - 1) S.store(a.state_out + (g.seq * a.heads + h) * states, a.dk, a.dv, a.dv, col0);
-    if (WALK == kSums && !moves) S.store(a.segments + slot * states, a.dk, a.dv, a.dv, col0);
+    if (OUT && a.state_out && g.index == g.count - 1) S.store(a.state_out + (g.seq * a.heads + h) * states, dk, dv, dv, col0);
+    if (WALK == kSums && !moves) S.store(a.segments + slot * states, dk, dv, dv, col0);
     if (WALK == kSums && moves) {
-        S.store(a.moves + slot * a.dk * a.dkp, a.dk, a.dk, a.dkp, col0);
+        S.store(a.moves + slot * a.dk * a.dkp, dk, dk, dkp, col0);
         if (a.moves_t)      // (rows from dk on are 0)
             S.each([&](f32x4 &x, int r, int d) {
-                if (d < a.dkp && col < cols) set<float>(a.moves_t + (slot * a.dk + col0) * a.dkp, (uint32_t(lm) * uint32_t(a.dkp) + d) * 4, d < a.dk ? x[r] : 0.0f);
+                if (d + 8 * lg < dkp && col < cols) set<float>(a.moves_t + (slot * dk + col0) * dkp, uint32_t(lm * dkp + d + 8 * lg) * 4, d + 8 * lg < dk ? x[r] : 0.0f);
             });
     }
 #endif
 }
 
 // Backwards: the gradient of the state, from the piece's end to its beginning; e and the gradient of v.
-template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk_back(const DeltaArgs &a, char *lds, const Piece &g, int64_t slot, int64_t h, int64_t tile) {
+template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk_back(const DeltaArgs &a, char *lds, const Piece &g, int64_t slot, int64_t h, int tile) {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int PARTS = kInputParts<T>, SP = kStateParts, KS = DK / 32, BUFFERS = kBuffers<T, DK>;
     constexpr int MATRIX = kRows<T, DK>, READ = kReadBack, SLOT = MATRIX * 2 + READ;
     const int l = threadIdx.x % 64, lm = l % 16, lg = l / 16;
-    const int64_t col0 = tile * 16, col = col0 + lm;
-    const bool works = col0 < a.dv;
+    const int dk = int(a.dk), dv = int(a.dv), dkp = int(a.dkp), dvp = int(a.dvp), col0 = tile * 16, col = col0 + lm;
+    const bool works = col0 < dv;
     const auto token_of = [&](int e) { return 16 * (e / 4) + 4 * lg + e % 4; };
     const int64_t chunk0 = first_piece(a, g.seq, kDeltaChunk) + g.begin / kDeltaChunk;
     const int chunks = int((g.len + 31) / 32);
@@ -351,44 +389,43 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk_back(
 
     State<DK> D;
     if (WALK == kSums || !works) D.fill(0.0f);
-    else if (a.d_segments) D.load(a.d_segments + slot * states, a.dk, a.dv, a.dv, col0);
-    else if (a.d_state_out) D.load(a.d_state_out + (g.seq * a.heads + h) * states, a.dk, a.dv, a.dv, col0);
+    else if (a.d_segments) D.load(a.d_segments + slot * states, dk, dv, dv, col0);
+    else if (a.d_state_out) D.load(a.d_state_out + (g.seq * a.heads + h) * states, dk, dv, dv, col0);
     else D.fill(0.0f);
 
     const T *kp = at_token<T>(a.k, a, g, g.begin, h), *qp = at_token<T>(a.q, a, g, g.begin, h);
     const T *dp = at_token<T>(a.d_o, a, g, g.begin, h) + col0;
     T *vp = WALK == kKept && a.dv_out.p ? const_cast<T *>(at_token<T>(a.dv_out, a, g, g.begin, h)) + col0 : nullptr;
     float *ep = WALK == kKept && a.e ? a.e + (h * a.n_tokens + g.first + g.begin) * a.dvp + col0 : nullptr;
-    const uint32_t d_tok = uint32_t(a.d_o.tok), v_tok = uint32_t(a.dv_out.tok), column = uint32_t(min(int64_t(lm), max(a.dv - 1 - col0, int64_t(0))));
+    const uint32_t column = uint32_t(min(lm, max(dv - 1 - col0, 0)));
     Stage<T, DK> rk, rq;
     StageRecord<READ, kRecordHead, kRecordMatrix> record;
     T d_next[8], d_now[8];
-    uint32_t d_at[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) d_at[e] = (token_of(e) * d_tok + column) * sizeof(T);
     const auto fetch = [&](int c) __attribute__((always_inline)) {
         const int left = left_of(c);
         record.fetch(a.chunks + ((chunk0 + c) * a.heads + h) * a.record);
-        rk.fetch(kp + int64_t(c) * 32 * a.k.tok, uint32_t(a.k.tok), left, int(a.dkp));
-        rq.fetch(qp + int64_t(c) * 32 * a.q.tok, uint32_t(a.q.tok), left, int(a.dkp));
+        rk.fetch(kp + int64_t(c) * 32 * a.k.tok, uint32_t(a.k.tok), left, dkp);
+        rq.fetch(qp + int64_t(c) * 32 * a.q.tok, uint32_t(a.q.tok), left, dkp);
         const T *d = dp + int64_t(c) * 32 * a.d_o.tok;
-        if (works)      // (of columns that are not there, the last one's)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) d_next[e] = get<T>(d, min(d_at[e], (uint32_t(left - 1) * d_tok + column) * uint32_t(sizeof(T))));
+        if (works) load_column(d_next, d, a.d_o.tok, left, column);      // (of columns that are not there, the last one's)
     };
     const auto put = [&](int c) __attribute__((always_inline)) {
         char *to = lds + c % BUFFERS * SLOT;
-        rk.put(to, left_of(c), int(a.dkp));
-        rq.put(to + MATRIX, left_of(c), int(a.dkp));
+        rk.put(to, left_of(c), dkp);
+        rq.put(to + MATRIX, left_of(c), dkp);
         record.put(to + 2 * MATRIX);
     };
 
+    // the gradient of the state after a block
+    float *kept = WALK == kKept && a.d_states ? a.d_states + ((first_piece(a, g.seq, kDeltaBlock) + g.begin / kDeltaBlock) * a.heads + h) * dk * dvp : nullptr;
+    const auto keep = [&](int c) __attribute__((always_inline)) { D.store(kept + int64_t(c / 2) * a.heads * dk * dvp, dk, dv, dvp, col0); };
     if (chunks) {
         fetch(chunks - 1);
         put(chunks - 1);
 #pragma unroll
         for (int e = 0; e < 8; ++e) d_now[e] = d_next[e];
     }
+    if (kept && works && chunks) keep(chunks - 1);
     __syncthreads();
     for (int c = chunks - 1; c >= 0; --c) {
         const char *k = lds + c % BUFFERS * SLOT, *q = k + MATRIX, *matrices = k + 2 * MATRIX + kRecordHead + l * 16;
@@ -397,10 +434,6 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk_back(
         if (c > 0) fetch(c - 1);
         f32x4 e_now[2], x_now[2];
         if (works) {
-            if (WALK == kKept && a.d_states && (c % 2 == 1 || c == chunks - 1)) {
-                const int64_t block = first_piece(a, g.seq, kDeltaBlock) + (g.begin + int64_t(c) * 32) / kDeltaBlock;
-                D.store(a.d_states + (block * a.heads + h) * a.dk * a.dvp, a.dk, a.dv, a.dvp, col0);
-            }
             f32x4 w[2], o[2], beta[2], rise[2], fall[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) w[i] = 0;
@@ -468,20 +501,17 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk_back(
 #pragma unroll
             for (int e = 0; e < 8; ++e) d_now[e] = d_next[e];
         }
-        if (WALK == kKept && works && col < a.dvp) {      // (behind the wait for what the next chunk brings)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t token = uint32_t(token_of(e));
-                if (left < 32 && int(token) >= left) continue;
-                if (ep) set<float>(ep + int64_t(c) * 32 * a.dvp, (token * uint32_t(a.dvp) + lm) * 4, col < a.dv ? e_now[e / 4][e % 4] : 0.0f);
-                if (vp && col < a.dv) set<T>(vp + int64_t(c) * 32 * a.dv_out.tok, (token * v_tok + lm) * sizeof(T), T(x_now[e / 4][e % 4]));
-            }
+        // (what is stored comes behind the wait for what the next chunk brings)
+        if (kept && works && c && c % 2 == 0) keep(c - 1);
+        if (WALK == kKept && works && col < dvp) {
+            if (ep) store_column(ep + int64_t(c) * 32 * dvp, dvp, left, [&](int e) { return col < dv ? e_now[e / 4][e % 4] : 0.0f; });
+            if (vp && col < dv) store_column(vp + int64_t(c) * 32 * a.dv_out.tok, a.dv_out.tok, left, [&](int e) { return T(x_now[e / 4][e % 4]); });
         }
         __syncthreads();
     }
     if (!works) return;
-    if (WALK == kKept && a.d_state_in && g.index == 0) D.store(a.d_state_in + (g.seq * a.heads + h) * states, a.dk, a.dv, a.dv, col0);
-    if (WALK == kSums) D.store(a.d_segments + slot * states, a.dk, a.dv, a.dv, col0);
+    if (WALK == kKept && a.d_state_in && g.index == 0) D.store(a.d_state_in + (g.seq * a.heads + h) * states, dk, dv, dv, col0);
+    if (WALK == kSums) D.store(a.d_segments + slot * states, dk, dv, dv, col0);
 #endif
 }
 
@@ -490,39 +520,40 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk_back(
 // ones on their way.  A sequence without tokens has its final state (its initial state's gradient) here.
 template <int DK> constexpr int kCarryWide = DK < 64 ? DK : 64;
 template <int DK> constexpr int kCarryLds = kStateParts * kCarryWide<DK> * DK * 2;
-template <int DK, bool BACK> __device__ __forceinline__ void carry(const DeltaArgs &a, char *lds, int64_t seq, int64_t h, int64_t tile) {
+template <int DK, bool BACK> __device__ __forceinline__ void carry(const DeltaArgs &a, char *lds, int64_t seq, int64_t h, int tile) {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int KS = DK / 32, SP = kStateParts, WIDE = kCarryWide<DK>, G = WIDE / 8, PART = DK * G * 16, LOADS = DK * G / 256 > 0 ? DK * G / 256 : 1;
     const int l = threadIdx.x % 64, lm = l % 16, lg = l / 16;
-    const int64_t col0 = tile * 16, states = a.dk * a.dv, own = (seq * a.heads + h) * states;
-    const bool works = col0 < a.dv;
+    const int dk = int(a.dk), dv = int(a.dv), dkp = int(a.dkp), col0 = tile * 16;
+    const int64_t states = a.dk * a.dv, own = (seq * a.heads + h) * states;
+    const bool works = col0 < dv;
     const int64_t id0 = first_piece(a, seq, a.seg_len);
     const int64_t tokens = a.offsets ? max(token_at(a, seq + 1) - token_at(a, seq), int64_t(0)) : a.n_tokens / a.n_seq;
-    const int count = int((tokens + a.seg_len - 1) / a.seg_len);
+    const int count = __builtin_amdgcn_readfirstlane(int((tokens + a.seg_len - 1) / a.seg_len));
     const float *in = BACK ? a.d_state_out : a.state_in;
     float *const out = BACK ? a.d_state_in : a.state_out, *const adds = BACK ? a.d_segments : a.segments;
     const float *const moves = BACK ? a.moves_t : a.moves;
     State<DK> S, next, later;
-    if (in && works) S.load(in + own, a.dk, a.dv, a.dv, col0);
+    if (in && works) S.load(in + own, dk, dv, dv, col0);
     else S.fill(0.0f);
-    if (count == 0 && out && works) S.store(out + own, a.dk, a.dv, a.dv, col0);
+    if (count == 0 && out && works) S.store(out + own, dk, dv, dv, col0);
     const auto slot_of = [&](int i) { return (id0 + (BACK ? count - 1 - i : i)) * a.heads + h; };
     // widths `wide` on of the rows of what segment i makes of a state
     Eight<float> held[LOADS];
     const auto fetch = [&](int i, int wide) __attribute__((always_inline)) {
-        const float *m = moves + slot_of(i) * a.dk * a.dkp;
+        const float *m = moves + slot_of(i) * dk * dkp;
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
             const int at = j * 256 + threadIdx.x, d = at / G, w = wide + at % G * 8;
-            get_eight(held[j], m, d < a.dk && w < a.dkp ? (uint32_t(d) * uint32_t(a.dkp) + w) * 4 : 0);
+            get_eight(held[j], m, d < dk && w < dkp ? uint32_t(d * dkp + w) * 4 : 0);
         }
     };
     if (count > 1) {
         fetch(0, 0);
-        if (works) next.load(adds + slot_of(0) * states, a.dk, a.dv, a.dv, col0);
+        if (works) next.load(adds + slot_of(0) * states, dk, dv, dv, col0);
     }
     for (int i = 0; i < count; ++i) {
-        if (works) S.store(adds + slot_of(i) * states, a.dk, a.dv, a.dv, col0);
+        if (works) S.store(adds + slot_of(i) * states, dk, dv, dv, col0);
         if (i + 1 == count) return;
 #pragma unroll
         for (int wide = 0; wide < DK; wide += WIDE) {
@@ -530,7 +561,7 @@ template <int DK, bool BACK> __device__ __forceinline__ void carry(const DeltaAr
 #pragma unroll
             for (int j = 0; j < LOADS; ++j) {
                 const int at = j * 256 + threadIdx.x, row = at / G, gr = at % G;
-                const bool in = row < a.dk && wide + gr * 8 < a.dkp;
+                const bool in = row < dk && wide + gr * 8 < dkp;
                 bf16x8 p[SP];
                 parts_of(held[j], p);
                 if (at < DK * G)
@@ -542,7 +573,7 @@ template <int DK, bool BACK> __device__ __forceinline__ void carry(const DeltaAr
                 fetch(i, wide + WIDE);
             } else if (i + 2 < count) {
                 fetch(i + 1, 0);
-                if (works) later.load(adds + slot_of(i + 1) * states, a.dk, a.dv, a.dv, col0);
+                if (works) later.load(adds + slot_of(i + 1) * states, dk, dv, dv, col0);
             }
             if (!works) continue;
 #pragma unroll
