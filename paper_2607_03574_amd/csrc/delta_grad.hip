@@ -48,14 +48,30 @@ template <class T> constexpr int kPair = 64 * 128;     // of a part of a pairs' 
 template <class T> constexpr int kArea = 2 * kResultParts<T> * kPair<T>;
 static_assert((2 * kResultParts<float> + kInputParts<float>) * kSlab<float> <= kArea<float>, "");
 
-// Four waves and a block: a wave has 64 tokens x 16 NT widths of dq and dk, and 16 rows of the pairs' matrices.
-template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(DeltaArgs a) {
+// Over the 16 lanes of a row, in all of them.
+__device__ inline float sum_of_16(float v) {
 #ifdef __HIP_DEVICE_COMPILE__
-    constexpr int PARTS = kInputParts<T>, HELD = kResultParts<T>, NT = DK <= 64 ? 1 : DK / 64, G = DK / 8, ROWS = 64 * G * 16;
-    constexpr int LOADS = 64 * G / 256, SLAB = kSlab<T>, PAIR = kPair<T>;
+    const auto turn = [&](auto by) __attribute__((always_inline)) {
+        v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + decltype(by)::value, 0xf, 0xf, false));     // row_ror
+    };
+    turn(std::integral_constant<int, 8>());
+    turn(std::integral_constant<int, 4>());
+    turn(std::integral_constant<int, 2>());
+    turn(std::integral_constant<int, 1>());
+#endif
+    return v;
+}
+
+// W waves and a block: a wave has 64 tokens x 16 NT widths of dq and dk, and 16 rows x 16 PT columns of the pairs' matrices.
+template <int DK> constexpr int kBlockWaves = DK >= 128 ? 8 : 4;
+template <class T, int DK> __global__ void __launch_bounds__(64 * kBlockWaves<DK>) delta_blocks(DeltaArgs a) {
+#ifdef __HIP_DEVICE_COMPILE__
+    constexpr int W = kBlockWaves<DK>, THREADS = 64 * W, PT = 16 / W;
+    constexpr int PARTS = kInputParts<T>, HELD = kResultParts<T>, NT = DK <= 16 * W ? 1 : DK / (16 * W), G = DK / 8, ROWS = 64 * G * 16;
+    constexpr int LOADS = 64 * G / THREADS, SLAB = kSlab<T>, PAIR = kPair<T>;
     __shared__ __align__(16) char area[kArea<T>], rows[PARTS * ROWS];
-    __shared__ double sum[64], row_sum[64], col_sum[4][64];
-    __shared__ float betas[64], rise[64], fall[64], dots[4][3][64], between[4];
+    __shared__ double sum[64], row_sum[W / 4][64], col_sum[4][64];
+    __shared__ float betas[64], rise[64], fall[64], dots[W][3][64], between[W];
     const uint32_t id = blockIdx.x / uint32_t(a.heads);
     const int64_t h = blockIdx.x - id * uint32_t(a.heads);
     const Piece g = find_piece(a, id, kDeltaBlock);
@@ -64,6 +80,7 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
     const int len = int(g.len);
     const int w0 = wave * 16 * NT;
     const bool has = w0 < DK;
+    const int row_tile = wave % 4, col_tile = wave / 4 * PT;
     const auto width = [&](int n) { return NT == 1 ? w0 + lm : w0 + 32 * (n / 2) + 8 * (lm / 4) + 4 * (n % 2) + lm % 4; };
 
     // (what is not there is read at another place, and is 0 when it is put)
@@ -72,14 +89,14 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
         const T *p = at_token<T>(x, a, g, g.begin, h);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int at = i * 256 + threadIdx.x, row = at / G, gr = at % G;
+            const int at = i * THREADS + threadIdx.x, row = at / G, gr = at % G;
             get_eight(held[i], p, row < len && gr * 8 < a.dkp ? (uint32_t(row) * uint32_t(x.tok) + gr * 8) * sizeof(T) : 0);
         }
     };
     const auto put_rows = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int at = i * 256 + threadIdx.x, row = at / G, gr = at % G;
+            const int at = i * THREADS + threadIdx.x, row = at / G, gr = at % G;
             const bool in = row < len && gr * 8 < a.dkp;
             bf16x8 p[PARTS];
             parts_of(held[i], p);
@@ -108,7 +125,9 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
     }
 
     // over 32 columns of v after the other: do S^T, X S^T, U D^T, do U^T, X U^T, e.m and <D, S>
-    const int srow = threadIdx.x / 4, sgr = threadIdx.x % 4;
+    // (of eight waves, four bring u and x, the others do)
+    const int srow = threadIdx.x % 256 / 4, sgr = threadIdx.x % 4;
+    const bool of_states = W == 4 || threadIdx.x < 256, of_do = W == 4 || threadIdx.x >= 256;
     const int64_t at_row = (h * a.n_tokens + g.first + g.begin) * a.dvp;
     const T *const dop = at_token<T>(a.d_o, a, g, g.begin, h);
     const float beta = srow < len ? float(*at_token<T>(a.beta, a, g, g.begin + srow, h)) : 0.0f;
@@ -119,9 +138,11 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
     const auto fetch = [&](int c) __attribute__((always_inline)) {
         const bool in = srow < len && c + sgr * 8 < dvp;
         const uint32_t off = in ? (uint32_t(srow) * uint32_t(dvp) + c + sgr * 8) * 4 : 0;
-        get_eight(m, a.m + at_row, off);
-        get_eight(e, a.e + at_row, off);
-        get_eight(o, dop, in ? (uint32_t(srow) * uint32_t(a.d_o.tok) + c + sgr * 8) * sizeof(T) : 0);
+        if (of_states) {
+            get_eight(m, a.m + at_row, off);
+            get_eight(e, a.e + at_row, off);
+        }
+        if (of_do) get_eight(o, dop, in ? (uint32_t(srow) * uint32_t(a.d_o.tok) + c + sgr * 8) * sizeof(T) : 0);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const uint32_t at = width(n) < a.dk && c + 8 * lg < dvp ? (uint32_t(width(n)) * uint32_t(dvp) + c + 8 * lg) * 4 : 0;
@@ -129,10 +150,10 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
             get_eight(D[n], dp, at);
         }
     };
-    f32x4 a1[4][NT], a2[4][NT], a3[4][NT], pd[4], ad[4];
+    f32x4 a1[4][NT], a2[4][NT], a3[4][NT], pd[PT], ad[PT];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        pd[i] = ad[i] = 0;
+        pd[i % PT] = ad[i % PT] = 0;
 #pragma unroll
         for (int n = 0; n < NT; ++n) a1[i][n] = a2[i][n] = a3[i][n] = 0;
     }
@@ -143,23 +164,28 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
         __syncthreads();
         {
             const bool in = srow < len && c + sgr * 8 < dvp;
-            bf16x8 u[HELD], x[HELD], p[PARTS];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float mi = in ? value(m, i) : 0.0f, ei = in ? value(e, i) : 0.0f;
-                db += ei * mi;
-                split(beta * mi, u, i);
-                split(beta * ei, x, i);
-            }
-            parts_of(o, p);
             const int at = srow * 64 + (sgr ^ turned<4>(srow)) * 16;
+            if (of_states) {
+                bf16x8 u[HELD], x[HELD];
 #pragma unroll
-            for (int q = 0; q < HELD; ++q) {
-                *reinterpret_cast<bf16x8 *>(of_u + q * SLAB + at) = u[q];
-                *reinterpret_cast<bf16x8 *>(of_x + q * SLAB + at) = x[q];
+                for (int i = 0; i < 8; ++i) {
+                    const float mi = in ? value(m, i) : 0.0f, ei = in ? value(e, i) : 0.0f;
+                    db += ei * mi;
+                    split(beta * mi, u, i);
+                    split(beta * ei, x, i);
+                }
+#pragma unroll
+                for (int q = 0; q < HELD; ++q) {
+                    *reinterpret_cast<bf16x8 *>(of_u + q * SLAB + at) = u[q];
+                    *reinterpret_cast<bf16x8 *>(of_x + q * SLAB + at) = x[q];
+                }
             }
+            if (of_do) {
+                bf16x8 p[PARTS];
+                parts_of(o, p);
 #pragma unroll
-            for (int q = 0; q < PARTS; ++q) *reinterpret_cast<bf16x8 *>(of_o + q * SLAB + at) = in ? p[q] : bf16x8(bf16(0.0f));
+                for (int q = 0; q < PARTS; ++q) *reinterpret_cast<bf16x8 *>(of_o + q * SLAB + at) = in ? p[q] : bf16x8(bf16(0.0f));
+            }
         }
         bf16x8 s[NT][HELD], d[NT][HELD];
 #pragma unroll
@@ -184,8 +210,8 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
             for (int q = 0; q < N; ++q) x[q] = *reinterpret_cast<const bf16x8 *>(from + q * SLAB + row * 64 + (lg ^ turned<4>(row)) * 16);
         };
         bf16x8 own_o[PARTS], own_x[HELD];
-        operand(of_o, wave, own_o);
-        operand(of_x, wave, own_x);
+        operand(of_o, row_tile, own_o);
+        operand(of_x, row_tile, own_x);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             bf16x8 u[HELD], x[HELD], p[PARTS];
@@ -200,9 +226,9 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
                     a3[t][n] = multiply<HELD - 1>(u, d[n], a3[t][n]);
                 }
             }
-            if (t <= wave) {
-                pd[t] = multiply<HELD - 1>(own_o, u, pd[t]);
-                ad[t] = multiply<HELD - 1>(own_x, u, ad[t]);
+            if (t / PT * PT == col_tile && t <= row_tile) {
+                pd[t % PT] = multiply<HELD - 1>(own_o, u, pd[t % PT]);
+                ad[t % PT] = multiply<HELD - 1>(own_x, u, ad[t % PT]);
             }
         }
     }
@@ -210,20 +236,20 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
     fetch_rows(a.k);
     // Pd and Ad, transposed, where the columns of v lay
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        const int j = 16 * t + lm;
+    for (int t = 0; t < PT; ++t) {
+        const int j = 16 * (col_tile + t) + lm;
         const double gj = sum[j];
         bf16x4 p[HELD], x[HELD];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int i = 16 * wave + 4 * lg + r;
+            const int i = 16 * row_tile + 4 * lg + r;
             const float decay = j <= i ? expf(float(sum[i] - gj)) : 0.0f;
             pd[t][r] = j <= i ? a.scale * decay * pd[t][r] : 0.0f;
             ad[t][r] = j < i ? -decay * ad[t][r] : 0.0f;
             split(pd[t][r], p, r);
             split(ad[t][r], x, r);
         }
-        const int at = j * 128 + ((2 * wave + lg / 2) ^ turned<8>(j)) * 16 + lg % 2 * 8;
+        const int at = j * 128 + ((2 * row_tile + lg / 2) ^ turned<8>(j)) * 16 + lg % 2 * 8;
 #pragma unroll
         for (int q = 0; q < HELD; ++q) {
             *reinterpret_cast<bf16x4 *>(area + q * PAIR + at) = p[q];
@@ -267,18 +293,25 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
         for (int q = 1; q < PARTS; ++q) v += float(*reinterpret_cast<const bf16 *>(p + q * ROWS));
         return v;
     };
-    // over the widths of the wave: the product of a token's row and what it gets
-    const auto dot = [&](int which, int t, const f32x4(&x)[NT]) __attribute__((always_inline)) {
+    // over the widths of the wave: the products of a token's row and what it gets
+    const auto dot = [&](int which, int t, const f32x4(&x)[NT], const f32x4(&y)[NT], auto both) __attribute__((always_inline)) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int token = 16 * t + 4 * lg + r;
-            float v = 0.0f;
+            float v = 0.0f, w = 0.0f;
             if (has)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) v += value_at(token, width(n)) * x[n][r];
-#pragma unroll
-            for (int s = 1; s < 16; s <<= 1) v += __shfl_xor(v, s);
+                for (int n = 0; n < NT; ++n) {
+                    const float at = value_at(token, width(n));
+                    v += at * x[n][r];
+                    if constexpr (decltype(both)::value) w += at * y[n][r];
+                }
+            v = sum_of_16(v);
             if (lm == 0) dots[wave][which][token] = v;
+            if constexpr (decltype(both)::value) {
+                w = sum_of_16(w);
+                if (lm == 0) dots[wave][which + 1][token] = w;
+            }
         }
     };
     f32x4 out[4][NT];
@@ -295,7 +328,7 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
                 a3[t][n][r] *= fall[i];
             }
         }
-        dot(0, t, a1[t]);
+        dot(0, t, a1[t], a1[t], std::false_type());
     }
     if (has) {
 #pragma unroll
@@ -318,8 +351,7 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
     __syncthreads();
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-        dot(1, t, a2[t]);
-        dot(2, t, a3[t]);
+        dot(1, t, a2[t], a3[t], std::true_type());
 #pragma unroll
         for (int n = 0; n < NT; ++n) out[t][n] += a3[t][n] - a2[t][n];
     }
@@ -350,15 +382,15 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
     }
     // what pairs add to dg: q k^T and k k^T of the wave's rows
     {
-        f32x4 qk[4], kk[4];
+        f32x4 qk[PT], kk[PT];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) qk[t] = kk[t] = 0;
+        for (int t = 0; t < PT; ++t) qk[t] = kk[t] = 0;
         const auto operand = [&](int tile, int ks, bf16x8(&x)[PARTS]) __attribute__((always_inline)) {
             const int row = 16 * tile + lm;
 #pragma unroll
             for (int q = 0; q < PARTS; ++q) x[q] = *reinterpret_cast<const bf16x8 *>(rows + q * ROWS + (row * G + ((4 * ks + lg) ^ turned<G>(row))) * 16);
         };
-        const int row = 16 * wave + lm;
+        const int row = 16 * row_tile + lm;
         const T *const qp = at_token<T>(a.q, a, g, g.begin, h);
 #pragma unroll
         for (int ks = 0; ks < DK / 32; ++ks) {
@@ -370,37 +402,37 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
 #pragma unroll
             for (int i = 0; i < PARTS; ++i)
                 if (!in) q[i] = bf16x8(bf16(0.0f));
-            operand(wave, ks, k);
+            operand(row_tile, ks, k);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                if (t > wave) continue;
+            for (int t = 0; t < PT; ++t) {
+                if (col_tile + t > row_tile) continue;
                 bf16x8 x[PARTS];
-                operand(t, ks, x);
+                operand(col_tile + t, ks, x);
                 qk[t] = multiply<HELD - 1>(q, x, qk[t]);
                 kk[t] = multiply<HELD - 1>(k, x, kk[t]);
             }
         }
         double of_row[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+        for (int t = 0; t < PT; ++t) {
             double of_col = 0;
-            const int j = 16 * t + lm;
+            const int j = 16 * (col_tile + t) + lm;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int i = 16 * wave + 4 * lg + r;
+                const int i = 16 * row_tile + 4 * lg + r;
                 const double w = j < i ? double(pd[t][r] * qk[t][r] + ad[t][r] * kk[t][r]) : 0.0;
                 of_row[r] += w;
                 of_col += w;
             }
             of_col += __shfl_xor(of_col, 16);
             of_col += __shfl_xor(of_col, 32);
-            if (lg == 0) col_sum[wave][j] = of_col;
+            if (lg == 0) col_sum[row_tile][j] = of_col;
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
 #pragma unroll
             for (int s = 1; s < 16; s <<= 1) of_row[r] += __shfl_xor(of_row[r], s);
-            if (lm == 0) row_sum[16 * wave + 4 * lg + r] = of_row[r];
+            if (lm == 0) row_sum[wave / 4][16 * row_tile + 4 * lg + r] = of_row[r];
         }
     }
 #pragma unroll
@@ -409,27 +441,29 @@ template <class T, int DK> __global__ void __launch_bounds__(256) delta_blocks(D
     __syncthreads();
     if (wave == 0 && a.dg.p) {
         float y = 0, z = 0, f = 0;
-        double c = 0;
+        double pairs = 0, whole = 0;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < W; ++w) {
             y += dots[w][0][l];
             z += dots[w][1][l];
             f += dots[w][2][l];
-            c += col_sum[w][l];
+            whole += between[w];
+            if (w < W / 4) pairs += row_sum[w][l];
+            if (w < 4) pairs -= col_sum[w][l];
         }
-        double after = double(y) - double(z) + row_sum[l] - c, before = f;
+        whole *= rise[63];
+        double after = double(y) - double(z) + pairs, before = f;
 #pragma unroll
         for (int s = 1; s < 64; s <<= 1) {
             const double x = __shfl_down(after, s), y2 = __shfl_up(before, s);
             if (l + s < 64) after += x;
             if (l >= s) before += y2;
         }
-        const double whole = rise[63] * (double(between[0]) + between[1] + between[2] + between[3]);
         if (l < len) *const_cast<T *>(at_token<T>(a.dg, a, g, g.begin + l, h)) = T(float(whole + (before - f) + after));
     }
     db += __shfl_xor(db, 1);
     db += __shfl_xor(db, 2);
-    if (a.dbeta.p && sgr == 0 && srow < len) *const_cast<T *>(at_token<T>(a.dbeta, a, g, g.begin + srow, h)) = T(db);
+    if (a.dbeta.p && of_states && sgr == 0 && srow < len) *const_cast<T *>(at_token<T>(a.dbeta, a, g, g.begin + srow, h)) = T(db);
     if (!has) return;
     const auto store = [&](const Heads &to, float *part, const f32x4(&x)[4][NT]) __attribute__((always_inline)) {
         if (!to.p) return;
@@ -518,7 +552,7 @@ template <class T> void delta_grad(DeltaArgs a, hipStream_t stream) {
             delta_grad_carry<DK><<<grid(a.n_seq, of_v), 256, 0, stream>>>(a);
         }
         delta_grad_walk<T, DK, kKept><<<grid(a.n_segments, of_v), 256, 0, stream>>>(a);
-        if (need && a.n_tokens) delta_blocks<T, DK><<<dim3(uint32_t(piece_ids(a, kDeltaBlock) * a.heads)), 256, 0, stream>>>(a);
+        if (need && a.n_tokens) delta_blocks<T, DK><<<dim3(uint32_t(piece_ids(a, kDeltaBlock) * a.heads)), 64 * kBlockWaves<DK>, 0, stream>>>(a);
     });
     if (a.dq_part && (a.dq.p || a.dk_out.p) && a.n_tokens) {
         const int64_t groups = std::min(ceil_div(a.n_tokens * a.dk, 256), kMostGroups);

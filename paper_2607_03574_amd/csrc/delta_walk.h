@@ -90,6 +90,11 @@ template <class T, int DK> __device__ inline void widths_operand(const char *row
 }
 #endif
 
+#ifdef __HIP_DEVICE_COMPILE__
+// Reads of memory stay on their side; arithmetic need not.
+__device__ inline void reads_stay() { __builtin_amdgcn_sched_barrier(0x000f); }
+#endif
+
 // A wave's columns of a state: widths 32 ks + 8 (l / 16) + 4 t + r of column col, [dk][cols] in memory.
 template <int DK> struct State {
     static constexpr int KS = DK / 32;
@@ -149,38 +154,59 @@ template <int DK> struct State {
 #endif
 };
 
-// A lane's eight tokens of a column: 16 (e / 4) + e % 4, and 4 (l / 16) more.  Of tokens that are not there, the last one.
-template <class T> __device__ inline void load_column(T (&v)[8], const T *p, int64_t tok, int left, uint32_t column) {
-    const uint32_t up = threadIdx.x % 64 / 16 * 4;
-    if (left == 32) {
-        const uint32_t at = here((up * uint32_t(tok) + column) * sizeof(T));
+// An address that is the same for the wave, in scalar registers.
+template <class P> __device__ inline P *same(P *p) {
+#ifdef __HIP_DEVICE_COMPILE__
+    const uint64_t v = reinterpret_cast<uint64_t>(p);
+    return reinterpret_cast<P *>(uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(v)))) |
+                                 uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(v >> 32)))) << 32);
+#else
+    return p;
+#endif
+}
+
+// A lane's eight tokens of a column: 16 (e / 4) + e % 4, and 4 (l / 16) more.  Accesses know the piece of memory that the chunk's
+// `left` tokens and `cols` columns lie in: what is beyond it is not stored, and loaded as 0 (or, of columns that are not there, as
+// any value).
+// (Bits in registers of their own: 16-bit values side by side would wait for one another.)
+template <class T> struct Bits {
+    uint32_t b[8];
+    __device__ inline void zero() {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b[e] = 0;
+    }
+#ifdef __HIP_DEVICE_COMPILE__
+    __device__ inline void load(const T *p, uint32_t tok, int left, int cols) {
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T *>(p), 0, ((left - 1) * tok + cols) * sizeof(T), 0x00020000);
+        const uint32_t at = (threadIdx.x % 64 / 16 * 4 * tok + threadIdx.x % 16) * sizeof(T);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            v[e] = get<T>(p, at);
-            p += e == 3 ? 13 * tok : tok;
+            const uint32_t off = at + (16 * (e / 4) + e % 4) * tok * uint32_t(sizeof(T));
+            if constexpr (sizeof(T) == 4) b[e] = __builtin_amdgcn_raw_buffer_load_b32(rsrc, off, 0, 0);
+            else b[e] = __builtin_amdgcn_raw_buffer_load_b16(rsrc, off, 0, 0);
         }
-    } else {
+    }
+#endif
+    __device__ inline float value(int e) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(b[e]);
+        else if constexpr (std::is_same<T, bf16>::value) return __uint_as_float(b[e] << 16);
+        else return float(__builtin_bit_cast(f16, uint16_t(b[e])));
+    }
+};
+#ifdef __HIP_DEVICE_COMPILE__
+template <class T> __device__ inline void store_column(T *p, uint32_t tok, int left, int cols, const f32x4 (&v)[2]) {
+    if (left == 1) tok = 256;       // (rows need not be apart where there is one)
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(p, 0, ((left - 1) * tok + cols) * sizeof(T), 0x00020000);
+    const uint32_t at = (threadIdx.x % 64 / 16 * 4 * tok + threadIdx.x % 16) * sizeof(T);
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            v[e] = get<T>(p, (min(16 * (e / 4) + e % 4 + up, uint32_t(left - 1)) * uint32_t(tok) + column) * sizeof(T));
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t off = at + (16 * (e / 4) + e % 4) * tok * uint32_t(sizeof(T));
+        const T x = T(v[e / 4][e % 4]);
+        if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, x), rsrc, off, 0, 0);
+        else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, x), rsrc, off, 0, 0);
     }
 }
-template <class T, class F> __device__ inline void store_column(T *p, int64_t tok, int left, F f) {
-    const uint32_t up = threadIdx.x % 64 / 16 * 4, at = here((up * uint32_t(tok) + threadIdx.x % 16) * sizeof(T));
-    if (left == 32) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            set<T>(p, at, f(e));
-            p += e == 3 ? 13 * tok : tok;
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (16 * (e / 4) + e % 4 + int(up) < left) set<T>(p, at, f(e));
-            p += e == 3 ? 13 * tok : tok;
-        }
-    }
-}
+#endif
 
 // Forwards.  tile: the wave's columns; from ceil(dv / 16) on (kSums) those of what the piece makes of a state.
 // (Inlined by force: called, its arrays would live in memory.)
@@ -191,6 +217,7 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const
     constexpr int MATRIX = kRows<T, DK>, READ = kRead<T, WALK>, SLOT = MATRIX * (OUT ? 2 : 1) + READ;
     const int l = threadIdx.x % 64, lm = l % 16, lg = l / 16;
     const int dk = int(a.dk), dv = int(a.dv), dkp = int(a.dkp), dvp = int(a.dvp), tiles = (dv + 15) / 16;
+    const float scale = a.scale;
     const bool moves = WALK == kSums && tile >= tiles;
     const int cols = moves ? dk : dv, col0 = (moves ? tile - tiles : tile) * 16, col = col0 + lm;
     const bool works = col0 < cols;
@@ -207,25 +234,21 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const
     else if (a.state_in) S.load(a.state_in + (g.seq * a.heads + h) * states, dk, dv, dv, col0);
     else S.fill(0.0f);
 
-    const T *kp = at_token<T>(a.k, a, g, g.begin, h), *qp = OUT ? at_token<T>(a.q, a, g, g.begin, h) : nullptr;
-    const T *vp = at_token<T>(a.v, a, g, g.begin, h) + (moves ? 0 : col0);
-    T *op = OUT ? const_cast<T *>(at_token<T>(a.o, a, g, g.begin, h)) + col0 : nullptr;
-    float *mp = WALK == kKept ? a.m + (h * a.n_tokens + g.first + g.begin) * a.dvp + col0 : nullptr;
-    const uint32_t column = uint32_t(min(lm, max(cols - 1 - col0, 0)));
+    const T *const kp = same(at_token<T>(a.k, a, g, g.begin, h)), *const qp = same(at_token<T>(a.q, a, g, g.begin, h));
+    const T *const vp = same(at_token<T>(a.v, a, g, g.begin, h) + (moves ? 0 : col0));
+    T *const op = OUT ? same(const_cast<T *>(at_token<T>(a.o, a, g, g.begin, h)) + col0) : nullptr;
+    float *const mp = WALK == kKept ? same(a.m + (h * a.n_tokens + g.first + g.begin) * a.dvp + col0) : nullptr;
     Stage<T, DK> rk, rq;
     StageRecord<READ, READ, 0> record;
-    T v_next[8];
-    // values of v: of columns and tokens that are not there, those of the last ones; they reach nothing
+    Bits<T> v_next, v_now;
     const auto fetch = [&](int c) __attribute__((always_inline)) {
         const int left = left_of(c);
         record.fetch(a.chunks + ((chunk0 + c) * a.heads + h) * a.record);
         rk.fetch(kp + int64_t(c) * 32 * a.k.tok, uint32_t(a.k.tok), left, dkp);
         if constexpr (OUT) rq.fetch(qp + int64_t(c) * 32 * a.q.tok, uint32_t(a.q.tok), left, dkp);
         const T *v = vp + int64_t(c) * 32 * a.v.tok;
-        if (moves || !works)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v_next[e] = T(0.0f);
-        else load_column(v_next, v, a.v.tok, left, column);
+        if (moves || !works) v_next.zero();
+        else v_next.load(v, uint32_t(a.v.tok), left, min(16, cols - col0));
     };
     const auto put = [&](int c) __attribute__((always_inline)) {
         char *to = lds + c % BUFFERS * SLOT;
@@ -235,14 +258,12 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const
     };
 
     // the state before a block
-    float *kept = WALK == kKept ? a.states + ((first_piece(a, g.seq, kDeltaBlock) + g.begin / kDeltaBlock) * a.heads + h) * dk * dvp : nullptr;
+    float *const kept = WALK == kKept ? same(a.states + ((first_piece(a, g.seq, kDeltaBlock) + g.begin / kDeltaBlock) * a.heads + h) * dk * dvp) : nullptr;
     const auto keep = [&](int c) __attribute__((always_inline)) { S.store(kept + int64_t(c / 2) * a.heads * dk * dvp, dk, dv, dvp, col0); };
-    T v_now[8];
     if (chunks) {
         fetch(0);
         put(0);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v_now[e] = v_next[e];
+        v_now = v_next;
     }
     if (WALK == kKept && works && chunks) keep(0);
     __syncthreads();
@@ -254,22 +275,36 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const
         f32x4 o[2];
         int first = 32;
         if (works) {
-            // Y = K S, Z = Q S
+            // Y = K S, Z = Q S; LDS is read one step ahead of what needs it
             f32x4 y[2], z[2], beta[2], rise[2], fall[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) y[i] = z[i] = 0;
+            bf16x8 kx[2][2][PARTS], qx[2][2][PARTS], tx[2][SP];
+            const auto read_rows = [&](int ks) __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    rows_operand<T, DK>(k, i, ks, kx[ks % 2][i]);
+                    if constexpr (OUT) rows_operand<T, DK>(q, i, ks, qx[ks % 2][i]);
+                }
+            };
+            read_rows(0);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                bf16x8 s[SP], x[PARTS];
+                if (ks + 1 < KS) {
+                    read_rows(ks + 1);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int p = 0; p < SP; ++p) tx[i][p] = *reinterpret_cast<const bf16x8 *>(matrices + (i * SP + p) * kTile);
+                }
+                reads_stay();
+                bf16x8 s[SP];
                 S.operand(ks, s);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    rows_operand<T, DK>(k, i, ks, x);
-                    y[i] = multiply<SP - 1>(x, s, y[i]);
-                    if constexpr (OUT) {
-                        rows_operand<T, DK>(q, i, ks, x);
-                        z[i] = multiply<HELD - 1>(x, s, z[i]);
-                    }
+                    y[i] = multiply<SP - 1>(kx[ks % 2][i], s, y[i]);
+                    if constexpr (OUT) z[i] = multiply<HELD - 1>(qx[ks % 2][i], s, z[i]);
                 }
             }
 #pragma unroll
@@ -286,7 +321,7 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const
             bool odd = false;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                v[e] = float(v_now[e]);
+                v[e] = v_now.value(e);
                 odd |= !finite(v[e]);
             }
             if (__ballot(odd)) {
@@ -303,14 +338,16 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const
             bf16x8 x[SP], w[SP], u[HELD];
 #pragma unroll
             for (int e = 0; e < 8; ++e) split(token_of(e) < fit ? v[e] - rise[e / 4][e % 4] * y[e / 4][e % 4] : 0.0f, x, e);
+            bf16x8 kt[2][2][PARTS], px[OUT ? 2 : 1][OUT ? HELD : 1];
+            const auto read_widths = [&](int ks) __attribute__((always_inline)) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) widths_operand<T, DK>(k, ks, t, kt[ks % 2][t]);
+            };
+            read_widths(0);
+            reads_stay();
             f32x4 m[2];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                bf16x8 t[SP];
-#pragma unroll
-                for (int p = 0; p < SP; ++p) t[p] = *reinterpret_cast<const bf16x8 *>(matrices + (i * SP + p) * kTile);
-                m[i] = multiply<SP - 1>(t, x, f32x4{0, 0, 0, 0});
-            }
+            for (int i = 0; i < 2; ++i) m[i] = multiply<SP - 1>(tx[i], x, f32x4{0, 0, 0, 0});
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float ue = beta[e / 4][e % 4] * m[e / 4][e % 4];
@@ -319,20 +356,23 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const
             }
             // S' = exp(G_last) S + K^T (fall U)
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
+            for (int ks = 0; ks < KS; ++ks) {
+                if (ks + 1 < KS) {
+                    read_widths(ks + 1);
+                } else if constexpr (OUT) {
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    bf16x8 kt[PARTS];
-                    widths_operand<T, DK>(k, ks, t, kt);
-                    S.s[ks][t] = multiply<SP - 1>(kt, w, S.s[ks][t] * whole);
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int p = 0; p < HELD; ++p) px[i][p] = *reinterpret_cast<const bf16x8 *>(matrices + kRecordMatrix + (i * HELD + p) * kTile);
                 }
+                reads_stay();
+#pragma unroll
+                for (int t = 0; t < 2; ++t) S.s[ks][t] = multiply<SP - 1>(kt[ks % 2][t], w, S.s[ks][t] * whole);
+            }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 if constexpr (OUT) {
-                    bf16x8 p[HELD];
-#pragma unroll
-                    for (int j = 0; j < HELD; ++j) p[j] = *reinterpret_cast<const bf16x8 *>(matrices + kRecordMatrix + (i * HELD + j) * kTile);
-                    o[i] = multiply<HELD - 1>(p, u, rise[i] * z[i]) * a.scale;
+                    o[i] = multiply<HELD - 1>(px[i], u, rise[i] * z[i]) * scale;
                 } else {
                     o[i] = m[i];
                 }
@@ -346,8 +386,7 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const
         if (BUFFERS == 1) __syncthreads();
         if (c + 1 < chunks) {
             put(c + 1);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v_now[e] = v_next[e];
+            v_now = v_next;
         }
         // (what is stored comes behind the wait for what the next chunk brings)
         if (WALK == kKept && works && c % 2 && c + 1 < chunks) keep(c + 1);
@@ -355,8 +394,9 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk(const
             if (__ballot(first < left))
 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[e / 4][e % 4] = token_of(e) < first ? o[e / 4][e % 4] : __builtin_nanf("");
-            if constexpr (OUT) store_column(op + int64_t(c) * 32 * a.o.tok, a.o.tok, left, [&](int e) { return T(o[e / 4][e % 4]); });
-            else store_column(mp + int64_t(c) * 32 * dvp, dvp, left, [&](int e) { return col < dv ? o[e / 4][e % 4] : 0.0f; });
+            if (!OUT && col >= dv) o[0] = o[1] = 0;
+            if constexpr (OUT) store_column(op + int64_t(c) * 32 * a.o.tok, uint32_t(a.o.tok), left, min(16, dv - col0), o);
+            else store_column(mp + int64_t(c) * 32 * dvp, uint32_t(dvp), left, min(16, dvp - col0), o);
         }
         __syncthreads();
     }
@@ -393,21 +433,20 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk_back(
     else if (a.d_state_out) D.load(a.d_state_out + (g.seq * a.heads + h) * states, dk, dv, dv, col0);
     else D.fill(0.0f);
 
-    const T *kp = at_token<T>(a.k, a, g, g.begin, h), *qp = at_token<T>(a.q, a, g, g.begin, h);
-    const T *dp = at_token<T>(a.d_o, a, g, g.begin, h) + col0;
-    T *vp = WALK == kKept && a.dv_out.p ? const_cast<T *>(at_token<T>(a.dv_out, a, g, g.begin, h)) + col0 : nullptr;
-    float *ep = WALK == kKept && a.e ? a.e + (h * a.n_tokens + g.first + g.begin) * a.dvp + col0 : nullptr;
-    const uint32_t column = uint32_t(min(lm, max(dv - 1 - col0, 0)));
+    const T *const kp = same(at_token<T>(a.k, a, g, g.begin, h)), *const qp = same(at_token<T>(a.q, a, g, g.begin, h));
+    const T *const dp = same(at_token<T>(a.d_o, a, g, g.begin, h) + col0);
+    T *const vp = WALK == kKept && a.dv_out.p ? same(const_cast<T *>(at_token<T>(a.dv_out, a, g, g.begin, h)) + col0) : nullptr;
+    float *const ep = WALK == kKept && a.e ? same(a.e + (h * a.n_tokens + g.first + g.begin) * a.dvp + col0) : nullptr;
     Stage<T, DK> rk, rq;
     StageRecord<READ, kRecordHead, kRecordMatrix> record;
-    T d_next[8], d_now[8];
+    Bits<T> d_next, d_now;
     const auto fetch = [&](int c) __attribute__((always_inline)) {
         const int left = left_of(c);
         record.fetch(a.chunks + ((chunk0 + c) * a.heads + h) * a.record);
         rk.fetch(kp + int64_t(c) * 32 * a.k.tok, uint32_t(a.k.tok), left, dkp);
         rq.fetch(qp + int64_t(c) * 32 * a.q.tok, uint32_t(a.q.tok), left, dkp);
         const T *d = dp + int64_t(c) * 32 * a.d_o.tok;
-        if (works) load_column(d_next, d, a.d_o.tok, left, column);      // (of columns that are not there, the last one's)
+        if (works) d_next.load(d, uint32_t(a.d_o.tok), left, min(16, dv - col0));
     };
     const auto put = [&](int c) __attribute__((always_inline)) {
         char *to = lds + c % BUFFERS * SLOT;
@@ -417,13 +456,12 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk_back(
     };
 
     // the gradient of the state after a block
-    float *kept = WALK == kKept && a.d_states ? a.d_states + ((first_piece(a, g.seq, kDeltaBlock) + g.begin / kDeltaBlock) * a.heads + h) * dk * dvp : nullptr;
+    float *const kept = WALK == kKept && a.d_states ? same(a.d_states + ((first_piece(a, g.seq, kDeltaBlock) + g.begin / kDeltaBlock) * a.heads + h) * dk * dvp) : nullptr;
     const auto keep = [&](int c) __attribute__((always_inline)) { D.store(kept + int64_t(c / 2) * a.heads * dk * dvp, dk, dv, dvp, col0); };
     if (chunks) {
         fetch(chunks - 1);
         put(chunks - 1);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) d_now[e] = d_next[e];
+        d_now = d_next;
     }
     if (kept && works && chunks) keep(chunks - 1);
     __syncthreads();
@@ -437,15 +475,27 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk_back(
             f32x4 w[2], o[2], beta[2], rise[2], fall[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) w[i] = 0;
+            bf16x8 kx[2][2][PARTS], tx[2][SP];
+            const auto read_rows = [&](int ks) __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) rows_operand<T, DK>(k, i, ks, kx[ks % 2][i]);
+            };
+            const auto read_matrix = [&](const char *from) __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int p = 0; p < SP; ++p) tx[i][p] = *reinterpret_cast<const bf16x8 *>(from + (i * SP + p) * kTile);
+            };
+            read_rows(0);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                bf16x8 s[SP], x[PARTS];
+                if (ks + 1 < KS) read_rows(ks + 1);
+                else read_matrix(matrices + kRecordMatrix);
+                reads_stay();
+                bf16x8 s[SP];
                 D.operand(ks, s);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    rows_operand<T, DK>(k, i, ks, x);
-                    w[i] = multiply<SP - 1>(x, s, w[i]);
-                }
+                for (int i = 0; i < 2; ++i) w[i] = multiply<SP - 1>(kx[ks % 2][i], s, w[i]);
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -456,56 +506,59 @@ template <class T, int DK, Walk WALK> __device__ __forceinline__ void walk_back(
             bf16x8 od[PARTS], du[SP], x[SP];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if (token_of(e) >= left) d_now[e] = T(0.0f);
-                split(float(d_now[e]), od, e);
+                if (token_of(e) >= left) d_now.b[e] = 0;
+                split(d_now.value(e), od, e);
             }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                bf16x8 t[SP];
-#pragma unroll
-                for (int p = 0; p < SP; ++p) t[p] = *reinterpret_cast<const bf16x8 *>(matrices + kRecordMatrix + (i * SP + p) * kTile);
-                o[i] = multiply<SP - 1>(t, od, f32x4{0, 0, 0, 0}) * a.scale + fall[i] * w[i];
-            }
+            for (int i = 0; i < 2; ++i) o[i] = multiply<SP - 1>(tx[i], od, f32x4{0, 0, 0, 0}) * a.scale + fall[i] * w[i];
+            read_matrix(matrices);
+            reads_stay();
 #pragma unroll
             for (int e = 0; e < 8; ++e) split(o[e / 4][e % 4], du, e);
+            bf16x8 kt[2][2][PARTS], qt[2][2][PARTS];
+            const auto read_widths = [&](int ks) __attribute__((always_inline)) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    widths_operand<T, DK>(q, ks, t, qt[ks % 2][t]);
+                    widths_operand<T, DK>(k, ks, t, kt[ks % 2][t]);
+                }
+            };
+            read_widths(0);
+            reads_stay();
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                bf16x8 t[SP];
-#pragma unroll
-                for (int p = 0; p < SP; ++p) t[p] = *reinterpret_cast<const bf16x8 *>(matrices + (i * SP + p) * kTile);
-                e_now[i] = multiply<SP - 1>(t, du, f32x4{0, 0, 0, 0});
+                e_now[i] = multiply<SP - 1>(tx[i], du, f32x4{0, 0, 0, 0});
                 x_now[i] = beta[i] * e_now[i];
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float up = rise[e / 4][e % 4];
-                split(up * a.scale * float(d_now[e]), du, e);
+                split(up * a.scale * d_now.value(e), du, e);
                 split(-up * x_now[e / 4][e % 4], x, e);
             }
             const float whole = head->bad < left ? __builtin_nanf("") : head->whole;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
+            for (int ks = 0; ks < KS; ++ks) {
+                if (ks + 1 < KS) read_widths(ks + 1);
+                reads_stay();
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    bf16x8 kt[PARTS];
-                    f32x4 d = D.s[ks][t] * whole;
-                    widths_operand<T, DK>(q, ks, t, kt);
-                    d = multiply<SP - 1>(kt, du, d);
-                    widths_operand<T, DK>(k, ks, t, kt);
-                    D.s[ks][t] = multiply<SP - 1>(kt, x, d);
+                    const f32x4 d = multiply<SP - 1>(qt[ks % 2][t], du, D.s[ks][t] * whole);
+                    D.s[ks][t] = multiply<SP - 1>(kt[ks % 2][t], x, d);
                 }
+            }
         }
         if (BUFFERS == 1) __syncthreads();
         if (c > 0) {
             put(c - 1);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) d_now[e] = d_next[e];
+            d_now = d_next;
         }
         // (what is stored comes behind the wait for what the next chunk brings)
         if (kept && works && c && c % 2 == 0) keep(c - 1);
         if (WALK == kKept && works && col < dvp) {
-            if (ep) store_column(ep + int64_t(c) * 32 * dvp, dvp, left, [&](int e) { return col < dv ? e_now[e / 4][e % 4] : 0.0f; });
-            if (vp && col < dv) store_column(vp + int64_t(c) * 32 * a.dv_out.tok, a.dv_out.tok, left, [&](int e) { return T(x_now[e / 4][e % 4]); });
+            if (col >= dv) e_now[0] = e_now[1] = 0;
+            if (ep) store_column(ep + int64_t(c) * 32 * dvp, uint32_t(dvp), left, min(16, dvp - col0), e_now);
+            if (vp && col < dv) store_column(vp + int64_t(c) * 32 * a.dv_out.tok, uint32_t(a.dv_out.tok), left, min(16, dv - col0), x_now);
         }
         __syncthreads();
     }
