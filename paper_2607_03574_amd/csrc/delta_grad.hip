@@ -105,25 +105,6 @@ template <class T, int DK> __global__ void __launch_bounds__(64 * kBlockWaves<DK
         }
     };
     fetch_rows(a.q);
-    put_rows();
-    if (wave == 0) {
-        double log_a = 0.0;
-        float beta = 0.0f;
-        if (l < len) {
-            beta = float(*at_token<T>(a.beta, a, g, g.begin + l, h));
-            log_a = log_decay(*at_token<T>(a.g, a, g, g.begin + l, h));
-        }
-#pragma unroll
-        for (int s = 1; s < 64; s <<= 1) {
-            const double before = __shfl_up(log_a, s);
-            if (l >= s) log_a += before;
-        }
-        sum[l] = log_a;
-        betas[l] = beta;
-        rise[l] = expf(float(log_a));
-        fall[l] = expf(float(__shfl(log_a, 63) - log_a));
-    }
-
     // over 32 columns of v after the other: do S^T, X S^T, U D^T, do U^T, X U^T, e.m and <D, S>
     // (of eight waves, four bring u and x, the others do)
     const int srow = threadIdx.x % 256 / 4, sgr = threadIdx.x % 4;
@@ -150,6 +131,26 @@ template <class T, int DK> __global__ void __launch_bounds__(64 * kBlockWaves<DK
             get_eight(D[n], dp, at);
         }
     };
+    fetch(0);
+    put_rows();
+    if (wave == 0) {
+        double log_a = 0.0;
+        float beta = 0.0f;
+        if (l < len) {
+            beta = float(*at_token<T>(a.beta, a, g, g.begin + l, h));
+            log_a = log_decay(*at_token<T>(a.g, a, g, g.begin + l, h));
+        }
+#pragma unroll
+        for (int s = 1; s < 64; s <<= 1) {
+            const double before = __shfl_up(log_a, s);
+            if (l >= s) log_a += before;
+        }
+        sum[l] = log_a;
+        betas[l] = beta;
+        rise[l] = expf(float(log_a));
+        fall[l] = expf(float(__shfl(log_a, 63) - log_a));
+    }
+
     f32x4 a1[4][NT], a2[4][NT], a3[4][NT], pd[PT], ad[PT];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -159,7 +160,6 @@ template <class T, int DK> __global__ void __launch_bounds__(64 * kBlockWaves<DK
     }
     float db = 0.0f, ds = 0.0f;
     char *const of_u = area, *const of_x = area + HELD * SLAB, *const of_o = area + 2 * HELD * SLAB;
-    fetch(0);
     for (int c = 0; c < dvp; c += 32) {
         __syncthreads();
         {
@@ -465,24 +465,30 @@ template <class T, int DK> __global__ void __launch_bounds__(64 * kBlockWaves<DK
     db += __shfl_xor(db, 2);
     if (a.dbeta.p && of_states && sgr == 0 && srow < len) *const_cast<T *>(at_token<T>(a.dbeta, a, g, g.begin + srow, h)) = T(db);
     if (!has) return;
+    // (the piece of memory that the block's rows lie in: what is beyond it is not stored)
+    const auto rows_to = [&](auto *p, uint32_t step, const f32x4(&x)[4][NT]) __attribute__((always_inline)) {
+        typedef std::remove_pointer_t<decltype(p)> V;
+        if (len == 1) step = 256;       // (rows need not be apart where there is one)
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(same(p), 0, ((len - 1) * step + uint32_t(a.dk)) * sizeof(V), 0x00020000);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            if (width(n) >= a.dk) continue;
+            const uint32_t at = (4 * lg * step + width(n)) * sizeof(V);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const uint32_t off = at + (16 * t + r) * step * uint32_t(sizeof(V));
+                    const V v = V(x[t][n][r]);
+                    if constexpr (sizeof(V) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), rsrc, off, 0, 0);
+                    else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), rsrc, off, 0, 0);
+                }
+        }
+    };
     const auto store = [&](const Heads &to, float *part, const f32x4(&x)[4][NT]) __attribute__((always_inline)) {
         if (!to.p) return;
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int token = 16 * t + 4 * lg + r;
-                if (token >= len) continue;
-                T *at = part ? nullptr : const_cast<T *>(at_token<T>(to, a, g, g.begin + token, h));
-                float *wide = part ? part + (h * a.n_tokens + g.first + g.begin + token) * a.dk : nullptr;
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const int64_t d = width(n);
-                    if (d >= a.dk) continue;
-                    if (part) wide[d] = x[t][n][r];
-                    else at[d] = T(x[t][n][r]);
-                }
-            }
+        if (part) rows_to(part + (h * a.n_tokens + g.first + g.begin) * a.dk, uint32_t(a.dk), x);
+        else rows_to(const_cast<T *>(at_token<T>(to, a, g, g.begin, h)), uint32_t(to.tok), x);
     };
     store(a.dq, a.dq_part, a1);
     store(a.dk_out, a.dk_part, out);

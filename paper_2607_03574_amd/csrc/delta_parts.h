@@ -171,7 +171,7 @@ inline int64_t piece_ids(const DeltaArgs &a, int64_t len) {
 // Token t of a sequence, head h.
 template <class T> __device__ inline const T *at_token(const Heads &x, const DeltaArgs &a, const Piece &g, int64_t t, int64_t h) {
     const int64_t row = a.offsets ? (g.first + t) * x.tok : g.seq * x.seq + t * x.tok;
-    return static_cast<const T *>(x.p) + row + h / x.group * x.head;
+    return static_cast<const T *>(x.p) + row + int64_t(uint32_t(h) / uint32_t(x.group)) * x.head;
 }
 
 // The record of a chunk and head: 32 values each of b, exp G and exp(G_last - G), exp(G_last), and the first token whose k,

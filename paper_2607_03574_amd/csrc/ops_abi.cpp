@@ -633,7 +633,7 @@ ndvm_status ndvm_delta_attention_grad(const ndvm_delta_shape *shape, const ndvm_
             if (!x || bad_heads(x, 0)) return bad(who, "null argument or bad stride");
             wanted |= x->data != nullptr;
         }
-        if (const ndvm_status st = check_rows_near(who, {q, k, v, d_o, dv})) return st;
+        if (const ndvm_status st = check_rows_near(who, {q, k, v, d_o, dq, dk, dv})) return st;
         if (s->n_seq == 0 || !wanted) return NDVM_OK;
         const size_t need = delta_need(s, offsets != nullptr, true);
         if (workspace_bytes < need) return fail(NDVM_E_NOMEM, who, "workspace too small");
