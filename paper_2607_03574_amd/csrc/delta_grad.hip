@@ -45,8 +45,10 @@ template <int DK> __global__ void __launch_bounds__(256) delta_grad_carry(DeltaA
 // A block's LDS: 32 columns of u, x and do as parts, later the pairs' matrices; the rows of q, later of k.
 template <class T> constexpr int kSlab = 64 * 64;      // bytes of 32 columns of a part
 template <class T> constexpr int kPair = 64 * 128;     // of a part of a pairs' matrix, [j][i]
-template <class T> constexpr int kArea = 2 * kResultParts<T> * kPair<T>;
-static_assert((2 * kResultParts<float> + kInputParts<float>) * kSlab<float> <= kArea<float>, "");
+template <class T> constexpr int kSlabs = (2 * kResultParts<T> + kInputParts<T>) * kSlab<T>;
+// two lots of columns, where there is room
+template <class T, int DK> constexpr int kLots = kInputParts<T> * DK <= 512 ? 2 : 1;
+template <class T, int DK> constexpr int kArea = std::max(kLots<T, DK> * kSlabs<T>, 2 * kResultParts<T> * kPair<T>);
 
 // Over the 16 lanes of a row, in all of them.
 __device__ inline float sum_of_16(float v) {
@@ -64,12 +66,14 @@ __device__ inline float sum_of_16(float v) {
 
 // W waves and a block: a wave has 64 tokens x 16 NT widths of dq and dk, and 16 rows x 16 PT columns of the pairs' matrices.
 template <int DK> constexpr int kBlockWaves = DK >= 128 ? 8 : 4;
-template <class T, int DK> __global__ void __launch_bounds__(64 * kBlockWaves<DK>) delta_blocks(DeltaArgs a) {
+// waves on a matrix unit
+template <class T, int DK> constexpr int kBlockResident = DK >= 128 || kInputParts<T> == 1 ? 2 : 1;
+template <class T, int DK> __global__ void __launch_bounds__(64 * kBlockWaves<DK>, (kBlockResident<T, DK>)) delta_blocks(DeltaArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int W = kBlockWaves<DK>, THREADS = 64 * W, PT = 16 / W;
     constexpr int PARTS = kInputParts<T>, HELD = kResultParts<T>, NT = DK <= 16 * W ? 1 : DK / (16 * W), G = DK / 8, ROWS = 64 * G * 16;
     constexpr int LOADS = 64 * G / THREADS, SLAB = kSlab<T>, PAIR = kPair<T>;
-    __shared__ __align__(16) char area[kArea<T>], rows[PARTS * ROWS];
+    __shared__ __align__(16) char area[kArea<T, DK>], rows[PARTS * ROWS];
     __shared__ double sum[64], row_sum[W / 4][64], col_sum[4][64];
     __shared__ float betas[64], rise[64], fall[64], dots[W][3][64], between[W];
     const uint32_t id = blockIdx.x / uint32_t(a.heads);
@@ -159,34 +163,36 @@ template <class T, int DK> __global__ void __launch_bounds__(64 * kBlockWaves<DK
         for (int n = 0; n < NT; ++n) a1[i][n] = a2[i][n] = a3[i][n] = 0;
     }
     float db = 0.0f, ds = 0.0f;
-    char *const of_u = area, *const of_x = area + HELD * SLAB, *const of_o = area + 2 * HELD * SLAB;
-    for (int c = 0; c < dvp; c += 32) {
-        __syncthreads();
-        {
-            const bool in = srow < len && c + sgr * 8 < dvp;
-            const int at = srow * 64 + (sgr ^ turned<4>(srow)) * 16;
-            if (of_states) {
-                bf16x8 u[HELD], x[HELD];
+    const auto put = [&](int c) __attribute__((always_inline)) {
+        char *const of_u = area + c / 32 % kLots<T, DK> * kSlabs<T>, *const of_x = of_u + HELD * SLAB, *const of_o = of_x + HELD * SLAB;
+        const bool in = srow < len && c + sgr * 8 < dvp;
+        const int at = srow * 64 + (sgr ^ turned<4>(srow)) * 16;
+        if (of_states) {
+            bf16x8 u[HELD], x[HELD];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float mi = in ? value(m, i) : 0.0f, ei = in ? value(e, i) : 0.0f;
-                    db += ei * mi;
-                    split(beta * mi, u, i);
-                    split(beta * ei, x, i);
-                }
-#pragma unroll
-                for (int q = 0; q < HELD; ++q) {
-                    *reinterpret_cast<bf16x8 *>(of_u + q * SLAB + at) = u[q];
-                    *reinterpret_cast<bf16x8 *>(of_x + q * SLAB + at) = x[q];
-                }
+            for (int i = 0; i < 8; ++i) {
+                const float mi = in ? value(m, i) : 0.0f, ei = in ? value(e, i) : 0.0f;
+                db += ei * mi;
+                split(beta * mi, u, i);
+                split(beta * ei, x, i);
             }
-            if (of_do) {
-                bf16x8 p[PARTS];
-                parts_of(o, p);
 #pragma unroll
-                for (int q = 0; q < PARTS; ++q) *reinterpret_cast<bf16x8 *>(of_o + q * SLAB + at) = in ? p[q] : bf16x8(bf16(0.0f));
+            for (int q = 0; q < HELD; ++q) {
+                *reinterpret_cast<bf16x8 *>(of_u + q * SLAB + at) = u[q];
+                *reinterpret_cast<bf16x8 *>(of_x + q * SLAB + at) = x[q];
             }
         }
+        if (of_do) {
+            bf16x8 p[PARTS];
+            parts_of(o, p);
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) *reinterpret_cast<bf16x8 *>(of_o + q * SLAB + at) = in ? p[q] : bf16x8(bf16(0.0f));
+        }
+    };
+    put(0);
+    __syncthreads();
+    for (int c = 0; c < dvp; c += 32) {
+        const char *const of_u = area + c / 32 % kLots<T, DK> * kSlabs<T>, *const of_x = of_u + HELD * SLAB, *const of_o = of_x + HELD * SLAB;
         bf16x8 s[NT][HELD], d[NT][HELD];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -201,7 +207,6 @@ template <class T, int DK> __global__ void __launch_bounds__(64 * kBlockWaves<DK
             for (int q = 0; q < HELD; ++q)
                 if (!in) s[n][q] = d[n][q] = bf16x8(bf16(0.0f));
         }
-        __syncthreads();
         if (c + 32 < dvp) fetch(c + 32);
         const auto operand = [&](const char *from, int tile, auto &x) __attribute__((always_inline)) {
             const int row = 16 * tile + lm;
@@ -231,8 +236,10 @@ template <class T, int DK> __global__ void __launch_bounds__(64 * kBlockWaves<DK
                 ad[t % PT] = multiply<HELD - 1>(own_x, u, ad[t % PT]);
             }
         }
+        if (kLots<T, DK> == 1) __syncthreads();
+        if (c + 32 < dvp) put(c + 32);
+        __syncthreads();
     }
-    __syncthreads();
     fetch_rows(a.k);
     // Pd and Ad, transposed, where the columns of v lay
 #pragma unroll
