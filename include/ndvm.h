@@ -611,7 +611,7 @@ ndvm_status ndvm_delta_attention(const ndvm_delta_shape *shape, const ndvm_heads
  * head, and its gradient.  A value of g below -128 has gradient 0.  What is not finite in a
  * head of a sequence may reach all of that head's gradients in that sequence, and those of
  * the heads of q and k it reads; other sequences and heads keep theirs.  Tokens of no
- * sequence are left as they are.
+ * sequence are left as they are.  At most 2^23 - 1 pairs of 64 tokens of a sequence and a head.
  */
 ndvm_status ndvm_delta_attention_grad(const ndvm_delta_shape *shape, const ndvm_heads *q, const ndvm_heads *k,
                                       const ndvm_heads *v, const ndvm_heads *g, const ndvm_heads *beta,

@@ -550,7 +550,13 @@ static ndvm_status check_delta_inputs(const char *who, const ndvm_delta_shape *s
     return NDVM_OK;
 }
 
-// The kernels count the 32 rows of a chunk in 32 bits.
+// The gradient's workgroups are of 512 threads.
+static ndvm_status check_delta_grad(const char *who, const ndvm_delta_shape *s) {
+    if ((s->n_tokens / kDeltaBlock + s->n_seq) * s->heads > kMostGroups / 2) return fail(NDVM_E_UNSUPPORTED, who, "too many tokens and heads");
+    return NDVM_OK;
+}
+
+// The kernels count the rows of a chunk or block in 32 bits.
 static ndvm_status check_rows_near(const char *who, std::initializer_list<const ndvm_heads *> all) {
     for (const ndvm_heads *x : all)
         if (x->tok_stride >= int64_t(1) << 24) return fail(NDVM_E_UNSUPPORTED, who, "rows are 2^24 values apart, or more");
@@ -591,6 +597,8 @@ ndvm_status ndvm_delta_attention_workspace_bytes(const ndvm_delta_shape *shape, 
         const char *who = "ndvm_delta_attention_workspace_bytes";
         if (!bytes) return bad(who, "null pointer");
         if (const ndvm_status st = check_delta(who, shape, true, packed != 0)) return st;
+        if (with_grad)
+            if (const ndvm_status st = check_delta_grad(who, shape)) return st;
         *bytes = delta_need(shape, packed != 0, with_grad != 0);
         return NDVM_OK;
     });
@@ -626,6 +634,7 @@ ndvm_status ndvm_delta_attention_grad(const ndvm_delta_shape *shape, const ndvm_
         const char *who = "ndvm_delta_attention_grad";
         const ndvm_delta_shape *s = shape;
         if (const ndvm_status st = check_delta(who, s, true, offsets != nullptr)) return st;
+        if (const ndvm_status st = check_delta_grad(who, s)) return st;
         if (const ndvm_status st = check_delta_inputs(who, s, s->n_tokens, q, k, v, g, beta)) return st;
         if (!d_o || bad_heads(d_o, s->n_tokens)) return bad(who, "null buffer or bad stride");
         bool wanted = d_initial != nullptr;

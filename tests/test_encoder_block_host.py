@@ -204,6 +204,9 @@ def test_delta_refusals():
     assert nd._delta_ws(shape(heads=65535, qk_heads=65535, n_seq=1, n_tokens=1 << 12, dk=256, dv=256), 0, 1, ctypes.byref(n)) == nd.OK
     assert n.value > 1 << 40
     assert nd._delta_ws(shape(heads=65535, qk_heads=65535, n_seq=1, n_tokens=1 << 13), 0, 1, ctypes.byref(n)) == nd.E_UNSUPPORTED
+    many = shape(n_seq=1 << 23, n_tokens=0, heads=1, qk_heads=1)
+    assert nd._delta_ws(many, 1, 0, ctypes.byref(n)) == nd.OK and nd._delta_ws(many, 1, 1, ctypes.byref(n)) == nd.E_UNSUPPORTED
+    assert gradient(many) == nd.E_UNSUPPORTED
     assert nd._delta_ws(shape(), 1, 1, None) == nd.E_ARG
 
 
