@@ -103,7 +103,7 @@ template <class E, class T, int TB, int NW> __global__ void __launch_bounds__(64
             float value, slope, sum = z[r];
             if (sizeof(E) == 1) sum = sum * x_scale * A.w_scale[c + r];
             if (bias) sum += float(bias[c + r]);
-            act_both<decltype(act)::value>(sum, value, slope);
+            act_of<T, decltype(act)::value>(sum, value, slope);
             if (more) value += float(more[c + r]);
             row[c + r] = T(value);
         }

@@ -69,6 +69,27 @@ template <int ACT> __device__ inline void act_both(float g, float &f, float &d) 
         d = 1.0f;
     }
 }
+// ... of what is stored in 16 bits: the normal distribution at -x <= 0 is exp(-x^2 / 2) t P(t), t = 1 / (1 + 0.36 x), P fitted to
+// it with weights 1 / itself: off by 9e-7 of the value at most, for all x.  (erff, for both signs' ranges, was 60 instructions of a
+// value: 8192 x 2048 x 8192 of 8-bit rows 234 us with it.)
+template <class T, int ACT> __device__ inline void act_of(float g, float &f, float &d) {
+    if constexpr (ACT == NDVM_ACT_GELU && sizeof(T) == 2) {
+        const float t = __builtin_amdgcn_rcpf(1.0f + 0.36f * fabsf(g)), e = __expf(-0.5f * g * g);
+        float q = 0.047056444f;
+        q = q * t - 0.17976522f;
+        q = q * t + 0.18095469f;
+        q = q * t + 0.026548903f;
+        q = q * t + 0.1397194f;
+        q = q * t + 0.14177243f;
+        q = q * t + 0.14371304f;
+        q = q * t * e;
+        const float p = g > 0.0f ? 1.0f - q : q;
+        f = g * p;
+        d = p + g * 0.39894228040143268f * e;
+    } else {
+        act_both<ACT>(g, f, d);
+    }
+}
 // Calls f with the activation as a constant: the branch is taken once, not for every value.
 template <class F> __device__ __attribute__((always_inline)) inline void with_act(int act, F f) {
     using std::integral_constant;
@@ -286,7 +307,7 @@ template <class T, Kind KIND, int ACT> __device__ __attribute__((always_inline))
         for (int r = 0; r < 8; ++r) {
             float value, slope;
             const float sum = A.x_scale ? z[r] * x_scale * w_scale[r] : z[r];
-            act_both<ACT>(A.bias ? sum + float(bias[r]) : sum, value, slope);
+            act_of<T, ACT>(A.bias ? sum + float(bias[r]) : sum, value, slope);
             v[r] = T(A.residual ? value + float(more[r]) : value);
         }
         T *row = static_cast<T *>(A.out) + m * A.ld;
@@ -301,7 +322,7 @@ template <class T, Kind KIND, int ACT> __device__ __attribute__((always_inline))
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
             float value, slope;
-            act_both<ACT>(z[r] + float(bias[r]), value, slope);
+            act_of<T, ACT>(z[r] + float(bias[r]), value, slope);
             // what lies beyond the operands is 0, whatever act does there
             float dz = n + r < A.n ? float(dy[r]) * slope : 0.0f;
             if constexpr (RANGED) {
