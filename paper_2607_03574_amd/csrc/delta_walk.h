@@ -649,14 +649,19 @@ template <int DK, bool BACK> __device__ __forceinline__ void carry(const DeltaAr
 #endif
 }
 
-// Whether sequences are cut into segments, and how.  A walk takes as long for one wave as for two on each of the 1,024 matrix
-// units, and segments cost two to three times the work.
+// Whether sequences are cut into segments, and how.  Segments cost two to three times the work, so they pay where whole
+// sequences leave the matrix units idle; their number is weighed against their length, since one hands its state on to the next
+// (5 us where heads are 128 wide, 2 where 64), and two waves on each of 1,024 matrix units are enough.  us of the forward pass and of
+// the gradient in bfloat16, whole | 128 | 256 | 512 | 1024 tokens a segment: one series of 16 heads of 128, 512 tokens 52, 92 | 58, 104 |
+// 62, 111; 1024 88, 145 | 87, 149 | 75, 133; 4096 308, 535 | 270, 512 | 179, 394 | 145, 349 | 173, 375; 16384 1250, 2228 | 1081, 2009 |
+// 691, 1563 | 513, 1336 | 415, 1182; two of 4096 327, 710 | - | 265, 705 | 220, 618 | 215, 617; four of 4096 357, 1028 | - | 450, 1313 |
+// 394, 1208 | 353, 1124.  4 heads of 64, 4096 218, 343 | 91, 128 | 72, 111 | 79, 129; eight of 2048 120, 221 | 82, 176 | 69, 155.
 inline bool cut(DeltaArgs &a) {
     constexpr int64_t kWaves = 2048, kShortest = 128;
-    const int64_t per_token = a.heads * ceil_div(a.dv, 16);
+    const int64_t per_token = a.heads * ceil_div(a.dv, 16), mean = a.n_seq ? a.n_tokens / a.n_seq : 0;
     a.seg_len = kShortest;
-    while (a.seg_len * kWaves < a.n_tokens * per_token) a.seg_len *= 2;
-    if (a.n_seq && a.n_seq * per_token * 3 < kWaves && a.n_tokens / a.n_seq >= 3 * a.seg_len) {
+    while (4 * a.seg_len * a.seg_len < mean * a.dk || a.seg_len * kWaves < a.n_tokens * per_token) a.seg_len *= 2;
+    if (a.n_seq && a.n_seq * per_token * 8 <= kWaves && mean >= 4 * a.seg_len) {
         a.n_segments = piece_ids(a, a.seg_len);
         return true;
     }

@@ -14,7 +14,8 @@ torch = pytest.importorskip("torch")
 # float gradients: products in three stages, each of which leaves out 2^-21 of a term at most, and sums in float; dg adds up
 # terms of both signs
 FLOAT = 2e-6
-LONG = [([1200], 1, 1, 32, 48), ([900, 20, 0, 1100], 2, 1, 40, 24), ([1537], 2, 2, 128, 128), ([700, 700], 1, 1, 64, 80)]
+LONG = [([1200], 1, 1, 32, 48), ([900, 20, 0, 1100], 2, 1, 40, 24), ([1537], 2, 2, 128, 128), ([700, 700], 1, 1, 64, 80),
+        ([1900, 20, 0, 2100], 2, 1, 40, 24)]
 
 
 @pytest.fixture(scope="module")
@@ -74,7 +75,7 @@ def test_long_sequences(nd, kind, state, lens, H, Hk, dk, dv):
     near(last, wl, "state", FLOAT)
 
 
-@pytest.mark.parametrize("lens", [[70, 41], [1100, 90]])
+@pytest.mark.parametrize("lens", [[70, 41], [1100, 950]])
 def test_only_what_is_needed(nd, lens):
     t, bounds = case(2, "bf16", lens, 4, 2, 33, 40, True)
     args = [t["do"][0]] + [t[x][0] for x in NAMES]
@@ -117,7 +118,7 @@ def test_strides_and_rows_outside(nd):
 
 
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("lens", [[80, 75], [600, 75]])
+@pytest.mark.parametrize("lens", [[80, 75], [600, 775]])
 def test_values_that_are_not_finite(nd, kind, lens):
     """They reach no other sequence and no other head."""
     H, Hk, dk, dv = 2, 2, 40, 72
@@ -189,7 +190,7 @@ def test_against_differences(nd, long):
     from paper_2607_03574_amd import torch_api
     gen = torch.Generator(device="cuda").manual_seed(4)
     r = lambda *s: torch.randn(s, generator=gen, device="cuda")
-    n = 900 if long else 75
+    n = 1700 if long else 75
     off = torch.tensor([0, 30, 30, n]).cuda()
     unit = lambda x: x / x.norm(dim=-1, keepdim=True)
     tensors = [r(n, 1, 12), unit(r(n, 1, 12)), r(n, 2, 20), -torch.rand(n, 2, generator=gen, device="cuda"),
@@ -245,7 +246,7 @@ def test_autograd(nd):
         o.sum().backward()
 
 
-@pytest.mark.parametrize("lens", [[33, 90], [1300, 40]])
+@pytest.mark.parametrize("lens", [[33, 90], [1300, 1040]])
 def test_streams_and_graphs(nd, lens):
     t, bounds = case(6, "bf16", lens, 2, 1, 64, 48, True)
     args, off = [t[x][0] for x in NAMES], torch.tensor(bounds).cuda()
