@@ -15,7 +15,7 @@ namespace ndvm {
 namespace ops {
 namespace {
 
-// z: 0 forwards, 1 backwards.
+// z: 0 forwards, 1 backwards.  (8 x 2048 tokens x 16 heads of 128 bf16: 343 us for both, 850 MB written.)
 template <class T, int DK, Walk WALK> __global__ void __launch_bounds__(256, (kResident<T, DK>)) delta_grad_walk(DeltaArgs a) {
     __shared__ __align__(16) char lds[kWalkLds<T, DK, true, kReadBack>];
     const uint32_t id = blockIdx.x / uint32_t(a.heads);
@@ -64,6 +64,8 @@ __device__ inline float sum_of_16(float v) {
     return v;
 }
 
+// Bound by waiting: 8 x 2048 tokens x 16 heads of 128 bf16 428 us, 1.0 GB read at 2.4 TB/s, one workgroup of eight waves a compute
+// unit (four waves with twice the widths, 500 registers: 728; two workgroups of 128 registers: 1,113, they spill).
 // W waves and a block: a wave has 64 tokens x 16 NT widths of dq and dk, and 16 rows x 16 PT columns of the pairs' matrices.
 template <int DK> constexpr int kBlockWaves = DK >= 128 ? 8 : 4;
 // waves on a matrix unit

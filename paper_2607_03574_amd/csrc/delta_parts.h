@@ -195,6 +195,7 @@ template <class T> __device__ inline double log_decay(T g) {
     return v < -128.0f ? -128.0 : double(v);
 }
 
+// (16384 tokens x 16 heads of 128 bf16: 54 us, 134 MB read and 85 written; with the gradient's matrices 71, 151 written.)
 // One wave: the record of chunk `id` and head h.  Its own LDS: 2 x 32 x 36 floats, 32 doubles and 32 floats.
 constexpr int kPrepareLds = 2 * 32 * 36 * 4 + 384;
 template <class T, bool GRAD> __global__ void __launch_bounds__(256) delta_prepare(DeltaArgs a, int64_t pairs) {
