@@ -298,8 +298,15 @@ template <class T, Kind KIND, int ACT> __device__ __attribute__((always_inline))
         float x_scale = 1.0f, w_scale[8];
         if (A.x_scale) {
             x_scale = A.x_scale[m];
+            typedef float eight_f __attribute__((ext_vector_type(8), aligned(4)));
+            if (all) {
+                const eight_f all_of_them = *reinterpret_cast<const eight_f *>(A.w_scale + n);
 #pragma unroll
-            for (int r = 0; r < 8; ++r) w_scale[r] = A.w_scale[min(n + r, A.n - 1)];
+                for (int r = 0; r < 8; ++r) w_scale[r] = all_of_them[r];
+            } else {
+#pragma unroll
+                for (int r = 0; r < 8; ++r) w_scale[r] = A.w_scale[min(n + r, A.n - 1)];
+            }
         }
         eight more = T(0.0f), v;
         if (A.residual) more = read(static_cast<const T *>(A.residual) + m * A.ld_r);
