@@ -297,3 +297,34 @@ def test_refusals(nd):
     assert e.value.status == nd.E_UNSUPPORTED
     with pytest.raises(nd.NdvmError):
         nd.delta_attention_step(q, k, v, g, b, torch.zeros(8, 4, 8, 8, device="cuda"))      # 9 streams, 8 slots
+
+
+def test_places_beyond_32_bits(nd):
+    """Rows 16 MB apart, in 5 GB, and states in slots of 4.4 GB: the same bits as side by side."""
+    n, d = 300, 16
+    t, bounds = case(21, "bf16", [n], 1, 1, d, d)
+    off, big = torch.tensor(bounds).cuda(), torch.empty(n, 1 << 23, dtype=torch.bfloat16, device="cuda")
+
+    def far(x, at):
+        view = big[:, at:at + x[0].numel()].view(x.shape)
+        view.copy_(x)
+        return view
+
+    near_by = [t[x][0] for x in ("do", *NAMES)]
+    apart = [far(x, 16 * i) for i, x in enumerate(near_by)]
+    assert apart[0].stride(0) == 1 << 23
+    out = big[:, 200:200 + d].view(n, 1, d)
+    o, last = nd.delta_attention(*apart[1:], offsets=off, out=out, final_state=True)
+    want = nd.delta_attention(*near_by[1:], offsets=off, final_state=True)
+    assert torch.equal(o, want[0]) and torch.equal(last, want[1])
+    got, want = (nd.delta_attention_grad(*x, offsets=off) for x in (apart, near_by))
+    assert all(torch.equal(a, b) for a, b in zip(got[:5], want[:5]))
+    del big, apart, out, o
+    t, _ = case(22, "bf16", [1, 1], 16, 16, 128, 128, True)
+    args, s0 = [t[x][0] for x in NAMES], t["s0"][0]
+    state = torch.empty(4200, 16, 128, 128, device="cuda")
+    slots = torch.tensor([0, 4199], device="cuda")
+    state[slots] = s0
+    small = s0.clone()
+    assert torch.equal(nd.delta_attention_step(*args, state, slots=slots), nd.delta_attention_step(*args, small))
+    assert torch.equal(state[slots], small)
