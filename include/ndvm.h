@@ -690,7 +690,8 @@ ndvm_status ndvm_linear(int dtype, int act, const void *x, int64_t rows, int64_t
  * bias is read only then).  dx [rows, n_in], dw [n_out, n_in], db [n_out]: any may be
  * NULL (not wanted); with rows = 0 dw and db are 0.  dz = dy act'(z) is an operand of
  * further products and is rounded to the tensors' type for them, in half as the
- * operands of ndvm_gated_ffn_grad are.  Sums are in float, in a fixed order.
+ * operands of ndvm_gated_ffn_grad are; db adds it up as it was before that.  Sums
+ * are in float, in a fixed order.
  */
 ndvm_status ndvm_linear_grad(int dtype, int act, const void *dy, int64_t ld_dy, const void *x, int64_t rows,
                              int64_t n_in, int64_t ld_x, const void *w, int64_t ld_w, int64_t n_out, const void *bias,

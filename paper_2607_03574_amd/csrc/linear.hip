@@ -322,35 +322,34 @@ __global__ void __launch_bounds__(256) pack8(Pack8Args a) {
     }
 }
 
-// ---- db: sums of dz over the rows, in parts of `groups` workgroups.  A thread eight columns of every eighth row of its
-// workgroup's; a second launch adds the parts up in order.
+// ---- db: sums of dz over the rows, in float before dz is rounded for the products.  With an activation the product that forms
+// dz leaves the sums of every 64 rows; without one dz is dy as it came, whose sums are taken in parts of `groups` workgroups, a
+// thread eight columns of every eighth row of its workgroup's.  A launch adds the parts up in order.
 struct ColumnArgs {
-    const void *p;              // [rows][ld] of E, `planes` apart by `plane`
-    int64_t rows, n, ld, plane;
-    int planes;
-    float *part;                // [groups][n]
-    ProductArgs scaled;         // of dz (largest)
+    const void *dy;             // [rows][ld]
+    int64_t rows, n, ld;
+    float *part;                // [groups][pad]
+    int64_t pad;
     void *to;
 };
 constexpr int64_t kColumnGroups = 64;
-template <class E, class T> __global__ void __launch_bounds__(256) column_sums(ColumnArgs a) {
-    typedef E eight __attribute__((ext_vector_type(8), aligned(sizeof(E))));
+template <class T> __global__ void __launch_bounds__(256) column_sums(ColumnArgs a) {
+    typedef T eight __attribute__((ext_vector_type(8), aligned(sizeof(T))));
     __shared__ float lds[8][256];
     const int x = threadIdx.x % 32, s = threadIdx.x / 32;
     const int64_t c = int64_t(blockIdx.x) * 256 + x * 8;
     const int have = int(min(max(a.n - c, int64_t(0)), int64_t(8)));
     float sum[8] = {};
-    for (int64_t row = int64_t(blockIdx.y) * 8 + s; row < a.rows; row += int64_t(gridDim.y) * 8)
-        for (int q = a.planes - 1; q >= 0; --q) {
-            const E *p = static_cast<const E *>(a.p) + q * a.plane + row * a.ld + c;
-            eight v = E(0.0f);
-            if (have == 8) v = *reinterpret_cast<const eight *>(p);
-            else
-                for (int r = 0; r < 8; ++r)
-                    if (r < have) v[r] = p[r];
+    for (int64_t row = int64_t(blockIdx.y) * 8 + s; row < a.rows; row += int64_t(gridDim.y) * 8) {
+        const T *p = static_cast<const T *>(a.dy) + row * a.ld + c;
+        eight v = T(0.0f);
+        if (have == 8) v = *reinterpret_cast<const eight *>(p);
+        else
+            for (int r = 0; r < 8; ++r)
+                if (r < have) v[r] = p[r];
 #pragma unroll
-            for (int r = 0; r < 8; ++r) sum[r] += float(v[r]);
-        }
+        for (int r = 0; r < 8; ++r) sum[r] += float(v[r]);
+    }
 #pragma unroll
     for (int r = 0; r < 8; ++r) lds[s][x * 8 + r] = sum[r];
     __syncthreads();
@@ -359,7 +358,7 @@ template <class E, class T> __global__ void __launch_bounds__(256) column_sums(C
     float v = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) v += lds[i][threadIdx.x];
-    a.part[int64_t(blockIdx.y) * a.n + col] = v;
+    a.part[int64_t(blockIdx.y) * a.pad + col] = v;
 }
 template <class T> __global__ void __launch_bounds__(256) column_fold(ColumnArgs a, int groups) {
     __shared__ float lds[8][32];
@@ -368,14 +367,16 @@ template <class T> __global__ void __launch_bounds__(256) column_fold(ColumnArgs
     float v = 0;
     if (c < a.n)
 #pragma unroll 8
-        for (int g = s; g < groups; g += 8) v += a.part[int64_t(g) * a.n + c];
+        for (int g = s; g < groups; g += 8) v += a.part[int64_t(g) * a.pad + c];
     lds[s][threadIdx.x % 32] = v;
     __syncthreads();
     if (s || c >= a.n) return;
 #pragma unroll
     for (int i = 1; i < 8; ++i) v += lds[i][threadIdx.x];
-    static_cast<T *>(a.to)[c] = T(v * unscaled<T>(a.scaled));
+    static_cast<T *>(a.to)[c] = T(v);
 }
+// what db takes of the workspace: sums of every 64 rows, or of as many groups as there are
+int64_t column_floats(int64_t rows, int64_t n_out) { return std::max(kColumnGroups, ceil_div(rows, 64)) * pad64(n_out); }
 
 constexpr int64_t kFewRows = 64;
 
@@ -396,7 +397,7 @@ size_t linear_bytes(int dtype, int act, int64_t rows, int64_t n_in, int64_t n_ou
         const Pieces c = linear_pieces(dtype, rows, n_in, n_out);
         if (c.dx > 1) s.take_floats(c.dx * rows * n_in);
         if (c.dw > 1) s.take_floats(c.dw * pad64(n_out) * n_in);
-        s.take_floats(kColumnGroups * n_out);
+        s.take_floats(column_floats(rows, n_out));
     }
     return s.used + 256;
 }
@@ -516,18 +517,17 @@ template <class T> void linear_8bit(const LinearArgs &a, hipStream_t stream) {
     if (g.bb == 256) launch_tiles8<T, 256, 256, 2, 4>(p, stream);
     else if (g.ba == 256) launch_tiles8<T, 256, 128, 4, 2>(p, stream);
     else launch_tiles8<T, 128, 128, 2, 2>(p, stream);
-    if (g.splits > 1) fold_linear<T, kLinear><<<dim3(uint32_t(ceil_div(p.out.pad_n / 8 * p.out.m, 256))), 256, 0, stream>>>(p.out);
+    if (g.splits > 1) fold_linear<T><<<dim3(uint32_t(ceil_div(p.out.pad_n / 8 * p.out.m, 256))), 256, 0, stream>>>(p.out);
 }
 
 template <class T> void linear_grad(const LinearArgs &a, hipStream_t stream) {
-    typedef typename Parts<T>::type P;
     Space s(aligned(a.ws));
     const int64_t pad_n = pad64(a.n_out);
     const Operands o = operands<T>(a, s, stream);
     Operand dz{a.dy, a.rows, a.ld_dy, 0};
     unsigned *largest = nullptr;
     ColumnArgs c{};
-    c.planes = 1;
+    if (a.db) c.part = s.take_floats(column_floats(a.rows, a.n_out));
     if (a.act != NDVM_ACT_NONE) {
         const Gated g = linear_cut(a.dtype, a.rows, a.n_in, a.n_out);
         ProductArgs p = formed(a, o, g, s);
@@ -536,10 +536,10 @@ template <class T> void linear_grad(const LinearArgs &a, hipStream_t stream) {
         p.p = s.take(a.dtype, a.rows, pad_n);
         p.ld_p = pad_n;
         p.plane_p = s.plane;
+        p.sums = c.part;
         if (std::is_same<T, f16>::value) p.largest = largest = reinterpret_cast<unsigned *>(s.take_floats(1));
         if (a.rows) launch_product<T, kLinearGrad>(g, p, pad_n, a.rows, stream);
         dz = Operand{p.p, a.rows, pad_n, p.plane_p};
-        c.planes = Parts<T>::count;
         // without rows nothing notes the largest: there is nothing to scale
         if (a.rows == 0) largest = nullptr;
     } else if ((a.dx || a.dw) && !(direct(a.dtype, a.dy, a.ld_dy, a.n_out) && a.n_out == pad_n)) {
@@ -584,20 +584,17 @@ template <class T> void linear_grad(const LinearArgs &a, hipStream_t stream) {
     if (cut.tile == 256) launch_pair<T, 256, 2, 4>(dx, dw, stream);
     else launch_pair<T, 128, 2, 2>(dx, dw, stream);
     if (!a.db) return;
-    // dy itself where it is dz
-    const bool own = a.act == NDVM_ACT_NONE;
-    c.p = own ? a.dy : dz.p;
-    c.ld = own ? a.ld_dy : dz.ld;
-    c.plane = dz.plane;
+    c.dy = a.dy;
+    c.ld = a.ld_dy;
     c.rows = a.rows;
     c.n = a.n_out;
-    c.part = s.take_floats(kColumnGroups * a.n_out);
-    c.scaled.largest = largest;
+    c.pad = pad_n;
     c.to = a.db;
-    const int64_t groups = std::min(ceil_div(a.rows, 64), kColumnGroups);
-    const dim3 grid(uint32_t(ceil_div(a.n_out, 256)), uint32_t(groups));
-    if (groups && own) column_sums<T, T><<<grid, 256, 0, stream>>>(c);
-    else if (groups) column_sums<P, T><<<grid, 256, 0, stream>>>(c);
+    int64_t groups = ceil_div(a.rows, 64);
+    if (a.act == NDVM_ACT_NONE) {
+        groups = std::min(groups, kColumnGroups);
+        if (groups) column_sums<T><<<dim3(uint32_t(ceil_div(a.n_out, 256)), uint32_t(groups)), 256, 0, stream>>>(c);
+    }
     column_fold<T><<<dim3(uint32_t(ceil_div(a.n_out, 32))), 256, 0, stream>>>(c, int(groups));
 }
 

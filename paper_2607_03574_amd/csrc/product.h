@@ -168,6 +168,7 @@ struct ProductArgs {
     int64_t pad_n;              // n_out padded to a multiple of 64
     unsigned *largest;          // gradient in half: see scale_of
     int again;
+    float *sums;                // [every 64 rows][pad_n]: their sums of dz in float, as it is before it is rounded; or null
 };
 enum Kind { kGated, kGatedGrad, kPlain, kLinear, kLinearGrad };
 constexpr bool of_two(Kind k) { return k == kGated || k == kGatedGrad; }
@@ -275,8 +276,8 @@ template <class T, Kind KIND, int ACT> __device__ __attribute__((always_inline))
     }
 }
 
-// ... of a row of x w^T: y, or dz = dy act'(z).
-template <class T, Kind KIND, int ACT> __device__ __attribute__((always_inline)) inline void linear_out(const ProductArgs &A, int64_t m, int64_t n, const float (&z)[8], float scale, float &top) {
+// ... of a row of x w^T: y, or dz = dy act'(z).  column: sums of dz over the rows so far.
+template <class T, Kind KIND, int ACT> __device__ __attribute__((always_inline)) inline void linear_out(const ProductArgs &A, int64_t m, int64_t n, const float (&z)[8], float scale, float &top, float (&column)[8]) {
     constexpr bool RANGED = std::is_same<T, f16>::value && KIND == kLinearGrad;
     typedef typename Parts<T>::type P;
     constexpr int PARTS = Parts<T>::count;
@@ -332,6 +333,7 @@ template <class T, Kind KIND, int ACT> __device__ __attribute__((always_inline))
             act_of<T, ACT>(z[r] + float(bias[r]), value, slope);
             // what lies beyond the operands is 0, whatever act does there
             float dz = n + r < A.n ? float(dy[r]) * slope : 0.0f;
+            column[r] += dz;
             if constexpr (RANGED) {
                 const float a = fabsf(dz);
                 top = fmaxf(top, a <= 3.402823466e38f ? a : 0.0f);
@@ -354,13 +356,14 @@ template <class T, Kind KIND, int ROWS, int COLS> struct Leaving {
     const ProductArgs &A;
     const int part;
     const float *stage;
-    float scale;
+    float scale, column[8] = {};
     __device__ inline Leaving(const ProductArgs &a, int p, const float *s) : A(a), part(p), stage(s) {
         scale = std::is_same<T, f16>::value && KIND == kLinearGrad && a.again && a.splits == 1 ? scale_of(a) : 1.0f;
     }
     // m0, n0: where they lie in C
-    __device__ __attribute__((always_inline)) inline void rows(int64_t m0, int64_t n0, float &top) const {
+    __device__ __attribute__((always_inline)) inline void rows(int64_t m0, int64_t n0, float &top) {
         constexpr int PER = COLS / 8;
+        static_assert(64 % PER == 0, "a lane has the same columns in every row");
         asm volatile("" ::: "memory");      // other lanes' values: a wave's accesses to LDS are in order
 #pragma unroll 1
         for (int at = threadIdx.x % 64; at < ROWS * PER; at += 64) {
@@ -375,9 +378,23 @@ template <class T, Kind KIND, int ROWS, int COLS> struct Leaving {
                 continue;
             }
             const float z[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
-            with_act_or_none(A.act, [&](auto act) __attribute__((always_inline)) { linear_out<T, KIND, decltype(act)::value>(A, m, n, z, scale, top); });
+            with_act_or_none(A.act, [&](auto act) __attribute__((always_inline)) { linear_out<T, KIND, decltype(act)::value>(A, m, n, z, scale, top, column); });
         }
         asm volatile("" ::: "memory");
+    }
+    // The wave's 64 rows m0 on, added up.
+    __device__ inline void sums(int64_t m0, int64_t n0) {
+        constexpr int PER = COLS / 8;
+#pragma unroll
+        for (int s = PER; s < 64; s <<= 1)
+#pragma unroll
+            for (int r = 0; r < 8; ++r) column[r] += __shfl_xor(column[r], s);
+        const int l = threadIdx.x % 64;
+        const int64_t n = n0 + l % PER * 8;
+        if (l >= PER || m0 >= A.m || n >= A.pad_n) return;
+        f32x4 *to = reinterpret_cast<f32x4 *>(A.sums + m0 / 64 * A.pad_n + n);
+        to[0] = f32x4{column[0], column[1], column[2], column[3]};
+        to[1] = f32x4{column[4], column[5], column[6], column[7]};
     }
 };
 __device__ inline void meet() {
@@ -688,6 +705,10 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
                     for (int i = 0; i < TA; ++i) *reinterpret_cast<f32x4 *>(stage + lm * (WA + 4) + i / 2 * 32 + lg * 8 + i % 2 * 4) = acc[i][c];
             leaving.rows(m0 + wb * WB + j * 16, n0 + wa * WA, top);
         }
+        if constexpr (KIND == kLinearGrad) {
+            static_assert(WB == 64, "");
+            if (A.sums && A.splits == 1 && !A.again) leaving.sums(m0 + wb * WB, n0 + wa * WA);
+        }
         if (std::is_same<T, f16>::value && KIND == kLinearGrad && A.splits == 1) note_largest(A, top);
     }
     if constexpr (GATED) {
@@ -815,28 +836,55 @@ template <class T, Kind KIND> __global__ void __launch_bounds__(256) fold_gated(
 }
 
 // ... of a linear one.
-template <class T, Kind KIND> __global__ void __launch_bounds__(256) fold_linear(ProductArgs A) {
-#ifdef __HIP_DEVICE_COMPILE__
-    if (nothing_to_do<T, KIND>(A)) return;
-    constexpr bool RANGED = std::is_same<T, f16>::value && KIND == kLinearGrad;
-    const float scale = RANGED && A.again ? scale_of(A) : 1.0f;
-    float top = 0;
-    const int64_t per = A.pad_n / 8, at = int64_t(blockIdx.x) * 256 + threadIdx.x, m = at / per, n = at % per * 8;
-    if (m < A.m && (KIND != kLinear || n < A.n)) {
-        f32x4 sum[2] = {};
-        for (int i = 0; i < A.splits; ++i) {
-            const f32x4 *p = reinterpret_cast<const f32x4 *>(A.part + (i * A.m + m) * A.pad_n + n);
-            sum[0] += p[0];
-            sum[1] += p[1];
-        }
-        with_act_or_none(A.act, [&](auto act) __attribute__((always_inline)) {
-            float z[8];
+__device__ inline void split_sums(const ProductArgs &A, int64_t m, int64_t n, float (&z)[8]) {
+    f32x4 sum[2] = {};
+    for (int i = 0; i < A.splits; ++i) {
+        const f32x4 *p = reinterpret_cast<const f32x4 *>(A.part + (i * A.m + m) * A.pad_n + n);
+        sum[0] += p[0];
+        sum[1] += p[1];
+    }
 #pragma unroll
-            for (int r = 0; r < 8; ++r) z[r] = sum[r / 4][r % 4];
-            linear_out<T, KIND, decltype(act)::value>(A, m, n, z, scale, top);
-        });
+    for (int r = 0; r < 8; ++r) z[r] = sum[r / 4][r % 4];
+}
+template <class T> __global__ void __launch_bounds__(256) fold_linear(ProductArgs A) {
+#ifdef __HIP_DEVICE_COMPILE__
+    float top = 0, column[8], z[8];
+    const int64_t per = A.pad_n / 8, at = int64_t(blockIdx.x) * 256 + threadIdx.x, m = at / per, n = at % per * 8;
+    if (m >= A.m || n >= A.n) return;
+    split_sums(A, m, n, z);
+    with_act_or_none(A.act, [&](auto act) __attribute__((always_inline)) { linear_out<T, kLinear, decltype(act)::value>(A, m, n, z, 1.0f, top, column); });
+#endif
+}
+// ... and of its gradient's: 64 rows of 64 columns a workgroup, eight lanes a row.
+template <class T> __global__ void __launch_bounds__(256) fold_linear_grad(ProductArgs A) {
+#ifdef __HIP_DEVICE_COMPILE__
+    if (nothing_to_do<T, kLinearGrad>(A)) return;
+    constexpr bool RANGED = std::is_same<T, f16>::value;
+    __shared__ float lds[4][64];
+    const float scale = RANGED && A.again ? scale_of(A) : 1.0f;
+    float top = 0, column[8] = {};
+    const int l = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t per = A.pad_n / 64, m0 = blockIdx.x / per * 64, n0 = blockIdx.x % per * 64, n = n0 + l % 8 * 8;
+#pragma unroll 1
+    for (int i = 0; i < 2; ++i) {
+        const int64_t m = m0 + wave * 16 + i * 8 + l / 8;
+        if (m >= A.m) continue;
+        float z[8];
+        split_sums(A, m, n, z);
+        with_act_or_none(A.act, [&](auto act) __attribute__((always_inline)) { linear_out<T, kLinearGrad, decltype(act)::value>(A, m, n, z, scale, top, column); });
     }
     if (RANGED) note_largest(A, top);
+    if (!A.sums || A.again) return;
+#pragma unroll
+    for (int s = 8; s < 64; s <<= 1)
+#pragma unroll
+        for (int r = 0; r < 8; ++r) column[r] += __shfl_xor(column[r], s);
+    if (l < 8)
+#pragma unroll
+        for (int r = 0; r < 8; ++r) lds[wave][l * 8 + r] = column[r];
+    __syncthreads();
+    if (wave) return;
+    A.sums[m0 / 64 * A.pad_n + n0 + l] = lds[0][l] + lds[1][l] + lds[2][l] + lds[3][l];
 #endif
 }
 
@@ -859,7 +907,8 @@ template <class T, Kind KIND> void launch_product(const Gated &c, ProductArgs a,
     const auto fold = [&]() {
         const dim3 grid(uint32_t(ceil_div(a.pad_n / 8 * a.m, 256)));
         if constexpr (of_two(KIND)) fold_gated<T, KIND><<<grid, 256, 0, stream>>>(a);
-        else fold_linear<T, KIND><<<grid, 256, 0, stream>>>(a);
+        else if constexpr (KIND == kLinear) fold_linear<T><<<grid, 256, 0, stream>>>(a);
+        else fold_linear_grad<T><<<dim3(uint32_t(a.pad_n / 64 * ceil_div(a.m, 64))), 256, 0, stream>>>(a);
     };
     sums();
     if (c.splits > 1) fold();
