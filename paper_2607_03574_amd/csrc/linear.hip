@@ -323,7 +323,8 @@ __global__ void __launch_bounds__(256) pack8(Pack8Args a) {
 }
 
 // ---- db: sums of dz over the rows, in float before dz is rounded for the products.  With an activation the product that forms
-// dz leaves the sums of every 64 rows; without one dz is dy as it came, whose sums are taken in parts of `groups` workgroups, a
+// dz leaves the sums of every 64 rows (4096 x 1024 x 4096 bf16, silu: db is 1.66e-3 off in norm, its own rounding; as a sum of dz
+// as it is rounded 2.32e-3); without one dz is dy as it came, whose sums are taken in parts of `groups` workgroups, a
 // thread eight columns of every eighth row of its workgroup's.  A launch adds the parts up in order.
 struct ColumnArgs {
     const void *dy;             // [rows][ld]
