@@ -450,6 +450,8 @@ ndvm_status ndvm_layer_norm_grad(int dtype, const void *dy, int64_t ld_dy, const
  * Rows at multiples of their ld; weight [n] may be NULL (1).  h: where the sum goes
  * (not read or written without a residual); rstd: float [rows], what the gradient
  * takes, may be NULL.  Results are the same bits whatever the number of rows.
+ * With a residual y and h may each lie where x or the residual does, at its address
+ * and ld (not both at the same): a stream of residuals is updated in place.
  */
 ndvm_status ndvm_rms_norm(int dtype, const void *x, int64_t rows, int64_t n, int64_t ld_x, const void *residual,
                           int64_t ld_residual, const void *weight, double eps, void *y, int64_t ld_y, void *h,
@@ -475,7 +477,8 @@ ndvm_status ndvm_rms_norm_grad(int dtype, const void *dy, int64_t ld_dy, const v
  * scale for each row, value = byte * scale, with
  *   scale = max(largest |value| of the row, 448 * 2^-126) / 448.
  * A row with a NaN has the scale NaN.  (Read by ndvm_linear_8bit.)
- * ndvm_rms_norm_8bit: y of ndvm_rms_norm, rounded once, to 8 bits;
+ * ndvm_rms_norm_8bit: y of ndvm_rms_norm, rounded once, to 8 bits (h may lie
+ *   where x or the residual does);
  * ndvm_quantize_rows: the rows of x.  ld_y is in bytes.
  */
 ndvm_status ndvm_rms_norm_8bit(int dtype, const void *x, int64_t rows, int64_t n, int64_t ld_x, const void *residual,

@@ -571,6 +571,17 @@ def _to_write(t, x, name):
     t.increment_version(x)
 
 
+def _apart(out, *inputs):
+    """Raises where `out` plainly lies over one of the (name, tensor) pairs, which the call reads after it has written there."""
+    at = out.data_ptr()
+    for name, x in inputs:
+        p = x.data_ptr()
+        if p == at or (out.is_contiguous() and x.is_contiguous() and p < at + out.numel() * out.element_size()
+                       and at < p + x.numel() * x.element_size()):
+            if out.numel() and x.numel():
+                raise ValueError(f"out shares memory with {name}")
+
+
 def _row_stride(x, name):
     """Stride of the rows (last axis) of a tensor whose other axes flatten into one."""
     shape = x.shape
@@ -699,8 +710,8 @@ def _rms_args(t, x, weight, residual):
 
 def rms_norm(x, weight=None, residual=None, eps: float = 1e-5, out=None, stream=None):
     """(y, h, rstd) of the rows (last axis) of x (ndvm_rms_norm): h = x + residual
-    (x itself without one), y its norm; rstd, float32 of x's leading shape, is what
-    rms_norm_grad takes.  (With autograd: torch_api.rms_norm.)"""
+    (x itself without one, which `out` may then not lie over), y its norm; rstd, float32
+    of x's leading shape, is what rms_norm_grad takes.  (With autograd: torch_api.rms_norm.)"""
     t = _t()
     dt, rows, n, ld, w, r, ld_r = _rms_args(t, x, weight, residual)
     with _On(t, stream, x.device) as s:
@@ -710,6 +721,8 @@ def rms_norm(x, weight=None, residual=None, eps: float = 1e-5, out=None, stream=
             _alike(x, ("out", out))
             if out.shape != x.shape:
                 raise ValueError("out must have the shape of x")
+            if r is None:
+                _apart(out, ("x", x))
             ld_out = _row_stride(out, "out")
             _to_write(t, out, "out")
         h = x if r is None else _like(t, x)

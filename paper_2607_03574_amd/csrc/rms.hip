@@ -129,7 +129,8 @@ template <class T, int L, int NV, Out OUT, bool PASSING> __global__ void __launc
     }
 }
 
-// A row of any length: 256 threads, two or three reads of it.
+// A row of any length: 256 threads, two or three reads of it.  (The later ones are of h as it was stored, by the thread that stored
+// it: x or the residual may be what h took the place of.)
 template <class T, Out OUT> __global__ void __launch_bounds__(256) rms_long(RmsArgs a) {
     constexpr int V = kVec<T>;
     __shared__ float lds[8];
@@ -137,20 +138,20 @@ template <class T, Out OUT> __global__ void __launch_bounds__(256) rms_long(RmsA
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T *x = static_cast<const T *>(a.x) + row * a.ld_x;
         const T *r = a.residual ? static_cast<const T *>(a.residual) + row * a.ld_r : nullptr;
-        const auto value = [&](int64_t c) { return joined(x + c, r ? r + c : nullptr, a.n - c); };
+        T *const held = r ? static_cast<T *>(a.h) + row * a.ld_h : nullptr;
         float rstd = 1.0f;
         if constexpr (OUT != kRows8) {
             float sq = 0;
             for (int64_t c = threadIdx.x * V; c < a.n; c += 256 * V) {
-                const vec<T> h = value(c);
+                const vec<T> h = joined(x + c, r ? r + c : nullptr, a.n - c);
 #pragma unroll
                 for (int j = 0; j < V; ++j) sq += float(h[j]) * float(h[j]);
-                if (r) store_vec(static_cast<T *>(a.h) + row * a.ld_h + c, h, a.n - c);
+                if (r) store_vec(held + c, h, a.n - c);
             }
             rstd = 1.0f / sqrtf(row_sum<256>(sq, threadIdx.x, lds) / float(a.n) + a.eps);
         }
         const auto result = [&](int64_t c, float (&y)[V]) {
-            const vec<T> h = value(c);
+            const vec<T> h = load_vec((r ? held : x) + c, a.n - c);
             vec<T> wv = T(1.0f);
             if (OUT != kRows8 && w) wv = load_vec(w + c, a.n - c);
 #pragma unroll
