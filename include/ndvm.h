@@ -677,6 +677,7 @@ ndvm_status ndvm_gated_ffn_grad(int dtype, int act, const void *dh, int64_t ld_d
  *   y = act(x w^T + bias) + residual
  * x [rows, n_in], w [n_out, n_in], residual and y [rows, n_out], rows at multiples of
  * their ld; bias [n_out]; bias and residual may be NULL (0).  act: NDVM_ACT_*.
+ * y may lie where the residual does, at its address and ld.
  * Limits: n_in, n_out <= 2^21, rows <= 2^22.
  */
 /* Workspace bytes of ndvm_linear (with_grad = 0) or its gradient.  Host only. */

@@ -978,8 +978,8 @@ def delta_attention(q, k, v, g, beta, offsets=None, scale=None, initial_state=No
     beta [.., heads]; with `offsets` (int64 [sequences + 1], on the device, from 0 to the
     number of tokens) the sequences lie one after the other in [tokens, heads, ..]; tokens
     outside them get no output.  heads: a multiple of qk_heads; scale: dk**-0.5 unless
-    given; states are float32 [sequences, heads, dk, dv].  (With autograd:
-    torch_api.delta_attention.)"""
+    given; states are float32 [sequences, heads, dk, dv]; `out` may not lie over an input.
+    (With autograd: torch_api.delta_attention.)"""
     t = _t()
     shape, lead, off, *heads = _delta_args(t, q, k, v, g, beta, offsets, scale)
     dims, dev = (shape.n_seq, shape.heads, shape.dk, shape.dv), q.device
@@ -989,6 +989,7 @@ def delta_attention(q, k, v, g, beta, offsets=None, scale=None, initial_state=No
             out = q.new_empty((*lead, shape.heads, shape.dv))
         else:
             _alike(q, ("out", out))
+            _apart(out, ("q", q), ("k", k), ("v", v), ("g", g), ("beta", beta))
             _to_write(t, out, "out")
         last = q.new_empty(dims, dtype=t.f32) if final_state else None
         ws, ws_ptr, need = _delta_workspace(t, q, shape, off is not None, 0)
@@ -1057,6 +1058,7 @@ def delta_attention_step(q, k, v, g, beta, state, slots=None, scale=None, out=No
             out = q.new_empty((n, H, dv))
         else:
             _alike(q, ("out", out))
+            _apart(out, ("q", q), ("k", k), ("v", v), ("g", g), ("beta", beta))
             _to_write(t, out, "out")
         _to_write(t, state, "state")
         _check(_delta_step(shape, *heads, st, state.shape[0], sl, one(out, "out", H, dv), s), "ndvm_delta_attention_step")
@@ -1136,7 +1138,7 @@ def _linear_sizes(x, weight, activation):
     return act, x.numel() // n_in if n_in else 0, n_in, n_out
 
 
-def _linear_out(t, x, dtype, n_out, residual, out):
+def _linear_out(t, x, weight, dtype, n_out, residual, out):
     """Output of a projection, and the residual's address and stride; under the call's stream."""
     shape = (*x.shape[:-1], n_out)
     r, ld_r = None, 0
@@ -1152,6 +1154,7 @@ def _linear_out(t, x, dtype, n_out, residual, out):
         raise TypeError("out must be a tensor of the output's type and device")
     if out.shape != shape:
         raise ValueError("out must be [.., n_out]")
+    _apart(out, ("x", x), ("weight", weight))
     ld = _row_stride(out, "out")
     _to_write(t, out, "out")
     return out, ld, r, ld_r
@@ -1160,7 +1163,7 @@ def _linear_out(t, x, dtype, n_out, residual, out):
 def linear(x, weight, bias=None, activation: Optional[str] = None, residual=None, out=None, stream=None):
     """act(x weight^T + bias) + residual (ndvm_linear) for x [.., n_in], weight [n_out, n_in],
     bias [n_out] and residual [.., n_out]; activation: None, silu, gelu, sigmoid or relu.
-    (With autograd: torch_api.linear.)"""
+    `out` may be the residual, not lie over x or weight.  (With autograd: torch_api.linear.)"""
     t = _t()
     dt = _op_type(t, x, "x")
     _alike(x, ("weight", weight))
@@ -1168,7 +1171,7 @@ def linear(x, weight, bias=None, activation: Optional[str] = None, residual=None
     ld_x, ld_w = _row_stride(x, "x"), _row_stride(weight, "weight")
     b = _of(bias, "bias", x.dtype, (n_out,), x.device)
     with _On(t, stream, x.device) as s:
-        out, ld_out, r, ld_r = _linear_out(t, x, x.dtype, n_out, residual, out)
+        out, ld_out, r, ld_r = _linear_out(t, x, weight, x.dtype, n_out, residual, out)
         need = _sz()
         _check(_linear_ws(dt, act, rows, n_in, n_out, 0, ctypes.byref(need)), "ndvm_linear_workspace_bytes")
         ws = x.new_empty(need.value, dtype=t.u8) if need.value else None
@@ -1221,7 +1224,7 @@ def linear_8bit(x, x_scale, weight, weight_scale, bias=None, activation: Optiona
     xs, ws_ = _of(x_scale, "x_scale", t.f32, x.shape[:-1], x.device), _of(weight_scale, "weight_scale", t.f32, (n_out,), x.device)
     b = _of(bias, "bias", dtype, (n_out,), x.device)
     with _On(t, stream, x.device) as s:
-        out, ld_out, r, ld_r = _linear_out(t, x, dtype, n_out, residual, out)
+        out, ld_out, r, ld_r = _linear_out(t, x, weight, dtype, n_out, residual, out)
         need = _sz()
         _check(_linear8_ws(rows, n_in, n_out, ctypes.byref(need)), "ndvm_linear_8bit_workspace_bytes")
         ws = x.new_empty(need.value, dtype=t.u8) if need.value else None
