@@ -66,12 +66,13 @@ def calibrate(tape: Tape, params, obs, steps: int, lr: float, beta1: float = 0.9
 
 # ---------------------------------------------------------------- encoder operators
 def _rows(x):
-    """x, or a copy of it where its rows are not contiguous or do not lie at one stride."""
+    """x, or a copy of it where its rows are not contiguous, do not lie at one stride, or lie over one another (one row
+    expanded to many)."""
     try:
-        _row_stride(x, "x")
+        apart = _row_stride(x, "x") >= x.shape[-1]
     except ValueError:
-        return x.contiguous()
-    return x
+        apart = False
+    return x if apart else x.contiguous()
 
 
 class LayerNorm(torch.autograd.Function):
