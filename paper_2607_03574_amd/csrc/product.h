@@ -278,8 +278,8 @@ template <class T, Kind KIND, int ACT> __device__ __attribute__((always_inline))
     }
 }
 
-// ... of a row of x w^T: y, or dz = dy act'(z).  column: sums of dz over the rows so far.
-template <class T, Kind KIND, int ACT> __device__ __attribute__((always_inline)) inline void linear_out(const ProductArgs &A, int64_t m, int64_t n, const float (&z)[8], float scale, float &top, float (&column)[8]) {
+// ... of a row of x w^T: y, or dz = dy act'(z), which is left in z too, in float.
+template <class T, Kind KIND, int ACT> __device__ __attribute__((always_inline)) inline void linear_out(const ProductArgs &A, int64_t m, int64_t n, float (&z)[8], float scale, float &top) {
     constexpr bool RANGED = std::is_same<T, f16>::value && KIND == kLinearGrad;
     typedef typename Parts<T>::type P;
     constexpr int PARTS = Parts<T>::count;
@@ -335,7 +335,7 @@ template <class T, Kind KIND, int ACT> __device__ __attribute__((always_inline))
             act_of<T, ACT>(z[r] + float(bias[r]), value, slope);
             // what lies beyond the operands is 0, whatever act does there
             float dz = n + r < A.n ? float(dy[r]) * slope : 0.0f;
-            column[r] += dz;
+            z[r] = dz;
             if constexpr (RANGED) {
                 const float a = fabsf(dz);
                 top = fmaxf(top, a <= 3.402823466e38f ? a : 0.0f);
@@ -354,16 +354,22 @@ template <class T, Kind KIND, int ACT> __device__ __attribute__((always_inline))
 #ifdef __HIP_DEVICE_COMPILE__
 // ROWS rows of COLS columns of a linear product, from the wave's own LDS (rows of COLS + 4 floats) to memory: eight
 // columns a lane, so that whole rows are read and written, and one copy of the code for all of a wave's accumulators.
+// Of a gradient, each lane's sums of dz lie behind the stage: in registers they are spilled beside the accumulators.
+template <Kind KIND, int ROWS, int COLS> constexpr int kStage = ROWS * (COLS + 4) + (KIND == kLinearGrad ? 512 : 0);
 template <class T, Kind KIND, int ROWS, int COLS> struct Leaving {
     const ProductArgs &A;
     const int part;
-    const float *stage;
-    float scale, column[8] = {};
-    __device__ inline Leaving(const ProductArgs &a, int p, const float *s) : A(a), part(p), stage(s) {
+    float *stage;
+    float scale;
+    bool summed;
+    __device__ inline f32x4 *own() const { return reinterpret_cast<f32x4 *>(stage + ROWS * (COLS + 4)) + threadIdx.x % 64; }
+    __device__ inline Leaving(const ProductArgs &a, int p, float *s) : A(a), part(p), stage(s) {
         scale = std::is_same<T, f16>::value && KIND == kLinearGrad && a.again && a.splits == 1 ? scale_of(a) : 1.0f;
+        summed = KIND == kLinearGrad && a.sums && a.splits == 1 && !a.again;
+        if (summed) own()[0] = own()[64] = 0;
     }
     // m0, n0: where they lie in C
-    __device__ __attribute__((always_inline)) inline void rows(int64_t m0, int64_t n0, float &top) {
+    __device__ __attribute__((always_inline)) inline void rows(int64_t m0, int64_t n0, float &top) const {
         constexpr int PER = COLS / 8;
         static_assert(64 % PER == 0, "a lane has the same columns in every row");
         asm volatile("" ::: "memory");      // other lanes' values: a wave's accesses to LDS are in order
@@ -379,24 +385,33 @@ template <class T, Kind KIND, int ROWS, int COLS> struct Leaving {
                 to[1] = v;
                 continue;
             }
-            const float z[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
-            with_act_or_none(A.act, [&](auto act) __attribute__((always_inline)) { linear_out<T, KIND, decltype(act)::value>(A, m, n, z, scale, top, column); });
+            float z[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
+            with_act_or_none(A.act, [&](auto act) __attribute__((always_inline)) { linear_out<T, KIND, decltype(act)::value>(A, m, n, z, scale, top); });
+            if (summed) {
+                own()[0] += f32x4{z[0], z[1], z[2], z[3]};
+                own()[64] += f32x4{z[4], z[5], z[6], z[7]};
+            }
         }
         asm volatile("" ::: "memory");
     }
     // The wave's 64 rows m0 on, added up.
-    __device__ inline void sums(int64_t m0, int64_t n0) {
+    __device__ inline void sums(int64_t m0, int64_t n0) const {
         constexpr int PER = COLS / 8;
+        if (!summed) return;
+        f32x4 u = own()[0], v = own()[64];
 #pragma unroll
         for (int s = PER; s < 64; s <<= 1)
 #pragma unroll
-            for (int r = 0; r < 8; ++r) column[r] += __shfl_xor(column[r], s);
+            for (int r = 0; r < 4; ++r) {
+                u[r] += __shfl_xor(u[r], s);
+                v[r] += __shfl_xor(v[r], s);
+            }
         const int l = threadIdx.x % 64;
         const int64_t n = n0 + l % PER * 8;
         if (l >= PER || m0 >= A.m || n >= A.pad_n) return;
         f32x4 *to = reinterpret_cast<f32x4 *>(A.sums + m0 / 64 * A.pad_n + n);
-        to[0] = f32x4{column[0], column[1], column[2], column[3]};
-        to[1] = f32x4{column[4], column[5], column[6], column[7]};
+        to[0] = u;
+        to[1] = v;
     }
 };
 __device__ inline void meet() {
@@ -693,8 +708,9 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
         }
     }
     if constexpr (KIND == kLinear || KIND == kLinearGrad) {
-        static_assert(16 * (WA + 4) * 4 * W / 4 <= (BA + BB) * kStep * 2, "");
-        float *stage = reinterpret_cast<float *>(wave % 4 == 0 ? buffer0 : wave % 4 == 1 ? buffer1 : wave % 4 == 2 ? buffer2 : buffer3) + wave / 4 * (16 * (WA + 4));
+        constexpr int STAGE = kStage<KIND, 16, WA>;
+        static_assert(STAGE * 4 * W / 4 <= (BA + BB) * kStep * 2, "");
+        float *stage = reinterpret_cast<float *>(wave % 4 == 0 ? buffer0 : wave % 4 == 1 ? buffer1 : wave % 4 == 2 ? buffer2 : buffer3) + wave / 4 * STAGE;
         meet();     // the buffers are everybody's until here
         float top = 0;
         Leaving<T, KIND, 16, WA> leaving(A, part, stage);
@@ -709,7 +725,7 @@ __device__ __attribute__((always_inline)) inline void product_tile(const Product
         }
         if constexpr (KIND == kLinearGrad) {
             static_assert(WB == 64, "");
-            if (A.sums && A.splits == 1 && !A.again) leaving.sums(m0 + wb * WB, n0 + wa * WA);
+            leaving.sums(m0 + wb * WB, n0 + wa * WA);
         }
         if (std::is_same<T, f16>::value && KIND == kLinearGrad && A.splits == 1) note_largest(A, top);
     }
@@ -850,43 +866,42 @@ __device__ inline void split_sums(const ProductArgs &A, int64_t m, int64_t n, fl
 }
 template <class T> __global__ void __launch_bounds__(256) fold_linear(ProductArgs A) {
 #ifdef __HIP_DEVICE_COMPILE__
-    float top = 0, column[8], z[8];
+    float top = 0, z[8];
     const int64_t per = A.pad_n / 8, at = int64_t(blockIdx.x) * 256 + threadIdx.x, m = at / per, n = at % per * 8;
     if (m >= A.m || n >= A.n) return;
     split_sums(A, m, n, z);
-    with_act_or_none(A.act, [&](auto act) __attribute__((always_inline)) { linear_out<T, kLinear, decltype(act)::value>(A, m, n, z, 1.0f, top, column); });
+    with_act_or_none(A.act, [&](auto act) __attribute__((always_inline)) { linear_out<T, kLinear, decltype(act)::value>(A, m, n, z, 1.0f, top); });
 #endif
 }
 // ... and of its gradient's: 64 rows of 64 columns a workgroup, eight lanes a row.
-template <class T> __global__ void __launch_bounds__(256) fold_linear_grad(ProductArgs A) {
+template <class T> __global__ void __launch_bounds__(512) fold_linear_grad(ProductArgs A) {
 #ifdef __HIP_DEVICE_COMPILE__
     if (nothing_to_do<T, kLinearGrad>(A)) return;
     constexpr bool RANGED = std::is_same<T, f16>::value;
-    __shared__ float lds[4][64];
+    __shared__ float lds[8][64];
     const float scale = RANGED && A.again ? scale_of(A) : 1.0f;
-    float top = 0, column[8] = {};
+    float top = 0, z[8] = {};
     const int l = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t per = A.pad_n / 64, m0 = blockIdx.x / per * 64, n0 = blockIdx.x % per * 64, n = n0 + l % 8 * 8;
-#pragma unroll 1
-    for (int i = 0; i < 2; ++i) {
-        const int64_t m = m0 + wave * 16 + i * 8 + l / 8;
-        if (m >= A.m) continue;
-        float z[8];
+    const int64_t per = A.pad_n / 64, m0 = blockIdx.x / per * 64, n0 = blockIdx.x % per * 64, n = n0 + l % 8 * 8, m = m0 + wave * 8 + l / 8;
+    if (m < A.m) {
         split_sums(A, m, n, z);
-        with_act_or_none(A.act, [&](auto act) __attribute__((always_inline)) { linear_out<T, kLinearGrad, decltype(act)::value>(A, m, n, z, scale, top, column); });
+        with_act_or_none(A.act, [&](auto act) __attribute__((always_inline)) { linear_out<T, kLinearGrad, decltype(act)::value>(A, m, n, z, scale, top); });
     }
     if (RANGED) note_largest(A, top);
     if (!A.sums || A.again) return;
 #pragma unroll
     for (int s = 8; s < 64; s <<= 1)
 #pragma unroll
-        for (int r = 0; r < 8; ++r) column[r] += __shfl_xor(column[r], s);
+        for (int r = 0; r < 8; ++r) z[r] += __shfl_xor(z[r], s);
     if (l < 8)
 #pragma unroll
-        for (int r = 0; r < 8; ++r) lds[wave][l * 8 + r] = column[r];
+        for (int r = 0; r < 8; ++r) lds[wave][l * 8 + r] = z[r];
     __syncthreads();
     if (wave) return;
-    A.sums[m0 / 64 * A.pad_n + n0 + l] = lds[0][l] + lds[1][l] + lds[2][l] + lds[3][l];
+    float sum = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) sum += lds[w][l];
+    A.sums[m0 / 64 * A.pad_n + n0 + l] = sum;
 #endif
 }
 
@@ -910,7 +925,7 @@ template <class T, Kind KIND> void launch_product(const Gated &c, ProductArgs a,
         const dim3 grid(uint32_t(ceil_div(a.pad_n / 8 * a.m, 256)));
         if constexpr (of_two(KIND)) fold_gated<T, KIND><<<grid, 256, 0, stream>>>(a);
         else if constexpr (KIND == kLinear) fold_linear<T><<<grid, 256, 0, stream>>>(a);
-        else fold_linear_grad<T><<<dim3(uint32_t(a.pad_n / 64 * ceil_div(a.m, 64))), 256, 0, stream>>>(a);
+        else fold_linear_grad<T><<<dim3(uint32_t(a.pad_n / 64 * ceil_div(a.m, 64))), 512, 0, stream>>>(a);
     };
     sums();
     if (c.splits > 1) fold();
