@@ -3,7 +3,7 @@
 // product leaves is the next one's operand as it stands (K S -> X -> M -> U -> S).  The four waves of a workgroup share the
 // rows of k and q and the chunk's record, which lie in LDS, one chunk ahead: one barrier a chunk.
 // Bound by the issue of vector and matrix instructions, two waves on a matrix unit: 630 and 82 of a chunk, half of the former for
-// the state's parts (16384 tokens x 16 heads of 128 bf16, 16 segments: outputs 117 us, sums and transitions 161; with the
+// the state's parts (16384 tokens x 16 heads of 128 bf16, 16 segments: outputs 115 us, sums and transitions 157; with the
 // widths divided among the waves, whose sums met in LDS, the whole call was 1,976, now 417).
 #pragma once
 #include "delta_parts.h"
@@ -655,10 +655,16 @@ template <int DK, bool BACK> __device__ __forceinline__ void carry(const DeltaAr
 // Whether sequences are cut into segments, and how.  Segments cost two to three times the work, so they pay where whole
 // sequences leave the matrix units idle; their number is weighed against their length, since one hands its state on to the next
 // (5 us where heads are 128 wide, 2 where 64), and two waves on each of 1,024 matrix units are enough.  us of the forward pass and of
-// the gradient in bfloat16, whole | 128 | 256 | 512 | 1024 tokens a segment: one series of 16 heads of 128, 512 tokens 52, 92 | 58, 104 |
-// 62, 111; 1024 88, 145 | 87, 149 | 75, 133; 4096 308, 535 | 270, 512 | 179, 394 | 145, 349 | 173, 375; 16384 1250, 2228 | 1081, 2009 |
-// 691, 1563 | 513, 1336 | 415, 1182; two of 4096 327, 710 | - | 265, 705 | 220, 618 | 215, 617; four of 4096 357, 1028 | - | 450, 1313 |
-// 394, 1208 | 353, 1124.  4 heads of 64, 4096 218, 343 | 91, 128 | 72, 111 | 79, 129; eight of 2048 120, 221 | 82, 176 | 69, 155.
+// the gradient in bfloat16, whole | 128 | 256 | 512 | 1024 tokens a segment; what the rule takes is in brackets.  16 heads of 128, one
+// series of 512 tokens 51, 93 | [58, 104] | 61, 111; 1024 87, 145 | 87, 147 | [75, 131]; 4096 311, 537 | 270, 511 | 178, 396 | [145, 353]
+// | 175, 375; 16384 1251, 2235 | 1075, 2015 | 688, 1569 | 512, 1338 | [420, 1184]; two of 1024 88, 171 | 105, 217 | [84, 183]; two of
+// 4096 332, 716 | 369, 851 | 264, 714 | [220, 628] | 216, 624; four of 4096 [365, 1030] | 583, 1517 | 457, 1325 | 394, 1217 | 351, 1121.
+// 4 heads of 64, 4096 220, 343 | 91, 127 | [71, 112] | 80, 129; eight of 2048 119, 221 | 82, 173 | [68, 153]; sixteen of 1024 69, 145 |
+// [67, 159] | 60, 146.  4 heads of 192, 1024 129, 257 | 310, 437 | [202, 306] | 184, 301; 4096 468, 795 | 1311, 1487 | 706, 882 |
+// [426, 595] | 373, 545; 16384 1819, 3170 | - | 2709, 3799 | 1499, 2134 | [922, 1586], at 2048 729, 1419.
+// It is off the best of these by up to 18% where sequences are barely long enough, and by up to 54% for heads of more than 128
+// widths, whose transitions cost most (in half and float, by up to 26%).  Only the mean length counts: among many short or
+// empty packed sequences a long one stays whole, 2.4 us for 32 of its tokens.
 inline bool cut(DeltaArgs &a) {
     constexpr int64_t kWaves = 2048, kShortest = 128;
     const int64_t per_token = a.heads * ceil_div(a.dv, 16), mean = a.n_seq ? a.n_tokens / a.n_seq : 0;
