@@ -72,8 +72,8 @@ template <int ACT> __device__ inline void act_both(float g, float &f, float &d) 
 }
 // ... of what is stored in 16 bits: the normal distribution at -x <= 0 is exp(-x^2 / 2) t P(t), t = 1 / (1 + 0.36 x), P fitted to
 // it with weights 1 / itself: off by 9.2e-7 of the value at most up to x = 13, where it leaves float's range; the exponent is rounded
-// twice, which is up to (x^2 + 14) 2^-24 more (emulated, 1.8e-6 of the value in all up to 5, 7.2e-6 up to 13).  (erff, for both signs' ranges, was 60
-// instructions of a value: 8192 x 2048 x 8192 of 8-bit rows 234 us with it.)
+// twice, which is up to (x^2 + 14) 2^-24 more (emulated, 1.8e-6 of the value in all up to 5, 7.2e-6 up to 13).  (erff, for both
+// signs' ranges, was 60 instructions of a value: 8192 x 2048 x 8192 of 8-bit rows 234 us with it, 200 without.)
 template <class T, int ACT> __device__ inline void act_of(float g, float &f, float &d) {
     if constexpr (ACT == NDVM_ACT_GELU && sizeof(T) == 2) {
         const float t = __builtin_amdgcn_rcpf(1.0f + 0.36f * fabsf(g)), e = __expf(-0.5f * g * g);
